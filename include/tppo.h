@@ -60,10 +60,13 @@ typedef enum {
     TPPO_OP_SELECT_TOKENS = 1,
     TPPO_OP_POLICY_LOSS = 2,
     TPPO_OP_VALUE_LOSS = 3,
-    TPPO_OP_LMHEAD = 4
+    TPPO_OP_LMHEAD = 4,
+    TPPO_OP_LAYER_NORM = 5, /* N = rows, V = columns                                         */
+    TPPO_OP_LINEAR = 6,     /* N = rows M, B = K, V = N of the product; see tppo_linear_fwd  */
+    TPPO_OP_MUON = 7        /* N = rows, V = columns of the matrix                           */
 } tppo_op;
 
-/* logits element types */
+/* element types */
 enum { TPPO_BF16 = 0, TPPO_F32 = 1 };
 
 /* where the gradient with respect to the logits goes */
@@ -418,6 +421,110 @@ int tppo_advance_batch(const int32_t *seq_begin, const int32_t *prompt_len,
                        int32_t *next_seq_begin, int32_t *next_tokens, int64_t capacity,
                        int32_t *free_slots, int32_t *slot_source, int32_t *counts,
                        void *stream);
+
+/*
+ * ---- Dense operators around the LM-head -----------------------------------------------------------
+ * The final layer norm that produces `hidden` and takes `dhidden`, the projections and the value
+ * head, and the update their weight gradients are turned into.  They follow the conventions above
+ * with two differences:
+ *   - matrices may be strided: element (r, c) is at r * ld + c, ld >= number of columns.  16-byte
+ *     aligned rows (base and ld) take the fast paths; any other base (aligned to its element) and ld
+ *     is handled.
+ *   - `status` ([1] int32, may be NULL) is ADDED TO: bits are set, never cleared, so one word that the
+ *     caller zeroes can collect the calls of a whole step.
+ * Reductions are done in a fixed order: results are run-to-run identical.
+ */
+
+/*
+ * Layer norm of M rows of N elements, statistics in fp32:
+ *     mean = sum_c x / N,  rstd = 1 / sqrt(sum_c (x - mean)^2 / N + eps),
+ *     y = (x - mean) * rstd * gamma + beta
+ *   x [M, N] of `dtype` (TPPO_BF16 or TPPO_F32), y [M, N] of the same type; y may be x itself with
+ *   the same row stride
+ *   gamma, beta  [N] of `param_dtype` (either type), each may be NULL (1 and 0)
+ *   mean, rstd   [M] fp32 out, each may be NULL: what tppo_layer_norm_bwd takes
+ *   eps >= 0
+ * A row that holds a NaN or an infinity, or whose variance leaves the range of fp32 (with eps = 0 that
+ * includes a variance of 0), has no statistics: its y, mean and rstd are written 0 and
+ * TPPO_DEV_NONFINITE is raised.
+ */
+int tppo_layer_norm_fwd(const void *x, int32_t dtype, int64_t M, int32_t N, int64_t ldx,
+                        const void *gamma, const void *beta, int32_t param_dtype, float eps,
+                        void *y, int64_t ldy, float *mean, float *rstd, int32_t *status,
+                        void *stream);
+
+/*
+ * Its backward pass.  With h = (x - mean) * rstd and a = dy * gamma:
+ *     dx = rstd * (a - sum_c a / N - h * sum_c (a h) / N),
+ *     dgamma[c] = sum_r dy * h,   dbeta[c] = sum_r dy
+ *   dy, x [M, N] of `dtype`; mean, rstd [M] fp32 from the forward call
+ *   dx [M, N] of `dtype` or NULL; may be dy itself with the same row stride (not x)
+ *   dgamma, dbeta [N] of `param_dtype`, each may be NULL; overwritten, not accumulated
+ *   workspace  tppo_workspace_bytes(TPPO_OP_LAYER_NORM, M, 0, 0, N) bytes; may be NULL when both
+ *              dgamma and dbeta are
+ * A row without statistics (rstd = 0) contributes nothing and gets dx = 0; so does a row whose dy or x
+ * is not finite, which raises TPPO_DEV_NONFINITE.  M = 0 writes dgamma = dbeta = 0.
+ */
+int tppo_layer_norm_bwd(const void *dy, const void *x, int32_t dtype, int64_t M, int32_t N,
+                        int64_t lddy, int64_t ldx, const void *gamma, int32_t param_dtype,
+                        const float *mean, const float *rstd, void *dx, int64_t lddx,
+                        void *dgamma, void *dbeta, int32_t *status,
+                        void *workspace, size_t workspace_bytes, void *stream);
+
+/* activations of the linear operator */
+enum {
+    TPPO_ACT_NONE = 0,
+    TPPO_ACT_RELU = 1,
+    TPPO_ACT_GELU = 2,      /* z * Phi(z)                                                       */
+    TPPO_ACT_GELU_TANH = 3, /* z / 2 * (1 + tanh(sqrt(2/pi) * (z + 0.044715 z^3)))              */
+    TPPO_ACT_SILU = 4       /* z / (1 + exp(-z))                                                */
+};
+
+/*
+ * Matrix product with bias, activation and residual in its epilogue:
+ *     z = x * weight + bias,   y = act(z) + residual
+ *   x [M, K] bf16, weight [K, N] bf16 (the layout of the LM-head weight); any K, N >= 1
+ *   bias      [N] of `bias_dtype` or NULL
+ *   residual  [M, N] bf16 or NULL; may be y itself when y is bf16 with the same row stride
+ *   y         [M, N] of `y_dtype` (fp32 e.g. for a value head, whose N is 1)
+ *   preact    [M, N] bf16 out or NULL: z, which tppo_linear_bwd needs unless the activation is
+ *             TPPO_ACT_NONE
+ *   workspace tppo_workspace_bytes(TPPO_OP_LINEAR, M, K, n_max, N) bytes.  The forward call uses it
+ *             only to copy an operand whose rows are not 16-byte aligned, and may be given NULL when x
+ *             and weight are aligned.  The query counts those copies when K or N is not a multiple of
+ *             8, or when n_max is 1: pass that for misaligned views (base or ld) of matrices whose
+ *             sizes are multiples of 8.
+ * Products are bf16, sums and the epilogue fp32, y is rounded once.  An element whose z or y is not
+ * finite or leaves the range of the type it is stored in is written 0 and raises TPPO_DEV_NONFINITE.
+ * No output may overlap x or weight.
+ * The first call on a device looks up the driver's tensor-map encoder (TPPO_ERR_CUDA if absent).
+ */
+int tppo_linear_fwd(const void *x, int64_t ldx, const void *weight, int64_t ldw,
+                    int64_t M, int32_t K, int32_t N, const void *bias, int32_t bias_dtype,
+                    int32_t activation, const void *residual, int64_t ldr,
+                    void *y, int32_t y_dtype, int64_t ldy, void *preact, int64_t ldp,
+                    int32_t *status, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Its backward pass.  With dz = dy * act'(z):
+ *     dx = dz * weight^T,   dweight = x^T * dz,   dbias[n] = sum_m dz        (dresidual = dy)
+ *   dy [M, N] of `dy_dtype`; preact [M, N] bf16 from the forward call (not read, and may be NULL, for
+ *   TPPO_ACT_NONE); act' of TPPO_ACT_RELU at 0 is 0
+ *   dx [M, K] bf16, dweight [K, N] bf16, dbias [N] of `bias_dtype`: each may be NULL; overwritten, not
+ *   accumulated.  No output may overlap an input.
+ *   x may be NULL without dweight, weight without dx
+ *   workspace as for tppo_linear_fwd: for dz, the partial sums of dbias and operand copies; may be
+ *   NULL when none is needed (TPPO_ACT_NONE, aligned bf16 operands, no dbias)
+ * dz is rounded to bf16 before the two products (dbias sums the unrounded values); an element of dz or
+ * of an output that is not finite or leaves the range of bf16 counts or is written as 0 and raises
+ * TPPO_DEV_NONFINITE.  M = 0 writes dweight = dbias = 0.
+ */
+int tppo_linear_bwd(const void *dy, int32_t dy_dtype, int64_t lddy, const void *x, int64_t ldx,
+                    const void *weight, int64_t ldw, int64_t M, int32_t K, int32_t N,
+                    int32_t activation, const void *preact, int64_t ldp,
+                    void *dx, int64_t lddx, void *dweight, int64_t lddw,
+                    void *dbias, int32_t bias_dtype, int32_t *status,
+                    void *workspace, size_t workspace_bytes, void *stream);
 
 #ifdef __cplusplus
 }

@@ -22,8 +22,10 @@ if not os.path.exists(LIB_PATH):
 _lib = C.CDLL(LIB_PATH)
 
 OP_EGAE, OP_SELECT_TOKENS, OP_POLICY_LOSS, OP_VALUE_LOSS, OP_LMHEAD = range(5)
+OP_LAYER_NORM, OP_LINEAR, OP_MUON = 5, 6, 7
 BF16, F32 = 0, 1
 DLOGITS_NONE, DLOGITS_FULL, DLOGITS_COMPACT = 0, 1, 2
+ACT_NONE, ACT_RELU, ACT_GELU, ACT_GELU_TANH, ACT_SILU = range(5)
 POLICY_AUTO, POLICY_TWO_PASS, POLICY_CLUSTER_SMEM = 0, 1, 2
 DEV_BAD_TARGET, DEV_WAIT_TIMEOUT, DEV_BAD_INDEX, DEV_BAD_SEGMENT, DEV_OVERFLOW, DEV_NONFINITE = 1, 2, 4, 8, 16, 32
 
@@ -70,6 +72,18 @@ _lib.tppo_lmhead_shard_fwd_bwd.argtypes = [_vp, _vp, _i64, _i32, _i32, _i32, _i3
 _lib.tppo_advance_batch.restype = C.c_int
 _lib.tppo_advance_batch.argtypes = [_vp, _vp, _vp, _vp, _vp, _vp, _i64, _vp, _vp, _i64, _i32, _i32,
                                     _vp, _vp, _vp, _vp, _i64, _vp, _vp, _vp, _vp]
+_lib.tppo_layer_norm_fwd.restype = C.c_int
+_lib.tppo_layer_norm_fwd.argtypes = [_vp, _i32, _i64, _i32, _i64, _vp, _vp, _i32, _f32, _vp, _i64, _vp,
+                                     _vp, _vp, _vp]
+_lib.tppo_layer_norm_bwd.restype = C.c_int
+_lib.tppo_layer_norm_bwd.argtypes = [_vp, _vp, _i32, _i64, _i32, _i64, _i64, _vp, _i32, _vp, _vp, _vp,
+                                     _i64, _vp, _vp, _vp, _vp, _sz, _vp]
+_lib.tppo_linear_fwd.restype = C.c_int
+_lib.tppo_linear_fwd.argtypes = [_vp, _i64, _vp, _i64, _i64, _i32, _i32, _vp, _i32, _i32, _vp, _i64, _vp,
+                                 _i32, _i64, _vp, _i64, _vp, _vp, _sz, _vp]
+_lib.tppo_linear_bwd.restype = C.c_int
+_lib.tppo_linear_bwd.argtypes = [_vp, _i32, _i64, _vp, _i64, _vp, _i64, _i64, _i32, _i32, _i32, _vp, _i64,
+                                 _vp, _i64, _vp, _i64, _vp, _i32, _vp, _vp, _sz, _vp]
 
 
 class TppoError(RuntimeError):
@@ -268,3 +282,80 @@ def tppo_advance_batch(seq_begin, prompt_len, prev_len, new_len, truncated, toke
         _ptr(next_prev_len, torch.int32), _ptr(next_seq_begin, torch.int32),
         _ptr(next_tokens, torch.int32), next_tokens.numel(), _ptr(free_slots, torch.int32),
         _ptr(slot_source, torch.int32), _ptr(counts, torch.int32), _stream()))
+
+
+_DTYPES = {torch.bfloat16: BF16, torch.float32: F32}
+
+
+def _on_device(*tensors):
+    """The dense operators take tensors of one device, which has to be the current one: the call goes
+    to its current stream."""
+    here = torch.cuda.current_device()
+    for t in tensors:
+        assert t is None or (t.is_cuda and t.device.index == here), f"tensors must be on cuda:{here}, the current device"
+
+
+def _matrix(t, shape=None, dtype=None):
+    """(pointer, row stride) of a matrix whose columns are contiguous; (None, 0) for None."""
+    if t is None:
+        return None, 0
+    assert t.dim() == 2 and (t.stride(1) == 1 or t.shape[1] == 1), "columns must be contiguous"
+    assert shape is None or tuple(t.shape) == tuple(shape), f"expected shape {tuple(shape)}, got {tuple(t.shape)}"
+    assert dtype is None or t.dtype == dtype, f"expected {dtype}, got {t.dtype}"
+    ld = t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
+    assert ld >= t.shape[1], "rows must not overlap"
+    return t.data_ptr(), ld
+
+
+def _vector(t, n, dtype=None):
+    assert t is None or (t.dim() == 1 and t.numel() == n), f"expected {n} elements"
+    return _ptr(t, dtype)
+
+
+def _type_of(*tensors):
+    """The common element type of the tensors given; BF16 when all are None."""
+    kinds = {t.dtype for t in tensors if t is not None}
+    assert len(kinds) <= 1, "these tensors must have the same type"
+    return _DTYPES[kinds.pop()] if kinds else BF16
+
+
+def tppo_layer_norm_fwd(x, gamma, beta, eps, y, mean, rstd, status):
+    M, N = x.shape
+    _on_device(x, gamma, beta, y, mean, rstd, status)
+    (px, ldx), (py, ldy) = _matrix(x), _matrix(y, x.shape, x.dtype)
+    _check(_lib.tppo_layer_norm_fwd(px, _DTYPES[x.dtype], M, N, ldx, _vector(gamma, N), _vector(beta, N),
+                                    _type_of(gamma, beta), eps, py, ldy, _vector(mean, M, torch.float32),
+                                    _vector(rstd, M, torch.float32), _ptr(status, torch.int32), _stream()))
+
+
+def tppo_layer_norm_bwd(dy, x, gamma, mean, rstd, dx, dgamma, dbeta, status, ws):
+    M, N = x.shape
+    _on_device(dy, x, gamma, mean, rstd, dx, dgamma, dbeta, status, ws)
+    (pd, lddy), (px, ldx), (po, lddx) = _matrix(dy, x.shape, x.dtype), _matrix(x), _matrix(dx, x.shape, x.dtype)
+    _check(_lib.tppo_layer_norm_bwd(pd, px, _DTYPES[x.dtype], M, N, lddy, ldx, _vector(gamma, N),
+                                    _type_of(gamma, dgamma, dbeta), _vector(mean, M, torch.float32),
+                                    _vector(rstd, M, torch.float32), po, lddx, _vector(dgamma, N),
+                                    _vector(dbeta, N), _ptr(status, torch.int32), _ptr(ws),
+                                    0 if ws is None else ws.numel(), _stream()))
+
+
+def tppo_linear_fwd(x, weight, bias, activation, residual, y, preact, status, ws):
+    (M, K), N = x.shape, weight.shape[1]
+    _on_device(x, weight, bias, residual, y, preact, status, ws)
+    bf = torch.bfloat16
+    (px, ldx), (pw, ldw) = _matrix(x, dtype=bf), _matrix(weight, (K, N), bf)
+    (pr, ldr), (py, ldy), (pp, ldp) = _matrix(residual, (M, N), bf), _matrix(y, (M, N)), _matrix(preact, (M, N), bf)
+    _check(_lib.tppo_linear_fwd(px, ldx, pw, ldw, M, K, N, _vector(bias, N), _type_of(bias), activation, pr, ldr,
+                                py, _DTYPES[y.dtype], ldy, pp, ldp, _ptr(status, torch.int32), _ptr(ws),
+                                0 if ws is None else ws.numel(), _stream()))
+
+
+def tppo_linear_bwd(dy, x, weight, activation, preact, dx, dweight, dbias, status, ws):
+    (M, K), N = x.shape, weight.shape[1]
+    _on_device(dy, x, weight, preact, dx, dweight, dbias, status, ws)
+    bf = torch.bfloat16
+    (pd, lddy), (px, ldx), (pw, ldw) = _matrix(dy, (M, N)), _matrix(x, dtype=bf), _matrix(weight, (K, N), bf)
+    (pp, ldp), (po, lddx), (pg, lddw) = _matrix(preact, (M, N), bf), _matrix(dx, (M, K), bf), _matrix(dweight, (K, N), bf)
+    _check(_lib.tppo_linear_bwd(pd, _DTYPES[dy.dtype], lddy, px, ldx, pw, ldw, M, K, N, activation, pp, ldp,
+                                po, lddx, pg, lddw, _vector(dbias, N), _type_of(dbias), _ptr(status, torch.int32),
+                                _ptr(ws), 0 if ws is None else ws.numel(), _stream()))

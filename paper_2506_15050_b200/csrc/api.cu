@@ -7,6 +7,8 @@ size_t select_workspace_bytes(int64_t N);
 size_t policy_workspace_bytes(int64_t R, int64_t n_max);
 size_t value_workspace_bytes();
 size_t lmhead_workspace_bytes(int64_t M, int32_t K, int32_t V);
+size_t norm_workspace_bytes(int64_t M, int32_t N);
+size_t linear_workspace_bytes(int64_t M, int32_t K, int32_t N, bool copies);
 }  // namespace tppo
 
 // Test hooks (see tppo_test_hooks in the header): read by the launchers of the two look-back kernels.
@@ -39,8 +41,8 @@ TPPO_API const char* tppo_status_string(int status) {
     }
 }
 
-// N doubles as the number of logits rows R for TPPO_OP_POLICY_LOSS and as M for TPPO_OP_LMHEAD
-// (B then carries K).
+// N doubles as the number of logits rows R for TPPO_OP_POLICY_LOSS and as M for TPPO_OP_LMHEAD and the
+// dense operators (B then carries K, V the columns).
 TPPO_API size_t tppo_workspace_bytes(int op, int64_t N, int32_t B, int64_t n_max, int32_t V) {
     if (N < 0 || n_max < 0) return 0;
     switch (op) {
@@ -49,6 +51,8 @@ TPPO_API size_t tppo_workspace_bytes(int op, int64_t N, int32_t B, int64_t n_max
         case TPPO_OP_POLICY_LOSS: return tppo::policy_workspace_bytes(N, n_max);
         case TPPO_OP_VALUE_LOSS: return tppo::value_workspace_bytes();
         case TPPO_OP_LMHEAD: return tppo::lmhead_workspace_bytes(N, B, V);
+        case TPPO_OP_LAYER_NORM: return tppo::norm_workspace_bytes(N, V);
+        case TPPO_OP_LINEAR: return tppo::linear_workspace_bytes(N, B, V, n_max != 0);
         default: return 0;
     }
 }

@@ -1,0 +1,103 @@
+// Helpers shared by the dense operators (layer norm, linear, orthogonalised update): typed element
+// access, row geometry checks and the launch of a programmatic dependent.
+#pragma once
+
+#include "common.cuh"
+#include "ptx.cuh"
+
+namespace tppo {
+
+typedef uint16_t bf16_bits;           // storage of one bf16 element
+
+__device__ __forceinline__ float load_f32(const float* p) { return *p; }
+__device__ __forceinline__ float load_f32(const bf16_bits* p) { return __uint_as_float(uint32_t(*p) << 16); }
+__device__ __forceinline__ void store_f32(float* p, float v) { *p = v; }
+__device__ __forceinline__ void store_f32(bf16_bits* p, float v) { *p = bf16_bits(pack_bf16x2(v, 0.f) & 0xffffu); }
+
+// VEC elements at p, which is aligned to min(16, VEC * sizeof(T)) bytes, widened to fp32.
+template <int VEC>
+__device__ __forceinline__ void load_vec(const float* p, float (&v)[VEC]) {
+    if constexpr (VEC % 4 == 0) {
+#pragma unroll
+        for (int i = 0; i < VEC; i += 4) {
+            const float4 w = *reinterpret_cast<const float4*>(p + i);
+            v[i] = w.x; v[i + 1] = w.y; v[i + 2] = w.z; v[i + 3] = w.w;
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) v[i] = p[i];
+    }
+}
+template <int VEC>
+__device__ __forceinline__ void load_vec(const bf16_bits* p, float (&v)[VEC]) {
+    if constexpr (VEC % 8 == 0) {
+#pragma unroll
+        for (int i = 0; i < VEC; i += 8) {
+            const uint4 w = *reinterpret_cast<const uint4*>(p + i);
+            v[i] = bf16_lo(w.x); v[i + 1] = bf16_hi(w.x); v[i + 2] = bf16_lo(w.y); v[i + 3] = bf16_hi(w.y);
+            v[i + 4] = bf16_lo(w.z); v[i + 5] = bf16_hi(w.z); v[i + 6] = bf16_lo(w.w); v[i + 7] = bf16_hi(w.w);
+        }
+    } else if constexpr (VEC == 4) {
+        const uint2 w = *reinterpret_cast<const uint2*>(p);
+        v[0] = bf16_lo(w.x); v[1] = bf16_hi(w.x); v[2] = bf16_lo(w.y); v[3] = bf16_hi(w.y);
+    } else {
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) v[i] = load_f32(p + i);
+    }
+}
+template <int VEC>
+__device__ __forceinline__ void store_vec(float* p, const float (&v)[VEC]) {
+    if constexpr (VEC % 4 == 0) {
+#pragma unroll
+        for (int i = 0; i < VEC; i += 4)
+            *reinterpret_cast<float4*>(p + i) = make_float4(v[i], v[i + 1], v[i + 2], v[i + 3]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) p[i] = v[i];
+    }
+}
+template <int VEC>
+__device__ __forceinline__ void store_vec(bf16_bits* p, const float (&v)[VEC]) {
+    if constexpr (VEC % 8 == 0) {
+#pragma unroll
+        for (int i = 0; i < VEC; i += 8)
+            *reinterpret_cast<uint4*>(p + i) =
+                make_uint4(pack_bf16x2(v[i], v[i + 1]), pack_bf16x2(v[i + 2], v[i + 3]),
+                           pack_bf16x2(v[i + 4], v[i + 5]), pack_bf16x2(v[i + 6], v[i + 7]));
+    } else if constexpr (VEC == 4) {
+        *reinterpret_cast<uint2*>(p) = make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
+    } else {
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) store_f32(p + i, v[i]);
+    }
+}
+
+__device__ __forceinline__ bool is_finite(float v) { return fabsf(v) <= kFltMax; }
+
+inline bool is_finite_host(float v) { return v - v == 0.f; }
+
+// The two halves of a programmatic dependent launch: the primary lets its dependent start, the
+// dependent waits for the primary's memory.
+__device__ __forceinline__ void pdl_launch() { asm volatile("griddepcontrol.launch_dependents;"); }
+__device__ __forceinline__ void pdl_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+
+// Launches `kernel` on `s`; with `dependent` its blocks may start while the previous kernel of the
+// stream still runs, so the kernel must call pdl_wait() before it touches that kernel's results --
+// or any memory that the work in front of it may still use.
+template <class... Args>
+cudaError_t launch_dense(void (*kernel)(Args...), dim3 grid, dim3 block, size_t smem, cudaStream_t s,
+                         bool dependent, Args... args) {
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = grid;
+    cfg.blockDim = block;
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = s;
+    cudaLaunchAttribute attr{};
+    attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr.val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = &attr;
+    cfg.numAttrs = dependent ? 1 : 0;
+    return cudaLaunchKernelEx(&cfg, kernel, args...);
+}
+
+}  // namespace tppo

@@ -1,0 +1,461 @@
+// The two tensor-core products behind the dense operators: D = A * B over 16-bit operands (bf16, or
+// fp16 with F16) with fp32 accumulation in tensor memory, and a caller-supplied epilogue that gets
+// finished fp32 values eight at a time along the contiguous dimension of its outputs.
+//
+//   dense_gemm_kernel   many output tiles: persistent CTAs, 128 x 256 tiles, two accumulators so
+//                       that the epilogue of a tile overlaps the main loop of the next.  Output
+//                       rows are accumulator rows.  With SYM only the tiles that touch the lower
+//                       triangle of a symmetric product are computed; the epilogue is called for the
+//                       mirrored elements too.
+//   dense_split_kernel  few output tiles (one to some hundred tokens, small matrices): the output is
+//                       taken TRANSPOSED -- the 128 accumulator rows run along the contiguous output
+//                       dimension, the BN columns along its rows, so that one token costs a 16-wide
+//                       instruction instead of a 128-high tile -- and the contraction is split over the
+//                       CTAs of a cluster, whose partial sums meet in distributed shared memory: no
+//                       workspace, no second launch, a fixed order of addition.
+//
+// Roles of a CTA's warps: 0 TMA loads, 1 tcgen05.mma, 2-9 epilogue.  Every wait is bounded; one that
+// runs out raises TPPO_DEV_WAIT_TIMEOUT, outputs are then incomplete, and tensor memory is released.
+#pragma once
+
+#include "dense_common.cuh"
+#include "umma.cuh"
+#include "umma_gemm.cuh"      // make_bf16_tensor_map
+
+namespace tppo {
+
+constexpr int kDenseTileM = 128;
+constexpr int kDenseTileK = 64;                       // one 128-byte swizzled row of 16-bit elements
+constexpr int kDenseThreads = 320;
+constexpr int kDenseEpiWarps = 8;
+constexpr uint32_t kDenseABytes = kDenseTileM * kDenseTileK * 2;      // 16 KB
+constexpr uint32_t kDenseBox64 = 64 * kDenseTileK * 2;                // 64 x 64 box of an MN-major operand
+constexpr uint32_t kDenseStageEpi = 32 * 32 * 4;                      // one warp's 32 x 32 fp32 chunk
+
+// Instruction descriptor (see umma::instr_desc_bf16) for either 16-bit format.
+template <bool F16>
+__host__ __device__ constexpr uint32_t dense_instr_desc(int n, int a_mn, int b_mn) {
+    const uint32_t d = umma::instr_desc_bf16(kDenseTileM, n, a_mn, b_mn);
+    return F16 ? d & ~((7u << 7) | (7u << 10)) : d;
+}
+
+// 8 consecutive fp32 columns of this thread's TMEM lane.
+__device__ __forceinline__ void tmem_ld8(uint32_t taddr, uint32_t (&v)[8]) {
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                 : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7])
+                 : "r"(taddr) : "memory");
+}
+__device__ __forceinline__ float4 ld_cluster_f32x4(uint32_t cluster_addr) {
+    float4 v;
+    asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];"
+                 : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(cluster_addr) : "memory");
+    return v;
+}
+
+// The operand ring both kernels share: producer and MMA issuer for one output tile.
+template <int AMAJ, int BMAJ, bool F16, int BN, int STAGES>
+struct DenseRing {
+    static constexpr uint32_t kBBytes = BN * kDenseTileK * 2;
+    static constexpr uint32_t kStage = kDenseABytes + kBBytes;
+    uint32_t base, full, empty;
+    int stage = 0;
+    uint32_t phase = 0;
+
+    __device__ __forceinline__ void next() {
+        if (++stage == STAGES) { stage = 0; phase ^= 1u; }
+    }
+    // Loads k steps [k0, k1) of the tile whose first A and B indices are am and bn.
+    __device__ __forceinline__ bool load(const CUtensorMap* ma, const CUtensorMap* mb, int am, int bn, int k0, int k1) {
+        for (int ks = k0; ks < k1; ++ks) {
+            if (!ptx::mbar_wait<false>(empty + 8 * stage, phase ^ 1u)) return false;
+            const uint32_t fb = full + 8 * stage, sa = base + stage * kStage, sb = sa + kDenseABytes;
+            ptx::mbar_arrive_expect_tx(fb, kStage);
+            const int k = ks * kDenseTileK;
+            if (AMAJ == 0) {
+                umma::tma_load_2d(sa, ma, fb, k, am);
+            } else {
+#pragma unroll
+                for (int q = 0; q < kDenseTileM / 64; ++q) umma::tma_load_2d(sa + q * kDenseBox64, ma, fb, am + 64 * q, k);
+            }
+            if (BMAJ == 0) {
+                umma::tma_load_2d(sb, mb, fb, k, bn);
+            } else {
+#pragma unroll
+                for (int q = 0; q < BN / 64; ++q) umma::tma_load_2d(sb + q * kDenseBox64, mb, fb, bn + 64 * q, k);
+            }
+            next();
+        }
+        return true;
+    }
+    // After a wait ran out: let the copies already issued land before the CTA's memory goes away.
+    __device__ __forceinline__ void drain() {
+        for (int s = 0; s < STAGES; ++s) {
+            const uint32_t issued = s < stage ? phase : phase ^ 1u;       // parity of the stage's last load
+            if (!ptx::mbar_wait<false>(full + 8 * s, issued)) return;
+        }
+    }
+    __device__ __forceinline__ bool multiply(uint32_t d, int steps) {
+        constexpr uint32_t idesc = dense_instr_desc<F16>(BN, AMAJ, BMAJ);
+        constexpr uint32_t a_kstep = AMAJ ? 16 * 128 : 32, b_kstep = BMAJ ? 16 * 128 : 32;
+        for (int ks = 0; ks < steps; ++ks) {
+            if (!ptx::mbar_wait<false>(full + 8 * stage, phase)) return false;
+            umma::fence_after_thread_sync();
+            const uint32_t sa = base + stage * kStage, sb = sa + kDenseABytes;
+            const uint64_t ad = umma::smem_desc(sa, AMAJ ? kDenseBox64 : 16, 1024);
+            const uint64_t bd = umma::smem_desc(sb, BMAJ ? kDenseBox64 : 16, 1024);
+#pragma unroll
+            for (int j = 0; j < kDenseTileK / 16; ++j)
+                umma::mma_bf16(d, umma::smem_desc_advance(ad, j * a_kstep), umma::smem_desc_advance(bd, j * b_kstep), idesc,
+                               (ks | j) != 0 ? 1u : 0u);
+            umma::mma_commit(empty + 8 * stage);
+            next();
+        }
+        return true;
+    }
+};
+
+// ---- many tiles ---------------------------------------------------------------------------------
+constexpr int kDenseBN = 256;
+constexpr int kDenseStages = 4;
+constexpr size_t kDenseSmem = size_t(kDenseStages) * (kDenseABytes + kDenseBN * 128) + kDenseEpiWarps * kDenseStageEpi +
+                              1024 /* alignment */ + 128 /* barriers */;
+
+struct DenseShape {
+    int32_t m_tiles, n_tiles, k_steps, total;
+    int32_t group_m;          // m-tiles per raster group: tiles of a group run next to each other in time
+};
+
+template <bool SYM>
+__device__ __forceinline__ void dense_tile(const DenseShape& g, int t, int& mt, int& nt) {
+    if (SYM) {      // rows 2p and 2p+1 of tiles hold p+1 tiles each, p(p+1) tiles lie in front of them
+        int p = int((sqrtf(4.f * float(t) + 1.f) - 1.f) * 0.5f);
+        while (p * (p + 1) > t) --p;
+        while ((p + 1) * (p + 2) <= t) ++p;
+        const int in = t - p * (p + 1);
+        mt = 2 * p + (in > p);
+        nt = in > p ? in - p - 1 : in;
+    } else {
+        const int per = g.group_m * g.n_tiles, gi = t / per, first = gi * g.group_m;
+        const int gm = min(g.group_m, g.m_tiles - first), in = t - gi * per;
+        mt = first + in % gm;
+        nt = in / gm;
+    }
+}
+
+// Epi: void operator()(int64_t row, int col, float (&v)[8]) const -- v holds columns col .. col+7 of
+// output row `row`; both may lie outside the matrix.
+template <int AMAJ, int BMAJ, bool F16, bool SYM, class Epi>
+__global__ void __launch_bounds__(kDenseThreads, 1)
+dense_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const DenseShape g,
+                  const Epi epi, int32_t* status) {
+    extern __shared__ uint8_t smem_raw[];
+    const uint32_t raw = ptx::smem_addr(smem_raw), base = (raw + 1023u) & ~1023u;
+    typedef DenseRing<AMAJ, BMAJ, F16, kDenseBN, kDenseStages> Ring;
+    const uint32_t stage_epi = base + kDenseStages * Ring::kStage;
+    const uint32_t bars = stage_epi + kDenseEpiWarps * kDenseStageEpi;
+    const uint32_t full = bars, empty = bars + 8 * kDenseStages;
+    const uint32_t acc_full = bars + 16 * kDenseStages, acc_empty = acc_full + 16, slot = acc_empty + 16;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < kDenseStages; ++s) {
+            ptx::mbar_init(full + 8 * s, 1);
+            ptx::mbar_init(empty + 8 * s, 1);
+        }
+        for (int a = 0; a < 2; ++a) {
+            ptx::mbar_init(acc_full + 8 * a, 1);
+            ptx::mbar_init(acc_empty + 8 * a, kDenseEpiWarps);
+        }
+        ptx::fence_mbar_init_cluster();
+        umma::prefetch_tensormap(&map_a);
+        umma::prefetch_tensormap(&map_b);
+    }
+    if (warp == 1) {
+        umma::tmem_alloc(slot, 512);
+        umma::tmem_relinquish();
+    }
+    umma::fence_before_thread_sync();
+    __syncthreads();
+    umma::fence_after_thread_sync();
+    const uint32_t tmem = *reinterpret_cast<uint32_t*>(smem_raw + (slot - raw));
+    // only now, with the tensor memory in hand: a dependent CTA on this SM allocates too
+    pdl_launch();
+    pdl_wait();
+
+    bool timed_out = false;
+    if (warp == 0) {
+        if (lane == 0) {
+            Ring ring{base, full, empty};
+            for (int t = blockIdx.x; t < g.total && !timed_out; t += gridDim.x) {
+                int mt, nt;
+                dense_tile<SYM>(g, t, mt, nt);
+                timed_out = !ring.load(&map_a, &map_b, mt * kDenseTileM, nt * kDenseBN, 0, g.k_steps);
+            }
+            if (timed_out) ring.drain();
+        }
+    } else if (warp == 1) {
+        if (lane == 0) {
+            Ring ring{base, full, empty};
+            int local = 0;
+            for (int t = blockIdx.x; t < g.total; t += gridDim.x, ++local) {
+                const int acc = local & 1;
+                if (!ptx::mbar_wait<false>(acc_empty + 8 * acc, ((local >> 1) & 1) ^ 1u)) { timed_out = true; break; }
+                umma::fence_after_thread_sync();
+                if (!ring.multiply(tmem + acc * kDenseBN, g.k_steps)) { timed_out = true; break; }
+                umma::mma_commit(acc_full + 8 * acc);
+            }
+        }
+    } else {
+        const int q = warp & 3, half = (warp - 2) >> 2;
+        const uint32_t sw = stage_epi + (warp - 2) * kDenseStageEpi;
+        int local = 0;
+        for (int t = blockIdx.x; t < g.total; t += gridDim.x, ++local) {
+            int mt, nt;
+            dense_tile<SYM>(g, t, mt, nt);
+            const int acc = local & 1;
+            if (!ptx::mbar_wait_warp<false>(acc_full + 8 * acc, (local >> 1) & 1)) { timed_out = true; break; }
+            umma::fence_after_thread_sync();
+            const int64_t m0 = int64_t(mt) * kDenseTileM + q * 32;
+#pragma unroll 1
+            for (int c = 0; c < kDenseBN / 2; c += 32) {
+                const int n0 = nt * kDenseBN + half * (kDenseBN / 2) + c;
+                if (SYM && n0 > m0) break;            // above the diagonal: another chunk's mirror image
+                if (epi.outside(m0, n0)) break;
+                uint32_t v[32];
+                umma::tmem_ld32(tmem + acc * kDenseBN + (uint32_t(q * 32) << 16) + half * (kDenseBN / 2) + c, v);
+                umma::tmem_ld_wait();
+                // row-per-lane to eight-columns-per-lane through shared memory; 16-byte pieces of a
+                // row are XORed with its low bits, so that neither side meets a bank conflict
+                __syncwarp();
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    ptx::sts128(sw + lane * 128 + ((j ^ (lane & 7)) << 4), make_uint4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]));
+                __syncwarp();
+#pragma unroll
+                for (int it = 0; it < 4; ++it) {
+                    const int r = it * 8 + (lane >> 2), j = (lane & 3) * 2;
+                    const uint4 lo = ptx::lds128(sw + r * 128 + ((j ^ (r & 7)) << 4));
+                    const uint4 hi = ptx::lds128(sw + r * 128 + (((j + 1) ^ (r & 7)) << 4));
+                    float w[8] = {__uint_as_float(lo.x), __uint_as_float(lo.y), __uint_as_float(lo.z), __uint_as_float(lo.w),
+                                  __uint_as_float(hi.x), __uint_as_float(hi.y), __uint_as_float(hi.z), __uint_as_float(hi.w)};
+                    epi(m0 + r, n0 + j * 4, w);
+                }
+                if (SYM && n0 < m0) {
+#pragma unroll
+                    for (int it = 0; it < 4; ++it) {
+                        const int col = it * 8 + (lane >> 2), r0 = (lane & 3) * 8;
+                        float w[8];
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) {
+                            uint32_t u;
+                            asm volatile("ld.shared.u32 %0, [%1];" : "=r"(u)
+                                         : "r"(sw + (r0 + i) * 128 + (((col >> 2) ^ i) << 4) + (col & 3) * 4));
+                            w[i] = __uint_as_float(u);
+                        }
+                        epi(int64_t(n0) + col, int(m0) + r0, w);
+                    }
+                }
+            }
+            umma::fence_before_thread_sync();
+            __syncwarp();
+            if (lane == 0) ptx::mbar_arrive(acc_empty + 8 * acc);
+        }
+    }
+    if (timed_out && status) atomicOr(status, TPPO_DEV_WAIT_TIMEOUT);
+    umma::fence_before_thread_sync();
+    __syncthreads();
+    if (warp == 1) {
+        __syncwarp();
+        umma::tmem_dealloc(tmem, 512);
+    }
+}
+
+// ---- few tiles ----------------------------------------------------------------------------------
+// Accumulator rows: output columns (contiguous); accumulator columns: output rows.  A is therefore
+// the operand indexed by the output column, B the one indexed by the output row.
+template <int BN> __host__ __device__ constexpr int dense_split_stages() { return BN <= 32 ? 5 : BN <= 64 ? 4 : 3; }
+template <int BN> __host__ __device__ constexpr size_t dense_split_smem() {
+    const size_t ring = size_t(dense_split_stages<BN>()) * (kDenseABytes + BN * 128), sums = size_t(BN) * 128 * 4;
+    return (ring > sums ? ring : sums) + 1024 + 128;
+}
+
+struct DenseSplitShape {
+    int32_t col_tiles;        // tiles along the output rows (BN each)
+    int32_t k_steps;
+};
+
+template <int AMAJ, int BMAJ, bool F16, int BN, class Epi>
+__global__ void __launch_bounds__(kDenseThreads)
+dense_split_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
+                   const DenseSplitShape g, const Epi epi, int32_t* status) {
+    constexpr int STAGES = dense_split_stages<BN>();
+    constexpr uint32_t kCols = BN < 32 ? 32 : BN;
+    extern __shared__ uint8_t smem_raw[];
+    // dynamic shared memory starts at the same address in every CTA of a kernel, so `base` is common to
+    // the cluster and the partial sums of all its CTAs lie at the same offset
+    const uint32_t raw = ptx::smem_addr(smem_raw), base = (raw + 1023u) & ~1023u;
+    typedef DenseRing<AMAJ, BMAJ, F16, BN, STAGES> Ring;
+    constexpr uint32_t kBody = uint32_t(dense_split_smem<BN>() - 1024 - 128);
+    const uint32_t bars = base + kBody;
+    const uint32_t full = bars, empty = bars + 8 * STAGES, acc_full = bars + 16 * STAGES, slot = acc_full + 8;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t rank = ptx::cluster_ctarank();
+    uint32_t splits;
+    asm volatile("mov.u32 %0, %cluster_nctarank;" : "=r"(splits));
+    const int tile = int(blockIdx.x / splits);
+    const int rt = tile / g.col_tiles, ct = tile % g.col_tiles;
+    const int k0 = int(int64_t(g.k_steps) * rank / splits), k1 = int(int64_t(g.k_steps) * (rank + 1) / splits);
+
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < STAGES; ++s) {
+            ptx::mbar_init(full + 8 * s, 1);
+            ptx::mbar_init(empty + 8 * s, 1);
+        }
+        ptx::mbar_init(acc_full, 1);
+        ptx::fence_mbar_init_cluster();
+        umma::prefetch_tensormap(&map_a);
+        umma::prefetch_tensormap(&map_b);
+    }
+    if (warp == 1) {
+        umma::tmem_alloc(slot, kCols);
+        umma::tmem_relinquish();
+    }
+    umma::fence_before_thread_sync();
+    __syncthreads();
+    umma::fence_after_thread_sync();
+    const uint32_t tmem = *reinterpret_cast<uint32_t*>(smem_raw + (slot - raw));
+    pdl_launch();
+    pdl_wait();
+
+    bool timed_out = false;
+    if (warp == 0) {
+        if (lane == 0) {
+            Ring ring{base, full, empty};
+            timed_out = !ring.load(&map_a, &map_b, rt * kDenseTileM, ct * BN, k0, k1);
+            if (timed_out) ring.drain();
+        }
+        __syncwarp();
+    } else if (warp == 1) {
+        if (lane == 0) {
+            Ring ring{base, full, empty};
+            timed_out = !ring.multiply(tmem, k1 - k0);
+            if (!timed_out) umma::mma_commit(acc_full);
+        }
+        __syncwarp();
+    } else {
+        const int q = warp & 3, half = (warp - 2) >> 2;
+        if (ptx::mbar_wait_warp<false>(acc_full, 0)) {
+            umma::fence_after_thread_sync();
+            // every MMA has completed, so the ring's bytes are free for the partial sums [BN][128]
+#pragma unroll 1
+            for (int c = half * (BN / 2); c < (half + 1) * (BN / 2); c += 8) {
+                uint32_t v[8];
+                tmem_ld8(tmem + (uint32_t(q * 32) << 16) + c, v);
+                umma::tmem_ld_wait();
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    asm volatile("st.shared.u32 [%0], %1;" ::"r"(base + ((c + i) * 128 + q * 32 + lane) * 4), "r"(v[i]) : "memory");
+            }
+        } else {
+            timed_out = true;
+        }
+    }
+    ptx::cluster_sync_all();
+    if (warp >= 2) {
+        // each CTA finishes its share of the (output row, eight output columns) units
+        const int units = BN * 16, per = (units + int(splits) - 1) / int(splits);
+        const int first = int(rank) * per, last = min(first + per, units);
+        for (int u = first + int(threadIdx.x) - 64; u < last; u += kDenseThreads - 64) {
+            const int64_t m = int64_t(ct) * BN + u / 16;
+            const int n = rt * kDenseTileM + (u % 16) * 8;
+            if (epi.outside(m, n)) continue;
+            float w[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+            const uint32_t at = base + ((u / 16) * 128 + (u % 16) * 8) * 4;
+            for (uint32_t s = 0; s < splits; ++s) {
+                const uint32_t p = ptx::map_to_cta(at, s);
+                const float4 a = ld_cluster_f32x4(p), b = ld_cluster_f32x4(p + 16);
+                w[0] += a.x; w[1] += a.y; w[2] += a.z; w[3] += a.w;
+                w[4] += b.x; w[5] += b.y; w[6] += b.z; w[7] += b.w;
+            }
+            epi(m, n, w);
+        }
+    }
+    if (timed_out && status) atomicOr(status, TPPO_DEV_WAIT_TIMEOUT);
+    umma::fence_before_thread_sync();
+    __syncwarp();
+    ptx::cluster_sync_all();          // no CTA leaves while another reads its sums
+    if (warp == 1) umma::tmem_dealloc(tmem, kCols);
+}
+
+// ---- host side ------------------------------------------------------------------------------------
+// One operand: a row-major 16-bit matrix [rows, cols] with row stride ld, 16-byte aligned rows.
+struct DenseOperand { const void* p; int64_t rows, cols, ld; };
+
+// D[m, n] = sum_k A(m, k) B(k, n).  AMAJ 0: a is [m, k]; 1: a is [k, m].  BMAJ 0: b is [n, k]; 1: b is [k, n].
+template <int AMAJ, int BMAJ, bool F16, bool SYM, class Epi>
+int dense_gemm(const DenseOperand& a, const DenseOperand& b, int64_t m, int64_t n, int64_t k, const Epi& epi,
+               int32_t* status, bool dependent, cudaStream_t s) {
+    CUtensorMap ma, mb;
+    if (!make_bf16_tensor_map(&ma, a.p, a.rows, a.cols, a.ld, AMAJ ? 64 : kDenseTileM) ||
+        !make_bf16_tensor_map(&mb, b.p, b.rows, b.cols, b.ld, BMAJ ? 64 : kDenseBN))
+        return TPPO_ERR_CUDA;
+    DenseShape g;
+    g.m_tiles = int32_t((m + kDenseTileM - 1) / kDenseTileM);
+    g.n_tiles = int32_t((n + kDenseBN - 1) / kDenseBN);
+    g.k_steps = int32_t((k + kDenseTileK - 1) / kDenseTileK);
+    g.group_m = 16;
+    const int32_t pairs = g.m_tiles / 2;
+    const int64_t total = SYM ? int64_t(pairs) * (pairs + 1) + (g.m_tiles % 2 ? pairs + 1 : 0) : int64_t(g.m_tiles) * g.n_tiles;
+    if (total > 0x7fffffff) return TPPO_ERR_UNSUPPORTED;
+    g.total = int32_t(total);
+    auto kernel = dense_gemm_kernel<AMAJ, BMAJ, F16, SYM, Epi>;
+    TPPO_CUDA_CHECK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, int(kDenseSmem)));
+    const int grid = g.total < kNumSms ? g.total : kNumSms;
+    TPPO_CUDA_CHECK(launch_dense(kernel, dim3(grid), dim3(kDenseThreads), kDenseSmem, s, dependent, ma, mb, g, epi, status));
+    return TPPO_OK;
+}
+
+// The same product through dense_split_kernel with the roles of the operands exchanged: the caller
+// passes the operand of the output's columns first.  AMAJ 0: a is [n, k]; 1: a is [k, n].
+// BMAJ 0: b is [m, k]; 1: b is [k, m].
+template <int AMAJ, int BMAJ, bool F16, int BN, class Epi>
+int dense_split(const DenseOperand& a, const DenseOperand& b, int64_t m, int64_t n, int64_t k, int splits, const Epi& epi,
+                int32_t* status, bool dependent, cudaStream_t s) {
+    CUtensorMap ma, mb;
+    if (!make_bf16_tensor_map(&ma, a.p, a.rows, a.cols, a.ld, AMAJ ? 64 : kDenseTileM) ||
+        !make_bf16_tensor_map(&mb, b.p, b.rows, b.cols, b.ld, BMAJ ? 64 : BN))
+        return TPPO_ERR_CUDA;
+    DenseSplitShape g;
+    const int64_t row_tiles = (n + kDenseTileM - 1) / kDenseTileM, col_tiles = (m + BN - 1) / BN;
+    g.col_tiles = int32_t(col_tiles);
+    g.k_steps = int32_t((k + kDenseTileK - 1) / kDenseTileK);
+    if (row_tiles * col_tiles * splits > 0x7fffffff) return TPPO_ERR_UNSUPPORTED;
+    auto kernel = dense_split_kernel<AMAJ, BMAJ, F16, BN, Epi>;
+    constexpr size_t smem = dense_split_smem<BN>();
+    TPPO_CUDA_CHECK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, int(smem)));
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = dim3(unsigned(row_tiles * col_tiles * splits));
+    cfg.blockDim = dim3(kDenseThreads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = s;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = unsigned(splits);
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[1].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = dependent ? 2 : 1;
+    TPPO_CUDA_CHECK(cudaLaunchKernelEx(&cfg, kernel, ma, mb, g, epi, status));
+    return TPPO_OK;
+}
+
+// How many CTAs share one tile's contraction: enough to fill the SMs (two CTAs fit on one), with at
+// least four k steps left to each so that its ring gets going.
+inline int dense_splits(int64_t tiles, int64_t k_steps) {
+    int s = 1;
+    while (s < 8 && tiles * s * 2 <= 2 * kNumSms && k_steps >= 4 * s * 2) s *= 2;
+    return s;
+}
+
+}  // namespace tppo

@@ -1,0 +1,379 @@
+// Matrix product with bias, activation and residual in its epilogue, and its backward pass:
+//     z = x W + bias,   y = act(z) + residual
+//     dz = dy * act'(z),   dx = dz W^T,   dweight = x^T dz,   dbias = sum over rows of dz
+// x [M, K], W [K, N] (the LM-head weight's layout) and the kept pre-activation z are bf16; products
+// are accumulated in fp32 on the tensor cores and everything up to the one rounding of y is fp32.
+//
+// dz is the one intermediate that is rounded: both gradients contract it on the tensor cores, so it
+// is formed once, in bf16 like the operand it meets, by a kernel that also sums dbias from the
+// unrounded values.  (Without an activation and with an aligned bf16 dy that kernel writes nothing
+// and dy itself is the operand.)
+//
+// Large outputs are tensor bound and take the persistent kernel; few rows, or few columns, are bound
+// by reading the weight (or x) once and take the split kernel, which spreads the contraction over a
+// cluster -- see dense_gemm.cuh.  TMA wants 16-byte aligned rows: operands whose row length or base
+// does not allow that are first copied into the workspace with a padded row stride.
+#include "dense_gemm.cuh"
+
+namespace tppo {
+namespace {
+
+__device__ __forceinline__ float act_value(float z, int act) {
+    switch (act) {
+        case TPPO_ACT_RELU: return fmaxf(z, 0.f);
+        case TPPO_ACT_GELU: return 0.5f * z * (1.f + erff(z * 0.70710678118654752f));
+        case TPPO_ACT_GELU_TANH: {
+            // 0.5 (1 + tanh u) = 1 / (1 + exp(-2u))
+            const float u = 0.79788456080286536f * fmaf(0.044715f * z * z, z, z);
+            return z / (1.f + expf(-2.f * u));
+        }
+        case TPPO_ACT_SILU: return z / (1.f + expf(-z));
+        default: return z;
+    }
+}
+__device__ __forceinline__ float act_slope(float z, int act) {
+    switch (act) {
+        case TPPO_ACT_RELU: return z > 0.f ? 1.f : 0.f;
+        case TPPO_ACT_GELU:
+            return 0.5f * (1.f + erff(z * 0.70710678118654752f)) + z * expf(-0.5f * z * z) * 0.39894228040143268f;
+        case TPPO_ACT_GELU_TANH: {
+            const float z2 = z * z;
+            const float u = 0.79788456080286536f * fmaf(0.044715f * z2, z, z);
+            const float p = 1.f / (1.f + expf(-2.f * u));           // 0.5 (1 + tanh u)
+            // where p has reached 0 or 1 the second term is 0 (z^3 may overflow there)
+            const float q = p * (1.f - p);
+            return q == 0.f ? p : fmaf(2.f * z * q, 0.79788456080286536f * fmaf(3.f * 0.044715f, z2, 1.f), p);
+        }
+        case TPPO_ACT_SILU: {
+            const float p = 1.f / (1.f + expf(-z));
+            const float q = p * (1.f - p);
+            return q == 0.f ? p : fmaf(z, q, p);
+        }
+        default: return 1.f;
+    }
+}
+
+// `count` (1..8) elements from v; one 16-byte store where the row allows it.
+__device__ __forceinline__ void put8(bf16_bits* p, const float (&v)[8], int count, bool vec) {
+    if (vec && count == 8) { store_vec<8>(p, v); return; }
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        if (i < count) store_f32(p + i, v[i]);
+}
+__device__ __forceinline__ void put8(float* p, const float (&v)[8], int count, bool vec) {
+    if (vec && count == 8) { store_vec<8>(p, v); return; }
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        if (i < count) p[i] = v[i];
+}
+template <class T>
+__device__ __forceinline__ void get8(const T* p, float (&v)[8], int count, bool vec) {
+    if (vec && count == 8) { load_vec<8>(p, v); return; }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = i < count ? load_f32(p + i) : 0.f;
+}
+
+// Forward epilogue.
+struct EpiLinear {
+    const void* bias; int32_t bias_f32;
+    const bf16_bits* residual; int64_t ldr;
+    void* y; int64_t ldy; int32_t y_f32;
+    bf16_bits* pre; int64_t ldp;
+    int64_t M; int32_t N; int32_t act;
+    int32_t vec_y, vec_r, vec_p, vec_b;
+    int32_t* status;
+
+    __device__ __forceinline__ bool outside(int64_t m, int n) const { return m >= M || n >= N; }
+    __device__ __forceinline__ void operator()(int64_t m, int n, float (&v)[8]) const {
+        if (outside(m, n)) return;
+        const int count = min(8, N - n);
+        float r[8];
+        if (residual) get8(residual + m * ldr + n, r, count, vec_r);
+        if (bias) {
+            float b[8];
+            if (bias_f32) get8(static_cast<const float*>(bias) + n, b, count, vec_b);
+            else get8(static_cast<const bf16_bits*>(bias) + n, b, count, vec_b);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] += b[i];
+        }
+        // z and y that are not finite, or leave the range of the type they are stored in, are written 0
+        bool bad = false;
+        float z[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float top = y_f32 ? kFltMax : kBf16Max;
+            z[i] = v[i];
+            float o = act_value(v[i], act);
+            if (residual) o += r[i];
+            const bool zok = fabsf(z[i]) <= (pre ? kBf16Max : kFltMax), ok = zok && fabsf(o) <= top;
+            if (!zok) z[i] = 0.f;
+            v[i] = ok ? o : 0.f;
+            bad |= !ok && i < count;
+        }
+        if (bad && status) atomicOr(status, TPPO_DEV_NONFINITE);
+        if (pre) put8(pre + m * ldp + n, z, count, vec_p);
+        if (y_f32) put8(static_cast<float*>(y) + m * ldy + n, v, count, vec_y);
+        else put8(static_cast<bf16_bits*>(y) + m * ldy + n, v, count, vec_y);
+    }
+};
+
+// Plain bf16 output (the two gradients).
+struct EpiStore {
+    bf16_bits* out; int64_t ld; int64_t M; int32_t N; int32_t vec;
+    int32_t* status;
+    __device__ __forceinline__ bool outside(int64_t m, int n) const { return m >= M || n >= N; }
+    __device__ __forceinline__ void operator()(int64_t m, int n, float (&v)[8]) const {
+        if (outside(m, n)) return;
+        const int count = min(8, N - n);
+        bool bad = false;
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (!(fabsf(v[i]) <= kBf16Max)) { bad |= i < count; v[i] = 0.f; }
+        if (bad && status) atomicOr(status, TPPO_DEV_NONFINITE);
+        put8(out + m * ld + n, v, count, vec);
+    }
+};
+
+// Copies a bf16 matrix into rows of ldo elements (a multiple of 8), eight elements per thread; the
+// tail of a row is filled with zeros.
+__global__ void __launch_bounds__(256) linear_repack_kernel(const bf16_bits* src, int64_t ld, int64_t rows, int32_t cols,
+                                                            bf16_bits* dst, int64_t ldo) {
+    const int64_t per = ldo / 8, total = rows * per;
+    for (int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x; i < total; i += int64_t(gridDim.x) * 256) {
+        const int64_t r = i / per;
+        const int c = int(i - r * per) * 8;
+        float v[8];
+        get8(src + r * ld + c, v, min(8, cols - c), false);
+        store_vec<8>(dst + r * ldo + c, v);
+    }
+}
+
+struct DzArgs {
+    const void* dy; int64_t lddy; int32_t vec_dy;
+    const bf16_bits* pre; int64_t ldp; int32_t vec_p;
+    bf16_bits* dz; int64_t ldz;             // NULL: dy itself is the operand
+    float* partial;                         // [gridDim.y][N] column sums or NULL
+    int64_t M; int32_t N; int32_t act;
+    int32_t* status;
+};
+
+// dz and the column sums behind dbias.  A block covers 256 columns (8 per thread, 32 threads) and every
+// (8 gridDim.y)-th row from its first; its eight warps' sums are added in warp order.
+template <class T>
+__global__ void __launch_bounds__(256) linear_dz_kernel(const DzArgs a) {
+    __shared__ float sums[8][256 + 8];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int n = blockIdx.x * 256 + lane * 8;
+    const int count = min(8, a.N - n);
+    float acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    bool bad = false;
+    if (count > 0) {
+        for (int64_t m = int64_t(blockIdx.y) * 8 + warp; m < a.M; m += int64_t(gridDim.y) * 8) {
+            float d[8];
+            get8(static_cast<const T*>(a.dy) + m * a.lddy + n, d, count, a.vec_dy);
+            if (a.act != TPPO_ACT_NONE) {
+                float z[8];
+                get8(a.pre + m * a.ldp + n, z, count, a.vec_p);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) d[i] *= act_slope(z[i], a.act);
+            }
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                if (!(fabsf(d[i]) <= kBf16Max)) { bad = true; d[i] = 0.f; }
+                acc[i] += d[i];
+            }
+            if (a.dz) store_vec<8>(a.dz + m * a.ldz + n, d);
+        }
+    }
+    if (bad && a.status) atomicOr(a.status, TPPO_DEV_NONFINITE);
+    if (!a.partial) return;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) sums[warp][lane * 8 + i] = acc[i];
+    __syncthreads();
+    const int c = blockIdx.x * 256 + threadIdx.x;
+    if (c < a.N) {
+        float t = 0.f;
+#pragma unroll
+        for (int w = 0; w < 8; ++w) t += sums[w][threadIdx.x];
+        a.partial[int64_t(blockIdx.y) * a.N + c] = t;
+    }
+}
+
+template <class T>
+__global__ void __launch_bounds__(256) linear_dbias_kernel(const float* partial, int32_t parts, int32_t N, T* dbias) {
+    const int c = blockIdx.x * 256 + threadIdx.x;
+    pdl_wait();
+    if (c >= N) return;
+    double t = 0.0;
+    for (int p = 0; p < parts; ++p) t += double(partial[int64_t(p) * N + c]);
+    store_f32(dbias + c, float(t));
+}
+
+int64_t pad8(int64_t n) { return (n + 7) / 8 * 8; }
+
+constexpr int kDzMaxParts = 256;
+
+// Workspace: dz, the partial sums of dbias, and (only where the sizes cannot meet TMA's alignment, or
+// the caller asked for them) padded copies of x and W.
+struct LinearWs { bf16_bits* dz; float* partial; bf16_bits* x; bf16_bits* w; size_t plain, bytes; };
+LinearWs linear_carve(void* ws, int64_t M, int32_t K, int32_t N) {
+    char* p = static_cast<char*>(ws);
+    const size_t dz = align_up(size_t(M) * pad8(N) * 2, kWsAlign), part = align_up(size_t(kDzMaxParts) * N * 4, kWsAlign);
+    const size_t x = align_up(size_t(M) * pad8(K) * 2, kWsAlign), w = align_up(size_t(K) * pad8(N) * 2, kWsAlign);
+    LinearWs r;
+    r.dz = reinterpret_cast<bf16_bits*>(p);
+    r.partial = reinterpret_cast<float*>(p + dz);
+    r.x = reinterpret_cast<bf16_bits*>(p + dz + part);
+    r.w = reinterpret_cast<bf16_bits*>(p + dz + part + x);
+    r.plain = dz + part;
+    r.bytes = dz + part + x + w;
+    return r;
+}
+
+bool tma_rows(const void* p, int64_t ld) { return aligned(p, 16) && ld % 8 == 0; }
+bool vec_rows(const void* p, int64_t ld, size_t esize) { return aligned(p, 16) && (ld * int64_t(esize)) % 16 == 0; }
+
+int repack(DenseOperand& o, bf16_bits* dst, cudaStream_t s) {
+    const int64_t ldo = pad8(o.cols), total = o.rows * (ldo / 8);
+    const int64_t blocks = (total + 255) / 256;
+    linear_repack_kernel<<<unsigned(blocks < 16 * kNumSms ? blocks : 16 * kNumSms), 256, 0, s>>>(
+        static_cast<const bf16_bits*>(o.p), o.ld, o.rows, int32_t(o.cols), dst, ldo);
+    TPPO_CUDA_CHECK(cudaGetLastError());
+    o.p = dst;
+    o.ld = ldo;
+    return TPPO_OK;
+}
+
+// D[m, n] by whichever kernel suits its number of tiles.  P: operand indexed by m (k-major when
+// PMAJ == 0), Q: operand indexed by n.
+template <int PMAJ, int QMAJ, class Epi>
+int product(const DenseOperand& P, const DenseOperand& Q, int64_t m, int64_t n, int64_t k, const Epi& epi, int32_t* status,
+            bool dependent, cudaStream_t s) {
+    const int64_t big = ((m + 127) / 128) * ((n + 255) / 256);
+    if (big >= kNumSms) return dense_gemm<PMAJ, QMAJ, false, false>(P, Q, m, n, k, epi, status, dependent, s);
+    const int64_t ks = (k + 63) / 64, rows = (n + 127) / 128;
+    if (PMAJ == 0 && m <= 16)
+        return dense_split<QMAJ, PMAJ, false, PMAJ ? 64 : 16>(Q, P, m, n, k, dense_splits(rows, ks), epi, status, dependent, s);
+    if (PMAJ == 0 && m <= 32)
+        return dense_split<QMAJ, PMAJ, false, PMAJ ? 64 : 32>(Q, P, m, n, k, dense_splits(rows, ks), epi, status, dependent, s);
+    if (m <= 64 || rows * ((m + 63) / 64) <= kNumSms)
+        return dense_split<QMAJ, PMAJ, false, 64>(Q, P, m, n, k, dense_splits(rows * ((m + 63) / 64), ks), epi, status, dependent, s);
+    return dense_split<QMAJ, PMAJ, false, 128>(Q, P, m, n, k, dense_splits(rows * ((m + 127) / 128), ks), epi, status, dependent, s);
+}
+
+bool act_known(int32_t a) { return a >= TPPO_ACT_NONE && a <= TPPO_ACT_SILU; }
+
+}  // namespace
+
+size_t linear_workspace_bytes(int64_t M, int32_t K, int32_t N, bool copies) {
+    if (K < 1 || N < 1) return 0;
+    const LinearWs w = linear_carve(nullptr, M, K, N);
+    return copies || K % 8 || N % 8 ? w.bytes : w.plain;
+}
+
+}  // namespace tppo
+
+using namespace tppo;
+
+TPPO_API int tppo_linear_fwd(const void* x, int64_t ldx, const void* weight, int64_t ldw, int64_t M, int32_t K, int32_t N,
+                             const void* bias, int32_t bias_dtype, int32_t activation, const void* residual, int64_t ldr,
+                             void* y, int32_t y_dtype, int64_t ldy, void* preact, int64_t ldp, int32_t* status,
+                             void* workspace, size_t workspace_bytes, void* stream) {
+    if (M < 0 || M > 0x7fffffffll || K < 1 || N < 1 || ldx < K || ldw < N || ldy < N || (residual && ldr < N) ||
+        (preact && ldp < N) || !act_known(activation))
+        return TPPO_ERR_INVALID_ARG;
+    if ((y_dtype != TPPO_BF16 && y_dtype != TPPO_F32) || (bias && bias_dtype != TPPO_BF16 && bias_dtype != TPPO_F32))
+        return TPPO_ERR_INVALID_ARG;
+    if (M == 0) return TPPO_OK;
+    const size_t ys = y_dtype == TPPO_F32 ? 4 : 2, bs = bias_dtype == TPPO_F32 ? 4 : 2;
+    if (!x || !weight || !y || !aligned(x, 2) || !aligned(weight, 2) || !aligned(bias, bs) || !aligned(residual, 2) ||
+        !aligned(y, ys) || !aligned(preact, 2) || !aligned(status, 4))
+        return TPPO_ERR_INVALID_ARG;
+    const bool copy_x = !tma_rows(x, ldx), copy_w = !tma_rows(weight, ldw);
+    const LinearWs w = linear_carve(workspace, M, K, N);
+    if ((copy_x || copy_w) && (!workspace || !aligned(workspace, kWsAlign) || workspace_bytes < w.bytes))
+        return TPPO_ERR_WORKSPACE;
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    DenseOperand X{x, M, K, ldx}, W{weight, K, N, ldw};
+    int rc;
+    if (copy_x && (rc = repack(X, w.x, s)) != TPPO_OK) return rc;
+    if (copy_w && (rc = repack(W, w.w, s)) != TPPO_OK) return rc;
+    EpiLinear e{};
+    e.bias = bias; e.bias_f32 = bias_dtype == TPPO_F32;
+    e.residual = static_cast<const bf16_bits*>(residual); e.ldr = ldr;
+    e.y = y; e.ldy = ldy; e.y_f32 = y_dtype == TPPO_F32;
+    e.pre = static_cast<bf16_bits*>(preact); e.ldp = ldp;
+    e.M = M; e.N = N; e.act = activation;
+    e.vec_y = vec_rows(y, ldy, ys); e.vec_r = vec_rows(residual, ldr, 2); e.vec_p = vec_rows(preact, ldp, 2);
+    e.vec_b = aligned(bias, 16);
+    e.status = status;
+    return product<0, 1>(X, W, M, N, K, e, status, false, s);
+}
+
+TPPO_API int tppo_linear_bwd(const void* dy, int32_t dy_dtype, int64_t lddy, const void* x, int64_t ldx, const void* weight,
+                             int64_t ldw, int64_t M, int32_t K, int32_t N, int32_t activation, const void* preact,
+                             int64_t ldp, void* dx, int64_t lddx, void* dweight, int64_t lddw, void* dbias,
+                             int32_t bias_dtype, int32_t* status, void* workspace, size_t workspace_bytes, void* stream) {
+    if (M < 0 || M > 0x7fffffffll || K < 1 || N < 1 || lddy < N || ldx < K || ldw < N || (dx && lddx < K) ||
+        (dweight && lddw < N) || !act_known(activation) || (activation != TPPO_ACT_NONE && ldp < N))
+        return TPPO_ERR_INVALID_ARG;
+    if ((dy_dtype != TPPO_BF16 && dy_dtype != TPPO_F32) || (dbias && bias_dtype != TPPO_BF16 && bias_dtype != TPPO_F32))
+        return TPPO_ERR_INVALID_ARG;
+    const size_t ds = dy_dtype == TPPO_F32 ? 4 : 2, bs = bias_dtype == TPPO_F32 ? 4 : 2;
+    if ((M > 0 && (!dy || (activation != TPPO_ACT_NONE && !preact) || (dx && !weight) || (dweight && !x))) ||
+        !aligned(dy, ds) || !aligned(x, 2) || !aligned(weight, 2) || !aligned(preact, 2) || !aligned(dx, 2) ||
+        !aligned(dweight, 2) || !aligned(dbias, bs) || !aligned(status, 4))
+        return TPPO_ERR_INVALID_ARG;
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    if (M == 0) {                                  // no rows: the weight's and the bias' sums are empty
+        if (dweight) TPPO_CUDA_CHECK(cudaMemset2DAsync(dweight, size_t(lddw) * 2, 0, size_t(N) * 2, size_t(K), s));
+        if (dbias) TPPO_CUDA_CHECK(cudaMemsetAsync(dbias, 0, size_t(N) * bs, s));
+        return TPPO_OK;
+    }
+    if (!dx && !dweight && !dbias) return TPPO_OK;
+    const bool products = dx || dweight;
+    const bool copy_x = dweight && !tma_rows(x, ldx), copy_w = dx && !tma_rows(weight, ldw);
+    const bool make_dz = products && (activation != TPPO_ACT_NONE || dy_dtype == TPPO_F32 || !tma_rows(dy, lddy));
+    const LinearWs w = linear_carve(workspace, M, K, N);
+    const size_t need = copy_x || copy_w ? w.bytes : make_dz || dbias ? w.plain : 0;
+    if (need && (!workspace || !aligned(workspace, kWsAlign) || workspace_bytes < need)) return TPPO_ERR_WORKSPACE;
+
+    DenseOperand X{x, M, K, ldx}, W{weight, K, N, ldw}, Z{dy, M, N, lddy};
+    int rc;
+    if (copy_x && (rc = repack(X, w.x, s)) != TPPO_OK) return rc;
+    if (copy_w && (rc = repack(W, w.w, s)) != TPPO_OK) return rc;
+    if (make_dz || dbias) {
+        DzArgs a{};
+        a.dy = dy; a.lddy = lddy; a.vec_dy = vec_rows(dy, lddy, ds);
+        a.pre = static_cast<const bf16_bits*>(preact); a.ldp = ldp; a.vec_p = vec_rows(preact, ldp, 2);
+        a.dz = make_dz ? w.dz : nullptr; a.ldz = pad8(N);
+        a.partial = dbias ? w.partial : nullptr;
+        a.M = M; a.N = N; a.act = activation; a.status = status;
+        const int gx = (N + 255) / 256;
+        int64_t gy = (M + 31) / 32, most = (16 * kNumSms + gx - 1) / gx;      // four rows per warp at least
+        if (gy > most) gy = most;
+        if (gy > kDzMaxParts) gy = kDzMaxParts;
+        if (dy_dtype == TPPO_F32) linear_dz_kernel<float><<<dim3(gx, unsigned(gy)), 256, 0, s>>>(a);
+        else linear_dz_kernel<bf16_bits><<<dim3(gx, unsigned(gy)), 256, 0, s>>>(a);
+        TPPO_CUDA_CHECK(cudaGetLastError());
+        if (make_dz) { Z.p = w.dz; Z.ld = a.ldz; }
+        if (dbias) {
+            const dim3 grid((N + 255) / 256);
+            if (bias_dtype == TPPO_F32)
+                TPPO_CUDA_CHECK(launch_dense(linear_dbias_kernel<float>, grid, dim3(256), 0, s, true,
+                                             static_cast<const float*>(w.partial), int32_t(gy), N, static_cast<float*>(dbias)));
+            else
+                TPPO_CUDA_CHECK(launch_dense(linear_dbias_kernel<bf16_bits>, grid, dim3(256), 0, s, true,
+                                             static_cast<const float*>(w.partial), int32_t(gy), N, static_cast<bf16_bits*>(dbias)));
+        }
+    }
+    if (dx) {        // dx[m, k] = sum_n dz[m, n] W[k, n]: both operands contiguous along the contraction
+        const EpiStore e{static_cast<bf16_bits*>(dx), lddx, M, K, vec_rows(dx, lddx, 2), status};
+        if ((rc = product<0, 0>(Z, W, M, K, N, e, status, false, s)) != TPPO_OK) return rc;
+    }
+    if (dweight) {   // dweight[k, n] = sum_m x[m, k] dz[m, n]: both contiguous along their outer index
+        const EpiStore e{static_cast<bf16_bits*>(dweight), lddw, K, N, vec_rows(dweight, lddw, 2), status};
+        if ((rc = product<1, 1>(X, Z, K, N, M, e, status, false, s)) != TPPO_OK) return rc;
+    }
+    return TPPO_OK;
+}

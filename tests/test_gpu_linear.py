@@ -1,0 +1,241 @@
+"""tppo_linear_fwd / _bwd.
+
+Whole numbers: with small integers as operands every product and sum is exact in fp32, so an fp32
+output has to be equal to the float64 product and a bf16 output to its one rounding -- any index or
+tail error shows.  Real numbers: a sum of K products in fp32 is off by at most K 2^-23 times the sum
+of magnitudes (2^-23: a tensor core may cut instead of round); what the epilogue adds is written at
+each check."""
+import pytest
+import torch
+
+from dense_util import BF, DEV, F32, F64, Guarded, U32, act64, gen, half_step, slope64, strided
+
+pytestmark = pytest.mark.gpu
+
+
+def whole(g, *shape, top=4):
+    return torch.randint(-top, top + 1, shape, generator=g, device=DEV).to(BF)
+
+
+def workspace(M, K, N, copies=0):
+    from paper_2506_15050_b200 import binding as b
+    ws = b.workspace(b.OP_LINEAR, M, K, copies, N, DEV)
+    ws.fill_(0xff)
+    return ws
+
+
+SIZES = [(1, 1, 1), (1, 8, 8), (1, 64, 256), (1, 5120, 640), (2, 5, 3), (5, 63, 7), (16, 64, 128), (17, 65, 129), (31, 200, 33),
+         (33, 515, 130), (64, 128, 64), (65, 72, 1000), (100, 1000, 40), (128, 64, 264), (129, 8, 257), (250, 77, 510),
+         (1000, 136, 1), (777, 300, 2), (1001, 515, 777), (300, 1024, 1024),
+         (2500, 72, 2000), (2561, 130, 2049), (19000, 24, 130)]
+
+
+@pytest.mark.parametrize("M,K,N", SIZES)
+def test_whole_numbers(M, K, N):
+    from paper_2506_15050_b200 import binding as b
+    g = gen(M + 7 * K + 31 * N)
+    x, w = whole(g, M, K), whole(g, K, N)
+    bias, residual = whole(g, N, top=9), whole(g, M, N, top=9)
+    ws, status = workspace(M, K, N), torch.zeros(1, dtype=torch.int32, device=DEV)
+    z = x.double() @ w.double()
+    y = Guarded(M, N, F32)
+    b.tppo_linear_fwd(x, w, None, b.ACT_NONE, None, y.t, None, status, ws)
+    assert torch.equal(y.t.double(), z)
+    y.check()
+    zb = z + bias.double()
+    yb, pre = Guarded(M, N, BF), Guarded(M, N, BF)
+    b.tppo_linear_fwd(x, w, bias, b.ACT_RELU, residual, yb.t, pre.t, status, ws)
+    assert torch.equal(yb.t, (torch.relu(zb) + residual.double()).to(BF)) and torch.equal(pre.t, zb.to(BF))
+    yb.check()
+    pre.check()
+    assert int(status) == 0
+
+    # backward: slopes 0 and 1, whole dy
+    dy = whole(g, M, N)
+    dz = dy.double() * (pre.t.double() > 0)
+    dx, dw = Guarded(M, K, BF), Guarded(K, N, BF)
+    db = torch.full((N,), float("nan"), device=DEV)
+    b.tppo_linear_bwd(dy, x, w, b.ACT_RELU, pre.t, dx.t, dw.t, db, status, ws)
+    assert torch.equal(dx.t, (dz @ w.double().t()).to(BF)) and torch.equal(dw.t, (x.double().t() @ dz).to(BF))
+    assert torch.equal(db.double(), dz.sum(0))
+    dx.check()
+    dw.check()
+    # without an activation, fp32 dy, bf16 dbias; any subset of the outputs
+    dx2, dw2, db2 = torch.empty_like(x), torch.empty_like(w), torch.empty(N, dtype=BF, device=DEV)
+    b.tppo_linear_bwd(dy.float(), x, w, b.ACT_NONE, None, dx2, None, None, status, ws)
+    b.tppo_linear_bwd(dy, x, w, b.ACT_NONE, None, None, dw2, None, status, ws)
+    b.tppo_linear_bwd(dy, x, w, b.ACT_NONE, None, None, None, db2, status, ws)
+    assert torch.equal(dx2, (dy.double() @ w.double().t()).to(BF)) and torch.equal(dw2, (x.double().t() @ dy.double()).to(BF))
+    assert torch.equal(db2, dy.double().sum(0).to(BF))
+    assert int(status) == 0
+
+
+@pytest.mark.parametrize("left,right", [(0, 8), (8, 16), (1, 0), (0, 3), (5, 3)])
+@pytest.mark.parametrize("M,K,N", [(3, 64, 40), (70, 72, 136), (130, 61, 75), (2500, 64, 2000)])
+def test_strided_rows_of_any_alignment(M, K, N, left, right):
+    from paper_2506_15050_b200 import binding as b
+    g = gen(left + 10 * right + M)
+    x, w, r, dy = whole(g, M, K), whole(g, K, N), whole(g, M, N), whole(g, M, N)
+    ws, status = workspace(M, K, N, 1), torch.zeros(1, dtype=torch.int32, device=DEV)
+    xs, wsd, rs, ds = (strided(t, left, right) for t in (x, w, r, dy))
+    y, pre = Guarded(M, N, BF, left, right), Guarded(M, N, BF, right, left)
+    b.tppo_linear_fwd(xs, wsd, None, b.ACT_RELU, rs, y.t, pre.t, status, ws)
+    z = x.double() @ w.double()
+    assert torch.equal(y.t, (torch.relu(z) + r.double()).to(BF)) and torch.equal(pre.t, z.to(BF))
+    dz = dy.double() * (pre.t.double() > 0)
+    dx, dw, db = Guarded(M, K, BF, left, right), Guarded(K, N, BF, right, left), torch.empty(N, device=DEV)
+    b.tppo_linear_bwd(ds, xs, wsd, b.ACT_RELU, pre.t, dx.t, dw.t, db, status, ws)
+    assert torch.equal(dx.t, (dz @ w.double().t()).to(BF)) and torch.equal(dw.t, (x.double().t() @ dz).to(BF))
+    b.tppo_linear_bwd(ds, xs, wsd, b.ACT_NONE, None, dx.t, dw.t, db, status, ws)
+    assert torch.equal(dx.t, (dy.double() @ w.double().t()).to(BF)) and torch.equal(db.double(), dy.double().sum(0))
+    for o in (y, pre, dx, dw):
+        o.check()
+    # the residual may be the output
+    acc = Guarded(M, N, BF, left, right)
+    acc.t.copy_(r)
+    b.tppo_linear_fwd(xs, wsd, None, b.ACT_NONE, acc.t, acc.t, None, status, ws)
+    assert torch.equal(acc.t, (z + r.double()).to(BF))
+    assert int(status) == 0
+
+
+def act_tol(z, act, e_z):
+    """The activations' slopes lie within 1.13 in magnitude; evaluated in fp32 from expf / erff (2 ulp
+    each) and fewer than ten further roundings of values of at most |z|: 16 u (|z| + 1e-6)."""
+    return 1.13 * e_z + 16 * U32 * (z.abs() + 1e-6)
+
+
+@pytest.mark.parametrize("act", range(5))
+@pytest.mark.parametrize("M,K,N", [(1, 300, 200), (40, 129, 77), (200, 512, 264), (2500, 96, 2000)])
+def test_real_numbers(M, K, N, act):
+    from paper_2506_15050_b200 import binding as b
+    g = gen(act + K)
+    x = torch.randn((M, K), generator=g, device=DEV).to(BF)
+    w = (torch.randn((K, N), generator=g, device=DEV) * 2 * K ** -0.5).to(BF)
+    bias = torch.randn(N, generator=g, device=DEV)
+    r = torch.randn((M, N), generator=g, device=DEV).to(BF)
+    ws, status = workspace(M, K, N), torch.zeros(1, dtype=torch.int32, device=DEV)
+    z = x.double() @ w.double() + bias.double()
+    e_z = (K + 2) * 2 * U32 * (x.double().abs() @ w.double().abs() + bias.double().abs())
+    for dt in (F32, BF):
+        y, pre = torch.empty((M, N), dtype=dt, device=DEV), torch.empty((M, N), dtype=BF, device=DEV)
+        b.tppo_linear_fwd(x, w, bias, act, r, y, pre, status, ws)
+        ref = act64(z, act) + r.double()
+        tol = act_tol(z, act, e_z) + ref.abs() * (half_step(dt) + U32)
+        assert bool(((y.double() - ref).abs() <= tol).all()), ((y.double() - ref).abs() / tol).max().item()
+        assert bool(((pre.double() - z).abs() <= e_z + z.abs() * half_step(BF)).all())
+    # backward from that preact: dz = dy act'(z), its bf16 rounding half a step; the slope 24 u
+    dy = torch.randn((M, N), generator=g, device=DEV)
+    dx, dw, db = torch.empty_like(x), torch.empty_like(w), torch.empty(N, device=DEV)
+    b.tppo_linear_bwd(dy, x, w, act, pre if act else None, dx, dw, db, status, ws)
+    dz = dy.double() * (slope64(pre.double(), act) if act else 1.0)
+    e_dz = dz.abs() * half_step(BF) + 24 * U32 * dy.double().abs() * (1 + pre.double().abs())
+    for got, ref, mag, err, n in ((dx, dz @ w.double().t(), dz.abs() @ w.double().abs().t(), e_dz @ w.double().abs().t(), N),
+                                  (dw, x.double().t() @ dz, x.double().abs().t() @ dz.abs(), x.double().abs().t() @ e_dz, M)):
+        tol = err * (1 + half_step(BF)) + n * 2 * U32 * mag * 1.01 + ref.abs() * half_step(BF)
+        assert bool(((got.double() - ref).abs() <= tol).all()), ((got.double() - ref).abs() / tol).max().item()
+    tol = (24 * U32 * dy.double().abs() * (1 + pre.double().abs())).sum(0) + (M / 8 + 300) * U32 * dz.abs().sum(0)
+    assert bool(((db.double() - dz.sum(0)).abs() <= tol).all())
+    assert int(status) == 0
+
+
+def test_gradient_against_differences():
+    """Central differences of <dy, y> in float64.  The gradients hold bf16 roundings (2^-8 of a value each
+    for dz and the output), so the directional derivative is off by 2^-7 of the sum of magnitudes at most."""
+    from paper_2506_15050_b200 import binding as b
+    M, K, N = 24, 40, 56
+    g = gen(3)
+    x, w = torch.randn((M, K), generator=g, device=DEV).to(BF), (torch.randn((K, N), generator=g, device=DEV) / 4).to(BF)
+    bias, dy = torch.randn(N, generator=g, device=DEV), torch.randn((M, N), generator=g, device=DEV)
+    for act in (2, 3, 4):
+        pre, y = torch.empty((M, N), dtype=BF, device=DEV), torch.empty((M, N), device=DEV)
+        dx, dw, db = torch.empty_like(x), torch.empty_like(w), torch.empty(N, device=DEV)
+        ws = workspace(M, K, N)
+        b.tppo_linear_fwd(x, w, bias, act, None, y, pre, None, ws)
+        b.tppo_linear_bwd(dy, x, w, act, pre, dx, dw, db, None, ws)
+        f = lambda x, w, c: (dy.double() * act64(x @ w + c, act)).sum()
+        args = [x.double(), w.double(), bias.double()]
+        for k, grad in enumerate((dx, dw, db)):
+            v = torch.randn(args[k].shape, generator=g, device=DEV, dtype=F64)
+            lo, hi = list(args), list(args)
+            lo[k], hi[k] = args[k] - 1e-4 * v, args[k] + 1e-4 * v
+            want, got = (f(*hi) - f(*lo)) / 2e-4, (grad.double() * v).sum()
+            # preact's own rounding moves act' by at most 1.2 |z| 2^-8: |z| < 8 here
+            assert abs(want - got) <= 2.0 ** -5 * (grad.double() * v).abs().sum()
+
+
+def test_far_activations_and_slopes():
+    """Large |z|: no overflow in between, tails exactly 0 or z."""
+    from paper_2506_15050_b200 import binding as b
+    z = torch.tensor([-3e38, -1e20, -300.0, -90.0, -20.0, -5.0, 0.0, 5.0, 20.0, 90.0, 300.0, 1e20, 3e38], device=DEV).to(BF)
+    x, w = torch.ones((1, 1), dtype=BF, device=DEV), z[None, :].contiguous()
+    N = z.numel()
+    ws = workspace(1, 1, N)
+    for act in range(5):
+        y, status = torch.empty((1, N), device=DEV), torch.zeros(1, dtype=torch.int32, device=DEV)
+        b.tppo_linear_fwd(x, w, None, act, None, y, None, status, ws)
+        ref = act64(z.double(), act)
+        if act == 3:
+            ref = torch.where(z.double().abs() > 1e3, torch.relu(z.double()), ref)
+        assert bool(((y[0].double() - ref).abs() <= act_tol(z.double(), act, 0.0) + 1e-38).all())
+        assert bool((y[0][z < -100] == 0).all()) or act == 0
+        db, dy = torch.empty(N, device=DEV), torch.ones((1, N), device=DEV)
+        b.tppo_linear_bwd(dy, x, w, act, z[None, :].contiguous(), None, None, db, status, ws)
+        far = z.double().clamp(-200, 200)                  # the slopes are 0 and 1 there already
+        ref = slope64(far, act) if act else torch.ones(N, dtype=F64, device=DEV)
+        assert bool(((db.double() - ref).abs() <= 24 * U32 * (1 + far.abs()) * 1.2).all())
+        assert int(status) == 0
+
+
+def test_elements_that_are_not_finite():
+    from paper_2506_15050_b200 import binding as b
+    for M, N in ((20, 48), (2500, 2000)):
+        K, g = 64, gen(1)
+        x, w, dy = whole(g, M, K), whole(g, K, N), whole(g, M, N)
+        x[3, 5], w[7, 11] = float("nan"), float("inf")
+        ws, status = workspace(M, K, N), torch.zeros(1, dtype=torch.int32, device=DEV)
+        y, pre = torch.empty((M, N), dtype=BF, device=DEV), torch.empty((M, N), dtype=BF, device=DEV)
+        b.tppo_linear_fwd(x, w, None, b.ACT_NONE, None, y, pre, status, ws)
+        ref = x.double() @ w.double()
+        ref = torch.where(torch.isfinite(ref), ref, 0.0)
+        assert torch.equal(y, ref.to(BF)) and torch.equal(pre, y) and int(status) == b.DEV_NONFINITE
+        status.zero_()
+        x[3, 5], w[7, 11] = 1.0, 2.0
+        dy[2, 9] = float("nan")
+        dx, dw, db = torch.empty_like(x), torch.empty_like(w), torch.empty(N, device=DEV)
+        b.tppo_linear_bwd(dy.float(), x, w, b.ACT_NONE, None, dx, dw, db, status, ws)
+        d = torch.nan_to_num(dy.double(), nan=0.0)
+        assert torch.equal(dx, (d @ w.double().t()).to(BF)) and torch.equal(dw, (x.double().t() @ d).to(BF))
+        assert torch.equal(db.double(), d.sum(0)) and int(status) == b.DEV_NONFINITE
+
+
+def test_no_rows():
+    from paper_2506_15050_b200 import binding as b
+    K, N = 24, 16
+    w = torch.ones((K, N), dtype=BF, device=DEV)
+    x, dy = torch.empty((0, K), dtype=BF, device=DEV), torch.empty((0, N), dtype=BF, device=DEV)
+    dw, db = Guarded(K, N, BF, 3, 2, fill=7.0), torch.ones(N, device=DEV)
+    b.tppo_linear_fwd(x, w, None, 0, None, torch.empty((0, N), dtype=BF, device=DEV), None, None, None)
+    b.tppo_linear_bwd(dy, x, w, 0, None, None, dw.t, db, None, None)
+    assert not dw.t.any() and not db.any()
+    dw.check()
+
+
+def test_refusals_on_the_device():
+    from paper_2506_15050_b200 import binding as b
+    x, w = torch.ones((4, 24), dtype=BF, device=DEV), torch.ones((24, 40), dtype=BF, device=DEV)
+    y = torch.full((4, 40), 7.0, dtype=BF, device=DEV)
+    with pytest.raises(b.TppoError) as e:                  # misaligned rows need the copies' workspace
+        b.tppo_linear_fwd(strided(x, 1, 0), w, None, 0, None, y, None, None, workspace(4, 24, 40))
+    assert e.value.status == 2
+    for bad in (lambda: b.tppo_linear_fwd(x, w, None, 9, None, y, None, None, None),):
+        with pytest.raises(b.TppoError) as e:
+            bad()
+        assert e.value.status == 1
+    for bad in (lambda: b.tppo_linear_fwd(x.float(), w, None, 0, None, y, None, None, None),
+                lambda: b.tppo_linear_fwd(x, w.t(), None, 0, None, y, None, None, None),
+                lambda: b.tppo_linear_fwd(x, w, None, 0, None, y[:3], None, None, None),
+                lambda: b.tppo_linear_fwd(x.cpu(), w, None, 0, None, y, None, None, None)):
+        with pytest.raises(AssertionError):
+            bad()
+    torch.cuda.synchronize()
+    assert bool((y == 7).all())
