@@ -5,13 +5,16 @@
 //     dgamma = sum_rows dy * h,   dbeta = sum_rows dy
 // All arithmetic is fp32; the inputs are read once and the outputs rounded once.
 //
-// Both passes are bound by HBM (2 resp. 3 elements moved per element).  A row lives in the registers
-// of a group of threads (one warp for short rows, up to a block for long ones), so mean and centred
-// variance are two sweeps over registers, not over memory.  The backward kernel's groups walk the
-// rows with a fixed stride and keep the gamma / beta sums of their columns in registers for the whole
-// walk; each block writes one partial row to the workspace and a second kernel adds the partial rows
-// in a fixed order, so the gradients do not depend on scheduling.  Rows longer than the registers of
-// a block hold take kernels that read the row again from L2 instead.
+// Both passes are bound by HBM (2 resp. 3 elements moved per element).  Forward, a row lives in the
+// registers of a few warps as the 16-byte pieces it was loaded in, so mean and centred variance are two
+// sweeps over registers.  Backward, the sums of gamma and beta want few columns per thread, so a row is spread
+// over a block; aligned rows are fed by bulk (TMA) copies through a shared-memory ring, which keeps
+// ~100 KB per block in flight while the block goes from row to row with one barrier each, and other
+// rows are loaded into registers some rows at a time.  Each block writes one partial row of column
+// sums to the workspace and a second kernel adds them in a fixed order, so the gradients do not depend
+// on scheduling.  Rows too long for either take kernels that read the row again from L2.
+#include <type_traits>
+
 #include "dense_common.cuh"
 
 namespace tppo {
@@ -26,65 +29,80 @@ struct NormFwdArgs {
     int32_t group;            // threads per row, a multiple of 32
 };
 
-// Sum over the group of `group` threads this thread belongs to.  A group of one warp needs no shared
-// memory; otherwise every thread of the block calls this together (`red`: one float per warp).
+// One 16-byte piece of a row as loaded, or one widened element (VEC 1).
+template <class T, int VEC> struct Piece {
+    uint4 w;
+    __device__ __forceinline__ void load(const T* p) { w = *reinterpret_cast<const uint4*>(p); }
+    __device__ __forceinline__ float get(int i) const {
+        const uint32_t u = VEC == 8 ? (i < 2 ? w.x : i < 4 ? w.y : i < 6 ? w.z : w.w) : (i == 0 ? w.x : i == 1 ? w.y : i == 2 ? w.z : w.w);
+        return VEC == 8 ? (i % 2 ? bf16_hi(u) : bf16_lo(u)) : __uint_as_float(u);
+    }
+};
+template <class T> struct Piece<T, 1> {
+    float w;
+    __device__ __forceinline__ void load(const T* p) { w = load_f32(p); }
+    __device__ __forceinline__ float get(int) const { return w; }
+};
+
+// VEC parameters, `otherwise` where there are none.
+template <int VEC, class P>
+__device__ __forceinline__ void load_params(const P* p, int col, float otherwise, float (&v)[VEC]) {
+    if (p) { load_vec<VEC>(p + col, v); return; }
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) v[i] = otherwise;
+}
+
+// Sum over the group of `group` threads this thread belongs to.  A group is one warp, or the whole
+// block, whose threads then call this together (`red`: one float per warp).
 __device__ __forceinline__ float group_sum(float v, int group, float* red) {
     v = warp_sum(v);
     if (group == 32) return v;
-    const int warp = threadIdx.x >> 5, per = group >> 5, first = warp / per * per;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    __syncthreads();                              // the previous sum has been read
+    if (lane == 0) red[warp] = v;
     __syncthreads();
-    if ((threadIdx.x & 31) == 0) red[warp] = v;
-    __syncthreads();
-    const int lane = threadIdx.x & 31;
-    return warp_sum(lane < per ? red[first + lane] : 0.f);
-}
-// Two sums at once.
-__device__ __forceinline__ float2 group_sum2(float2 v, int group, float2* red) {
-    v.x = warp_sum(v.x);
-    v.y = warp_sum(v.y);
-    if (group == 32) return v;
-    const int warp = threadIdx.x >> 5, per = group >> 5, first = warp / per * per;
-    __syncthreads();
-    if ((threadIdx.x & 31) == 0) red[warp] = v;
-    __syncthreads();
-    const int lane = threadIdx.x & 31;
-    const float2 w = lane < per ? red[first + lane] : make_float2(0.f, 0.f);
-    return make_float2(warp_sum(w.x), warp_sum(w.y));
+    return warp_sum(lane < (group >> 5) ? red[lane] : 0.f);
 }
 
-// Element c*group*VEC + t*VEC + i of the row sits in v[c][i] of the group's thread t.
+// Element (c * group + t) * VEC + i of the row sits in piece c of the group's thread t.
 template <class T, class P, int VEC, int CH>
 __global__ void __launch_bounds__(kNormMaxThreads) norm_fwd_kernel(const NormFwdArgs a) {
     __shared__ float red[32];
     const int t = threadIdx.x % a.group;
     const int64_t r = int64_t(blockIdx.x) * (blockDim.x / a.group) + threadIdx.x / a.group;
-    const bool have = r < a.M;                    // the last block may hold fewer rows
+    const bool have = r < a.M;                    // the last block may hold fewer rows than warps
     const T* x = static_cast<const T*>(a.x) + (have ? r : 0) * a.ldx;
-    float v[CH][VEC];
-    float s = 0.f;
+    Piece<T, VEC> raw[CH];
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
         const int col = (c * a.group + t) * VEC;
-        if (have && col < a.N) {
-            load_vec<VEC>(x + col, v[c]);
-#pragma unroll
-            for (int i = 0; i < VEC; ++i) s += v[c][i];
-        }
+        if (have && col < a.N) raw[c].load(x + col);
     }
-    const float mean = group_sum(s, a.group, red) / float(a.N);
-    s = 0.f;
+    // widened once: unpacking again in every sweep costs more issue slots than the arithmetic
+    float v[CH][VEC], s[2] = {0.f, 0.f};            // two chains of additions
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
-        const int col = (c * a.group + t) * VEC;
-        if (have && col < a.N) {
+        if (have && (c * a.group + t) * VEC < a.N) {
 #pragma unroll
             for (int i = 0; i < VEC; ++i) {
-                v[c][i] -= mean;
-                s = fmaf(v[c][i], v[c][i], s);
+                v[c][i] = raw[c].get(i);
+                s[(c + i) & 1] = s[(c + i) & 1] + v[c][i];
             }
         }
     }
-    const float var = group_sum(s, a.group, red) / float(a.N);
+    const float mean = group_sum(s[0] + s[1], a.group, red) / float(a.N);
+    s[0] = s[1] = 0;
+#pragma unroll
+    for (int c = 0; c < CH; ++c) {
+        if (have && (c * a.group + t) * VEC < a.N) {
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) {
+                v[c][i] = v[c][i] - mean;
+                s[(c + i) & 1] = fmaf(v[c][i], v[c][i], s[(c + i) & 1]);
+            }
+        }
+    }
+    const float var = group_sum(s[0] + s[1], a.group, red) / float(a.N);
     const float rstd = rsqrtf(var + a.eps);
     // a NaN or infinity in the row, or a variance outside fp32: no statistics, the row is written 0
     const bool good = is_finite(var) && is_finite(rstd);
@@ -97,19 +115,23 @@ __global__ void __launch_bounds__(kNormMaxThreads) norm_fwd_kernel(const NormFwd
     T* y = static_cast<T*>(a.y) + r * a.ldy;
     const P* gamma = static_cast<const P*>(a.gamma);
     const P* beta = static_cast<const P*>(a.beta);
+    if (!good) {
+        float zero[VEC];
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) zero[i] = 0;
+        for (int col = t * VEC; col < a.N; col += a.group * VEC) store_vec<VEC>(y + col, zero);
+        return;
+    }
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
         const int col = (c * a.group + t) * VEC;
         if (col < a.N) {
             float g[VEC], b[VEC];
-            if (gamma) load_vec<VEC>(gamma + col, g);
-            if (beta) load_vec<VEC>(beta + col, b);
+            load_params<VEC>(gamma, col, 1.f, g);
+            load_params<VEC>(beta, col, 0.f, b);
 #pragma unroll
-            for (int i = 0; i < VEC; ++i) {
-                const float h = v[c][i] * rstd;
-                v[c][i] = good ? fmaf(h, gamma ? g[i] : 1.f, beta ? b[i] : 0.f) : 0.f;
-            }
-            store_vec<VEC>(y + col, v[c]);
+            for (int i = 0; i < VEC; ++i) b[i] = fmaf(v[c][i] * rstd, g[i], b[i]);
+            store_vec<VEC>(y + col, b);
         }
     }
 }
@@ -152,76 +174,106 @@ struct NormBwdArgs {
     int32_t* status;
     int64_t M; int32_t N; int64_t lddy, ldx, lddx;
     int32_t group;
+    int32_t stages;                // ring kernel
 };
 
-template <class T, class P, int VEC, int CH>
-__global__ void __launch_bounds__(CH * VEC >= 16 ? 512 : kNormMaxThreads) norm_bwd_kernel(const NormBwdArgs a) {
-    extern __shared__ float cols[];               // [2][N], used when a block holds several groups
-    __shared__ float2 red[32];
-    const int t = threadIdx.x % a.group, grp = threadIdx.x / a.group, groups = blockDim.x / a.group;
-    const P* gamma = static_cast<const P*>(a.gamma);
-    const float inv_n = 1.f / float(a.N);
-    float dg[CH][VEC], db[CH][VEC];
-#pragma unroll
-    for (int c = 0; c < CH; ++c)
-#pragma unroll
-        for (int i = 0; i < VEC; ++i) dg[c][i] = db[c][i] = 0.f;
-    const int64_t step = int64_t(gridDim.x) * groups;
-    for (int64_t base = int64_t(blockIdx.x) * groups; base < a.M; base += step) {
-        const int64_t r = base + grp;
-        const bool have = r < a.M;
-        const int64_t rr = have ? r : 0;
-        const T* x = static_cast<const T*>(a.x) + rr * a.ldx;
-        const T* dy = static_cast<const T*>(a.dy) + rr * a.lddy;
-        const float rstd = have ? a.rstd[rr] : 0.f, mean = have ? a.mean[rr] : 0.f;
-        float h[CH][VEC], d[CH][VEC], g[CH][VEC];
-        float2 s = make_float2(0.f, 0.f);
-#pragma unroll
-        for (int c = 0; c < CH; ++c) {
-            const int col = (c * a.group + t) * VEC;
-            if (have && col < a.N) {
-                load_vec<VEC>(x + col, h[c]);
-                load_vec<VEC>(dy + col, d[c]);
-                if (gamma) load_vec<VEC>(gamma + col, g[c]);
-#pragma unroll
-                for (int i = 0; i < VEC; ++i) {
-                    if (!gamma) g[c][i] = 1.f;
-                    h[c][i] = (h[c][i] - mean) * rstd;
-                    const float av = d[c][i] * g[c][i];
-                    s.x += av;
-                    s.y = fmaf(av, h[c][i], s.y);
-                }
-            }
-        }
-        s = group_sum2(s, a.group, red);
-        const float c1 = s.x * inv_n, c2 = s.y * inv_n;
-        // rstd 0 marks a row without statistics; sums that are not finite come from a NaN or an
-        // infinity in x or dy: neither kind contributes, its dx is 0
-        const bool finite = is_finite(c1) && is_finite(c2) && is_finite(rstd);
-        const bool good = finite && rstd != 0.f;
-        if (!have) continue;
-        if (!finite && t == 0 && a.status) atomicOr(a.status, TPPO_DEV_NONFINITE);
-        T* dx = a.dx ? static_cast<T*>(a.dx) + r * a.lddx : nullptr;
+// The threads' share of one row.  With e = x - mean, k = sum(a e) / N * rstd^2 and q = -rstd sum(a) / N:
+//     dx = rstd a + q - (rstd k) e,   dgamma += dy (e rstd),   dbeta += dy
+// e is formed twice from the pieces instead of being kept in registers.
+template <class T, class P, int VEC, int CH> struct NormRow {
+    Piece<T, VEC> x[CH], d[CH];
+
+    // (sum of a, sum of a * (x - mean))
+    __device__ __forceinline__ float2 sums(const NormBwdArgs& a, int t, float mean) const {
+        const P* gamma = static_cast<const P*>(a.gamma);
+        float s[2] = {0.f, 0.f}, q[2] = {0.f, 0.f};      // two chains of additions each
 #pragma unroll
         for (int c = 0; c < CH; ++c) {
             const int col = (c * a.group + t) * VEC;
             if (col < a.N) {
-                float o[VEC];
+                float g[VEC];
+                load_params<VEC>(gamma, col, 1.f, g);
 #pragma unroll
                 for (int i = 0; i < VEC; ++i) {
-                    if (good) {
-                        dg[c][i] = fmaf(d[c][i], h[c][i], dg[c][i]);
-                        db[c][i] += d[c][i];
-                    }
-                    o[i] = good ? rstd * (d[c][i] * g[c][i] - c1 - h[c][i] * c2) : 0.f;
+                    const float av = d[c].get(i) * g[i];
+                    s[i & 1] += av;
+                    q[i & 1] = fmaf(av, x[c].get(i) - mean, q[i & 1]);
                 }
-                if (dx) store_vec<VEC>(dx + col, o);
+            }
+        }
+        return make_float2(s[0] + s[1], q[0] + q[1]);
+    }
+    __device__ __forceinline__ void finish(const NormBwdArgs& a, int t, int64_t r, float mean, float rstd, float c1, float c2, bool good,
+                                           float (&dg)[CH][VEC], float (&db)[CH][VEC]) const {
+        const P* gamma = static_cast<const P*>(a.gamma);
+        T* dx = a.dx ? static_cast<T*>(a.dx) + r * a.lddx : nullptr;
+        if (!good) {
+            float zero[VEC];
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) zero[i] = 0;
+            if (dx)
+                for (int col = t * VEC; col < a.N; col += a.group * VEC) store_vec<VEC>(dx + col, zero);
+            return;
+        }
+        const float q = -rstd * c1, k = -rstd * c2;
+#pragma unroll
+        for (int c = 0; c < CH; ++c) {
+            const int col = (c * a.group + t) * VEC;
+            if (col < a.N) {
+                float g[VEC];
+                load_params<VEC>(gamma, col, 1.f, g);
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) {
+                    const float dv = d[c].get(i), h = (x[c].get(i) - mean) * rstd;
+                    dg[c][i] = fmaf(dv, h, dg[c][i]);
+                    db[c][i] += dv;
+                    g[i] = fmaf(dv * g[i], rstd, fmaf(h, k, q));
+                }
+                if (dx) store_vec<VEC>(dx + col, g);
             }
         }
     }
+};
+
+// Sums over a warp of V values per lane (V a power of two up to 8): lane l ends up with the total of
+// value l % V.  Each of the first log2(V) exchanges halves the number of values.
+template <int V>
+__device__ __forceinline__ float warp_sum_many(float (&v)[V]) {
+    const int lane = threadIdx.x & 31;
+    int n = V;
+#pragma unroll
+    for (int o = 1; o < V; o <<= 1) {
+        n >>= 1;
+        const bool up = lane & o;
+#pragma unroll
+        for (int i = 0; i < V / 2; ++i) {
+            if (i < n) {
+                // values are paired by the bit of their index that this exchange settles
+                const float keep = up ? v[2 * i + 1] : v[2 * i], give = up ? v[2 * i] : v[2 * i + 1];
+                v[i] = keep + __shfl_xor_sync(0xffffffffu, give, o);
+            }
+        }
+    }
+#pragma unroll
+    for (int o = V; o < 32; o <<= 1) v[0] += __shfl_xor_sync(0xffffffffu, v[0], o);
+    return v[0];
+}
+
+// rstd 0 marks a row without statistics; sums that are not finite come from a NaN or an infinity in x
+// or dy: neither kind contributes, its dx is 0.
+__device__ __forceinline__ bool norm_row_good(float c1, float c2, float rstd, bool first, int32_t* status) {
+    const bool finite = is_finite(c1) && is_finite(c2) && is_finite(rstd);
+    if (!finite && first && status) atomicOr(status, TPPO_DEV_NONFINITE);
+    return finite && rstd != 0.f;
+}
+
+// This thread's column sums into the block's partial row; the groups of a block add theirs one after
+// the other: a fixed order.  `cols`: [2][N] shared floats, used with more than one group.
+template <int VEC, int CH>
+__device__ __forceinline__ void norm_put_partial(const NormBwdArgs& a, int t, int grp, int groups, float* cols,
+                                                 const float (&dg)[CH][VEC], const float (&db)[CH][VEC]) {
     if (!a.partial) return;
     float* out = a.partial + int64_t(blockIdx.x) * 2 * a.N;
-    // the groups of a block add their columns one after the other: a fixed order
     for (int k = 0; k < groups; ++k) {
         if (grp == k) {
 #pragma unroll
@@ -242,10 +294,147 @@ __global__ void __launch_bounds__(CH * VEC >= 16 ? 512 : kNormMaxThreads) norm_b
     }
 }
 
-// Rows of any length: dx row by row; `row` keeps (c1, c2) and the row's flag for the column sums.
+// Rows of any alignment, ROWS of a group's rows at a time in registers.
+template <class T, class P, int VEC, int CH, int ROWS>
+__global__ void __launch_bounds__(512) norm_bwd_kernel(const NormBwdArgs a) {
+    constexpr int VALUES = 2 * ROWS;
+    extern __shared__ float cols[];
+    __shared__ float red[2][16][VALUES];
+    const int t = threadIdx.x % a.group, grp = threadIdx.x / a.group, groups = blockDim.x / a.group;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, per = a.group >> 5, first = warp / per * per;
+    const float inv_n = 1.f / float(a.N);
+    float dg[CH][VEC], db[CH][VEC];
+#pragma unroll
+    for (int c = 0; c < CH; ++c)
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) dg[c][i] = db[c][i] = 0;
+    const int64_t step = int64_t(gridDim.x) * groups;
+    int flip = 0;
+    for (int64_t base = int64_t(blockIdx.x) * groups; base < a.M; base += step * ROWS, flip ^= 1) {
+        const int64_t r0 = base + grp;
+        NormRow<T, P, VEC, CH> row[ROWS];
+        float mean[ROWS], rstd[ROWS], s[VALUES];
+#pragma unroll
+        for (int k = 0; k < ROWS; ++k) {
+            const int64_t r = r0 + k * step;
+            mean[k] = rstd[k] = 0.f;
+            if (r < a.M) {
+                mean[k] = a.mean[r];
+                rstd[k] = a.rstd[r];
+                const T* x = static_cast<const T*>(a.x) + r * a.ldx;
+                const T* dy = static_cast<const T*>(a.dy) + r * a.lddy;
+#pragma unroll
+                for (int c = 0; c < CH; ++c) {
+                    const int col = (c * a.group + t) * VEC;
+                    if (col < a.N) {
+                        row[k].x[c].load(x + col);
+                        row[k].d[c].load(dy + col);
+                    }
+                }
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < ROWS; ++k) {
+            s[2 * k] = s[2 * k + 1] = 0.f;
+            if (r0 + k * step < a.M) {
+                const float2 v = row[k].sums(a, t, mean[k]);
+                s[2 * k] = v.x;
+                s[2 * k + 1] = v.y * rstd[k];
+            }
+        }
+        float total = warp_sum_many<VALUES>(s);               // of value lane % VALUES
+        if (per > 1) {
+            // one barrier per trip (the groups of a block make the same number of them): the two halves
+            // of `red` alternate
+            if (lane < VALUES) red[flip][warp][lane] = total;
+            __syncthreads();
+            total = 0.f;
+            for (int w = lane / VALUES; w < per; w += 32 / VALUES) total += red[flip][first + w][lane % VALUES];
+#pragma unroll
+            for (int o = VALUES; o < 32; o <<= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
+        }
+#pragma unroll
+        for (int k = 0; k < ROWS; ++k) {
+            const int64_t r = r0 + k * step;
+            const float c1 = __shfl_sync(0xffffffffu, total, 2 * k) * inv_n;
+            const float c2 = __shfl_sync(0xffffffffu, total, 2 * k + 1) * inv_n;
+            if (r < a.M) {
+                const bool good = norm_row_good(c1, c2, rstd[k], t == 0, a.status);
+                row[k].finish(a, t, r, mean[k], rstd[k], c1, c2, good, dg, db);
+            }
+        }
+    }
+    norm_put_partial<VEC, CH>(a, t, grp, groups, cols, dg, db);
+}
+
+// Aligned rows: a block per row, x and dy rows brought in by bulk copies `stages` rows ahead.
+template <class T, class P, int VEC, int CH>
+__global__ void __launch_bounds__(CH * VEC > 16 ? 512 : 640) norm_bwd_ring_kernel(const NormBwdArgs a) {
+    extern __shared__ __align__(128) uint8_t ring[];     // [stages][x row, dy row], then one barrier per stage
+    __shared__ float red[2][2][32];
+    const int t = threadIdx.x, warp = t >> 5, lane = t & 31, warps = blockDim.x >> 5;
+    const uint32_t row_bytes = uint32_t(a.N) * sizeof(T), stage_bytes = 2 * row_bytes;
+    const uint32_t base = ptx::smem_addr(ring), full = base + a.stages * stage_bytes;
+    const float inv_n = 1.f / float(a.N);
+    const int64_t step = gridDim.x;
+    auto issue = [&](int64_t r, int s) {
+        const uint32_t bar = full + 8 * s, at = base + s * stage_bytes;
+        ptx::mbar_arrive_expect_tx(bar, stage_bytes);
+        ptx::bulk_load(at, static_cast<const T*>(a.x) + r * a.ldx, row_bytes, bar);
+        ptx::bulk_load(at + row_bytes, static_cast<const T*>(a.dy) + r * a.lddy, row_bytes, bar);
+    };
+    if (t == 0) {
+        for (int s = 0; s < a.stages; ++s) ptx::mbar_init(full + 8 * s, 1);
+        ptx::fence_mbar_init_cluster();
+        for (int s = 0; s < a.stages && blockIdx.x + s * step < a.M; ++s) issue(blockIdx.x + s * step, s);
+    }
+    __syncthreads();
+    float dg[CH][VEC], db[CH][VEC];
+#pragma unroll
+    for (int c = 0; c < CH; ++c)
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) dg[c][i] = db[c][i] = 0;
+    int stage = 0, flip = 0;
+    uint32_t phase = 0;
+    bool timed_out = false;
+    float next_mean = a.mean[blockIdx.x], next_rstd = a.rstd[blockIdx.x];
+    for (int64_t r = blockIdx.x; r < a.M; r += step, flip ^= 1) {
+        const float mean = next_mean, rstd = next_rstd;
+        if (r + step < a.M) { next_mean = a.mean[r + step]; next_rstd = a.rstd[r + step]; }
+        // a wait that ran out is not repeated: the sums are then garbage, and flagged
+        if (!timed_out) timed_out = !ptx::mbar_wait<false>(full + 8 * stage, phase);
+        NormRow<T, P, VEC, CH> row;
+        const uint8_t* at = ring + stage * stage_bytes;
+#pragma unroll
+        for (int c = 0; c < CH; ++c) {
+            const int col = (c * a.group + t) * VEC;
+            if (col < a.N) {
+                row.x[c].load(reinterpret_cast<const T*>(at) + col);
+                row.d[c].load(reinterpret_cast<const T*>(at + row_bytes) + col);
+            }
+        }
+        const float2 part = row.sums(a, t, mean);
+        float s[2] = {part.x, part.y * rstd};
+        const float mine = warp_sum_many<2>(s);
+        if (lane < 2) red[flip][lane][warp] = mine;
+        __syncthreads();                          // the partial sums are there, and the stage has been read
+        if (t == 0 && r + a.stages * step < a.M) issue(r + a.stages * step, stage);
+        if (++stage == a.stages) { stage = 0; phase ^= 1u; }
+        float w[2] = {0.f, 0.f};
+        if (lane < warps) { w[0] = red[flip][0][lane]; w[1] = red[flip][1][lane]; }
+        const float total = warp_sum_many<2>(w);
+        const float c1 = __shfl_sync(0xffffffffu, total, 0) * inv_n, c2 = __shfl_sync(0xffffffffu, total, 1) * inv_n;
+        const bool good = norm_row_good(c1, c2, rstd, t == 0, a.status);
+        row.finish(a, t, r, mean, rstd, c1, c2, good, dg, db);
+    }
+    if (timed_out && a.status) atomicOr(a.status, TPPO_DEV_WAIT_TIMEOUT);
+    norm_put_partial<VEC, CH>(a, t, 0, 1, nullptr, dg, db);
+}
+
+// Rows of any length: dx and, in row_flag, which rows count in the column sums.
 template <class T, class P>
 __global__ void __launch_bounds__(kNormMaxThreads) norm_bwd_long_kernel(const NormBwdArgs a, float* row_flag) {
-    __shared__ float2 red[32];
+    __shared__ float red[32];
     const int64_t r = blockIdx.x;
     const T* x = static_cast<const T*>(a.x) + r * a.ldx;
     const T* dy = static_cast<const T*>(a.dy) + r * a.lddy;
@@ -257,14 +446,9 @@ __global__ void __launch_bounds__(kNormMaxThreads) norm_bwd_long_kernel(const No
         s.x += av;
         s.y = fmaf(av, (load_f32(x + c) - mean) * rstd, s.y);
     }
-    s = group_sum2(s, blockDim.x, red);
-    const float c1 = s.x / float(a.N), c2 = s.y / float(a.N);
-    const bool finite = is_finite(c1) && is_finite(c2) && is_finite(rstd);
-    const bool good = finite && rstd != 0.f;
-    if (threadIdx.x == 0) {
-        if (row_flag) row_flag[r] = good ? 1.f : 0.f;
-        if (!finite && a.status) atomicOr(a.status, TPPO_DEV_NONFINITE);
-    }
+    const float c1 = group_sum(s.x, blockDim.x, red) / float(a.N), c2 = group_sum(s.y, blockDim.x, red) / float(a.N);
+    const bool good = norm_row_good(c1, c2, rstd, threadIdx.x == 0, a.status);
+    if (row_flag && threadIdx.x == 0) row_flag[r] = good ? 1.f : 0.f;
     if (!a.dx) return;
     T* dx = static_cast<T*>(a.dx) + r * a.lddx;
     for (int c = threadIdx.x; c < a.N; c += blockDim.x) {
@@ -274,8 +458,7 @@ __global__ void __launch_bounds__(kNormMaxThreads) norm_bwd_long_kernel(const No
     }
 }
 
-// Column sums of long rows: one thread per column, blockIdx.y takes every gridDim.y-th row.  Runs
-// before the kernel above when dx overwrites dy, after it otherwise -- see the launcher.
+// Column sums of long rows: one thread per column, blockIdx.y takes every gridDim.y-th row.
 template <class T>
 __global__ void __launch_bounds__(256) norm_cols_kernel(const NormBwdArgs a, const float* row_flag) {
     const int c = blockIdx.x * 256 + threadIdx.x;
@@ -293,57 +476,42 @@ __global__ void __launch_bounds__(256) norm_cols_kernel(const NormBwdArgs a, con
     out[a.N + c] = db;
 }
 
-// dgamma / dbeta = the sum of `parts` partial rows, in ascending order within each of the 8 strands of
+// dgamma / dbeta = the sum of `parts` partial rows, in ascending order within each of the 16 strands of
 // a column and then over the strands; fp64, rounded once.
 template <class P>
-__global__ void __launch_bounds__(256) norm_sum_kernel(const float* partial, int32_t parts, int32_t N, P* dgamma,
+__global__ void __launch_bounds__(512) norm_sum_kernel(const float* partial, int32_t parts, int32_t N, P* dgamma,
                                                        P* dbeta) {
-    __shared__ double s[8][33];
+    __shared__ double s[16][33];
     pdl_wait();
     const int lane = threadIdx.x & 31, strand = threadIdx.x >> 5;
     const int64_t j = int64_t(blockIdx.x) * 32 + lane;           // column of the [2N]-wide partial row
     double t = 0.0;
-    if (j < 2 * int64_t(N))
-        for (int p = strand; p < parts; p += 8) t += double(partial[int64_t(p) * 2 * N + j]);
+    if (j < 2 * int64_t(N)) {
+#pragma unroll 4
+        for (int p = strand; p < parts; p += 16) t += double(partial[int64_t(p) * 2 * N + j]);
+    }
     s[strand][lane] = t;
     __syncthreads();
     if (strand == 0 && j < 2 * int64_t(N)) {
         t = 0.0;
 #pragma unroll
-        for (int k = 0; k < 8; ++k) t += s[k][lane];
+        for (int k = 0; k < 16; ++k) t += s[k][lane];
         if (j < N) { if (dgamma) store_f32(dgamma + j, float(t)); }
         else if (dbeta) store_f32(dbeta + (j - N), float(t));
     }
-}
-
-// How a row of N elements is spread: vectors of `vec`, `ch` per thread, `group` threads.
-struct NormPlan { int vec, ch, group, groups; };
-
-
-// Smallest ch of the ladder whose group stays within `limit` threads; ch 0 when none does.
-NormPlan norm_plan(int32_t N, int vec, const int* ladder, int rungs, int limit) {
-    const int64_t nvec = (int64_t(N) + vec - 1) / vec;
-    for (int k = 0; k < rungs; ++k) {
-        const int64_t g = ((nvec + ladder[k] - 1) / ladder[k] + 31) / 32 * 32;
-        if (g <= limit || (k == rungs - 1 && g <= kNormMaxThreads)) {
-            const int group = int(g);
-            const int groups = group >= 256 ? 1 : 256 / group;
-            return {vec, ladder[k], group, groups};
-        }
-    }
-    return {vec, 0, 0, 0};
 }
 
 bool rows_aligned(const void* p, int64_t ld, size_t esize) {
     return aligned(p, 16) && (ld * int64_t(esize)) % 16 == 0;
 }
 
-template <class T, class P, int VEC, int CH>
-int norm_fwd_launch(const NormFwdArgs& a, const NormPlan& p, cudaStream_t s) {
-    const int64_t blocks = (a.M + p.groups - 1) / p.groups;
-    norm_fwd_kernel<T, P, VEC, CH><<<unsigned(blocks), p.group * p.groups, 0, s>>>(a);
-    TPPO_CUDA_CHECK(cudaGetLastError());
-    return TPPO_OK;
+// Calls f.template operator()<CH>() with the smallest CH of the list that is at least `need`.
+template <int... CH, class F>
+int with_pieces(int need, F&& f) {
+    int rc = TPPO_ERR_UNSUPPORTED;
+    bool done = false;
+    ((!done && need <= CH ? (done = true, rc = f(std::integral_constant<int, CH>())) : 0), ...);
+    return rc;
 }
 
 template <class T, class P>
@@ -351,24 +519,31 @@ int norm_fwd_typed(NormFwdArgs a, cudaStream_t s) {
     constexpr int V = 16 / sizeof(T);
     const bool vec = a.N % V == 0 && rows_aligned(a.x, a.ldx, sizeof(T)) && rows_aligned(a.y, a.ldy, sizeof(T)) &&
                      (!a.gamma || aligned(a.gamma, 16)) && (!a.beta || aligned(a.beta, 16));
-    static const int ladder_v[] = {1, 2, 4}, ladder_s[] = {4, 16};
-    const NormPlan p = vec ? norm_plan(a.N, V, ladder_v, 3, 320) : norm_plan(a.N, 1, ladder_s, 2, 512);
-    a.group = p.group;
-    if (p.ch == 0) {
+    // Four 16-byte pieces (eight single elements) per thread: few registers, so that some 40 warps per SM
+    // keep ~80 KB in flight.  Rows longer than 1024 such threads hold take 8 (16) per thread, then the
+    // kernel that reads the row again.  With few rows more threads share a row, for shorter chains.
+    const int64_t pieces = vec ? a.N / V : a.N;
+    int64_t per = vec ? 4 : 8;
+    while (per > 1 && a.M * ((pieces + per - 1) / per) < int64_t(kNumSms) * 512 && pieces <= per / 2 * 512) per /= 2;
+    if (pieces > per * kNormMaxThreads) per *= 2;
+    if (pieces > per * kNormMaxThreads) {
         norm_fwd_long_kernel<T, P><<<unsigned(a.M), kNormMaxThreads, 0, s>>>(a);
         TPPO_CUDA_CHECK(cudaGetLastError());
         return TPPO_OK;
     }
-    if (vec) {
-        if (p.ch == 1) return norm_fwd_launch<T, P, V, 1>(a, p, s);
-        if (p.ch == 2) return norm_fwd_launch<T, P, V, 2>(a, p, s);
-        return norm_fwd_launch<T, P, V, 4>(a, p, s);
-    }
-    if (p.ch == 4) return norm_fwd_launch<T, P, 1, 4>(a, p, s);
-    return norm_fwd_launch<T, P, 1, 16>(a, p, s);
+    a.group = int32_t((pieces + per * 32 - 1) / (per * 32) * 32);
+    const int groups = a.group == 32 ? 4 : 1;
+    const unsigned blocks = unsigned((a.M + groups - 1) / groups);
+    const auto go = [&](auto vecs, auto ch) -> int {
+        norm_fwd_kernel<T, P, decltype(vecs)::value, decltype(ch)::value><<<blocks, a.group * groups, 0, s>>>(a);
+        TPPO_CUDA_CHECK(cudaGetLastError());
+        return TPPO_OK;
+    };
+    if (vec) return with_pieces<1, 2, 4, 8>(int(per), [&](auto ch) { return go(std::integral_constant<int, V>(), ch); });
+    return with_pieces<1, 2, 4, 8, 16>(int(per), [&](auto ch) { return go(std::integral_constant<int, 1>(), ch); });
 }
 
-constexpr int kNormMaxParts = 4 * kNumSms;
+constexpr int kNormMaxParts = 2 * kNumSms;
 
 struct NormWs { float* partial; float* row_flag; size_t bytes; };
 NormWs norm_carve(void* ws, int64_t M, int32_t N) {
@@ -378,34 +553,69 @@ NormWs norm_carve(void* ws, int64_t M, int32_t N) {
     return {reinterpret_cast<float*>(p), reinterpret_cast<float*>(p + a), a + b};
 }
 
-template <class T, class P, int VEC, int CH>
-int norm_bwd_launch(const NormBwdArgs& a, const NormPlan& p, int* parts, cudaStream_t s) {
-    const int threads = p.group * p.groups;
-    const int64_t rows = (a.M + p.groups - 1) / p.groups;
-    const int per_sm = threads >= 1024 ? 1 : threads >= 512 ? 2 : 4;
-    const int64_t most = int64_t(kNumSms) * per_sm;
-    const int grid = int(rows < most ? rows : most);
-    *parts = grid;
-    const size_t smem = p.groups > 1 && a.partial ? size_t(a.N) * 8 : 0;
-    norm_bwd_kernel<T, P, VEC, CH><<<grid, threads, smem, s>>>(a);
-    TPPO_CUDA_CHECK(cudaGetLastError());
-    return TPPO_OK;
-}
+constexpr size_t kRingBytes = 112 * 1024, kRingBytesAlone = 224 * 1024;
 
 template <class T, class P>
 int norm_bwd_typed(NormBwdArgs a, P* dgamma, P* dbeta, float* row_flag, cudaStream_t s) {
     constexpr int V = 16 / sizeof(T);
     const bool vec = a.N % V == 0 && rows_aligned(a.x, a.ldx, sizeof(T)) && rows_aligned(a.dy, a.lddy, sizeof(T)) &&
                      (!a.dx || rows_aligned(a.dx, a.lddx, sizeof(T))) && (!a.gamma || aligned(a.gamma, 16));
-    // wide threads (16 sums or more of each kind) keep to 512 threads so that nothing spills
-    static const int ladder_b[] = {1, 2}, ladder_f[] = {2, 4}, ladder_s[] = {4, 16};
-    const NormPlan p = vec ? (V == 8 ? norm_plan(a.N, V, ladder_b, 2, 320) : norm_plan(a.N, V, ladder_f, 2, 320))
-                           : norm_plan(a.N, 1, ladder_s, 2, 512);
-    a.group = p.group;
-    int rc = TPPO_OK, parts = 0;
-    if (p.ch == 0 || (p.ch * p.vec >= 16 && p.group > 512)) {
-        // the column sums read dy, which dx may overwrite: statistics and flags first, then the sums,
-        // then dx
+    const int64_t pieces = vec ? a.N / V : a.N;
+    const size_t stage = 2 * size_t(a.N) * sizeof(T);
+    int parts = 0, rc = TPPO_OK;
+    if (vec && a.M >= kNumSms && pieces >= 128 && stage * 2 <= kRingBytesAlone && pieces <= 512 * (32 / V)) {
+        // two blocks per SM where their rings of at least three rows fit beside each other
+        const bool pair = stage * 3 <= kRingBytes;
+        const size_t budget = pair ? kRingBytes : kRingBytesAlone;
+        int64_t stages = int64_t(budget / stage);
+        if (stages > 8) stages = 8;
+        a.stages = int32_t(stages);
+        const int need = int((pieces + 319) / 320);
+        const size_t smem = size_t(stages) * stage + 8 * 8;
+        const int64_t most = kNumSms * (pair ? 2 : 1);
+        parts = int(a.M < most ? a.M : most);
+        const auto go = [&](auto ch) -> int {
+            constexpr int CH = decltype(ch)::value;
+            a.group = int32_t((pieces + CH * 32 - 1) / (CH * 32) * 32);
+            auto kernel = norm_bwd_ring_kernel<T, P, V, CH>;
+            TPPO_CUDA_CHECK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, int(smem)));
+            kernel<<<unsigned(parts), a.group, smem, s>>>(a);
+            TPPO_CUDA_CHECK(cudaGetLastError());
+            return TPPO_OK;
+        };
+        if constexpr (V == 8) rc = pieces > 2 * 512 ? go(std::integral_constant<int, 4>()) : with_pieces<1, 2>(need > 2 ? 2 : need, go);
+        else rc = pieces > 4 * 512 ? go(std::integral_constant<int, 8>()) : with_pieces<1, 2, 4>(need > 4 ? 4 : need, go);
+    } else if (pieces <= 512 * (vec ? 16 / V : 16)) {
+        // the fewest columns per thread (16 at most) that keep a row within 256 threads, else 512
+        static const int ladder[] = {1, 2, 4, 6, 8, 12, 16};
+        int need = 0, group = 0;
+        for (int k = 0; k < 14 && !need; ++k) {
+            const int ch = ladder[k % 7];
+            if (ch * (vec ? V : 1) > 16 || (vec && ch != 1 && ch != 2 && ch != 4)) continue;
+            const int64_t g = (pieces + ch * 32 - 1) / (ch * 32) * 32;
+            if (g <= (k < 7 ? 256 : 512)) { need = ch; group = int(g); }
+        }
+        a.group = group;
+        const int groups = group >= 128 ? 1 : 256 / group;
+        const int64_t rows = (a.M + groups - 1) / groups;
+        const int64_t most = kNumSms * 2;
+        parts = int(rows < most ? rows : most);
+        const size_t smem = groups > 1 && a.partial ? size_t(a.N) * 8 : 0;
+        const auto go = [&](auto vecs, auto ch) -> int {
+            constexpr int VEC = decltype(vecs)::value, CH = decltype(ch)::value;
+            // some sixteen elements of x and of dy in flight per thread and trip, at most four rows
+            constexpr int ROWS = VEC * CH > 8 ? 1 : VEC * CH > 4 ? 2 : 4;
+            norm_bwd_kernel<T, P, VEC, CH, ROWS><<<unsigned(parts), a.group * groups, smem, s>>>(a);
+            TPPO_CUDA_CHECK(cudaGetLastError());
+            return TPPO_OK;
+        };
+        if (vec) rc = with_pieces<1, 2, 4>(need, [&](auto ch) -> int {
+            if constexpr (decltype(ch)::value * V > 16) return TPPO_ERR_UNSUPPORTED;
+            else return go(std::integral_constant<int, V>(), ch);
+        });
+        else rc = with_pieces<1, 2, 4, 6, 8, 12, 16>(need, [&](auto ch) { return go(std::integral_constant<int, 1>(), ch); });
+    } else {
+        // the column sums read dy, which dx may overwrite: flags first, then the sums, then dx
         NormBwdArgs b = a;
         if (a.partial) {
             b.dx = nullptr;
@@ -419,14 +629,9 @@ int norm_bwd_typed(NormBwdArgs a, P* dgamma, P* dbeta, float* row_flag, cudaStre
             norm_bwd_long_kernel<T, P><<<unsigned(a.M), kNormMaxThreads, 0, s>>>(a, nullptr);
             TPPO_CUDA_CHECK(cudaGetLastError());
         }
-    } else if (vec) {
-        if (V == 8) rc = p.ch == 1 ? norm_bwd_launch<T, P, V, 1>(a, p, &parts, s) : norm_bwd_launch<T, P, V, 2>(a, p, &parts, s);
-        else rc = p.ch == 2 ? norm_bwd_launch<T, P, V, 2>(a, p, &parts, s) : norm_bwd_launch<T, P, V, 4>(a, p, &parts, s);
-    } else {
-        rc = p.ch == 4 ? norm_bwd_launch<T, P, 1, 4>(a, p, &parts, s) : norm_bwd_launch<T, P, 1, 16>(a, p, &parts, s);
     }
     if (rc != TPPO_OK || !a.partial) return rc;
-    TPPO_CUDA_CHECK(launch_dense(norm_sum_kernel<P>, dim3(unsigned((2 * int64_t(a.N) + 31) / 32)), dim3(256), 0, s, true,
+    TPPO_CUDA_CHECK(launch_dense(norm_sum_kernel<P>, dim3(unsigned((2 * int64_t(a.N) + 31) / 32)), dim3(512), 0, s, true,
                                  static_cast<const float*>(a.partial), int32_t(parts), a.N, dgamma, dbeta));
     return TPPO_OK;
 }
@@ -482,7 +687,7 @@ TPPO_API int tppo_layer_norm_bwd(const void* dy, const void* x, int32_t dtype, i
         return TPPO_OK;
     }
     if (!dx && !params) return TPPO_OK;
-    const NormBwdArgs a{dy, x, gamma, mean, rstd, dx, params ? w.partial : nullptr, status, M, N, lddy, ldx, lddx, 0};
+    const NormBwdArgs a{dy, x, gamma, mean, rstd, dx, params ? w.partial : nullptr, status, M, N, lddy, ldx, lddx, 0, 0};
     if (dtype == TPPO_BF16) {
         if (param_dtype == TPPO_F32)
             return norm_bwd_typed<bf16_bits, float>(a, static_cast<float*>(dgamma), static_cast<float*>(dbeta), w.row_flag, s);
