@@ -526,6 +526,31 @@ int tppo_linear_bwd(const void *dy, int32_t dy_dtype, int64_t lddy, const void *
                     void *dbias, int32_t bias_dtype, int32_t *status,
                     void *workspace, size_t workspace_bytes, void *stream);
 
+/*
+ * Orthogonalised update of a weight matrix (what its gradient, e.g. dweight of the calls above, is
+ * turned into), by Newton-Schulz products:
+ *     momentum = mu * momentum + grad,   U = nesterov ? grad + mu * momentum : momentum
+ *     X = U / (|U|_F + eps);  `steps` times:  A = X X^T,  B = b A + c A^2,  X = a X + B X
+ *     update = scale * X,                (a, b, c) = (3.4445, -4.7750, 2.0315)
+ * which drives every singular value of X to between 0.68 and 1.21 and leaves its singular vectors.
+ * (The products are taken from the smaller side; the result is the same.)
+ *   grad      [R, C] of `grad_dtype`; not changed, unless `update` is grad itself
+ *   momentum  [R, C] fp32 in/out, or NULL: U = grad (mu and nesterov are then not used)
+ *   eps >= 0; 1 <= steps <= 16 (five is customary)
+ *   scale     e.g. sqrt(max(1, R / C)); the caller applies weight -= lr * update
+ *   update    [R, C] bf16 out; may be grad itself when that is bf16 with the same row stride
+ *   workspace tppo_workspace_bytes(TPPO_OP_MUON, R, 0, 0, C) bytes
+ * Precision: momentum and X are fp32; operands of the products are rounded to fp16, sums are fp32.  The
+ * error of X before its rounding to bf16 is about 1e-3 of its norm after five steps.
+ * A gradient or momentum element that is not finite, or becomes so, counts as 0 (momentum is written 0
+ * there) and raises TPPO_DEV_NONFINITE.  U = 0 gives update = 0.
+ */
+int tppo_muon_orthogonalize(const void *grad, int32_t grad_dtype, int64_t ldg,
+                            float *momentum, int64_t ldm, int64_t R, int32_t C,
+                            float mu, int32_t nesterov, float eps, int32_t steps, float scale,
+                            void *update, int64_t ldu, int32_t *status,
+                            void *workspace, size_t workspace_bytes, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -84,6 +84,9 @@ _lib.tppo_linear_fwd.argtypes = [_vp, _i64, _vp, _i64, _i64, _i32, _i32, _vp, _i
 _lib.tppo_linear_bwd.restype = C.c_int
 _lib.tppo_linear_bwd.argtypes = [_vp, _i32, _i64, _vp, _i64, _vp, _i64, _i64, _i32, _i32, _i32, _vp, _i64,
                                  _vp, _i64, _vp, _i64, _vp, _i32, _vp, _vp, _sz, _vp]
+_lib.tppo_muon_orthogonalize.restype = C.c_int
+_lib.tppo_muon_orthogonalize.argtypes = [_vp, _i32, _i64, _vp, _i64, _i64, _i32, _f32, _i32, _f32, _i32, _f32,
+                                         _vp, _i64, _vp, _vp, _sz, _vp]
 
 
 class TppoError(RuntimeError):
@@ -359,3 +362,13 @@ def tppo_linear_bwd(dy, x, weight, activation, preact, dx, dweight, dbias, statu
     _check(_lib.tppo_linear_bwd(pd, _DTYPES[dy.dtype], lddy, px, ldx, pw, ldw, M, K, N, activation, pp, ldp,
                                 po, lddx, pg, lddw, _vector(dbias, N), _type_of(dbias), _ptr(status, torch.int32),
                                 _ptr(ws), 0 if ws is None else ws.numel(), _stream()))
+
+
+def tppo_muon_orthogonalize(grad, momentum, mu, nesterov, eps, steps, scale, update, status, ws):
+    R, Cn = grad.shape
+    _on_device(grad, momentum, update, status, ws)
+    (pg, ldg), (pm, ldm) = _matrix(grad), _matrix(momentum, grad.shape, torch.float32)
+    pu, ldu = _matrix(update, grad.shape, torch.bfloat16)
+    _check(_lib.tppo_muon_orthogonalize(pg, _DTYPES[grad.dtype], ldg, pm, ldm, R, Cn, mu, 1 if nesterov else 0, eps,
+                                        steps, scale, pu, ldu, _ptr(status, torch.int32), _ptr(ws), ws.numel(),
+                                        _stream()))

@@ -9,6 +9,7 @@ size_t value_workspace_bytes();
 size_t lmhead_workspace_bytes(int64_t M, int32_t K, int32_t V);
 size_t norm_workspace_bytes(int64_t M, int32_t N);
 size_t linear_workspace_bytes(int64_t M, int32_t K, int32_t N, bool copies);
+size_t muon_workspace_bytes(int64_t R, int32_t C);
 }  // namespace tppo
 
 // Test hooks (see tppo_test_hooks in the header): read by the launchers of the two look-back kernels.
@@ -53,6 +54,7 @@ TPPO_API size_t tppo_workspace_bytes(int op, int64_t N, int32_t B, int64_t n_max
         case TPPO_OP_LMHEAD: return tppo::lmhead_workspace_bytes(N, B, V);
         case TPPO_OP_LAYER_NORM: return tppo::norm_workspace_bytes(N, V);
         case TPPO_OP_LINEAR: return tppo::linear_workspace_bytes(N, B, V, n_max != 0);
+        case TPPO_OP_MUON: return tppo::muon_workspace_bytes(N, V);
         default: return 0;
     }
 }

@@ -458,4 +458,23 @@ inline int dense_splits(int64_t tiles, int64_t k_steps) {
     return s;
 }
 
+// D[m, n] by whichever kernel suits its number of tiles: the persistent one when its 128 x 256 tiles
+// fill the SMs, the split one otherwise.  P: the operand indexed by m (PMAJ 0: [m, k], 1: [k, m]), Q: the
+// one indexed by n (QMAJ 0: [n, k], 1: [k, n]).  SYM: D is symmetric (m = n).
+template <int PMAJ, int QMAJ, bool F16, bool SYM, class Epi>
+int dense_product(const DenseOperand& P, const DenseOperand& Q, int64_t m, int64_t n, int64_t k, const Epi& epi,
+                  int32_t* status, bool dependent, cudaStream_t s) {
+    const int64_t mt = (m + 127) / 128, nt = (n + 255) / 256;
+    const int64_t big = SYM ? mt / 2 * (mt / 2 + 1) + (mt % 2 ? mt / 2 + 1 : 0) : mt * nt;
+    if (big >= kNumSms) return dense_gemm<PMAJ, QMAJ, F16, SYM>(P, Q, m, n, k, epi, status, dependent, s);
+    const int64_t ks = (k + 63) / 64, rows = (n + 127) / 128;
+    // one operand box of 64 outer indices is the least an MN-major operand can be loaded in
+    constexpr int B16 = PMAJ ? 64 : 16, B32 = PMAJ ? 64 : 32;
+    if (m <= 16 && !PMAJ) return dense_split<QMAJ, PMAJ, F16, B16>(Q, P, m, n, k, dense_splits(rows, ks), epi, status, dependent, s);
+    if (m <= 32 && !PMAJ) return dense_split<QMAJ, PMAJ, F16, B32>(Q, P, m, n, k, dense_splits(rows, ks), epi, status, dependent, s);
+    const int64_t by64 = rows * ((m + 63) / 64);
+    if (by64 <= kNumSms) return dense_split<QMAJ, PMAJ, F16, 64>(Q, P, m, n, k, dense_splits(by64, ks), epi, status, dependent, s);
+    return dense_split<QMAJ, PMAJ, F16, 128>(Q, P, m, n, k, dense_splits(rows * ((m + 127) / 128), ks), epi, status, dependent, s);
+}
+
 }  // namespace tppo

@@ -244,23 +244,6 @@ int repack(DenseOperand& o, bf16_bits* dst, cudaStream_t s) {
     return TPPO_OK;
 }
 
-// D[m, n] by whichever kernel suits its number of tiles.  P: operand indexed by m (k-major when
-// PMAJ == 0), Q: operand indexed by n.
-template <int PMAJ, int QMAJ, class Epi>
-int product(const DenseOperand& P, const DenseOperand& Q, int64_t m, int64_t n, int64_t k, const Epi& epi, int32_t* status,
-            bool dependent, cudaStream_t s) {
-    const int64_t big = ((m + 127) / 128) * ((n + 255) / 256);
-    if (big >= kNumSms) return dense_gemm<PMAJ, QMAJ, false, false>(P, Q, m, n, k, epi, status, dependent, s);
-    const int64_t ks = (k + 63) / 64, rows = (n + 127) / 128;
-    if (PMAJ == 0 && m <= 16)
-        return dense_split<QMAJ, PMAJ, false, PMAJ ? 64 : 16>(Q, P, m, n, k, dense_splits(rows, ks), epi, status, dependent, s);
-    if (PMAJ == 0 && m <= 32)
-        return dense_split<QMAJ, PMAJ, false, PMAJ ? 64 : 32>(Q, P, m, n, k, dense_splits(rows, ks), epi, status, dependent, s);
-    if (m <= 64 || rows * ((m + 63) / 64) <= kNumSms)
-        return dense_split<QMAJ, PMAJ, false, 64>(Q, P, m, n, k, dense_splits(rows * ((m + 63) / 64), ks), epi, status, dependent, s);
-    return dense_split<QMAJ, PMAJ, false, 128>(Q, P, m, n, k, dense_splits(rows * ((m + 127) / 128), ks), epi, status, dependent, s);
-}
-
 bool act_known(int32_t a) { return a >= TPPO_ACT_NONE && a <= TPPO_ACT_SILU; }
 
 }  // namespace
@@ -307,7 +290,7 @@ TPPO_API int tppo_linear_fwd(const void* x, int64_t ldx, const void* weight, int
     e.vec_y = vec_rows(y, ldy, ys); e.vec_r = vec_rows(residual, ldr, 2); e.vec_p = vec_rows(preact, ldp, 2);
     e.vec_b = aligned(bias, 16);
     e.status = status;
-    return product<0, 1>(X, W, M, N, K, e, status, false, s);
+    return dense_product<0, 1, false, false>(X, W, M, N, K, e, status, false, s);
 }
 
 TPPO_API int tppo_linear_bwd(const void* dy, int32_t dy_dtype, int64_t lddy, const void* x, int64_t ldx, const void* weight,
@@ -369,11 +352,11 @@ TPPO_API int tppo_linear_bwd(const void* dy, int32_t dy_dtype, int64_t lddy, con
     }
     if (dx) {        // dx[m, k] = sum_n dz[m, n] W[k, n]: both operands contiguous along the contraction
         const EpiStore e{static_cast<bf16_bits*>(dx), lddx, M, K, vec_rows(dx, lddx, 2), status};
-        if ((rc = product<0, 0>(Z, W, M, K, N, e, status, false, s)) != TPPO_OK) return rc;
+        if ((rc = dense_product<0, 0, false, false>(Z, W, M, K, N, e, status, false, s)) != TPPO_OK) return rc;
     }
     if (dweight) {   // dweight[k, n] = sum_m x[m, k] dz[m, n]: both contiguous along their outer index
         const EpiStore e{static_cast<bf16_bits*>(dweight), lddw, K, N, vec_rows(dweight, lddw, 2), status};
-        if ((rc = product<1, 1>(X, Z, K, N, M, e, status, false, s)) != TPPO_OK) return rc;
+        if ((rc = dense_product<1, 1, false, false>(X, Z, K, N, M, e, status, false, s)) != TPPO_OK) return rc;
     }
     return TPPO_OK;
 }
