@@ -288,31 +288,39 @@ def tppo_advance_batch(seq_begin, prompt_len, prev_len, new_len, truncated, toke
 
 
 _DTYPES = {torch.bfloat16: BF16, torch.float32: F32}
+_raw_stream, _current_device = torch._C._cuda_getCurrentRawStream, torch.cuda.current_device
 
 
-def _on_device(*tensors):
-    """The dense operators take tensors of one device, which has to be the current one: the call goes
-    to its current stream."""
-    here = torch.cuda.current_device()
-    for t in tensors:
-        assert t is None or (t.is_cuda and t.device.index == here), f"tensors must be on cuda:{here}, the current device"
-
-
-def _matrix(t, shape=None, dtype=None):
-    """(pointer, row stride) of a matrix whose columns are contiguous; (None, 0) for None."""
+def _matrix(t, here, rows, cols, dtype=None):
+    """(pointer, row stride) of a [rows, cols] matrix on device `here` whose columns are contiguous;
+    (None, 0) for None.  The dense operators run on the current device and its current stream."""
     if t is None:
         return None, 0
-    assert t.dim() == 2 and (t.stride(1) == 1 or t.shape[1] == 1), "columns must be contiguous"
-    assert shape is None or tuple(t.shape) == tuple(shape), f"expected shape {tuple(shape)}, got {tuple(t.shape)}"
+    assert t.get_device() == here, f"tensors must be on cuda:{here}, the current device"
+    assert t.shape == (rows, cols), f"expected shape {(rows, cols)}, got {tuple(t.shape)}"
     assert dtype is None or t.dtype == dtype, f"expected {dtype}, got {t.dtype}"
-    ld = t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t.shape[1])
-    assert ld >= t.shape[1], "rows must not overlap"
+    ld, one = t.stride()
+    assert one == 1 or cols == 1, "columns must be contiguous"
+    if rows <= 1:
+        ld = max(ld, cols)
+    assert ld >= cols, "rows must not overlap"
     return t.data_ptr(), ld
 
 
-def _vector(t, n, dtype=None):
-    assert t is None or (t.dim() == 1 and t.numel() == n), f"expected {n} elements"
-    return _ptr(t, dtype)
+def _vector(t, here, n, dtype=None):
+    if t is None:
+        return None
+    assert t.get_device() == here, f"tensors must be on cuda:{here}, the current device"
+    assert t.shape == (n,) and t.is_contiguous(), f"expected {n} contiguous elements"
+    assert dtype is None or t.dtype == dtype, f"expected {dtype}, got {t.dtype}"
+    return t.data_ptr()
+
+
+def _scratch(t, here):
+    if t is None:
+        return None, 0
+    assert t.get_device() == here and t.is_contiguous(), f"the workspace must be contiguous and on cuda:{here}"
+    return t.data_ptr(), t.numel() * t.element_size()
 
 
 def _type_of(*tensors):
@@ -323,52 +331,57 @@ def _type_of(*tensors):
 
 
 def tppo_layer_norm_fwd(x, gamma, beta, eps, y, mean, rstd, status):
-    M, N = x.shape
-    _on_device(x, gamma, beta, y, mean, rstd, status)
-    (px, ldx), (py, ldy) = _matrix(x), _matrix(y, x.shape, x.dtype)
-    _check(_lib.tppo_layer_norm_fwd(px, _DTYPES[x.dtype], M, N, ldx, _vector(gamma, N), _vector(beta, N),
-                                    _type_of(gamma, beta), eps, py, ldy, _vector(mean, M, torch.float32),
-                                    _vector(rstd, M, torch.float32), _ptr(status, torch.int32), _stream()))
+    (M, N), dt, here = x.shape, x.dtype, _current_device()
+    (px, ldx), (py, ldy) = _matrix(x, here, M, N), _matrix(y, here, M, N, dt)
+    _check(_lib.tppo_layer_norm_fwd(
+        px, _DTYPES[dt], M, N, ldx, _vector(gamma, here, N), _vector(beta, here, N), _type_of(gamma, beta), eps, py, ldy,
+        _vector(mean, here, M, torch.float32), _vector(rstd, here, M, torch.float32),
+        _vector(status, here, 1, torch.int32), _raw_stream(here)))
 
 
 def tppo_layer_norm_bwd(dy, x, gamma, mean, rstd, dx, dgamma, dbeta, status, ws):
-    M, N = x.shape
-    _on_device(dy, x, gamma, mean, rstd, dx, dgamma, dbeta, status, ws)
-    (pd, lddy), (px, ldx), (po, lddx) = _matrix(dy, x.shape, x.dtype), _matrix(x), _matrix(dx, x.shape, x.dtype)
-    _check(_lib.tppo_layer_norm_bwd(pd, px, _DTYPES[x.dtype], M, N, lddy, ldx, _vector(gamma, N),
-                                    _type_of(gamma, dgamma, dbeta), _vector(mean, M, torch.float32),
-                                    _vector(rstd, M, torch.float32), po, lddx, _vector(dgamma, N),
-                                    _vector(dbeta, N), _ptr(status, torch.int32), _ptr(ws),
-                                    0 if ws is None else ws.numel(), _stream()))
+    (M, N), dt, here = x.shape, x.dtype, _current_device()
+    pd, lddy = _matrix(dy, here, M, N, dt)
+    px, ldx = _matrix(x, here, M, N)
+    po, lddx = _matrix(dx, here, M, N, dt)
+    _check(_lib.tppo_layer_norm_bwd(
+        pd, px, _DTYPES[dt], M, N, lddy, ldx, _vector(gamma, here, N), _type_of(gamma, dgamma, dbeta),
+        _vector(mean, here, M, torch.float32), _vector(rstd, here, M, torch.float32), po, lddx,
+        _vector(dgamma, here, N), _vector(dbeta, here, N), _vector(status, here, 1, torch.int32),
+        *_scratch(ws, here), _raw_stream(here)))
 
 
 def tppo_linear_fwd(x, weight, bias, activation, residual, y, preact, status, ws):
-    (M, K), N = x.shape, weight.shape[1]
-    _on_device(x, weight, bias, residual, y, preact, status, ws)
-    bf = torch.bfloat16
-    (px, ldx), (pw, ldw) = _matrix(x, dtype=bf), _matrix(weight, (K, N), bf)
-    (pr, ldr), (py, ldy), (pp, ldp) = _matrix(residual, (M, N), bf), _matrix(y, (M, N)), _matrix(preact, (M, N), bf)
-    _check(_lib.tppo_linear_fwd(px, ldx, pw, ldw, M, K, N, _vector(bias, N), _type_of(bias), activation, pr, ldr,
-                                py, _DTYPES[y.dtype], ldy, pp, ldp, _ptr(status, torch.int32), _ptr(ws),
-                                0 if ws is None else ws.numel(), _stream()))
+    (M, K), N, here, bf = x.shape, weight.shape[1], _current_device(), torch.bfloat16
+    px, ldx = _matrix(x, here, M, K, bf)
+    pw, ldw = _matrix(weight, here, K, N, bf)
+    pr, ldr = _matrix(residual, here, M, N, bf)
+    py, ldy = _matrix(y, here, M, N)
+    pp, ldp = _matrix(preact, here, M, N, bf)
+    _check(_lib.tppo_linear_fwd(
+        px, ldx, pw, ldw, M, K, N, _vector(bias, here, N), _type_of(bias), activation, pr, ldr, py, _DTYPES[y.dtype], ldy,
+        pp, ldp, _vector(status, here, 1, torch.int32), *_scratch(ws, here), _raw_stream(here)))
 
 
 def tppo_linear_bwd(dy, x, weight, activation, preact, dx, dweight, dbias, status, ws):
-    (M, K), N = x.shape, weight.shape[1]
-    _on_device(dy, x, weight, preact, dx, dweight, dbias, status, ws)
-    bf = torch.bfloat16
-    (pd, lddy), (px, ldx), (pw, ldw) = _matrix(dy, (M, N)), _matrix(x, dtype=bf), _matrix(weight, (K, N), bf)
-    (pp, ldp), (po, lddx), (pg, lddw) = _matrix(preact, (M, N), bf), _matrix(dx, (M, K), bf), _matrix(dweight, (K, N), bf)
-    _check(_lib.tppo_linear_bwd(pd, _DTYPES[dy.dtype], lddy, px, ldx, pw, ldw, M, K, N, activation, pp, ldp,
-                                po, lddx, pg, lddw, _vector(dbias, N), _type_of(dbias), _ptr(status, torch.int32),
-                                _ptr(ws), 0 if ws is None else ws.numel(), _stream()))
+    (M, K), N, here, bf = x.shape, weight.shape[1], _current_device(), torch.bfloat16
+    pd, lddy = _matrix(dy, here, M, N)
+    px, ldx = _matrix(x, here, M, K, bf)
+    pw, ldw = _matrix(weight, here, K, N, bf)
+    pp, ldp = _matrix(preact, here, M, N, bf)
+    po, lddx = _matrix(dx, here, M, K, bf)
+    pg, lddw = _matrix(dweight, here, K, N, bf)
+    _check(_lib.tppo_linear_bwd(
+        pd, _DTYPES[dy.dtype], lddy, px, ldx, pw, ldw, M, K, N, activation, pp, ldp, po, lddx, pg, lddw,
+        _vector(dbias, here, N), _type_of(dbias), _vector(status, here, 1, torch.int32), *_scratch(ws, here),
+        _raw_stream(here)))
 
 
 def tppo_muon_orthogonalize(grad, momentum, mu, nesterov, eps, steps, scale, update, status, ws):
-    R, Cn = grad.shape
-    _on_device(grad, momentum, update, status, ws)
-    (pg, ldg), (pm, ldm) = _matrix(grad), _matrix(momentum, grad.shape, torch.float32)
-    pu, ldu = _matrix(update, grad.shape, torch.bfloat16)
-    _check(_lib.tppo_muon_orthogonalize(pg, _DTYPES[grad.dtype], ldg, pm, ldm, R, Cn, mu, 1 if nesterov else 0, eps,
-                                        steps, scale, pu, ldu, _ptr(status, torch.int32), _ptr(ws), ws.numel(),
-                                        _stream()))
+    (R, cols), here = grad.shape, _current_device()
+    pg, ldg = _matrix(grad, here, R, cols)
+    pm, ldm = _matrix(momentum, here, R, cols, torch.float32)
+    pu, ldu = _matrix(update, here, R, cols, torch.bfloat16)
+    _check(_lib.tppo_muon_orthogonalize(
+        pg, _DTYPES[grad.dtype], ldg, pm, ldm, R, cols, mu, 1 if nesterov else 0, eps, steps, scale, pu, ldu,
+        _vector(status, here, 1, torch.int32), *_scratch(ws, here), _raw_stream(here)))

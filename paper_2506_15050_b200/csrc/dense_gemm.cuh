@@ -142,8 +142,10 @@ __device__ __forceinline__ void dense_tile(const DenseShape& g, int t, int& mt, 
     }
 }
 
-// Epi: void operator()(int64_t row, int col, float (&v)[8]) const -- v holds columns col .. col+7 of
-// output row `row`; both may lie outside the matrix.
+// Epi: bool outside(row, col) const -- nothing at or beyond (row, col) belongs to the matrix
+//      void load(row, col, Loads&) const -- starts reading what the elements (row, col .. col+7) need
+//      void operator()(row, col, float (&v)[8], const Loads&) const -- finishes them
+// Rows and columns may lie outside the matrix.
 template <int AMAJ, int BMAJ, bool F16, bool SYM, class Epi>
 __global__ void __launch_bounds__(kDenseThreads, 1)
 dense_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const DenseShape g,
@@ -221,6 +223,10 @@ dense_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
                 const int n0 = nt * kDenseBN + half * (kDenseBN / 2) + c;
                 if (SYM && n0 > m0) break;            // above the diagonal: another chunk's mirror image
                 if (epi.outside(m0, n0)) break;
+                // what the epilogue reads is on its way while the accumulator is fetched and turned
+                typename Epi::Loads ahead[4];
+#pragma unroll
+                for (int it = 0; it < 4; ++it) epi.load(m0 + it * 8 + (lane >> 2), n0 + (lane & 3) * 8, ahead[it]);
                 uint32_t v[32];
                 umma::tmem_ld32(tmem + acc * kDenseBN + (uint32_t(q * 32) << 16) + half * (kDenseBN / 2) + c, v);
                 umma::tmem_ld_wait();
@@ -238,9 +244,11 @@ dense_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
                     const uint4 hi = ptx::lds128(sw + r * 128 + (((j + 1) ^ (r & 7)) << 4));
                     float w[8] = {__uint_as_float(lo.x), __uint_as_float(lo.y), __uint_as_float(lo.z), __uint_as_float(lo.w),
                                   __uint_as_float(hi.x), __uint_as_float(hi.y), __uint_as_float(hi.z), __uint_as_float(hi.w)};
-                    epi(m0 + r, n0 + j * 4, w);
+                    epi(m0 + r, n0 + j * 4, w, ahead[it]);
                 }
                 if (SYM && n0 < m0) {
+#pragma unroll
+                    for (int it = 0; it < 4; ++it) epi.load(int64_t(n0) + it * 8 + (lane >> 2), int(m0) + (lane & 3) * 8, ahead[it]);
 #pragma unroll
                     for (int it = 0; it < 4; ++it) {
                         const int col = it * 8 + (lane >> 2), r0 = (lane & 3) * 8;
@@ -252,7 +260,7 @@ dense_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
                                          : "r"(sw + (r0 + i) * 128 + (((col >> 2) ^ i) << 4) + (col & 3) * 4));
                             w[i] = __uint_as_float(u);
                         }
-                        epi(int64_t(n0) + col, int(m0) + r0, w);
+                        epi(int64_t(n0) + col, int(m0) + r0, w, ahead[it]);
                     }
                 }
             }
@@ -369,6 +377,8 @@ dense_split_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
             const int64_t m = int64_t(ct) * BN + u / 16;
             const int n = rt * kDenseTileM + (u % 16) * 8;
             if (epi.outside(m, n)) continue;
+            typename Epi::Loads ahead;
+            epi.load(m, n, ahead);
             float w[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
             const uint32_t at = base + ((u / 16) * 128 + (u % 16) * 8) * 4;
             for (uint32_t s = 0; s < splits; ++s) {
@@ -377,7 +387,7 @@ dense_split_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
                 w[0] += a.x; w[1] += a.y; w[2] += a.z; w[3] += a.w;
                 w[4] += b.x; w[5] += b.y; w[6] += b.z; w[7] += b.w;
             }
-            epi(m, n, w);
+            epi(m, n, w, ahead);
         }
     }
     if (timed_out && status) atomicOr(status, TPPO_DEV_WAIT_TIMEOUT);
@@ -450,12 +460,16 @@ int dense_split(const DenseOperand& a, const DenseOperand& b, int64_t m, int64_t
     return TPPO_OK;
 }
 
-// How many CTAs share one tile's contraction: enough to fill the SMs (two CTAs fit on one), with at
-// least four k steps left to each so that its ring gets going.
+// How many CTAs share one tile's contraction: the number that leaves the fewest k steps (and four steps'
+// worth of start and end per CTA) to the busiest SM, with at least two steps for each CTA.
 inline int dense_splits(int64_t tiles, int64_t k_steps) {
-    int s = 1;
-    while (s < 8 && tiles * s * 2 <= 2 * kNumSms && k_steps >= 4 * s * 2) s *= 2;
-    return s;
+    int best = 1;
+    int64_t least = INT64_MAX;
+    for (int s = 1; s <= 8 && (s == 1 || k_steps >= 2 * s); ++s) {
+        const int64_t cost = (tiles * s + kNumSms - 1) / kNumSms * ((k_steps + s - 1) / s + 4);
+        if (cost < least) { least = cost; best = s; }
+    }
+    return best;
 }
 
 // D[m, n] by whichever kernel suits its number of tiles: the persistent one when its 128 x 256 tiles

@@ -18,38 +18,64 @@
 namespace tppo {
 namespace {
 
-__device__ __forceinline__ float act_value(float z, int act) {
+// Activation and slope.  1 / (1 + exp(-t)) is formed with the fast division (2 ulp; it returns 0 where
+// the denominator passes 2^126, which is the limit there).
+__device__ __forceinline__ float sigmoid(float t) { return __fdividef(1.f, 1.f + expf(-t)); }
+
+template <int ACT>
+__device__ __forceinline__ float act_value(float z) {
+    if constexpr (ACT == TPPO_ACT_RELU) return fmaxf(z, 0.f);
+    if constexpr (ACT == TPPO_ACT_GELU) return 0.5f * z * (1.f + erff(z * 0.70710678118654752f));
+    if constexpr (ACT == TPPO_ACT_GELU_TANH)          // 0.5 (1 + tanh u) = sigmoid(2u)
+        return z * sigmoid(1.59576912160573071f * fmaf(0.044715f * z * z, z, z));
+    if constexpr (ACT == TPPO_ACT_SILU) return z * sigmoid(z);
+    return z;
+}
+template <int ACT>
+__device__ __forceinline__ float act_slope(float z) {
+    if constexpr (ACT == TPPO_ACT_RELU) return z > 0.f ? 1.f : 0.f;
+    if constexpr (ACT == TPPO_ACT_GELU)
+        return 0.5f * (1.f + erff(z * 0.70710678118654752f)) + z * expf(-0.5f * z * z) * 0.39894228040143268f;
+    if constexpr (ACT == TPPO_ACT_GELU_TANH) {
+        const float z2 = z * z, p = sigmoid(1.59576912160573071f * fmaf(0.044715f * z2, z, z));
+        // where p has reached 0 or 1 the second term is 0 (z^3 may overflow there)
+        const float q = p * (1.f - p);
+        return q == 0.f ? p : fmaf(z * q, 1.59576912160573071f * fmaf(3.f * 0.044715f, z2, 1.f), p);
+    }
+    if constexpr (ACT == TPPO_ACT_SILU) {
+        const float p = sigmoid(z), q = p * (1.f - p);
+        return q == 0.f ? p : fmaf(z, q, p);
+    }
+    return 1.f;
+}
+template <int ACT>
+__device__ __forceinline__ void act_values(const float (&z)[8], float (&o)[8]) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) o[i] = act_value<ACT>(z[i]);
+}
+template <int ACT>
+__device__ __forceinline__ void act_slopes(const float (&z)[8], float (&o)[8]) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) o[i] = act_slope<ACT>(z[i]);
+}
+// One (uniform) branch per eight elements: inside the loop it would cost more than the arithmetic, and
+// the eight chains of arithmetic would not overlap.
+__device__ __forceinline__ void act_values(int act, const float (&z)[8], float (&o)[8]) {
     switch (act) {
-        case TPPO_ACT_RELU: return fmaxf(z, 0.f);
-        case TPPO_ACT_GELU: return 0.5f * z * (1.f + erff(z * 0.70710678118654752f));
-        case TPPO_ACT_GELU_TANH: {
-            // 0.5 (1 + tanh u) = 1 / (1 + exp(-2u))
-            const float u = 0.79788456080286536f * fmaf(0.044715f * z * z, z, z);
-            return z / (1.f + expf(-2.f * u));
-        }
-        case TPPO_ACT_SILU: return z / (1.f + expf(-z));
-        default: return z;
+        case TPPO_ACT_RELU: act_values<TPPO_ACT_RELU>(z, o); break;
+        case TPPO_ACT_GELU: act_values<TPPO_ACT_GELU>(z, o); break;
+        case TPPO_ACT_GELU_TANH: act_values<TPPO_ACT_GELU_TANH>(z, o); break;
+        case TPPO_ACT_SILU: act_values<TPPO_ACT_SILU>(z, o); break;
+        default: act_values<TPPO_ACT_NONE>(z, o);
     }
 }
-__device__ __forceinline__ float act_slope(float z, int act) {
+__device__ __forceinline__ void act_slopes(int act, const float (&z)[8], float (&o)[8]) {
     switch (act) {
-        case TPPO_ACT_RELU: return z > 0.f ? 1.f : 0.f;
-        case TPPO_ACT_GELU:
-            return 0.5f * (1.f + erff(z * 0.70710678118654752f)) + z * expf(-0.5f * z * z) * 0.39894228040143268f;
-        case TPPO_ACT_GELU_TANH: {
-            const float z2 = z * z;
-            const float u = 0.79788456080286536f * fmaf(0.044715f * z2, z, z);
-            const float p = 1.f / (1.f + expf(-2.f * u));           // 0.5 (1 + tanh u)
-            // where p has reached 0 or 1 the second term is 0 (z^3 may overflow there)
-            const float q = p * (1.f - p);
-            return q == 0.f ? p : fmaf(2.f * z * q, 0.79788456080286536f * fmaf(3.f * 0.044715f, z2, 1.f), p);
-        }
-        case TPPO_ACT_SILU: {
-            const float p = 1.f / (1.f + expf(-z));
-            const float q = p * (1.f - p);
-            return q == 0.f ? p : fmaf(z, q, p);
-        }
-        default: return 1.f;
+        case TPPO_ACT_RELU: act_slopes<TPPO_ACT_RELU>(z, o); break;
+        case TPPO_ACT_GELU: act_slopes<TPPO_ACT_GELU>(z, o); break;
+        case TPPO_ACT_GELU_TANH: act_slopes<TPPO_ACT_GELU_TANH>(z, o); break;
+        case TPPO_ACT_SILU: act_slopes<TPPO_ACT_SILU>(z, o); break;
+        default: act_slopes<TPPO_ACT_NONE>(z, o);
     }
 }
 
@@ -73,6 +99,11 @@ __device__ __forceinline__ void get8(const T* p, float (&v)[8], int count, bool 
     for (int i = 0; i < 8; ++i) v[i] = i < count ? load_f32(p + i) : 0.f;
 }
 
+__device__ __forceinline__ void widen8(const uint4& w, float (&v)[8]) {
+    v[0] = bf16_lo(w.x); v[1] = bf16_hi(w.x); v[2] = bf16_lo(w.y); v[3] = bf16_hi(w.y);
+    v[4] = bf16_lo(w.z); v[5] = bf16_hi(w.z); v[6] = bf16_lo(w.w); v[7] = bf16_hi(w.w);
+}
+
 // Forward epilogue.
 struct EpiLinear {
     const void* bias; int32_t bias_f32;
@@ -83,12 +114,16 @@ struct EpiLinear {
     int32_t vec_y, vec_r, vec_p, vec_b;
     int32_t* status;
 
+    struct Loads { uint4 r; };                    // the residual, where one 16-byte load fetches it
+
     __device__ __forceinline__ bool outside(int64_t m, int n) const { return m >= M || n >= N; }
-    __device__ __forceinline__ void operator()(int64_t m, int n, float (&v)[8]) const {
+    __device__ __forceinline__ bool fast(int64_t m, int n) const { return residual && vec_r && m < M && n + 8 <= N; }
+    __device__ __forceinline__ void load(int64_t m, int n, Loads& l) const {
+        if (fast(m, n)) l.r = *reinterpret_cast<const uint4*>(residual + m * ldr + n);
+    }
+    __device__ __forceinline__ void operator()(int64_t m, int n, float (&v)[8], const Loads& l) const {
         if (outside(m, n)) return;
         const int count = min(8, N - n);
-        float r[8];
-        if (residual) get8(residual + m * ldr + n, r, count, vec_r);
         if (bias) {
             float b[8];
             if (bias_f32) get8(static_cast<const float*>(bias) + n, b, count, vec_b);
@@ -96,24 +131,34 @@ struct EpiLinear {
 #pragma unroll
             for (int i = 0; i < 8; ++i) v[i] += b[i];
         }
-        // z and y that are not finite, or leave the range of the type they are stored in, are written 0
-        bool bad = false;
-        float z[8];
+        float o[8];
+        act_values(act, v, o);
+        if (residual) {
+            float r[8];
+            if (fast(m, n)) widen8(l.r, r);
+            else get8(residual + m * ldr + n, r, count, false);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const float top = y_f32 ? kFltMax : kBf16Max;
-            z[i] = v[i];
-            float o = act_value(v[i], act);
-            if (residual) o += r[i];
-            const bool zok = fabsf(z[i]) <= (pre ? kBf16Max : kFltMax), ok = zok && fabsf(o) <= top;
-            if (!zok) z[i] = 0.f;
-            v[i] = ok ? o : 0.f;
-            bad |= !ok && i < count;
+            for (int i = 0; i < 8; ++i) o[i] += r[i];
         }
-        if (bad && status) atomicOr(status, TPPO_DEV_NONFINITE);
-        if (pre) put8(pre + m * ldp + n, z, count, vec_p);
-        if (y_f32) put8(static_cast<float*>(y) + m * ldy + n, v, count, vec_y);
-        else put8(static_cast<bf16_bits*>(y) + m * ldy + n, v, count, vec_y);
+        // z and y that are not finite, or leave the range of the type they are stored in, are written 0
+        const float top = y_f32 ? kFltMax : kBf16Max, ztop = pre ? kBf16Max : kFltMax;
+        float worst = 0.f;                        // a NaN is carried along by the comparison's form
+#pragma unroll
+        for (int i = 0; i < 8; ++i) worst = fabsf(o[i]) <= top && fabsf(v[i]) <= ztop ? worst : 1.f;
+        if (worst != 0.f) {
+            bool bad = false;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const bool zok = fabsf(v[i]) <= ztop, ok = zok && fabsf(o[i]) <= top;
+                if (!zok) v[i] = 0.f;
+                if (!ok) o[i] = 0.f;
+                bad |= !ok && i < count;
+            }
+            if (bad && status) atomicOr(status, TPPO_DEV_NONFINITE);
+        }
+        if (pre) put8(pre + m * ldp + n, v, count, vec_p);
+        if (y_f32) put8(static_cast<float*>(y) + m * ldy + n, o, count, vec_y);
+        else put8(static_cast<bf16_bits*>(y) + m * ldy + n, o, count, vec_y);
     }
 };
 
@@ -121,8 +166,10 @@ struct EpiLinear {
 struct EpiStore {
     bf16_bits* out; int64_t ld; int64_t M; int32_t N; int32_t vec;
     int32_t* status;
+    struct Loads {};
     __device__ __forceinline__ bool outside(int64_t m, int n) const { return m >= M || n >= N; }
-    __device__ __forceinline__ void operator()(int64_t m, int n, float (&v)[8]) const {
+    __device__ __forceinline__ void load(int64_t, int, Loads&) const {}
+    __device__ __forceinline__ void operator()(int64_t m, int n, float (&v)[8], const Loads&) const {
         if (outside(m, n)) return;
         const int count = min(8, N - n);
         bool bad = false;
@@ -158,7 +205,8 @@ struct DzArgs {
 };
 
 // dz and the column sums behind dbias.  A block covers 256 columns (8 per thread, 32 threads) and every
-// (8 gridDim.y)-th row from its first; its eight warps' sums are added in warp order.
+// (8 gridDim.y)-th row from its first, two rows per trip so that four loads are in flight; its eight
+// warps' sums are added in warp order.
 template <class T>
 __global__ void __launch_bounds__(256) linear_dz_kernel(const DzArgs a) {
     __shared__ float sums[8][256 + 8];
@@ -167,22 +215,37 @@ __global__ void __launch_bounds__(256) linear_dz_kernel(const DzArgs a) {
     const int count = min(8, a.N - n);
     float acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
     bool bad = false;
+    const T* dy = static_cast<const T*>(a.dy);
     if (count > 0) {
-        for (int64_t m = int64_t(blockIdx.y) * 8 + warp; m < a.M; m += int64_t(gridDim.y) * 8) {
-            float d[8];
-            get8(static_cast<const T*>(a.dy) + m * a.lddy + n, d, count, a.vec_dy);
-            if (a.act != TPPO_ACT_NONE) {
-                float z[8];
-                get8(a.pre + m * a.ldp + n, z, count, a.vec_p);
+        const int64_t step = int64_t(gridDim.y) * 8;
+        for (int64_t m0 = int64_t(blockIdx.y) * 8 + warp; m0 < a.M; m0 += 2 * step) {
+            float d[2][8], z[2][8];
 #pragma unroll
-                for (int i = 0; i < 8; ++i) d[i] *= act_slope(z[i], a.act);
+            for (int k = 0; k < 2; ++k) {
+                const int64_t m = m0 + k * step;
+                if (m < a.M) {
+                    get8(dy + m * a.lddy + n, d[k], count, a.vec_dy);
+                    if (a.act != TPPO_ACT_NONE) get8(a.pre + m * a.ldp + n, z[k], count, a.vec_p);
+                }
             }
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                if (!(fabsf(d[i]) <= kBf16Max)) { bad = true; d[i] = 0.f; }
-                acc[i] += d[i];
+            for (int k = 0; k < 2; ++k) {
+                const int64_t m = m0 + k * step;
+                if (m < a.M) {
+                    if (a.act != TPPO_ACT_NONE) {
+                        float slope[8];
+                        act_slopes(a.act, z[k], slope);
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) d[k][i] *= slope[i];
+                    }
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        if (!(fabsf(d[k][i]) <= kBf16Max)) { bad = true; d[k][i] = 0.f; }
+                        acc[i] += d[k][i];
+                    }
+                    if (a.dz) store_vec<8>(a.dz + m * a.ldz + n, d[k]);
+                }
             }
-            if (a.dz) store_vec<8>(a.dz + m * a.ldz + n, d);
         }
     }
     if (bad && a.status) atomicOr(a.status, TPPO_DEV_NONFINITE);
@@ -199,14 +262,26 @@ __global__ void __launch_bounds__(256) linear_dz_kernel(const DzArgs a) {
     }
 }
 
+// dbias: the partial rows in ascending order within each of a column's 16 strands, then the strands.
 template <class T>
-__global__ void __launch_bounds__(256) linear_dbias_kernel(const float* partial, int32_t parts, int32_t N, T* dbias) {
-    const int c = blockIdx.x * 256 + threadIdx.x;
+__global__ void __launch_bounds__(512) linear_dbias_kernel(const float* partial, int32_t parts, int32_t N, T* dbias) {
+    __shared__ double s[16][33];
+    const int lane = threadIdx.x & 31, strand = threadIdx.x >> 5;
+    const int64_t c = int64_t(blockIdx.x) * 32 + lane;
     pdl_wait();
-    if (c >= N) return;
     double t = 0.0;
-    for (int p = 0; p < parts; ++p) t += double(partial[int64_t(p) * N + c]);
-    store_f32(dbias + c, float(t));
+    if (c < N) {
+#pragma unroll 4
+        for (int p = strand; p < parts; p += 16) t += double(partial[int64_t(p) * N + c]);
+    }
+    s[strand][lane] = t;
+    __syncthreads();
+    if (strand == 0 && c < N) {
+        t = 0.0;
+#pragma unroll
+        for (int k = 0; k < 16; ++k) t += s[k][lane];
+        store_f32(dbias + c, float(t));
+    }
 }
 
 int64_t pad8(int64_t n) { return (n + 7) / 8 * 8; }
@@ -341,12 +416,12 @@ TPPO_API int tppo_linear_bwd(const void* dy, int32_t dy_dtype, int64_t lddy, con
         TPPO_CUDA_CHECK(cudaGetLastError());
         if (make_dz) { Z.p = w.dz; Z.ld = a.ldz; }
         if (dbias) {
-            const dim3 grid((N + 255) / 256);
+            const dim3 grid((N + 31) / 32);
             if (bias_dtype == TPPO_F32)
-                TPPO_CUDA_CHECK(launch_dense(linear_dbias_kernel<float>, grid, dim3(256), 0, s, true,
+                TPPO_CUDA_CHECK(launch_dense(linear_dbias_kernel<float>, grid, dim3(512), 0, s, true,
                                              static_cast<const float*>(w.partial), int32_t(gy), N, static_cast<float*>(dbias)));
             else
-                TPPO_CUDA_CHECK(launch_dense(linear_dbias_kernel<bf16_bits>, grid, dim3(256), 0, s, true,
+                TPPO_CUDA_CHECK(launch_dense(linear_dbias_kernel<bf16_bits>, grid, dim3(512), 0, s, true,
                                              static_cast<const float*>(w.partial), int32_t(gy), N, static_cast<bf16_bits*>(dbias)));
         }
     }

@@ -55,8 +55,7 @@ __device__ __forceinline__ void store_operand(f16_bits* p, const float (&v)[8]) 
         make_uint4(pack_f16x2(v[0] * kScale, v[1] * kScale), pack_f16x2(v[2] * kScale, v[3] * kScale),
                    pack_f16x2(v[4] * kScale, v[5] * kScale), pack_f16x2(v[6] * kScale, v[7] * kScale));
 }
-__device__ __forceinline__ void load_operand(const f16_bits* p, float (&v)[8]) {
-    const uint4 w = *reinterpret_cast<const uint4*>(p);
+__device__ __forceinline__ void widen_operand(const uint4& w, float (&v)[8]) {
     const float2 a = unpack_f16x2(w.x), b = unpack_f16x2(w.y), c = unpack_f16x2(w.z), d = unpack_f16x2(w.w);
     v[0] = a.x * kUnscale; v[1] = a.y * kUnscale; v[2] = b.x * kUnscale; v[3] = b.y * kUnscale;
     v[4] = c.x * kUnscale; v[5] = c.y * kUnscale; v[6] = d.x * kUnscale; v[7] = d.y * kUnscale;
@@ -155,8 +154,10 @@ __global__ void __launch_bounds__(kMuonThreads) muon_normalise_kernel(const doub
 // A = X X^T.  With `diag` its diagonal goes there and the stored operand has zeros instead.
 struct EpiA {
     f16_bits* out; int64_t ld; int32_t m; float* diag;
+    struct Loads {};
+    __device__ __forceinline__ void load(int64_t, int, Loads&) const {}
     __device__ __forceinline__ bool outside(int64_t r, int c) const { return r >= m || c >= m; }
-    __device__ __forceinline__ void operator()(int64_t r, int c, float (&v)[8]) const {
+    __device__ __forceinline__ void operator()(int64_t r, int c, float (&v)[8], const Loads&) const {
         if (outside(r, c)) return;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
@@ -170,11 +171,15 @@ struct EpiA {
 // B = b A + c A^2, from the accumulated square of the stored A.
 struct EpiB {
     const f16_bits* a; f16_bits* out; int64_t ld; int32_t m; const float* diag_a; float* diag_b;
+    struct Loads { uint4 a; };
+    __device__ __forceinline__ void load(int64_t r, int c, Loads& l) const {
+        if (!outside(r, c)) l.a = *reinterpret_cast<const uint4*>(a + r * ld + c);
+    }
     __device__ __forceinline__ bool outside(int64_t r, int c) const { return r >= m || c >= m; }
-    __device__ __forceinline__ void operator()(int64_t r, int c, float (&v)[8]) const {
+    __device__ __forceinline__ void operator()(int64_t r, int c, float (&v)[8], const Loads& l) const {
         if (outside(r, c)) return;
         float o[8];
-        load_operand(a + r * ld + c, o);
+        widen_operand(l.a, o);
         const float dr = diag_a ? diag_a[r] : 0.f;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
@@ -199,11 +204,17 @@ struct EpiX {
     const float* diag_b;
     bf16_bits* update; int64_t ldu; int32_t vec_u; float scale;
     int64_t R; int32_t C;
+    struct Loads { float4 lo, hi; };
     __device__ __forceinline__ bool outside(int64_t r, int c) const { return r >= R || c >= C; }
-    __device__ __forceinline__ void operator()(int64_t r, int c, float (&v)[8]) const {
+    __device__ __forceinline__ void load(int64_t r, int c, Loads& l) const {
         if (outside(r, c)) return;
-        float x[8];
-        load_vec<8>(x32 + r * ldx + c, x);
+        const float4* p = reinterpret_cast<const float4*>(x32 + r * ldx + c);
+        l.lo = p[0];
+        l.hi = p[1];
+    }
+    __device__ __forceinline__ void operator()(int64_t r, int c, float (&v)[8], const Loads& l) const {
+        if (outside(r, c)) return;
+        const float x[8] = {l.lo.x, l.lo.y, l.lo.z, l.lo.w, l.hi.x, l.hi.y, l.hi.z, l.hi.w};
         const float norm = inverse ? *inverse : 1.f;
         const float row = !RIGHT && diag_b ? diag_b[r] : 0.f;
 #pragma unroll
