@@ -81,12 +81,11 @@ inline bool is_finite_host(float v) { return v - v == 0.f; }
 __device__ __forceinline__ void pdl_launch() { asm volatile("griddepcontrol.launch_dependents;"); }
 __device__ __forceinline__ void pdl_wait() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 
-// Launches `kernel` on `s`; with `dependent` its blocks may start while the previous kernel of the
-// stream still runs, so the kernel must call pdl_wait() before it touches that kernel's results --
-// or any memory that the work in front of it may still use.
-template <class... Args>
-cudaError_t launch_dense(void (*kernel)(Args...), dim3 grid, dim3 block, size_t smem, cudaStream_t s,
-                         bool dependent, Args... args) {
+// Launches `kernel` on `s` as a programmatic dependent of whatever precedes it there: its blocks may
+// start while that still runs, so every kernel launched this way calls pdl_wait() before it touches
+// global memory.
+template <class... Params, class... Args>
+cudaError_t launch_dense(void (*kernel)(Params...), dim3 grid, dim3 block, size_t smem, cudaStream_t s, const Args&... args) {
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = grid;
     cfg.blockDim = block;
@@ -96,8 +95,8 @@ cudaError_t launch_dense(void (*kernel)(Args...), dim3 grid, dim3 block, size_t 
     attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr.val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = &attr;
-    cfg.numAttrs = dependent ? 1 : 0;
-    return cudaLaunchKernelEx(&cfg, kernel, args...);
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, kernel, Params(args)...);
 }
 
 }  // namespace tppo

@@ -335,6 +335,20 @@ dense_split_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
     pdl_launch();
     pdl_wait();
 
+    // each CTA finishes its share of the (output row, eight output columns) units; what the epilogue of a
+    // thread's first units reads is fetched while the product runs
+    const int units = BN * 16, per = (units + int(splits) - 1) / int(splits);
+    const int u0 = int(rank) * per + int(threadIdx.x) - 64, last = min(int(rank) * per + per, units);
+    constexpr int kAhead = BN >= 64 ? 4 : BN / 16;
+    typename Epi::Loads ahead[kAhead];
+    if (warp >= 2) {
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+            const int u = u0 + i * (kDenseThreads - 64);
+            if (u < last) epi.load(int64_t(ct) * BN + u / 16, rt * kDenseTileM + (u % 16) * 8, ahead[i]);
+        }
+    }
+
     bool timed_out = false;
     if (warp == 0) {
         if (lane == 0) {
@@ -370,15 +384,10 @@ dense_split_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
     }
     ptx::cluster_sync_all();
     if (warp >= 2) {
-        // each CTA finishes its share of the (output row, eight output columns) units
-        const int units = BN * 16, per = (units + int(splits) - 1) / int(splits);
-        const int first = int(rank) * per, last = min(first + per, units);
-        for (int u = first + int(threadIdx.x) - 64; u < last; u += kDenseThreads - 64) {
+        auto finish = [&](int u, const typename Epi::Loads& l) {
             const int64_t m = int64_t(ct) * BN + u / 16;
             const int n = rt * kDenseTileM + (u % 16) * 8;
-            if (epi.outside(m, n)) continue;
-            typename Epi::Loads ahead;
-            epi.load(m, n, ahead);
+            if (epi.outside(m, n)) return;
             float w[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
             const uint32_t at = base + ((u / 16) * 128 + (u % 16) * 8) * 4;
             for (uint32_t s = 0; s < splits; ++s) {
@@ -387,7 +396,15 @@ dense_split_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
                 w[0] += a.x; w[1] += a.y; w[2] += a.z; w[3] += a.w;
                 w[4] += b.x; w[5] += b.y; w[6] += b.z; w[7] += b.w;
             }
-            epi(m, n, w, ahead);
+            epi(m, n, w, l);
+        };
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i)
+            if (u0 + i * (kDenseThreads - 64) < last) finish(u0 + i * (kDenseThreads - 64), ahead[i]);
+        for (int u = u0 + kAhead * (kDenseThreads - 64); u < last; u += kDenseThreads - 64) {
+            typename Epi::Loads l;
+            epi.load(int64_t(ct) * BN + u / 16, rt * kDenseTileM + (u % 16) * 8, l);
+            finish(u, l);
         }
     }
     if (timed_out && status) atomicOr(status, TPPO_DEV_WAIT_TIMEOUT);
@@ -404,7 +421,7 @@ struct DenseOperand { const void* p; int64_t rows, cols, ld; };
 // D[m, n] = sum_k A(m, k) B(k, n).  AMAJ 0: a is [m, k]; 1: a is [k, m].  BMAJ 0: b is [n, k]; 1: b is [k, n].
 template <int AMAJ, int BMAJ, bool F16, bool SYM, class Epi>
 int dense_gemm(const DenseOperand& a, const DenseOperand& b, int64_t m, int64_t n, int64_t k, const Epi& epi,
-               int32_t* status, bool dependent, cudaStream_t s) {
+               int32_t* status, cudaStream_t s) {
     CUtensorMap ma, mb;
     if (!make_bf16_tensor_map(&ma, a.p, a.rows, a.cols, a.ld, AMAJ ? 64 : kDenseTileM) ||
         !make_bf16_tensor_map(&mb, b.p, b.rows, b.cols, b.ld, BMAJ ? 64 : kDenseBN))
@@ -421,7 +438,7 @@ int dense_gemm(const DenseOperand& a, const DenseOperand& b, int64_t m, int64_t 
     auto kernel = dense_gemm_kernel<AMAJ, BMAJ, F16, SYM, Epi>;
     TPPO_CUDA_CHECK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, int(kDenseSmem)));
     const int grid = g.total < kNumSms ? g.total : kNumSms;
-    TPPO_CUDA_CHECK(launch_dense(kernel, dim3(grid), dim3(kDenseThreads), kDenseSmem, s, dependent, ma, mb, g, epi, status));
+    TPPO_CUDA_CHECK(launch_dense(kernel, dim3(grid), dim3(kDenseThreads), kDenseSmem, s, ma, mb, g, epi, status));
     return TPPO_OK;
 }
 
@@ -430,7 +447,7 @@ int dense_gemm(const DenseOperand& a, const DenseOperand& b, int64_t m, int64_t 
 // BMAJ 0: b is [m, k]; 1: b is [k, m].
 template <int AMAJ, int BMAJ, bool F16, int BN, class Epi>
 int dense_split(const DenseOperand& a, const DenseOperand& b, int64_t m, int64_t n, int64_t k, int splits, const Epi& epi,
-                int32_t* status, bool dependent, cudaStream_t s) {
+                int32_t* status, cudaStream_t s) {
     CUtensorMap ma, mb;
     if (!make_bf16_tensor_map(&ma, a.p, a.rows, a.cols, a.ld, AMAJ ? 64 : kDenseTileM) ||
         !make_bf16_tensor_map(&mb, b.p, b.rows, b.cols, b.ld, BMAJ ? 64 : BN))
@@ -455,7 +472,7 @@ int dense_split(const DenseOperand& a, const DenseOperand& b, int64_t m, int64_t
     attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[1].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
-    cfg.numAttrs = dependent ? 2 : 1;
+    cfg.numAttrs = 2;
     TPPO_CUDA_CHECK(cudaLaunchKernelEx(&cfg, kernel, ma, mb, g, epi, status));
     return TPPO_OK;
 }
@@ -477,18 +494,18 @@ inline int dense_splits(int64_t tiles, int64_t k_steps) {
 // one indexed by n (QMAJ 0: [n, k], 1: [k, n]).  SYM: D is symmetric (m = n).
 template <int PMAJ, int QMAJ, bool F16, bool SYM, class Epi>
 int dense_product(const DenseOperand& P, const DenseOperand& Q, int64_t m, int64_t n, int64_t k, const Epi& epi,
-                  int32_t* status, bool dependent, cudaStream_t s) {
+                  int32_t* status, cudaStream_t s) {
     const int64_t mt = (m + 127) / 128, nt = (n + 255) / 256;
     const int64_t big = SYM ? mt / 2 * (mt / 2 + 1) + (mt % 2 ? mt / 2 + 1 : 0) : mt * nt;
-    if (big >= kNumSms) return dense_gemm<PMAJ, QMAJ, F16, SYM>(P, Q, m, n, k, epi, status, dependent, s);
+    if (big >= kNumSms) return dense_gemm<PMAJ, QMAJ, F16, SYM>(P, Q, m, n, k, epi, status, s);
     const int64_t ks = (k + 63) / 64, rows = (n + 127) / 128;
     // one operand box of 64 outer indices is the least an MN-major operand can be loaded in
     constexpr int B16 = PMAJ ? 64 : 16, B32 = PMAJ ? 64 : 32;
-    if (m <= 16 && !PMAJ) return dense_split<QMAJ, PMAJ, F16, B16>(Q, P, m, n, k, dense_splits(rows, ks), epi, status, dependent, s);
-    if (m <= 32 && !PMAJ) return dense_split<QMAJ, PMAJ, F16, B32>(Q, P, m, n, k, dense_splits(rows, ks), epi, status, dependent, s);
+    if (m <= 16 && !PMAJ) return dense_split<QMAJ, PMAJ, F16, B16>(Q, P, m, n, k, dense_splits(rows, ks), epi, status, s);
+    if (m <= 32 && !PMAJ) return dense_split<QMAJ, PMAJ, F16, B32>(Q, P, m, n, k, dense_splits(rows, ks), epi, status, s);
     const int64_t by64 = rows * ((m + 63) / 64);
-    if (by64 <= kNumSms) return dense_split<QMAJ, PMAJ, F16, 64>(Q, P, m, n, k, dense_splits(by64, ks), epi, status, dependent, s);
-    return dense_split<QMAJ, PMAJ, F16, 128>(Q, P, m, n, k, dense_splits(rows * ((m + 127) / 128), ks), epi, status, dependent, s);
+    if (by64 <= kNumSms) return dense_split<QMAJ, PMAJ, F16, 64>(Q, P, m, n, k, dense_splits(by64, ks), epi, status, s);
+    return dense_split<QMAJ, PMAJ, F16, 128>(Q, P, m, n, k, dense_splits(rows * ((m + 127) / 128), ks), epi, status, s);
 }
 
 }  // namespace tppo

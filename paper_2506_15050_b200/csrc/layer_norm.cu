@@ -68,6 +68,8 @@ __device__ __forceinline__ float group_sum(float v, int group, float* red) {
 template <class T, class P, int VEC, int CH>
 __global__ void __launch_bounds__(kNormMaxThreads) norm_fwd_kernel(const NormFwdArgs a) {
     __shared__ float red[32];
+    pdl_launch();
+    pdl_wait();
     const int t = threadIdx.x % a.group;
     const int64_t r = int64_t(blockIdx.x) * (blockDim.x / a.group) + threadIdx.x / a.group;
     const bool have = r < a.M;                    // the last block may hold fewer rows than warps
@@ -140,6 +142,8 @@ __global__ void __launch_bounds__(kNormMaxThreads) norm_fwd_kernel(const NormFwd
 template <class T, class P>
 __global__ void __launch_bounds__(kNormMaxThreads) norm_fwd_long_kernel(const NormFwdArgs a) {
     __shared__ float red[32];
+    pdl_launch();
+    pdl_wait();
     const int64_t r = blockIdx.x;
     const T* x = static_cast<const T*>(a.x) + r * a.ldx;
     float s = 0.f;
@@ -300,6 +304,8 @@ __global__ void __launch_bounds__(512) norm_bwd_kernel(const NormBwdArgs a) {
     constexpr int VALUES = 2 * ROWS;
     extern __shared__ float cols[];
     __shared__ float red[2][16][VALUES];
+    pdl_launch();
+    pdl_wait();
     const int t = threadIdx.x % a.group, grp = threadIdx.x / a.group, groups = blockDim.x / a.group;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, per = a.group >> 5, first = warp / per * per;
     const float inv_n = 1.f / float(a.N);
@@ -383,6 +389,8 @@ __global__ void __launch_bounds__(CH * VEC > 16 ? 512 : 640) norm_bwd_ring_kerne
         ptx::bulk_load(at, static_cast<const T*>(a.x) + r * a.ldx, row_bytes, bar);
         ptx::bulk_load(at + row_bytes, static_cast<const T*>(a.dy) + r * a.lddy, row_bytes, bar);
     };
+    pdl_launch();
+    pdl_wait();
     if (t == 0) {
         for (int s = 0; s < a.stages; ++s) ptx::mbar_init(full + 8 * s, 1);
         ptx::fence_mbar_init_cluster();
@@ -435,6 +443,8 @@ __global__ void __launch_bounds__(CH * VEC > 16 ? 512 : 640) norm_bwd_ring_kerne
 template <class T, class P>
 __global__ void __launch_bounds__(kNormMaxThreads) norm_bwd_long_kernel(const NormBwdArgs a, float* row_flag) {
     __shared__ float red[32];
+    pdl_launch();
+    pdl_wait();
     const int64_t r = blockIdx.x;
     const T* x = static_cast<const T*>(a.x) + r * a.ldx;
     const T* dy = static_cast<const T*>(a.dy) + r * a.lddy;
@@ -461,6 +471,8 @@ __global__ void __launch_bounds__(kNormMaxThreads) norm_bwd_long_kernel(const No
 // Column sums of long rows: one thread per column, blockIdx.y takes every gridDim.y-th row.
 template <class T>
 __global__ void __launch_bounds__(256) norm_cols_kernel(const NormBwdArgs a, const float* row_flag) {
+    pdl_launch();
+    pdl_wait();
     const int c = blockIdx.x * 256 + threadIdx.x;
     if (c >= a.N) return;
     float dg = 0.f, db = 0.f;
@@ -482,6 +494,7 @@ template <class P>
 __global__ void __launch_bounds__(512) norm_sum_kernel(const float* partial, int32_t parts, int32_t N, P* dgamma,
                                                        P* dbeta) {
     __shared__ double s[16][33];
+    pdl_launch();
     pdl_wait();
     const int lane = threadIdx.x & 31, strand = threadIdx.x >> 5;
     const int64_t j = int64_t(blockIdx.x) * 32 + lane;           // column of the [2N]-wide partial row
@@ -527,16 +540,14 @@ int norm_fwd_typed(NormFwdArgs a, cudaStream_t s) {
     while (per > 1 && a.M * ((pieces + per - 1) / per) < int64_t(kNumSms) * 512 && pieces <= per / 2 * 512) per /= 2;
     if (pieces > per * kNormMaxThreads) per *= 2;
     if (pieces > per * kNormMaxThreads) {
-        norm_fwd_long_kernel<T, P><<<unsigned(a.M), kNormMaxThreads, 0, s>>>(a);
-        TPPO_CUDA_CHECK(cudaGetLastError());
+        TPPO_CUDA_CHECK(launch_dense(norm_fwd_long_kernel<T, P>, dim3(unsigned(a.M)), dim3(kNormMaxThreads), 0, s, a));
         return TPPO_OK;
     }
     a.group = int32_t((pieces + per * 32 - 1) / (per * 32) * 32);
     const int groups = a.group == 32 ? 4 : 1;
     const unsigned blocks = unsigned((a.M + groups - 1) / groups);
     const auto go = [&](auto vecs, auto ch) -> int {
-        norm_fwd_kernel<T, P, decltype(vecs)::value, decltype(ch)::value><<<blocks, a.group * groups, 0, s>>>(a);
-        TPPO_CUDA_CHECK(cudaGetLastError());
+        TPPO_CUDA_CHECK(launch_dense(norm_fwd_kernel<T, P, decltype(vecs)::value, decltype(ch)::value>, dim3(blocks), dim3(a.group * groups), 0, s, a));
         return TPPO_OK;
     };
     if (vec) return with_pieces<1, 2, 4, 8>(int(per), [&](auto ch) { return go(std::integral_constant<int, V>(), ch); });
@@ -579,8 +590,7 @@ int norm_bwd_typed(NormBwdArgs a, P* dgamma, P* dbeta, float* row_flag, cudaStre
             a.group = int32_t((pieces + CH * 32 - 1) / (CH * 32) * 32);
             auto kernel = norm_bwd_ring_kernel<T, P, V, CH>;
             TPPO_CUDA_CHECK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, int(smem)));
-            kernel<<<unsigned(parts), a.group, smem, s>>>(a);
-            TPPO_CUDA_CHECK(cudaGetLastError());
+            TPPO_CUDA_CHECK(launch_dense(kernel, dim3(unsigned(parts)), dim3(a.group), smem, s, a));
             return TPPO_OK;
         };
         if constexpr (V == 8) rc = pieces > 2 * 512 ? go(std::integral_constant<int, 4>()) : with_pieces<1, 2>(need > 2 ? 2 : need, go);
@@ -605,8 +615,7 @@ int norm_bwd_typed(NormBwdArgs a, P* dgamma, P* dbeta, float* row_flag, cudaStre
             constexpr int VEC = decltype(vecs)::value, CH = decltype(ch)::value;
             // some sixteen elements of x and of dy in flight per thread and trip, at most four rows
             constexpr int ROWS = VEC * CH > 8 ? 1 : VEC * CH > 4 ? 2 : 4;
-            norm_bwd_kernel<T, P, VEC, CH, ROWS><<<unsigned(parts), a.group * groups, smem, s>>>(a);
-            TPPO_CUDA_CHECK(cudaGetLastError());
+            TPPO_CUDA_CHECK(launch_dense(norm_bwd_kernel<T, P, VEC, CH, ROWS>, dim3(unsigned(parts)), dim3(a.group * groups), smem, s, a));
             return TPPO_OK;
         };
         if (vec) rc = with_pieces<1, 2, 4>(need, [&](auto ch) -> int {
@@ -619,19 +628,16 @@ int norm_bwd_typed(NormBwdArgs a, P* dgamma, P* dbeta, float* row_flag, cudaStre
         NormBwdArgs b = a;
         if (a.partial) {
             b.dx = nullptr;
-            norm_bwd_long_kernel<T, P><<<unsigned(a.M), kNormMaxThreads, 0, s>>>(b, row_flag);
-            TPPO_CUDA_CHECK(cudaGetLastError());
+            TPPO_CUDA_CHECK(launch_dense(norm_bwd_long_kernel<T, P>, dim3(unsigned(a.M)), dim3(kNormMaxThreads), 0, s, b, row_flag));
             parts = int(a.M < 64 ? a.M : 64);
-            norm_cols_kernel<T><<<dim3((a.N + 255) / 256, parts), 256, 0, s>>>(a, row_flag);
-            TPPO_CUDA_CHECK(cudaGetLastError());
+            TPPO_CUDA_CHECK(launch_dense(norm_cols_kernel<T>, dim3(dim3((a.N + 255) / 256, parts)), dim3(256), 0, s, a, row_flag));
         }
         if (a.dx) {
-            norm_bwd_long_kernel<T, P><<<unsigned(a.M), kNormMaxThreads, 0, s>>>(a, nullptr);
-            TPPO_CUDA_CHECK(cudaGetLastError());
+            TPPO_CUDA_CHECK(launch_dense(norm_bwd_long_kernel<T, P>, dim3(unsigned(a.M)), dim3(kNormMaxThreads), 0, s, a, nullptr));
         }
     }
     if (rc != TPPO_OK || !a.partial) return rc;
-    TPPO_CUDA_CHECK(launch_dense(norm_sum_kernel<P>, dim3(unsigned((2 * int64_t(a.N) + 31) / 32)), dim3(512), 0, s, true,
+    TPPO_CUDA_CHECK(launch_dense(norm_sum_kernel<P>, dim3(unsigned((2 * int64_t(a.N) + 31) / 32)), dim3(512), 0, s,
                                  static_cast<const float*>(a.partial), int32_t(parts), a.N, dgamma, dbeta));
     return TPPO_OK;
 }

@@ -18,33 +18,60 @@
 namespace tppo {
 namespace {
 
-// Activation and slope.  1 / (1 + exp(-t)) is formed with the fast division (2 ulp; it returns 0 where
-// the denominator passes 2^126, which is the limit there).
-__device__ __forceinline__ float sigmoid(float t) { return __fdividef(1.f, 1.f + expf(-t)); }
+// Activations and slopes in a dozen instructions each: the backward pass evaluates one slope per six
+// bytes it moves, and with the library's expf, erff and division it is bound by them (247 us for
+// 16384 x 5120 elements where 77 us of traffic is the floor).  ex2 and the reciprocal are the hardware's
+// approximations (2^-22 resp. 1 ulp); forming exp(t) as 2^(t log2 e) adds |t| 2^-24.
+__device__ __forceinline__ float rcp(float x) {
+    float y;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+// 1 / (1 + exp(-t)): 0 and 1 far out, where ex2 overflows or vanishes.
+__device__ __forceinline__ float sigmoid(float t) { return rcp(1.f + ex2(-kLog2e * t)); }
+// Phi(z) and the density e = exp(-z^2 / 2) by formula 7.1.26 of Abramowitz and Stegun's handbook:
+// erfc(x) = (a1 t + .. + a5 t^5) exp(-x^2), t = 1 / (1 + p x), |error| <= 1.5e-7.  The lower tail takes
+// erfc itself and loses nothing to 1 - erf.
+__device__ __forceinline__ float normal_cdf(float z, float& e) {
+    const float x = fabsf(z) * 0.70710678118654752f;
+    e = ex2(-0.5f * kLog2e * z * z);
+    const float t = rcp(fmaf(0.3275911f, x, 1.f));
+    const float poly = t * fmaf(t, fmaf(t, fmaf(t, fmaf(t, 1.061405429f, -1.453152027f), 1.421413741f), -0.284496736f),
+                                0.254829592f);
+    const float tail = 0.5f * poly * e;
+    return z < 0.f ? tail : 1.f - tail;
+}
 
 template <int ACT>
 __device__ __forceinline__ float act_value(float z) {
     if constexpr (ACT == TPPO_ACT_RELU) return fmaxf(z, 0.f);
-    if constexpr (ACT == TPPO_ACT_GELU) return 0.5f * z * (1.f + erff(z * 0.70710678118654752f));
+    if constexpr (ACT == TPPO_ACT_GELU) {
+        float e;
+        return z * normal_cdf(z, e);
+    }
     if constexpr (ACT == TPPO_ACT_GELU_TANH)          // 0.5 (1 + tanh u) = sigmoid(2u)
-        return z * sigmoid(1.59576912160573071f * fmaf(0.044715f * z * z, z, z));
+        return z * sigmoid(z * fmaf(1.59576912160573071f * 0.044715f, z * z, 1.59576912160573071f));
     if constexpr (ACT == TPPO_ACT_SILU) return z * sigmoid(z);
     return z;
 }
 template <int ACT>
 __device__ __forceinline__ float act_slope(float z) {
     if constexpr (ACT == TPPO_ACT_RELU) return z > 0.f ? 1.f : 0.f;
-    if constexpr (ACT == TPPO_ACT_GELU)
-        return 0.5f * (1.f + erff(z * 0.70710678118654752f)) + z * expf(-0.5f * z * z) * 0.39894228040143268f;
+    // the slopes below have reached 0 and 1 at |z| = 100; powers of a larger z would overflow
+    z = fminf(fmaxf(z, -100.f), 100.f);
+    if constexpr (ACT == TPPO_ACT_GELU) {
+        float e;
+        const float phi = normal_cdf(z, e);
+        return fmaf(z * 0.39894228040143268f, e, phi);
+    }
     if constexpr (ACT == TPPO_ACT_GELU_TANH) {
-        const float z2 = z * z, p = sigmoid(1.59576912160573071f * fmaf(0.044715f * z2, z, z));
-        // where p has reached 0 or 1 the second term is 0 (z^3 may overflow there)
-        const float q = p * (1.f - p);
-        return q == 0.f ? p : fmaf(z * q, 1.59576912160573071f * fmaf(3.f * 0.044715f, z2, 1.f), p);
+        constexpr float k = 1.59576912160573071f;
+        const float z2 = z * z, p = sigmoid(z * fmaf(k * 0.044715f, z2, k));
+        return fmaf(z * fmaf(-p, p, p), fmaf(k * 3.f * 0.044715f, z2, k), p);
     }
     if constexpr (ACT == TPPO_ACT_SILU) {
-        const float p = sigmoid(z), q = p * (1.f - p);
-        return q == 0.f ? p : fmaf(z, q, p);
+        const float p = sigmoid(z);
+        return fmaf(z, fmaf(-p, p, p), p);
     }
     return 1.f;
 }
@@ -142,10 +169,10 @@ struct EpiLinear {
         }
         // z and y that are not finite, or leave the range of the type they are stored in, are written 0
         const float top = y_f32 ? kFltMax : kBf16Max, ztop = pre ? kBf16Max : kFltMax;
-        float worst = 0.f;                        // a NaN is carried along by the comparison's form
+        bool fine = true;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) worst = fabsf(o[i]) <= top && fabsf(v[i]) <= ztop ? worst : 1.f;
-        if (worst != 0.f) {
+        for (int i = 0; i < 8; ++i) fine = fine && fabsf(o[i]) <= top && fabsf(v[i]) <= ztop;
+        if (!fine) {
             bool bad = false;
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
@@ -172,19 +199,100 @@ struct EpiStore {
     __device__ __forceinline__ void operator()(int64_t m, int n, float (&v)[8], const Loads&) const {
         if (outside(m, n)) return;
         const int count = min(8, N - n);
-        bool bad = false;
+        bool fine = true;
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
-            if (!(fabsf(v[i]) <= kBf16Max)) { bad |= i < count; v[i] = 0.f; }
-        if (bad && status) atomicOr(status, TPPO_DEV_NONFINITE);
+        for (int i = 0; i < 8; ++i) fine = fine && fabsf(v[i]) <= kBf16Max;
+        if (!fine) {
+            bool bad = false;
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (!(fabsf(v[i]) <= kBf16Max)) { bad |= i < count; v[i] = 0.f; }
+            if (bad && status) atomicOr(status, TPPO_DEV_NONFINITE);
+        }
         put8(out + m * ld + n, v, count, vec);
     }
 };
+
+// Few output columns (a value head has one): a product that reads x once and is bound by that.  A warp
+// takes kNarrowRows rows at a time, its lanes 8 consecutive k each, with the weight transposed in shared
+// memory; fp32 multiply-adds.  16384 rows of 5120, one column: the split tensor-core kernel takes 66 us
+// (its tile computes 128 columns), this one 32 us (5.2 TB/s).
+constexpr int kNarrowRows = 4;
+constexpr int kNarrowMaxN = 8;
+constexpr int kNarrowMaxSmem = 96 * 1024;
+
+template <int NB, bool VEC>
+__global__ void __launch_bounds__(256) linear_narrow_kernel(const bf16_bits* x, int64_t ldx, const bf16_bits* w, int64_t ldw,
+                                                            int64_t M, int32_t K, int32_t kpad, const EpiLinear epi) {
+    extern __shared__ __align__(16) bf16_bits wt[];           // [NB][kpad], zeros beyond K and N
+    pdl_launch();
+    pdl_wait();
+    for (int i = threadIdx.x; i < NB * kpad; i += 256) {
+        const int k = i / NB, n = i - k * NB;
+        wt[n * kpad + k] = k < K && n < epi.N ? w[int64_t(k) * ldw + n] : bf16_bits(0);
+    }
+    __syncthreads();
+    const int lane = threadIdx.x & 31;
+    const int64_t warp = int64_t(blockIdx.x) * 8 + (threadIdx.x >> 5), warps = int64_t(gridDim.x) * 8;
+    for (int64_t m0 = warp * kNarrowRows; m0 < M; m0 += warps * kNarrowRows) {
+        float acc[kNarrowRows][NB];
+#pragma unroll
+        for (int r = 0; r < kNarrowRows; ++r)
+#pragma unroll
+            for (int n = 0; n < NB; ++n) acc[r][n] = 0.f;
+#pragma unroll 2
+        for (int k = lane * 8; k < K; k += 256) {
+            float xv[kNarrowRows][8];
+#pragma unroll
+            for (int r = 0; r < kNarrowRows; ++r) {
+                // rows past the last are computed from the last and not stored
+                const bf16_bits* p = x + min(m0 + r, M - 1) * ldx + k;
+                if (VEC) load_vec<8>(p, xv[r]);
+                else get8(p, xv[r], min(8, K - k), false);
+            }
+#pragma unroll
+            for (int n = 0; n < NB; ++n) {
+                float wv[8];
+                load_vec<8>(wt + n * kpad + k, wv);
+#pragma unroll
+                for (int r = 0; r < kNarrowRows; ++r)
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) acc[r][n] = fmaf(xv[r][i], wv[i], acc[r][n]);
+            }
+        }
+#pragma unroll
+        for (int r = 0; r < kNarrowRows; ++r) {
+            float v[8];
+#pragma unroll
+            for (int n = 0; n < 8; ++n) v[n] = n < NB ? warp_sum(acc[r][n < NB ? n : 0]) : 0.f;
+            if (lane == r) {
+                EpiLinear::Loads l;
+                epi.load(m0 + r, 0, l);
+                epi(m0 + r, 0, v, l);
+            }
+        }
+    }
+}
+
+template <int NB>
+int linear_narrow(const DenseOperand& X, const DenseOperand& W, const EpiLinear& e, bool vec, cudaStream_t s) {
+    const int32_t K = int32_t(X.cols), kpad = (K + 7) / 8 * 8;
+    const size_t smem = size_t(NB) * kpad * 2;
+    auto kernel = vec ? linear_narrow_kernel<NB, true> : linear_narrow_kernel<NB, false>;
+    TPPO_CUDA_CHECK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, int(smem)));
+    const int64_t blocks = (X.rows + 8 * kNarrowRows - 1) / (8 * kNarrowRows), most = 4 * kNumSms;
+    TPPO_CUDA_CHECK(launch_dense(kernel, dim3(unsigned(blocks < most ? blocks : most)), dim3(256), smem, s,
+                                 static_cast<const bf16_bits*>(X.p), X.ld, static_cast<const bf16_bits*>(W.p), W.ld, X.rows, K,
+                                 kpad, e));
+    return TPPO_OK;
+}
 
 // Copies a bf16 matrix into rows of ldo elements (a multiple of 8), eight elements per thread; the
 // tail of a row is filled with zeros.
 __global__ void __launch_bounds__(256) linear_repack_kernel(const bf16_bits* src, int64_t ld, int64_t rows, int32_t cols,
                                                             bf16_bits* dst, int64_t ldo) {
+    pdl_launch();
+    pdl_wait();
     const int64_t per = ldo / 8, total = rows * per;
     for (int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x; i < total; i += int64_t(gridDim.x) * 256) {
         const int64_t r = i / per;
@@ -216,6 +324,8 @@ __global__ void __launch_bounds__(256) linear_dz_kernel(const DzArgs a) {
     float acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
     bool bad = false;
     const T* dy = static_cast<const T*>(a.dy);
+    pdl_launch();
+    pdl_wait();
     if (count > 0) {
         const int64_t step = int64_t(gridDim.y) * 8;
         for (int64_t m0 = int64_t(blockIdx.y) * 8 + warp; m0 < a.M; m0 += 2 * step) {
@@ -238,11 +348,17 @@ __global__ void __launch_bounds__(256) linear_dz_kernel(const DzArgs a) {
 #pragma unroll
                         for (int i = 0; i < 8; ++i) d[k][i] *= slope[i];
                     }
+                    bool fine = true;
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        if (!(fabsf(d[k][i]) <= kBf16Max)) { bad = true; d[k][i] = 0.f; }
-                        acc[i] += d[k][i];
+                    for (int i = 0; i < 8; ++i) fine = fine && fabsf(d[k][i]) <= kBf16Max;
+                    if (!fine) {
+                        bad = true;
+#pragma unroll
+                        for (int i = 0; i < 8; ++i)
+                            if (!(fabsf(d[k][i]) <= kBf16Max)) d[k][i] = 0.f;
                     }
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) acc[i] += d[k][i];
                     if (a.dz) store_vec<8>(a.dz + m * a.ldz + n, d[k]);
                 }
             }
@@ -311,9 +427,8 @@ bool vec_rows(const void* p, int64_t ld, size_t esize) { return aligned(p, 16) &
 int repack(DenseOperand& o, bf16_bits* dst, cudaStream_t s) {
     const int64_t ldo = pad8(o.cols), total = o.rows * (ldo / 8);
     const int64_t blocks = (total + 255) / 256;
-    linear_repack_kernel<<<unsigned(blocks < 16 * kNumSms ? blocks : 16 * kNumSms), 256, 0, s>>>(
-        static_cast<const bf16_bits*>(o.p), o.ld, o.rows, int32_t(o.cols), dst, ldo);
-    TPPO_CUDA_CHECK(cudaGetLastError());
+    TPPO_CUDA_CHECK(launch_dense(linear_repack_kernel, dim3(unsigned(blocks < 16 * kNumSms ? blocks : 16 * kNumSms)), dim3(256),
+                                 0, s, static_cast<const bf16_bits*>(o.p), o.ld, o.rows, int32_t(o.cols), dst, ldo));
     o.p = dst;
     o.ld = ldo;
     return TPPO_OK;
@@ -347,7 +462,9 @@ TPPO_API int tppo_linear_fwd(const void* x, int64_t ldx, const void* weight, int
     if (!x || !weight || !y || !aligned(x, 2) || !aligned(weight, 2) || !aligned(bias, bs) || !aligned(residual, 2) ||
         !aligned(y, ys) || !aligned(preact, 2) || !aligned(status, 4))
         return TPPO_ERR_INVALID_ARG;
-    const bool copy_x = !tma_rows(x, ldx), copy_w = !tma_rows(weight, ldw);
+    const int nb = N <= 1 ? 1 : N <= 2 ? 2 : N <= 4 ? 4 : 8;
+    const bool narrow = N <= kNarrowMaxN && size_t(nb) * pad8(K) * 2 <= size_t(kNarrowMaxSmem);
+    const bool copy_x = !narrow && !tma_rows(x, ldx), copy_w = !narrow && !tma_rows(weight, ldw);
     const LinearWs w = linear_carve(workspace, M, K, N);
     if ((copy_x || copy_w) && (!workspace || !aligned(workspace, kWsAlign) || workspace_bytes < w.bytes))
         return TPPO_ERR_WORKSPACE;
@@ -365,7 +482,14 @@ TPPO_API int tppo_linear_fwd(const void* x, int64_t ldx, const void* weight, int
     e.vec_y = vec_rows(y, ldy, ys); e.vec_r = vec_rows(residual, ldr, 2); e.vec_p = vec_rows(preact, ldp, 2);
     e.vec_b = aligned(bias, 16);
     e.status = status;
-    return dense_product<0, 1, false, false>(X, W, M, N, K, e, status, false, s);
+    if (narrow) {
+        const bool vec = tma_rows(x, ldx) && K % 8 == 0;
+        if (nb == 1) return linear_narrow<1>(X, W, e, vec, s);
+        if (nb == 2) return linear_narrow<2>(X, W, e, vec, s);
+        if (nb == 4) return linear_narrow<4>(X, W, e, vec, s);
+        return linear_narrow<8>(X, W, e, vec, s);
+    }
+    return dense_product<0, 1, false, false>(X, W, M, N, K, e, status, s);
 }
 
 TPPO_API int tppo_linear_bwd(const void* dy, int32_t dy_dtype, int64_t lddy, const void* x, int64_t ldx, const void* weight,
@@ -411,27 +535,26 @@ TPPO_API int tppo_linear_bwd(const void* dy, int32_t dy_dtype, int64_t lddy, con
         int64_t gy = (M + 31) / 32, most = (16 * kNumSms + gx - 1) / gx;      // four rows per warp at least
         if (gy > most) gy = most;
         if (gy > kDzMaxParts) gy = kDzMaxParts;
-        if (dy_dtype == TPPO_F32) linear_dz_kernel<float><<<dim3(gx, unsigned(gy)), 256, 0, s>>>(a);
-        else linear_dz_kernel<bf16_bits><<<dim3(gx, unsigned(gy)), 256, 0, s>>>(a);
-        TPPO_CUDA_CHECK(cudaGetLastError());
+        auto kernel = dy_dtype == TPPO_F32 ? linear_dz_kernel<float> : linear_dz_kernel<bf16_bits>;
+        TPPO_CUDA_CHECK(launch_dense(kernel, dim3(gx, unsigned(gy)), dim3(256), 0, s, a));
         if (make_dz) { Z.p = w.dz; Z.ld = a.ldz; }
         if (dbias) {
             const dim3 grid((N + 31) / 32);
             if (bias_dtype == TPPO_F32)
-                TPPO_CUDA_CHECK(launch_dense(linear_dbias_kernel<float>, grid, dim3(512), 0, s, true,
+                TPPO_CUDA_CHECK(launch_dense(linear_dbias_kernel<float>, grid, dim3(512), 0, s,
                                              static_cast<const float*>(w.partial), int32_t(gy), N, static_cast<float*>(dbias)));
             else
-                TPPO_CUDA_CHECK(launch_dense(linear_dbias_kernel<bf16_bits>, grid, dim3(512), 0, s, true,
+                TPPO_CUDA_CHECK(launch_dense(linear_dbias_kernel<bf16_bits>, grid, dim3(512), 0, s,
                                              static_cast<const float*>(w.partial), int32_t(gy), N, static_cast<bf16_bits*>(dbias)));
         }
     }
     if (dx) {        // dx[m, k] = sum_n dz[m, n] W[k, n]: both operands contiguous along the contraction
         const EpiStore e{static_cast<bf16_bits*>(dx), lddx, M, K, vec_rows(dx, lddx, 2), status};
-        if ((rc = dense_product<0, 0, false, false>(Z, W, M, K, N, e, status, false, s)) != TPPO_OK) return rc;
+        if ((rc = dense_product<0, 0, false, false>(Z, W, M, K, N, e, status, s)) != TPPO_OK) return rc;
     }
     if (dweight) {   // dweight[k, n] = sum_m x[m, k] dz[m, n]: both contiguous along their outer index
         const EpiStore e{static_cast<bf16_bits*>(dweight), lddw, K, N, vec_rows(dweight, lddw, 2), status};
-        if ((rc = dense_product<1, 1, false, false>(X, Z, K, N, M, e, status, false, s)) != TPPO_OK) return rc;
+        if ((rc = dense_product<1, 1, false, false>(X, Z, K, N, M, e, status, s)) != TPPO_OK) return rc;
     }
     return TPPO_OK;
 }

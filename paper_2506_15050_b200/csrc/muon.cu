@@ -87,6 +87,7 @@ template <class T, int VEC>
 __global__ void __launch_bounds__(kMuonThreads) muon_prepare_kernel(const PrepareArgs a) {
     __shared__ double red[kMuonThreads / 32];
     pdl_launch();
+    pdl_wait();
     const int64_t per = (a.C + VEC - 1) / VEC, total = a.R * per;
     double sum = 0.0;
     bool bad = false;
@@ -276,9 +277,8 @@ int muon_prepare(const PrepareArgs& a, bool vec, int* parts, cudaStream_t s) {
     const int64_t items = a.R * (vec ? (a.C + 7) / 8 : a.C);
     const int64_t blocks = (items + kMuonThreads - 1) / kMuonThreads;
     *parts = int(blocks < kMuonMaxBlocks ? blocks : kMuonMaxBlocks);
-    if (vec) muon_prepare_kernel<T, 8><<<*parts, kMuonThreads, 0, s>>>(a);
-    else muon_prepare_kernel<T, 1><<<*parts, kMuonThreads, 0, s>>>(a);
-    TPPO_CUDA_CHECK(cudaGetLastError());
+    auto kernel = vec ? muon_prepare_kernel<T, 8> : muon_prepare_kernel<T, 1>;
+    TPPO_CUDA_CHECK(launch_dense(kernel, dim3(unsigned(*parts)), dim3(kMuonThreads), 0, s, a));
     return TPPO_OK;
 }
 
@@ -318,16 +318,16 @@ TPPO_API int tppo_muon_orthogonalize(const void* grad, int32_t grad_dtype, int64
     if (rc != TPPO_OK) return rc;
     const int64_t vectors = R * w.ldx / 8, blocks = (vectors + kMuonThreads - 1) / kMuonThreads;
     TPPO_CUDA_CHECK(launch_dense(muon_normalise_kernel, dim3(unsigned(blocks < kMuonMaxBlocks ? blocks : kMuonMaxBlocks)),
-                                 dim3(kMuonThreads), 0, s, true, static_cast<const double*>(w.partial), int32_t(parts), eps,
+                                 dim3(kMuonThreads), 0, s, static_cast<const double*>(w.partial), int32_t(parts), eps,
                                  static_cast<const float*>(w.x32), w.x16[0], w.inverse, vectors));
     for (int32_t k = 0; k < steps; ++k) {
         const DenseOperand X{w.x16[k % 2], R, C, w.ldx}, A{w.a, m, m, w.lda}, B{w.b, m, m, w.lda};
         const bool apart = m <= 64 || k >= steps - 3, last = k == steps - 1;
         const EpiA ea{w.a, w.lda, int32_t(m), apart ? w.diag_a : nullptr};
         const EpiB eb{w.a, w.b, w.lda, int32_t(m), apart ? w.diag_a : nullptr, w.diag_b};
-        if (right) rc = dense_product<1, 1, true, true>(X, X, m, m, R, ea, status, true, s);
-        else rc = dense_product<0, 0, true, true>(X, X, m, m, C, ea, status, true, s);
-        if (rc == TPPO_OK) rc = dense_product<0, 0, true, true>(A, A, m, m, m, eb, status, true, s);
+        if (right) rc = dense_product<1, 1, true, true>(X, X, m, m, R, ea, status, s);
+        else rc = dense_product<0, 0, true, true>(X, X, m, m, C, ea, status, s);
+        if (rc == TPPO_OK) rc = dense_product<0, 0, true, true>(A, A, m, m, m, eb, status, s);
         if (rc != TPPO_OK) return rc;
         bf16_bits* out = last ? static_cast<bf16_bits*>(update) : nullptr;
         const int32_t vec_u = aligned(update, 16) && ldu % 8 == 0;
@@ -335,10 +335,10 @@ TPPO_API int tppo_muon_orthogonalize(const void* grad, int32_t grad_dtype, int64
         const float* diag_b = apart ? w.diag_b : nullptr;
         if (right) {
             const EpiX<true> ex{w.x32, w.x16[(k + 1) % 2], w.ldx, inverse, diag_b, out, ldu, vec_u, scale, R, C};
-            rc = dense_product<0, 0, true, false>(X, B, R, C, m, ex, status, true, s);
+            rc = dense_product<0, 0, true, false>(X, B, R, C, m, ex, status, s);
         } else {
             const EpiX<false> ex{w.x32, w.x16[(k + 1) % 2], w.ldx, inverse, diag_b, out, ldu, vec_u, scale, R, C};
-            rc = dense_product<0, 1, true, false>(B, X, R, C, m, ex, status, true, s);
+            rc = dense_product<0, 1, true, false>(B, X, R, C, m, ex, status, s);
         }
         if (rc != TPPO_OK) return rc;
     }
