@@ -45,13 +45,6 @@ __device__ __forceinline__ void tmem_ld8(uint32_t taddr, uint32_t (&v)[8]) {
                  : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7])
                  : "r"(taddr) : "memory");
 }
-__device__ __forceinline__ float4 ld_cluster_f32x4(uint32_t cluster_addr) {
-    float4 v;
-    asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];"
-                 : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(cluster_addr) : "memory");
-    return v;
-}
-
 // The operand ring both kernels share: producer and MMA issuer for one output tile.
 template <int AMAJ, int BMAJ, bool F16, int BN, int STAGES>
 struct DenseRing {
@@ -223,10 +216,15 @@ dense_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
                 const int n0 = nt * kDenseBN + half * (kDenseBN / 2) + c;
                 if (SYM && n0 > m0) break;            // above the diagonal: another chunk's mirror image
                 if (epi.outside(m0, n0)) break;
-                // what the epilogue reads is on its way while the accumulator is fetched and turned
+                // eight trips of a lane finish eight elements each: four as they are, four mirrored.  What the
+                // epilogue reads is fetched four trips ahead, for the first ones while the accumulator is
+                // fetched and turned.
+                const int trips = SYM && n0 < m0 ? 8 : 4;
+                auto row_of = [&](int it) { return (it < 4 ? m0 : int64_t(n0)) + (it & 3) * 8 + (lane >> 2); };
+                auto col_of = [&](int it) { return (it < 4 ? n0 : int(m0)) + (lane & 3) * 8; };
                 typename Epi::Loads ahead[4];
 #pragma unroll
-                for (int it = 0; it < 4; ++it) epi.load(m0 + it * 8 + (lane >> 2), n0 + (lane & 3) * 8, ahead[it]);
+                for (int it = 0; it < 4; ++it) epi.load(row_of(it), col_of(it), ahead[it]);
                 uint32_t v[32];
                 umma::tmem_ld32(tmem + acc * kDenseBN + (uint32_t(q * 32) << 16) + half * (kDenseBN / 2) + c, v);
                 umma::tmem_ld_wait();
@@ -237,22 +235,25 @@ dense_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
                 for (int j = 0; j < 8; ++j)
                     ptx::sts128(sw + lane * 128 + ((j ^ (lane & 7)) << 4), make_uint4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]));
                 __syncwarp();
+                // one copy of the epilogue's code: unrolled it does not fit the instruction cache (134 us
+                // instead of XX for 16384 x 5120 outputs of a 128-long contraction)
+#pragma unroll 1
+                for (int it = 0; it < trips; ++it) {
+                    const typename Epi::Loads mine = ahead[0];
 #pragma unroll
-                for (int it = 0; it < 4; ++it) {
-                    const int r = it * 8 + (lane >> 2), j = (lane & 3) * 2;
-                    const uint4 lo = ptx::lds128(sw + r * 128 + ((j ^ (r & 7)) << 4));
-                    const uint4 hi = ptx::lds128(sw + r * 128 + (((j + 1) ^ (r & 7)) << 4));
-                    float w[8] = {__uint_as_float(lo.x), __uint_as_float(lo.y), __uint_as_float(lo.z), __uint_as_float(lo.w),
-                                  __uint_as_float(hi.x), __uint_as_float(hi.y), __uint_as_float(hi.z), __uint_as_float(hi.w)};
-                    epi(m0 + r, n0 + j * 4, w, ahead[it]);
-                }
-                if (SYM && n0 < m0) {
-#pragma unroll
-                    for (int it = 0; it < 4; ++it) epi.load(int64_t(n0) + it * 8 + (lane >> 2), int(m0) + (lane & 3) * 8, ahead[it]);
-#pragma unroll
-                    for (int it = 0; it < 4; ++it) {
-                        const int col = it * 8 + (lane >> 2), r0 = (lane & 3) * 8;
-                        float w[8];
+                    for (int i = 0; i < 3; ++i) ahead[i] = ahead[i + 1];
+                    if (SYM && it + 4 < trips) epi.load(row_of(it + 4), col_of(it + 4), ahead[3]);
+                    float w[8];
+                    if (!SYM || it < 4) {
+                        const int r = it * 8 + (lane >> 2), j = (lane & 3) * 2;
+                        const uint4 lo = ptx::lds128(sw + r * 128 + ((j ^ (r & 7)) << 4));
+                        const uint4 hi = ptx::lds128(sw + r * 128 + (((j + 1) ^ (r & 7)) << 4));
+                        w[0] = __uint_as_float(lo.x); w[1] = __uint_as_float(lo.y);
+                        w[2] = __uint_as_float(lo.z); w[3] = __uint_as_float(lo.w);
+                        w[4] = __uint_as_float(hi.x); w[5] = __uint_as_float(hi.y);
+                        w[6] = __uint_as_float(hi.z); w[7] = __uint_as_float(hi.w);
+                    } else {
+                        const int col = (it & 3) * 8 + (lane >> 2), r0 = (lane & 3) * 8;
 #pragma unroll
                         for (int i = 0; i < 8; ++i) {
                             uint32_t u;
@@ -260,8 +261,8 @@ dense_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
                                          : "r"(sw + (r0 + i) * 128 + (((col >> 2) ^ i) << 4) + (col & 3) * 4));
                             w[i] = __uint_as_float(u);
                         }
-                        epi(int64_t(n0) + col, int(m0) + r0, w, ahead[it]);
                     }
+                    epi(row_of(it), col_of(it), w, mine);
                 }
             }
             umma::fence_before_thread_sync();
@@ -281,10 +282,27 @@ dense_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
 // ---- few tiles ----------------------------------------------------------------------------------
 // Accumulator rows: output columns (contiguous); accumulator columns: output rows.  A is therefore
 // the operand indexed by the output column, B the one indexed by the output row.
-template <int BN> __host__ __device__ constexpr int dense_split_stages() { return BN <= 32 ? 5 : BN <= 64 ? 4 : 3; }
+//
+// Each of the cluster's CTAs owns ceil(BN / CTAs) accumulator columns: every CTA stores its partial sums
+// straight from tensor memory into the owner's shared memory, and after one cluster barrier the owner
+// adds them in rank order and runs the epilogue.  (Letting the owner fetch them instead costs a second
+// barrier and a remote round trip: 11-13 us instead of 8-9 per launch of a chain of small products.)
+// Up to 64 columns the sums have memory of their own and two CTAs share an SM; wider tiles lay them over
+// the operand ring, which needs one more barrier (every CTA has consumed its ring) but leaves 192 KB to
+// the ring: at some 2000 clocks of loaded L2 latency the operand rate is the bytes in flight, and a
+// 128-column tile with 128 KB was bound by them.
+template <int BN> __host__ __device__ constexpr bool dense_split_overlay() { return BN >= 128; }
+template <int BN> __host__ __device__ constexpr int dense_split_stages() {
+    return BN <= 16 ? 5 : BN <= 32 ? 4 : BN <= 64 ? 3 : BN <= 128 ? 6 : 4;
+}
+template <int BN> __host__ __device__ constexpr uint32_t dense_split_ring() {
+    return uint32_t(dense_split_stages<BN>()) * (kDenseABytes + BN * 128);
+}
+template <int BN> __host__ __device__ constexpr uint32_t dense_split_body() {
+    return dense_split_ring<BN>() + (dense_split_overlay<BN>() ? 0u : (BN + 8) * 128 * 4);
+}
 template <int BN> __host__ __device__ constexpr size_t dense_split_smem() {
-    const size_t ring = size_t(dense_split_stages<BN>()) * (kDenseABytes + BN * 128), sums = size_t(BN) * 128 * 4;
-    return (ring > sums ? ring : sums) + 1024 + 128;
+    return dense_split_body<BN>() + 1024 /* alignment */ + 128 /* barriers */;
 }
 
 struct DenseSplitShape {
@@ -296,21 +314,20 @@ template <int AMAJ, int BMAJ, bool F16, int BN, class Epi>
 __global__ void __launch_bounds__(kDenseThreads)
 dense_split_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
                    const DenseSplitShape g, const Epi epi, int32_t* status) {
-    constexpr int STAGES = dense_split_stages<BN>();
+    constexpr int STAGES = dense_split_stages<BN>(), kEpiThreads = kDenseThreads - 64;
     constexpr uint32_t kCols = BN < 32 ? 32 : BN;
     extern __shared__ uint8_t smem_raw[];
-    // dynamic shared memory starts at the same address in every CTA of a kernel, so `base` is common to
-    // the cluster and the partial sums of all its CTAs lie at the same offset
+    // dynamic shared memory starts at the same address in every CTA of a kernel, so `sums` is common to
+    // the cluster
     const uint32_t raw = ptx::smem_addr(smem_raw), base = (raw + 1023u) & ~1023u;
     typedef DenseRing<AMAJ, BMAJ, F16, BN, STAGES> Ring;
-    constexpr uint32_t kBody = uint32_t(dense_split_smem<BN>() - 1024 - 128);
-    const uint32_t bars = base + kBody;
+    const uint32_t sums = base + (dense_split_overlay<BN>() ? 0u : dense_split_ring<BN>()), bars = base + dense_split_body<BN>();
     const uint32_t full = bars, empty = bars + 8 * STAGES, acc_full = bars + 16 * STAGES, slot = acc_full + 8;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const uint32_t rank = ptx::cluster_ctarank();
-    uint32_t splits;
+    const int rank = int(ptx::cluster_ctarank());
+    int splits;
     asm volatile("mov.u32 %0, %cluster_nctarank;" : "=r"(splits));
-    const int tile = int(blockIdx.x / splits);
+    const int tile = int(blockIdx.x) / splits;
     const int rt = tile / g.col_tiles, ct = tile % g.col_tiles;
     const int k0 = int(int64_t(g.k_steps) * rank / splits), k1 = int(int64_t(g.k_steps) * (rank + 1) / splits);
 
@@ -330,22 +347,25 @@ dense_split_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
     }
     umma::fence_before_thread_sync();
     __syncthreads();
+    ptx::cluster_sync_all();                 // every CTA of the cluster runs: its shared memory may be written
     umma::fence_after_thread_sync();
     const uint32_t tmem = *reinterpret_cast<uint32_t*>(smem_raw + (slot - raw));
     pdl_launch();
     pdl_wait();
 
-    // each CTA finishes its share of the (output row, eight output columns) units; what the epilogue of a
-    // thread's first units reads is fetched while the product runs
-    const int units = BN * 16, per = (units + int(splits) - 1) / int(splits);
-    const int u0 = int(rank) * per + int(threadIdx.x) - 64, last = min(int(rank) * per + per, units);
+    // this CTA's columns and, per thread, (output row, eight output columns) units; what the epilogue
+    // reads is fetched kAhead units ahead, for the first ones while the product runs
+    const int own = (BN + splits - 1) / splits, c0 = rank * own;
+    const int units = max(0, min(own, BN - c0)) * 16;
+    const int64_t row0 = int64_t(ct) * BN + c0;
+    const int col0 = rt * kDenseTileM, u0 = int(threadIdx.x) - 64;
     constexpr int kAhead = BN >= 64 ? 4 : BN / 16;
     typename Epi::Loads ahead[kAhead];
     if (warp >= 2) {
 #pragma unroll
         for (int i = 0; i < kAhead; ++i) {
-            const int u = u0 + i * (kDenseThreads - 64);
-            if (u < last) epi.load(int64_t(ct) * BN + u / 16, rt * kDenseTileM + (u % 16) * 8, ahead[i]);
+            const int u = u0 + i * kEpiThreads;
+            if (u < units) epi.load(row0 + u / 16, col0 + (u % 16) * 8, ahead[i]);
         }
     }
 
@@ -365,53 +385,60 @@ dense_split_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
         }
         __syncwarp();
     } else {
-        const int q = warp & 3, half = (warp - 2) >> 2;
-        if (ptx::mbar_wait_warp<false>(acc_full, 0)) {
-            umma::fence_after_thread_sync();
-            // every MMA has completed, so the ring's bytes are free for the partial sums [BN][128]
+        timed_out = !ptx::mbar_wait_warp<false>(acc_full, 0);
+    }
+    if (dense_split_overlay<BN>()) ptx::cluster_sync_all();      // every ring of the cluster has been consumed
+    if (warp >= 2 && !timed_out) {
+        const int q = warp & 3, half = (warp - 2) >> 2, r = q * 32 + lane;
+        constexpr int kChunk = BN >= 64 ? 32 : 8;
+        umma::fence_after_thread_sync();
 #pragma unroll 1
-            for (int c = half * (BN / 2); c < (half + 1) * (BN / 2); c += 8) {
-                uint32_t v[8];
-                tmem_ld8(tmem + (uint32_t(q * 32) << 16) + c, v);
-                umma::tmem_ld_wait();
+        for (int c = half * (BN / 2); c < (half + 1) * (BN / 2); c += kChunk) {
+            uint32_t v[kChunk];
+            if constexpr (kChunk == 32) umma::tmem_ld32(tmem + (uint32_t(q * 32) << 16) + c, v);
+            else tmem_ld8(tmem + (uint32_t(q * 32) << 16) + c, v);
+            umma::tmem_ld_wait();
+            int owner = c / own, in = c - owner * own;
 #pragma unroll
-                for (int i = 0; i < 8; ++i)
-                    asm volatile("st.shared.u32 [%0], %1;" ::"r"(base + ((c + i) * 128 + q * 32 + lane) * 4), "r"(v[i]) : "memory");
+            for (int i = 0; i < kChunk; ++i) {
+                // [source rank][owned column][128 rows] at the owner
+                const uint32_t at = ptx::map_to_cta(sums + ((rank * own + in) * 128 + r) * 4, uint32_t(owner));
+                asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(at), "r"(v[i]) : "memory");
+                if (++in == own) { in = 0; ++owner; }
             }
-        } else {
-            timed_out = true;
         }
     }
-    ptx::cluster_sync_all();
+    umma::fence_before_thread_sync();
+    ptx::cluster_sync_all();                 // all partial sums have arrived; nobody writes here any more
+    umma::fence_after_thread_sync();
     if (warp >= 2) {
-        auto finish = [&](int u, const typename Epi::Loads& l) {
-            const int64_t m = int64_t(ct) * BN + u / 16;
-            const int n = rt * kDenseTileM + (u % 16) * 8;
-            if (epi.outside(m, n)) return;
-            float w[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-            const uint32_t at = base + ((u / 16) * 128 + (u % 16) * 8) * 4;
-            for (uint32_t s = 0; s < splits; ++s) {
-                const uint32_t p = ptx::map_to_cta(at, s);
-                const float4 a = ld_cluster_f32x4(p), b = ld_cluster_f32x4(p + 16);
-                w[0] += a.x; w[1] += a.y; w[2] += a.z; w[3] += a.w;
-                w[4] += b.x; w[5] += b.y; w[6] += b.z; w[7] += b.w;
-            }
-            epi(m, n, w, l);
-        };
+        // not unrolled: the code runs a few times per launch, and fetching it costs more than running it
+        // (0.7 us per copy)
+#pragma unroll 1
+        for (int u = u0; u < units; u += kEpiThreads) {
+            const int64_t m = row0 + u / 16;
+            const int n = col0 + (u % 16) * 8;
+            const typename Epi::Loads mine = ahead[0];
 #pragma unroll
-        for (int i = 0; i < kAhead; ++i)
-            if (u0 + i * (kDenseThreads - 64) < last) finish(u0 + i * (kDenseThreads - 64), ahead[i]);
-        for (int u = u0 + kAhead * (kDenseThreads - 64); u < last; u += kDenseThreads - 64) {
-            typename Epi::Loads l;
-            epi.load(int64_t(ct) * BN + u / 16, rt * kDenseTileM + (u % 16) * 8, l);
-            finish(u, l);
+            for (int i = 0; i + 1 < kAhead; ++i) ahead[i] = ahead[i + 1];
+            const int v = u + kAhead * kEpiThreads;
+            if (v < units) epi.load(row0 + v / 16, col0 + (v % 16) * 8, ahead[kAhead - 1]);
+            if (epi.outside(m, n)) continue;
+            float w[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+            uint32_t p = sums + ((u / 16) * 128 + (u % 16) * 8) * 4;
+            for (int s = 0; s < splits; ++s, p += uint32_t(own) * 512) {
+                const uint4 a = ptx::lds128(p), b = ptx::lds128(p + 16);
+                w[0] += __uint_as_float(a.x); w[1] += __uint_as_float(a.y);
+                w[2] += __uint_as_float(a.z); w[3] += __uint_as_float(a.w);
+                w[4] += __uint_as_float(b.x); w[5] += __uint_as_float(b.y);
+                w[6] += __uint_as_float(b.z); w[7] += __uint_as_float(b.w);
+            }
+            epi(m, n, w, mine);
         }
+    } else if (warp == 1) {
+        umma::tmem_dealloc(tmem, kCols);     // all tensor-memory loads are behind the barrier
     }
     if (timed_out && status) atomicOr(status, TPPO_DEV_WAIT_TIMEOUT);
-    umma::fence_before_thread_sync();
-    __syncwarp();
-    ptx::cluster_sync_all();          // no CTA leaves while another reads its sums
-    if (warp == 1) umma::tmem_dealloc(tmem, kCols);
 }
 
 // ---- host side ------------------------------------------------------------------------------------
@@ -477,35 +504,55 @@ int dense_split(const DenseOperand& a, const DenseOperand& b, int64_t m, int64_t
     return TPPO_OK;
 }
 
-// How many CTAs share one tile's contraction: the number that leaves the fewest k steps (and four steps'
-// worth of start and end per CTA) to the busiest SM, with at least two steps for each CTA.
-inline int dense_splits(int64_t tiles, int64_t k_steps) {
-    int best = 1;
-    int64_t least = INT64_MAX;
-    for (int s = 1; s <= 8 && (s == 1 || k_steps >= 2 * s); ++s) {
-        const int64_t cost = (tiles * s + kNumSms - 1) / kNumSms * ((k_steps + s - 1) / s + 4);
-        if (cost < least) { least = cost; best = s; }
+// How a product is cut: bn 0 = the persistent kernel, else the split kernel's accumulator columns (output
+// rows) per tile and the CTAs that share a tile's contraction.  The choice is the least estimated time
+// in SM clocks; the constants were fitted to measured launches (16 sizes from 256^3 to 2048 x 5120 x 5120,
+// every cut of each; the choice is within a few percent of the best of them but for two at 12 %):
+//   start and end of a CTA 5000, of two on one SM 7500; a k step is bound by its operand bytes at 64 per clock, its MMA at two
+//   clocks per column, or 2500 clocks of latency over the stages in flight on the SM; sending a column of
+//   partial sums 28, finishing one 62; a 128 x 256 tile of the persistent kernel 650 per step and
+//   11500 for the last epilogue, which nothing overlaps.
+struct DenseCut { int bn, splits; };
+inline DenseCut dense_cut(int64_t m, int64_t n, int64_t k, int64_t big_tiles, int least_bn) {
+    // CTAs that fit on the GPU at once in clusters of s, at two and at one per SM (the driver's count)
+    static const int64_t pair[9] = {0, 296, 296, 279, 284, 280, 270, 259, 264};
+    static const int64_t alone[9] = {0, 148, 148, 135, 132, 130, 132, 105, 120};
+    const int64_t rows = (n + 127) / 128, ks = (k + 63) / 64;
+    DenseCut best{0, 1};
+    int64_t least = 5000 + (big_tiles + kNumSms - 1) / kNumSms * ks * 650 + 11500;
+    for (int bn = least_bn; bn <= 256; bn *= 2) {
+        const int64_t tiles = rows * ((m + bn - 1) / bn);
+        const int64_t stages = bn <= 16 ? 5 : bn <= 32 ? 4 : bn <= 64 ? 3 : bn <= 128 ? 6 : 4;
+        for (int s = 1; s <= 8 && (s == 1 || ks >= 2 * s); ++s) {
+            const int64_t slots = bn <= 64 ? pair[s] : alone[s];
+            const int64_t waves = (tiles * s + slots - 1) / slots, steps = (ks + s - 1) / s;
+            const int64_t both = bn <= 64 && tiles * s > kNumSms ? 2 : 1;         // CTAs that share an SM
+            int64_t step = 2500 / (stages * both);
+            if (step < 2 * (128 + bn)) step = 2 * (128 + bn);
+            const int64_t cost = waves * (2500 * (1 + both) + steps * both * step + ((bn + s - 1) / s * 62 + bn * 28) * (1 + both) / 2);
+            if (cost < least) { least = cost; best = {bn, s}; }
+        }
+        if (bn >= m) break;                  // one tile holds all output rows already
     }
     return best;
 }
 
-// D[m, n] by whichever kernel suits its number of tiles: the persistent one when its 128 x 256 tiles
-// fill the SMs, the split one otherwise.  P: the operand indexed by m (PMAJ 0: [m, k], 1: [k, m]), Q: the
-// one indexed by n (QMAJ 0: [n, k], 1: [k, n]).  SYM: D is symmetric (m = n).
+// D[m, n].  P: the operand indexed by m (PMAJ 0: [m, k], 1: [k, m]), Q: the one indexed by n (QMAJ 0:
+// [n, k], 1: [k, n]).  SYM: D is symmetric (m = n); the persistent kernel then computes half of it.
 template <int PMAJ, int QMAJ, bool F16, bool SYM, class Epi>
 int dense_product(const DenseOperand& P, const DenseOperand& Q, int64_t m, int64_t n, int64_t k, const Epi& epi,
                   int32_t* status, cudaStream_t s) {
     const int64_t mt = (m + 127) / 128, nt = (n + 255) / 256;
     const int64_t big = SYM ? mt / 2 * (mt / 2 + 1) + (mt % 2 ? mt / 2 + 1 : 0) : mt * nt;
-    if (big >= kNumSms) return dense_gemm<PMAJ, QMAJ, F16, SYM>(P, Q, m, n, k, epi, status, s);
-    const int64_t ks = (k + 63) / 64, rows = (n + 127) / 128;
     // one operand box of 64 outer indices is the least an MN-major operand can be loaded in
     constexpr int B16 = PMAJ ? 64 : 16, B32 = PMAJ ? 64 : 32;
-    if (m <= 16 && !PMAJ) return dense_split<QMAJ, PMAJ, F16, B16>(Q, P, m, n, k, dense_splits(rows, ks), epi, status, s);
-    if (m <= 32 && !PMAJ) return dense_split<QMAJ, PMAJ, F16, B32>(Q, P, m, n, k, dense_splits(rows, ks), epi, status, s);
-    const int64_t by64 = rows * ((m + 63) / 64);
-    if (by64 <= kNumSms) return dense_split<QMAJ, PMAJ, F16, 64>(Q, P, m, n, k, dense_splits(by64, ks), epi, status, s);
-    return dense_split<QMAJ, PMAJ, F16, 128>(Q, P, m, n, k, dense_splits(rows * ((m + 127) / 128), ks), epi, status, s);
+    const DenseCut c = dense_cut(m, n, k, big, B16);
+    if (c.bn == 0) return dense_gemm<PMAJ, QMAJ, F16, SYM>(P, Q, m, n, k, epi, status, s);
+    if (c.bn == 16) return dense_split<QMAJ, PMAJ, F16, B16>(Q, P, m, n, k, c.splits, epi, status, s);
+    if (c.bn == 32) return dense_split<QMAJ, PMAJ, F16, B32>(Q, P, m, n, k, c.splits, epi, status, s);
+    if (c.bn == 64) return dense_split<QMAJ, PMAJ, F16, 64>(Q, P, m, n, k, c.splits, epi, status, s);
+    if (c.bn == 128) return dense_split<QMAJ, PMAJ, F16, 128>(Q, P, m, n, k, c.splits, epi, status, s);
+    return dense_split<QMAJ, PMAJ, F16, 256>(Q, P, m, n, k, c.splits, epi, status, s);
 }
 
 }  // namespace tppo

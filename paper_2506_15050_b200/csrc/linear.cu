@@ -227,9 +227,19 @@ __global__ void __launch_bounds__(256) linear_narrow_kernel(const bf16_bits* x, 
     extern __shared__ __align__(16) bf16_bits wt[];           // [NB][kpad], zeros beyond K and N
     pdl_launch();
     pdl_wait();
-    for (int i = threadIdx.x; i < NB * kpad; i += 256) {
-        const int k = i / NB, n = i - k * NB;
-        wt[n * kpad + k] = k < K && n < epi.N ? w[int64_t(k) * ldw + n] : bf16_bits(0);
+    // eight independent loads per trip: the rows of x wait for this
+    for (int i0 = threadIdx.x; i0 < NB * kpad; i0 += 8 * 256) {
+        bf16_bits v[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const int i = i0 + j * 256, k = i / NB, n = i % NB;
+            v[j] = k < K && n < epi.N ? w[int64_t(k) * ldw + n] : bf16_bits(0);
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const int i = i0 + j * 256, k = i / NB, n = i % NB;
+            if (i < NB * kpad) wt[n * kpad + k] = v[j];
+        }
     }
     __syncthreads();
     const int lane = threadIdx.x & 31;
@@ -304,18 +314,46 @@ __global__ void __launch_bounds__(256) linear_repack_kernel(const bf16_bits* src
 }
 
 struct DzArgs {
-    const void* dy; int64_t lddy; int32_t vec_dy;
-    const bf16_bits* pre; int64_t ldp; int32_t vec_p;
+    const void* dy; int64_t lddy;
+    const bf16_bits* pre; int64_t ldp;
     bf16_bits* dz; int64_t ldz;             // NULL: dy itself is the operand
     float* partial;                         // [gridDim.y][N] column sums or NULL
     int64_t M; int32_t N; int32_t act;
     int32_t* status;
 };
 
+// Eight elements as loaded: 16-byte pieces, or (VEC false) element by element with `count` of them there.
+template <class T, bool VEC> struct Eight {
+    static constexpr int kWords = int(sizeof(T)) / 2;
+    uint4 w[VEC ? kWords : 1];
+    float f[VEC ? 1 : 8];
+    __device__ __forceinline__ void load(const T* p, int count) {
+        if constexpr (VEC) {
+#pragma unroll
+            for (int i = 0; i < kWords; ++i) w[i] = reinterpret_cast<const uint4*>(p)[i];
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) f[i] = i < count ? load_f32(p + i) : 0.f;
+        }
+    }
+    __device__ __forceinline__ float get(int i) const {
+        if constexpr (!VEC) {
+            return f[i];
+        } else {
+            const uint4& q = w[i / (8 / kWords)];
+            const uint32_t u[4] = {q.x, q.y, q.z, q.w};
+            if constexpr (sizeof(T) == 4) return __uint_as_float(u[i % 4]);
+            else return i % 2 ? bf16_hi(u[i / 2]) : bf16_lo(u[i / 2]);
+        }
+    }
+};
+
 // dz and the column sums behind dbias.  A block covers 256 columns (8 per thread, 32 threads) and every
-// (8 gridDim.y)-th row from its first, two rows per trip so that four loads are in flight; its eight
-// warps' sums are added in warp order.
-template <class T>
+// (8 gridDim.y)-th row from its first, kDzRows of them per trip with all loads issued before the first
+// is used; its eight warps' sums are added in warp order.  Bound by HBM: 503 MB for 16384 x 5120 bf16.
+constexpr int kDzRows = 4;
+
+template <class T, bool VEC, bool ACT>
 __global__ void __launch_bounds__(256) linear_dz_kernel(const DzArgs a) {
     __shared__ float sums[8][256 + 8];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -323,43 +361,50 @@ __global__ void __launch_bounds__(256) linear_dz_kernel(const DzArgs a) {
     const int count = min(8, a.N - n);
     float acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
     bool bad = false;
-    const T* dy = static_cast<const T*>(a.dy);
+    const T* dy = static_cast<const T*>(a.dy) + n;
+    const bf16_bits* pre = a.pre + n;
     pdl_launch();
     pdl_wait();
     if (count > 0) {
         const int64_t step = int64_t(gridDim.y) * 8;
-        for (int64_t m0 = int64_t(blockIdx.y) * 8 + warp; m0 < a.M; m0 += 2 * step) {
-            float d[2][8], z[2][8];
+        for (int64_t m0 = int64_t(blockIdx.y) * 8 + warp; m0 < a.M; m0 += kDzRows * step) {
+            Eight<T, VEC> d[kDzRows];
+            Eight<bf16_bits, VEC> z[kDzRows];
 #pragma unroll
-            for (int k = 0; k < 2; ++k) {
+            for (int k = 0; k < kDzRows; ++k) {
                 const int64_t m = m0 + k * step;
                 if (m < a.M) {
-                    get8(dy + m * a.lddy + n, d[k], count, a.vec_dy);
-                    if (a.act != TPPO_ACT_NONE) get8(a.pre + m * a.ldp + n, z[k], count, a.vec_p);
+                    d[k].load(dy + m * a.lddy, count);
+                    if (ACT) z[k].load(pre + m * a.ldp, count);
                 }
             }
 #pragma unroll
-            for (int k = 0; k < 2; ++k) {
+            for (int k = 0; k < kDzRows; ++k) {
                 const int64_t m = m0 + k * step;
                 if (m < a.M) {
-                    if (a.act != TPPO_ACT_NONE) {
-                        float slope[8];
-                        act_slopes(a.act, z[k], slope);
+                    float v[8];
 #pragma unroll
-                        for (int i = 0; i < 8; ++i) d[k][i] *= slope[i];
+                    for (int i = 0; i < 8; ++i) v[i] = d[k].get(i);
+                    if (ACT) {
+                        float zv[8], slope[8];
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) zv[i] = z[k].get(i);
+                        act_slopes(a.act, zv, slope);
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) v[i] *= slope[i];
                     }
                     bool fine = true;
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) fine = fine && fabsf(d[k][i]) <= kBf16Max;
+                    for (int i = 0; i < 8; ++i) fine = fine && fabsf(v[i]) <= kBf16Max;
                     if (!fine) {
                         bad = true;
 #pragma unroll
                         for (int i = 0; i < 8; ++i)
-                            if (!(fabsf(d[k][i]) <= kBf16Max)) d[k][i] = 0.f;
+                            if (!(fabsf(v[i]) <= kBf16Max)) v[i] = 0.f;
                     }
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) acc[i] += d[k][i];
-                    if (a.dz) store_vec<8>(a.dz + m * a.ldz + n, d[k]);
+                    for (int i = 0; i < 8; ++i) acc[i] += v[i];
+                    if (a.dz) store_vec<8>(a.dz + m * a.ldz + n, v);
                 }
             }
         }
@@ -376,6 +421,12 @@ __global__ void __launch_bounds__(256) linear_dz_kernel(const DzArgs a) {
         for (int w = 0; w < 8; ++w) t += sums[w][threadIdx.x];
         a.partial[int64_t(blockIdx.y) * a.N + c] = t;
     }
+}
+
+template <class T>
+void (*linear_dz_pick(bool vec, bool act))(const DzArgs) {
+    if (vec) return act ? linear_dz_kernel<T, true, true> : linear_dz_kernel<T, true, false>;
+    return act ? linear_dz_kernel<T, false, true> : linear_dz_kernel<T, false, false>;
 }
 
 // dbias: the partial rows in ascending order within each of a column's 16 strands, then the strands.
@@ -526,16 +577,18 @@ TPPO_API int tppo_linear_bwd(const void* dy, int32_t dy_dtype, int64_t lddy, con
     if (copy_w && (rc = repack(W, w.w, s)) != TPPO_OK) return rc;
     if (make_dz || dbias) {
         DzArgs a{};
-        a.dy = dy; a.lddy = lddy; a.vec_dy = vec_rows(dy, lddy, ds);
-        a.pre = static_cast<const bf16_bits*>(preact); a.ldp = ldp; a.vec_p = vec_rows(preact, ldp, 2);
+        a.dy = dy; a.lddy = lddy;
+        a.pre = static_cast<const bf16_bits*>(preact); a.ldp = ldp;
         a.dz = make_dz ? w.dz : nullptr; a.ldz = pad8(N);
         a.partial = dbias ? w.partial : nullptr;
         a.M = M; a.N = N; a.act = activation; a.status = status;
         const int gx = (N + 255) / 256;
-        int64_t gy = (M + 31) / 32, most = (16 * kNumSms + gx - 1) / gx;      // four rows per warp at least
+        int64_t gy = (M + 31) / 32, most = (6 * kNumSms + gx - 1) / gx;       // four rows per warp at least
         if (gy > most) gy = most;
         if (gy > kDzMaxParts) gy = kDzMaxParts;
-        auto kernel = dy_dtype == TPPO_F32 ? linear_dz_kernel<float> : linear_dz_kernel<bf16_bits>;
+        const bool act = activation != TPPO_ACT_NONE;
+        const bool vec = N % 8 == 0 && vec_rows(dy, lddy, ds) && (!act || vec_rows(preact, ldp, 2));
+        auto kernel = dy_dtype == TPPO_F32 ? linear_dz_pick<float>(vec, act) : linear_dz_pick<bf16_bits>(vec, act);
         TPPO_CUDA_CHECK(launch_dense(kernel, dim3(gx, unsigned(gy)), dim3(256), 0, s, a));
         if (make_dz) { Z.p = w.dz; Z.ld = a.ldz; }
         if (dbias) {
