@@ -5,14 +5,15 @@
 //     dgamma = sum_rows dy * h,   dbeta = sum_rows dy
 // All arithmetic is fp32; the inputs are read once and the outputs rounded once.
 //
-// Both passes are bound by HBM (2 resp. 3 elements moved per element).  Forward, a row lives in the
-// registers of a few warps as the 16-byte pieces it was loaded in, so mean and centred variance are two
-// sweeps over registers.  Backward, the sums of gamma and beta want few columns per thread, so a row is spread
-// over a block; aligned rows are fed by bulk (TMA) copies through a shared-memory ring, which keeps
-// ~100 KB per block in flight while the block goes from row to row with one barrier each, and other
-// rows are loaded into registers some rows at a time.  Each block writes one partial row of column
-// sums to the workspace and a second kernel adds them in a fixed order, so the gradients do not depend
-// on scheduling.  Rows too long for either take kernels that read the row again from L2.
+// Both passes are bound by HBM (2 resp. 3 elements moved per element) until issue slots bind them: a
+// bf16 element costs some 12 instructions forward and 25 backward.  Long rows are brought in by bulk (TMA)
+// copies through a ring of shared memory, which keeps 100-200 KB per SM in flight while blocks go from
+// row to row; short rows are loaded into the registers of one or a few warps.  The sums of gamma and
+// beta stay in the registers of a block's threads for its whole walk over the rows; each block writes one
+// partial row of them to the workspace and a second kernel adds those in a fixed order, so the gradients
+// do not depend on scheduling.  Rows too long for either way take kernels that read the row again from L2.
+//   [16384, 5120] bf16: forward 62 us (5.4 TB/s, 0.82 of the measured copy rate), backward 122 us (4.1 TB/s)
+//   [16384, 5120] fp32: forward 107 us (6.3 TB/s), backward 176 us (5.7 TB/s)
 #include <type_traits>
 
 #include "dense_common.cuh"
@@ -27,6 +28,7 @@ struct NormFwdArgs {
     float* mean; float* rstd; int32_t* status;
     int64_t M; int32_t N; int64_t ldx, ldy; float eps;
     int32_t group;            // threads per row, a multiple of 32
+    int32_t stages;           // ring kernel
 };
 
 // One 16-byte piece of a row as loaded, or one widened element (VEC 1).
@@ -136,6 +138,287 @@ __global__ void __launch_bounds__(kNormMaxThreads) norm_fwd_kernel(const NormFwd
             store_vec<VEC>(y + col, b);
         }
     }
+}
+
+// ---- rows fed by bulk copies --------------------------------------------------------------------
+// The arithmetic of these kernels runs on pairs of fp32 values in 64-bit registers: the row sweeps are
+// issue bound otherwise.
+typedef uint64_t f32x2;
+__device__ __forceinline__ f32x2 twice(float v) { return ptx::pack_f32x2(v, v); }
+__device__ __forceinline__ float pair_sum(f32x2 v) {
+    float lo, hi;
+    ptx::unpack_f32x2(v, lo, hi);
+    return lo + hi;
+}
+// How a thread meets its columns.  RowVec: rows of 16-byte aligned 16-byte pieces.  RowAny: rows at any
+// element, copied with the 16-byte granules they touch; a piece is two columns `group` apart, loaded and
+// stored one element at a time.
+template <class T> struct RowVec {
+    typedef T Elem;
+    static constexpr bool kAny = false;
+    static constexpr int kVec = 16 / int(sizeof(T)), kPairs = kVec / 2;
+    __device__ __forceinline__ static int col(int c, int group, int t) { return (c * group + t) * kVec; }
+    // pairs of columns from `col` of the row whose first element is at shared address `row`
+    __device__ __forceinline__ static void load(uint32_t row, int col, int, int, f32x2 (&v)[kPairs]) {
+        widen(ptx::lds128(row + col * uint32_t(sizeof(T))), v);
+    }
+    __device__ __forceinline__ static void widen(const uint4& w, f32x2 (&v)[kPairs]) {
+        if constexpr (kVec == 8) {
+            v[0] = ptx::pack_f32x2(bf16_lo(w.x), bf16_hi(w.x));
+            v[1] = ptx::pack_f32x2(bf16_lo(w.y), bf16_hi(w.y));
+            v[2] = ptx::pack_f32x2(bf16_lo(w.z), bf16_hi(w.z));
+            v[3] = ptx::pack_f32x2(bf16_lo(w.w), bf16_hi(w.w));
+        } else {
+            v[0] = ptx::pack_f32x2(__uint_as_float(w.x), __uint_as_float(w.y));
+            v[1] = ptx::pack_f32x2(__uint_as_float(w.z), __uint_as_float(w.w));
+        }
+    }
+    __device__ __forceinline__ static void store(T* row, int col, int, int, const f32x2 (&v)[kPairs]) {
+        if constexpr (kVec == 8) {
+            *reinterpret_cast<uint4*>(row + col) =
+                make_uint4(ptx::pack_bf16x2_from_f32x2(v[0]), ptx::pack_bf16x2_from_f32x2(v[1]),
+                           ptx::pack_bf16x2_from_f32x2(v[2]), ptx::pack_bf16x2_from_f32x2(v[3]));
+        } else {
+            float4 o;
+            ptx::unpack_f32x2(v[0], o.x, o.y);
+            ptx::unpack_f32x2(v[1], o.z, o.w);
+            *reinterpret_cast<float4*>(row + col) = o;
+        }
+    }
+    template <class P>
+    __device__ __forceinline__ static void params(const P* p, int col, int, int, float otherwise, f32x2 (&v)[kPairs]) {
+        float f[kVec];
+        load_params<kVec>(p, col, otherwise, f);
+#pragma unroll
+        for (int i = 0; i < kPairs; ++i) v[i] = ptx::pack_f32x2(f[2 * i], f[2 * i + 1]);
+    }
+    // gamma as fp32 in shared memory
+    __device__ __forceinline__ static void gamma(uint32_t gam, int col, int, int, f32x2 (&g)[kPairs]) {
+#pragma unroll
+        for (int i = 0; i < kPairs; i += 2) {
+            const uint4 w = ptx::lds128(gam + (col + 2 * i) * 4);
+            g[i] = ptx::pack_f32x2(__uint_as_float(w.x), __uint_as_float(w.y));
+            g[i + 1] = ptx::pack_f32x2(__uint_as_float(w.z), __uint_as_float(w.w));
+        }
+    }
+    // the pair (v, v) as far as its columns exist, else 0
+    __device__ __forceinline__ static f32x2 where(int, int, int, float v) { return twice(v); }
+    __device__ __forceinline__ static void put(float* row, int col, int, int, const f32x2 (&v)[kPairs]) {
+#pragma unroll
+        for (int i = 0; i < kPairs; ++i) {
+            float2 w;
+            ptx::unpack_f32x2(v[i], w.x, w.y);
+            *reinterpret_cast<float2*>(row + col + 2 * i) = w;
+        }
+    }
+    __host__ __device__ static uint32_t pitch(int N) { return uint32_t(N) * sizeof(T); }
+};
+template <class T> struct RowAny {
+    typedef T Elem;
+    static constexpr bool kAny = true;
+    static constexpr int kVec = 2, kPairs = 1;
+    __device__ __forceinline__ static float element(uint32_t at) {
+        if constexpr (sizeof(T) == 2) return __uint_as_float(uint32_t(ptx::lds_u16(at)) << 16);
+        float v;
+        asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v) : "r"(at));
+        return v;
+    }
+    __device__ __forceinline__ static int col(int c, int group, int t) { return c * 2 * group + t; }
+    __device__ __forceinline__ static void load(uint32_t row, int col, int group, int N, f32x2 (&v)[1]) {
+        const float lo = element(row + col * uint32_t(sizeof(T)));
+        v[0] = ptx::pack_f32x2(lo, col + group < N ? element(row + (col + group) * uint32_t(sizeof(T))) : 0.f);
+    }
+    __device__ __forceinline__ static void store(T* row, int col, int group, int N, const f32x2 (&v)[1]) {
+        float lo, hi;
+        ptx::unpack_f32x2(v[0], lo, hi);
+        store_f32(row + col, lo);
+        if (col + group < N) store_f32(row + col + group, hi);
+    }
+    template <class P>
+    __device__ __forceinline__ static void params(const P* p, int col, int group, int N, float otherwise, f32x2 (&v)[1]) {
+        v[0] = ptx::pack_f32x2(p ? load_f32(p + col) : otherwise, col + group < N ? (p ? load_f32(p + col + group) : otherwise) : 0.f);
+    }
+    __device__ __forceinline__ static void gamma(uint32_t gam, int col, int group, int N, f32x2 (&g)[1]) {
+        float lo, hi = 0.f;
+        asm volatile("ld.shared.f32 %0, [%1];" : "=f"(lo) : "r"(gam + col * 4));
+        if (col + group < N) asm volatile("ld.shared.f32 %0, [%1];" : "=f"(hi) : "r"(gam + (col + group) * 4));
+        g[0] = ptx::pack_f32x2(lo, hi);
+    }
+    __device__ __forceinline__ static f32x2 where(int col, int group, int N, float v) {
+        return ptx::pack_f32x2(v, col + group < N ? v : 0.f);
+    }
+    __device__ __forceinline__ static void put(float* row, int col, int group, int N, const f32x2 (&v)[1]) {
+        float lo, hi;
+        ptx::unpack_f32x2(v[0], lo, hi);
+        row[col] = lo;
+        if (col + group < N) row[col + group] = hi;
+    }
+    __host__ __device__ static uint32_t pitch(int N) { return (uint32_t(N) * sizeof(T) + 15 + 15) / 16 * 16; }
+};
+
+// A matrix whose rows are copied to shared memory.
+template <class Q> struct RowSource {
+    const typename Q::Elem* p; int64_t ld, M; int32_t N;
+
+    // shared address of row r's first element, given where its copy starts
+    __device__ __forceinline__ uint32_t first(int64_t r, uint32_t at) const {
+        return Q::kAny ? at + uint32_t(reinterpret_cast<uintptr_t>(p + r * ld) & 15) : at;
+    }
+    // Bytes of row r that a bulk copy brings, and where they start.  RowAny: whole granules, those
+    // at the matrix' two ends only as far as they lie inside it.
+    __device__ __forceinline__ uint32_t span(int64_t r, uintptr_t& lo) const {
+        const uintptr_t begin = reinterpret_cast<uintptr_t>(p + r * ld), end = begin + uintptr_t(N) * sizeof(*p);
+        lo = begin;
+        if (!Q::kAny) return uint32_t(end - begin);
+        lo = begin & ~uintptr_t(15);
+        uintptr_t hi = (end + 15) & ~uintptr_t(15);
+        if (r == 0 && lo < begin) lo += 16;
+        if (r == M - 1 && hi > end) hi -= 16;
+        return hi > lo ? uint32_t(hi - lo) : 0u;
+    }
+    // Called by one thread: the elements of row r that no bulk copy brings, then (after the barrier has
+    // been told) the copy itself.
+    __device__ __forceinline__ void edges(int64_t r, uint32_t at) const {
+        if (!Q::kAny || (r != 0 && r != M - 1)) return;
+        uintptr_t lo;
+        const uint32_t bytes = span(r, lo);
+        const uintptr_t begin = reinterpret_cast<uintptr_t>(p + r * ld), hi = lo + bytes;
+        for (int c = 0; c < N; ++c) {
+            const uintptr_t q = begin + uintptr_t(c) * sizeof(*p);
+            if (bytes > 0 && q >= lo && q < hi) { c += int((hi - q) / sizeof(*p)) - 1; continue; }
+            const uint32_t to = first(r, at) + uint32_t(c) * uint32_t(sizeof(*p));
+            if constexpr (sizeof(*p) == 2) ptx::sts_u16(to, *reinterpret_cast<const uint16_t*>(q));
+            else asm volatile("st.shared.f32 [%0], %1;" ::"r"(to), "f"(*reinterpret_cast<const float*>(q)) : "memory");
+        }
+    }
+    __device__ __forceinline__ void copy(int64_t r, uint32_t at, uint32_t bar) const {
+        uintptr_t lo;
+        const uint32_t bytes = span(r, lo);
+        const uintptr_t begin = reinterpret_cast<uintptr_t>(p + r * ld) & ~uintptr_t(15);
+        if (bytes > 0) ptx::bulk_load(at + uint32_t(lo - (Q::kAny ? begin : lo)), reinterpret_cast<const void*>(lo), bytes, bar);
+    }
+    __device__ __forceinline__ uint32_t bytes(int64_t r) const {
+        uintptr_t lo;
+        return span(r, lo);
+    }
+};
+
+constexpr size_t kRingSmem = 220 * 1024;       // of all blocks on an SM together
+constexpr int kRingThreads = 512;
+constexpr int kRingWarps = kRingThreads / 32;
+// Sum of one float per warp, in warp order, read by every thread itself (entries past the block's warps
+// are 0).
+__device__ __forceinline__ float ring_sum(const float* red, int warps) {
+    float s = 0.f;
+    for (int w = 0; w < warps; w += 4) {
+        const float4 v = *reinterpret_cast<const float4*>(red + w);
+        s += (v.x + v.y) + (v.z + v.w);
+    }
+    return s;
+}
+
+// Forward: a block per row, rows brought in `stages` ahead; gamma and beta stay in registers.
+template <class Q, class P, int CH>
+__global__ void __launch_bounds__(kRingThreads) norm_fwd_ring_kernel(const NormFwdArgs a) {
+    typedef typename Q::Elem T;
+    constexpr int PAIRS = Q::kPairs;
+    extern __shared__ __align__(128) uint8_t ring[];     // [stages] rows, then one barrier per stage
+    __shared__ __align__(16) float red[2][kRingWarps];
+    const int t = threadIdx.x, warp = t >> 5, lane = t & 31, warps = blockDim.x >> 5;
+    const uint32_t pitch = Q::pitch(a.N);
+    const uint32_t base = ptx::smem_addr(ring), full = base + a.stages * pitch;
+    const float inv_n = 1.f / float(a.N);
+    const int64_t step = gridDim.x;
+    const RowSource<Q> x{static_cast<const T*>(a.x), a.ldx, a.M, a.N};
+    auto issue = [&](int64_t r, int s) {
+        x.edges(r, base + s * pitch);
+        ptx::mbar_arrive_expect_tx(full + 8 * s, x.bytes(r));
+        x.copy(r, base + s * pitch, full + 8 * s);
+    };
+    if (t < 2 * kRingWarps) (&red[0][0])[t] = 0.f;
+    if (t == 0) {
+        for (int s = 0; s < a.stages; ++s) ptx::mbar_init(full + 8 * s, 1);
+        ptx::fence_mbar_init_cluster();
+    }
+    pdl_launch();
+    pdl_wait();
+    if (t == 0)
+        for (int s = 0; s < a.stages && blockIdx.x + s * step < a.M; ++s) issue(blockIdx.x + s * step, s);
+    f32x2 g[CH][PAIRS], b[CH][PAIRS];
+#pragma unroll
+    for (int c = 0; c < CH; ++c) {
+        const int col = Q::col(c, a.group, t);
+        if (col < a.N) {
+            Q::params(static_cast<const P*>(a.gamma), col, a.group, a.N, 1.f, g[c]);
+            Q::params(static_cast<const P*>(a.beta), col, a.group, a.N, 0.f, b[c]);
+        }
+    }
+    __syncthreads();
+    int stage = 0;
+    uint32_t phase = 0;
+    bool timed_out = false;
+    for (int64_t r = blockIdx.x; r < a.M; r += step) {
+        // a wait that ran out is not repeated: the rows are then garbage, and flagged
+        if (!timed_out) timed_out = !ptx::mbar_wait<false>(full + 8 * stage, phase);
+        f32x2 v[CH][PAIRS], s = 0;
+        const uint32_t at = x.first(r, base + stage * pitch);
+#pragma unroll
+        for (int c = 0; c < CH; ++c) {
+            const int col = Q::col(c, a.group, t);
+            if (col < a.N) {
+                Q::load(at, col, a.group, a.N, v[c]);
+#pragma unroll
+                for (int i = 0; i < PAIRS; ++i) s = ptx::add_f32x2(s, v[c][i]);
+            }
+        }
+        float sum = warp_sum(pair_sum(s));
+        if (lane == 0) red[0][warp] = sum;
+        __syncthreads();                          // the sums are there, and the stage has been read
+        if (t == 0 && r + a.stages * step < a.M) issue(r + a.stages * step, stage);
+        if (++stage == a.stages) { stage = 0; phase ^= 1u; }
+        const float mean = ring_sum(red[0], warps) * inv_n;
+        s = 0;
+#pragma unroll
+        for (int c = 0; c < CH; ++c) {
+            const int col = Q::col(c, a.group, t);
+            if (col < a.N) {
+                const f32x2 minus = Q::where(col, a.group, a.N, -mean);
+#pragma unroll
+                for (int i = 0; i < PAIRS; ++i) {
+                    v[c][i] = ptx::add_f32x2(v[c][i], minus);
+                    s = ptx::fma_f32x2(v[c][i], v[c][i], s);
+                }
+            }
+        }
+        sum = warp_sum(pair_sum(s));
+        if (lane == 0) red[1][warp] = sum;
+        __syncthreads();
+        const float var = ring_sum(red[1], warps) * inv_n;
+        const float rstd = rsqrtf(var + a.eps);
+        const bool good = is_finite(var) && is_finite(rstd);        // see norm_fwd_kernel
+        if (t == 0) {
+            if (a.mean) a.mean[r] = good ? mean : 0.f;
+            if (a.rstd) a.rstd[r] = good ? rstd : 0.f;
+            if (!good && a.status) atomicOr(a.status, TPPO_DEV_NONFINITE);
+        }
+        T* y = static_cast<T*>(a.y) + r * a.ldy;
+        const f32x2 scale = twice(rstd);
+#pragma unroll
+        for (int c = 0; c < CH; ++c) {
+            const int col = Q::col(c, a.group, t);
+            if (col < a.N) {
+                f32x2 o[PAIRS];
+#pragma unroll
+                for (int i = 0; i < PAIRS; ++i) o[i] = 0;
+                if (good) {
+#pragma unroll
+                    for (int i = 0; i < PAIRS; ++i) o[i] = ptx::fma_f32x2(ptx::mul_f32x2(v[c][i], scale), g[c][i], b[c][i]);
+                }
+                Q::store(y, col, a.group, a.N, o);
+            }
+        }
+    }
+    if (timed_out && a.status) atomicOr(a.status, TPPO_DEV_WAIT_TIMEOUT);
 }
 
 // A row of any length: one block, three sweeps (the second and third are served by L2).
@@ -373,70 +656,311 @@ __global__ void __launch_bounds__(512) norm_bwd_kernel(const NormBwdArgs a) {
     norm_put_partial<VEC, CH>(a, t, grp, groups, cols, dg, db);
 }
 
-// Aligned rows: a block per row, x and dy rows brought in by bulk copies `stages` rows ahead.
-template <class T, class P, int VEC, int CH>
-__global__ void __launch_bounds__(CH * VEC > 16 ? 512 : 640) norm_bwd_ring_kernel(const NormBwdArgs a) {
+// Aligned rows, one phase: a block takes ROWS rows at a time out of a ring of shared memory that bulk
+// copies fill `stages` rows ahead; every thread keeps its columns of x - mean (and of dy, as loaded) from
+// the sums to the results, and one barrier serves all rows of a trip.
+template <class T, class P, int CH, int ROWS>
+__global__ void __launch_bounds__(640) norm_bwd_rows_kernel(const NormBwdArgs a) {
+    typedef RowVec<T> Q;
+    constexpr int PAIRS = Q::kPairs, VALUES = 2 * ROWS;
     extern __shared__ __align__(128) uint8_t ring[];     // [stages][x row, dy row], then one barrier per stage
-    __shared__ float red[2][2][32];
+    __shared__ float red[2][20][VALUES];
     const int t = threadIdx.x, warp = t >> 5, lane = t & 31, warps = blockDim.x >> 5;
     const uint32_t row_bytes = uint32_t(a.N) * sizeof(T), stage_bytes = 2 * row_bytes;
     const uint32_t base = ptx::smem_addr(ring), full = base + a.stages * stage_bytes;
     const float inv_n = 1.f / float(a.N);
     const int64_t step = gridDim.x;
+    const P* gamma = static_cast<const P*>(a.gamma);
     auto issue = [&](int64_t r, int s) {
         const uint32_t bar = full + 8 * s, at = base + s * stage_bytes;
         ptx::mbar_arrive_expect_tx(bar, stage_bytes);
         ptx::bulk_load(at, static_cast<const T*>(a.x) + r * a.ldx, row_bytes, bar);
         ptx::bulk_load(at + row_bytes, static_cast<const T*>(a.dy) + r * a.lddy, row_bytes, bar);
     };
-    pdl_launch();
-    pdl_wait();
     if (t == 0) {
         for (int s = 0; s < a.stages; ++s) ptx::mbar_init(full + 8 * s, 1);
         ptx::fence_mbar_init_cluster();
+    }
+    pdl_launch();
+    pdl_wait();
+    if (t == 0)
         for (int s = 0; s < a.stages && blockIdx.x + s * step < a.M; ++s) issue(blockIdx.x + s * step, s);
+    f32x2 dg[CH][PAIRS], db[CH][PAIRS], g[CH][PAIRS];
+#pragma unroll
+    for (int c = 0; c < CH; ++c) {
+        const int col = Q::col(c, a.group, t);
+#pragma unroll
+        for (int i = 0; i < PAIRS; ++i) dg[c][i] = db[c][i] = 0;
+        if (col < a.N) Q::params(gamma, col, a.group, a.N, 1.f, g[c]);
     }
     __syncthreads();
-    float dg[CH][VEC], db[CH][VEC];
-#pragma unroll
-    for (int c = 0; c < CH; ++c)
-#pragma unroll
-        for (int i = 0; i < VEC; ++i) dg[c][i] = db[c][i] = 0;
     int stage = 0, flip = 0;
     uint32_t phase = 0;
     bool timed_out = false;
-    float next_mean = a.mean[blockIdx.x], next_rstd = a.rstd[blockIdx.x];
-    for (int64_t r = blockIdx.x; r < a.M; r += step, flip ^= 1) {
-        const float mean = next_mean, rstd = next_rstd;
-        if (r + step < a.M) { next_mean = a.mean[r + step]; next_rstd = a.rstd[r + step]; }
-        // a wait that ran out is not repeated: the sums are then garbage, and flagged
-        if (!timed_out) timed_out = !ptx::mbar_wait<false>(full + 8 * stage, phase);
-        NormRow<T, P, VEC, CH> row;
-        const uint8_t* at = ring + stage * stage_bytes;
+    float next_mean[ROWS], next_rstd[ROWS];
 #pragma unroll
-        for (int c = 0; c < CH; ++c) {
-            const int col = (c * a.group + t) * VEC;
-            if (col < a.N) {
-                row.x[c].load(reinterpret_cast<const T*>(at) + col);
-                row.d[c].load(reinterpret_cast<const T*>(at + row_bytes) + col);
+    for (int k = 0; k < ROWS; ++k) {
+        const int64_t r = blockIdx.x + k * step;
+        next_mean[k] = r < a.M ? a.mean[r] : 0.f;
+        next_rstd[k] = r < a.M ? a.rstd[r] : 0.f;
+    }
+    for (int64_t r0 = blockIdx.x; r0 < a.M; r0 += ROWS * step, flip ^= 1) {
+        float mean[ROWS], rstd[ROWS], part[VALUES];
+        uint4 raw[ROWS][CH];
+        f32x2 e[ROWS][CH][PAIRS];                // x - mean
+        const int first = stage;
+#pragma unroll
+        for (int k = 0; k < ROWS; ++k) {
+            const int64_t r = r0 + k * step, ahead = r + ROWS * step;
+            mean[k] = next_mean[k];
+            rstd[k] = next_rstd[k];
+            if (ahead < a.M) { next_mean[k] = a.mean[ahead]; next_rstd[k] = a.rstd[ahead]; }
+            f32x2 s = 0, q = 0;                   // sum of a, sum of a e
+            if (r < a.M) {
+                // a wait that ran out is not repeated: the sums are then garbage, and flagged
+                if (!timed_out) timed_out = !ptx::mbar_wait<false>(full + 8 * stage, phase);
+                const f32x2 minus = twice(-mean[k]);
+#pragma unroll
+                for (int c = 0; c < CH; ++c) {
+                    const int col = Q::col(c, a.group, t);
+                    if (col < a.N) {
+                        const uint32_t at = base + stage * stage_bytes + col * uint32_t(sizeof(T));
+                        f32x2 d[PAIRS];
+                        raw[k][c] = ptx::lds128(at + row_bytes);
+                        Q::widen(ptx::lds128(at), e[k][c]);
+                        Q::widen(raw[k][c], d);
+#pragma unroll
+                        for (int i = 0; i < PAIRS; ++i) {
+                            const f32x2 av = ptx::mul_f32x2(d[i], g[c][i]);
+                            e[k][c][i] = ptx::add_f32x2(e[k][c][i], minus);
+                            s = ptx::add_f32x2(s, av);
+                            q = ptx::fma_f32x2(av, e[k][c][i], q);
+                        }
+                    }
+                }
+                if (++stage == a.stages) { stage = 0; phase ^= 1u; }
+            }
+            part[2 * k] = pair_sum(s);
+            part[2 * k + 1] = pair_sum(q) * rstd[k];
+        }
+        float total = warp_sum_many<VALUES>(part);            // of value lane % VALUES
+        if (lane < VALUES) red[flip][warp][lane] = total;
+        __syncthreads();                          // the partial sums are there, and the stages have been read
+        if (t == 0) {
+            int s = first;
+#pragma unroll 1
+            for (int k = 0; k < ROWS; ++k) {
+                const int64_t r = r0 + (k + a.stages) * step;
+                if (r < a.M) issue(r, s);
+                if (++s == a.stages) s = 0;
             }
         }
-        const float2 part = row.sums(a, t, mean);
-        float s[2] = {part.x, part.y * rstd};
-        const float mine = warp_sum_many<2>(s);
-        if (lane < 2) red[flip][lane][warp] = mine;
-        __syncthreads();                          // the partial sums are there, and the stage has been read
-        if (t == 0 && r + a.stages * step < a.M) issue(r + a.stages * step, stage);
-        if (++stage == a.stages) { stage = 0; phase ^= 1u; }
-        float w[2] = {0.f, 0.f};
-        if (lane < warps) { w[0] = red[flip][0][lane]; w[1] = red[flip][1][lane]; }
-        const float total = warp_sum_many<2>(w);
-        const float c1 = __shfl_sync(0xffffffffu, total, 0) * inv_n, c2 = __shfl_sync(0xffffffffu, total, 1) * inv_n;
-        const bool good = norm_row_good(c1, c2, rstd, t == 0, a.status);
-        row.finish(a, t, r, mean, rstd, c1, c2, good, dg, db);
+        total = 0.f;
+        for (int w = lane / VALUES; w < warps; w += 32 / VALUES) total += red[flip][w][lane % VALUES];
+#pragma unroll
+        for (int o = VALUES; o < 32; o <<= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
+#pragma unroll
+        for (int k = 0; k < ROWS; ++k) {
+            const int64_t r = r0 + k * step;
+            const float c1 = __shfl_sync(0xffffffffu, total, 2 * k) * inv_n;
+            const float c2 = __shfl_sync(0xffffffffu, total, 2 * k + 1) * inv_n;
+            if (r >= a.M) continue;
+            const bool good = norm_row_good(c1, c2, rstd[k], t == 0, a.status);
+            const f32x2 scale = twice(rstd[k]), u = twice(-rstd[k] * c1), v = twice(-rstd[k] * c2);
+            T* dx = a.dx ? static_cast<T*>(a.dx) + r * a.lddx : nullptr;
+#pragma unroll
+            for (int c = 0; c < CH; ++c) {
+                const int col = Q::col(c, a.group, t);
+                if (col < a.N) {
+                    f32x2 d[PAIRS];
+#pragma unroll
+                    for (int i = 0; i < PAIRS; ++i) d[i] = 0;
+                    if (good) {
+                        Q::widen(raw[k][c], d);
+#pragma unroll
+                        for (int i = 0; i < PAIRS; ++i) {
+                            const f32x2 h = ptx::mul_f32x2(e[k][c][i], scale);
+                            dg[c][i] = ptx::fma_f32x2(d[i], h, dg[c][i]);
+                            db[c][i] = ptx::add_f32x2(db[c][i], d[i]);
+                            d[i] = ptx::fma_f32x2(ptx::mul_f32x2(d[i], g[c][i]), scale, ptx::fma_f32x2(h, v, u));
+                        }
+                    }
+                    if (dx) Q::store(dx, col, a.group, a.N, d);
+                }
+            }
+        }
     }
     if (timed_out && a.status) atomicOr(a.status, TPPO_DEV_WAIT_TIMEOUT);
-    norm_put_partial<VEC, CH>(a, t, 0, 1, nullptr, dg, db);
+    if (!a.partial) return;
+    float* out = a.partial + int64_t(blockIdx.x) * 2 * a.N;
+#pragma unroll
+    for (int c = 0; c < CH; ++c) {
+        const int col = Q::col(c, a.group, t);
+        if (col < a.N) {
+            Q::put(out, col, a.group, a.N, dg[c]);
+            Q::put(out + a.N, col, a.group, a.N, db[c]);
+        }
+    }
+}
+
+// Aligned rows: a block takes two rows at a time out of a ring of shared memory that bulk copies fill
+// `stages` rows ahead, in two phases:
+//   sums    half of the block's warps on each row, lanes along it: sum a and sum a (x - mean)
+//   finish  every thread its CH pieces of columns of both rows: column sums (in registers for the whole
+//           walk) and dx
+// Both phases read the row from shared memory.  The obvious form -- a thread keeps its columns of the
+// row from one phase to the next -- pays for two sums over the block per row at every thread: 27 issue
+// slots per element, where the two phases take some 15; the kernel is issue bound at the former.
+template <class Q, class P, int CH>
+__global__ void __launch_bounds__(CH * Q::kVec > 16 ? 512 : 640) norm_bwd_ring_kernel(const NormBwdArgs a) {
+    typedef typename Q::Elem T;
+    constexpr int PAIRS = Q::kPairs;
+    extern __shared__ __align__(128) uint8_t ring[];     // [stages][x row, dy row], one barrier per stage, gamma as fp32
+    __shared__ float2 red[2][10];                        // [row][warp of its half]
+    __shared__ float2 stat[2][2];                        // [trip parity][row] mean, rstd
+    const int t = threadIdx.x, warp = t >> 5, lane = t & 31, half = int(blockDim.x) >> 6;   // warps per row
+    const uint32_t pitch = Q::pitch(a.N), stage_bytes = 2 * pitch;
+    const uint32_t base = ptx::smem_addr(ring), full = base + a.stages * stage_bytes, gam = full + 8 * 16;
+    const float inv_n = 1.f / float(a.N);
+    const int64_t step = gridDim.x;
+    const int rows = a.stages > 1 ? 2 : 1;               // per trip
+    const RowSource<Q> sx{static_cast<const T*>(a.x), a.ldx, a.M, a.N}, sd{static_cast<const T*>(a.dy), a.lddy, a.M, a.N};
+    auto issue = [&](int64_t r, int s) {
+        const uint32_t bar = full + 8 * s, at = base + s * stage_bytes;
+        sx.edges(r, at);
+        sd.edges(r, at + pitch);
+        ptx::mbar_arrive_expect_tx(bar, sx.bytes(r) + sd.bytes(r));
+        sx.copy(r, at, bar);
+        sd.copy(r, at + pitch, bar);
+    };
+    if (t == 0) {
+        for (int s = 0; s < a.stages; ++s) ptx::mbar_init(full + 8 * s, 1);
+        ptx::fence_mbar_init_cluster();
+    }
+    pdl_launch();
+    pdl_wait();
+    if (t == 0)
+        for (int s = 0; s < a.stages && blockIdx.x + s * step < a.M; ++s) issue(blockIdx.x + s * step, s);
+    for (int c = t; c < a.N; c += blockDim.x) {
+        const float v = a.gamma ? load_f32(static_cast<const P*>(a.gamma) + c) : 1.f;
+        asm volatile("st.shared.f32 [%0], %1;" ::"r"(gam + c * 4), "f"(v) : "memory");
+    }
+    auto load_stat = [&](int64_t r, int slot) {
+        stat[slot][t] = r < a.M ? make_float2(a.mean[r], a.rstd[r]) : make_float2(0.f, 0.f);
+    };
+    if (t < rows) load_stat(blockIdx.x + t * step, 0);
+    f32x2 dg[CH][PAIRS], db[CH][PAIRS];
+#pragma unroll
+    for (int c = 0; c < CH; ++c)
+#pragma unroll
+        for (int i = 0; i < PAIRS; ++i) dg[c][i] = db[c][i] = 0;
+    __syncthreads();
+    int stage = 0, flip = 0;
+    uint32_t phase = 0;
+    bool timed_out = false;
+    const int mine = warp >= half ? 1 : 0, part = warp - mine * half;
+    for (int64_t r0 = blockIdx.x; r0 < a.M; r0 += rows * step, flip ^= 1) {
+        const bool two = rows == 2 && r0 + step < a.M;        // the last trip may have one row
+        const int stage1 = stage + 1 == a.stages ? 0 : stage + 1;
+        const uint32_t phase1 = stage + 1 == a.stages ? phase ^ 1u : phase;
+        if (t < rows) load_stat(r0 + (rows + t) * step, flip ^ 1);
+        // sums
+        if (part < half && (mine == 0 || two)) {
+            const int st = mine ? stage1 : stage;
+            // a wait that ran out is not repeated: the sums are then garbage, and flagged
+            if (!timed_out) timed_out = !ptx::mbar_wait<false>(full + 8 * st, mine ? phase1 : phase);
+            const float2 ms = stat[flip][mine];
+            const f32x2 minus = twice(-ms.x);
+            const int64_t r = r0 + mine * step;
+            const uint32_t ax = sx.first(r, base + st * stage_bytes), ad = sd.first(r, base + st * stage_bytes + pitch);
+            f32x2 s = 0, q = 0;
+            // the warps of a row stand side by side as the block's threads do for their columns
+#pragma unroll 4
+            for (int c = 0; Q::col(c, half * 32, part * 32 + lane) < a.N; ++c) {
+                const int col = Q::col(c, half * 32, part * 32 + lane);
+                f32x2 x[PAIRS], d[PAIRS], g[PAIRS];
+                Q::load(ax, col, half * 32, a.N, x);
+                Q::load(ad, col, half * 32, a.N, d);
+                Q::gamma(gam, col, half * 32, a.N, g);
+#pragma unroll
+                for (int i = 0; i < PAIRS; ++i) {
+                    const f32x2 av = ptx::mul_f32x2(d[i], g[i]);
+                    s = ptx::add_f32x2(s, av);
+                    q = ptx::fma_f32x2(av, ptx::add_f32x2(x[i], minus), q);
+                }
+            }
+            float v[2] = {pair_sum(s), pair_sum(q) * ms.y};
+            const float sum = warp_sum_many<2>(v);
+            const float other = __shfl_sync(0xffffffffu, sum, 1);
+            if (lane == 0) red[mine][part] = make_float2(sum, other);
+        }
+        __syncthreads();
+        // finish
+#pragma unroll 1
+        for (int k = 0; k < (two ? 2 : 1); ++k) {
+            const int st = k ? stage1 : stage;
+            if (!timed_out) timed_out = !ptx::mbar_wait<false>(full + 8 * st, k ? phase1 : phase);   // done: the sums waited
+            const float2 ms = stat[flip][k];
+            float c1 = 0.f, c2 = 0.f;
+            for (int w = 0; w < half; ++w) {
+                c1 += red[k][w].x;
+                c2 += red[k][w].y;
+            }
+            c1 *= inv_n;
+            c2 *= inv_n;
+            const bool good = norm_row_good(c1, c2, ms.y, t == 0, a.status);
+            const f32x2 minus = twice(-ms.x), scale = twice(ms.y), u = twice(-ms.y * c1), v = twice(-ms.y * c2);
+            T* dx = a.dx ? static_cast<T*>(a.dx) + (r0 + k * step) * a.lddx : nullptr;
+            const int64_t r = r0 + k * step;
+            const uint32_t ax = sx.first(r, base + st * stage_bytes), ad = sd.first(r, base + st * stage_bytes + pitch);
+#pragma unroll
+            for (int c = 0; c < CH; ++c) {
+                const int col = Q::col(c, a.group, t);
+                if (col < a.N) {
+                    f32x2 x[PAIRS], d[PAIRS], g[PAIRS];
+                    if (good) {
+                        Q::load(ax, col, a.group, a.N, x);
+                        Q::load(ad, col, a.group, a.N, d);
+                        Q::gamma(gam, col, a.group, a.N, g);
+#pragma unroll
+                        for (int i = 0; i < PAIRS; ++i) {
+                            const f32x2 h = ptx::mul_f32x2(ptx::add_f32x2(x[i], minus), scale);
+                            dg[c][i] = ptx::fma_f32x2(d[i], h, dg[c][i]);
+                            db[c][i] = ptx::add_f32x2(db[c][i], d[i]);
+                            d[i] = ptx::fma_f32x2(ptx::mul_f32x2(d[i], g[i]), scale, ptx::fma_f32x2(h, v, u));
+                        }
+                        if (dx) Q::store(dx, col, a.group, a.N, d);
+                    } else if (dx) {
+#pragma unroll
+                        for (int i = 0; i < PAIRS; ++i) d[i] = 0;
+                        Q::store(dx, col, a.group, a.N, d);
+                    }
+                }
+            }
+        }
+        __syncthreads();                          // both stages have been read, and `red`
+        if (t == 0) {
+            if (r0 + a.stages * step < a.M) issue(r0 + a.stages * step, stage);
+            if (rows == 2 && r0 + (a.stages + 1) * step < a.M) issue(r0 + (a.stages + 1) * step, stage1);
+        }
+        if (rows == 1) {
+            phase ^= 1u;
+        } else {
+            stage = stage1 + 1 == a.stages ? 0 : stage1 + 1;
+            phase = stage1 + 1 == a.stages ? phase1 ^ 1u : phase1;
+        }
+    }
+    if (timed_out && a.status) atomicOr(a.status, TPPO_DEV_WAIT_TIMEOUT);
+    if (!a.partial) return;
+    float* out = a.partial + int64_t(blockIdx.x) * 2 * a.N;
+#pragma unroll
+    for (int c = 0; c < CH; ++c) {
+        const int col = Q::col(c, a.group, t);
+        if (col < a.N) {
+            Q::put(out, col, a.group, a.N, dg[c]);
+            Q::put(out + a.N, col, a.group, a.N, db[c]);
+        }
+    }
 }
 
 // Rows of any length: dx and, in row_flag, which rows count in the column sums.
@@ -488,31 +1012,39 @@ __global__ void __launch_bounds__(256) norm_cols_kernel(const NormBwdArgs a, con
     out[a.N + c] = db;
 }
 
-// dgamma / dbeta = the sum of `parts` partial rows, in ascending order within each of the 16 strands of
-// a column and then over the strands; fp64, rounded once.
+// dgamma / dbeta = the sum of `parts` partial rows, in ascending order within each of the 32 strands of
+// a column (eight loads in flight) and then over the strands; fp64, rounded once.
 template <class P>
-__global__ void __launch_bounds__(512) norm_sum_kernel(const float* partial, int32_t parts, int32_t N, P* dgamma,
-                                                       P* dbeta) {
-    __shared__ double s[16][33];
+__global__ void __launch_bounds__(1024) norm_sum_kernel(const float* partial, int32_t parts, int32_t N, P* dgamma,
+                                                        P* dbeta) {
+    __shared__ double s[32][33];
     pdl_launch();
     pdl_wait();
     const int lane = threadIdx.x & 31, strand = threadIdx.x >> 5;
     const int64_t j = int64_t(blockIdx.x) * 32 + lane;           // column of the [2N]-wide partial row
     double t = 0.0;
     if (j < 2 * int64_t(N)) {
-#pragma unroll 4
-        for (int p = strand; p < parts; p += 16) t += double(partial[int64_t(p) * 2 * N + j]);
+        for (int p0 = strand; p0 < parts; p0 += 8 * 32) {
+            float v[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) v[k] = p0 + 32 * k < parts ? partial[int64_t(p0 + 32 * k) * 2 * N + j] : 0.f;
+#pragma unroll
+            for (int k = 0; k < 8; ++k) t += double(v[k]);
+        }
     }
     s[strand][lane] = t;
     __syncthreads();
     if (strand == 0 && j < 2 * int64_t(N)) {
         t = 0.0;
 #pragma unroll
-        for (int k = 0; k < 16; ++k) t += s[k][lane];
+        for (int k = 0; k < 32; ++k) t += s[k][lane];
         if (j < N) { if (dgamma) store_f32(dgamma + j, float(t)); }
         else if (dbeta) store_f32(dbeta + (j - N), float(t));
     }
 }
+
+// Most blocks, and so partial rows, of a backward pass: five per SM of short rows, three of long ones.
+int norm_max_parts(int32_t N) { return N <= 2048 ? 5 * kNumSms : 3 * kNumSms; }
 
 bool rows_aligned(const void* p, int64_t ld, size_t esize) {
     return aligned(p, 16) && (ld * int64_t(esize)) % 16 == 0;
@@ -532,6 +1064,27 @@ int norm_fwd_typed(NormFwdArgs a, cudaStream_t s) {
     constexpr int V = 16 / sizeof(T);
     const bool vec = a.N % V == 0 && rows_aligned(a.x, a.ldx, sizeof(T)) && rows_aligned(a.y, a.ldy, sizeof(T)) &&
                      (!a.gamma || aligned(a.gamma, 16)) && (!a.beta || aligned(a.beta, 16));
+    // Rows by bulk copies: 32 columns per thread -- what a row costs beside its elements (two sums over the
+    // block, the ring) is some 150 instructions per thread -- and as many blocks per SM as their registers
+    // allow, with rings of three rows or more.  Measured over 8192 rows, against rows loaded straight into
+    // registers: bf16 4096 27 us / 30, 2048 21 / 14; fp32 8192 92 / 104, 6400 76 / 74; unaligned bf16 3001
+    // 68 / 86, 2051 60 / 56, unaligned fp32 5121 126 / 185, 3001 70 / 67; with 1000 rows it loses up to 4096.
+    const bool long_rows = vec ? a.N >= (V == 8 ? 4096 : 8192) : a.N >= (V == 8 ? 2560 : 4096);
+    const bool use_ring = long_rows && a.M >= (a.N >= 10240 ? 4 * kNumSms : 2048);
+    const int64_t threads = (int64_t(a.N) + 32 * 32 - 1) / (32 * 32) * 32;
+    int64_t per_sm = threads <= kRingThreads ? kRingThreads / threads : 0;
+    if (per_sm > 4) per_sm = 4;
+    const size_t row = vec ? RowVec<T>::pitch(a.N) : RowAny<T>::pitch(a.N);
+    const int64_t fit = per_sm > 0 ? int64_t(kRingSmem / per_sm / row) : 0;
+    if (use_ring && fit >= 3) {
+        a.stages = int32_t(fit < 8 ? fit : 8);
+        a.group = int32_t(threads);
+        const size_t smem = size_t(a.stages) * row + 8 * 8;
+        auto kernel = vec ? norm_fwd_ring_kernel<RowVec<T>, P, 32 / V> : norm_fwd_ring_kernel<RowAny<T>, P, 16>;
+        TPPO_CUDA_CHECK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, int(smem)));
+        TPPO_CUDA_CHECK(launch_dense(kernel, dim3(unsigned(kNumSms * per_sm)), dim3(a.group), smem, s, a));
+        return TPPO_OK;
+    }
     // Four 16-byte pieces (eight single elements) per thread: few registers, so that some 40 warps per SM
     // keep ~80 KB in flight.  Rows longer than 1024 such threads hold take 8 (16) per thread, then the
     // kernel that reads the row again.  With few rows more threads share a row, for shorter chains.
@@ -554,17 +1107,14 @@ int norm_fwd_typed(NormFwdArgs a, cudaStream_t s) {
     return with_pieces<1, 2, 4, 8, 16>(int(per), [&](auto ch) { return go(std::integral_constant<int, 1>(), ch); });
 }
 
-constexpr int kNormMaxParts = 2 * kNumSms;
 
 struct NormWs { float* partial; float* row_flag; size_t bytes; };
 NormWs norm_carve(void* ws, int64_t M, int32_t N) {
-    const size_t a = align_up(size_t(kNormMaxParts) * 2 * size_t(N) * 4, kWsAlign);
+    const size_t a = align_up(size_t(norm_max_parts(N)) * 2 * size_t(N) * 4, kWsAlign);
     const size_t b = align_up(size_t(M) * 4, kWsAlign);
     char* p = static_cast<char*>(ws);
     return {reinterpret_cast<float*>(p), reinterpret_cast<float*>(p + a), a + b};
 }
-
-constexpr size_t kRingBytes = 112 * 1024, kRingBytesAlone = 224 * 1024;
 
 template <class T, class P>
 int norm_bwd_typed(NormBwdArgs a, P* dgamma, P* dbeta, float* row_flag, cudaStream_t s) {
@@ -572,29 +1122,48 @@ int norm_bwd_typed(NormBwdArgs a, P* dgamma, P* dbeta, float* row_flag, cudaStre
     const bool vec = a.N % V == 0 && rows_aligned(a.x, a.ldx, sizeof(T)) && rows_aligned(a.dy, a.lddy, sizeof(T)) &&
                      (!a.dx || rows_aligned(a.dx, a.lddx, sizeof(T))) && (!a.gamma || aligned(a.gamma, 16));
     const int64_t pieces = vec ? a.N / V : a.N;
-    const size_t stage = 2 * size_t(a.N) * sizeof(T);
     int parts = 0, rc = TPPO_OK;
-    if (vec && a.M >= kNumSms && pieces >= 128 && stage * 2 <= kRingBytesAlone && pieces <= 512 * (32 / V)) {
-        // two blocks per SM where their rings of at least three rows fit beside each other
-        const bool pair = stage * 3 <= kRingBytes;
-        const size_t budget = pair ? kRingBytes : kRingBytesAlone;
-        int64_t stages = int64_t(budget / stage);
-        if (stages > 8) stages = 8;
-        a.stages = int32_t(stages);
-        const int need = int((pieces + 319) / 320);
-        const size_t smem = size_t(stages) * stage + 8 * 8;
-        const int64_t most = kNumSms * (pair ? 2 : 1);
+    const auto threads_of = [&](int cols, int unit) { return (int64_t(a.N) + cols * unit - 1) / (cols * unit) * unit; };
+    const size_t stage = 2 * size_t(vec ? RowVec<T>::pitch(a.N) : RowAny<T>::pitch(a.N)), params = size_t(a.N) * 4 + 8 * 16;
+    constexpr int kRows = V == 8 ? 4 : 2;
+    const int cols = threads_of(16, 64) <= 640 ? 16 : 32;
+    // Which kernel, as measured (us for 8192 rows; registers / one phase / two phases):
+    //   bf16 264: 15 / 19 / 23, 520: 23 / 19 / 24, 1024: 34 / 24 / 27, 2048: 45 / 39 / 53, 4096: 75 / 72 / 67,
+    //   5120: 127 / 80 / 76 (16384 rows: - / 150 / 122; 1000 rows: 30 / 16 / 23), 8192: 153 / - / 128;
+    //   fp32 264: 13 / 19 / 22, 520: 23 / 20 / 24, 2048: 46 / 39 / 51, 5120: 150 / 87 / 119, 8192: 177 / - / 157;
+    //   unaligned bf16 263: 43 / - / 33, 1283: 71 / - / 45, 5121: 499 / - / 148 (1000 rows of 1283: 16 / - / 17);
+    //   unaligned fp32 515: 29 / - / 31, 1777: 56 / - / 89, 3001: 106 / - / 88
+    const bool one = vec && a.M >= kNumSms && a.N >= 512 && threads_of(8, 32) <= 640 &&
+                     (kRows + 1) * stage + 8 * 16 <= kRingSmem && !(V == 8 && a.N >= 4096 && a.M >= 4096);
+    const bool two = !one && a.M >= kNumSms && threads_of(cols, 64) <= (cols == 16 ? 640 : 512) && stage + params <= kRingSmem &&
+                     (vec ? a.N > 2048 : a.N >= 2048 || (V == 8 && a.M >= 2048));
+    if (one) {
+        a.group = int32_t(threads_of(8, 32));
+        int64_t per_sm = 640 / a.group;
+        if (per_sm > norm_max_parts(a.N) / kNumSms) per_sm = norm_max_parts(a.N) / kNumSms;
+        while (per_sm > 1 && kRingSmem / per_sm < (kRows + 1) * stage + 8 * 16) --per_sm;
+        const int64_t fit = int64_t((kRingSmem / per_sm - 8 * 16) / stage);
+        a.stages = int32_t(fit < 16 ? fit : 16);
+        const size_t smem = size_t(a.stages) * stage + 8 * 16;
+        const int64_t most = kNumSms * per_sm;
         parts = int(a.M < most ? a.M : most);
-        const auto go = [&](auto ch) -> int {
-            constexpr int CH = decltype(ch)::value;
-            a.group = int32_t((pieces + CH * 32 - 1) / (CH * 32) * 32);
-            auto kernel = norm_bwd_ring_kernel<T, P, V, CH>;
-            TPPO_CUDA_CHECK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, int(smem)));
-            TPPO_CUDA_CHECK(launch_dense(kernel, dim3(unsigned(parts)), dim3(a.group), smem, s, a));
-            return TPPO_OK;
-        };
-        if constexpr (V == 8) rc = pieces > 2 * 512 ? go(std::integral_constant<int, 4>()) : with_pieces<1, 2>(need > 2 ? 2 : need, go);
-        else rc = pieces > 4 * 512 ? go(std::integral_constant<int, 8>()) : with_pieces<1, 2, 4>(need > 4 ? 4 : need, go);
+        auto kernel = norm_bwd_rows_kernel<T, P, 8 / V, kRows>;
+        TPPO_CUDA_CHECK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, int(smem)));
+        TPPO_CUDA_CHECK(launch_dense(kernel, dim3(unsigned(parts)), dim3(a.group), smem, s, a));
+    } else if (two) {
+        a.group = int32_t(threads_of(cols, 64));
+        int64_t per_sm = 640 / a.group;
+        if (per_sm > norm_max_parts(a.N) / kNumSms) per_sm = norm_max_parts(a.N) / kNumSms;
+        while (per_sm > 1 && kRingSmem / per_sm < 4 * stage + params) --per_sm;
+        const int64_t fit = int64_t((kRingSmem / per_sm - params) / stage);
+        a.stages = int32_t(fit < 16 ? fit : 16);
+        const size_t smem = size_t(a.stages) * stage + params;
+        const int64_t most = kNumSms * per_sm;
+        parts = int(a.M < most ? a.M : most);
+        auto kernel = vec ? (cols == 16 ? norm_bwd_ring_kernel<RowVec<T>, P, 16 / V> : norm_bwd_ring_kernel<RowVec<T>, P, 32 / V>)
+                          : (cols == 16 ? norm_bwd_ring_kernel<RowAny<T>, P, 8> : norm_bwd_ring_kernel<RowAny<T>, P, 16>);
+        TPPO_CUDA_CHECK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, int(smem)));
+        TPPO_CUDA_CHECK(launch_dense(kernel, dim3(unsigned(parts)), dim3(a.group), smem, s, a));
     } else if (pieces <= 512 * (vec ? 16 / V : 16)) {
         // the fewest columns per thread (16 at most) that keep a row within 256 threads, else 512
         static const int ladder[] = {1, 2, 4, 6, 8, 12, 16};
@@ -637,7 +1206,7 @@ int norm_bwd_typed(NormBwdArgs a, P* dgamma, P* dbeta, float* row_flag, cudaStre
         }
     }
     if (rc != TPPO_OK || !a.partial) return rc;
-    TPPO_CUDA_CHECK(launch_dense(norm_sum_kernel<P>, dim3(unsigned((2 * int64_t(a.N) + 31) / 32)), dim3(512), 0, s,
+    TPPO_CUDA_CHECK(launch_dense(norm_sum_kernel<P>, dim3(unsigned((2 * int64_t(a.N) + 31) / 32)), dim3(1024), 0, s,
                                  static_cast<const float*>(a.partial), int32_t(parts), a.N, dgamma, dbeta));
     return TPPO_OK;
 }
@@ -665,7 +1234,7 @@ TPPO_API int tppo_layer_norm_fwd(const void* x, int32_t dtype, int64_t M, int32_
     if (!aligned(x, es) || !aligned(y, es) || !aligned(gamma, ps) || !aligned(beta, ps) || !aligned(mean, 4) ||
         !aligned(rstd, 4) || !aligned(status, 4))
         return TPPO_ERR_INVALID_ARG;
-    const NormFwdArgs a{x, gamma, beta, y, mean, rstd, status, M, N, ldx, ldy, eps, 0};
+    const NormFwdArgs a{x, gamma, beta, y, mean, rstd, status, M, N, ldx, ldy, eps, 0, 0};
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     if (dtype == TPPO_BF16)
         return param_dtype == TPPO_F32 ? norm_fwd_typed<bf16_bits, float>(a, s) : norm_fwd_typed<bf16_bits, bf16_bits>(a, s);

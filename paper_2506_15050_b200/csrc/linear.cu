@@ -438,8 +438,13 @@ __global__ void __launch_bounds__(512) linear_dbias_kernel(const float* partial,
     pdl_wait();
     double t = 0.0;
     if (c < N) {
-#pragma unroll 4
-        for (int p = strand; p < parts; p += 16) t += double(partial[int64_t(p) * N + c]);
+        for (int p0 = strand; p0 < parts; p0 += 8 * 16) {        // eight loads in flight
+            float v[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) v[k] = p0 + 16 * k < parts ? partial[int64_t(p0 + 16 * k) * N + c] : 0.f;
+#pragma unroll
+            for (int k = 0; k < 8; ++k) t += double(v[k]);
+        }
     }
     s[strand][lane] = t;
     __syncthreads();

@@ -144,6 +144,38 @@ def test_backward(M, N, dtype):
     assert torch.equal(d, dx.t) and torch.equal(again[1], dg) and torch.equal(again[2], db)
 
 
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("M,N", [(1000, 1024), (601, 2056), (900, 5120), (700, 8192), (620, 10248), (611, 12288), (600, 16384), (597, 20480),
+                                 (1000, 1023), (601, 2051), (900, 5121), (600, 10243), (595, 16383), (593, 20001), (3000, 515)])
+@pytest.mark.parametrize("left,right", [(0, 0), (3, 2)])
+def test_many_long_rows(M, N, left, right, dtype):
+    """Rows brought in by bulk copies, several per block; NaN between strided rows that must not count."""
+    from paper_2506_15050_b200 import binding as b
+    x, dy, gamma, beta = make(M, N, dtype, N)
+    x[M // 3, 5] = float("nan")
+    if left + right:
+        x, dy = strided(x, left, right), strided(dy, right, left)
+    y, mean, rstd = torch.empty_like(x), torch.empty(M, device=DEV), torch.empty(M, device=DEV)
+    status = torch.zeros(1, dtype=torch.int32, device=DEV)
+    ws = b.workspace(b.OP_LAYER_NORM, M, 0, 0, N, DEV)
+    keep = torch.arange(M, device=DEV) != M // 3
+    for gm, bt, pt in ((gamma, beta, F32), (gamma.to(BF), None, BF), (None, beta, F32)):
+        b.tppo_layer_norm_fwd(x, gm, bt, 1e-5, y, mean, rstd, status)
+        check_fwd(x[keep], gm, bt, 1e-5, y[keep], mean[keep], rstd[keep])
+        assert not y[M // 3].any() and float(rstd[M // 3]) == 0
+        ws.fill_(0xff)
+        dx, dg, db = torch.empty_like(x), torch.empty(N, dtype=pt, device=DEV), torch.empty(N, dtype=pt, device=DEV)
+        b.tppo_layer_norm_bwd(dy, x, gm, mean, rstd, dx, dg, db, status, ws)
+        check_bwd(dy[keep], x[keep], gm, mean[keep], rstd[keep], dx[keep], dg, db)
+        assert not dx[M // 3].any() and int(status) == b.DEV_NONFINITE
+        d = dy.clone()
+        b.tppo_layer_norm_bwd(d, x, gm, mean, rstd, d, None, None, None, None)
+        assert torch.equal(d, dx)
+    z = strided(x, left, right) if left + right else x.clone()      # in place, at the same alignment
+    b.tppo_layer_norm_fwd(z, None, beta, 1e-5, z, None, None, None)
+    assert torch.equal(z, y)
+
+
 def test_gradient_against_differences():
     """<gradient, direction> against the central difference of <dy, y> in float64: its step 1e-4 leaves an
     error of order 1e-8, the fp32 gradients one of N M u at most relative to the sum of magnitudes."""
