@@ -490,10 +490,11 @@ enum {
  *   preact    [M, N] bf16 out or NULL: z, which tppo_linear_bwd needs unless the activation is
  *             TPPO_ACT_NONE
  *   workspace tppo_workspace_bytes(TPPO_OP_LINEAR, M, K, n_max, N) bytes.  The forward call uses it
- *             only to copy an operand whose rows are not 16-byte aligned, and may be given NULL when x
- *             and weight are aligned.  The query counts those copies when K or N is not a multiple of
- *             8, or when n_max is 1: pass that for misaligned views (base or ld) of matrices whose
- *             sizes are multiples of 8.
+ *             only to copy an operand whose rows are not 16-byte aligned -- or, where that makes a large
+ *             product faster and there is room, not whole 128-byte lines -- and may be given NULL when x
+ *             and weight are 16-byte aligned.  The query counts those copies when K or N is not a
+ *             multiple of 64, or when n_max is 1: pass that for misaligned views (base or ld) of
+ *             matrices whose sizes are multiples of 64.
  * Products are bf16, sums and the epilogue fp32, y is rounded once.  An element whose z or y is not
  * finite or leaves the range of the type it is stored in is written 0 and raises TPPO_DEV_NONFINITE.
  * No output may overlap x or weight.

@@ -138,6 +138,8 @@ __device__ __forceinline__ void dense_tile(const DenseShape& g, int t, int& mt, 
 // Epi: bool outside(row, col) const -- nothing at or beyond (row, col) belongs to the matrix
 //      void load(row, col, Loads&) const -- starts reading what the elements (row, col .. col+7) need
 //      void operator()(row, col, float (&v)[8], const Loads&) const -- finishes them
+//      kRows; if true also bool by_rows() const (uniform), void leave(...) const: operator() but for the
+//      stores of the main output, whose values it leaves in v, and void put(row, col, float) const
 // Rows and columns may lie outside the matrix.
 template <int AMAJ, int BMAJ, bool F16, bool SYM, class Epi>
 __global__ void __launch_bounds__(kDenseThreads, 1)
@@ -235,8 +237,12 @@ dense_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
                 for (int j = 0; j < 8; ++j)
                     ptx::sts128(sw + lane * 128 + ((j ^ (lane & 7)) << 4), make_uint4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]));
                 __syncwarp();
+                // rows of the output that take no 16-byte stores: the finished values go back to shared memory,
+                // and a warp stores 32 consecutive elements at a time
+                bool by_rows = false;
+                if constexpr (Epi::kRows) by_rows = epi.by_rows();
                 // one copy of the epilogue's code: unrolled it does not fit the instruction cache (134 us
-                // instead of XX for 16384 x 5120 outputs of a 128-long contraction)
+                // instead of 113 for 16384 x 5120 outputs of a 128-long contraction)
 #pragma unroll 1
                 for (int it = 0; it < trips; ++it) {
                     const typename Epi::Loads mine = ahead[0];
@@ -262,7 +268,30 @@ dense_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
                             w[i] = __uint_as_float(u);
                         }
                     }
+                    if constexpr (Epi::kRows) {
+                        if (by_rows) {
+                            const int r = it * 8 + (lane >> 2), j = (lane & 3) * 2;
+                            epi.leave(row_of(it), col_of(it), w, mine);
+                            ptx::sts128(sw + r * 128 + ((j ^ (r & 7)) << 4),
+                                        make_uint4(__float_as_uint(w[0]), __float_as_uint(w[1]), __float_as_uint(w[2]), __float_as_uint(w[3])));
+                            ptx::sts128(sw + r * 128 + (((j + 1) ^ (r & 7)) << 4),
+                                        make_uint4(__float_as_uint(w[4]), __float_as_uint(w[5]), __float_as_uint(w[6]), __float_as_uint(w[7])));
+                            continue;
+                        }
+                    }
                     epi(row_of(it), col_of(it), w, mine);
+                }
+                if constexpr (Epi::kRows) {
+                    if (by_rows) {
+                        __syncwarp();
+#pragma unroll 8
+                        for (int r = 0; r < 32; ++r) {
+                            float f;
+                            asm volatile("ld.shared.f32 %0, [%1];" : "=f"(f)
+                                         : "r"(sw + r * 128 + (((lane >> 2) ^ (r & 7)) << 4) + (lane & 3) * 4));
+                            epi.put(m0 + r, n0 + lane, f);
+                        }
+                    }
                 }
             }
             umma::fence_before_thread_sync();

@@ -141,6 +141,7 @@ struct EpiLinear {
     int32_t vec_y, vec_r, vec_p, vec_b;
     int32_t* status;
 
+    static constexpr bool kRows = true;
     struct Loads { uint4 r; };                    // the residual, where one 16-byte load fetches it
 
     __device__ __forceinline__ bool outside(int64_t m, int n) const { return m >= M || n >= N; }
@@ -148,7 +149,14 @@ struct EpiLinear {
     __device__ __forceinline__ void load(int64_t m, int n, Loads& l) const {
         if (fast(m, n)) l.r = *reinterpret_cast<const uint4*>(residual + m * ldr + n);
     }
-    __device__ __forceinline__ void operator()(int64_t m, int n, float (&v)[8], const Loads& l) const {
+    __device__ __forceinline__ bool by_rows() const { return !vec_y; }
+    __device__ __forceinline__ void put(int64_t m, int n, float v) const {
+        if (outside(m, n)) return;
+        if (y_f32) static_cast<float*>(y)[m * ldy + n] = v;
+        else store_f32(static_cast<bf16_bits*>(y) + m * ldy + n, v);
+    }
+    // v: the sums in, y out; stores the pre-activation
+    __device__ __forceinline__ void leave(int64_t m, int n, float (&v)[8], const Loads& l) const {
         if (outside(m, n)) return;
         const int count = min(8, N - n);
         if (bias) {
@@ -184,8 +192,15 @@ struct EpiLinear {
             if (bad && status) atomicOr(status, TPPO_DEV_NONFINITE);
         }
         if (pre) put8(pre + m * ldp + n, v, count, vec_p);
-        if (y_f32) put8(static_cast<float*>(y) + m * ldy + n, o, count, vec_y);
-        else put8(static_cast<bf16_bits*>(y) + m * ldy + n, o, count, vec_y);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = o[i];
+    }
+    __device__ __forceinline__ void operator()(int64_t m, int n, float (&v)[8], const Loads& l) const {
+        if (outside(m, n)) return;
+        leave(m, n, v, l);
+        const int count = min(8, N - n);
+        if (y_f32) put8(static_cast<float*>(y) + m * ldy + n, v, count, vec_y);
+        else put8(static_cast<bf16_bits*>(y) + m * ldy + n, v, count, vec_y);
     }
 };
 
@@ -193,10 +208,15 @@ struct EpiLinear {
 struct EpiStore {
     bf16_bits* out; int64_t ld; int64_t M; int32_t N; int32_t vec;
     int32_t* status;
+    static constexpr bool kRows = true;
     struct Loads {};
     __device__ __forceinline__ bool outside(int64_t m, int n) const { return m >= M || n >= N; }
     __device__ __forceinline__ void load(int64_t, int, Loads&) const {}
-    __device__ __forceinline__ void operator()(int64_t m, int n, float (&v)[8], const Loads&) const {
+    __device__ __forceinline__ bool by_rows() const { return !vec; }
+    __device__ __forceinline__ void put(int64_t m, int n, float v) const {
+        if (!outside(m, n)) store_f32(out + m * ld + n, v);
+    }
+    __device__ __forceinline__ void leave(int64_t m, int n, float (&v)[8], const Loads&) const {
         if (outside(m, n)) return;
         const int count = min(8, N - n);
         bool fine = true;
@@ -209,7 +229,11 @@ struct EpiStore {
                 if (!(fabsf(v[i]) <= kBf16Max)) { bad |= i < count; v[i] = 0.f; }
             if (bad && status) atomicOr(status, TPPO_DEV_NONFINITE);
         }
-        put8(out + m * ld + n, v, count, vec);
+    }
+    __device__ __forceinline__ void operator()(int64_t m, int n, float (&v)[8], const Loads& l) const {
+        if (outside(m, n)) return;
+        leave(m, n, v, l);
+        put8(out + m * ld + n, v, min(8, N - n), vec);
     }
 };
 
@@ -297,19 +321,61 @@ int linear_narrow(const DenseOperand& X, const DenseOperand& W, const EpiLinear&
     return TPPO_OK;
 }
 
-// Copies a bf16 matrix into rows of ldo elements (a multiple of 8), eight elements per thread; the
-// tail of a row is filled with zeros.
+// Copies a bf16 matrix into rows of ldo elements (whole lines), eight elements per thread; the tail of a
+// row is filled with zeros.  A row that starts at any element is read in aligned 16-byte granules, two per
+// eight elements, shifted together; granules that reach beyond the matrix are read by element.
 __global__ void __launch_bounds__(256) linear_repack_kernel(const bf16_bits* src, int64_t ld, int64_t rows, int32_t cols,
                                                             bf16_bits* dst, int64_t ldo) {
     pdl_launch();
     pdl_wait();
-    const int64_t per = ldo / 8, total = rows * per;
-    for (int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x; i < total; i += int64_t(gridDim.x) * 256) {
-        const int64_t r = i / per;
-        const int c = int(i - r * per) * 8;
-        float v[8];
-        get8(src + r * ld + c, v, min(8, cols - c), false);
-        store_vec<8>(dst + r * ldo + c, v);
+    const int per = int(ldo / 8);
+    const uintptr_t begin = reinterpret_cast<uintptr_t>(src), end = begin + uintptr_t((rows - 1) * ld + cols) * 2;
+    const int64_t total = rows * per;
+    for (int64_t i0 = int64_t(blockIdx.x) * 256; i0 < total; i0 += int64_t(gridDim.x) * 256) {
+        // the first row of the block's pieces by one 64-bit division, the thread's by a 32-bit one
+        const int64_t r0 = i0 / per;
+        const uint32_t in = uint32_t(i0 - r0 * per) + threadIdx.x;
+        const int64_t r = r0 + in / uint32_t(per);
+        if (r < rows) {
+            const int c = int(in % uint32_t(per)) * 8, count = min(8, cols - c);
+            uint4 o = make_uint4(0u, 0u, 0u, 0u);
+            if (count > 0) {
+                const bf16_bits* p = src + r * ld + c;
+                const uintptr_t at = reinterpret_cast<uintptr_t>(p), low = at & ~uintptr_t(15);
+                const int shift = int(at & 15);
+                if (low >= begin && low + (shift ? 32 : 16) <= end) {
+                    const uint4 a = *reinterpret_cast<const uint4*>(low);
+                    const uint4 b = shift ? *reinterpret_cast<const uint4*>(low + 16) : a;
+                    uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+                    if (shift & 8) {
+#pragma unroll
+                        for (int i = 0; i < 6; ++i) w[i] = w[i + 2];
+                    }
+                    if (shift & 4) {
+#pragma unroll
+                        for (int i = 0; i < 5; ++i) w[i] = w[i + 1];
+                    }
+                    if (shift & 2) {
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) w[i] = __funnelshift_r(w[i], w[i + 1], 16);
+                    }
+                    if (count < 8) {
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            if (2 * i >= count) w[i] = 0u;
+                            else if (2 * i + 1 >= count) w[i] &= 0xffffu;
+                        }
+                    }
+                    o = make_uint4(w[0], w[1], w[2], w[3]);
+                } else {
+                    uint32_t h[8];
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) h[i] = i < count ? p[i] : 0u;
+                    o = make_uint4(h[0] | h[1] << 16, h[2] | h[3] << 16, h[4] | h[5] << 16, h[6] | h[7] << 16);
+                }
+            }
+            *reinterpret_cast<uint4*>(dst + r * ldo + c) = o;
+        }
     }
 }
 
@@ -456,17 +522,20 @@ __global__ void __launch_bounds__(512) linear_dbias_kernel(const float* partial,
     }
 }
 
-int64_t pad8(int64_t n) { return (n + 7) / 8 * 8; }
+// Row stride of the workspace's matrices: whole 128-byte lines.  At other pitches the tensor copies'
+// 128-byte rows straddle two lines each: 4096 x 3000 x 3000 takes 95 us with rows of 6000 bytes and 58 us
+// with rows of 6016.
+int64_t pad64(int64_t n) { return (n + 63) / 64 * 64; }
 
 constexpr int kDzMaxParts = 256;
 
-// Workspace: dz, the partial sums of dbias, and (only where the sizes cannot meet TMA's alignment, or
-// the caller asked for them) padded copies of x and W.
+// Workspace: dz, the partial sums of dbias, and (only where the sizes do not make whole lines, or the
+// caller asked for them) padded copies of x and W.
 struct LinearWs { bf16_bits* dz; float* partial; bf16_bits* x; bf16_bits* w; size_t plain, bytes; };
 LinearWs linear_carve(void* ws, int64_t M, int32_t K, int32_t N) {
     char* p = static_cast<char*>(ws);
-    const size_t dz = align_up(size_t(M) * pad8(N) * 2, kWsAlign), part = align_up(size_t(kDzMaxParts) * N * 4, kWsAlign);
-    const size_t x = align_up(size_t(M) * pad8(K) * 2, kWsAlign), w = align_up(size_t(K) * pad8(N) * 2, kWsAlign);
+    const size_t dz = align_up(size_t(M) * pad64(N) * 2, kWsAlign), part = align_up(size_t(kDzMaxParts) * N * 4, kWsAlign);
+    const size_t x = align_up(size_t(M) * pad64(K) * 2, kWsAlign), w = align_up(size_t(K) * pad64(N) * 2, kWsAlign);
     LinearWs r;
     r.dz = reinterpret_cast<bf16_bits*>(p);
     r.partial = reinterpret_cast<float*>(p + dz);
@@ -478,13 +547,19 @@ LinearWs linear_carve(void* ws, int64_t M, int32_t K, int32_t N) {
 }
 
 bool tma_rows(const void* p, int64_t ld) { return aligned(p, 16) && ld % 8 == 0; }
+// Whether a [rows, cols] operand that TMA takes as it is is better copied to whole lines first: a product
+// loses a fifth of its time (at 1.2 PFLOP/s) to each operand with straddling rows, a copy moves four bytes
+// per element at 5 TB/s after 2 us.
+bool worth_copying(const void* p, int64_t ld, int64_t rows, int64_t cols, double flops) {
+    return (ld % 64 != 0 || !aligned(p, 128)) && 0.2 * flops / 1.2e15 > double(rows) * double(cols) * 4 / 5e12 + 2e-6;
+}
 bool vec_rows(const void* p, int64_t ld, size_t esize) { return aligned(p, 16) && (ld * int64_t(esize)) % 16 == 0; }
 
 int repack(DenseOperand& o, bf16_bits* dst, cudaStream_t s) {
-    const int64_t ldo = pad8(o.cols), total = o.rows * (ldo / 8);
-    const int64_t blocks = (total + 255) / 256;
-    TPPO_CUDA_CHECK(launch_dense(linear_repack_kernel, dim3(unsigned(blocks < 16 * kNumSms ? blocks : 16 * kNumSms)), dim3(256),
-                                 0, s, static_cast<const bf16_bits*>(o.p), o.ld, o.rows, int32_t(o.cols), dst, ldo));
+    const int64_t ldo = pad64(o.cols);
+    const int64_t blocks = (o.rows * (ldo / 8) + 255) / 256;
+    TPPO_CUDA_CHECK(launch_dense(linear_repack_kernel, dim3(unsigned(blocks < 16 * kNumSms ? blocks : 16 * kNumSms)), dim3(256), 0, s,
+                                 static_cast<const bf16_bits*>(o.p), o.ld, o.rows, int32_t(o.cols), dst, ldo));
     o.p = dst;
     o.ld = ldo;
     return TPPO_OK;
@@ -497,7 +572,7 @@ bool act_known(int32_t a) { return a >= TPPO_ACT_NONE && a <= TPPO_ACT_SILU; }
 size_t linear_workspace_bytes(int64_t M, int32_t K, int32_t N, bool copies) {
     if (K < 1 || N < 1) return 0;
     const LinearWs w = linear_carve(nullptr, M, K, N);
-    return copies || K % 8 || N % 8 ? w.bytes : w.plain;
+    return copies || K % 64 || N % 64 ? w.bytes : w.plain;
 }
 
 }  // namespace tppo
@@ -519,11 +594,16 @@ TPPO_API int tppo_linear_fwd(const void* x, int64_t ldx, const void* weight, int
         !aligned(y, ys) || !aligned(preact, 2) || !aligned(status, 4))
         return TPPO_ERR_INVALID_ARG;
     const int nb = N <= 1 ? 1 : N <= 2 ? 2 : N <= 4 ? 4 : 8;
-    const bool narrow = N <= kNarrowMaxN && size_t(nb) * pad8(K) * 2 <= size_t(kNarrowMaxSmem);
-    const bool copy_x = !narrow && !tma_rows(x, ldx), copy_w = !narrow && !tma_rows(weight, ldw);
+    const bool narrow = N <= kNarrowMaxN && size_t(nb) * ((K + 7) / 8 * 8) * 2 <= size_t(kNarrowMaxSmem);
+    bool copy_x = !narrow && !tma_rows(x, ldx), copy_w = !narrow && !tma_rows(weight, ldw);
     const LinearWs w = linear_carve(workspace, M, K, N);
-    if ((copy_x || copy_w) && (!workspace || !aligned(workspace, kWsAlign) || workspace_bytes < w.bytes))
-        return TPPO_ERR_WORKSPACE;
+    const bool room = workspace && aligned(workspace, kWsAlign) && workspace_bytes >= w.bytes;
+    if ((copy_x || copy_w) && !room) return TPPO_ERR_WORKSPACE;
+    if (room && !narrow) {
+        const double flops = 2.0 * double(M) * K * N;
+        copy_x = copy_x || worth_copying(x, ldx, M, K, flops);
+        copy_w = copy_w || worth_copying(weight, ldw, K, N, flops);
+    }
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     DenseOperand X{x, M, K, ldx}, W{weight, K, N, ldw};
     int rc;
@@ -570,11 +650,18 @@ TPPO_API int tppo_linear_bwd(const void* dy, int32_t dy_dtype, int64_t lddy, con
     }
     if (!dx && !dweight && !dbias) return TPPO_OK;
     const bool products = dx || dweight;
-    const bool copy_x = dweight && !tma_rows(x, ldx), copy_w = dx && !tma_rows(weight, ldw);
-    const bool make_dz = products && (activation != TPPO_ACT_NONE || dy_dtype == TPPO_F32 || !tma_rows(dy, lddy));
+    bool copy_x = dweight && !tma_rows(x, ldx), copy_w = dx && !tma_rows(weight, ldw);
+    bool make_dz = products && (activation != TPPO_ACT_NONE || dy_dtype == TPPO_F32 || !tma_rows(dy, lddy));
     const LinearWs w = linear_carve(workspace, M, K, N);
     const size_t need = copy_x || copy_w ? w.bytes : make_dz || dbias ? w.plain : 0;
-    if (need && (!workspace || !aligned(workspace, kWsAlign) || workspace_bytes < need)) return TPPO_ERR_WORKSPACE;
+    const size_t have = workspace && aligned(workspace, kWsAlign) ? workspace_bytes : 0;
+    if (need > have) return TPPO_ERR_WORKSPACE;
+    const double flops = 2.0 * double(M) * K * N;
+    if (have >= w.bytes) {
+        copy_x = copy_x || (dweight && worth_copying(x, ldx, M, K, flops));
+        copy_w = copy_w || (dx && worth_copying(weight, ldw, K, N, flops));
+    }
+    if (have >= w.plain && products && !make_dz) make_dz = worth_copying(dy, lddy, M, N, (dx && dweight ? 2 : 1) * flops);
 
     DenseOperand X{x, M, K, ldx}, W{weight, K, N, ldw}, Z{dy, M, N, lddy};
     int rc;
@@ -584,7 +671,7 @@ TPPO_API int tppo_linear_bwd(const void* dy, int32_t dy_dtype, int64_t lddy, con
         DzArgs a{};
         a.dy = dy; a.lddy = lddy;
         a.pre = static_cast<const bf16_bits*>(preact); a.ldp = ldp;
-        a.dz = make_dz ? w.dz : nullptr; a.ldz = pad8(N);
+        a.dz = make_dz ? w.dz : nullptr; a.ldz = pad64(N);
         a.partial = dbias ? w.partial : nullptr;
         a.M = M; a.N = N; a.act = activation; a.status = status;
         const int gx = (N + 255) / 256;

@@ -48,8 +48,8 @@ __device__ __forceinline__ uint32_t pack_f16x2(float lo, float hi) {
 __device__ __forceinline__ float2 unpack_f16x2(uint32_t w) {
     return __half22float2(*reinterpret_cast<const __half2*>(&w));
 }
-// Eight stored operand elements: value * 2^13 in fp16 (rows of workspace matrices are padded to
-// multiples of eight elements).
+// Eight stored operand elements: value * 2^13 in fp16 (rows of workspace matrices are padded, so the
+// eight always exist).
 __device__ __forceinline__ void store_operand(f16_bits* p, const float (&v)[8]) {
     *reinterpret_cast<uint4*>(p) =
         make_uint4(pack_f16x2(v[0] * kScale, v[1] * kScale), pack_f16x2(v[2] * kScale, v[3] * kScale),
@@ -81,49 +81,64 @@ struct PrepareArgs {
     int32_t* status;
 };
 
-// Momentum and U.  VEC elements per thread (8 where rows are aligned, else 1).  A gradient or momentum
-// element that is not finite counts as 0.
+// Momentum and U.  A warp takes 32 * VEC consecutive elements of a row (VEC 8 where rows are aligned, else
+// 1); a gradient or momentum element that is not finite counts as 0.  14 bytes move per element of a
+// bf16 gradient, and nothing else bounds it.
 template <class T, int VEC>
 __global__ void __launch_bounds__(kMuonThreads) muon_prepare_kernel(const PrepareArgs a) {
     __shared__ double red[kMuonThreads / 32];
     pdl_launch();
     pdl_wait();
-    const int64_t per = (a.C + VEC - 1) / VEC, total = a.R * per;
+    constexpr int kRun = VEC == 1 ? 4 : 1;       // 32-element runs per trip: loads in flight
+    const int lane = threadIdx.x & 31;
+    const uint32_t per = uint32_t((a.C + 32 * VEC * kRun - 1) / (32 * VEC * kRun));
+    const int64_t warps = int64_t(gridDim.x) * (kMuonThreads / 32), total = a.R * per;
     double sum = 0.0;
     bool bad = false;
-    for (int64_t i = int64_t(blockIdx.x) * kMuonThreads + threadIdx.x; i < total; i += int64_t(gridDim.x) * kMuonThreads) {
+    for (int64_t i = int64_t(blockIdx.x) * (kMuonThreads / 32) + (threadIdx.x >> 5); i < total; i += warps) {
         const int64_t r = i / per;
-        const int64_t c = (i - r * per) * VEC;
-        float g[VEC];
-        load_vec<VEC>(static_cast<const T*>(a.grad) + r * a.ldg + c, g);
+        const int c0 = int(uint32_t(i - r * per)) * 32 * VEC * kRun + lane * VEC;
+        float g[kRun][VEC], m[kRun][VEC];
+        float* pm = a.momentum + r * a.ldm;
 #pragma unroll
-        for (int k = 0; k < VEC; ++k)
-            if (!is_finite(g[k])) { g[k] = 0.f; bad = true; }
-        if (a.momentum) {
-            float m[VEC];
-            float* pm = a.momentum + r * a.ldm + c;
-            load_vec<VEC>(pm, m);
-#pragma unroll
-            for (int k = 0; k < VEC; ++k) {
-                m[k] = fmaf(a.mu, m[k], g[k]);
-                if (!is_finite(m[k])) { m[k] = 0.f; bad = true; }
-                g[k] = a.nesterov ? fmaf(a.mu, m[k], g[k]) : m[k];
-                if (!is_finite(g[k])) { g[k] = 0.f; bad = true; }
+        for (int q = 0; q < kRun; ++q) {
+            const int c = c0 + q * 32;
+            if (c < a.C) {
+                load_vec<VEC>(static_cast<const T*>(a.grad) + r * a.ldg + c, g[q]);
+                if (a.momentum) load_vec<VEC>(pm + c, m[q]);
             }
-            store_vec<VEC>(pm, m);
         }
-        float s = 0.f;
-        double wide = 0.0;
 #pragma unroll
-        for (int k = 0; k < VEC; ++k) s = fmaf(g[k], g[k], s);
-        // fp32 squares under- or overflow far from 1; those few go in fp64
-        if (s > 1e-30f && s < 1e30f) wide = double(s);
-        else {
+        for (int q = 0; q < kRun; ++q) {
+            const int c = c0 + q * 32;
+            if (c < a.C) {
 #pragma unroll
-            for (int k = 0; k < VEC; ++k) wide += double(g[k]) * double(g[k]);
+                for (int k = 0; k < VEC; ++k)
+                    if (!is_finite(g[q][k])) { g[q][k] = 0.f; bad = true; }
+                if (a.momentum) {
+#pragma unroll
+                    for (int k = 0; k < VEC; ++k) {
+                        m[q][k] = fmaf(a.mu, m[q][k], g[q][k]);
+                        if (!is_finite(m[q][k])) { m[q][k] = 0.f; bad = true; }
+                        g[q][k] = a.nesterov ? fmaf(a.mu, m[q][k], g[q][k]) : m[q][k];
+                        if (!is_finite(g[q][k])) { g[q][k] = 0.f; bad = true; }
+                    }
+                    store_vec<VEC>(pm + c, m[q]);
+                }
+                float s = 0.f;
+#pragma unroll
+                for (int k = 0; k < VEC; ++k) s = fmaf(g[q][k], g[q][k], s);
+                // fp32 squares under- or overflow far from 1; those few go in fp64
+                double wide = double(s);
+                if (!(s > 1e-30f && s < 1e30f)) {
+                    wide = 0.0;
+#pragma unroll
+                    for (int k = 0; k < VEC; ++k) wide += double(g[q][k]) * double(g[q][k]);
+                }
+                sum += wide;
+                store_vec<VEC>(a.x32 + r * a.ldx + c, g[q]);
+            }
         }
-        sum += wide;
-        store_vec<VEC>(a.x32 + r * a.ldx + c, g);
     }
     sum = block_sum(sum, red);
     if (threadIdx.x == 0) a.partial[blockIdx.x] = sum;
@@ -155,6 +170,7 @@ __global__ void __launch_bounds__(kMuonThreads) muon_normalise_kernel(const doub
 // A = X X^T.  With `diag` its diagonal goes there and the stored operand has zeros instead.
 struct EpiA {
     f16_bits* out; int64_t ld; int32_t m; float* diag;
+    static constexpr bool kRows = false;
     struct Loads {};
     __device__ __forceinline__ void load(int64_t, int, Loads&) const {}
     __device__ __forceinline__ bool outside(int64_t r, int c) const { return r >= m || c >= m; }
@@ -172,6 +188,7 @@ struct EpiA {
 // B = b A + c A^2, from the accumulated square of the stored A.
 struct EpiB {
     const f16_bits* a; f16_bits* out; int64_t ld; int32_t m; const float* diag_a; float* diag_b;
+    static constexpr bool kRows = false;
     struct Loads { uint4 a; };
     __device__ __forceinline__ void load(int64_t r, int c, Loads& l) const {
         if (!outside(r, c)) l.a = *reinterpret_cast<const uint4*>(a + r * ld + c);
@@ -205,6 +222,7 @@ struct EpiX {
     const float* diag_b;
     bf16_bits* update; int64_t ldu; int32_t vec_u; float scale;
     int64_t R; int32_t C;
+    static constexpr bool kRows = false;
     struct Loads { float4 lo, hi; };
     __device__ __forceinline__ bool outside(int64_t r, int c) const { return r >= R || c >= C; }
     __device__ __forceinline__ void load(int64_t r, int c, Loads& l) const {
@@ -250,8 +268,10 @@ struct MuonWs {
 MuonWs muon_carve(void* ws, int64_t R, int32_t C) {
     MuonWs w;
     const int64_t m = R < C ? R : C;
-    w.ldx = (int64_t(C) + 7) / 8 * 8;
-    w.lda = (m + 7) / 8 * 8;
+    // rows of whole 128-byte lines: at a pitch of 6000 bytes the tensor copies' 128-byte rows straddle two
+    // lines each, and the products of a 3000 x 3000 matrix take 2.3 times as long
+    w.ldx = (int64_t(C) + 63) / 64 * 64;
+    w.lda = (m + 63) / 64 * 64;
     char* p = static_cast<char*>(ws);
     size_t at = 0;
     auto take = [&](size_t bytes) {
@@ -274,8 +294,8 @@ MuonWs muon_carve(void* ws, int64_t R, int32_t C) {
 
 template <class T>
 int muon_prepare(const PrepareArgs& a, bool vec, int* parts, cudaStream_t s) {
-    const int64_t items = a.R * (vec ? (a.C + 7) / 8 : a.C);
-    const int64_t blocks = (items + kMuonThreads - 1) / kMuonThreads;
+    const int run = vec ? 32 * 8 : 32 * 4;        // elements per warp and trip
+    const int64_t blocks = (a.R * ((a.C + run - 1) / run) + kMuonThreads / 32 - 1) / (kMuonThreads / 32);
     *parts = int(blocks < kMuonMaxBlocks ? blocks : kMuonMaxBlocks);
     auto kernel = vec ? muon_prepare_kernel<T, 8> : muon_prepare_kernel<T, 1>;
     TPPO_CUDA_CHECK(launch_dense(kernel, dim3(unsigned(*parts)), dim3(kMuonThreads), 0, s, a));

@@ -27,7 +27,8 @@ def workspace(M, K, N, copies=0):
 SIZES = [(1, 1, 1), (1, 8, 8), (1, 64, 256), (1, 5120, 640), (2, 5, 3), (5, 63, 7), (16, 64, 128), (17, 65, 129), (31, 200, 33),
          (33, 515, 130), (64, 128, 64), (65, 72, 1000), (100, 1000, 40), (128, 64, 264), (129, 8, 257), (250, 77, 510),
          (1000, 136, 1), (777, 300, 2), (1001, 515, 777), (300, 1024, 1024),
-         (2500, 72, 2000), (2561, 130, 2049), (19000, 24, 130)]
+         (2500, 72, 2000), (2561, 130, 2049), (19000, 24, 130),
+         (5000, 1000, 1000), (4100, 1004, 1501)]
 
 
 @pytest.mark.parametrize("M,K,N", SIZES)
@@ -225,7 +226,10 @@ def test_refusals_on_the_device():
     x, w = torch.ones((4, 24), dtype=BF, device=DEV), torch.ones((24, 40), dtype=BF, device=DEV)
     y = torch.full((4, 40), 7.0, dtype=BF, device=DEV)
     with pytest.raises(b.TppoError) as e:                  # misaligned rows need the copies' workspace
-        b.tppo_linear_fwd(strided(x, 1, 0), w, None, 0, None, y, None, None, workspace(4, 24, 40))
+        b.tppo_linear_fwd(strided(x, 1, 0), w, None, 0, None, y, None, None, None)
+    assert e.value.status == 2
+    with pytest.raises(b.TppoError) as e:                  # and so does dz
+        b.tppo_linear_bwd(y, x, w, b.ACT_RELU, y, x.clone(), None, None, None, None)
     assert e.value.status == 2
     for bad in (lambda: b.tppo_linear_fwd(x, w, None, 9, None, y, None, None, None),):
         with pytest.raises(b.TppoError) as e:
