@@ -4,7 +4,8 @@
  * The library computes the part of a Truncated-PPO training step that the paper's method changes:
  * EGAE advantages over possibly truncated responses (Section 3.1, Eq. 6), the policy / value
  * token filter (Section 3.2), and the two losses restricted to the surviving tokens (Eq. 1 and
- * Eq. 4-5; the advantage, policy and value steps of Algorithm 1).
+ * Eq. 4-5; the advantage, policy and value steps of Algorithm 1).  Beside it stand the dense operators
+ * of the block around the LM-head: layer norm, linear with a fused epilogue, orthogonalised update.
  *
  * Conventions that hold for every entry point
  *   - Every array pointer is a DEVICE pointer unless the comment says "host".  The caller owns all
@@ -98,7 +99,8 @@ void tppo_test_hooks(int32_t lookback_polls, int32_t no_publish);
 
 /*
  * Workspace bytes needed by one call of `op`.  N = packed tokens, B = sequences / segments,
- * n_max = capacity of the selected-token list, V = vocabulary (0 where it does not apply).
+ * n_max = capacity of the selected-token list, V = vocabulary (0 where it does not apply); the dense
+ * operators say at each entry point what the four stand for.
  * Returns 0 for an unknown op.  Host call, launches nothing.
  */
 size_t tppo_workspace_bytes(int op, int64_t N, int32_t B, int64_t n_max, int32_t V);

@@ -1,5 +1,6 @@
 """B200-native T-PPO token-selective update path (EGAE scan, token compaction, fused
-log-softmax + clipped-surrogate loss with gradient, value loss).
+log-softmax + clipped-surrogate loss with gradient, value loss) and the dense operators around its
+LM-head (layer norm, linear with a fused epilogue, orthogonalised update).
 
 The arithmetic runs in hand-written sm_100a CUDA kernels behind a C ABI (include/tppo.h);
 ``binding`` marshals torch device tensors into that ABI and ``synth`` draws the synthetic
