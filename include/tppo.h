@@ -434,7 +434,8 @@ int tppo_advance_batch(const int32_t *seq_begin, const int32_t *prompt_len,
  *     is handled.
  *   - `status` ([1] int32, may be NULL) is ADDED TO: bits are set, never cleared, so one word that the
  *     caller zeroes can collect the calls of a whole step.
- * Reductions are done in a fixed order: results are run-to-run identical.
+ * Reductions are done in a fixed order: results are run-to-run identical.  Row and column counts up to
+ * 2^30 (TPPO_ERR_UNSUPPORTED beyond).
  */
 
 /*
@@ -499,7 +500,7 @@ enum {
  *             matrices whose sizes are multiples of 64.
  * Products are bf16, sums and the epilogue fp32, y is rounded once.  An element whose z or y is not
  * finite or leaves the range of the type it is stored in is written 0 and raises TPPO_DEV_NONFINITE.
- * No output may overlap x or weight.
+ * No output may overlap x, weight or another output.
  * The first call on a device looks up the driver's tensor-map encoder (TPPO_ERR_CUDA if absent).
  */
 int tppo_linear_fwd(const void *x, int64_t ldx, const void *weight, int64_t ldw,
@@ -514,7 +515,7 @@ int tppo_linear_fwd(const void *x, int64_t ldx, const void *weight, int64_t ldw,
  *   dy [M, N] of `dy_dtype`; preact [M, N] bf16 from the forward call (not read, and may be NULL, for
  *   TPPO_ACT_NONE); act' of TPPO_ACT_RELU at 0 is 0
  *   dx [M, K] bf16, dweight [K, N] bf16, dbias [N] of `bias_dtype`: each may be NULL; overwritten, not
- *   accumulated.  No output may overlap an input.
+ *   accumulated.  No output may overlap an input or another output.
  *   x may be NULL without dweight, weight without dx
  *   workspace as for tppo_linear_fwd: for dz, the partial sums of dbias and operand copies; may be
  *   NULL when none is needed (TPPO_ACT_NONE, aligned bf16 operands, no dbias)

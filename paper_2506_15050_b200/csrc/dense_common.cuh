@@ -76,6 +76,9 @@ __device__ __forceinline__ bool is_finite(float v) { return fabsf(v) <= kFltMax;
 
 inline bool is_finite_host(float v) { return v - v == 0.f; }
 
+// Rows and columns beyond this would take tile and column arithmetic past 32 bits.
+constexpr int64_t kDenseMaxSize = int64_t(1) << 30;
+
 // The two halves of a programmatic dependent launch: the primary lets its dependent start, the
 // dependent waits for the primary's memory.
 __device__ __forceinline__ void pdl_launch() { asm volatile("griddepcontrol.launch_dependents;"); }

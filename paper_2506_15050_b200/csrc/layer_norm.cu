@@ -1225,9 +1225,10 @@ using namespace tppo;
 TPPO_API int tppo_layer_norm_fwd(const void* x, int32_t dtype, int64_t M, int32_t N, int64_t ldx, const void* gamma,
                                  const void* beta, int32_t param_dtype, float eps, void* y, int64_t ldy, float* mean,
                                  float* rstd, int32_t* status, void* stream) {
-    if (M < 0 || N < 1 || M > 0x7fffffffll || ldx < N || ldy < N || !(eps >= 0.f) || !is_finite_host(eps))
+    if (M < 0 || N < 1 || ldx < N || ldy < N || !(eps >= 0.f) || !is_finite_host(eps))
         return TPPO_ERR_INVALID_ARG;
     if (!type_known(dtype) || ((gamma || beta) && !type_known(param_dtype))) return TPPO_ERR_INVALID_ARG;
+    if (M > kDenseMaxSize || N > kDenseMaxSize) return TPPO_ERR_UNSUPPORTED;
     if (M == 0) return TPPO_OK;
     if (!x || !y) return TPPO_ERR_INVALID_ARG;
     const size_t es = type_size(dtype), ps = type_size(param_dtype);
@@ -1246,8 +1247,9 @@ TPPO_API int tppo_layer_norm_bwd(const void* dy, const void* x, int32_t dtype, i
                                  const float* rstd, void* dx, int64_t lddx, void* dgamma, void* dbeta, int32_t* status,
                                  void* workspace, size_t workspace_bytes, void* stream) {
     const bool params = dgamma || dbeta;
-    if (M < 0 || N < 1 || M > 0x7fffffffll || lddy < N || ldx < N || (dx && lddx < N)) return TPPO_ERR_INVALID_ARG;
+    if (M < 0 || N < 1 || lddy < N || ldx < N || (dx && lddx < N)) return TPPO_ERR_INVALID_ARG;
     if (!type_known(dtype) || ((gamma || params) && !type_known(param_dtype))) return TPPO_ERR_INVALID_ARG;
+    if (M > kDenseMaxSize || N > kDenseMaxSize) return TPPO_ERR_UNSUPPORTED;
     if (M > 0 && (!dy || !x || !mean || !rstd)) return TPPO_ERR_INVALID_ARG;
     const size_t es = type_size(dtype), ps = type_size(param_dtype);
     if (!aligned(dy, es) || !aligned(x, es) || !aligned(dx, es) || !aligned(gamma, ps) || !aligned(dgamma, ps) ||

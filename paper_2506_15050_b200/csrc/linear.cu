@@ -570,7 +570,7 @@ bool act_known(int32_t a) { return a >= TPPO_ACT_NONE && a <= TPPO_ACT_SILU; }
 }  // namespace
 
 size_t linear_workspace_bytes(int64_t M, int32_t K, int32_t N, bool copies) {
-    if (K < 1 || N < 1) return 0;
+    if (K < 1 || N < 1 || M > kDenseMaxSize || K > kDenseMaxSize || N > kDenseMaxSize) return 0;
     const LinearWs w = linear_carve(nullptr, M, K, N);
     return copies || K % 64 || N % 64 ? w.bytes : w.plain;
 }
@@ -583,11 +583,12 @@ TPPO_API int tppo_linear_fwd(const void* x, int64_t ldx, const void* weight, int
                              const void* bias, int32_t bias_dtype, int32_t activation, const void* residual, int64_t ldr,
                              void* y, int32_t y_dtype, int64_t ldy, void* preact, int64_t ldp, int32_t* status,
                              void* workspace, size_t workspace_bytes, void* stream) {
-    if (M < 0 || M > 0x7fffffffll || K < 1 || N < 1 || ldx < K || ldw < N || ldy < N || (residual && ldr < N) ||
+    if (M < 0 || K < 1 || N < 1 || ldx < K || ldw < N || ldy < N || (residual && ldr < N) ||
         (preact && ldp < N) || !act_known(activation))
         return TPPO_ERR_INVALID_ARG;
     if ((y_dtype != TPPO_BF16 && y_dtype != TPPO_F32) || (bias && bias_dtype != TPPO_BF16 && bias_dtype != TPPO_F32))
         return TPPO_ERR_INVALID_ARG;
+    if (M > kDenseMaxSize || K > kDenseMaxSize || N > kDenseMaxSize) return TPPO_ERR_UNSUPPORTED;
     if (M == 0) return TPPO_OK;
     const size_t ys = y_dtype == TPPO_F32 ? 4 : 2, bs = bias_dtype == TPPO_F32 ? 4 : 2;
     if (!x || !weight || !y || !aligned(x, 2) || !aligned(weight, 2) || !aligned(bias, bs) || !aligned(residual, 2) ||
@@ -632,11 +633,12 @@ TPPO_API int tppo_linear_bwd(const void* dy, int32_t dy_dtype, int64_t lddy, con
                              int64_t ldw, int64_t M, int32_t K, int32_t N, int32_t activation, const void* preact,
                              int64_t ldp, void* dx, int64_t lddx, void* dweight, int64_t lddw, void* dbias,
                              int32_t bias_dtype, int32_t* status, void* workspace, size_t workspace_bytes, void* stream) {
-    if (M < 0 || M > 0x7fffffffll || K < 1 || N < 1 || lddy < N || ldx < K || ldw < N || (dx && lddx < K) ||
+    if (M < 0 || K < 1 || N < 1 || lddy < N || ldx < K || ldw < N || (dx && lddx < K) ||
         (dweight && lddw < N) || !act_known(activation) || (activation != TPPO_ACT_NONE && ldp < N))
         return TPPO_ERR_INVALID_ARG;
     if ((dy_dtype != TPPO_BF16 && dy_dtype != TPPO_F32) || (dbias && bias_dtype != TPPO_BF16 && bias_dtype != TPPO_F32))
         return TPPO_ERR_INVALID_ARG;
+    if (M > kDenseMaxSize || K > kDenseMaxSize || N > kDenseMaxSize) return TPPO_ERR_UNSUPPORTED;
     const size_t ds = dy_dtype == TPPO_F32 ? 4 : 2, bs = bias_dtype == TPPO_F32 ? 4 : 2;
     if ((M > 0 && (!dy || (activation != TPPO_ACT_NONE && !preact) || (dx && !weight) || (dweight && !x))) ||
         !aligned(dy, ds) || !aligned(x, 2) || !aligned(weight, 2) || !aligned(preact, 2) || !aligned(dx, 2) ||

@@ -305,7 +305,7 @@ int muon_prepare(const PrepareArgs& a, bool vec, int* parts, cudaStream_t s) {
 }  // namespace
 
 size_t muon_workspace_bytes(int64_t R, int32_t C) {
-    return R < 1 || C < 1 || R > 0x7fffffffll ? 0 : muon_carve(nullptr, R, C).bytes;
+    return R < 1 || C < 1 || R > kDenseMaxSize || C > kDenseMaxSize ? 0 : muon_carve(nullptr, R, C).bytes;
 }
 
 }  // namespace tppo
@@ -316,10 +316,11 @@ TPPO_API int tppo_muon_orthogonalize(const void* grad, int32_t grad_dtype, int64
                                      int64_t R, int32_t C, float mu, int32_t nesterov, float eps, int32_t steps, float scale,
                                      void* update, int64_t ldu, int32_t* status, void* workspace, size_t workspace_bytes,
                                      void* stream) {
-    if (R < 0 || R > 0x7fffffffll || C < 1 || ldg < C || ldu < C || (momentum && ldm < C) || steps < 1 || steps > 16 ||
+    if (R < 0 || C < 1 || ldg < C || ldu < C || (momentum && ldm < C) || steps < 1 || steps > 16 ||
         !(eps >= 0.f) || !is_finite_host(eps) || !is_finite_host(scale) || (momentum && !is_finite_host(mu)) ||
         (grad_dtype != TPPO_BF16 && grad_dtype != TPPO_F32))
         return TPPO_ERR_INVALID_ARG;
+    if (R > kDenseMaxSize || C > kDenseMaxSize) return TPPO_ERR_UNSUPPORTED;
     if (R == 0) return TPPO_OK;
     const size_t gs = grad_dtype == TPPO_F32 ? 4 : 2;
     if (!grad || !update || !aligned(grad, gs) || !aligned(update, 2) || !aligned(momentum, 4) || !aligned(status, 4))

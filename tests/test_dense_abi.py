@@ -4,7 +4,7 @@ import ctypes
 import pytest
 
 VP, I32, I64, F32, SZ = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_float, ctypes.c_size_t
-INVALID, WORKSPACE = 1, 2
+INVALID, WORKSPACE, UNSUPPORTED = 1, 2, 3
 LAYER_NORM, LINEAR, MUON = 5, 6, 7
 
 
@@ -60,7 +60,8 @@ def test_layer_norm_refusals(lib, p):
         (dict(x=None), INVALID), (dict(y=None), INVALID), (dict(M=-1), INVALID), (dict(N=0), INVALID), (dict(ldx=15), INVALID),
         (dict(ldy=15), INVALID), (dict(dtype=2), INVALID), (dict(pdtype=2), INVALID), (dict(eps=-1e-5), INVALID),
         (dict(eps=float("nan")), INVALID), (dict(eps=float("inf")), INVALID), (dict(x=a + 1), INVALID), (dict(gamma=a + 2), INVALID),
-        (dict(mean=a + 2), INVALID), (dict(status=a + 1), INVALID), (dict(M=1 << 31), INVALID)])
+        (dict(mean=a + 2), INVALID), (dict(status=a + 1), INVALID), (dict(M=(1 << 30) + 1), UNSUPPORTED),
+        (dict(N=(1 << 30) + 1, ldx=1 << 31, ldy=1 << 31), UNSUPPORTED)])
     assert lib.tppo_layer_norm_fwd(*[dict(good, M=0, x=None, y=None)[k] for k in args]) == 0
     args = "dy x dtype M N lddy ldx gamma pdtype mean rstd dx lddx dgamma dbeta status ws bytes stream".split()
     good = dict(dy=a, x=a, dtype=1, M=4, N=16, lddy=16, ldx=16, gamma=a, pdtype=1, mean=a, rstd=a, dx=a, lddx=16, dgamma=a, dbeta=a,
@@ -85,7 +86,7 @@ def test_linear_refusals(lib, p):
         (dict(ldp=23), INVALID), (dict(act=5), INVALID), (dict(act=-1), INVALID), (dict(ydtype=2), INVALID), (dict(bdtype=2), INVALID),
         (dict(x=a + 1), INVALID), (dict(y=a + 2, ydtype=1), INVALID), (dict(bias=a + 2, bdtype=1), INVALID), (dict(status=a + 2), INVALID),
         (dict(x=a + 2), WORKSPACE), (dict(ldw=25), WORKSPACE), (dict(ldw=25, ws=a, bytes=256), WORKSPACE),
-        (dict(ldw=25, ws=a + 8, bytes=1 << 30), WORKSPACE)])
+        (dict(ldw=25, ws=a + 8, bytes=1 << 30), WORKSPACE), (dict(M=1 << 31), UNSUPPORTED), (dict(K=(1 << 30) + 8, ldx=1 << 31), UNSUPPORTED)])
     assert lib.tppo_linear_fwd(*[dict(good, M=0, x=None, w=None, y=None)[k] for k in args]) == 0
     args = "dy dtype lddy x ldx w ldw M K N act pre ldp dx lddx dw lddw db bdtype status ws bytes stream".split()
     good = dict(dy=a, dtype=0, lddy=24, x=a, ldx=16, w=a, ldw=24, M=4, K=16, N=24, act=2, pre=a, ldp=24, dx=a, lddx=16, dw=a, lddw=24, db=a,

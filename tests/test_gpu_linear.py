@@ -24,7 +24,7 @@ def workspace(M, K, N, copies=0):
     return ws
 
 
-SIZES = [(1, 1, 1), (1, 8, 8), (1, 64, 256), (1, 5120, 640), (2, 5, 3), (5, 63, 7), (16, 64, 128), (17, 65, 129), (31, 200, 33),
+SIZES = [(1, 1, 1), (200, 1, 100), (5000, 1, 2000), (1, 8, 8), (1, 64, 256), (1, 5120, 640), (2, 5, 3), (5, 63, 7), (16, 64, 128), (17, 65, 129), (31, 200, 33),
          (33, 515, 130), (64, 128, 64), (65, 72, 1000), (100, 1000, 40), (128, 64, 264), (129, 8, 257), (250, 77, 510),
          (1000, 136, 1), (777, 300, 2), (1001, 515, 777), (300, 1024, 1024),
          (2500, 72, 2000), (2561, 130, 2049), (19000, 24, 130),
@@ -219,6 +219,24 @@ def test_no_rows():
     b.tppo_linear_bwd(dy, x, w, 0, None, None, dw.t, db, None, None)
     assert not dw.t.any() and not db.any()
     dw.check()
+
+
+def test_outputs_beyond_32_bits():
+    """More than 2^31 elements of y, dx and dz; whole numbers, the last rows compared."""
+    from paper_2506_15050_b200 import binding as b
+    M, K, N, g = 530_001, 64, 4096, gen(2)
+    x, w = whole(g, M, K), whole(g, K, N)
+    y, ws = torch.empty((M, N), dtype=BF, device=DEV), workspace(M, K, N)
+    b.tppo_linear_fwd(x, w, None, b.ACT_RELU, None, y, None, None, ws)
+    for s in (slice(0, 300), slice(524_200, 524_400), slice(M - 300, M)):
+        assert torch.equal(y[s], torch.relu(x[s].double() @ w.double()).to(BF))
+    # backward: the kept pre-activation may be any bf16 matrix with the same signs
+    dx, dw, db = torch.empty_like(x), torch.empty_like(w), torch.empty(N, device=DEV)
+    dy = torch.ones((1, N), dtype=BF, device=DEV).expand(M, N).contiguous()
+    b.tppo_linear_bwd(dy, x, w, b.ACT_RELU, y, dx, dw, db, None, ws)
+    for s in (slice(0, 300), slice(524_200, 524_400), slice(M - 300, M)):
+        assert torch.equal(dx[s], ((y[s] > 0).double() @ w.double().t()).to(BF))
+    assert torch.equal(db.double(), (y > 0).sum(0).double())
 
 
 def test_refusals_on_the_device():
