@@ -138,8 +138,11 @@ __device__ __forceinline__ void dense_tile(const DenseShape& g, int t, int& mt, 
 // Epi: bool outside(row, col) const -- nothing at or beyond (row, col) belongs to the matrix
 //      void load(row, col, Loads&) const -- starts reading what the elements (row, col .. col+7) need
 //      void operator()(row, col, float (&v)[8], const Loads&) const -- finishes them
-//      kRows; if true also bool by_rows() const (uniform), void leave(...) const: operator() but for the
-//      stores of the main output, whose values it leaves in v, and void put(row, col, float) const
+// and for the persistent kernel, whose lanes go down their eight columns eight rows at a time (without
+// SYM): Cursor, what stays the same on the way and where it has got to; open(Cursor&, row, col);
+// fetch(cursor, trip, Loads&) as load; finish<true>(cursor, v, loads) as operator(), moving on.
+// kRows: whether there are bool by_rows() const (uniform), finish<false> -- all but the stores of the
+// main output, whose values stay in v -- and put(row, col, float), which stores one.
 // Rows and columns may lie outside the matrix.
 template <int AMAJ, int BMAJ, bool F16, bool SYM, class Epi>
 __global__ void __launch_bounds__(kDenseThreads, 1)
@@ -225,8 +228,15 @@ dense_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
                 auto row_of = [&](int it) { return (it < 4 ? m0 : int64_t(n0)) + (it & 3) * 8 + (lane >> 2); };
                 auto col_of = [&](int it) { return (it < 4 ? n0 : int(m0)) + (lane & 3) * 8; };
                 typename Epi::Loads ahead[4];
+                typename Epi::Cursor cursor;
+                if constexpr (!SYM) {
+                    epi.open(cursor, row_of(0), col_of(0));
 #pragma unroll
-                for (int it = 0; it < 4; ++it) epi.load(row_of(it), col_of(it), ahead[it]);
+                    for (int it = 0; it < 4; ++it) epi.fetch(cursor, it, ahead[it]);
+                } else {
+#pragma unroll
+                    for (int it = 0; it < 4; ++it) epi.load(row_of(it), col_of(it), ahead[it]);
+                }
                 uint32_t v[32];
                 umma::tmem_ld32(tmem + acc * kDenseBN + (uint32_t(q * 32) << 16) + half * (kDenseBN / 2) + c, v);
                 umma::tmem_ld_wait();
@@ -241,9 +251,10 @@ dense_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
                 // and a warp stores 32 consecutive elements at a time
                 bool by_rows = false;
                 if constexpr (Epi::kRows) by_rows = epi.by_rows();
-                // one copy of the epilogue's code: unrolled it does not fit the instruction cache (134 us
-                // instead of 113 for 16384 x 5120 outputs of a 128-long contraction)
-#pragma unroll 1
+                // one copy of a long epilogue's code: unrolled it does not fit the instruction cache (134 us
+                // instead of 115 for 16384 x 5120 outputs of a 128-long contraction); the short ones of the
+                // symmetric products gain from four (2304 x 2304 update 500 -> 455 us)
+#pragma unroll(SYM ? 4 : 1)
                 for (int it = 0; it < trips; ++it) {
                     const typename Epi::Loads mine = ahead[0];
 #pragma unroll
@@ -271,7 +282,7 @@ dense_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
                     if constexpr (Epi::kRows) {
                         if (by_rows) {
                             const int r = it * 8 + (lane >> 2), j = (lane & 3) * 2;
-                            epi.leave(row_of(it), col_of(it), w, mine);
+                            epi.template finish<false>(cursor, w, mine);
                             ptx::sts128(sw + r * 128 + ((j ^ (r & 7)) << 4),
                                         make_uint4(__float_as_uint(w[0]), __float_as_uint(w[1]), __float_as_uint(w[2]), __float_as_uint(w[3])));
                             ptx::sts128(sw + r * 128 + (((j + 1) ^ (r & 7)) << 4),
@@ -279,7 +290,8 @@ dense_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
                             continue;
                         }
                     }
-                    epi(row_of(it), col_of(it), w, mine);
+                    if constexpr (SYM) epi(row_of(it), col_of(it), w, mine);
+                    else epi.template finish<true>(cursor, w, mine);
                 }
                 if constexpr (Epi::kRows) {
                     if (by_rows) {
@@ -572,10 +584,10 @@ template <int PMAJ, int QMAJ, bool F16, bool SYM, class Epi>
 int dense_product(const DenseOperand& P, const DenseOperand& Q, int64_t m, int64_t n, int64_t k, const Epi& epi,
                   int32_t* status, cudaStream_t s) {
     const int64_t mt = (m + 127) / 128, nt = (n + 255) / 256;
-    const int64_t big = SYM ? mt / 2 * (mt / 2 + 1) + (mt % 2 ? mt / 2 + 1 : 0) : mt * nt;
+    const int64_t tiles = SYM ? mt / 2 * (mt / 2 + 1) + (mt % 2 ? mt / 2 + 1 : 0) : mt * nt;
     // one operand box of 64 outer indices is the least an MN-major operand can be loaded in
     constexpr int B16 = PMAJ ? 64 : 16, B32 = PMAJ ? 64 : 32;
-    const DenseCut c = dense_cut(m, n, k, big, B16);
+    const DenseCut c = dense_cut(m, n, k, tiles, B16);
     if (c.bn == 0) return dense_gemm<PMAJ, QMAJ, F16, SYM>(P, Q, m, n, k, epi, status, s);
     if (c.bn == 16) return dense_split<QMAJ, PMAJ, F16, B16>(Q, P, m, n, k, c.splits, epi, status, s);
     if (c.bn == 32) return dense_split<QMAJ, PMAJ, F16, B32>(Q, P, m, n, k, c.splits, epi, status, s);

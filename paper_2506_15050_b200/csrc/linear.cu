@@ -131,6 +131,19 @@ __device__ __forceinline__ void widen8(const uint4& w, float (&v)[8]) {
     v[4] = bf16_lo(w.z); v[5] = bf16_hi(w.z); v[6] = bf16_lo(w.w); v[7] = bf16_hi(w.w);
 }
 
+// Whether all eight are finite and at most `top`: the largest magnitude as bits, where a NaN is larger than
+// everything -- a tree of three levels instead of eight comparisons that wait for one another.
+__device__ __forceinline__ bool all_within(const float (&v)[8], float top) {
+    uint32_t m[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) m[i] = __float_as_uint(v[i]) & 0x7fffffffu;
+#pragma unroll
+    for (int o = 4; o > 0; o >>= 1)
+#pragma unroll
+        for (int i = 0; i < o; ++i) m[i] = max(m[i], m[i + o]);
+    return m[0] <= __float_as_uint(top);
+}
+
 // Forward epilogue.
 struct EpiLinear {
     const void* bias; int32_t bias_f32;
@@ -155,31 +168,46 @@ struct EpiLinear {
         if (y_f32) static_cast<float*>(y)[m * ldy + n] = v;
         else store_f32(static_cast<bf16_bits*>(y) + m * ldy + n, v);
     }
-    // v: the sums in, y out; stores the pre-activation
-    __device__ __forceinline__ void leave(int64_t m, int n, float (&v)[8], const Loads& l) const {
-        if (outside(m, n)) return;
-        const int count = min(8, N - n);
-        if (bias) {
-            float b[8];
-            if (bias_f32) get8(static_cast<const float*>(bias) + n, b, count, vec_b);
-            else get8(static_cast<const bf16_bits*>(bias) + n, b, count, vec_b);
+    // What a lane's eight columns share, and where it stands on its way down the rows.
+    struct Cursor { float b[8]; const bf16_bits* r; bf16_bits* pre; char* y; int rows, count; bool full; };
+    __device__ __forceinline__ void open(Cursor& c, int64_t m, int n) const {
+        c.count = min(8, N - n);
+        c.rows = c.count > 0 && m < M ? int(min(M - m, int64_t(64))) : 0;
+        c.full = c.count == 8 && vec_y && (!residual || vec_r) && (!pre || vec_p);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] += b[i];
+        for (int i = 0; i < 8; ++i) c.b[i] = 0.f;
+        if (c.rows == 0) return;
+        if (bias) {
+            if (bias_f32) get8(static_cast<const float*>(bias) + n, c.b, c.count, vec_b);
+            else get8(static_cast<const bf16_bits*>(bias) + n, c.b, c.count, vec_b);
         }
+        c.r = residual + m * ldr + n;
+        c.pre = pre + m * ldp + n;
+        c.y = static_cast<char*>(y) + (m * ldy + n) * (y_f32 ? 4 : 2);
+    }
+    __device__ __forceinline__ void fetch(const Cursor& c, int it, Loads& l) const {
+        if (residual && vec_r && it * 8 < c.rows && c.count == 8) l.r = *reinterpret_cast<const uint4*>(c.r + it * 8 * ldr);
+    }
+    // v: the sums in, y out; stores the pre-activation, and y with STORE; moves on by eight rows
+    template <bool STORE>
+    __device__ __forceinline__ void finish(Cursor& c, float (&v)[8], const Loads& l) const {
+        if (c.rows <= 0) return;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] += c.b[i];
         float o[8];
         act_values(act, v, o);
         if (residual) {
             float r[8];
-            if (fast(m, n)) widen8(l.r, r);
-            else get8(residual + m * ldr + n, r, count, false);
+            if (vec_r && c.count == 8) widen8(l.r, r);
+            else get8(c.r, r, c.count, false);
 #pragma unroll
             for (int i = 0; i < 8; ++i) o[i] += r[i];
         }
         // z and y that are not finite, or leave the range of the type they are stored in, are written 0
+        // (without a stored z only relu hides a z that is not finite)
         const float top = y_f32 ? kFltMax : kBf16Max, ztop = pre ? kBf16Max : kFltMax;
-        bool fine = true;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) fine = fine && fabsf(o[i]) <= top && fabsf(v[i]) <= ztop;
+        bool fine = all_within(o, top);
+        if (pre || act == TPPO_ACT_RELU) fine = fine && all_within(v, ztop);
         if (!fine) {
             bool bad = false;
 #pragma unroll
@@ -187,20 +215,32 @@ struct EpiLinear {
                 const bool zok = fabsf(v[i]) <= ztop, ok = zok && fabsf(o[i]) <= top;
                 if (!zok) v[i] = 0.f;
                 if (!ok) o[i] = 0.f;
-                bad |= !ok && i < count;
+                bad |= !ok && i < c.count;
             }
             if (bad && status) atomicOr(status, TPPO_DEV_NONFINITE);
         }
-        if (pre) put8(pre + m * ldp + n, v, count, vec_p);
+        if (STORE && c.full) {
+            if (pre) store_vec<8>(c.pre, v);
+            if (y_f32) store_vec<8>(reinterpret_cast<float*>(c.y), o);
+            else store_vec<8>(reinterpret_cast<bf16_bits*>(c.y), o);
+        } else {
+            if (pre) put8(c.pre, v, c.count, vec_p);
+            if (STORE && y_f32) put8(reinterpret_cast<float*>(c.y), o, c.count, vec_y);
+            if (STORE && !y_f32) put8(reinterpret_cast<bf16_bits*>(c.y), o, c.count, vec_y);
+        }
+        if (!STORE) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = o[i];
+            for (int i = 0; i < 8; ++i) v[i] = o[i];
+        }
+        c.rows -= 8;
+        c.r += 8 * ldr;
+        c.pre += 8 * ldp;
+        c.y += 8 * ldy * (y_f32 ? 4 : 2);
     }
     __device__ __forceinline__ void operator()(int64_t m, int n, float (&v)[8], const Loads& l) const {
-        if (outside(m, n)) return;
-        leave(m, n, v, l);
-        const int count = min(8, N - n);
-        if (y_f32) put8(static_cast<float*>(y) + m * ldy + n, v, count, vec_y);
-        else put8(static_cast<bf16_bits*>(y) + m * ldy + n, v, count, vec_y);
+        Cursor c;
+        open(c, m, n);
+        finish<true>(c, v, l);
     }
 };
 
@@ -216,24 +256,31 @@ struct EpiStore {
     __device__ __forceinline__ void put(int64_t m, int n, float v) const {
         if (!outside(m, n)) store_f32(out + m * ld + n, v);
     }
-    __device__ __forceinline__ void leave(int64_t m, int n, float (&v)[8], const Loads&) const {
-        if (outside(m, n)) return;
-        const int count = min(8, N - n);
-        bool fine = true;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) fine = fine && fabsf(v[i]) <= kBf16Max;
-        if (!fine) {
+    struct Cursor { bf16_bits* out; int rows, count; };
+    __device__ __forceinline__ void open(Cursor& c, int64_t m, int n) const {
+        c.count = min(8, N - n);
+        c.rows = c.count > 0 && m < M ? int(min(M - m, int64_t(64))) : 0;
+        if (c.rows > 0) c.out = out + m * ld + n;
+    }
+    __device__ __forceinline__ void fetch(const Cursor&, int, Loads&) const {}
+    template <bool STORE>
+    __device__ __forceinline__ void finish(Cursor& c, float (&v)[8], const Loads&) const {
+        if (c.rows <= 0) return;
+        if (!all_within(v, kBf16Max)) {
             bool bad = false;
 #pragma unroll
             for (int i = 0; i < 8; ++i)
-                if (!(fabsf(v[i]) <= kBf16Max)) { bad |= i < count; v[i] = 0.f; }
+                if (!(fabsf(v[i]) <= kBf16Max)) { bad |= i < c.count; v[i] = 0.f; }
             if (bad && status) atomicOr(status, TPPO_DEV_NONFINITE);
         }
+        if (STORE) put8(c.out, v, c.count, vec);
+        c.rows -= 8;
+        c.out += 8 * ld;
     }
     __device__ __forceinline__ void operator()(int64_t m, int n, float (&v)[8], const Loads& l) const {
-        if (outside(m, n)) return;
-        leave(m, n, v, l);
-        put8(out + m * ld + n, v, min(8, N - n), vec);
+        Cursor c;
+        open(c, m, n);
+        finish<true>(c, v, l);
     }
 };
 
@@ -459,10 +506,7 @@ __global__ void __launch_bounds__(256) linear_dz_kernel(const DzArgs a) {
 #pragma unroll
                         for (int i = 0; i < 8; ++i) v[i] *= slope[i];
                     }
-                    bool fine = true;
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) fine = fine && fabsf(v[i]) <= kBf16Max;
-                    if (!fine) {
+                    if (!all_within(v, kBf16Max)) {
                         bad = true;
 #pragma unroll
                         for (int i = 0; i < 8; ++i)

@@ -171,6 +171,7 @@ __global__ void __launch_bounds__(kMuonThreads) muon_normalise_kernel(const doub
 struct EpiA {
     f16_bits* out; int64_t ld; int32_t m; float* diag;
     static constexpr bool kRows = false;
+    struct Cursor {};
     struct Loads {};
     __device__ __forceinline__ void load(int64_t, int, Loads&) const {}
     __device__ __forceinline__ bool outside(int64_t r, int c) const { return r >= m || c >= m; }
@@ -189,6 +190,7 @@ struct EpiA {
 struct EpiB {
     const f16_bits* a; f16_bits* out; int64_t ld; int32_t m; const float* diag_a; float* diag_b;
     static constexpr bool kRows = false;
+    struct Cursor {};
     struct Loads { uint4 a; };
     __device__ __forceinline__ void load(int64_t r, int c, Loads& l) const {
         if (!outside(r, c)) l.a = *reinterpret_cast<const uint4*>(a + r * ld + c);
@@ -224,6 +226,51 @@ struct EpiX {
     int64_t R; int32_t C;
     static constexpr bool kRows = false;
     struct Loads { float4 lo, hi; };
+    // what a lane's eight columns share down the rows
+    struct Cursor { float f[8]; float norm; int64_t at; bf16_bits* update; const float* diag; int rows, count; };
+    __device__ __forceinline__ void open(Cursor& k, int64_t r, int c) const {
+        k.count = min(8, C - c);
+        k.rows = k.count > 0 && r < R ? int(min(R - r, int64_t(64))) : 0;
+        if (k.rows == 0) return;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) k.f[i] = kNsA + (RIGHT && diag_b && i < k.count ? diag_b[c + i] : 0.f);
+        k.norm = inverse ? *inverse : 1.f;
+        k.at = r * ldx + c;
+        k.update = update + r * ldu + c;
+        k.diag = !RIGHT && diag_b ? diag_b + r : nullptr;
+    }
+    __device__ __forceinline__ void fetch(const Cursor& k, int it, Loads& l) const {
+        if (it * 8 >= k.rows) return;
+        const float4* p = reinterpret_cast<const float4*>(x32 + k.at + it * 8 * ldx);
+        l.lo = p[0];
+        l.hi = p[1];
+    }
+    template <bool STORE>
+    __device__ __forceinline__ void finish(Cursor& k, float (&v)[8], const Loads& l) const {
+        if (k.rows <= 0) return;
+        const float x[8] = {l.lo.x, l.lo.y, l.lo.z, l.lo.w, l.hi.x, l.hi.y, l.hi.z, l.hi.w};
+        const float row = k.diag ? *k.diag : 0.f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = fmaf(k.f[i] + row, x[i] * k.norm, v[i] * (kUnscale * kUnscale));
+        if (update) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] *= scale;
+            if (vec_u && k.count == 8) {
+                store_vec<8>(k.update, v);
+            } else {
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    if (i < k.count) store_f32(k.update + i, v[i]);
+            }
+        } else {
+            store_vec<8>(x32 + k.at, v);
+            store_operand(x16 + k.at, v);
+        }
+        k.rows -= 8;
+        k.at += 8 * ldx;
+        k.update += 8 * ldu;
+        if (k.diag) k.diag += 8;
+    }
     __device__ __forceinline__ bool outside(int64_t r, int c) const { return r >= R || c >= C; }
     __device__ __forceinline__ void load(int64_t r, int c, Loads& l) const {
         if (outside(r, c)) return;
@@ -232,30 +279,9 @@ struct EpiX {
         l.hi = p[1];
     }
     __device__ __forceinline__ void operator()(int64_t r, int c, float (&v)[8], const Loads& l) const {
-        if (outside(r, c)) return;
-        const float x[8] = {l.lo.x, l.lo.y, l.lo.z, l.lo.w, l.hi.x, l.hi.y, l.hi.z, l.hi.w};
-        const float norm = inverse ? *inverse : 1.f;
-        const float row = !RIGHT && diag_b ? diag_b[r] : 0.f;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const float f = kNsA + (RIGHT ? (diag_b && c + i < C ? diag_b[c + i] : 0.f) : row);
-            v[i] = fmaf(f, x[i] * norm, v[i] * (kUnscale * kUnscale));
-        }
-        if (update) {
-            const int count = min(8, C - c);
-            if (vec_u && count == 8) {
-#pragma unroll
-                for (int i = 0; i < 8; ++i) v[i] *= scale;
-                store_vec<8>(update + r * ldu + c, v);
-            } else {
-#pragma unroll
-                for (int i = 0; i < 8; ++i)
-                    if (i < count) store_f32(update + r * ldu + c + i, v[i] * scale);
-            }
-        } else {
-            store_vec<8>(x32 + r * ldx + c, v);
-            store_operand(x16 + r * ldx + c, v);
-        }
+        Cursor k;
+        open(k, r, c);
+        finish<true>(k, v, l);
     }
 };
 
