@@ -139,8 +139,8 @@ __device__ __forceinline__ void dense_tile(const DenseShape& g, int t, int& mt, 
 //      void load(row, col, Loads&) const -- starts reading what the elements (row, col .. col+7) need
 //      void operator()(row, col, float (&v)[8], const Loads&) const -- finishes them
 // and for the persistent kernel, whose lanes go down their eight columns eight rows at a time (without
-// SYM): Cursor, what stays the same on the way and where it has got to; open(Cursor&, row, col);
-// fetch(cursor, trip, Loads&) as load; finish<true>(cursor, v, loads) as operator(), moving on.
+// SYM): Cursor, what stays the same on the way; open(Cursor&, row, col); fetch(cursor, trip, Loads&) as
+// load; finish<true>(cursor, trip, v, loads) as operator().
 // kRows: whether there are bool by_rows() const (uniform), finish<false> -- all but the stores of the
 // main output, whose values stay in v -- and put(row, col, float), which stores one.
 // Rows and columns may lie outside the matrix.
@@ -282,7 +282,7 @@ dense_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
                     if constexpr (Epi::kRows) {
                         if (by_rows) {
                             const int r = it * 8 + (lane >> 2), j = (lane & 3) * 2;
-                            epi.template finish<false>(cursor, w, mine);
+                            epi.template finish<false>(cursor, it, w, mine);
                             ptx::sts128(sw + r * 128 + ((j ^ (r & 7)) << 4),
                                         make_uint4(__float_as_uint(w[0]), __float_as_uint(w[1]), __float_as_uint(w[2]), __float_as_uint(w[3])));
                             ptx::sts128(sw + r * 128 + (((j + 1) ^ (r & 7)) << 4),
@@ -291,7 +291,7 @@ dense_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
                         }
                     }
                     if constexpr (SYM) epi(row_of(it), col_of(it), w, mine);
-                    else epi.template finish<true>(cursor, w, mine);
+                    else epi.template finish<true>(cursor, it, w, mine);
                 }
                 if constexpr (Epi::kRows) {
                     if (by_rows) {

@@ -168,12 +168,11 @@ struct EpiLinear {
         if (y_f32) static_cast<float*>(y)[m * ldy + n] = v;
         else store_f32(static_cast<bf16_bits*>(y) + m * ldy + n, v);
     }
-    // What a lane's eight columns share, and where it stands on its way down the rows.
-    struct Cursor { float b[8]; const bf16_bits* r; bf16_bits* pre; char* y; int rows, count; bool full; };
+    // What a lane's eight columns share down the rows.
+    struct Cursor { float b[8]; const bf16_bits* r; bf16_bits* pre; char* y; int rows, count; };
     __device__ __forceinline__ void open(Cursor& c, int64_t m, int n) const {
         c.count = min(8, N - n);
         c.rows = c.count > 0 && m < M ? int(min(M - m, int64_t(64))) : 0;
-        c.full = c.count == 8 && vec_y && (!residual || vec_r) && (!pre || vec_p);
 #pragma unroll
         for (int i = 0; i < 8; ++i) c.b[i] = 0.f;
         if (c.rows == 0) return;
@@ -188,10 +187,10 @@ struct EpiLinear {
     __device__ __forceinline__ void fetch(const Cursor& c, int it, Loads& l) const {
         if (residual && vec_r && it * 8 < c.rows && c.count == 8) l.r = *reinterpret_cast<const uint4*>(c.r + it * 8 * ldr);
     }
-    // v: the sums in, y out; stores the pre-activation, and y with STORE; moves on by eight rows
+    // v: the sums in, y out; stores the pre-activation, and y with STORE
     template <bool STORE>
-    __device__ __forceinline__ void finish(Cursor& c, float (&v)[8], const Loads& l) const {
-        if (c.rows <= 0) return;
+    __device__ __forceinline__ void finish(const Cursor& c, int it, float (&v)[8], const Loads& l) const {
+        if (it * 8 >= c.rows) return;
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[i] += c.b[i];
         float o[8];
@@ -199,7 +198,7 @@ struct EpiLinear {
         if (residual) {
             float r[8];
             if (vec_r && c.count == 8) widen8(l.r, r);
-            else get8(c.r, r, c.count, false);
+            else get8(c.r + it * 8 * ldr, r, c.count, false);
 #pragma unroll
             for (int i = 0; i < 8; ++i) o[i] += r[i];
         }
@@ -219,28 +218,19 @@ struct EpiLinear {
             }
             if (bad && status) atomicOr(status, TPPO_DEV_NONFINITE);
         }
-        if (STORE && c.full) {
-            if (pre) store_vec<8>(c.pre, v);
-            if (y_f32) store_vec<8>(reinterpret_cast<float*>(c.y), o);
-            else store_vec<8>(reinterpret_cast<bf16_bits*>(c.y), o);
+        if (pre) put8(c.pre + it * 8 * ldp, v, c.count, vec_p);
+        if (STORE) {
+            if (y_f32) put8(reinterpret_cast<float*>(c.y) + it * 8 * ldy, o, c.count, vec_y);
+            else put8(reinterpret_cast<bf16_bits*>(c.y) + it * 8 * ldy, o, c.count, vec_y);
         } else {
-            if (pre) put8(c.pre, v, c.count, vec_p);
-            if (STORE && y_f32) put8(reinterpret_cast<float*>(c.y), o, c.count, vec_y);
-            if (STORE && !y_f32) put8(reinterpret_cast<bf16_bits*>(c.y), o, c.count, vec_y);
-        }
-        if (!STORE) {
 #pragma unroll
             for (int i = 0; i < 8; ++i) v[i] = o[i];
         }
-        c.rows -= 8;
-        c.r += 8 * ldr;
-        c.pre += 8 * ldp;
-        c.y += 8 * ldy * (y_f32 ? 4 : 2);
     }
     __device__ __forceinline__ void operator()(int64_t m, int n, float (&v)[8], const Loads& l) const {
         Cursor c;
         open(c, m, n);
-        finish<true>(c, v, l);
+        finish<true>(c, 0, v, l);
     }
 };
 
@@ -264,8 +254,8 @@ struct EpiStore {
     }
     __device__ __forceinline__ void fetch(const Cursor&, int, Loads&) const {}
     template <bool STORE>
-    __device__ __forceinline__ void finish(Cursor& c, float (&v)[8], const Loads&) const {
-        if (c.rows <= 0) return;
+    __device__ __forceinline__ void finish(const Cursor& c, int it, float (&v)[8], const Loads&) const {
+        if (it * 8 >= c.rows) return;
         if (!all_within(v, kBf16Max)) {
             bool bad = false;
 #pragma unroll
@@ -273,14 +263,12 @@ struct EpiStore {
                 if (!(fabsf(v[i]) <= kBf16Max)) { bad |= i < c.count; v[i] = 0.f; }
             if (bad && status) atomicOr(status, TPPO_DEV_NONFINITE);
         }
-        if (STORE) put8(c.out, v, c.count, vec);
-        c.rows -= 8;
-        c.out += 8 * ld;
+        if (STORE) put8(c.out + it * 8 * ld, v, c.count, vec);
     }
     __device__ __forceinline__ void operator()(int64_t m, int n, float (&v)[8], const Loads& l) const {
         Cursor c;
         open(c, m, n);
-        finish<true>(c, v, l);
+        finish<true>(c, 0, v, l);
     }
 };
 

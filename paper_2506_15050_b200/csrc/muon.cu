@@ -246,30 +246,28 @@ struct EpiX {
         l.hi = p[1];
     }
     template <bool STORE>
-    __device__ __forceinline__ void finish(Cursor& k, float (&v)[8], const Loads& l) const {
-        if (k.rows <= 0) return;
+    __device__ __forceinline__ void finish(const Cursor& k, int it, float (&v)[8], const Loads& l) const {
+        if (it * 8 >= k.rows) return;
         const float x[8] = {l.lo.x, l.lo.y, l.lo.z, l.lo.w, l.hi.x, l.hi.y, l.hi.z, l.hi.w};
-        const float row = k.diag ? *k.diag : 0.f;
+        const float row = k.diag ? k.diag[it * 8] : 0.f;
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[i] = fmaf(k.f[i] + row, x[i] * k.norm, v[i] * (kUnscale * kUnscale));
         if (update) {
 #pragma unroll
             for (int i = 0; i < 8; ++i) v[i] *= scale;
+            bf16_bits* p = k.update + it * 8 * ldu;
             if (vec_u && k.count == 8) {
-                store_vec<8>(k.update, v);
+                store_vec<8>(p, v);
             } else {
 #pragma unroll
                 for (int i = 0; i < 8; ++i)
-                    if (i < k.count) store_f32(k.update + i, v[i]);
+                    if (i < k.count) store_f32(p + i, v[i]);
             }
         } else {
-            store_vec<8>(x32 + k.at, v);
-            store_operand(x16 + k.at, v);
+            const int64_t at = k.at + it * 8 * ldx;
+            store_vec<8>(x32 + at, v);
+            store_operand(x16 + at, v);
         }
-        k.rows -= 8;
-        k.at += 8 * ldx;
-        k.update += 8 * ldu;
-        if (k.diag) k.diag += 8;
     }
     __device__ __forceinline__ bool outside(int64_t r, int c) const { return r >= R || c >= C; }
     __device__ __forceinline__ void load(int64_t r, int c, Loads& l) const {
@@ -281,7 +279,7 @@ struct EpiX {
     __device__ __forceinline__ void operator()(int64_t r, int c, float (&v)[8], const Loads& l) const {
         Cursor k;
         open(k, r, c);
-        finish<true>(k, v, l);
+        finish<true>(k, 0, v, l);
     }
 };
 
