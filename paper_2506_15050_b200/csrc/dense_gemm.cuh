@@ -138,12 +138,107 @@ __device__ __forceinline__ void dense_tile(const DenseShape& g, int t, int& mt, 
 // Epi: bool outside(row, col) const -- nothing at or beyond (row, col) belongs to the matrix
 //      void load(row, col, Loads&) const -- starts reading what the elements (row, col .. col+7) need
 //      void operator()(row, col, float (&v)[8], const Loads&) const -- finishes them
-// and for the persistent kernel, whose lanes go down their eight columns eight rows at a time (without
-// SYM): Cursor, what stays the same on the way; open(Cursor&, row, col); fetch(cursor, trip, Loads&) as
+// and for the persistent kernel, whose lanes go down their eight columns eight rows at a time: Cursor, what stays the same on the way; open(Cursor&, row, col); fetch(cursor, trip, Loads&) as
 // load; finish<true>(cursor, trip, v, loads) as operator().
 // kRows: whether there are bool by_rows() const (uniform), finish<false> -- all but the stores of the
 // main output, whose values stay in v -- and put(row, col, float), which stores one.
 // Rows and columns may lie outside the matrix.
+// One warp's share of a finished tile: 32 accumulator rows (output rows m0 ..) by 128 columns (output
+// columns n_first ..) at tensor-memory address `taddr`, 32 x 32 at a time.  `sw`: its 4 KB of shared
+// memory, in which 16-byte pieces are XORed with a swizzle of their row, so that rows written by lane,
+// pieces of rows and pieces of columns all are read and written without a bank conflict.
+__device__ __forceinline__ uint32_t dense_piece(int row, int piece) {
+    return uint32_t(row * 128 + ((piece ^ (row & 7) ^ ((row >> 3) << 1)) << 4));
+}
+template <bool SYM, class Epi>
+__device__ __forceinline__ void dense_epilogue(const Epi& epi, int64_t m0, int n_first, uint32_t taddr, uint32_t sw) {
+    const int lane = threadIdx.x & 31;
+    // rows of the output that take no 16-byte stores: the finished values go back to shared memory, and a
+    // warp stores 32 consecutive elements at a time
+    bool by_rows = false;
+    if constexpr (Epi::kRows) by_rows = epi.by_rows();
+#pragma unroll 1
+    for (int c = 0; c < kDenseBN / 2; c += 32) {
+        const int n0 = n_first + c;
+        if (SYM && n0 > m0) break;            // above the diagonal: another chunk's mirror image
+        if (epi.outside(m0, n0)) break;
+        // a lane finishes eight elements of four rows, eight apart -- and, below the diagonal of a symmetric
+        // product, of their mirror images.  What the epilogue reads is fetched while the accumulator is
+        // fetched and turned.
+        constexpr int kPasses = SYM ? 2 : 1;
+        const bool mirrored = SYM && n0 < m0;
+        typename Epi::Cursor cursor[kPasses];
+        typename Epi::Loads ahead[kPasses][4];
+        epi.open(cursor[0], m0 + (lane >> 2), n0 + (lane & 3) * 8);
+#pragma unroll
+        for (int it = 0; it < 4; ++it) epi.fetch(cursor[0], it, ahead[0][it]);
+        if constexpr (SYM) {
+            if (mirrored) {
+                epi.open(cursor[1], int64_t(n0) + (lane >> 2), int(m0) + (lane & 3) * 8);
+#pragma unroll
+                for (int it = 0; it < 4; ++it) epi.fetch(cursor[1], it, ahead[1][it]);
+            }
+        }
+        uint32_t v[32];
+        umma::tmem_ld32(taddr + c, v);
+        umma::tmem_ld_wait();
+        __syncwarp();
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            ptx::sts128(sw + dense_piece(lane, j), make_uint4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]));
+        __syncwarp();
+        // one copy of a long epilogue's code: unrolled it does not fit the instruction cache (134 us instead
+        // of 116 for 16384 x 5120 outputs of a 128-long contraction); the short ones of the symmetric
+        // products gain from four (2304 x 2304 update 500 -> 455 us)
+#pragma unroll(SYM ? 4 : 1)
+        for (int it = 0; it < 4; ++it) {
+            const typename Epi::Loads mine = ahead[0][0];
+#pragma unroll
+            for (int i = 0; i < 3; ++i) ahead[0][i] = ahead[0][i + 1];
+            const int r = it * 8 + (lane >> 2), j = (lane & 3) * 2;
+            const uint4 lo = ptx::lds128(sw + dense_piece(r, j)), hi = ptx::lds128(sw + dense_piece(r, j + 1));
+            float w[8] = {__uint_as_float(lo.x), __uint_as_float(lo.y), __uint_as_float(lo.z), __uint_as_float(lo.w),
+                          __uint_as_float(hi.x), __uint_as_float(hi.y), __uint_as_float(hi.z), __uint_as_float(hi.w)};
+            if constexpr (Epi::kRows) {
+                if (by_rows) {
+                    epi.template finish<false>(cursor[0], it, w, mine);
+                    ptx::sts128(sw + dense_piece(r, j), make_uint4(__float_as_uint(w[0]), __float_as_uint(w[1]),
+                                                                   __float_as_uint(w[2]), __float_as_uint(w[3])));
+                    ptx::sts128(sw + dense_piece(r, j + 1), make_uint4(__float_as_uint(w[4]), __float_as_uint(w[5]),
+                                                                       __float_as_uint(w[6]), __float_as_uint(w[7])));
+                    continue;
+                }
+            }
+            epi.template finish<true>(cursor[0], it, w, mine);
+        }
+        if constexpr (Epi::kRows) {
+            if (by_rows) {
+                __syncwarp();
+#pragma unroll 8
+                for (int r = 0; r < 32; ++r) {
+                    float f;
+                    asm volatile("ld.shared.f32 %0, [%1];" : "=f"(f) : "r"(sw + dense_piece(r, lane >> 2) + (lane & 3) * 4));
+                    epi.put(m0 + r, n0 + lane, f);
+                }
+            }
+        }
+        if constexpr (SYM) {
+            if (mirrored) {
+#pragma unroll
+                for (int it = 0; it < 4; ++it) {
+                    const int col = it * 8 + (lane >> 2), r0 = (lane & 3) * 8;
+                    float w[8];
+#pragma unroll
+                    for (int i = 0; i < 8; ++i)
+                        asm volatile("ld.shared.f32 %0, [%1];" : "=f"(w[i])
+                                     : "r"(sw + dense_piece(r0 + i, col >> 2) + (col & 3) * 4));
+                    epi.template finish<true>(cursor[1], it, w, ahead[1][it]);
+                }
+            }
+        }
+    }
+}
+
 template <int AMAJ, int BMAJ, bool F16, bool SYM, class Epi>
 __global__ void __launch_bounds__(kDenseThreads, 1)
 dense_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const DenseShape g,
@@ -215,97 +310,8 @@ dense_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
             const int acc = local & 1;
             if (!ptx::mbar_wait_warp<false>(acc_full + 8 * acc, (local >> 1) & 1)) { timed_out = true; break; }
             umma::fence_after_thread_sync();
-            const int64_t m0 = int64_t(mt) * kDenseTileM + q * 32;
-#pragma unroll 1
-            for (int c = 0; c < kDenseBN / 2; c += 32) {
-                const int n0 = nt * kDenseBN + half * (kDenseBN / 2) + c;
-                if (SYM && n0 > m0) break;            // above the diagonal: another chunk's mirror image
-                if (epi.outside(m0, n0)) break;
-                // eight trips of a lane finish eight elements each: four as they are, four mirrored.  What the
-                // epilogue reads is fetched four trips ahead, for the first ones while the accumulator is
-                // fetched and turned.
-                const int trips = SYM && n0 < m0 ? 8 : 4;
-                auto row_of = [&](int it) { return (it < 4 ? m0 : int64_t(n0)) + (it & 3) * 8 + (lane >> 2); };
-                auto col_of = [&](int it) { return (it < 4 ? n0 : int(m0)) + (lane & 3) * 8; };
-                typename Epi::Loads ahead[4];
-                typename Epi::Cursor cursor;
-                if constexpr (!SYM) {
-                    epi.open(cursor, row_of(0), col_of(0));
-#pragma unroll
-                    for (int it = 0; it < 4; ++it) epi.fetch(cursor, it, ahead[it]);
-                } else {
-#pragma unroll
-                    for (int it = 0; it < 4; ++it) epi.load(row_of(it), col_of(it), ahead[it]);
-                }
-                uint32_t v[32];
-                umma::tmem_ld32(tmem + acc * kDenseBN + (uint32_t(q * 32) << 16) + half * (kDenseBN / 2) + c, v);
-                umma::tmem_ld_wait();
-                // row-per-lane to eight-columns-per-lane through shared memory; 16-byte pieces of a
-                // row are XORed with its low bits, so that neither side meets a bank conflict
-                __syncwarp();
-#pragma unroll
-                for (int j = 0; j < 8; ++j)
-                    ptx::sts128(sw + lane * 128 + ((j ^ (lane & 7)) << 4), make_uint4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]));
-                __syncwarp();
-                // rows of the output that take no 16-byte stores: the finished values go back to shared memory,
-                // and a warp stores 32 consecutive elements at a time
-                bool by_rows = false;
-                if constexpr (Epi::kRows) by_rows = epi.by_rows();
-                // one copy of a long epilogue's code: unrolled it does not fit the instruction cache (134 us
-                // instead of 115 for 16384 x 5120 outputs of a 128-long contraction); the short ones of the
-                // symmetric products gain from four (2304 x 2304 update 500 -> 455 us)
-#pragma unroll(SYM ? 4 : 1)
-                for (int it = 0; it < trips; ++it) {
-                    const typename Epi::Loads mine = ahead[0];
-#pragma unroll
-                    for (int i = 0; i < 3; ++i) ahead[i] = ahead[i + 1];
-                    if (SYM && it + 4 < trips) epi.load(row_of(it + 4), col_of(it + 4), ahead[3]);
-                    float w[8];
-                    if (!SYM || it < 4) {
-                        const int r = it * 8 + (lane >> 2), j = (lane & 3) * 2;
-                        const uint4 lo = ptx::lds128(sw + r * 128 + ((j ^ (r & 7)) << 4));
-                        const uint4 hi = ptx::lds128(sw + r * 128 + (((j + 1) ^ (r & 7)) << 4));
-                        w[0] = __uint_as_float(lo.x); w[1] = __uint_as_float(lo.y);
-                        w[2] = __uint_as_float(lo.z); w[3] = __uint_as_float(lo.w);
-                        w[4] = __uint_as_float(hi.x); w[5] = __uint_as_float(hi.y);
-                        w[6] = __uint_as_float(hi.z); w[7] = __uint_as_float(hi.w);
-                    } else {
-                        const int col = (it & 3) * 8 + (lane >> 2), r0 = (lane & 3) * 8;
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) {
-                            uint32_t u;
-                            asm volatile("ld.shared.u32 %0, [%1];" : "=r"(u)
-                                         : "r"(sw + (r0 + i) * 128 + (((col >> 2) ^ i) << 4) + (col & 3) * 4));
-                            w[i] = __uint_as_float(u);
-                        }
-                    }
-                    if constexpr (Epi::kRows) {
-                        if (by_rows) {
-                            const int r = it * 8 + (lane >> 2), j = (lane & 3) * 2;
-                            epi.template finish<false>(cursor, it, w, mine);
-                            ptx::sts128(sw + r * 128 + ((j ^ (r & 7)) << 4),
-                                        make_uint4(__float_as_uint(w[0]), __float_as_uint(w[1]), __float_as_uint(w[2]), __float_as_uint(w[3])));
-                            ptx::sts128(sw + r * 128 + (((j + 1) ^ (r & 7)) << 4),
-                                        make_uint4(__float_as_uint(w[4]), __float_as_uint(w[5]), __float_as_uint(w[6]), __float_as_uint(w[7])));
-                            continue;
-                        }
-                    }
-                    if constexpr (SYM) epi(row_of(it), col_of(it), w, mine);
-                    else epi.template finish<true>(cursor, it, w, mine);
-                }
-                if constexpr (Epi::kRows) {
-                    if (by_rows) {
-                        __syncwarp();
-#pragma unroll 8
-                        for (int r = 0; r < 32; ++r) {
-                            float f;
-                            asm volatile("ld.shared.f32 %0, [%1];" : "=f"(f)
-                                         : "r"(sw + r * 128 + (((lane >> 2) ^ (r & 7)) << 4) + (lane & 3) * 4));
-                            epi.put(m0 + r, n0 + lane, f);
-                        }
-                    }
-                }
-            }
+            dense_epilogue<SYM>(epi, int64_t(mt) * kDenseTileM + q * 32, nt * kDenseBN + half * (kDenseBN / 2),
+                                tmem + acc * kDenseBN + (uint32_t(q * 32) << 16) + half * (kDenseBN / 2), sw);
             umma::fence_before_thread_sync();
             __syncwarp();
             if (lane == 0) ptx::mbar_arrive(acc_empty + 8 * acc);

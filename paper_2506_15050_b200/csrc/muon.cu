@@ -171,18 +171,33 @@ __global__ void __launch_bounds__(kMuonThreads) muon_normalise_kernel(const doub
 struct EpiA {
     f16_bits* out; int64_t ld; int32_t m; float* diag;
     static constexpr bool kRows = false;
-    struct Cursor {};
     struct Loads {};
-    __device__ __forceinline__ void load(int64_t, int, Loads&) const {}
+    struct Cursor { f16_bits* out; int rows, off; };       // off: row - first column
     __device__ __forceinline__ bool outside(int64_t r, int c) const { return r >= m || c >= m; }
-    __device__ __forceinline__ void operator()(int64_t r, int c, float (&v)[8], const Loads&) const {
-        if (outside(r, c)) return;
+    __device__ __forceinline__ void load(int64_t, int, Loads&) const {}
+    __device__ __forceinline__ void open(Cursor& k, int64_t r, int c) const {
+        k.rows = outside(r, c) ? 0 : int(m - r);
+        k.out = out + r * ld + c;
+        k.off = int(r) - c;
+    }
+    __device__ __forceinline__ void fetch(const Cursor&, int, Loads&) const {}
+    template <bool STORE>
+    __device__ __forceinline__ void finish(const Cursor& k, int it, float (&v)[8], const Loads&) const {
+        if (it * 8 >= k.rows) return;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            v[i] *= kUnscale * kUnscale;
-            if (diag && r == c + i) { diag[r] = v[i]; v[i] = 0.f; }
+        for (int i = 0; i < 8; ++i) v[i] *= kUnscale * kUnscale;
+        const int on = k.off + it * 8;            // where the row meets the diagonal
+        if (diag && on >= 0 && on < 8) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (i == on) { diag[m - k.rows + it * 8] = v[i]; v[i] = 0.f; }
         }
-        store_operand(out + r * ld + c, v);
+        store_operand(k.out + it * 8 * ld, v);
+    }
+    __device__ __forceinline__ void operator()(int64_t r, int c, float (&v)[8], const Loads& l) const {
+        Cursor k;
+        open(k, r, c);
+        finish<true>(k, 0, v, l);
     }
 };
 
@@ -190,29 +205,52 @@ struct EpiA {
 struct EpiB {
     const f16_bits* a; f16_bits* out; int64_t ld; int32_t m; const float* diag_a; float* diag_b;
     static constexpr bool kRows = false;
-    struct Cursor {};
-    struct Loads { uint4 a; };
-    __device__ __forceinline__ void load(int64_t r, int c, Loads& l) const {
-        if (!outside(r, c)) l.a = *reinterpret_cast<const uint4*>(a + r * ld + c);
-    }
+    struct Loads { uint4 a; float d; };
+    struct Cursor { float f[8]; int64_t at; int rows, off; };
     __device__ __forceinline__ bool outside(int64_t r, int c) const { return r >= m || c >= m; }
-    __device__ __forceinline__ void operator()(int64_t r, int c, float (&v)[8], const Loads& l) const {
+    __device__ __forceinline__ void open(Cursor& k, int64_t r, int c) const {
+        k.rows = outside(r, c) ? 0 : int(m - r);
+        k.at = r * ld + c;
+        k.off = int(r) - c;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) k.f[i] = kNsB;
+        if (diag_a && k.rows > 0) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (c + i < m) k.f[i] = fmaf(kNsC, diag_a[c + i], kNsB);
+        }
+    }
+    __device__ __forceinline__ void fetch(const Cursor& k, int it, Loads& l) const {
+        if (it * 8 >= k.rows) return;
+        l.a = *reinterpret_cast<const uint4*>(a + k.at + it * 8 * ld);
+        l.d = diag_a ? diag_a[m - k.rows + it * 8] : 0.f;
+    }
+    __device__ __forceinline__ void load(int64_t r, int c, Loads& l) const {
         if (outside(r, c)) return;
+        l.a = *reinterpret_cast<const uint4*>(a + r * ld + c);
+        l.d = diag_a ? diag_a[r] : 0.f;
+    }
+    template <bool STORE>
+    __device__ __forceinline__ void finish(const Cursor& k, int it, float (&v)[8], const Loads& l) const {
+        if (it * 8 >= k.rows) return;
         float o[8];
         widen_operand(l.a, o);
-        const float dr = diag_a ? diag_a[r] : 0.f;
+        const int on = k.off + it * 8;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             const float sq = kNsC * (v[i] * (kUnscale * kUnscale));
-            float f = kNsB;
-            if (diag_a) f += kNsC * (dr + (c + i < m ? diag_a[c + i] : 0.f));
-            v[i] = fmaf(f, o[i], sq);
-            if (diag_a && r == c + i) {
-                diag_b[r] = fmaf(fmaf(kNsC, dr, kNsB), dr, sq);
+            v[i] = fmaf(fmaf(kNsC, l.d, k.f[i]), o[i], sq);
+            if (diag_a && i == on) {
+                diag_b[m - k.rows + it * 8] = fmaf(fmaf(kNsC, l.d, kNsB), l.d, sq);
                 v[i] = 0.f;
             }
         }
-        store_operand(out + r * ld + c, v);
+        store_operand(out + k.at + it * 8 * ld, v);
+    }
+    __device__ __forceinline__ void operator()(int64_t r, int c, float (&v)[8], const Loads& l) const {
+        Cursor k;
+        open(k, r, c);
+        finish<true>(k, 0, v, l);
     }
 };
 
