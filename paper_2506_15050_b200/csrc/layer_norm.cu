@@ -12,7 +12,7 @@
 // beta stay in the registers of a block's threads for its whole walk over the rows; each block writes one
 // partial row of them to the workspace and a second kernel adds those in a fixed order, so the gradients
 // do not depend on scheduling.  Rows too long for either way take kernels that read the row again from L2.
-//   [16384, 5120] bf16: forward 62 us (5.4 TB/s, 0.82 of the measured copy rate), backward 122 us (4.1 TB/s)
+//   [16384, 5120] bf16: forward 63 us (5.3 TB/s, 0.81 of the measured copy rate), backward 128 us (3.9 TB/s)
 //   [16384, 5120] fp32: forward 107 us (6.3 TB/s), backward 176 us (5.7 TB/s)
 #include <type_traits>
 
