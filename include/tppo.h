@@ -449,7 +449,8 @@ int tppo_advance_batch(const int32_t *seq_begin, const int32_t *prompt_len,
  *   eps >= 0
  * A row that holds a NaN or an infinity, or whose variance leaves the range of fp32 (with eps = 0 that
  * includes a variance of 0), has no statistics: its y, mean and rstd are written 0 and
- * TPPO_DEV_NONFINITE is raised.
+ * TPPO_DEV_NONFINITE is raised.  gamma and beta are taken as they are: one that is not finite, or carries a
+ * y past the range of its type, leaves such elements in y.
  */
 int tppo_layer_norm_fwd(const void *x, int32_t dtype, int64_t M, int32_t N, int64_t ldx,
                         const void *gamma, const void *beta, int32_t param_dtype, float eps,
@@ -466,7 +467,8 @@ int tppo_layer_norm_fwd(const void *x, int32_t dtype, int64_t M, int32_t N, int6
  *   workspace  tppo_workspace_bytes(TPPO_OP_LAYER_NORM, M, 0, 0, N) bytes; may be NULL when both
  *              dgamma and dbeta are
  * A row without statistics (rstd = 0) contributes nothing and gets dx = 0; so does a row whose dy or x
- * is not finite, which raises TPPO_DEV_NONFINITE.  M = 0 writes dgamma = dbeta = 0.
+ * is not finite, which raises TPPO_DEV_NONFINITE.  Elements of dx and sums over rows that leave the range
+ * of their type become infinities.  M = 0 writes dgamma = dbeta = 0.
  */
 int tppo_layer_norm_bwd(const void *dy, const void *x, int32_t dtype, int64_t M, int32_t N,
                         int64_t lddy, int64_t ldx, const void *gamma, int32_t param_dtype,
@@ -521,7 +523,9 @@ int tppo_linear_fwd(const void *x, int64_t ldx, const void *weight, int64_t ldw,
  *   NULL when none is needed (TPPO_ACT_NONE, aligned bf16 operands, no dbias)
  * dz is rounded to bf16 before the two products (dbias sums the unrounded values); an element of dz or
  * of an output that is not finite or leaves the range of bf16 counts or is written as 0 and raises
- * TPPO_DEV_NONFINITE.  M = 0 writes dweight = dbias = 0.
+ * TPPO_DEV_NONFINITE.  (Where dy itself can be the operand -- TPPO_ACT_NONE, aligned bf16 -- the products may
+ * take it as it is: its elements that are not finite then make every element of dx and dweight that they
+ * enter 0.)  M = 0 writes dweight = dbias = 0.
  */
 int tppo_linear_bwd(const void *dy, int32_t dy_dtype, int64_t lddy, const void *x, int64_t ldx,
                     const void *weight, int64_t ldw, int64_t M, int32_t K, int32_t N,
@@ -541,7 +545,7 @@ int tppo_linear_bwd(const void *dy, int32_t dy_dtype, int64_t lddy, const void *
  *   grad      [R, C] of `grad_dtype`; not changed, unless `update` is grad itself
  *   momentum  [R, C] fp32 in/out, or NULL: U = grad (mu and nesterov are then not used)
  *   eps >= 0; 1 <= steps <= 16 (five is customary)
- *   scale     e.g. sqrt(max(1, R / C)); the caller applies weight -= lr * update
+ *   scale     e.g. sqrt(max(1, R / C)), at most 1e38 in magnitude; the caller applies weight -= lr * update
  *   update    [R, C] bf16 out; may be grad itself when that is bf16 with the same row stride
  *   workspace tppo_workspace_bytes(TPPO_OP_MUON, R, 0, 0, C) bytes
  * Precision: momentum and X are fp32; operands of the products are rounded to fp16, sums are fp32.  The

@@ -287,7 +287,12 @@ def tppo_advance_batch(seq_begin, prompt_len, prev_len, new_len, truncated, toke
         _ptr(slot_source, torch.int32), _ptr(counts, torch.int32), _stream()))
 
 
-_DTYPES = {torch.bfloat16: BF16, torch.float32: F32}
+class _Types(dict):
+    def __missing__(self, dtype):
+        raise AssertionError(f"expected torch.bfloat16 or torch.float32, got {dtype}")
+
+
+_DTYPES = _Types({torch.bfloat16: BF16, torch.float32: F32})
 _raw_stream, _current_device = torch._C._cuda_getCurrentRawStream, torch.cuda.current_device
 
 

@@ -72,6 +72,9 @@ __device__ __forceinline__ void store_vec(bf16_bits* p, const float (&v)[VEC]) {
     }
 }
 
+// The largest finite value of an element type.
+__device__ __forceinline__ float top_of(const float*) { return kFltMax; }
+__device__ __forceinline__ float top_of(const bf16_bits*) { return kBf16Max; }
 __device__ __forceinline__ bool is_finite(float v) { return fabsf(v) <= kFltMax; }
 
 inline bool is_finite_host(float v) { return v - v == 0.f; }

@@ -532,7 +532,8 @@ void (*linear_dz_pick(bool vec, bool act))(const DzArgs) {
 
 // dbias: the partial rows in ascending order within each of a column's 16 strands, then the strands.
 template <class T>
-__global__ void __launch_bounds__(512) linear_dbias_kernel(const float* partial, int32_t parts, int32_t N, T* dbias) {
+__global__ void __launch_bounds__(512) linear_dbias_kernel(const float* partial, int32_t parts, int32_t N, T* dbias,
+                                                           int32_t* status) {
     __shared__ double s[16][33];
     const int lane = threadIdx.x & 31, strand = threadIdx.x >> 5;
     const int64_t c = int64_t(blockIdx.x) * 32 + lane;
@@ -553,7 +554,10 @@ __global__ void __launch_bounds__(512) linear_dbias_kernel(const float* partial,
         t = 0.0;
 #pragma unroll
         for (int k = 0; k < 16; ++k) t += s[k][lane];
-        store_f32(dbias + c, float(t));
+        // a sum beyond the type, or partial sums beyond fp32
+        const bool fine = fabs(t) <= double(top_of(dbias));
+        if (!fine && status) atomicOr(status, TPPO_DEV_NONFINITE);
+        store_f32(dbias + c, fine ? float(t) : 0.f);
     }
 }
 
@@ -724,10 +728,11 @@ TPPO_API int tppo_linear_bwd(const void* dy, int32_t dy_dtype, int64_t lddy, con
             const dim3 grid((N + 31) / 32);
             if (bias_dtype == TPPO_F32)
                 TPPO_CUDA_CHECK(launch_dense(linear_dbias_kernel<float>, grid, dim3(512), 0, s,
-                                             static_cast<const float*>(w.partial), int32_t(gy), N, static_cast<float*>(dbias)));
+                                             static_cast<const float*>(w.partial), int32_t(gy), N, static_cast<float*>(dbias), status));
             else
                 TPPO_CUDA_CHECK(launch_dense(linear_dbias_kernel<bf16_bits>, grid, dim3(512), 0, s,
-                                             static_cast<const float*>(w.partial), int32_t(gy), N, static_cast<bf16_bits*>(dbias)));
+                                             static_cast<const float*>(w.partial), int32_t(gy), N, static_cast<bf16_bits*>(dbias),
+                                             status));
         }
     }
     if (dx) {        // dx[m, k] = sum_n dz[m, n] W[k, n]: both operands contiguous along the contraction

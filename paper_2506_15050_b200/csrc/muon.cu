@@ -147,9 +147,11 @@ __global__ void __launch_bounds__(kMuonThreads) muon_prepare_kernel(const Prepar
     if (bad && a.status) atomicOr(a.status, TPPO_DEV_NONFINITE);
 }
 
-// X's first operand U / (|U| + eps); every block adds the partial sums in the same order.
+// X's first operand U / (|U| + eps); every block adds the partial sums in the same order.  The first step
+// multiplies U by `inverse` again, so that U itself need not be written once more -- but where that
+// factor nears the ends of fp32's range the quotient is taken in fp64 and U replaced by it.
 __global__ void __launch_bounds__(kMuonThreads) muon_normalise_kernel(const double* partial, int32_t parts, float eps,
-                                                                      const float* x32, f16_bits* x16, float* inverse,
+                                                                      float* x32, f16_bits* x16, float* inverse,
                                                                       int64_t vectors) {
     __shared__ double red[kMuonThreads / 32];
     pdl_launch();
@@ -158,13 +160,20 @@ __global__ void __launch_bounds__(kMuonThreads) muon_normalise_kernel(const doub
     for (int i = threadIdx.x; i < parts; i += kMuonThreads) s += partial[i];
     const double norm = sqrt(block_sum(s, red)) + double(eps);
     const double inv = norm > 0.0 ? 1.0 / norm : 0.0;
-    const float f = inv < double(kFltMax) ? float(inv) : 0.f;
+    const bool far = norm > 0.0 && !(inv > 1e-30 && inv < 1e30);
+    const float f = far ? 1.f : float(inv);
     if (blockIdx.x == 0 && threadIdx.x == 0) *inverse = f;
     for (int64_t i = int64_t(blockIdx.x) * kMuonThreads + threadIdx.x; i < vectors; i += int64_t(gridDim.x) * kMuonThreads) {
         float v[8];
         load_vec<8>(x32 + i * 8, v);
+        if (far) {
 #pragma unroll
-        for (int k = 0; k < 8; ++k) v[k] *= f;
+            for (int k = 0; k < 8; ++k) v[k] = float(double(v[k]) * inv);
+            store_vec<8>(x32 + i * 8, v);
+        } else {
+#pragma unroll
+            for (int k = 0; k < 8; ++k) v[k] *= f;
+        }
         store_operand(x16 + i * 8, v);
     }
 }
@@ -381,7 +390,7 @@ TPPO_API int tppo_muon_orthogonalize(const void* grad, int32_t grad_dtype, int64
                                      void* update, int64_t ldu, int32_t* status, void* workspace, size_t workspace_bytes,
                                      void* stream) {
     if (R < 0 || C < 1 || ldg < C || ldu < C || (momentum && ldm < C) || steps < 1 || steps > 16 ||
-        !(eps >= 0.f) || !is_finite_host(eps) || !is_finite_host(scale) || (momentum && !is_finite_host(mu)) ||
+        !(eps >= 0.f) || !is_finite_host(eps) || !(fabsf(scale) <= 1e38f) || (momentum && !is_finite_host(mu)) ||
         (grad_dtype != TPPO_BF16 && grad_dtype != TPPO_F32))
         return TPPO_ERR_INVALID_ARG;
     if (R > kDenseMaxSize || C > kDenseMaxSize) return TPPO_ERR_UNSUPPORTED;
@@ -404,7 +413,7 @@ TPPO_API int tppo_muon_orthogonalize(const void* grad, int32_t grad_dtype, int64
     const int64_t vectors = R * w.ldx / 8, blocks = (vectors + kMuonThreads - 1) / kMuonThreads;
     TPPO_CUDA_CHECK(launch_dense(muon_normalise_kernel, dim3(unsigned(blocks < kMuonMaxBlocks ? blocks : kMuonMaxBlocks)),
                                  dim3(kMuonThreads), 0, s, static_cast<const double*>(w.partial), int32_t(parts), eps,
-                                 static_cast<const float*>(w.x32), w.x16[0], w.inverse, vectors));
+                                 w.x32, w.x16[0], w.inverse, vectors));
     for (int32_t k = 0; k < steps; ++k) {
         const DenseOperand X{w.x16[k % 2], R, C, w.ldx}, A{w.a, m, m, w.lda}, B{w.b, m, m, w.lda};
         const bool apart = m <= 64 || k >= steps - 3, last = k == steps - 1;

@@ -112,3 +112,17 @@ def test_muon_refusals(lib, p):
         (dict(g=a + 1), INVALID), (dict(m=a + 2), INVALID), (dict(u=a + 1), INVALID), (dict(ws=None), WORKSPACE), (dict(ws=a + 64), WORKSPACE),
         (dict(bytes=4096), WORKSPACE), (dict(bytes=lib.tppo_workspace_bytes(MUON, 4, 0, 0, 24) - 1), WORKSPACE)])
     assert lib.tppo_muon_orthogonalize(*[dict(good, R=0, g=None, u=None)[k] for k in args]) == 0
+
+
+def test_muon_scale_is_bounded(lib, p):
+    a = p[1]
+    for scale in (1.1e38, -3e38, float("inf")):               # times a singular value it could leave bf16
+        assert lib.tppo_muon_orthogonalize(a, 0, 24, None, 0, 4, 24, 0.0, 0, 1e-7, 5, scale, a, 24, None, a, 1 << 30, None) == INVALID
+
+
+def test_other_types_are_refused():
+    import torch
+
+    from paper_2506_15050_b200 import binding as b
+    with pytest.raises(AssertionError, match="bfloat16 or torch.float32"):
+        b._type_of(torch.ones(3, dtype=torch.float16))

@@ -209,6 +209,34 @@ def test_elements_that_are_not_finite():
         assert torch.equal(db.double(), d.sum(0)) and int(status) == b.DEV_NONFINITE
 
 
+def test_bias_gradient_beyond_its_type():
+    """Sums of finite dy that leave the range of dbias are written 0; the other columns keep theirs."""
+    from paper_2506_15050_b200 import binding as b
+    M, K, N = 70, 16, 24
+    x, w = torch.ones((M, K), dtype=BF, device=DEV), torch.ones((K, N), dtype=BF, device=DEV)
+    dy = torch.ones((M, N), dtype=BF, device=DEV)
+    dy[:, 5] = 1e37                                         # 70 of them pass both types' largest value
+    for dt in (BF, F32):
+        db, status = torch.empty(N, dtype=dt, device=DEV), torch.zeros(1, dtype=torch.int32, device=DEV)
+        b.tppo_linear_bwd(dy, x, w, b.ACT_NONE, None, None, None, db, status, workspace(M, K, N))
+        assert db.tolist() == [0.0 if n == 5 else 70.0 for n in range(N)] and int(status) == b.DEV_NONFINITE
+
+
+def test_gradient_operand_that_is_not_finite():
+    """A NaN of a bf16 dy that the products take as it is: what it enters is 0, the rest stays exact."""
+    from paper_2506_15050_b200 import binding as b
+    M, K, N, g = 40, 64, 64, gen(5)
+    x, w, dy = whole(g, M, K), whole(g, K, N), whole(g, M, N)
+    dy[3, 9] = float("nan")
+    dx, dw, status = torch.empty_like(x), torch.empty_like(w), torch.zeros(1, dtype=torch.int32, device=DEV)
+    b.tppo_linear_bwd(dy, x, w, b.ACT_NONE, None, dx, dw, None, status, workspace(M, K, N))
+    d = torch.nan_to_num(dy.double(), nan=0.0)
+    rx, rw = d @ w.double().t(), x.double().t() @ d
+    rx[3], rw[:, 9] = 0.0, 0.0
+    assert torch.equal(dx.double(), rx.to(BF).double()) and torch.equal(dw.double(), rw.to(BF).double())
+    assert int(status) == b.DEV_NONFINITE
+
+
 def test_no_rows():
     from paper_2506_15050_b200 import binding as b
     K, N = 24, 16

@@ -187,3 +187,15 @@ def test_extreme_values():
     ref[7, 8] = 0.0
     assert bool(torch.isfinite(m).all()) and near(up, reference(ref, 5, 1e-7))
     call(x[:0], update=torch.empty((0, 70), dtype=BF, device=DEV))
+
+
+@pytest.mark.parametrize("R,C", [(16, 24), (300, 120)])
+@pytest.mark.parametrize("power", [-149, 120])
+def test_norms_at_the_ends_of_the_range(R, C, power):
+    """Whole numbers times a power of two that leaves them exact in fp32; the reciprocal of the norm is not
+    representable there, the quotient is that of the whole numbers."""
+    x = torch.randint(-120, 121, (R, C), generator=gen(R + power + 200), device=DEV).float()
+    ref = reference(x, 5, 0.0)
+    y = (x.double() * 2.0 ** power).float()
+    assert torch.equal(y.double() * 2.0 ** -power, x.double())
+    assert near(call(y, eps=0.0), ref)
