@@ -116,6 +116,7 @@ constexpr size_t kDenseSmem = size_t(kDenseStages) * (kDenseABytes + kDenseBN * 
 struct DenseShape {
     int32_t m_tiles, n_tiles, k_steps, total;
     int32_t group_m;          // m-tiles per raster group: tiles of a group run next to each other in time
+    Link link;
 };
 
 template <bool SYM>
@@ -277,8 +278,7 @@ dense_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
     umma::fence_after_thread_sync();
     const uint32_t tmem = *reinterpret_cast<uint32_t*>(smem_raw + (slot - raw));
     // only now, with the tensor memory in hand: a dependent CTA on this SM allocates too
-    pdl_launch();
-    pdl_wait();
+    link_begin(g.link);
 
     bool timed_out = false;
     if (warp == 0) {
@@ -327,6 +327,7 @@ dense_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
         __syncwarp();
         umma::tmem_dealloc(tmem, 512);
     }
+    link_end(g.link);
 }
 
 // ---- few tiles ----------------------------------------------------------------------------------
@@ -358,6 +359,7 @@ template <int BN> __host__ __device__ constexpr size_t dense_split_smem() {
 struct DenseSplitShape {
     int32_t col_tiles;        // tiles along the output rows (BN each)
     int32_t k_steps;
+    Link link;
 };
 
 template <int AMAJ, int BMAJ, bool F16, int BN, class Epi>
@@ -400,8 +402,7 @@ dense_split_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
     ptx::cluster_sync_all();                 // every CTA of the cluster runs: its shared memory may be written
     umma::fence_after_thread_sync();
     const uint32_t tmem = *reinterpret_cast<uint32_t*>(smem_raw + (slot - raw));
-    pdl_launch();
-    pdl_wait();
+    link_begin(g.link);
 
     // this CTA's columns and, per thread, (output row, eight output columns) units; what the epilogue
     // reads is fetched kAhead units ahead, for the first ones while the product runs
@@ -489,6 +490,7 @@ dense_split_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
         umma::tmem_dealloc(tmem, kCols);     // all tensor-memory loads are behind the barrier
     }
     if (timed_out && status) atomicOr(status, TPPO_DEV_WAIT_TIMEOUT);
+    link_end(g.link);
 }
 
 // ---- host side ------------------------------------------------------------------------------------
@@ -498,7 +500,7 @@ struct DenseOperand { const void* p; int64_t rows, cols, ld; };
 // D[m, n] = sum_k A(m, k) B(k, n).  AMAJ 0: a is [m, k]; 1: a is [k, m].  BMAJ 0: b is [n, k]; 1: b is [k, n].
 template <int AMAJ, int BMAJ, bool F16, bool SYM, class Epi>
 int dense_gemm(const DenseOperand& a, const DenseOperand& b, int64_t m, int64_t n, int64_t k, const Epi& epi,
-               int32_t* status, cudaStream_t s) {
+               int32_t* status, cudaStream_t s, Link link) {
     CUtensorMap ma, mb;
     if (!make_bf16_tensor_map(&ma, a.p, a.rows, a.cols, a.ld, AMAJ ? 64 : kDenseTileM) ||
         !make_bf16_tensor_map(&mb, b.p, b.rows, b.cols, b.ld, BMAJ ? 64 : kDenseBN))
@@ -508,6 +510,7 @@ int dense_gemm(const DenseOperand& a, const DenseOperand& b, int64_t m, int64_t 
     g.n_tiles = int32_t((n + kDenseBN - 1) / kDenseBN);
     g.k_steps = int32_t((k + kDenseTileK - 1) / kDenseTileK);
     g.group_m = 16;
+    g.link = link;
     const int32_t pairs = g.m_tiles / 2;
     const int64_t total = SYM ? int64_t(pairs) * (pairs + 1) + (g.m_tiles % 2 ? pairs + 1 : 0) : int64_t(g.m_tiles) * g.n_tiles;
     if (total > 0x7fffffff) return TPPO_ERR_UNSUPPORTED;
@@ -524,7 +527,7 @@ int dense_gemm(const DenseOperand& a, const DenseOperand& b, int64_t m, int64_t 
 // BMAJ 0: b is [m, k]; 1: b is [k, m].
 template <int AMAJ, int BMAJ, bool F16, int BN, class Epi>
 int dense_split(const DenseOperand& a, const DenseOperand& b, int64_t m, int64_t n, int64_t k, int splits, const Epi& epi,
-                int32_t* status, cudaStream_t s) {
+                int32_t* status, cudaStream_t s, Link link) {
     CUtensorMap ma, mb;
     if (!make_bf16_tensor_map(&ma, a.p, a.rows, a.cols, a.ld, AMAJ ? 64 : kDenseTileM) ||
         !make_bf16_tensor_map(&mb, b.p, b.rows, b.cols, b.ld, BMAJ ? 64 : BN))
@@ -533,6 +536,7 @@ int dense_split(const DenseOperand& a, const DenseOperand& b, int64_t m, int64_t
     const int64_t row_tiles = (n + kDenseTileM - 1) / kDenseTileM, col_tiles = (m + BN - 1) / BN;
     g.col_tiles = int32_t(col_tiles);
     g.k_steps = int32_t((k + kDenseTileK - 1) / kDenseTileK);
+    g.link = link;
     if (row_tiles * col_tiles * splits > 0x7fffffff) return TPPO_ERR_UNSUPPORTED;
     auto kernel = dense_split_kernel<AMAJ, BMAJ, F16, BN, Epi>;
     constexpr size_t smem = dense_split_smem<BN>();
@@ -591,18 +595,18 @@ inline DenseCut dense_cut(int64_t m, int64_t n, int64_t k, int64_t big_tiles, in
 // [n, k], 1: [k, n]).  SYM: D is symmetric (m = n); the persistent kernel then computes half of it.
 template <int PMAJ, int QMAJ, bool F16, bool SYM, class Epi>
 int dense_product(const DenseOperand& P, const DenseOperand& Q, int64_t m, int64_t n, int64_t k, const Epi& epi,
-                  int32_t* status, cudaStream_t s) {
+                  int32_t* status, cudaStream_t s, Link link = kChain) {
     const int64_t mt = (m + 127) / 128, nt = (n + 255) / 256;
     const int64_t tiles = SYM ? mt / 2 * (mt / 2 + 1) + (mt % 2 ? mt / 2 + 1 : 0) : mt * nt;
     // one operand box of 64 outer indices is the least an MN-major operand can be loaded in
     constexpr int B16 = PMAJ ? 64 : 16, B32 = PMAJ ? 64 : 32;
     const DenseCut c = dense_cut(m, n, k, tiles, B16);
-    if (c.bn == 0) return dense_gemm<PMAJ, QMAJ, F16, SYM>(P, Q, m, n, k, epi, status, s);
-    if (c.bn == 16) return dense_split<QMAJ, PMAJ, F16, B16>(Q, P, m, n, k, c.splits, epi, status, s);
-    if (c.bn == 32) return dense_split<QMAJ, PMAJ, F16, B32>(Q, P, m, n, k, c.splits, epi, status, s);
-    if (c.bn == 64) return dense_split<QMAJ, PMAJ, F16, 64>(Q, P, m, n, k, c.splits, epi, status, s);
-    if (c.bn == 128) return dense_split<QMAJ, PMAJ, F16, 128>(Q, P, m, n, k, c.splits, epi, status, s);
-    return dense_split<QMAJ, PMAJ, F16, 256>(Q, P, m, n, k, c.splits, epi, status, s);
+    if (c.bn == 0) return dense_gemm<PMAJ, QMAJ, F16, SYM>(P, Q, m, n, k, epi, status, s, link);
+    if (c.bn == 16) return dense_split<QMAJ, PMAJ, F16, B16>(Q, P, m, n, k, c.splits, epi, status, s, link);
+    if (c.bn == 32) return dense_split<QMAJ, PMAJ, F16, B32>(Q, P, m, n, k, c.splits, epi, status, s, link);
+    if (c.bn == 64) return dense_split<QMAJ, PMAJ, F16, 64>(Q, P, m, n, k, c.splits, epi, status, s, link);
+    if (c.bn == 128) return dense_split<QMAJ, PMAJ, F16, 128>(Q, P, m, n, k, c.splits, epi, status, s, link);
+    return dense_split<QMAJ, PMAJ, F16, 256>(Q, P, m, n, k, c.splits, epi, status, s, link);
 }
 
 }  // namespace tppo

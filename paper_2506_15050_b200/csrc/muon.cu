@@ -152,10 +152,9 @@ __global__ void __launch_bounds__(kMuonThreads) muon_prepare_kernel(const Prepar
 // factor nears the ends of fp32's range the quotient is taken in fp64 and U replaced by it.
 __global__ void __launch_bounds__(kMuonThreads) muon_normalise_kernel(const double* partial, int32_t parts, float eps,
                                                                       float* x32, f16_bits* x16, float* inverse,
-                                                                      int64_t vectors) {
+                                                                      int64_t vectors, Link link) {
     __shared__ double red[kMuonThreads / 32];
-    pdl_launch();
-    pdl_wait();
+    link_begin(link);
     double s = 0.0;
     for (int i = threadIdx.x; i < parts; i += kMuonThreads) s += partial[i];
     const double norm = sqrt(block_sum(s, red)) + double(eps);
@@ -413,7 +412,8 @@ TPPO_API int tppo_muon_orthogonalize(const void* grad, int32_t grad_dtype, int64
     const int64_t vectors = R * w.ldx / 8, blocks = (vectors + kMuonThreads - 1) / kMuonThreads;
     TPPO_CUDA_CHECK(launch_dense(muon_normalise_kernel, dim3(unsigned(blocks < kMuonMaxBlocks ? blocks : kMuonMaxBlocks)),
                                  dim3(kMuonThreads), 0, s, static_cast<const double*>(w.partial), int32_t(parts), eps,
-                                 w.x32, w.x16[0], w.inverse, vectors));
+                                 w.x32, w.x16[0], w.inverse, vectors,
+                                 stream_link(R * w.ldx)));
     for (int32_t k = 0; k < steps; ++k) {
         const DenseOperand X{w.x16[k % 2], R, C, w.ldx}, A{w.a, m, m, w.lda}, B{w.b, m, m, w.lda};
         const bool apart = m <= 64 || k >= steps - 3, last = k == steps - 1;

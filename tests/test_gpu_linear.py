@@ -5,6 +5,8 @@ output has to be equal to the float64 product and a bf16 output to its one round
 tail error shows.  Real numbers: a sum of K products in fp32 is off by at most K 2^-23 times the sum
 of magnitudes (2^-23: a tensor core may cut instead of round); what the epilogue adds is written at
 each check."""
+import math
+
 import pytest
 import torch
 
@@ -235,6 +237,63 @@ def test_gradient_operand_that_is_not_finite():
     rx[3], rw[:, 9] = 0.0, 0.0
     assert torch.equal(dx.double(), rx.to(BF).double()) and torch.equal(dw.double(), rw.to(BF).double())
     assert int(status) == b.DEV_NONFINITE
+
+
+@pytest.mark.parametrize("M,K,N,act", [(1001, 515, 777, 2), (300, 264, 520, 1), (2500, 1000, 2000, 0), (40, 24, 16, 4)])
+def test_calls_one_behind_the_other(M, K, N, act):
+    """Backward calls that share a workspace, each taking the dx of the one before as its dy: launches of a
+    call that run side by side must neither overtake what they need nor leave anything behind them open."""
+    from paper_2506_15050_b200 import binding as b
+    g = gen(M + act)
+    ws, wt = workspace(M, K, N), workspace(M, N, K)
+    x, z = torch.randn((M, K), generator=g, device=DEV).to(BF), torch.randn((M, N), generator=g, device=DEV).to(BF)
+    w = (torch.randn((K, N), generator=g, device=DEV) / math.sqrt(N)).to(BF)
+    back = (torch.randn((N, K), generator=g, device=DEV) / math.sqrt(K)).to(BF)
+    dy0 = torch.randn((M, N), generator=g, device=DEV).to(BF)
+
+    def chain(wait):
+        dy, out = dy0, []
+        for k in range(6):
+            dx, dw, db = torch.empty_like(x), torch.empty_like(w), torch.empty(N, device=DEV)
+            b.tppo_linear_bwd(dy, x, w, act, z, dx, dw, db, None, ws)
+            wait()
+            dn, dv = torch.empty_like(dy), torch.empty_like(back)
+            b.tppo_linear_bwd(dx, z, back, act, x, dn, dv, None, None, wt)
+            wait()
+            out += [dx, dw, db, dn, dv]
+            dy = dn
+        torch.cuda.synchronize()
+        return out
+
+    apart = chain(torch.cuda.synchronize)
+    for _ in range(3):
+        assert all(torch.equal(p, q) for p, q in zip(chain(lambda: None), apart))
+
+
+@pytest.mark.parametrize("left,right", [(0, 0), (8, 8), (3, 2)])
+@pytest.mark.parametrize("M,K,N", [(9000, 5120, 1), (3001, 2056, 2), (2500, 4100, 3), (70, 2050, 5), (1300, 520, 8), (1, 7000, 4),
+                                   (5000, 3, 6), (200_000, 40, 1)])
+def test_gradients_of_few_columns(M, K, N, left, right):
+    from paper_2506_15050_b200 import binding as b
+    g = gen(M + K + N)
+    x, w, dy, z = whole(g, M, K, top=2), whole(g, K, N), whole(g, M, N, top=2), whole(g, M, N)
+    dz = dy.double() * (z.double() > 0)
+    rx, rw, rb = (dz @ w.double().t()).to(BF), (x.double().t() @ dz).to(BF), dz.sum(0)
+    x, w, dy, z = (strided(t, left, right) for t in (x, w, dy, z))
+    ws, status = workspace(M, K, N, 1), torch.zeros(1, dtype=torch.int32, device=DEV)
+    for f in (lambda t: t, lambda t: t.float()):                 # dy in either type
+        dx, dw, db = Guarded(M, K, BF, left, right), Guarded(K, N, BF, right, left), torch.full((N,), float("nan"), device=DEV)
+        b.tppo_linear_bwd(f(dy), x, w, b.ACT_RELU, z, dx.t, dw.t, db, status, ws)
+        assert torch.equal(dx.t, rx) and torch.equal(dw.t, rw) and torch.equal(db.double(), rb)
+        dx.check()
+        dw.check()
+    # any subset of the outputs
+    dx, dw, db = (torch.empty(n, dtype=BF, device=DEV) for n in ((M, K), (K, N), N))
+    b.tppo_linear_bwd(dy, x, w, b.ACT_RELU, z, dx, None, None, status, ws)
+    b.tppo_linear_bwd(dy, x, w, b.ACT_RELU, z, None, dw, None, status, ws)
+    b.tppo_linear_bwd(dy, x, w, b.ACT_RELU, z, None, None, db, status, ws)
+    assert torch.equal(dx, rx) and torch.equal(dw, rw) and torch.equal(db, rb.to(BF))
+    assert int(status) == 0
 
 
 def test_no_rows():
