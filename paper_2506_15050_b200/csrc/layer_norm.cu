@@ -12,8 +12,8 @@
 // beta stay in the registers of a block's threads for its whole walk over the rows; each block writes one
 // partial row of them to the workspace and a second kernel adds those in a fixed order, so the gradients
 // do not depend on scheduling.  Rows too long for either way take kernels that read the row again from L2.
-//   [16384, 5120] bf16: forward 63 us (5.3 TB/s, 0.81 of the measured copy rate), backward 128 us (3.9 TB/s)
-//   [16384, 5120] fp32: forward 107 us (6.3 TB/s), backward 176 us (5.7 TB/s)
+//   [16384, 5120] bf16: forward 63 us (5.3 TB/s, 0.81 of the measured copy rate), backward 112 us (4.5 TB/s)
+//   [16384, 5120] fp32: forward 107 us (6.3 TB/s), backward 165 us (6.1 TB/s)
 #include <type_traits>
 
 #include "dense_common.cuh"
@@ -657,25 +657,33 @@ __global__ void __launch_bounds__(512) norm_bwd_kernel(const NormBwdArgs a) {
 }
 
 // Aligned rows, one phase: a block takes ROWS rows at a time out of a ring of shared memory that bulk
-// copies fill `stages` rows ahead; every thread keeps its columns of x - mean (and of dy, as loaded) from
+// copies fill `stages` such groups of rows ahead, one barrier for each group (one per row keeps the compiler
+// from loading a row while it waits for the next: 72 us instead of 47 for 16384 x 2048); every thread keeps its columns of x - mean (and of dy, as loaded) from
 // the sums to the results, and one barrier serves all rows of a trip.
-template <class T, class P, int CH, int ROWS>
-__global__ void __launch_bounds__(640) norm_bwd_rows_kernel(const NormBwdArgs a) {
+template <class T, class P, int CH, int ROWS, int THREADS>
+__global__ void __launch_bounds__(THREADS) norm_bwd_rows_kernel(const NormBwdArgs a) {
     typedef RowVec<T> Q;
     constexpr int PAIRS = Q::kPairs, VALUES = 2 * ROWS;
-    extern __shared__ __align__(128) uint8_t ring[];     // [stages][x row, dy row], then one barrier per stage
+    extern __shared__ __align__(128) uint8_t ring[];     // [stages][ROWS][x row, dy row], then one barrier per stage
     __shared__ float red[2][20][VALUES];
     const int t = threadIdx.x, warp = t >> 5, lane = t & 31, warps = blockDim.x >> 5;
-    const uint32_t row_bytes = uint32_t(a.N) * sizeof(T), stage_bytes = 2 * row_bytes;
+    const uint32_t row_bytes = uint32_t(a.N) * sizeof(T), stage_bytes = ROWS * 2 * row_bytes;
     const uint32_t base = ptx::smem_addr(ring), full = base + a.stages * stage_bytes;
     const float inv_n = 1.f / float(a.N);
     const int64_t step = gridDim.x;
     const P* gamma = static_cast<const P*>(a.gamma);
-    auto issue = [&](int64_t r, int s) {
-        const uint32_t bar = full + 8 * s, at = base + s * stage_bytes;
-        ptx::mbar_arrive_expect_tx(bar, stage_bytes);
-        ptx::bulk_load(at, static_cast<const T*>(a.x) + r * a.ldx, row_bytes, bar);
-        ptx::bulk_load(at + row_bytes, static_cast<const T*>(a.dy) + r * a.lddy, row_bytes, bar);
+    // by the first warp: rows r0, r0 + step, .. into stage s, a lane per copy
+    auto issue = [&](int64_t r0, int s) {
+        if (r0 >= a.M) return;
+        const uint32_t bar = full + 8 * s;
+        const int64_t r = r0 + (lane >> 1) * step;
+        const bool mine = lane < 2 * ROWS && r < a.M;
+        const uint32_t copies = __popc(__ballot_sync(0xffffffffu, mine));
+        if (lane == 0) ptx::mbar_arrive_expect_tx(bar, copies * row_bytes);
+        __syncwarp();
+        if (mine)
+            ptx::bulk_load(base + s * stage_bytes + lane * row_bytes,
+                           lane & 1 ? static_cast<const T*>(a.dy) + r * a.lddy : static_cast<const T*>(a.x) + r * a.ldx, row_bytes, bar);
     };
     if (t == 0) {
         for (int s = 0; s < a.stages; ++s) ptx::mbar_init(full + 8 * s, 1);
@@ -683,8 +691,10 @@ __global__ void __launch_bounds__(640) norm_bwd_rows_kernel(const NormBwdArgs a)
     }
     pdl_launch();
     pdl_wait();
-    if (t == 0)
-        for (int s = 0; s < a.stages && blockIdx.x + s * step < a.M; ++s) issue(blockIdx.x + s * step, s);
+    if (warp == 0) {
+        __syncwarp();
+        for (int s = 0; s < a.stages; ++s) issue(blockIdx.x + s * ROWS * step, s);
+    }
     f32x2 dg[CH][PAIRS], db[CH][PAIRS], g[CH][PAIRS];
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
@@ -708,7 +718,9 @@ __global__ void __launch_bounds__(640) norm_bwd_rows_kernel(const NormBwdArgs a)
         float mean[ROWS], rstd[ROWS], part[VALUES];
         uint4 raw[ROWS][CH];
         f32x2 e[ROWS][CH][PAIRS];                // x - mean
-        const int first = stage;
+        // a wait that ran out is not repeated: the sums are then garbage, and flagged
+        if (!timed_out) timed_out = !ptx::mbar_wait<false>(full + 8 * stage, phase);
+        const uint32_t here = base + stage * stage_bytes;
 #pragma unroll
         for (int k = 0; k < ROWS; ++k) {
             const int64_t r = r0 + k * step, ahead = r + ROWS * step;
@@ -717,14 +729,12 @@ __global__ void __launch_bounds__(640) norm_bwd_rows_kernel(const NormBwdArgs a)
             if (ahead < a.M) { next_mean[k] = a.mean[ahead]; next_rstd[k] = a.rstd[ahead]; }
             f32x2 s = 0, q = 0;                   // sum of a, sum of a e
             if (r < a.M) {
-                // a wait that ran out is not repeated: the sums are then garbage, and flagged
-                if (!timed_out) timed_out = !ptx::mbar_wait<false>(full + 8 * stage, phase);
                 const f32x2 minus = twice(-mean[k]);
 #pragma unroll
                 for (int c = 0; c < CH; ++c) {
                     const int col = Q::col(c, a.group, t);
                     if (col < a.N) {
-                        const uint32_t at = base + stage * stage_bytes + col * uint32_t(sizeof(T));
+                        const uint32_t at = here + k * 2 * row_bytes + col * uint32_t(sizeof(T));
                         f32x2 d[PAIRS];
                         raw[k][c] = ptx::lds128(at + row_bytes);
                         Q::widen(ptx::lds128(at), e[k][c]);
@@ -738,23 +748,15 @@ __global__ void __launch_bounds__(640) norm_bwd_rows_kernel(const NormBwdArgs a)
                         }
                     }
                 }
-                if (++stage == a.stages) { stage = 0; phase ^= 1u; }
             }
             part[2 * k] = pair_sum(s);
             part[2 * k + 1] = pair_sum(q) * rstd[k];
         }
         float total = warp_sum_many<VALUES>(part);            // of value lane % VALUES
         if (lane < VALUES) red[flip][warp][lane] = total;
-        __syncthreads();                          // the partial sums are there, and the stages have been read
-        if (t == 0) {
-            int s = first;
-#pragma unroll 1
-            for (int k = 0; k < ROWS; ++k) {
-                const int64_t r = r0 + (k + a.stages) * step;
-                if (r < a.M) issue(r, s);
-                if (++s == a.stages) s = 0;
-            }
-        }
+        __syncthreads();                          // the partial sums are there, and the stage has been read
+        if (warp == 0) issue(r0 + int64_t(a.stages) * ROWS * step, stage);
+        if (++stage == a.stages) { stage = 0; phase ^= 1u; }
         total = 0.f;
         for (int w = lane / VALUES; w < warps; w += 32 / VALUES) total += red[flip][w][lane % VALUES];
 #pragma unroll
@@ -1043,8 +1045,8 @@ __global__ void __launch_bounds__(1024) norm_sum_kernel(const float* partial, in
     }
 }
 
-// Most blocks, and so partial rows, of a backward pass: five per SM of short rows, three of long ones.
-int norm_max_parts(int32_t N) { return N <= 2048 ? 5 * kNumSms : 3 * kNumSms; }
+// Most blocks, and so partial rows, of a backward pass: eight per SM of short rows, three of long ones.
+int norm_max_parts(int32_t N) { return N <= 512 ? 8 * kNumSms : N <= 2048 ? 5 * kNumSms : 3 * kNumSms; }
 
 bool rows_aligned(const void* p, int64_t ld, size_t esize) {
     return aligned(p, 16) && (ld * int64_t(esize)) % 16 == 0;
@@ -1125,29 +1127,36 @@ int norm_bwd_typed(NormBwdArgs a, P* dgamma, P* dbeta, float* row_flag, cudaStre
     int parts = 0, rc = TPPO_OK;
     const auto threads_of = [&](int cols, int unit) { return (int64_t(a.N) + cols * unit - 1) / (cols * unit) * unit; };
     const size_t stage = 2 * size_t(vec ? RowVec<T>::pitch(a.N) : RowAny<T>::pitch(a.N)), params = size_t(a.N) * 4 + 8 * 16;
-    constexpr int kRows = V == 8 ? 4 : 2;
+    // rows per trip of the one-phase kernel and threads per SM: what the registers hold
+    const bool wide = threads_of(8, 32) > 512;
+    const int per_trip = V == 8 && !wide ? 4 : 2, resident = V == 8 && !wide ? 512 : 640;
     const int cols = threads_of(16, 64) <= 640 ? 16 : 32;
-    // Which kernel, as measured (us for 8192 rows; registers / one phase / two phases):
-    //   bf16 264: 15 / 19 / 23, 520: 23 / 19 / 24, 1024: 34 / 24 / 27, 2048: 45 / 39 / 53, 4096: 75 / 72 / 67,
-    //   5120: 127 / 80 / 76 (16384 rows: - / 150 / 122; 1000 rows: 30 / 16 / 23), 8192: 153 / - / 128;
-    //   fp32 264: 13 / 19 / 22, 520: 23 / 20 / 24, 2048: 46 / 39 / 51, 5120: 150 / 87 / 119, 8192: 177 / - / 157;
-    //   unaligned bf16 263: 43 / - / 33, 1283: 71 / - / 45, 5121: 499 / - / 148 (1000 rows of 1283: 16 / - / 17);
-    //   unaligned fp32 515: 29 / - / 31, 1777: 56 / - / 89, 3001: 106 / - / 88
+    // Which kernel, as measured (us; registers / one phase / two phases):
+    //   bf16, 16384 rows of 256: 15 / 16 / -, 512: 21 / 19 / 24, 2048: 90 / 47 / 106, 4096: 150 / 83 / 114, 5120: - / 112
+    //   / 128; 8192 rows of 8192: 153 / - / 128; 4096 rows of 384: 12 / 11 / -, 256: 11 / 11 / -;
+    //   fp32, 16384 rows of 256: 15 / 21 / -, 384: 22 / 24 / -, 512: 44 / 27 / -; 8192 rows of 2048: 46 / 34 / 51, 5120:
+    //   150 / 83 / 119, 8192: 177 / - / 157;
+    //   unaligned bf16, 8192 rows of 263: 43 / - / 33, 1283: 71 / - / 45, 5121: 499 / - / 148 (1000 rows of 1283: 16 / - / 17);
+    //   unaligned fp32, 8192 rows of 515: 29 / - / 31, 1777: 56 / - / 89, 3001: 106 / - / 88
     const bool one = vec && a.M >= kNumSms && a.N >= 512 && threads_of(8, 32) <= 640 &&
-                     (kRows + 1) * stage + 8 * 16 <= kRingSmem && !(V == 8 && a.N >= 4096 && a.M >= 4096);
+                     2 * per_trip * stage + 8 * 16 <= kRingSmem;
     const bool two = !one && a.M >= kNumSms && threads_of(cols, 64) <= (cols == 16 ? 640 : 512) && stage + params <= kRingSmem &&
                      (vec ? a.N > 2048 : a.N >= 2048 || (V == 8 && a.M >= 2048));
     if (one) {
         a.group = int32_t(threads_of(8, 32));
-        int64_t per_sm = 640 / a.group;
+        int64_t per_sm = resident / a.group;
         if (per_sm > norm_max_parts(a.N) / kNumSms) per_sm = norm_max_parts(a.N) / kNumSms;
-        while (per_sm > 1 && kRingSmem / per_sm < (kRows + 1) * stage + 8 * 16) --per_sm;
-        const int64_t fit = int64_t((kRingSmem / per_sm - 8 * 16) / stage);
+        while (per_sm > 1 && kRingSmem / per_sm < 2 * per_trip * stage + 8 * 16) --per_sm;
+        const int64_t fit = int64_t((kRingSmem / per_sm - 8 * 16) / (per_trip * stage));
         a.stages = int32_t(fit < 16 ? fit : 16);
-        const size_t smem = size_t(a.stages) * stage + 8 * 16;
-        const int64_t most = kNumSms * per_sm;
-        parts = int(a.M < most ? a.M : most);
-        auto kernel = norm_bwd_rows_kernel<T, P, 8 / V, kRows>;
+        const size_t smem = size_t(a.stages) * per_trip * stage + 8 * 16;
+        // a block makes a whole trip at least, where that leaves one per SM: partial rows cost too (1000 x 1024 10 -> 8 us)
+        const int64_t most = kNumSms * per_sm, trips = a.M / per_trip;
+        parts = int(trips > most ? most : trips > kNumSms ? trips : kNumSms);
+        auto kernel = norm_bwd_rows_kernel<T, P, 8 / V, 2, 640>;
+        if constexpr (V == 8) {
+            if (!wide) kernel = norm_bwd_rows_kernel<T, P, 1, 4, 512>;
+        }
         TPPO_CUDA_CHECK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, int(smem)));
         TPPO_CUDA_CHECK(launch_dense(kernel, dim3(unsigned(parts)), dim3(a.group), smem, s, a));
     } else if (two) {
