@@ -1128,22 +1128,25 @@ int norm_bwd_typed(NormBwdArgs a, P* dgamma, P* dbeta, float* row_flag, cudaStre
     const auto threads_of = [&](int cols, int unit) { return (int64_t(a.N) + cols * unit - 1) / (cols * unit) * unit; };
     const size_t stage = 2 * size_t(vec ? RowVec<T>::pitch(a.N) : RowAny<T>::pitch(a.N)), params = size_t(a.N) * 4 + 8 * 16;
     // rows per trip of the one-phase kernel and threads per SM: what the registers hold
-    const bool wide = threads_of(8, 32) > 512;
-    const int per_trip = V == 8 && !wide ? 4 : 2, resident = V == 8 && !wide ? 512 : 640;
+    const int64_t eight = threads_of(8, 32);
+    const bool deep = eight > 640;              // 16 columns per thread
+    const int per_trip = deep ? V / 4 : V == 8 && eight <= 512 ? 4 : 2;
+    const int resident = deep || (V == 8 && eight <= 512) ? 512 : 640;
+    const int64_t row_threads = deep ? threads_of(16, 32) : eight;
     const int cols = threads_of(16, 64) <= 640 ? 16 : 32;
     // Which kernel, as measured (us; registers / one phase / two phases):
     //   bf16, 16384 rows of 256: 15 / 16 / -, 512: 21 / 19 / 24, 2048: 90 / 47 / 106, 4096: 150 / 83 / 114, 5120: - / 112
-    //   / 128; 8192 rows of 8192: 153 / - / 128; 4096 rows of 384: 12 / 11 / -, 256: 11 / 11 / -;
+    //   / 128 (187 with 16 columns per thread); 8192 rows of 6144: - / 104 / 116, 8192: 153 / 118 / 128; 4096 rows of 384: 12 / 11 / -, 256: 11 / 11 / -;
     //   fp32, 16384 rows of 256: 15 / 21 / -, 384: 22 / 24 / -, 512: 44 / 27 / -; 8192 rows of 2048: 46 / 34 / 51, 5120:
-    //   150 / 83 / 119, 8192: 177 / - / 157;
+    //   150 / 83 / 119, 6144: - / 99 / 124, 8192: 177 / 146 / 158;
     //   unaligned bf16, 8192 rows of 263: 43 / - / 33, 1283: 71 / - / 45, 5121: 499 / - / 148 (1000 rows of 1283: 16 / - / 17);
     //   unaligned fp32, 8192 rows of 515: 29 / - / 31, 1777: 56 / - / 89, 3001: 106 / - / 88
-    const bool one = vec && a.M >= kNumSms && a.N >= 512 && threads_of(8, 32) <= 640 &&
+    const bool one = vec && a.M >= kNumSms && a.N >= 512 && row_threads <= resident &&
                      2 * per_trip * stage + 8 * 16 <= kRingSmem;
     const bool two = !one && a.M >= kNumSms && threads_of(cols, 64) <= (cols == 16 ? 640 : 512) && stage + params <= kRingSmem &&
                      (vec ? a.N > 2048 : a.N >= 2048 || (V == 8 && a.M >= 2048));
     if (one) {
-        a.group = int32_t(threads_of(8, 32));
+        a.group = int32_t(row_threads);
         int64_t per_sm = resident / a.group;
         if (per_sm > norm_max_parts(a.N) / kNumSms) per_sm = norm_max_parts(a.N) / kNumSms;
         while (per_sm > 1 && kRingSmem / per_sm < 2 * per_trip * stage + 8 * 16) --per_sm;
@@ -1155,8 +1158,9 @@ int norm_bwd_typed(NormBwdArgs a, P* dgamma, P* dbeta, float* row_flag, cudaStre
         parts = int(trips > most ? most : trips > kNumSms ? trips : kNumSms);
         auto kernel = norm_bwd_rows_kernel<T, P, 8 / V, 2, 640>;
         if constexpr (V == 8) {
-            if (!wide) kernel = norm_bwd_rows_kernel<T, P, 1, 4, 512>;
+            if (eight <= 512) kernel = norm_bwd_rows_kernel<T, P, 1, 4, 512>;
         }
+        if (deep) kernel = norm_bwd_rows_kernel<T, P, 16 / V, V / 4, 512>;
         TPPO_CUDA_CHECK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, int(smem)));
         TPPO_CUDA_CHECK(launch_dense(kernel, dim3(unsigned(parts)), dim3(a.group), smem, s, a));
     } else if (two) {

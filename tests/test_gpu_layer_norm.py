@@ -176,6 +176,28 @@ def test_many_long_rows(M, N, left, right, dtype):
     assert torch.equal(z, y)
 
 
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("M,N", [(148, 512), (149, 640), (295, 1536), (593, 768), (1185, 520), (2369, 512), (5001, 2048), (150, 6144), (447, 7168),
+                                 (297, 4608)])
+def test_last_rows_of_a_walk(M, N, dtype):
+    """Blocks whose last trip holds some of its rows only, aligned rows inside a wider matrix of NaN."""
+    from paper_2506_15050_b200 import binding as b
+    x, dy, gamma, _ = make(M, N, dtype, M + N, offset=0.0)
+    _, m, r, _ = norm64(x, None, None, 1e-5)
+    mean, rstd = m.float(), r.float()
+    x, dy, dx = strided(x, 8, 16), strided(dy, 16, 8), Guarded(M, N, dtype, 8, 8)
+    ws, status = b.workspace(b.OP_LAYER_NORM, M, 0, 0, N, DEV), torch.zeros(1, dtype=torch.int32, device=DEV)
+    ws.fill_(0xff)
+    dg, db = torch.empty(N, device=DEV), torch.empty(N, device=DEV)
+    b.tppo_layer_norm_bwd(dy, x, gamma, mean, rstd, dx.t, dg, db, status, ws)
+    check_bwd(dy, x, gamma, mean, rstd, dx.t, dg, db)
+    dx.check()
+    assert int(status) == 0
+    one = [torch.empty_like(t) for t in (dg, db)]
+    b.tppo_layer_norm_bwd(dy, x, gamma, mean, rstd, None, *one, status, ws)
+    assert torch.equal(one[0], dg) and torch.equal(one[1], db)
+
+
 def test_gradient_against_differences():
     """<gradient, direction> against the central difference of <dy, y> in float64: its step 1e-4 leaves an
     error of order 1e-8, the fp32 gradients one of N M u at most relative to the sum of magnitudes."""
