@@ -1130,13 +1130,14 @@ int norm_bwd_typed(NormBwdArgs a, P* dgamma, P* dbeta, float* row_flag, cudaStre
     // rows per trip of the one-phase kernel and threads per SM: what the registers hold
     const int64_t eight = threads_of(8, 32);
     const bool deep = eight > 640;              // 16 columns per thread
-    const int per_trip = deep ? V / 4 : V == 8 && eight <= 512 ? 4 : 2;
+    const int per_trip = deep ? 1 : V == 8 && eight <= 512 ? 4 : 2;
     const int resident = deep || (V == 8 && eight <= 512) ? 512 : 640;
     const int64_t row_threads = deep ? threads_of(16, 32) : eight;
     const int cols = threads_of(16, 64) <= 640 ? 16 : 32;
     // Which kernel, as measured (us; registers / one phase / two phases):
     //   bf16, 16384 rows of 256: 15 / 16 / -, 512: 21 / 19 / 24, 2048: 90 / 47 / 106, 4096: 150 / 83 / 114, 5120: - / 112
-    //   / 128 (187 with 16 columns per thread); 8192 rows of 6144: - / 104 / 116, 8192: 153 / 118 / 128; 4096 rows of 384: 12 / 11 / -, 256: 11 / 11 / -;
+    //   / 128 (187 with 16 columns per thread); 8192 rows of 6144: - / 90 / 116 (two rows per trip 105: it spills),
+    //   8192: 153 / 99 / 128; 4096 rows of 384: 12 / 11 / -, 256: 11 / 11 / -;
     //   fp32, 16384 rows of 256: 15 / 21 / -, 384: 22 / 24 / -, 512: 44 / 27 / -; 8192 rows of 2048: 46 / 34 / 51, 5120:
     //   150 / 83 / 119, 6144: - / 99 / 124, 8192: 177 / 146 / 158;
     //   unaligned bf16, 8192 rows of 263: 43 / - / 33, 1283: 71 / - / 45, 5121: 499 / - / 148 (1000 rows of 1283: 16 / - / 17);
@@ -1160,7 +1161,7 @@ int norm_bwd_typed(NormBwdArgs a, P* dgamma, P* dbeta, float* row_flag, cudaStre
         if constexpr (V == 8) {
             if (eight <= 512) kernel = norm_bwd_rows_kernel<T, P, 1, 4, 512>;
         }
-        if (deep) kernel = norm_bwd_rows_kernel<T, P, 16 / V, V / 4, 512>;
+        if (deep) kernel = norm_bwd_rows_kernel<T, P, 16 / V, 1, 512>;
         TPPO_CUDA_CHECK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, int(smem)));
         TPPO_CUDA_CHECK(launch_dense(kernel, dim3(unsigned(parts)), dim3(a.group), smem, s, a));
     } else if (two) {
