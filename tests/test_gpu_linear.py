@@ -270,6 +270,38 @@ def test_calls_one_behind_the_other(M, K, N, act):
         assert all(torch.equal(p, q) for p, q in zip(chain(lambda: None), apart))
 
 
+@pytest.mark.parametrize("M,K,N", [(1001, 515, 777), (300, 264, 520), (2500, 1000, 2)])
+def test_captured_calls_one_behind_the_other(M, K, N):
+    from paper_2506_15050_b200 import binding as b
+    g = gen(M)
+    ws = workspace(M, K, N)
+    x, z, dy = (torch.randn((M, c), generator=g, device=DEV).to(BF) for c in (K, N, N))
+    w = (torch.randn((K, N), generator=g, device=DEV) / math.sqrt(N)).to(BF)
+    outs = [[torch.empty_like(x), torch.empty_like(w), torch.empty(N, device=DEV), torch.empty((M, N), dtype=BF, device=DEV)] for _ in range(4)]
+
+    def chain():
+        for dx, dw, db, y in outs:                           # each forward call reads the gradients just written
+            b.tppo_linear_bwd(dy, x, w, b.ACT_GELU, z, dx, dw, db, None, ws)
+            b.tppo_linear_fwd(dx, dw, db, b.ACT_NONE, None, y, None, None, ws)
+
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        chain()
+        side.synchronize()
+        want = [t.clone() for t in outs[0]]
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            chain()
+        for o in outs:
+            for t in o:
+                t.fill_(7.0)
+        for _ in range(3):
+            graph.replay()
+        side.synchronize()
+    assert all(torch.equal(t, v) for o in outs for t, v in zip(o, want))
+    del graph
+
+
 @pytest.mark.parametrize("left,right", [(0, 0), (8, 8), (3, 2)])
 @pytest.mark.parametrize("M,K,N", [(9000, 5120, 1), (3001, 2056, 2), (2500, 4100, 3), (70, 2050, 5), (1300, 520, 8), (1, 7000, 4),
                                    (5000, 3, 6), (200_000, 40, 1)])
