@@ -304,6 +304,10 @@ template <class Q> struct RowSource {
 };
 
 constexpr size_t kRingSmem = 220 * 1024;       // of all blocks on an SM together
+// What the ring kernels may be launched with.  A function's limit is state of the device that all calls share:
+// it is set to the same value every time, since another host thread may be about to launch with more than
+// this call needs.
+constexpr int kRingLimit = int(kRingSmem) + 128;
 constexpr int kRingThreads = 512;
 constexpr int kRingWarps = kRingThreads / 32;
 // Sum of one float per warp, in warp order, read by every thread itself (entries past the block's warps
@@ -1083,7 +1087,7 @@ int norm_fwd_typed(NormFwdArgs a, cudaStream_t s) {
         a.group = int32_t(threads);
         const size_t smem = size_t(a.stages) * row + 8 * 8;
         auto kernel = vec ? norm_fwd_ring_kernel<RowVec<T>, P, 32 / V> : norm_fwd_ring_kernel<RowAny<T>, P, 16>;
-        TPPO_CUDA_CHECK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, int(smem)));
+        TPPO_CUDA_CHECK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kRingLimit));
         TPPO_CUDA_CHECK(launch_dense(kernel, dim3(unsigned(kNumSms * per_sm)), dim3(a.group), smem, s, a));
         return TPPO_OK;
     }
@@ -1162,7 +1166,7 @@ int norm_bwd_typed(NormBwdArgs a, P* dgamma, P* dbeta, float* row_flag, cudaStre
             if (eight <= 512) kernel = norm_bwd_rows_kernel<T, P, 1, 4, 512>;
         }
         if (deep) kernel = norm_bwd_rows_kernel<T, P, 16 / V, 1, 512>;
-        TPPO_CUDA_CHECK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, int(smem)));
+        TPPO_CUDA_CHECK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kRingLimit));
         TPPO_CUDA_CHECK(launch_dense(kernel, dim3(unsigned(parts)), dim3(a.group), smem, s, a));
     } else if (two) {
         a.group = int32_t(threads_of(cols, 64));
@@ -1176,7 +1180,7 @@ int norm_bwd_typed(NormBwdArgs a, P* dgamma, P* dbeta, float* row_flag, cudaStre
         parts = int(a.M < most ? a.M : most);
         auto kernel = vec ? (cols == 16 ? norm_bwd_ring_kernel<RowVec<T>, P, 16 / V> : norm_bwd_ring_kernel<RowVec<T>, P, 32 / V>)
                           : (cols == 16 ? norm_bwd_ring_kernel<RowAny<T>, P, 8> : norm_bwd_ring_kernel<RowAny<T>, P, 16>);
-        TPPO_CUDA_CHECK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, int(smem)));
+        TPPO_CUDA_CHECK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kRingLimit));
         TPPO_CUDA_CHECK(launch_dense(kernel, dim3(unsigned(parts)), dim3(a.group), smem, s, a));
     } else if (pieces <= 512 * (vec ? 16 / V : 16)) {
         // the fewest columns per thread (16 at most) that keep a row within 256 threads, else 512

@@ -352,7 +352,8 @@ int linear_narrow(const DenseOperand& X, const DenseOperand& W, const EpiLinear&
     const int32_t K = int32_t(X.cols), kpad = (K + 7) / 8 * 8;
     const size_t smem = size_t(NB) * kpad * 2;
     auto kernel = vec ? linear_narrow_kernel<NB, true> : linear_narrow_kernel<NB, false>;
-    TPPO_CUDA_CHECK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, int(smem)));
+    // the same value in every call: another host thread may be about to launch with more than this one needs
+    TPPO_CUDA_CHECK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kNarrowMaxSmem));
     const int64_t blocks = (X.rows + 8 * kNarrowRows - 1) / (8 * kNarrowRows), most = 4 * kNumSms;
     TPPO_CUDA_CHECK(launch_dense(kernel, dim3(unsigned(blocks < most ? blocks : most)), dim3(256), smem, s,
                                  static_cast<const bf16_bits*>(X.p), X.ld, static_cast<const bf16_bits*>(W.p), W.ld, X.rows, K,

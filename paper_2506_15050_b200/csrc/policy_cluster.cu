@@ -362,7 +362,8 @@ static int plan_and_launch(const PolicyArgs& a, cudaStream_t s, int forced_stage
     const uint32_t smem_bytes = kClCtlBytes + stages * stride;
 
     auto kern = policy_cluster_kernel<C, OUT>;
-    if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, int(smem_bytes)) != cudaSuccess)
+    // the same value in every call: another host thread may be about to launch with more than this one needs
+    if (cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, max_optin) != cudaSuccess)
         return TPPO_ERR_CUDA;
     cudaLaunchConfig_t lc = {};
     cudaLaunchAttribute attr[1];
