@@ -290,6 +290,8 @@ template <class Q> struct RowSource {
             if constexpr (sizeof(*p) == 2) ptx::sts_u16(to, *reinterpret_cast<const uint16_t*>(q));
             else asm volatile("st.shared.f32 [%0], %1;" ::"r"(to), "f"(*reinterpret_cast<const float*>(q)) : "memory");
         }
+        // the stage's next row is written by a bulk copy of this thread: another proxy, ordered behind these stores
+        ptx::fence_proxy_async_smem();
     }
     __device__ __forceinline__ void copy(int64_t r, uint32_t at, uint32_t bar) const {
         uintptr_t lo;

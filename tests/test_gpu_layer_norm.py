@@ -264,3 +264,22 @@ def test_row_offsets_beyond_32_bits():
     mean, rstd, y = torch.empty(M, device=DEV), torch.empty(M, device=DEV), torch.empty_like(x)
     b.tppo_layer_norm_fwd(v, gamma, beta, 1e-5, y, mean, rstd, None)
     check_fwd(x, gamma, beta, 1e-5, y, mean, rstd)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("M,N", [(2100, 5120), (2500, 4096), (2049, 8192), (2100, 3001), (2048, 4100), (2600, 2571)])
+@pytest.mark.parametrize("left,right", [(0, 0), (8, 8), (1, 2)])
+def test_forward_of_many_rows(M, N, left, right, dtype):
+    """Two to four blocks per SM, each with its own ring, and several rows per block; the first and the last
+    row of a matrix at any alignment hold elements that no bulk copy brings, and their stages are used again."""
+    from paper_2506_15050_b200 import binding as b
+    x, _, gamma, beta = make(M, N, dtype, M + N)
+    if left + right:
+        x = strided(x, left, right)
+    for gm, bt in ((gamma, beta), (gamma.to(BF), None)):
+        y = Guarded(M, N, dtype, left, right)
+        mean, rstd, status = torch.empty(M, device=DEV), torch.empty(M, device=DEV), torch.zeros(1, dtype=torch.int32, device=DEV)
+        b.tppo_layer_norm_fwd(x, gm, bt, 1e-5, y.t, mean, rstd, status)
+        check_fwd(x, gm, bt, 1e-5, y.t, mean, rstd)
+        y.check()
+        assert int(status) == 0
