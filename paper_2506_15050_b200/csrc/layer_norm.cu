@@ -323,6 +323,20 @@ __device__ __forceinline__ float ring_sum(const float* red, int warps) {
     return s;
 }
 
+// A wait that ran out is not repeated: the rows are then garbage, and flagged.  Where it was the issuing
+// thread's, no further copy is issued, and before the block's memory goes away those in flight are awaited
+// here, each within the limit again: one stage per `step` rows, from row `lost` on, which was the one waited
+// for.  (`lost` is in shared memory and read behind the loop: a call or a register inside it costs up to 6 %.)
+__device__ __forceinline__ void ring_drain(uint32_t full, int stages, int64_t lost, int64_t step, int64_t M) {
+    const int64_t trip = (lost - int64_t(blockIdx.x)) / step;
+    int stage = int(trip % stages);
+    uint32_t phase = uint32_t(trip / stages) & 1u;
+    for (int k = 0; k < stages && lost < M; ++k, lost += step) {
+        if (!ptx::mbar_wait<false>(full + 8 * stage, phase)) return;
+        if (++stage == stages) { stage = 0; phase ^= 1u; }
+    }
+}
+
 // Forward: a block per row, rows brought in `stages` ahead; gamma and beta stay in registers.
 template <class Q, class P, int CH>
 __global__ void __launch_bounds__(kRingThreads) norm_fwd_ring_kernel(const NormFwdArgs a) {
@@ -330,6 +344,7 @@ __global__ void __launch_bounds__(kRingThreads) norm_fwd_ring_kernel(const NormF
     constexpr int PAIRS = Q::kPairs;
     extern __shared__ __align__(128) uint8_t ring[];     // [stages] rows, then one barrier per stage
     __shared__ __align__(16) float red[2][kRingWarps];
+    __shared__ int64_t lost;
     const int t = threadIdx.x, warp = t >> 5, lane = t & 31, warps = blockDim.x >> 5;
     const uint32_t pitch = Q::pitch(a.N);
     const uint32_t base = ptx::smem_addr(ring), full = base + a.stages * pitch;
@@ -343,6 +358,7 @@ __global__ void __launch_bounds__(kRingThreads) norm_fwd_ring_kernel(const NormF
     };
     if (t < 2 * kRingWarps) (&red[0][0])[t] = 0.f;
     if (t == 0) {
+        lost = -1;
         for (int s = 0; s < a.stages; ++s) ptx::mbar_init(full + 8 * s, 1);
         ptx::fence_mbar_init_cluster();
     }
@@ -364,8 +380,8 @@ __global__ void __launch_bounds__(kRingThreads) norm_fwd_ring_kernel(const NormF
     uint32_t phase = 0;
     bool timed_out = false;
     for (int64_t r = blockIdx.x; r < a.M; r += step) {
-        // a wait that ran out is not repeated: the rows are then garbage, and flagged
         if (!timed_out) timed_out = !ptx::mbar_wait<false>(full + 8 * stage, phase);
+        if (timed_out && t == 0 && lost < 0) lost = r;
         f32x2 v[CH][PAIRS], s = 0;
         const uint32_t at = x.first(r, base + stage * pitch);
 #pragma unroll
@@ -380,7 +396,7 @@ __global__ void __launch_bounds__(kRingThreads) norm_fwd_ring_kernel(const NormF
         float sum = warp_sum(pair_sum(s));
         if (lane == 0) red[0][warp] = sum;
         __syncthreads();                          // the sums are there, and the stage has been read
-        if (t == 0 && r + a.stages * step < a.M) issue(r + a.stages * step, stage);
+        if (t == 0 && !timed_out && r + a.stages * step < a.M) issue(r + a.stages * step, stage);
         if (++stage == a.stages) { stage = 0; phase ^= 1u; }
         const float mean = ring_sum(red[0], warps) * inv_n;
         s = 0;
@@ -424,7 +440,10 @@ __global__ void __launch_bounds__(kRingThreads) norm_fwd_ring_kernel(const NormF
             }
         }
     }
-    if (timed_out && a.status) atomicOr(a.status, TPPO_DEV_WAIT_TIMEOUT);
+    if (timed_out) {
+        if (t == 0) ring_drain(full, a.stages, lost, step, a.M);
+        if (a.status) atomicOr(a.status, TPPO_DEV_WAIT_TIMEOUT);
+    }
 }
 
 // A row of any length: one block, three sweeps (the second and third are served by L2).
@@ -672,6 +691,7 @@ __global__ void __launch_bounds__(THREADS) norm_bwd_rows_kernel(const NormBwdArg
     constexpr int PAIRS = Q::kPairs, VALUES = 2 * ROWS;
     extern __shared__ __align__(128) uint8_t ring[];     // [stages][ROWS][x row, dy row], then one barrier per stage
     __shared__ float red[2][20][VALUES];
+    __shared__ int64_t lost;
     const int t = threadIdx.x, warp = t >> 5, lane = t & 31, warps = blockDim.x >> 5;
     const uint32_t row_bytes = uint32_t(a.N) * sizeof(T), stage_bytes = ROWS * 2 * row_bytes;
     const uint32_t base = ptx::smem_addr(ring), full = base + a.stages * stage_bytes;
@@ -692,6 +712,7 @@ __global__ void __launch_bounds__(THREADS) norm_bwd_rows_kernel(const NormBwdArg
                            lane & 1 ? static_cast<const T*>(a.dy) + r * a.lddy : static_cast<const T*>(a.x) + r * a.ldx, row_bytes, bar);
     };
     if (t == 0) {
+        lost = -1;
         for (int s = 0; s < a.stages; ++s) ptx::mbar_init(full + 8 * s, 1);
         ptx::fence_mbar_init_cluster();
     }
@@ -724,8 +745,7 @@ __global__ void __launch_bounds__(THREADS) norm_bwd_rows_kernel(const NormBwdArg
         float mean[ROWS], rstd[ROWS], part[VALUES];
         uint4 raw[ROWS][CH];
         f32x2 e[ROWS][CH][PAIRS];                // x - mean
-        // a wait that ran out is not repeated: the sums are then garbage, and flagged
-        if (!timed_out) timed_out = !ptx::mbar_wait<false>(full + 8 * stage, phase);
+        if (!timed_out) timed_out = !ptx::mbar_wait_warp<false>(full + 8 * stage, phase);   // one answer per warp: the first issues
         const uint32_t here = base + stage * stage_bytes;
 #pragma unroll
         for (int k = 0; k < ROWS; ++k) {
@@ -761,7 +781,10 @@ __global__ void __launch_bounds__(THREADS) norm_bwd_rows_kernel(const NormBwdArg
         float total = warp_sum_many<VALUES>(part);            // of value lane % VALUES
         if (lane < VALUES) red[flip][warp][lane] = total;
         __syncthreads();                          // the partial sums are there, and the stage has been read
-        if (warp == 0) issue(r0 + int64_t(a.stages) * ROWS * step, stage);
+        if (warp == 0) {
+            if (!timed_out) issue(r0 + int64_t(a.stages) * ROWS * step, stage);
+            else if (t == 0 && lost < 0) lost = r0;
+        }
         if (++stage == a.stages) { stage = 0; phase ^= 1u; }
         total = 0.f;
         for (int w = lane / VALUES; w < warps; w += 32 / VALUES) total += red[flip][w][lane % VALUES];
@@ -798,7 +821,10 @@ __global__ void __launch_bounds__(THREADS) norm_bwd_rows_kernel(const NormBwdArg
             }
         }
     }
-    if (timed_out && a.status) atomicOr(a.status, TPPO_DEV_WAIT_TIMEOUT);
+    if (timed_out) {
+        if (t == 0) ring_drain(full, a.stages, lost, ROWS * step, a.M);
+        if (a.status) atomicOr(a.status, TPPO_DEV_WAIT_TIMEOUT);
+    }
     if (!a.partial) return;
     float* out = a.partial + int64_t(blockIdx.x) * 2 * a.N;
 #pragma unroll
@@ -826,6 +852,7 @@ __global__ void __launch_bounds__(CH * Q::kVec > 16 ? 512 : 640) norm_bwd_ring_k
     extern __shared__ __align__(128) uint8_t ring[];     // [stages][x row, dy row], one barrier per stage, gamma as fp32
     __shared__ float2 red[2][10];                        // [row][warp of its half]
     __shared__ float2 stat[2][2];                        // [trip parity][row] mean, rstd
+    __shared__ int64_t lost;
     const int t = threadIdx.x, warp = t >> 5, lane = t & 31, half = int(blockDim.x) >> 6;   // warps per row
     const uint32_t pitch = Q::pitch(a.N), stage_bytes = 2 * pitch;
     const uint32_t base = ptx::smem_addr(ring), full = base + a.stages * stage_bytes, gam = full + 8 * 16;
@@ -842,6 +869,7 @@ __global__ void __launch_bounds__(CH * Q::kVec > 16 ? 512 : 640) norm_bwd_ring_k
         sd.copy(r, at + pitch, bar);
     };
     if (t == 0) {
+        lost = -1;
         for (int s = 0; s < a.stages; ++s) ptx::mbar_init(full + 8 * s, 1);
         ptx::fence_mbar_init_cluster();
     }
@@ -875,7 +903,6 @@ __global__ void __launch_bounds__(CH * Q::kVec > 16 ? 512 : 640) norm_bwd_ring_k
         // sums
         if (part < half && (mine == 0 || two)) {
             const int st = mine ? stage1 : stage;
-            // a wait that ran out is not repeated: the sums are then garbage, and flagged
             if (!timed_out) timed_out = !ptx::mbar_wait<false>(full + 8 * st, mine ? phase1 : phase);
             const float2 ms = stat[flip][mine];
             const f32x2 minus = twice(-ms.x);
@@ -948,8 +975,12 @@ __global__ void __launch_bounds__(CH * Q::kVec > 16 ? 512 : 640) norm_bwd_ring_k
         }
         __syncthreads();                          // both stages have been read, and `red`
         if (t == 0) {
-            if (r0 + a.stages * step < a.M) issue(r0 + a.stages * step, stage);
-            if (rows == 2 && r0 + (a.stages + 1) * step < a.M) issue(r0 + (a.stages + 1) * step, stage1);
+            if (!timed_out) {
+                if (r0 + a.stages * step < a.M) issue(r0 + a.stages * step, stage);
+                if (rows == 2 && r0 + (a.stages + 1) * step < a.M) issue(r0 + (a.stages + 1) * step, stage1);
+            } else if (lost < 0) {
+                lost = r0;                        // or the row behind it: row r0 is there then
+            }
         }
         if (rows == 1) {
             phase ^= 1u;
@@ -958,7 +989,10 @@ __global__ void __launch_bounds__(CH * Q::kVec > 16 ? 512 : 640) norm_bwd_ring_k
             phase = stage1 + 1 == a.stages ? phase1 ^ 1u : phase1;
         }
     }
-    if (timed_out && a.status) atomicOr(a.status, TPPO_DEV_WAIT_TIMEOUT);
+    if (timed_out) {
+        if (t == 0) ring_drain(full, a.stages, lost, step, a.M);
+        if (a.status) atomicOr(a.status, TPPO_DEV_WAIT_TIMEOUT);
+    }
     if (!a.partial) return;
     float* out = a.partial + int64_t(blockIdx.x) * 2 * a.N;
 #pragma unroll
