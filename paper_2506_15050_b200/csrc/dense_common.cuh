@@ -93,8 +93,12 @@ __device__ __forceinline__ void pdl_wait() { asm volatile("griddepcontrol.wait;"
 //   kLead    lets what follows start only when every block of this launch has seen its predecessor's end
 //            -- so that the follower may run beside it.
 //   kBeside  follows a kLead, or a kBeside behind one, and needs nothing that these write: everything
-//            before them is complete and visible when it starts.  It waits for its predecessor before it
-//            ends, so that its own end covers theirs for whatever comes next.
+//            before them was complete, and performed for the whole lead's grid, when it was let start.  It
+//            begins with no wait, which is what the documentation ties visibility to, so it takes none on trust:
+//            a gpu-scope fence (and one towards the copy engine's proxy) stands before its first load, and what
+//            a call rewrites in its workspace each time is read at L2 (tensor copies, __ldcg), where the
+//            lead's wait has it.  It waits for its predecessor before it ends, so that its own end covers
+//            theirs for whatever comes next.
 //   kTail    what follows starts when this launch has ended.  A product's CTA that waits on an SM holds nearly all
 //            of its shared memory, which a kernel that streams through L1 then lacks (16384 x 5120: dz 109
 //            us instead of 116, 20 us of a whole backward pass).
@@ -104,7 +108,8 @@ enum : int32_t { kChain = 0, kLead = 1, kBeside = 2, kTail = 4 };
 typedef int32_t Link;
 __device__ __forceinline__ void link_begin(Link link) {
     if (!(link & (kLead | kTail))) pdl_launch();
-    if (!(link & kBeside)) pdl_wait();
+    if (link & kBeside) asm volatile("fence.acq_rel.gpu;\n\tfence.proxy.async.global;" ::: "memory");
+    else pdl_wait();
     if (link & kLead) pdl_launch();
 }
 __device__ __forceinline__ void link_end(Link link) {

@@ -546,7 +546,7 @@ __global__ void __launch_bounds__(512) linear_dbias_kernel(const float* partial,
         for (int p0 = strand; p0 < parts; p0 += 8 * 16) {        // eight loads in flight
             float v[8];
 #pragma unroll
-            for (int k = 0; k < 8; ++k) v[k] = p0 + 16 * k < parts ? partial[int64_t(p0 + 16 * k) * N + c] : 0.f;
+            for (int k = 0; k < 8; ++k) v[k] = p0 + 16 * k < parts ? __ldcg(partial + int64_t(p0 + 16 * k) * N + c) : 0.f;   // at L2: see kBeside
 #pragma unroll
             for (int k = 0; k < 8; ++k) t += double(v[k]);
         }

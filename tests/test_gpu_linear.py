@@ -380,3 +380,32 @@ def test_refusals_on_the_device():
             bad()
     torch.cuda.synchronize()
     assert bool((y == 7).all())
+
+
+@pytest.mark.parametrize("M,K,N,act", [(1001, 515, 777, 2), (300, 264, 520, 1), (4100, 520, 2050, 4), (65, 72, 1000, 0)])
+def test_buffers_refilled_before_each_call(M, K, N, act):
+    """Every operand is written anew, in place, right before each call, which then rewrites its workspace: what
+    runs side by side in a call may not see the values that the call before left in these places."""
+    from paper_2506_15050_b200 import binding as b
+    g = gen(M + K)
+    r = lambda *s: [torch.randn(s, generator=g, device=DEV).to(BF) for _ in range(5)]
+    sets = list(zip(r(M, N), r(M, K), r(K, N), r(M, N)))
+    ws = workspace(M, K, N)
+    call = lambda dy, x, w, z, o: b.tppo_linear_bwd(dy, x, w, act, z if act else None, *o, None, ws)
+    empty = lambda: (torch.empty((M, K), dtype=BF, device=DEV), torch.empty((K, N), dtype=BF, device=DEV), torch.empty(N, device=DEV))
+    want = []
+    for s in sets:
+        o = empty()
+        call(*s, o)
+        torch.cuda.synchronize()
+        want.append(o)
+    mine, got, out = [t.clone() for t in sets[0]], [], empty()
+    for _ in range(4):
+        for s, w in zip(sets, want):
+            for a, t in zip(mine, s):
+                a.copy_(t)
+            call(*mine, out)
+            got.append((tuple(t.clone() for t in out), w))
+    torch.cuda.synchronize()
+    for o, w in got:
+        assert all(torch.equal(a, t) for a, t in zip(o, w))
