@@ -369,7 +369,9 @@ def tppo_linear_fwd(x, weight, bias, activation, residual, y, preact, status, ws
 
 
 def tppo_linear_bwd(dy, x, weight, activation, preact, dx, dweight, dbias, status, ws):
-    (M, K), N, here, bf = x.shape, weight.shape[1], _current_device(), torch.bfloat16
+    """x may be None without dweight, weight without dx; K is the other operand's then."""
+    (M, N), here, bf = dy.shape, _current_device(), torch.bfloat16
+    K = x.shape[1] if x is not None else weight.shape[0] if weight is not None else 1       # dbias alone needs none
     pd, lddy = _matrix(dy, here, M, N)
     px, ldx = _matrix(x, here, M, K, bf)
     pw, ldw = _matrix(weight, here, K, N, bf)

@@ -909,7 +909,7 @@ TPPO_API int tppo_linear_bwd(const void* dy, int32_t dy_dtype, int64_t lddy, con
                              int64_t ldw, int64_t M, int32_t K, int32_t N, int32_t activation, const void* preact,
                              int64_t ldp, void* dx, int64_t lddx, void* dweight, int64_t lddw, void* dbias,
                              int32_t bias_dtype, int32_t* status, void* workspace, size_t workspace_bytes, void* stream) {
-    if (M < 0 || K < 1 || N < 1 || lddy < N || ldx < K || ldw < N || (dx && lddx < K) ||
+    if (M < 0 || K < 1 || N < 1 || lddy < N || (x && ldx < K) || (weight && ldw < N) || (dx && lddx < K) ||
         (dweight && lddw < N) || !act_known(activation) || (activation != TPPO_ACT_NONE && ldp < N))
         return TPPO_ERR_INVALID_ARG;
     if ((dy_dtype != TPPO_BF16 && dy_dtype != TPPO_F32) || (dbias && bias_dtype != TPPO_BF16 && bias_dtype != TPPO_F32))

@@ -126,3 +126,15 @@ def test_other_types_are_refused():
     from paper_2506_15050_b200 import binding as b
     with pytest.raises(AssertionError, match="bfloat16 or torch.float32"):
         b._type_of(torch.ones(3, dtype=torch.float16))
+
+
+def test_linear_backward_without_an_operand(lib, p):
+    """x is not needed without dweight, weight not without dx: neither they nor their strides are looked at."""
+    a = p[1]
+    args = "dy dtype lddy x ldx w ldw M K N act pre ldp dx lddx dw lddw db bdtype status ws bytes stream".split()
+    good = dict(dy=a, dtype=0, lddy=24, x=None, ldx=0, w=None, ldw=0, M=0, K=16, N=24, act=0, pre=None, ldp=0, dx=None, lddx=0, dw=None, lddw=0,
+                db=None, bdtype=1, status=None, ws=None, bytes=0, stream=None)
+    for change in (dict(), dict(x=a, ldx=16), dict(w=a, ldw=24), dict(M=4), dict(M=4, x=a, ldx=16)):
+        assert lib.tppo_linear_bwd(*[dict(good, **change)[k] for k in args]) == 0
+    refused(lib.tppo_linear_bwd, args, dict(good, M=4), [
+        (dict(x=a, ldx=15), INVALID), (dict(w=a, ldw=23), INVALID), (dict(dx=a, lddx=16), INVALID), (dict(dw=a, lddw=24), INVALID)])

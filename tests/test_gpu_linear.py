@@ -409,3 +409,17 @@ def test_buffers_refilled_before_each_call(M, K, N, act):
     torch.cuda.synchronize()
     for o, w in got:
         assert all(torch.equal(a, t) for a, t in zip(o, w))
+
+
+def test_gradients_without_one_of_the_operands():
+    from paper_2506_15050_b200 import binding as b
+    for M, K, N in ((40, 64, 72), (33, 130, 2)):
+        g = gen(M)
+        x, w, dy = whole(g, M, K), whole(g, K, N), whole(g, M, N)
+        dx, dw, db, ws = torch.empty_like(x), torch.empty_like(w), torch.empty(N, device=DEV), workspace(M, K, N)
+        b.tppo_linear_bwd(dy, None, w, b.ACT_NONE, None, dx, None, None, None, ws)
+        b.tppo_linear_bwd(dy, x, None, b.ACT_NONE, None, None, dw, db, None, ws)
+        assert torch.equal(dx, (dy.double() @ w.double().t()).to(BF)) and torch.equal(dw, (x.double().t() @ dy.double()).to(BF))
+        assert torch.equal(db.double(), dy.double().sum(0))
+    b.tppo_linear_bwd(dy, None, None, b.ACT_NONE, None, None, None, db.zero_(), None, ws)
+    assert torch.equal(db.double(), dy.double().sum(0))
