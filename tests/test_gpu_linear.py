@@ -423,3 +423,25 @@ def test_gradients_without_one_of_the_operands():
         assert torch.equal(db.double(), dy.double().sum(0))
     b.tppo_linear_bwd(dy, None, None, b.ACT_NONE, None, None, None, db.zero_(), None, ws)
     assert torch.equal(db.double(), dy.double().sum(0))
+
+
+def test_gelu_tails():
+    """gelu of -12 .. -1 and its slope, each relative to itself.  Phi(z) is a product of exp(-z^2/2), whose argument
+    carries three roundings of a number that it multiplies by z^2 / 2 (1.5 z^2 u) and ex2 four, a polynomial
+    in t whose terms add up to 1.8 times its value in magnitude, eight roundings each (15 u), its fit (1.5 u),
+    t (4 u) and three more products: 1.5 z^2 + 28 roundings, 32 here."""
+    from paper_2506_15050_b200 import binding as b
+    z = -(1 + 11 * torch.arange(2001, device=DEV) / 2000).to(BF)
+    N = z.numel()
+    x, w = torch.ones((1, 1), dtype=BF, device=DEV), z[None, :].contiguous()
+    y, ws = torch.empty((1, N), device=DEV), workspace(1, 1, N)
+    b.tppo_linear_fwd(x, w, None, b.ACT_GELU, None, y, None, None, ws)
+    ref = act64(z.double(), 2)
+    rel = (1.5 * z.double() ** 2 + 32) * U32
+    err = ((y[0].double() - ref) / ref).abs()
+    assert bool((err <= rel).all()), (err / rel).max().item()
+    db, dy = torch.empty(N, device=DEV), torch.ones((1, N), device=DEV)
+    b.tppo_linear_bwd(dy, x, w, b.ACT_GELU, w, None, None, db, None, ws)
+    terms = act64(z.double(), 2).abs() / z.double().abs() + z.double().abs() * torch.exp(-z.double() ** 2 / 2) / math.sqrt(2 * math.pi)
+    err = (db.double() - slope64(z.double(), 2)).abs()
+    assert bool((err <= rel * terms).all()), (err / (rel * terms)).max().item()
