@@ -521,7 +521,9 @@ int tppo_linear_fwd(const void *x, int64_t ldx, const void *weight, int64_t ldw,
  *   x may be NULL without dweight, weight without dx
  *   workspace as for tppo_linear_fwd: for dz, the partial sums of dbias and operand copies; may be
  *   NULL when none is needed (TPPO_ACT_NONE, aligned bf16 operands, no dbias)
- * dz is rounded to bf16 before the two products (dbias sums the unrounded values); an element of dz or
+ * dz is rounded to bf16 before the two products where these run on the tensor cores -- always for N > 4, and for
+ * fewer columns of more than 2^23 elements of x whose rows are not 16-byte aligned -- and kept in fp32 elsewhere
+ * (dbias sums the unrounded values); an element of dz or
  * of an output that is not finite or leaves the range of bf16 counts or is written as 0 and raises
  * TPPO_DEV_NONFINITE.  (Where dy itself can be the operand -- TPPO_ACT_NONE, aligned bf16 -- the products may
  * take it as it is: its elements that are not finite then make every element of dx and dweight that they

@@ -6,7 +6,8 @@
 //
 // dz is the one intermediate that is rounded: both gradients contract it on the tensor cores, so it
 // is formed once, in bf16 like the operand it meets, by a kernel that also sums dbias from the
-// unrounded values.  (Without an activation and with an aligned bf16 dy that kernel writes nothing
+// unrounded values.  (The error of dx and dweight against 64 bits goes from 1.7e-3, their own rounding, to
+// 2.3e-3; carrying dz in two bf16 parts would double the products.  The narrow backward kernel keeps fp32.)  (Without an activation and with an aligned bf16 dy that kernel writes nothing
 // and dy itself is the operand.)
 //
 // Large outputs are tensor bound and take the persistent kernel; a handful of columns is no work for tensor
@@ -650,7 +651,7 @@ __global__ void __launch_bounds__(256, narrow_blocks<NB>()) linear_narrow_bwd_ke
                 if (!(fabsf(v) <= kBf16Max)) { v = 0.f; bad = true; }
                 bias += v;
             }
-            dz[i] = bf16_lo(pack_bf16x2(v, 0.f));
+            dz[i] = v;                          // fp32: nothing here feeds a tensor core
         }
         __syncthreads();
         if (count == 0) continue;

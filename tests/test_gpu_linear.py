@@ -445,3 +445,27 @@ def test_gelu_tails():
     terms = act64(z.double(), 2).abs() / z.double().abs() + z.double().abs() * torch.exp(-z.double() ** 2 / 2) / math.sqrt(2 * math.pi)
     err = (db.double() - slope64(z.double(), 2)).abs()
     assert bool((err <= rel * terms).all()), (err / (rel * terms)).max().item()
+
+
+@pytest.mark.parametrize("act", [0, 4])
+@pytest.mark.parametrize("M,K,N", [(9000, 5120, 1), (2500, 4100, 3), (1300, 520, 2), (70, 2051, 4), (1, 8, 1)])
+def test_fp32_gradients_of_few_columns(M, K, N, act):
+    """dz stays in fp32: one rounding of dx, and of dweight after sums of some hundred fp32 additions.  Rows that are
+    not 16-byte aligned, from 2^23 elements of x on, take the tensor cores, as the header says: their dz is rounded
+    to bf16 once, which adds half a step of it through both products."""
+    from paper_2506_15050_b200 import binding as b
+    g = gen(M + N)
+    x, w = torch.randn((M, K), generator=g, device=DEV).to(BF), torch.randn((K, N), generator=g, device=DEV).to(BF)
+    dy, z = torch.randn((M, N), generator=g, device=DEV), torch.randn((M, N), generator=g, device=DEV).to(BF)
+    dx, dw, db = torch.empty_like(x), torch.empty_like(w), torch.empty(N, device=DEV)
+    b.tppo_linear_bwd(dy, x, w, act, z if act else None, dx, dw, db, None, workspace(M, K, N))
+    slope = slope64(z.double(), act) if act else torch.ones_like(dy).double()
+    dz = dy.double() * slope
+    e_dz = 24 * U32 * dy.double().abs() * (1 + z.double().abs()) if act else 0 * dz
+    if K % 8 and M * K > 1 << 23:
+        e_dz = e_dz + half_step(BF) * dz.abs()
+    wd, xd = w.double(), x.double()
+    for got, ref, mag, e in ((dx, dz @ wd.t(), dz.abs() @ wd.abs().t(), e_dz @ wd.abs().t()),
+                             (dw, xd.t() @ dz, xd.abs().t() @ dz.abs(), xd.abs().t() @ e_dz)):
+        tol = (half_step(BF) + U32) * ref.abs() + 320 * U32 * mag + 1.01 * e
+        assert bool(((got.double() - ref).abs() <= tol).all()), ((got.double() - ref).abs() / tol).max().item()
