@@ -469,6 +469,9 @@ constexpr int kDzRows = 4;
 
 template <class T, bool VEC, bool ACT>
 __global__ void __launch_bounds__(256) linear_dz_kernel(const DzArgs a) {
+    // Without an activation a bf16 dy is the products' operand as it is, elements that are not finite with it;
+    // whether it is read in place or from a copy made here is a matter of alignment and speed.
+    constexpr bool AS_IS = !ACT && sizeof(T) == 2;
     __shared__ float sums[8][256 + 8];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int n = blockIdx.x * 256 + lane * 8;
@@ -506,6 +509,9 @@ __global__ void __launch_bounds__(256) linear_dz_kernel(const DzArgs a) {
 #pragma unroll
                         for (int i = 0; i < 8; ++i) v[i] *= slope[i];
                     }
+                    float kept[8];
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) kept[i] = v[i];
                     if (!all_within(v, kBf16Max)) {
                         bad = true;
 #pragma unroll
@@ -514,7 +520,8 @@ __global__ void __launch_bounds__(256) linear_dz_kernel(const DzArgs a) {
                     }
 #pragma unroll
                     for (int i = 0; i < 8; ++i) acc[i] += v[i];
-                    if (a.dz) store_vec<8>(a.dz + m * a.ldz + n, v);
+                    // a copy of a bf16 dy goes to the products as dy itself would (see AS_IS)
+                    if (a.dz) store_vec<8>(a.dz + m * a.ldz + n, AS_IS ? kept : v);
                 }
             }
         }
@@ -643,15 +650,20 @@ __global__ void __launch_bounds__(256, narrow_blocks<NB>()) linear_narrow_bwd_ke
         __syncthreads();                        // the chunk before has been used
         for (int i = t; i < kNarrowChunk * NB; i += T) {
             const int r = i / NB, n = i % NB;
-            float v = 0.f;
+            float v = 0.f, d = 0.f;
             if (r < rows && n < a.N) {
                 const int64_t at = (base + r) * a.lddy + n;
                 v = a.dy_f32 ? static_cast<const float*>(a.dy)[at] : load_f32(static_cast<const bf16_bits*>(a.dy) + at);
                 if (a.act != TPPO_ACT_NONE) v *= act_slope_of(a.act, load_f32(a.pre + (base + r) * a.ldp + n));
-                if (!(fabsf(v) <= kBf16Max)) { v = 0.f; bad = true; }
+                d = v;
+                if (!(fabsf(v) <= kBf16Max)) {
+                    bad = true;
+                    v = 0.f;
+                    if (a.act != TPPO_ACT_NONE || a.dy_f32) d = 0.f;      // a bf16 dy goes on as it is: see AS_IS
+                }
                 bias += v;
             }
-            dz[i] = v;                          // fp32: nothing here feeds a tensor core
+            dz[i] = d;                          // fp32: nothing here feeds a tensor core
         }
         __syncthreads();
         if (count == 0) continue;

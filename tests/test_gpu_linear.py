@@ -469,3 +469,28 @@ def test_fp32_gradients_of_few_columns(M, K, N, act):
                              (dw, xd.t() @ dz, xd.abs().t() @ dz.abs(), xd.abs().t() @ e_dz)):
         tol = (half_step(BF) + U32) * ref.abs() + 320 * U32 * mag + 1.01 * e
         assert bool(((got.double() - ref).abs() <= tol).all()), ((got.double() - ref).abs() / tol).max().item()
+
+
+@pytest.mark.parametrize("left,right", [(0, 0), (8, 8), (3, 2)])
+@pytest.mark.parametrize("M,K,N", [(40, 64, 64), (70, 2050, 1), (300, 520, 3), (200, 130, 77), (4100, 4000, 2008)])
+def test_one_rule_for_gradients_that_are_not_finite(M, K, N, left, right):
+    """A NaN or an infinity in dy counts as 0 where dz is made (an activation, or fp32), and makes what it enters 0 where
+    a bf16 dy is the operand itself -- whatever the sizes and alignments choose beneath."""
+    from paper_2506_15050_b200 import binding as b
+    g = gen(M + N)
+    x, w, dy, z = whole(g, M, K), whole(g, K, N), whole(g, M, N), whole(g, M, N)
+    rows, cols = torch.tensor([3, M - 1], device=DEV), torch.tensor([N // 2, N - 1], device=DEV)
+    dy[rows[0], cols[0]], dy[rows[1], cols[1]] = float("nan"), -float("inf")
+    d = torch.where(torch.isfinite(dy), dy, 0.0).double()
+    x, w, dy, z = (strided(t, left, right) for t in (x, w, dy, z))
+    ws = workspace(M, K, N, 1)
+    for act, grad, through in ((b.ACT_NONE, dy, True), (b.ACT_NONE, dy.float(), False), (b.ACT_RELU, dy, False)):
+        dx, dw, db = (torch.empty(s, dtype=BF, device=DEV) for s in ((M, K), (K, N), (N,)))
+        status = torch.zeros(1, dtype=torch.int32, device=DEV)
+        b.tppo_linear_bwd(grad, x, w, act, z if act else None, dx, dw, db, status, ws)
+        dz = d * (z.double() > 0) if act else d
+        rx, rw = dz @ w.double().t(), x.double().t() @ dz
+        if through:
+            rx[rows], rw[:, cols] = 0.0, 0.0
+        assert torch.equal(dx, rx.to(BF)) and torch.equal(dw, rw.to(BF)) and torch.equal(db, dz.sum(0).to(BF))
+        assert int(status) == b.DEV_NONFINITE
