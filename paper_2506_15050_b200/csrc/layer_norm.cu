@@ -398,7 +398,10 @@ __global__ void __launch_bounds__(kRingThreads) norm_fwd_ring_kernel(const NormF
         __syncthreads();                          // the sums are there, and the stage has been read
         if (t == 0 && !timed_out && r + a.stages * step < a.M) issue(r + a.stages * step, stage);
         if (++stage == a.stages) { stage = 0; phase ^= 1u; }
-        const float mean = ring_sum(red[0], warps) * inv_n;
+        // one step on the residual (Markstein's correction of a quotient): sum * (1 / N) alone may miss the value of a
+        // row that holds nothing else
+        const float total = ring_sum(red[0], warps), about = total * inv_n;
+        const float mean = fmaf(fmaf(-about, float(a.N), total), inv_n, about);
         s = 0;
 #pragma unroll
         for (int c = 0; c < CH; ++c) {

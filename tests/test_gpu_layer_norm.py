@@ -283,3 +283,18 @@ def test_forward_of_many_rows(M, N, left, right, dtype):
         check_fwd(x, gm, bt, 1e-5, y.t, mean, rstd)
         y.check()
         assert int(status) == 0
+
+
+@pytest.mark.parametrize("dtype,M,N", [(BF, 2100, 5192), (BF, 2100, 2565), (F32, 2100, 9236), (F32, 2100, 4657), (BF, 620, 10384)])
+def test_rows_of_one_value(dtype, M, N):
+    """Eight bits times at most 2^14 columns: every partial sum is exact, so the mean is the value, y = beta, and with
+    eps = 0 the row has no statistics."""
+    from paper_2506_15050_b200 import binding as b
+    c = (torch.arange(M, device=DEV) % 128 + 128).to(dtype) / 128
+    x = c[:, None].expand(M, N).contiguous()
+    beta = torch.randn(N, generator=gen(N), device=DEV)
+    y, mean, rstd, status = torch.empty_like(x), torch.empty(M, device=DEV), torch.empty(M, device=DEV), torch.zeros(1, dtype=torch.int32, device=DEV)
+    b.tppo_layer_norm_fwd(x, None, beta, 1e-5, y, mean, rstd, status)
+    assert torch.equal(mean, c.float()) and torch.equal(y, beta.to(dtype).expand(M, N)) and int(status) == 0
+    b.tppo_layer_norm_fwd(x, None, beta, 0.0, y, mean, rstd, status)
+    assert not y.any() and not mean.any() and not rstd.any() and int(status) == b.DEV_NONFINITE
