@@ -498,8 +498,9 @@ enum {
  *             only to copy an operand whose rows are not 16-byte aligned -- or, where that makes a large
  *             product faster and there is room, not whole 128-byte lines -- and may be given NULL when x
  *             and weight are 16-byte aligned.  The query counts those copies when K or N is not a
- *             multiple of 64, or when n_max is 1: pass that for misaligned views (base or ld) of
- *             matrices whose sizes are multiples of 64.
+ *             multiple of 64 -- for N <= 4, when K is not a multiple of 8 -- or when n_max is 1: pass that for
+ *             misaligned views (base or ld) of matrices of other sizes.  (With N <= 4 such views need no more
+ *             than the plain query says; the backward call is faster with the copies from 2^23 elements on.)
  * Products are bf16, sums and the epilogue fp32, y is rounded once.  An element whose z or y is not
  * finite or leaves the range of the type it is stored in is written 0 and raises TPPO_DEV_NONFINITE.
  * No output may overlap x, weight or another output.

@@ -1089,6 +1089,8 @@ __global__ void __launch_bounds__(1024) norm_sum_kernel(const float* partial, in
 }
 
 // Most blocks, and so partial rows, of a backward pass: eight per SM of short rows, three of long ones.
+constexpr int kNormColParts = 64;              // partial rows of norm_cols_kernel
+constexpr int32_t kNormRingCols = 512 * 32;    // most columns of the kernels that walk over rows: threads times columns of each
 int norm_max_parts(int32_t N) { return N <= 512 ? 8 * kNumSms : N <= 2048 ? 5 * kNumSms : 3 * kNumSms; }
 
 bool rows_aligned(const void* p, int64_t ld, size_t esize) {
@@ -1155,7 +1157,10 @@ int norm_fwd_typed(NormFwdArgs a, cudaStream_t s) {
 
 struct NormWs { float* partial; float* row_flag; size_t bytes; };
 NormWs norm_carve(void* ws, int64_t M, int32_t N) {
-    const size_t a = align_up(size_t(norm_max_parts(N)) * 2 * size_t(N) * 4, kWsAlign);
+    // no more partial rows than rows; rows of more than 16384 columns are summed by norm_cols_kernel
+    int64_t parts = N > kNormRingCols ? kNormColParts : norm_max_parts(N);
+    if (parts > M) parts = M < 1 ? 1 : M;
+    const size_t a = align_up(size_t(parts) * 2 * size_t(N) * 4, kWsAlign);
     const size_t b = align_up(size_t(M) * 4, kWsAlign);
     char* p = static_cast<char*>(ws);
     return {reinterpret_cast<float*>(p), reinterpret_cast<float*>(p + a), a + b};
@@ -1255,7 +1260,7 @@ int norm_bwd_typed(NormBwdArgs a, P* dgamma, P* dbeta, float* row_flag, cudaStre
         if (a.partial) {
             b.dx = nullptr;
             TPPO_CUDA_CHECK(launch_dense(norm_bwd_long_kernel<T, P>, dim3(unsigned(a.M)), dim3(kNormMaxThreads), 0, s, b, row_flag));
-            parts = int(a.M < 64 ? a.M : 64);
+            parts = int(a.M < kNormColParts ? a.M : kNormColParts);
             TPPO_CUDA_CHECK(launch_dense(norm_cols_kernel<T>, dim3(dim3((a.N + 255) / 256, parts)), dim3(256), 0, s, a, row_flag));
         }
         if (a.dx) {

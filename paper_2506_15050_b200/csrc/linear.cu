@@ -290,6 +290,8 @@ struct EpiStore {
 constexpr int kNarrowRows = 4;
 constexpr int kNarrowMaxN = 8;
 constexpr int kNarrowMaxSmem = 96 * 1024;
+int narrow_columns(int32_t N) { return N <= 1 ? 1 : N <= 2 ? 2 : N <= 4 ? 4 : 8; }
+bool narrow_fits(int nb, int32_t K) { return size_t(nb) * ((size_t(K) + 7) / 8 * 8) * 2 <= size_t(kNarrowMaxSmem); }
 
 template <int NB, bool VEC>
 __global__ void __launch_bounds__(256) linear_narrow_kernel(const bf16_bits* x, int64_t ldx, const bf16_bits* w, int64_t ldw,
@@ -799,6 +801,13 @@ NarrowGrid narrow_grid(int64_t M, int32_t K, int nb) {
     return g;
 }
 
+// At least that grid's bytes, for every M and K up to these: y threads K <= 148 threads_per_SM 8 columns each.
+size_t narrow_room(int64_t M, int32_t K, int nb) {
+    const size_t sm_threads = nb == 1 ? 1024 : 512, y_most = kNumSms * sm_threads / 32, wide = kNumSms * sm_threads * 8;
+    const size_t by_grid = (wide > size_t(K) ? wide : size_t(K)) + y_most, by_rows = (size_t(M) / (4 * nb) + 1) * (size_t(K) + 1);
+    return (by_grid < by_rows ? by_grid : by_rows) * nb * 4;
+}
+
 template <int NB>
 int linear_narrow_bwd(const NarrowBwdArgs& a, const NarrowGrid& g, bool vec, bf16_bits* dweight, int64_t lddw, void* dbias,
                       bool bias_f32, cudaStream_t s) {
@@ -866,6 +875,9 @@ bool act_known(int32_t a) { return a >= TPPO_ACT_NONE && a <= TPPO_ACT_SILU; }
 size_t linear_workspace_bytes(int64_t M, int32_t K, int32_t N, bool copies) {
     if (K < 1 || N < 1 || M > kDenseMaxSize || K > kDenseMaxSize || N > kDenseMaxSize) return 0;
     const LinearWs w = linear_carve(nullptr, M, K, N);
+    // a value head: no products, unless rows at odd places or a weight beyond shared memory ask for them
+    const int nb = narrow_columns(N);
+    if (!copies && N <= kNarrowBwdMaxN && K % 8 == 0 && narrow_fits(nb, K)) return align_up(narrow_room(M, K, nb), kWsAlign);
     return copies || K % 64 || N % 64 ? w.bytes : w.plain;
 }
 
@@ -888,8 +900,8 @@ TPPO_API int tppo_linear_fwd(const void* x, int64_t ldx, const void* weight, int
     if (!x || !weight || !y || !aligned(x, 2) || !aligned(weight, 2) || !aligned(bias, bs) || !aligned(residual, 2) ||
         !aligned(y, ys) || !aligned(preact, 2) || !aligned(status, 4))
         return TPPO_ERR_INVALID_ARG;
-    const int nb = N <= 1 ? 1 : N <= 2 ? 2 : N <= 4 ? 4 : 8;
-    const bool narrow = N <= kNarrowMaxN && size_t(nb) * ((K + 7) / 8 * 8) * 2 <= size_t(kNarrowMaxSmem);
+    const int nb = narrow_columns(N);
+    const bool narrow = N <= kNarrowMaxN && narrow_fits(nb, K);
     bool copy_x = !narrow && !tma_rows(x, ldx), copy_w = !narrow && !tma_rows(weight, ldw);
     const LinearWs w = linear_carve(workspace, M, K, N);
     const bool room = workspace && aligned(workspace, kWsAlign) && workspace_bytes >= w.bytes;
@@ -948,11 +960,16 @@ TPPO_API int tppo_linear_bwd(const void* dy, int32_t dy_dtype, int64_t lddy, con
     if (!dx && !dweight && !dbias) return TPPO_OK;
     const LinearWs w = linear_carve(workspace, M, K, N);
     const size_t have = workspace && aligned(workspace, kWsAlign) ? workspace_bytes : 0;
+    const bool products = dx || dweight;
+    bool copy_x = dweight && !tma_rows(x, ldx), copy_w = dx && !tma_rows(weight, ldw);
+    bool make_dz = products && (activation != TPPO_ACT_NONE || dy_dtype == TPPO_F32 || !tma_rows(dy, lddy));
+    const size_t need = copy_x || copy_w ? w.bytes : make_dz || dbias ? w.plain : 0;
     const bool narrow_vec = K % 8 == 0 && (!dweight || tma_rows(x, ldx)) && (!dx || tma_rows(dx, lddx));
     // 16384 x 5120, us against the tensor-core products: one column 61 / 129, four 92 / 130, eight 242 / 133; rows
     // that are read by element lose from some 2^23 of them on (16384 x 5121 x 1 432 / 307, 4000 x 1001 x 1 15 / 33)
-    if (N <= kNarrowBwdMaxN && (narrow_vec || M * K <= (int64_t(1) << 23))) {
-        const int nb = N <= 1 ? 1 : N <= 2 ? 2 : 4;
+    // -- and are taken all the same where the products' operands have no room
+    if (N <= kNarrowBwdMaxN && (narrow_vec || M * K <= (int64_t(1) << 23) || need > have)) {
+        const int nb = narrow_columns(N);
         const NarrowGrid g = narrow_grid(M, K, nb);
         const bool sums = dweight || dbias;
         if (!sums || have >= g.bytes) {
@@ -966,10 +983,6 @@ TPPO_API int tppo_linear_bwd(const void* dy, int32_t dy_dtype, int64_t lddy, con
             return linear_narrow_bwd<4>(a, g, narrow_vec, dw, lddw, dbias, f, s);
         }
     }
-    const bool products = dx || dweight;
-    bool copy_x = dweight && !tma_rows(x, ldx), copy_w = dx && !tma_rows(weight, ldw);
-    bool make_dz = products && (activation != TPPO_ACT_NONE || dy_dtype == TPPO_F32 || !tma_rows(dy, lddy));
-    const size_t need = copy_x || copy_w ? w.bytes : make_dz || dbias ? w.plain : 0;
     if (need > have) return TPPO_ERR_WORKSPACE;
     const double flops = 2.0 * double(M) * K * N;
     if (have >= w.bytes) {

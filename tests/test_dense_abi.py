@@ -138,3 +138,21 @@ def test_linear_backward_without_an_operand(lib, p):
         assert lib.tppo_linear_bwd(*[dict(good, **change)[k] for k in args]) == 0
     refused(lib.tppo_linear_bwd, args, dict(good, M=4), [
         (dict(x=a, ldx=15), INVALID), (dict(w=a, ldw=23), INVALID), (dict(dx=a, lddx=16), INVALID), (dict(dw=a, lddw=24), INVALID)])
+
+
+def test_workspaces_follow_the_path(lib):
+    """Rows beyond the kernels that walk over them take 64 partial rows, no call more partial rows than rows, and a
+    value head only its partial sums; none needs less for more rows or columns of the same kind."""
+    w = lib.tppo_workspace_bytes
+    assert w(LAYER_NORM, 16384, 0, 0, 70001) <= 64 * 2 * 4 * 70001 + 4 * 16384 + 512
+    assert w(LAYER_NORM, 1, 0, 0, 5120) <= 2 * 4 * 5120 + 512
+    assert w(LAYER_NORM, 16384, 0, 0, 16384) >= 148 * 2 * 4 * 16384
+    assert 4 << 20 <= w(LINEAR, 16384, 5120, 0, 1) <= 6 << 20
+    assert w(LINEAR, 1, 5120, 0, 4) <= 1 << 18
+    assert w(LINEAR, 16384, 5120, 1, 1) >= 2 * 16384 * 5120                # misaligned views on request: operand copies
+    assert w(LINEAR, 16384, 5121, 0, 1) >= 2 * 16384 * 5121 and w(LINEAR, 16384, 5120, 0, 5) >= 2 * 16384 * 5120
+    for N in (1, 2, 3, 4):
+        sizes = [w(LINEAR, 16384, K, 0, N) for K in (8, 64, 2048, 2056, 5120, 8192)]
+        assert sizes == sorted(sizes)
+        sizes = [w(LINEAR, M, 2048, 0, N) for M in (1, 4, 100, 1000, 10000, 100000)]
+        assert sizes == sorted(sizes)

@@ -298,3 +298,17 @@ def test_rows_of_one_value(dtype, M, N):
     assert torch.equal(mean, c.float()) and torch.equal(y, beta.to(dtype).expand(M, N)) and int(status) == 0
     b.tppo_layer_norm_fwd(x, None, beta, 0.0, y, mean, rstd, status)
     assert not y.any() and not mean.any() and not rstd.any() and int(status) == b.DEV_NONFINITE
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("M,N", [(1, 64), (3, 520), (147, 5120), (150, 640), (600, 16384), (10, 16385), (200, 20001)])
+def test_gradients_in_a_workspace_of_the_size_asked_for(M, N, dtype):
+    from paper_2506_15050_b200 import binding as b
+    x, dy, gamma, _ = make(M, N, dtype, M + N, offset=0.0)
+    _, m, r, _ = norm64(x, None, None, 1e-5)
+    n = b.tppo_workspace_bytes(b.OP_LAYER_NORM, M, 0, 0, N)
+    room = torch.full((n + 4096,), 0xff, dtype=torch.uint8, device=DEV)
+    dx, dg, db = torch.empty_like(x), torch.empty(N, device=DEV), torch.empty(N, device=DEV)
+    b.tppo_layer_norm_bwd(dy, x, gamma, m.float(), r.float(), dx, dg, db, None, room[:n])
+    check_bwd(dy, x, gamma, m.float(), r.float(), dx, dg, db)
+    assert bool((room[n:] == 0xff).all())

@@ -494,3 +494,24 @@ def test_one_rule_for_gradients_that_are_not_finite(M, K, N, left, right):
             rx[rows], rw[:, cols] = 0.0, 0.0
         assert torch.equal(dx, rx.to(BF)) and torch.equal(dw, rw.to(BF)) and torch.equal(db, dz.sum(0).to(BF))
         assert int(status) == b.DEV_NONFINITE
+
+
+@pytest.mark.parametrize("left,right", [(0, 0), (8, 8), (3, 2)])
+@pytest.mark.parametrize("M,K,N", [(2100, 5120, 1), (9000, 2048, 1), (1, 64, 1), (5000, 4104, 4), (700, 2056, 2), (20000, 512, 3)])
+def test_value_head_in_its_own_workspace(M, K, N, left, right):
+    """The bytes that the query asks for and no more, at any alignment; what lies behind them stays as it is."""
+    from paper_2506_15050_b200 import binding as b
+    g = gen(M + K + N)
+    x, w, dy = whole(g, M, K, top=2), whole(g, K, N), whole(g, M, N, top=2)
+    rx, rw, rb = (dy.double() @ w.double().t()).to(BF), (x.double().t() @ dy.double()).to(BF), dy.double().sum(0)
+    y = x.double() @ w.double()
+    x, w, dy = (strided(t, left, right) for t in (x, w, dy))
+    n = b.tppo_workspace_bytes(b.OP_LINEAR, M, K, 0, N)
+    room = torch.full((n + 1024,), 0xff, dtype=torch.uint8, device=DEV)
+    out, dx, dw, db = torch.empty((M, N), device=DEV), Guarded(M, K, BF, left, right), Guarded(K, N, BF, right, left), torch.empty(N, device=DEV)
+    b.tppo_linear_fwd(x, w, None, b.ACT_NONE, None, out, None, None, room[:n])
+    b.tppo_linear_bwd(dy, x, w, b.ACT_NONE, None, dx.t, dw.t, db, None, room[:n])
+    assert torch.equal(out.double(), y) and torch.equal(dx.t, rx) and torch.equal(dw.t, rw) and torch.equal(db.double(), rb)
+    dx.check()
+    dw.check()
+    assert bool((room[n:] == 0xff).all())
