@@ -312,3 +312,35 @@ def test_gradients_in_a_workspace_of_the_size_asked_for(M, N, dtype):
     b.tppo_layer_norm_bwd(dy, x, gamma, m.float(), r.float(), dx, dg, db, None, room[:n])
     check_bwd(dy, x, gamma, m.float(), r.float(), dx, dg, db)
     assert bool((room[n:] == 0xff).all())
+
+
+@pytest.mark.parametrize("M,N,ld,left", [(530_001, 4104, 4104, 0), (530_001, 4101, 4104, 3), (262_200, 8200, 8200, 0)])
+def test_more_than_2_to_31_elements(M, N, ld, left):
+    """Whole matrices past 32 bits through the kernels that walk over rows: the first rows, those around 2^31 elements
+    and the last ones, and the gradients' sums over all rows (M / 148 additions in a block at most, then fp64)."""
+    from paper_2506_15050_b200 import binding as b
+    assert M * ld > 1 << 31
+    g = gen(N)
+    x, dy = (torch.empty((M, ld), dtype=BF, device=DEV)[:, left:left + N] for _ in range(2))
+    for m in range(0, M, 60_000):
+        for t in (x, dy):
+            t[m:m + 60_000] = torch.randn((min(60_000, M - m), N), generator=g, device=DEV).to(BF)
+    gamma = 1 + 0.3 * torch.randn(N, generator=g, device=DEV)
+    mean, rstd, y, dx = torch.empty(M, device=DEV), torch.empty(M, device=DEV), torch.empty_like(x), torch.empty_like(x)
+    dg, db, status = torch.empty(N, device=DEV), torch.empty(N, device=DEV), torch.zeros(1, dtype=torch.int32, device=DEV)
+    b.tppo_layer_norm_fwd(x, gamma, None, 1e-5, y, mean, rstd, status)
+    b.tppo_layer_norm_bwd(dy, x, gamma, mean, rstd, dx, dg, db, status, b.workspace(b.OP_LAYER_NORM, M, 0, 0, N, DEV))
+    edge = (1 << 31) // ld
+    for s in (slice(0, 300), slice(edge - 150, edge + 150), slice(M - 300, M)):
+        check_fwd(x[s], gamma, None, 1e-5, y[s], mean[s], rstd[s])
+        check_bwd(dy[s], x[s], gamma, mean[s], rstd[s], dx[s], None, None)
+    sums = [torch.zeros(N, dtype=torch.float64, device=DEV) for _ in range(4)]
+    for m in range(0, M, 60_000):
+        s = slice(m, m + 60_000)
+        d, h = dy[s].double(), (x[s].double() - mean[s, None].double()) * rstd[s, None].double()
+        for k, t in enumerate((d * h, d)):
+            sums[k] += t.sum(0)
+            sums[k + 2] += t.abs().sum(0)
+    for got, ref, mag in zip((dg, db), sums[:2], sums[2:]):
+        assert bool(((got.double() - ref).abs() <= (M / 148 + 44) * U32 * mag + ref.abs() * half_step(F32)).all())
+    assert int(status) == 0

@@ -515,3 +515,28 @@ def test_value_head_in_its_own_workspace(M, K, N, left, right):
     dx.check()
     dw.check()
     assert bool((room[n:] == 0xff).all())
+
+
+def test_weight_gradient_over_rows_beyond_32_bits():
+    """dweight contracts 530001 rows of a dz of more than 2^31 elements; sums of whole numbers below 2^24."""
+    from paper_2506_15050_b200 import binding as b
+    M, K, N, g = 530_001, 64, 4096, gen(12)
+    x, w, z = whole(g, M, K), whole(g, K, N), torch.empty((M, N), dtype=BF, device=DEV)
+    for m in range(0, M, 50_000):
+        z[m:m + 50_000] = whole(g, min(50_000, M - m), N)
+    dy = torch.ones((M, N), dtype=BF, device=DEV)
+    dw, db = torch.empty_like(w), torch.empty(N, device=DEV)
+    b.tppo_linear_bwd(dy, x, w, b.ACT_RELU, z, None, dw, db, None, workspace(M, K, N))
+    ref, cols = torch.zeros((K, N), dtype=F64, device=DEV), torch.zeros(N, dtype=F64, device=DEV)
+    for m in range(0, M, 50_000):
+        on = (z[m:m + 50_000] > 0).double()
+        ref += x[m:m + 50_000].double().t() @ on
+        cols += on.sum(0)
+    assert torch.equal(dw, ref.to(BF)) and torch.equal(db.double(), cols)
+
+
+@pytest.mark.parametrize("M,K,N,act", [(4200, 1000, 2056, 2), (8200, 1030, 1030, 4)])
+def test_long_streams_one_behind_the_other(M, K, N, act):
+    """From 2^23 elements of dz on, what follows a stream starts at its end."""
+    assert M * N > 1 << 23
+    test_calls_one_behind_the_other(M, K, N, act)

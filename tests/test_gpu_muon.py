@@ -199,3 +199,40 @@ def test_norms_at_the_ends_of_the_range(R, C, power):
     y = (x.double() * 2.0 ** power).float()
     assert torch.equal(y.double() * 2.0 ** -power, x.double())
     assert near(call(y, eps=0.0), ref)
+
+
+@pytest.mark.parametrize("R,C", [(256, 1024), (1030, 519), (700, 100), (2500, 2300), (2300, 5200), (5000, 2310)])
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_documented_precision(R, C, dtype):
+    """Five steps on random matrices: X within about 1e-3 of its norm (1.5e-3 here), then one rounding whose error is
+    at most half a step, evenly spread: 2^-8 / sqrt(3) of the norm.  Together 2.71e-3."""
+    grad = torch.randn((R, C), generator=gen(R * C), device=DEV).to(dtype)
+    ref = reference(grad, 5, 1e-7)
+    assert (call(grad).double() - ref).norm() <= math.hypot(1.5e-3, half_step(BF) / math.sqrt(3)) * ref.norm()
+
+
+@pytest.mark.parametrize("tall", [True, False])
+def test_more_than_2_to_31_elements(tall):
+    """A long side of 2^22 and a bit.  X after each step is U times a polynomial of U^T U, so the reference needs
+    the small side's products only; some columns (rows) of it are compared, at the bound of `near` each."""
+    n, m, g = (1 << 22) + 77, 520, gen(31)
+    assert n * m > 1 << 31
+    u = torch.empty((n, m) if tall else (m, n), dtype=BF, device=DEV)
+    gram, step = torch.zeros((m, m), dtype=F64, device=DEV), 1 << 18
+    mix = torch.randn((m, m), generator=g, device=DEV) * m ** -0.5 + torch.eye(m, device=DEV)
+    part = lambda k: u[k:k + step] if tall else u[:, k:k + step].t()
+    for k in range(0, n, step):
+        part(k).copy_(torch.randn((min(step, n - k), m), generator=g, device=DEV) @ mix)
+        gram += part(k).double().t() @ part(k).double()
+    norm = gram.trace().sqrt()
+    p = torch.eye(m, dtype=F64, device=DEV) / norm          # X = U p, A = p^T gram p
+    for _ in range(5):
+        a = p.t() @ gram @ p
+        p = p @ (NS[0] * torch.eye(m, dtype=F64, device=DEV) + NS[1] * a + NS[2] * a @ a)
+    up = torch.empty_like(u)
+    call(u, eps=0.0, update=up)
+    edge = (1 << 31) // m if tall else 0
+    for k in (0, edge, n - 500):
+        got = up[k:k + 500] if tall else up[:, k:k + 500].t()
+        ref = (u[k:k + 500] if tall else u[:, k:k + 500].t()).double() @ p
+        assert near(got, ref), float((got.double() - ref).norm() / ref.norm())
