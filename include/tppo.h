@@ -447,7 +447,7 @@ int tppo_advance_batch(const int32_t *seq_begin, const int32_t *prompt_len,
  *   gamma, beta  [N] of `param_dtype` (either type), each may be NULL (1 and 0)
  *   mean, rstd   [M] fp32 out, each may be NULL: what tppo_layer_norm_bwd takes
  *   eps >= 0
- * A row that holds a NaN or an infinity, or whose variance leaves the range of fp32 (with eps = 0 that
+ * A row that holds a NaN or an infinity, or whose sum or variance leaves the range of fp32 (with eps = 0 that
  * includes a variance of 0), has no statistics: its y, mean and rstd are written 0 and
  * TPPO_DEV_NONFINITE is raised.  gamma and beta are taken as they are: one that is not finite, or carries a
  * y past the range of its type, leaves such elements in y.
@@ -467,7 +467,8 @@ int tppo_layer_norm_fwd(const void *x, int32_t dtype, int64_t M, int32_t N, int6
  *   workspace  tppo_workspace_bytes(TPPO_OP_LAYER_NORM, M, 0, 0, N) bytes; may be NULL when both
  *              dgamma and dbeta are
  * A row without statistics (rstd = 0) contributes nothing and gets dx = 0; so does a row whose dy or x
- * is not finite, which raises TPPO_DEV_NONFINITE.  Elements of dx and sums over rows that leave the range
+ * is not finite or whose sums of a and a h are not (a gamma that is not finite makes them so in every row), which
+ * raises TPPO_DEV_NONFINITE.  Elements of dx and sums over rows that leave the range
  * of their type become infinities.  M = 0 writes dgamma = dbeta = 0.
  */
 int tppo_layer_norm_bwd(const void *dy, const void *x, int32_t dtype, int64_t M, int32_t N,
@@ -542,7 +543,8 @@ int tppo_linear_bwd(const void *dy, int32_t dy_dtype, int64_t lddy, const void *
  *     momentum = mu * momentum + grad,   U = nesterov ? grad + mu * momentum : momentum
  *     X = U / (|U|_F + eps);  `steps` times:  A = X X^T,  B = b A + c A^2,  X = a X + B X
  *     update = scale * X,                (a, b, c) = (3.4445, -4.7750, 2.0315)
- * which drives every singular value of X to between 0.68 and 1.21 and leaves its singular vectors.
+ * which multiplies small singular values of X by up to 3.44 per step, keeps those that have come near 1 between
+ * 0.68 and 1.21, and leaves the singular vectors.  Five steps bring up what is above some 1.5e-3 of the norm.
  * (The products are taken from the smaller side; the result is the same.)
  *   grad      [R, C] of `grad_dtype`; not changed, unless `update` is grad itself
  *   momentum  [R, C] fp32 in/out, or NULL: U = grad (mu and nesterov are then not used)

@@ -5,15 +5,16 @@
 //     dgamma = sum_rows dy * h,   dbeta = sum_rows dy
 // All arithmetic is fp32; the inputs are read once and the outputs rounded once.
 //
-// Both passes are bound by HBM (2 resp. 3 elements moved per element) until issue slots bind them: a
-// bf16 element costs some 12 instructions forward and 25 backward.  Long rows are brought in by bulk (TMA)
-// copies through a ring of shared memory, which keeps 100-200 KB per SM in flight while blocks go from
+// Both passes have 2 resp. 3 elements to move per element, and fp32 rows are bound by that.  Of bf16 rows an
+// element costs some 12 instructions forward and 25 backward, and what the SM has resident waits together:
+// backward at 5120 columns one block of 640 threads, at one barrier per trip (61 % of the issue slots used,
+// fixed latency first among the stalls).  Long rows are brought in by bulk (TMA) copies through a ring of shared memory, which keeps 100-200 KB per SM in flight while blocks go from
 // row to row; short rows are loaded into the registers of one or a few warps.  The sums of gamma and
 // beta stay in the registers of a block's threads for its whole walk over the rows; each block writes one
 // partial row of them to the workspace and a second kernel adds those in a fixed order, so the gradients
 // do not depend on scheduling.  Rows too long for either way take kernels that read the row again from L2.
-//   [16384, 5120] bf16: forward 63 us (5.3 TB/s, 0.81 of the measured copy rate), backward 112 us (4.5 TB/s)
-//   [16384, 5120] fp32: forward 107 us (6.3 TB/s), backward 165 us (6.1 TB/s)
+//   [16384, 5120] bf16: forward 62 us (5.4 TB/s, 0.82 of the measured copy rate), backward 109 us (4.6 TB/s)
+//   [16384, 5120] fp32: forward 107 us (6.3 TB/s), backward 168 us (6.0 TB/s)
 #include <type_traits>
 
 #include "dense_common.cuh"
@@ -141,8 +142,8 @@ __global__ void __launch_bounds__(kNormMaxThreads) norm_fwd_kernel(const NormFwd
 }
 
 // ---- rows fed by bulk copies --------------------------------------------------------------------
-// The arithmetic of these kernels runs on pairs of fp32 values in 64-bit registers: the row sweeps are
-// issue bound otherwise.
+// The arithmetic of these kernels runs on pairs of fp32 values in 64-bit registers: fewer instructions, though
+// plain floats take the same time within 3 %.
 typedef uint64_t f32x2;
 __device__ __forceinline__ f32x2 twice(float v) { return ptx::pack_f32x2(v, v); }
 __device__ __forceinline__ float pair_sum(f32x2 v) {
@@ -840,14 +841,14 @@ __global__ void __launch_bounds__(THREADS) norm_bwd_rows_kernel(const NormBwdArg
     }
 }
 
-// Aligned rows: a block takes two rows at a time out of a ring of shared memory that bulk copies fill
+// Rows that one phase does not hold in registers -- aligned ones of more than 8192 columns -- or that are not
+// 16-byte aligned: a block takes two rows at a time out of a ring of shared memory that bulk copies fill
 // `stages` rows ahead, in two phases:
 //   sums    half of the block's warps on each row, lanes along it: sum a and sum a (x - mean)
 //   finish  every thread its CH pieces of columns of both rows: column sums (in registers for the whole
 //           walk) and dx
-// Both phases read the row from shared memory.  The obvious form -- a thread keeps its columns of the
-// row from one phase to the next -- pays for two sums over the block per row at every thread: 27 issue
-// slots per element, where the two phases take some 15; the kernel is issue bound at the former.
+// Both phases read the row from shared memory.  Where the registers have the room, one phase with one barrier
+// for several rows is faster (the table in norm_bwd_typed: 47 us against 106 for 16384 x 2048).
 template <class Q, class P, int CH>
 __global__ void __launch_bounds__(CH * Q::kVec > 16 ? 512 : 640) norm_bwd_ring_kernel(const NormBwdArgs a) {
     typedef typename Q::Elem T;
@@ -1183,9 +1184,9 @@ int norm_bwd_typed(NormBwdArgs a, P* dgamma, P* dbeta, float* row_flag, cudaStre
     const int64_t row_threads = deep ? threads_of(16, 32) : eight;
     const int cols = threads_of(16, 64) <= 640 ? 16 : 32;
     // Which kernel, as measured (us; registers / one phase / two phases):
-    //   bf16, 16384 rows of 256: 15 / 16 / -, 512: 21 / 19 / 24, 2048: 90 / 47 / 106, 4096: 150 / 83 / 114, 5120: - / 112
+    //   bf16, 16384 rows of 256: 15 / 16 / -, 512: 21 / 19 / 24, 2048: 90 / 47 / 106, 4096: 150 / 83 / 114, 5120: - / 109
     //   / 128 (187 with 16 columns per thread); 8192 rows of 6144: - / 90 / 116 (two rows per trip 105: it spills),
-    //   8192: 153 / 99 / 128; 4096 rows of 384: 12 / 11 / -, 256: 11 / 11 / -;
+    //   8192: 153 / 100 / 128; 4096 rows of 384: 12 / 11 / -, 256: 11 / 11 / -;
     //   fp32, 16384 rows of 256: 15 / 21 / -, 384: 22 / 24 / -, 512: 44 / 27 / -; 8192 rows of 2048: 46 / 34 / 51, 5120:
     //   150 / 83 / 119, 6144: - / 99 / 124, 8192: 177 / 146 / 158;
     //   unaligned bf16, 8192 rows of 263: 43 / - / 33, 1283: 71 / - / 45, 5121: 499 / - / 148 (1000 rows of 1283: 16 / - / 17);

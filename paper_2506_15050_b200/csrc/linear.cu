@@ -16,8 +16,10 @@
 // cluster -- see dense_gemm.cuh.  TMA wants 16-byte aligned rows: operands whose row length or base
 // does not allow that are first copied into the workspace with a padded row stride.
 //   16384 x 5120 x 5120: the bare product 600 us (1430 TFLOP/s, the sustained cuBLAS rate: power bound), with
-//   bias, gelu_tanh, residual and a kept z 770-810 us; backward 1280-1550 us by temperature, of which dz 109.
-//   1 x 5120 x 5120: 12.9 us (4.1 TB/s with the launch's start and end).
+//   bias, gelu_tanh, residual and a kept z 750-810 us; backward 1490-1550 us, of which dz 109 (one call behind the
+//   other, SM clock at the power cap).
+//   1 x 5120 x 5120: 12.8 us a call, replayed 12.2 with weights that come from HBM (4.3 TB/s with the launch's start
+//   and end) and 8.7 with one that stays in L2.
 #include "dense_gemm.cuh"
 
 namespace tppo {

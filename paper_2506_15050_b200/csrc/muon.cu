@@ -26,8 +26,8 @@
 // mirrors them: m^2 n + m^3 + 2 m^2 n flop per step for an m x n matrix, m <= n, instead of
 // 4 m^2 n + 2 m^3.  Large matrices are tensor bound, under the power cap; small ones are a chain of
 // three launches per step and two before, each the programmatic dependent of the one before.
-//   five steps: 5120 x 5120 2500-2900 us by temperature (920-1070 TFLOP/s of the work above),
-//   4096 x 4096 1280, 2048 x 2048 327, 256 x 1024 76 (seventeen launches).
+//   five steps: 5120 x 5120 2760-2980 us (900-970 TFLOP/s of the work above; SM clock at the power cap),
+//   4096 x 4096 1280, 2048 x 2048 327, 256 x 1024 78 (seventeen launches).
 #include <cuda_fp16.h>
 
 #include "dense_gemm.cuh"
