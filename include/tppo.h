@@ -524,11 +524,11 @@ int tppo_linear_fwd(const void *x, int64_t ldx, const void *weight, int64_t ldw,
  *   workspace as for tppo_linear_fwd: for dz, the partial sums of dbias and operand copies; may be
  *   NULL when none is needed (TPPO_ACT_NONE, aligned bf16 operands, no dbias)
  * dz is rounded to bf16 before the two products where these run on the tensor cores -- always for N > 4, and for
- * fewer columns of more than 2^23 elements of x whose rows are not 16-byte aligned -- and kept in fp32 elsewhere
- * (dbias sums the unrounded values); an element of dz or of an output that is not finite or leaves the range of
- * bf16 counts or is written as 0 and raises TPPO_DEV_NONFINITE.  One exception: with TPPO_ACT_NONE a bf16 dy is the
- * products' operand as it is, so its elements that are not finite make every element of dx and dweight that they
- * enter 0 (dbias leaves them out).  M = 0 writes dweight = dbias = 0.
+ * fewer columns of more than 2^23 elements of x where rows of x or dx are not 16-byte aligned -- and kept in fp32
+ * elsewhere (dbias sums the unrounded values).  An element of dz or of an output that is not finite or leaves the
+ * range of bf16 counts or is written as 0 and raises TPPO_DEV_NONFINITE.  One exception: with TPPO_ACT_NONE a bf16
+ * dy is the products' operand as it is, so its elements that are not finite make every element of dx and dweight
+ * that they enter 0 (dbias leaves them out).  M = 0 writes dweight = dbias = 0.
  */
 int tppo_linear_bwd(const void *dy, int32_t dy_dtype, int64_t lddy, const void *x, int64_t ldx,
                     const void *weight, int64_t ldw, int64_t M, int32_t K, int32_t N,

@@ -8,11 +8,12 @@
 // Both passes have 2 resp. 3 elements to move per element, and fp32 rows are bound by that.  Of bf16 rows an
 // element costs some 12 instructions forward and 25 backward, and what the SM has resident waits together:
 // backward at 5120 columns one block of 640 threads, at one barrier per trip (61 % of the issue slots used,
-// fixed latency first among the stalls).  Long rows are brought in by bulk (TMA) copies through a ring of shared memory, which keeps 100-200 KB per SM in flight while blocks go from
-// row to row; short rows are loaded into the registers of one or a few warps.  The sums of gamma and
-// beta stay in the registers of a block's threads for its whole walk over the rows; each block writes one
-// partial row of them to the workspace and a second kernel adds those in a fixed order, so the gradients
-// do not depend on scheduling.  Rows too long for either way take kernels that read the row again from L2.
+// fixed latency first among the stalls).  Long rows are brought in by bulk (TMA) copies through a ring of
+// shared memory, which keeps 100-200 KB per SM in flight while blocks go from row to row; short rows are
+// loaded into the registers of one or a few warps.  The sums of gamma and beta stay in the registers of a
+// block's threads for its whole walk over the rows; each block writes one partial row of them to the
+// workspace and a second kernel adds those in a fixed order, so the gradients do not depend on scheduling.
+// Rows too long for either way take kernels that read the row again from L2.
 //   [16384, 5120] bf16: forward 62 us (5.4 TB/s, 0.82 of the measured copy rate), backward 109 us (4.6 TB/s)
 //   [16384, 5120] fp32: forward 107 us (6.3 TB/s), backward 168 us (6.0 TB/s)
 #include <type_traits>
@@ -1158,10 +1159,16 @@ int norm_fwd_typed(NormFwdArgs a, cudaStream_t s) {
 
 struct NormWs { float* partial; float* row_flag; size_t bytes; };
 NormWs norm_carve(void* ws, int64_t M, int32_t N) {
-    // no more partial rows than rows; rows of more than 16384 columns are summed by norm_cols_kernel
-    int64_t parts = N > kNormRingCols ? kNormColParts : norm_max_parts(N);
-    if (parts > M) parts = M < 1 ? 1 : M;
-    const size_t a = align_up(size_t(parts) * 2 * size_t(N) * 4, kWsAlign);
+    // no more partial rows than rows; rows of more than 16384 columns are summed by norm_cols_kernel.  Fewer columns
+    // may take more partial rows: the room is that of every N up to this one.
+    size_t most = 0;
+    for (int32_t n : {512, 2048, kNormRingCols, N}) {
+        if (n > N) n = N;
+        int64_t parts = n > kNormRingCols ? kNormColParts : norm_max_parts(n);
+        if (parts > M) parts = M < 1 ? 1 : M;
+        if (most < size_t(parts) * n) most = size_t(parts) * n;
+    }
+    const size_t a = align_up(most * 2 * 4, kWsAlign);
     const size_t b = align_up(size_t(M) * 4, kWsAlign);
     char* p = static_cast<char*>(ws);
     return {reinterpret_cast<float*>(p), reinterpret_cast<float*>(p + a), a + b};

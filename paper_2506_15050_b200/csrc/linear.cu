@@ -7,8 +7,8 @@
 // dz is the one intermediate that is rounded: both gradients contract it on the tensor cores, so it
 // is formed once, in bf16 like the operand it meets, by a kernel that also sums dbias from the
 // unrounded values.  (The error of dx and dweight against 64 bits goes from 1.7e-3, their own rounding, to
-// 2.3e-3; carrying dz in two bf16 parts would double the products.  The narrow backward kernel keeps fp32.)  (Without an activation and with an aligned bf16 dy that kernel writes nothing
-// and dy itself is the operand.)
+// 2.3e-3; carrying dz in two bf16 parts would double the products.  The narrow backward kernel keeps fp32.
+// Without an activation and with an aligned bf16 dy that kernel writes nothing and dy itself is the operand.)
 //
 // Large outputs are tensor bound and take the persistent kernel; a handful of columns is no work for tensor
 // cores and takes the narrow kernels, both ways; few rows, or few columns, are bound
@@ -564,7 +564,7 @@ __global__ void __launch_bounds__(512) linear_dbias_kernel(const float* partial,
         for (int p0 = strand; p0 < parts; p0 += 8 * 16) {        // eight loads in flight
             float v[8];
 #pragma unroll
-            for (int k = 0; k < 8; ++k) v[k] = p0 + 16 * k < parts ? __ldcg(partial + int64_t(p0 + 16 * k) * N + c) : 0.f;   // at L2: see kBeside
+            for (int k = 0; k < 8; ++k) v[k] = p0 + 16 * k < parts ? __ldcg(partial + int64_t(p0 + 16 * k) * N + c) : 0.f;   // see kBeside
 #pragma unroll
             for (int k = 0; k < 8; ++k) t += double(v[k]);
         }

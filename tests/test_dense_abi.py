@@ -142,9 +142,10 @@ def test_linear_backward_without_an_operand(lib, p):
 
 def test_workspaces_follow_the_path(lib):
     """Rows beyond the kernels that walk over them take 64 partial rows, no call more partial rows than rows, and a
-    value head only its partial sums; none needs less for more rows or columns of the same kind."""
+    value head only its partial sums; a workspace of the largest sizes serves the smaller ones of the same kind."""
     w = lib.tppo_workspace_bytes
-    assert w(LAYER_NORM, 16384, 0, 0, 70001) <= 64 * 2 * 4 * 70001 + 4 * 16384 + 512
+    assert w(LAYER_NORM, 16384, 0, 0, 70001) <= 3 * 148 * 2 * 4 * 16384 + 4 * 16384 + 512      # what 16384 columns take
+    assert w(LAYER_NORM, 64, 0, 0, 70001) <= 64 * 2 * 4 * 70001 + 4 * 64 + 512
     assert w(LAYER_NORM, 1, 0, 0, 5120) <= 2 * 4 * 5120 + 512
     assert w(LAYER_NORM, 16384, 0, 0, 16384) >= 148 * 2 * 4 * 16384
     assert 4 << 20 <= w(LINEAR, 16384, 5120, 0, 1) <= 6 << 20
@@ -155,4 +156,7 @@ def test_workspaces_follow_the_path(lib):
         sizes = [w(LINEAR, 16384, K, 0, N) for K in (8, 64, 2048, 2056, 5120, 8192)]
         assert sizes == sorted(sizes)
         sizes = [w(LINEAR, M, 2048, 0, N) for M in (1, 4, 100, 1000, 10000, 100000)]
+        assert sizes == sorted(sizes)
+    for M in (1, 100, 600, 16384):
+        sizes = [w(LAYER_NORM, M, 0, 0, N) for N in (1, 511, 512, 513, 2048, 2049, 16384, 16385, 70001, 1 << 20)]
         assert sizes == sorted(sizes)
