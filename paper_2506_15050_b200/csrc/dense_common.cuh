@@ -78,6 +78,8 @@ __device__ __forceinline__ float top_of(const bf16_bits*) { return kBf16Max; }
 __device__ __forceinline__ bool is_finite(float v) { return fabsf(v) <= kFltMax; }
 
 inline bool is_finite_host(float v) { return v - v == 0.f; }
+// Whether every row of a matrix starts on a 16-byte boundary.
+inline bool rows_aligned(const void* p, int64_t ld, size_t esize) { return aligned(p, 16) && (ld * int64_t(esize)) % 16 == 0; }
 
 // Rows and columns beyond this would take tile and column arithmetic past 32 bits.
 constexpr int64_t kDenseMaxSize = int64_t(1) << 30;

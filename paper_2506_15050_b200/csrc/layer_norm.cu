@@ -14,7 +14,7 @@
 // block's threads for its whole walk over the rows; each block writes one partial row of them to the
 // workspace and a second kernel adds those in a fixed order, so the gradients do not depend on scheduling.
 // Rows too long for either way take kernels that read the row again from L2.
-//   [16384, 5120] bf16: forward 62 us (5.4 TB/s, 0.82 of the measured copy rate), backward 109 us (4.6 TB/s)
+//   [16384, 5120] bf16: forward 62-64 us (5.3 TB/s, 0.81 of the measured copy rate), backward 109-112 us (4.5 TB/s)
 //   [16384, 5120] fp32: forward 107 us (6.3 TB/s), backward 168 us (6.0 TB/s)
 #include <type_traits>
 
@@ -1094,10 +1094,6 @@ __global__ void __launch_bounds__(1024) norm_sum_kernel(const float* partial, in
 constexpr int kNormColParts = 64;              // partial rows of norm_cols_kernel
 constexpr int32_t kNormRingCols = 512 * 32;    // most columns of the kernels that walk over rows: threads times columns of each
 int norm_max_parts(int32_t N) { return N <= 512 ? 8 * kNumSms : N <= 2048 ? 5 * kNumSms : 3 * kNumSms; }
-
-bool rows_aligned(const void* p, int64_t ld, size_t esize) {
-    return aligned(p, 16) && (ld * int64_t(esize)) % 16 == 0;
-}
 
 // Calls f.template operator()<CH>() with the smallest CH of the list that is at least `need`.
 template <int... CH, class F>

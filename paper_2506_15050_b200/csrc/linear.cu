@@ -851,14 +851,13 @@ LinearWs linear_carve(void* ws, int64_t M, int32_t K, int32_t N) {
     return r;
 }
 
-bool tma_rows(const void* p, int64_t ld) { return aligned(p, 16) && ld % 8 == 0; }
+bool tma_rows(const void* p, int64_t ld) { return rows_aligned(p, ld, 2); }
 // Whether a [rows, cols] operand that TMA takes as it is is better copied to whole lines first: a product
 // loses a fifth of its time (at 1.2 PFLOP/s) to each operand with straddling rows, a copy moves four bytes
 // per element at 5 TB/s after 2 us.
 bool worth_copying(const void* p, int64_t ld, int64_t rows, int64_t cols, double flops) {
     return (ld % 64 != 0 || !aligned(p, 128)) && 0.2 * flops / 1.2e15 > double(rows) * double(cols) * 4 / 5e12 + 2e-6;
 }
-bool vec_rows(const void* p, int64_t ld, size_t esize) { return aligned(p, 16) && (ld * int64_t(esize)) % 16 == 0; }
 
 int repack(DenseOperand& o, bf16_bits* dst, cudaStream_t s, Link link) {
     const int64_t ldo = pad64(o.cols);
@@ -925,7 +924,7 @@ TPPO_API int tppo_linear_fwd(const void* x, int64_t ldx, const void* weight, int
     e.y = y; e.ldy = ldy; e.y_f32 = y_dtype == TPPO_F32;
     e.pre = static_cast<bf16_bits*>(preact); e.ldp = ldp;
     e.M = M; e.N = N; e.act = activation;
-    e.vec_y = vec_rows(y, ldy, ys); e.vec_r = vec_rows(residual, ldr, 2); e.vec_p = vec_rows(preact, ldp, 2);
+    e.vec_y = rows_aligned(y, ldy, ys); e.vec_r = rows_aligned(residual, ldr, 2); e.vec_p = rows_aligned(preact, ldp, 2);
     e.vec_b = aligned(bias, 16);
     e.status = status;
     if (narrow) {
@@ -1016,17 +1015,17 @@ TPPO_API int tppo_linear_bwd(const void* dy, int32_t dy_dtype, int64_t lddy, con
         if (gy > kDzMaxParts) gy = kDzMaxParts;
         parts = int32_t(gy);
         const bool act = activation != TPPO_ACT_NONE;
-        const bool vec = N % 8 == 0 && vec_rows(dy, lddy, ds) && (!act || vec_rows(preact, ldp, 2));
+        const bool vec = N % 8 == 0 && rows_aligned(dy, lddy, ds) && (!act || rows_aligned(preact, ldp, 2));
         auto kernel = dy_dtype == TPPO_F32 ? linear_dz_pick<float>(vec, act) : linear_dz_pick<bf16_bits>(vec, act);
         TPPO_CUDA_CHECK(launch_dense(kernel, dim3(gx, unsigned(gy)), dim3(256), 0, s, a));
         if (make_dz) { Z.p = w.dz; Z.ld = a.ldz; }
     }
     if (dx) {        // dx[m, k] = sum_n dz[m, n] W[k, n]: both operands contiguous along the contraction
-        const EpiStore e{static_cast<bf16_bits*>(dx), lddx, M, K, vec_rows(dx, lddx, 2), status};
+        const EpiStore e{static_cast<bf16_bits*>(dx), lddx, M, K, rows_aligned(dx, lddx, 2), status};
         if ((rc = dense_product<0, 0, false, false>(Z, W, M, K, N, e, status, s, second.next())) != TPPO_OK) return rc;
     }
     if (dweight) {   // dweight[k, n] = sum_m x[m, k] dz[m, n]: both contiguous along their outer index
-        const EpiStore e{static_cast<bf16_bits*>(dweight), lddw, K, N, vec_rows(dweight, lddw, 2), status};
+        const EpiStore e{static_cast<bf16_bits*>(dweight), lddw, K, N, rows_aligned(dweight, lddw, 2), status};
         if ((rc = dense_product<1, 1, false, false>(X, Z, K, N, M, e, status, s, second.next())) != TPPO_OK) return rc;
     }
     if (dbias) {
