@@ -64,7 +64,9 @@ typedef enum {
     TPPO_OP_LMHEAD = 4,
     TPPO_OP_LAYER_NORM = 5, /* N = rows, V = columns                                         */
     TPPO_OP_LINEAR = 6,     /* N = rows M, B = K, V = N of the product; see tppo_linear_fwd  */
-    TPPO_OP_MUON = 7        /* N = rows, V = columns of the matrix                           */
+    TPPO_OP_MUON = 7,       /* N = rows, V = columns of the matrix                           */
+    TPPO_OP_RESIDUAL_NORM = 8, /* N = rows, V = columns                                      */
+    TPPO_OP_GRAD_NORM = 9   /* N = number of tensors                                         */
 } tppo_op;
 
 /* element types */
@@ -426,8 +428,9 @@ int tppo_advance_batch(const int32_t *seq_begin, const int32_t *prompt_len,
 
 /*
  * ---- Dense operators around the LM-head -----------------------------------------------------------
- * The final layer norm that produces `hidden` and takes `dhidden`, the projections and the value
- * head, and the update their weight gradients are turned into.  They follow the conventions above
+ * The final layer norm that produces `hidden` and takes `dhidden`, the projections (in 16 and 8 bits) and the
+ * value head, the join of a block with the residual stream, the norm of all gradients, and the update they are
+ * turned into.  They follow the conventions above
  * with two differences:
  *   - matrices may be strided: element (r, c) is at r * ld + c, ld >= number of columns.  16-byte
  *     aligned rows (base and ld) take the fast paths; any other base (aligned to its element) and ld
@@ -562,6 +565,149 @@ int tppo_muon_orthogonalize(const void *grad, int32_t grad_dtype, int64_t ldg,
                             float mu, int32_t nesterov, float eps, int32_t steps, float scale,
                             void *update, int64_t ldu, int32_t *status,
                             void *workspace, size_t workspace_bytes, void *stream);
+
+/* the norms of the residual join: bits */
+enum {
+    TPPO_NORM_POST = 1, /* of the block's output, before it joins the residual stream */
+    TPPO_NORM_PRE = 2   /* of the joined stream, for the next block                   */
+};
+
+/*
+ * Residual join: a block's output z is normed, gated and added to the scaled residual stream, and the sum is
+ * normed for the next block.  Per row, with root-mean-square norms in fp32:
+ *     rstd_post = 1 / sqrt(sum_c z^2 / N + eps),   p = z * rstd_post * gamma_post    (p = z without TPPO_NORM_POST)
+ *     h = alpha * residual + gate * p
+ *     rstd_pre = 1 / sqrt(sum_c h^2 / N + eps),    n = h * rstd_pre * gamma_pre      (no n without TPPO_NORM_PRE)
+ *   z, residual [M, N] of `dtype` (TPPO_BF16 or TPPO_F32)
+ *   gate        NULL (1); one row [N] of `param_dtype`, shared by all rows, with ldg = 0; or [M, N] of `dtype`
+ *               with ldg >= N
+ *   gamma_post, gamma_pre [N] of `param_dtype` or NULL (1; always NULL without their norm)
+ *   norms       any combination of the bits above
+ *   h           [M, N] of `dtype` out; may be residual itself or z itself with the same row stride
+ *   n           [M, N] of `dtype` out, given exactly with TPPO_NORM_PRE; may be z itself (then h may not)
+ *   rstd_post, rstd_pre [M] fp32 out or NULL: what the backward call takes
+ *   alpha finite, eps >= 0
+ * Each output is rounded once; n is formed from the unrounded h.  A row that has no statistics (a NaN or
+ * infinity in it, in its gate or in gamma_post; sums of squares or of magnitudes outside fp32; with eps = 0 a row
+ * of zeros to be normed) gets h, n and rstd of 0 and raises TPPO_DEV_NONFINITE.  gamma_pre is taken as it is,
+ * and elements that leave the range of their type become infinities.
+ */
+int tppo_residual_norm_fwd(const void *z, int64_t ldz, const void *residual, int64_t ldr,
+                           const void *gate, int64_t ldg, int32_t dtype, int64_t M, int32_t N,
+                           const void *gamma_post, const void *gamma_pre, int32_t param_dtype,
+                           float alpha, float eps, int32_t norms, void *h, int64_t ldh, void *n, int64_t ldn,
+                           float *rstd_post, float *rstd_pre, int32_t *status, void *stream);
+
+/*
+ * Its backward pass.  With hh = h * rstd_pre, zz = z * rstd_post (z without TPPO_NORM_POST):
+ *     d = dh + rstd_pre * (dn * gamma_pre - hh * sum_c (dn * gamma_pre * hh) / N)     (d = dh without TPPO_NORM_PRE)
+ *     dresidual = alpha * d,   dgate = d * zz * gamma_post,   a = d * gate * gamma_post,
+ *     dz = rstd_post * (a - zz * sum_c (a * zz) / N)                                  (dz = a without TPPO_NORM_POST)
+ *     dgamma_post[c] = sum_r d * gate * zz,   dgamma_pre[c] = sum_r dn * hh,   and dgate summed over r for a row
+ *   dh          [M, N] of `dtype` or NULL (0): gradient of h from further down the residual stream
+ *   dn          [M, N] of `dtype`, given exactly with TPPO_NORM_PRE
+ *   z; h as the forward call stored it (with TPPO_NORM_PRE only, else NULL); rstd_post, rstd_pre of its norms
+ *   dz, dresidual [M, N] of `dtype`, each may be NULL; dresidual may be dh itself, dz may be dn itself, with the same
+ *               row stride
+ *   dgate       like gate ([N] of `param_dtype` with ldg = 0, or [M, N] of `dtype` with row stride lddg) or NULL
+ *   dgamma_post, dgamma_pre [N] of `param_dtype` or NULL; overwritten, not accumulated
+ *   workspace   tppo_workspace_bytes(TPPO_OP_RESIDUAL_NORM, M, 0, 0, N) bytes; may be NULL when no column sums
+ *               (dgamma_post, dgamma_pre, dgate of a row) are asked for
+ * A row without statistics (an rstd of 0) contributes nothing and gets gradients of 0; so does a row in which a
+ * gradient, activation or parameter that enters a product above is not finite or makes its sums so, which raises
+ * TPPO_DEV_NONFINITE.  Elements and sums over rows that leave the range of their type become infinities.  M = 0
+ * writes the column sums 0.
+ */
+int tppo_residual_norm_bwd(const void *dh, int64_t lddh, const void *dn, int64_t lddn, const void *z, int64_t ldz,
+                           const void *h, int64_t ldh, const void *gate, int64_t ldg, int32_t dtype,
+                           int64_t M, int32_t N, const void *gamma_post, const void *gamma_pre, int32_t param_dtype,
+                           const float *rstd_post, const float *rstd_pre, float alpha, int32_t norms,
+                           void *dz, int64_t lddz, void *dresidual, int64_t lddr, void *dgate, int64_t lddg,
+                           void *dgamma_post, void *dgamma_pre, int32_t *status,
+                           void *workspace, size_t workspace_bytes, void *stream);
+
+/* how elements share a scale: bits of the quantiser's and the product's `block` */
+enum {
+    TPPO_FP8_ROWS = 1,  /* 128 consecutive elements along the contraction                      */
+    TPPO_FP8_SQUARE = 2 /* 128 x 128 elements (weights: one scale serves both of their layouts) */
+};
+
+/*
+ * 8-bit values (e4m3: four significant bits, up to 448) with one fp32 scale per block of 128: x ~ q * scale.  The
+ * scale is the least power of two 2^e, e >= -126, for which the block's largest magnitude is at most 448 * 2^e (1 for
+ * a block of zeros), so that x / scale is exact, q is x / scale rounded once (to nearest even), and q * scale is
+ * exact in bf16.  q holds the rows of x as they are, for products that contract over x's columns; qt is x
+ * transposed, for products that contract over x's rows, with blocks of its own along them.
+ *   x       [M, K] of `dtype` (TPPO_BF16 or TPPO_F32)
+ *   q       [M, K] 8-bit out or NULL;  scale out:
+ *             TPPO_FP8_ROWS    [ceil(K / 128), M] with row stride lds: scale of (row m, columns 128 b ..) at (b, m)
+ *             TPPO_FP8_SQUARE  [ceil(M / 128), ceil(K / 128)] with row stride lds
+ *   qt      [K, M] 8-bit out or NULL;  scale_t out:
+ *             TPPO_FP8_ROWS    [ceil(M / 128), K] with row stride ldst
+ *             TPPO_FP8_SQUARE  [ceil(K / 128), ceil(M / 128)] with row stride ldst: the transpose of scale
+ * q, qt: base and row stride multiples of 16 bytes; with TPPO_FP8_ROWS scale, scale_t likewise (row strides multiples
+ * of 4).  Padding between rows is not written.  An element that is not finite counts as 0 and raises TPPO_DEV_NONFINITE.
+ */
+int tppo_fp8_quantize(const void *x, int32_t dtype, int64_t ldx, int64_t M, int64_t K, int32_t block,
+                      void *q, int64_t ldq, float *scale, int64_t lds,
+                      void *qt, int64_t ldqt, float *scale_t, int64_t ldst, int32_t *status, void *stream);
+
+/*
+ * Product of two such matrices, both given with the contraction along their rows:
+ *     y[m, n] = sum_b a_scale(b, m) * b_scale(b, n) * sum_{k in block b} a[m, k] * b[n, k]
+ *   a        [M, K], a_scale [ceil(K / 128), M] as TPPO_FP8_ROWS gives them
+ *   b        [N, K], b_scale as `b_block` says: TPPO_FP8_ROWS [ceil(K / 128), N], or TPPO_FP8_SQUARE
+ *            [ceil(N / 128), ceil(K / 128)]
+ *   y        [M, N] of `y_dtype`, rounded once
+ * With a weight w [K, N] quantised in squares (q, qt), activations x and gradients dy in rows (q, qt):
+ *     x w        = product of x's q  and w's qt (TPPO_FP8_SQUARE)
+ *     dy w^T     = product of dy's q and w's q  (TPPO_FP8_SQUARE)
+ *     x^T dy     = product of x's qt and dy's qt (TPPO_FP8_ROWS)
+ * Any fp32 scales are taken.  Sums within a block are those of the tensor cores, scaled and added up in fp32.
+ * An element of y that is not finite or leaves the range of its type is written 0 and raises TPPO_DEV_NONFINITE.
+ * K = 0 gives y = 0.  Alignment as for the quantiser; y may be strided at any element.  y may not overlap an input.
+ * The first call on a device looks up the driver's tensor-map encoder (TPPO_ERR_CUDA if absent).
+ */
+int tppo_fp8_matmul(const void *a, int64_t lda, const float *a_scale, int64_t ldas,
+                    const void *b, int64_t ldb, const float *b_scale, int64_t ldbs, int32_t b_block,
+                    int64_t M, int64_t N, int64_t K, void *y, int32_t y_dtype, int64_t ldy,
+                    int32_t *status, void *stream);
+
+/* One of many tensors: n contiguous elements of `dtype` (TPPO_BF16 or TPPO_F32) at the device address `data`,
+ * which may be NULL when n is 0.  Any alignment of its element. */
+typedef struct {
+    void *data;
+    int64_t n;
+    int32_t dtype;
+    int32_t reserved; /* 0 */
+} tppo_tensor;
+
+/*
+ * Sum of squares and norm over all elements of `count` gradients:
+ *     sum_sq = sum_i sum_e g_i[e]^2   (64 bits),   norm = sqrt(sum_sq)   (fp32)
+ *   grads     HOST array of `count` tensors, read before the call returns; the addresses become part of the
+ *             launch (a captured call keeps them).  A tensor listed twice counts twice.
+ *   sum_sq    [1] fp64 out;  norm [1] fp32 out or NULL
+ *   workspace tppo_workspace_bytes(TPPO_OP_GRAD_NORM, count, 0, 0, 0) bytes
+ * With a gradient element that is not finite both results are +infinity and TPPO_DEV_NONFINITE is raised; a norm
+ * beyond fp32 is +infinity as well, sum_sq is then still right.  With several ranks, each holding some of the gradients, add up their sum_sq and
+ * pass the sum to tppo_grad_clip.
+ */
+int tppo_grad_norm(const tppo_tensor *grads, int32_t count, double *sum_sq, float *norm, int32_t *status,
+                   void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Gradients scaled down to a norm of at most max_norm:
+ *     coef = min(1, max_norm / sqrt(sum_sq)),   out_i = coef * g_i
+ *   sum_sq    [1] fp64 from tppo_grad_norm, on the device;  max_norm finite, >= 0
+ *   out       HOST array of `count` tensors of the same lengths, of either type each; or NULL: in place.  An
+ *             output is its gradient itself or overlaps none of the tensors.  In place, a coefficient of 1 leaves the
+ *             gradients untouched (and unread).
+ *   coef      [1] fp32 out or NULL
+ * A sum_sq that is not finite gives coef = 0, outputs of 0 and TPPO_DEV_NONFINITE: a step without effect.
+ */
+int tppo_grad_clip(const tppo_tensor *grads, int32_t count, const double *sum_sq, double max_norm,
+                   const tppo_tensor *out, float *coef, int32_t *status, void *stream);
 
 #ifdef __cplusplus
 }

@@ -22,7 +22,9 @@ if not os.path.exists(LIB_PATH):
 _lib = C.CDLL(LIB_PATH)
 
 OP_EGAE, OP_SELECT_TOKENS, OP_POLICY_LOSS, OP_VALUE_LOSS, OP_LMHEAD = range(5)
-OP_LAYER_NORM, OP_LINEAR, OP_MUON = 5, 6, 7
+OP_LAYER_NORM, OP_LINEAR, OP_MUON, OP_RESIDUAL_NORM, OP_GRAD_NORM = 5, 6, 7, 8, 9
+NORM_POST, NORM_PRE = 1, 2
+FP8_ROWS, FP8_SQUARE = 1, 2
 BF16, F32 = 0, 1
 DLOGITS_NONE, DLOGITS_FULL, DLOGITS_COMPACT = 0, 1, 2
 ACT_NONE, ACT_RELU, ACT_GELU, ACT_GELU_TANH, ACT_SILU = range(5)
@@ -87,6 +89,20 @@ _lib.tppo_linear_bwd.argtypes = [_vp, _i32, _i64, _vp, _i64, _vp, _i64, _i64, _i
 _lib.tppo_muon_orthogonalize.restype = C.c_int
 _lib.tppo_muon_orthogonalize.argtypes = [_vp, _i32, _i64, _vp, _i64, _i64, _i32, _f32, _i32, _f32, _i32, _f32,
                                          _vp, _i64, _vp, _vp, _sz, _vp]
+_lib.tppo_residual_norm_fwd.restype = C.c_int
+_lib.tppo_residual_norm_fwd.argtypes = [_vp, _i64, _vp, _i64, _vp, _i64, _i32, _i64, _i32, _vp, _vp, _i32, _f32, _f32, _i32,
+                                        _vp, _i64, _vp, _i64, _vp, _vp, _vp, _vp]
+_lib.tppo_residual_norm_bwd.restype = C.c_int
+_lib.tppo_residual_norm_bwd.argtypes = [_vp, _i64, _vp, _i64, _vp, _i64, _vp, _i64, _vp, _i64, _i32, _i64, _i32, _vp, _vp,
+                                        _i32, _vp, _vp, _f32, _i32, _vp, _i64, _vp, _i64, _vp, _i64, _vp, _vp, _vp, _vp, _sz, _vp]
+_lib.tppo_fp8_quantize.restype = C.c_int
+_lib.tppo_fp8_quantize.argtypes = [_vp, _i32, _i64, _i64, _i64, _i32, _vp, _i64, _vp, _i64, _vp, _i64, _vp, _i64, _vp, _vp]
+_lib.tppo_fp8_matmul.restype = C.c_int
+_lib.tppo_fp8_matmul.argtypes = [_vp, _i64, _vp, _i64, _vp, _i64, _vp, _i64, _i32, _i64, _i64, _i64, _vp, _i32, _i64, _vp, _vp]
+_lib.tppo_grad_norm.restype = C.c_int
+_lib.tppo_grad_norm.argtypes = [_vp, _i32, _vp, _vp, _vp, _vp, _sz, _vp]
+_lib.tppo_grad_clip.restype = C.c_int
+_lib.tppo_grad_clip.argtypes = [_vp, _i32, _vp, C.c_double, _vp, _vp, _vp, _vp]
 
 
 class TppoError(RuntimeError):
@@ -392,3 +408,133 @@ def tppo_muon_orthogonalize(grad, momentum, mu, nesterov, eps, steps, scale, upd
     _check(_lib.tppo_muon_orthogonalize(
         pg, _DTYPES[grad.dtype], ldg, pm, ldm, R, cols, mu, 1 if nesterov else 0, eps, steps, scale, pu, ldu,
         _vector(status, here, 1, torch.int32), *_scratch(ws, here), _raw_stream(here)))
+
+
+def _gate(gate, here, M, N, dtype):
+    """(pointer, row stride) of a gate: a row of N shared by all rows (stride 0), or a matrix."""
+    if gate is None or gate.dim() == 1:
+        return _vector(gate, here, N), 0
+    return _matrix(gate, here, M, N, dtype)
+
+
+def _row(gate):
+    return gate if gate is not None and gate.dim() == 1 else None
+
+
+def tppo_residual_norm_fwd(z, residual, gate, gamma_post, gamma_pre, alpha, eps, norms, h, n, rstd_post, rstd_pre, status):
+    (M, N), dt, here = z.shape, z.dtype, _current_device()
+    (pz, ldz), (pr, ldr) = _matrix(z, here, M, N), _matrix(residual, here, M, N, dt)
+    pg, ldg = _gate(gate, here, M, N, dt)
+    (ph, ldh), (pn, ldn) = _matrix(h, here, M, N, dt), _matrix(n, here, M, N, dt)
+    _check(_lib.tppo_residual_norm_fwd(
+        pz, ldz, pr, ldr, pg, ldg, _DTYPES[dt], M, N, _vector(gamma_post, here, N), _vector(gamma_pre, here, N),
+        _type_of(gamma_post, gamma_pre, _row(gate)), alpha, eps, norms, ph, ldh, pn, ldn,
+        _vector(rstd_post, here, M, torch.float32), _vector(rstd_pre, here, M, torch.float32),
+        _vector(status, here, 1, torch.int32), _raw_stream(here)))
+
+
+def tppo_residual_norm_bwd(dh, dn, z, h, gate, gamma_post, gamma_pre, rstd_post, rstd_pre, alpha, norms, dz, dresidual, dgate,
+                           dgamma_post, dgamma_pre, status, ws):
+    """h is read with NORM_PRE only."""
+    (M, N), dt, here = z.shape, z.dtype, _current_device()
+    if not norms & NORM_PRE:
+        h = None
+    (pdh, lddh), (pdn, lddn) = _matrix(dh, here, M, N, dt), _matrix(dn, here, M, N, dt)
+    (pz, ldz), (ph, ldh) = _matrix(z, here, M, N), _matrix(h, here, M, N, dt)
+    pg, ldg = _gate(gate, here, M, N, dt)
+    (po, lddz), (pr, lddr) = _matrix(dz, here, M, N, dt), _matrix(dresidual, here, M, N, dt)
+    assert dgate is None or (gate is not None and dgate.dim() == gate.dim()), "dgate must have the gate's form"
+    pdg, lddg = _gate(dgate, here, M, N, dt)
+    _check(_lib.tppo_residual_norm_bwd(
+        pdh, lddh, pdn, lddn, pz, ldz, ph, ldh, pg, ldg, _DTYPES[dt], M, N, _vector(gamma_post, here, N),
+        _vector(gamma_pre, here, N), _type_of(gamma_post, gamma_pre, _row(gate), _row(dgate), dgamma_post, dgamma_pre),
+        _vector(rstd_post, here, M, torch.float32), _vector(rstd_pre, here, M, torch.float32), alpha, norms, po, lddz, pr, lddr,
+        pdg, lddg, _vector(dgamma_post, here, N), _vector(dgamma_pre, here, N), _vector(status, here, 1, torch.int32),
+        *_scratch(ws, here), _raw_stream(here)))
+
+
+_F8 = torch.float8_e4m3fn
+
+
+def fp8_empty(rows, cols, device):
+    """An uninitialised [rows, cols] matrix of 8-bit values whose rows start on 16-byte boundaries."""
+    return torch.empty((rows, -(-cols // 16) * 16), dtype=_F8, device=device)[:, :cols]
+
+
+def fp8_scales(rows, cols, block, device):
+    """Uninitialised scales of a [rows, cols] matrix of 8-bit values: [column blocks, rows] for FP8_ROWS, [row
+    blocks, column blocks] for FP8_SQUARE."""
+    kb = -(-cols // 128)
+    if block == FP8_SQUARE:
+        return torch.empty((-(-rows // 128), kb), dtype=torch.float32, device=device)
+    return torch.empty((kb, -(-rows // 4) * 4), dtype=torch.float32, device=device)[:, :rows]
+
+
+def _scales(t, here, rows, cols, block):
+    kb = -(-cols // 128)
+    return _matrix(t, here, *((-(-rows // 128), kb) if block == FP8_SQUARE else (kb, rows)), torch.float32)
+
+
+def tppo_fp8_quantize(x, block, q, scale, qt, scale_t, status):
+    """q with scale, or qt with scale_t, may be None (see fp8_empty, fp8_scales for what they are)."""
+    (M, K), here = x.shape, _current_device()
+    px, ldx = _matrix(x, here, M, K)
+    (pq, ldq), (ps, lds) = _matrix(q, here, M, K, _F8), _scales(scale, here, M, K, block)
+    (pt, ldt), (pst, ldst) = _matrix(qt, here, K, M, _F8), _scales(scale_t, here, K, M, block)
+    _check(_lib.tppo_fp8_quantize(px, _DTYPES[x.dtype], ldx, M, K, block, pq, ldq, ps, lds, pt, ldt, pst, ldst,
+                                  _vector(status, here, 1, torch.int32), _raw_stream(here)))
+
+
+def tppo_fp8_matmul(a, a_scale, b, b_scale, b_block, y, status):
+    (M, K), N, here = a.shape, b.shape[0], _current_device()
+    (pa, lda), (pas, ldas) = _matrix(a, here, M, K, _F8), _scales(a_scale, here, M, K, FP8_ROWS)
+    (pb, ldb), (pbs, ldbs) = _matrix(b, here, N, K, _F8), _scales(b_scale, here, N, K, b_block)
+    py, ldy = _matrix(y, here, M, N)
+    _check(_lib.tppo_fp8_matmul(pa, lda, pas, ldas, pb, ldb, pbs, ldbs, b_block, M, N, K, py, _DTYPES[y.dtype], ldy,
+                                _vector(status, here, 1, torch.int32), _raw_stream(here)))
+
+
+class _Tensor(C.Structure):
+    _fields_ = [("data", _vp), ("n", _i64), ("dtype", _i32), ("reserved", _i32)]
+
+
+class TensorList:
+    """The tensors of a gradient norm as the library takes them (see tensor_list)."""
+
+    def __init__(self, tensors):
+        self.tensors = list(tensors)            # kept alive
+        self.count = len(self.tensors)
+        self.device = self.tensors[0].get_device() if self.tensors else None
+        self.array = (_Tensor * self.count)()
+        for a, t in zip(self.array, self.tensors):
+            assert t.is_cuda and t.get_device() == self.device, "tensors must be on one CUDA device"
+            assert t.is_contiguous(), "tensors must be contiguous"
+            a.data, a.n, a.dtype = t.data_ptr() if t.numel() else None, t.numel(), _DTYPES[t.dtype]
+        self.pointer = C.addressof(self.array)
+
+    def on(self, here):
+        assert self.device is None or self.device == here, f"tensors must be on cuda:{here}, the current device"
+        return self.pointer if self.count else None
+
+
+def tensor_list(tensors) -> TensorList:
+    """Made once for tensors that stay where they are, e.g. the gradients of a model."""
+    return TensorList(tensors)
+
+
+def tppo_grad_norm(grads, sum_sq, norm, status, ws):
+    """grads: a TensorList."""
+    here = _current_device()
+    _check(_lib.tppo_grad_norm(grads.on(here), grads.count, _vector(sum_sq, here, 1, torch.float64),
+                               _vector(norm, here, 1, torch.float32), _vector(status, here, 1, torch.int32),
+                               *_scratch(ws, here), _raw_stream(here)))
+
+
+def tppo_grad_clip(grads, sum_sq, max_norm, out, coef, status):
+    """grads: a TensorList; out: one of the same lengths, or grads itself or None for in place."""
+    here = _current_device()
+    if out is not None:
+        assert out.count == grads.count, "out must have as many tensors as grads"
+    _check(_lib.tppo_grad_clip(grads.on(here), grads.count, _vector(sum_sq, here, 1, torch.float64), max_norm,
+                               None if out is None else out.on(here), _vector(coef, here, 1, torch.float32),
+                               _vector(status, here, 1, torch.int32), _raw_stream(here)))

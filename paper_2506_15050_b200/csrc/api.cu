@@ -10,6 +10,8 @@ size_t lmhead_workspace_bytes(int64_t M, int32_t K, int32_t V);
 size_t norm_workspace_bytes(int64_t M, int32_t N);
 size_t linear_workspace_bytes(int64_t M, int32_t K, int32_t N, bool copies);
 size_t muon_workspace_bytes(int64_t R, int32_t C);
+size_t residual_norm_workspace_bytes(int64_t M, int32_t N);
+size_t grad_norm_workspace_bytes(int64_t count);
 }  // namespace tppo
 
 // Test hooks (see tppo_test_hooks in the header): read by the launchers of the two look-back kernels.
@@ -42,8 +44,8 @@ TPPO_API const char* tppo_status_string(int status) {
     }
 }
 
-// N doubles as the number of logits rows R for TPPO_OP_POLICY_LOSS and as M for TPPO_OP_LMHEAD and the
-// dense operators (B then carries K, V the columns).
+// N doubles as the number of logits rows R for TPPO_OP_POLICY_LOSS, as M for TPPO_OP_LMHEAD and the
+// dense operators (B then carries K, V the columns), and as the number of tensors for TPPO_OP_GRAD_NORM.
 TPPO_API size_t tppo_workspace_bytes(int op, int64_t N, int32_t B, int64_t n_max, int32_t V) {
     if (N < 0 || n_max < 0) return 0;
     switch (op) {
@@ -55,6 +57,8 @@ TPPO_API size_t tppo_workspace_bytes(int op, int64_t N, int32_t B, int64_t n_max
         case TPPO_OP_LAYER_NORM: return tppo::norm_workspace_bytes(N, V);
         case TPPO_OP_LINEAR: return tppo::linear_workspace_bytes(N, B, V, n_max != 0);
         case TPPO_OP_MUON: return tppo::muon_workspace_bytes(N, V);
+        case TPPO_OP_RESIDUAL_NORM: return tppo::residual_norm_workspace_bytes(N, V);
+        case TPPO_OP_GRAD_NORM: return tppo::grad_norm_workspace_bytes(N);
         default: return 0;
     }
 }

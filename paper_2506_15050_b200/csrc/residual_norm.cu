@@ -1,0 +1,813 @@
+// The residual join: a block's output normed, gated and added to the scaled residual stream, and the sum normed
+// for the next block; forward and backward with the parameters' gradients.  With root-mean-square norms,
+//     h = alpha * residual + gate * gamma_post * z * r1,   n = h * r2 * gamma_pre
+//     d = dh + r2 * (a2 - h r2^2 mean(a2 h)),  a2 = dn * gamma_pre;   dresidual = alpha * d
+//     a1 = d * gate * gamma_post,   dz = r1 * (a1 - z r1^2 mean(a1 z)),   dgate = d * z * r1 * gamma_post
+//     dgamma_post = sum_rows d * gate * z * r1,   dgamma_pre = sum_rows dn * h * r2
+// All arithmetic is fp32; each input is read once, each output rounded once.  4 elements move forward and 6
+// backward per element of a row (one and two more with a gate per element), so HBM is the bound.
+//
+// One block per SM, cut into groups of warps that walk rows of their own.  Each thread brings its 16-byte
+// pieces of the next rows into a ring of shared memory of its own with cp.async: what it copies only it reads,
+// so the ring needs no barrier, and 100-200 KB per SM stay in flight whatever the arithmetic does.  gate *
+// gamma_post and gamma_pre sit in shared memory as fp32 for the block's life.
+//
+// Forward needs two sums over the row, one behind the other.  Backward takes one: with w = gate gamma_post z,
+//     sum(a1 z) = sum((dh + r2 a2) w) - r2^3 mean(a2 h) sum(h w),
+// three sums that do not wait for one another, met at one barrier per row.  (The same expansion of sum(h^2) would
+// lose all its digits where the block's output cancels the residual, so the forward pass does not use it.)
+//
+// Rows that do not start on 16-byte boundaries are read by the same aligned pieces, the first and last of which
+// hold elements of neighbouring rows or of nothing (a piece with one element of the row in it is mapped), masked
+// when they are used and stored element by element.  A block only takes rows that start at the same place of
+// a piece, so that a thread's columns, parameters and column sums stay its own.
+// Rows that do not fit, and matrices whose rows do not start at the same place of a piece, take one block per
+// row and read it again for each sweep.
+#include "dense_common.cuh"
+
+namespace tppo {
+namespace {
+
+constexpr int kJoinThreads = 640;                         // of a block at up to 48 elements per thread
+constexpr int kJoinSmem = 224 * 1024;
+constexpr int kJoinAnyThreads = 512, kJoinAnyBlocks = kNumSms * 2;
+constexpr int kJoinStages = 4;
+
+enum { kZ = 0, kRes = 1, kGate = 2, kFwdIn = 3 };         // forward inputs
+enum { kH = 1, kDn = 3, kDh = 4, kBwdIn = 5 };            // backward: z, h, gate, dn, dh
+
+struct JoinArgs {
+    const void* in[kBwdIn];                               // matrices, NULL where there is none
+    int64_t ld[kBwdIn];
+    int32_t slot[kBwdIn];                                 // place in a stage
+    const void* gate_row; const void* gamma_post; const void* gamma_pre;      // NULL: 1
+    int32_t p32;                                          // parameters are fp32
+    void* out[3]; int64_t ldo[3];                         // h, n | dz, dresidual, dgate
+    float* r_post; float* r_pre;                          // out | in; NULL in the backward pass: no such norm
+    float* partial;                                       // column sums: [blocks][2][N]
+    int32_t* status;
+    int64_t M; int32_t N; float alpha, eps; int32_t norms;
+    int32_t T, groups, stages, arrays;                    // threads per group; groups per block; stages; matrices per stage
+    int32_t shift_step;                                   // rows start (first row's + r * this) elements into a piece
+};
+
+template <class T> struct Join { static constexpr int VEC = 16 / sizeof(T); };
+
+__device__ __forceinline__ float param(const void* p, int64_t i, bool f32) {
+    return !p ? 1.f : f32 ? static_cast<const float*>(p)[i] : load_f32(static_cast<const bf16_bits*>(p) + i);
+}
+__device__ __forceinline__ void put_param(void* p, int64_t i, bool f32, float v) {
+    if (f32) store_f32(static_cast<float*>(p) + i, v);
+    else store_f32(static_cast<bf16_bits*>(p) + i, v);
+}
+
+__device__ __forceinline__ void copy16(uint32_t dst, const void* src) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
+__device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+// Until at most `stages - 1` of this thread's groups of copies are outstanding.
+__device__ __forceinline__ void copy_wait(int stages) {
+    switch (stages) {
+        case 1: asm volatile("cp.async.wait_group 0;" ::: "memory"); break;
+        case 2: asm volatile("cp.async.wait_group 1;" ::: "memory"); break;
+        case 3: asm volatile("cp.async.wait_group 2;" ::: "memory"); break;
+        default: asm volatile("cp.async.wait_group 3;" ::: "memory"); break;
+    }
+}
+
+// A thread's pieces of a row: piece c covers columns col(c) .. col(c) + VEC - 1.
+template <class T, int E>
+struct JoinColumns {
+    static constexpr int VEC = Join<T>::VEC;
+    int first, step, N;
+    __device__ __forceinline__ int col(int c) const { return first + c * step; }
+    __device__ __forceinline__ bool any(int c) const { return col(c) < N && col(c) + VEC > 0; }
+    __device__ __forceinline__ bool all(int c) const { return col(c) >= 0 && col(c) + VEC <= N; }
+    __device__ __forceinline__ bool has(int c, int i) const { return unsigned(col(c) + i) < unsigned(N); }
+};
+
+template <class T>
+__device__ __forceinline__ void join_widen(uint4 w, float (&v)[Join<T>::VEC]) {
+    if constexpr (sizeof(T) == 2) {
+        v[0] = bf16_lo(w.x); v[1] = bf16_hi(w.x); v[2] = bf16_lo(w.y); v[3] = bf16_hi(w.y);
+        v[4] = bf16_lo(w.z); v[5] = bf16_hi(w.z); v[6] = bf16_lo(w.w); v[7] = bf16_hi(w.w);
+    } else {
+        v[0] = __uint_as_float(w.x); v[1] = __uint_as_float(w.y); v[2] = __uint_as_float(w.z); v[3] = __uint_as_float(w.w);
+    }
+}
+// The widened piece; 0 outside the row.
+template <class T, class C>
+__device__ __forceinline__ void join_piece(const C& k, int c, uint32_t at, float (&v)[Join<T>::VEC]) {
+    join_widen<T>(ptx::lds128(at), v);
+    if (!k.all(c)) {
+#pragma unroll
+        for (int i = 0; i < Join<T>::VEC; ++i) v[i] = k.has(c, i) ? v[i] : 0.f;
+    }
+}
+template <class T, class C>
+__device__ __forceinline__ void join_store(const C& k, int c, T* row, const float (&v)[Join<T>::VEC]) {
+    if (k.all(c)) {
+        store_vec<Join<T>::VEC>(row + k.col(c), v);
+    } else {
+#pragma unroll
+        for (int i = 0; i < Join<T>::VEC; ++i)
+            if (k.has(c, i)) store_f32(row + k.col(c) + i, v[i]);
+    }
+}
+// VEC parameters of piece p, kept as planes of float4 so that neighbouring threads read neighbouring 16 bytes.
+template <int VEC>
+__device__ __forceinline__ void join_params(uint32_t base, int p, int pieces, float (&v)[VEC]) {
+#pragma unroll
+    for (int j = 0; j < VEC / 4; ++j) {
+        const uint4 w = ptx::lds128(base + (j * pieces + p) * 16);
+        v[4 * j] = __uint_as_float(w.x); v[4 * j + 1] = __uint_as_float(w.y);
+        v[4 * j + 2] = __uint_as_float(w.z); v[4 * j + 3] = __uint_as_float(w.w);
+    }
+}
+
+// Sums over a group's warps in a fixed order.  `red`: two sets of V * 32 floats per group, used in turn, so that
+// one barrier per sum suffices.
+struct GroupSum {
+    float* red; int warps, warp, bar, threads, turn;
+    template <int V>
+    __device__ __forceinline__ void operator()(float (&v)[V]) {
+#pragma unroll
+        for (int i = 0; i < V; ++i) v[i] = warp_sum(v[i]);
+        if (warps == 1) return;
+        float* r = red + turn * V * 32;
+        turn ^= 1;
+        if ((threadIdx.x & 31) == 0) {
+#pragma unroll
+            for (int i = 0; i < V; ++i) r[i * 32 + warp] = v[i];
+        }
+        asm volatile("bar.sync %0, %1;" ::"r"(bar), "r"(threads) : "memory");
+#pragma unroll
+        for (int i = 0; i < V; ++i) v[i] = 0;
+        for (int w = 0; w < warps; ++w) {
+#pragma unroll
+            for (int i = 0; i < V; ++i) v[i] += r[i * 32 + w];
+        }
+    }
+};
+constexpr int kJoinRedBytes = 20 * 2 * 3 * 32 * 4;        // 20 groups
+
+// What both passes set up: this thread's group, columns, ring and the parameters in shared memory.
+template <class T, int E, int IN>
+struct JoinThread {
+    static constexpr int VEC = Join<T>::VEC, CH = E / VEC;
+    int t, group, pieces;
+    JoinColumns<T, E> k;
+    uint32_t ring, post, pre;
+    int64_t row, step;                                    // first row, rows between two of this group
+    GroupSum sum;
+
+    __device__ __forceinline__ JoinThread(const JoinArgs& a, uint8_t* smem) {
+        group = int(threadIdx.x) / a.T;
+        t = int(threadIdx.x) % a.T;
+        pieces = a.T * CH;
+        row = int64_t(blockIdx.x) + int64_t(group) * gridDim.x;
+        step = int64_t(a.groups) * gridDim.x;
+        const uintptr_t start = reinterpret_cast<uintptr_t>(a.in[kZ]) / sizeof(T);
+        const int shift = int((start + uint64_t(row) * uint64_t(a.shift_step)) % VEC);
+        k.first = t * VEC - shift;
+        k.step = a.T * VEC;
+        k.N = a.N;
+        float* red = reinterpret_cast<float*>(smem);
+        sum = GroupSum{red + group * 2 * 3 * 32, a.T / 32, t / 32, a.groups == 1 ? 0 : group + 1, a.T, 0};
+        post = ptx::smem_addr(smem) + kJoinRedBytes;
+        pre = post + uint32_t(pieces) * VEC * 4;
+        ring = pre + uint32_t(pieces) * VEC * 4 + uint32_t(group * a.stages * a.arrays) * uint32_t(pieces) * 16;
+    }
+    __device__ __forceinline__ uint32_t at(const JoinArgs& a, int stage, int m, int c) const {
+        return ring + (uint32_t((stage * a.arrays + a.slot[m]) * CH + c) * uint32_t(a.T) + uint32_t(t)) * 16;
+    }
+    // Starts the copies of row r; always one group of copies, so that waits can count them.
+    __device__ __forceinline__ void fetch(const JoinArgs& a, int64_t r, int stage) const {
+        if (r < a.M) {
+#pragma unroll
+            for (int m = 0; m < IN; ++m) {
+                if (!a.in[m]) continue;
+                const T* p = static_cast<const T*>(a.in[m]) + r * a.ld[m];
+#pragma unroll
+                for (int c = 0; c < CH; ++c)
+                    if (k.any(c)) copy16(at(a, stage, m, c), p + k.col(c));
+            }
+        }
+        copy_commit();
+    }
+    // The block's parameters: gate row * gamma_post, gamma_pre; 0 outside the row.
+    __device__ __forceinline__ void params(const JoinArgs& a, uint8_t* smem) const {
+        float* q = reinterpret_cast<float*>(smem + kJoinRedBytes);
+        const int shift = t * VEC - k.first;
+        for (int e = int(threadIdx.x); e < pieces * VEC; e += int(blockDim.x)) {
+            const int col = e - shift, at = (e % VEC / 4 * pieces + e / VEC) * 4 + e % 4;
+            const bool in = unsigned(col) < unsigned(a.N);
+            q[at] = in ? param(a.gate_row, col, a.p32) * param(a.gamma_post, col, a.p32) : 0.f;
+            q[at + pieces * VEC] = in ? param(a.gamma_pre, col, a.p32) : 0.f;
+        }
+    }
+};
+
+template <class T, int E>
+__global__ void __launch_bounds__(E <= 16 ? 1024 : kJoinThreads, 1) join_fwd_kernel(const __grid_constant__ JoinArgs a) {
+    extern __shared__ __align__(16) uint8_t smem[];
+    typedef JoinThread<T, E, kFwdIn> Thread;
+    constexpr int VEC = Thread::VEC, CH = Thread::CH;
+    Thread th(a, smem);
+    pdl_launch();
+    pdl_wait();
+    for (int s = 0; s < a.stages; ++s) th.fetch(a, th.row + s * th.step, s);
+    th.params(a, smem);
+    __syncthreads();
+    const bool post = a.norms & TPPO_NORM_POST, pre = a.norms & TPPO_NORM_PRE, gated = a.in[kGate] != nullptr;
+    const float inv = 1.f / float(a.N);
+    int stage = 0;
+    for (int64_t r = th.row; r < a.M; r += th.step) {
+        copy_wait(a.stages);
+        float r1 = 1.f, s[1] = {0.f};
+        bool good = true;
+        if (post) {
+#pragma unroll
+            for (int c = 0; c < CH; ++c) {
+                if (!th.k.any(c)) continue;
+                float z[VEC];
+                join_piece<T>(th.k, c, th.at(a, stage, kZ, c), z);
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) s[0] = fmaf(z[i], z[i], s[0]);
+            }
+            th.sum(s);
+            r1 = rsqrtf(fmaf(s[0], inv, a.eps));
+            good = is_finite(s[0]) && is_finite(r1);
+        }
+        float h[CH][VEC];
+        s[0] = 0;
+#pragma unroll
+        for (int c = 0; c < CH; ++c) {
+            if (!th.k.any(c)) continue;
+            float z[VEC], g[VEC];
+            join_piece<T>(th.k, c, th.at(a, stage, kZ, c), z);
+            join_piece<T>(th.k, c, th.at(a, stage, kRes, c), h[c]);
+            join_params<VEC>(th.post, c * a.T + th.t, th.pieces, g);
+            if (gated) {
+                float w[VEC];
+                join_piece<T>(th.k, c, th.at(a, stage, kGate, c), w);
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) g[i] *= w[i];
+            }
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) {
+                h[c][i] = fmaf(z[i] * r1, g[i], a.alpha * h[c][i]);
+                s[0] = pre ? fmaf(h[c][i], h[c][i], s[0]) : s[0] + fabsf(h[c][i]);
+            }
+        }
+        th.fetch(a, r + a.stages * th.step, stage);
+        if (++stage == a.stages) stage = 0;
+        th.sum(s);
+        const float r2 = pre ? rsqrtf(fmaf(s[0], inv, a.eps)) : 1.f;
+        good = good && is_finite(s[0]) && is_finite(r2);
+        if (th.t == 0) {
+            if (a.r_post) a.r_post[r] = good ? r1 : 0.f;
+            if (a.r_pre) a.r_pre[r] = good ? r2 : 0.f;
+            if (!good && a.status) atomicOr(a.status, TPPO_DEV_NONFINITE);
+        }
+        T* ho = static_cast<T*>(a.out[0]) + r * a.ldo[0];
+        T* no = static_cast<T*>(a.out[1]) + (pre ? r * a.ldo[1] : 0);
+#pragma unroll
+        for (int c = 0; c < CH; ++c) {
+            if (!th.k.any(c)) continue;
+            if (!good) {
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) h[c][i] = 0;
+            }
+            join_store<T>(th.k, c, ho, h[c]);
+            if (pre) {
+                float g[VEC];
+                join_params<VEC>(th.pre, c * a.T + th.t, th.pieces, g);
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) g[i] = good ? h[c][i] * r2 * g[i] : 0.f;
+                join_store<T>(th.k, c, no, g);
+            }
+        }
+    }
+}
+
+// The scalars of a row's backward pass, from its three sums.
+struct JoinRow { float r1, r2, k2, k1; bool good; };
+__device__ __forceinline__ JoinRow join_row(const JoinArgs& a, float r1, float r2, const float (&s)[3]) {
+    const bool post = a.norms & TPPO_NORM_POST, pre = a.norms & TPPO_NORM_PRE;
+    const float inv = 1.f / float(a.N);
+    JoinRow w;
+    w.r1 = post ? r1 : 1.f;
+    w.r2 = pre ? r2 : 0.f;
+    w.k2 = pre ? s[0] * inv * r2 * r2 * r2 : 0.f;                         // d = dh + r2 a2 - k2 h
+    w.k1 = post ? (s[1] - w.k2 * s[2]) * inv * r1 * r1 * r1 : 0.f;        // dz = r1 a1 - k1 z
+    const bool stats = !((post && r1 == 0.f) || (pre && r2 == 0.f));
+    w.good = is_finite(s[0]) && is_finite(s[1]) && is_finite(s[2]) && is_finite(w.k2) && is_finite(w.k1);
+    if (!w.good && stats && threadIdx.x % a.T == 0 && a.status) atomicOr(a.status, TPPO_DEV_NONFINITE);
+    w.good = w.good && stats;
+    return w;
+}
+
+template <class T, int E>
+__global__ void __launch_bounds__(kJoinThreads, 1) join_bwd_kernel(const __grid_constant__ JoinArgs a) {
+    extern __shared__ __align__(16) uint8_t smem[];
+    typedef JoinThread<T, E, kBwdIn> Thread;
+    constexpr int VEC = Thread::VEC, CH = Thread::CH;
+    Thread th(a, smem);
+    pdl_launch();
+    pdl_wait();
+    for (int s = 0; s < a.stages; ++s) th.fetch(a, th.row + s * th.step, s);
+    th.params(a, smem);
+    __syncthreads();
+    const bool pre = a.norms & TPPO_NORM_PRE, gated = a.in[kGate] != nullptr, add = a.in[kDh] != nullptr;
+    float sum_post[CH][VEC], sum_pre[CH][VEC];
+#pragma unroll
+    for (int c = 0; c < CH; ++c)
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) sum_post[c][i] = sum_pre[c][i] = 0;
+    int stage = 0;
+    const bool post = a.norms & TPPO_NORM_POST;
+    float r1_next = post && th.row < a.M ? a.r_post[th.row] : 1.f, r2_next = pre && th.row < a.M ? a.r_pre[th.row] : 0.f;
+    for (int64_t r = th.row; r < a.M; r += th.step) {
+        const float r1 = r1_next, r2 = r2_next;
+        if (r + th.step < a.M) {                          // a row ahead, like the copies
+            if (post) r1_next = a.r_post[r + th.step];
+            if (pre) r2_next = a.r_pre[r + th.step];
+        }
+        copy_wait(a.stages);
+        float s[3] = {0.f, 0.f, 0.f};
+#pragma unroll
+        for (int c = 0; c < CH; ++c) {
+            if (!th.k.any(c)) continue;
+            float w[VEC], d[VEC], g[VEC];
+            join_piece<T>(th.k, c, th.at(a, stage, kZ, c), w);
+            join_params<VEC>(th.post, c * a.T + th.t, th.pieces, g);
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) w[i] *= g[i];
+            if (gated) {
+                join_piece<T>(th.k, c, th.at(a, stage, kGate, c), g);
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) w[i] *= g[i];
+            }
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) d[i] = 0;
+            if (add) join_piece<T>(th.k, c, th.at(a, stage, kDh, c), d);
+            if (pre) {
+                float n[VEC], h[VEC];
+                join_piece<T>(th.k, c, th.at(a, stage, kDn, c), n);
+                join_piece<T>(th.k, c, th.at(a, stage, kH, c), h);
+                join_params<VEC>(th.pre, c * a.T + th.t, th.pieces, g);
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) {
+                    const float a2 = n[i] * g[i];
+                    s[0] = fmaf(a2, h[i], s[0]);
+                    s[2] = fmaf(h[i], w[i], s[2]);
+                    d[i] = fmaf(r2, a2, d[i]);
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) s[1] = fmaf(d[i], w[i], s[1]);
+        }
+        th.sum(s);
+        const JoinRow w = join_row(a, r1, r2, s);
+        T* dz = static_cast<T*>(a.out[0]) + (a.out[0] ? r * a.ldo[0] : 0);
+        T* dres = static_cast<T*>(a.out[1]) + (a.out[1] ? r * a.ldo[1] : 0);
+        T* dgate = static_cast<T*>(a.out[2]) + (a.out[2] ? r * a.ldo[2] : 0);
+#pragma unroll
+        for (int c = 0; c < CH; ++c) {
+            if (!th.k.any(c)) continue;
+            float z[VEC], d[VEC], g[VEC], v[VEC];
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) d[i] = 0;
+            if (add) join_piece<T>(th.k, c, th.at(a, stage, kDh, c), d);
+            if (pre) {
+                float n[VEC], h[VEC];
+                join_piece<T>(th.k, c, th.at(a, stage, kDn, c), n);
+                join_piece<T>(th.k, c, th.at(a, stage, kH, c), h);
+                join_params<VEC>(th.pre, c * a.T + th.t, th.pieces, g);
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) {
+                    if (w.good) sum_pre[c][i] = fmaf(n[i], h[i] * w.r2, sum_pre[c][i]);
+                    d[i] = fmaf(-w.k2, h[i], fmaf(w.r2, n[i] * g[i], d[i]));
+                }
+            }
+            if (a.out[1]) {
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) v[i] = w.good ? a.alpha * d[i] : 0.f;
+                join_store<T>(th.k, c, dres, v);
+            }
+            join_piece<T>(th.k, c, th.at(a, stage, kZ, c), z);
+            join_params<VEC>(th.post, c * a.T + th.t, th.pieces, g);
+            if (gated) {
+                join_piece<T>(th.k, c, th.at(a, stage, kGate, c), v);
+                if (a.out[2]) {
+                    float o[VEC];
+#pragma unroll
+                    for (int i = 0; i < VEC; ++i) o[i] = w.good ? d[i] * (z[i] * w.r1) * g[i] : 0.f;
+                    join_store<T>(th.k, c, dgate, o);
+                }
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) d[i] *= v[i];
+            }
+            if (w.good) {
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) sum_post[c][i] = fmaf(d[i], z[i] * w.r1, sum_post[c][i]);
+            }
+            if (a.out[0]) {
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) v[i] = w.good ? fmaf(-w.k1, z[i], w.r1 * (d[i] * g[i])) : 0.f;
+                join_store<T>(th.k, c, dz, v);
+            }
+        }
+        th.fetch(a, r + a.stages * th.step, stage);
+        if (++stage == a.stages) stage = 0;
+    }
+    if (!a.partial) return;
+    // the groups' sums meet in the ring's memory: group 0 adds the others' to its own, in order
+    asm volatile("cp.async.wait_group 0;" ::: "memory");
+    __syncthreads();
+    float* all = reinterpret_cast<float*>(smem + kJoinRedBytes);           // [group][2 * E][T]
+    if (th.group > 0) {
+#pragma unroll
+        for (int c = 0; c < CH; ++c)
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) {
+                all[((th.group - 1) * 2 * E + c * VEC + i) * a.T + th.t] = sum_post[c][i];
+                all[((th.group - 1) * 2 * E + E + c * VEC + i) * a.T + th.t] = sum_pre[c][i];
+            }
+    }
+    __syncthreads();
+    if (th.group > 0) return;
+    float* part = a.partial + int64_t(blockIdx.x) * 2 * a.N;
+#pragma unroll
+    for (int c = 0; c < CH; ++c)
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) {
+            for (int g = 1; g < a.groups; ++g) {
+                sum_post[c][i] += all[((g - 1) * 2 * E + c * VEC + i) * a.T + th.t];
+                sum_pre[c][i] += all[((g - 1) * 2 * E + E + c * VEC + i) * a.T + th.t];
+            }
+            if (th.k.has(c, i)) {
+                part[th.k.col(c) + i] = sum_post[c][i];
+                part[int64_t(a.N) + th.k.col(c) + i] = sum_pre[c][i];
+            }
+        }
+}
+
+// ---- any length and alignment: one block per row, swept once per sum -----------------------------------------
+template <int V>
+__device__ __forceinline__ void block_sums(float (&v)[V], float* red) {
+#pragma unroll
+    for (int i = 0; i < V; ++i) v[i] = warp_sum(v[i]);
+    __syncthreads();                                      // the previous sums have been read
+    if ((threadIdx.x & 31) == 0) {
+#pragma unroll
+        for (int i = 0; i < V; ++i) red[i * 32 + (threadIdx.x >> 5)] = v[i];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+        v[i] = 0;
+        for (int w = 0; w < kJoinAnyThreads / 32; ++w) v[i] += red[i * 32 + w];
+    }
+}
+
+template <class T>
+__global__ void __launch_bounds__(kJoinAnyThreads) join_fwd_any_kernel(const __grid_constant__ JoinArgs a) {
+    __shared__ float red[32];
+    pdl_launch();
+    pdl_wait();
+    const bool post = a.norms & TPPO_NORM_POST, pre = a.norms & TPPO_NORM_PRE;
+    const float inv = 1.f / float(a.N);
+    for (int64_t r = blockIdx.x; r < a.M; r += gridDim.x) {
+        const T* z = static_cast<const T*>(a.in[kZ]) + r * a.ld[kZ];
+        const T* res = static_cast<const T*>(a.in[kRes]) + r * a.ld[kRes];
+        const T* gate = a.in[kGate] ? static_cast<const T*>(a.in[kGate]) + r * a.ld[kGate] : nullptr;
+        T* ho = static_cast<T*>(a.out[0]) + r * a.ldo[0];
+        T* no = pre ? static_cast<T*>(a.out[1]) + r * a.ldo[1] : nullptr;
+        float r1 = 1.f, s[1] = {0.f};
+        bool good = true;
+        if (post) {
+#pragma unroll 4
+            for (int c = threadIdx.x; c < a.N; c += kJoinAnyThreads) s[0] = fmaf(load_f32(z + c), load_f32(z + c), s[0]);
+            block_sums(s, red);
+            r1 = rsqrtf(fmaf(s[0], inv, a.eps));
+            good = is_finite(s[0]) && is_finite(r1);
+        }
+        auto join = [&](int c) {
+            float g = param(a.gate_row, c, a.p32) * param(a.gamma_post, c, a.p32);
+            if (gate) g *= load_f32(gate + c);
+            return fmaf(load_f32(z + c) * r1, g, a.alpha * load_f32(res + c));
+        };
+        s[0] = 0;
+#pragma unroll 4
+        for (int c = threadIdx.x; c < a.N; c += kJoinAnyThreads) {
+            const float h = join(c);
+            s[0] = pre ? fmaf(h, h, s[0]) : s[0] + fabsf(h);
+        }
+        block_sums(s, red);
+        const float r2 = pre ? rsqrtf(fmaf(s[0], inv, a.eps)) : 1.f;
+        good = good && is_finite(s[0]) && is_finite(r2);
+        if (threadIdx.x == 0) {
+            if (a.r_post) a.r_post[r] = good ? r1 : 0.f;
+            if (a.r_pre) a.r_pre[r] = good ? r2 : 0.f;
+            if (!good && a.status) atomicOr(a.status, TPPO_DEV_NONFINITE);
+        }
+        // h or n may be z or residual: an element is read before it is written, by the same thread
+#pragma unroll 4
+        for (int c = threadIdx.x; c < a.N; c += kJoinAnyThreads) {
+            const float h = join(c);
+            store_f32(ho + c, good ? h : 0.f);
+            if (pre) store_f32(no + c, good ? h * r2 * param(a.gamma_pre, c, a.p32) : 0.f);
+        }
+    }
+}
+
+template <class T>
+__global__ void __launch_bounds__(kJoinAnyThreads) join_bwd_any_kernel(const __grid_constant__ JoinArgs a) {
+    __shared__ float red[3 * 32];
+    pdl_launch();
+    pdl_wait();
+    const bool pre = a.norms & TPPO_NORM_PRE;
+    float* part = a.partial ? a.partial + int64_t(blockIdx.x) * 2 * a.N : nullptr;
+    for (int64_t r = blockIdx.x; r < a.M; r += gridDim.x) {
+        const T* z = static_cast<const T*>(a.in[kZ]) + r * a.ld[kZ];
+        const T* h = pre ? static_cast<const T*>(a.in[kH]) + r * a.ld[kH] : nullptr;
+        const T* dn = pre ? static_cast<const T*>(a.in[kDn]) + r * a.ld[kDn] : nullptr;
+        const T* dh = a.in[kDh] ? static_cast<const T*>(a.in[kDh]) + r * a.ld[kDh] : nullptr;
+        const T* gate = a.in[kGate] ? static_cast<const T*>(a.in[kGate]) + r * a.ld[kGate] : nullptr;
+        const float r1 = a.r_post ? a.r_post[r] : 1.f, r2 = a.r_pre ? a.r_pre[r] : 0.f;
+        float s[3] = {0.f, 0.f, 0.f};
+#pragma unroll 2
+        for (int c = threadIdx.x; c < a.N; c += kJoinAnyThreads) {
+            float g = param(a.gate_row, c, a.p32) * param(a.gamma_post, c, a.p32);
+            if (gate) g *= load_f32(gate + c);
+            const float w = load_f32(z + c) * g;
+            float d = dh ? load_f32(dh + c) : 0.f;
+            if (pre) {
+                const float a2 = load_f32(dn + c) * param(a.gamma_pre, c, a.p32), hv = load_f32(h + c);
+                s[0] = fmaf(a2, hv, s[0]);
+                s[2] = fmaf(hv, w, s[2]);
+                d = fmaf(r2, a2, d);
+            }
+            s[1] = fmaf(d, w, s[1]);
+        }
+        block_sums(s, red);
+        const JoinRow w = join_row(a, r1, r2, s);
+#pragma unroll 2
+        for (int c = threadIdx.x; c < a.N; c += kJoinAnyThreads) {
+            const float zv = load_f32(z + c), gp = param(a.gamma_post, c, a.p32), gr = param(a.gate_row, c, a.p32);
+            const float gv = gate ? load_f32(gate + c) : 1.f;
+            float d = dh ? load_f32(dh + c) : 0.f, tp = 0.f;
+            if (pre) {
+                const float nv = load_f32(dn + c), hv = load_f32(h + c);
+                tp = nv * (hv * w.r2);
+                d = fmaf(-w.k2, hv, fmaf(w.r2, nv * param(a.gamma_pre, c, a.p32), d));
+            }
+            const float g = gr * gp;
+            if (a.out[1]) store_f32(static_cast<T*>(a.out[1]) + r * a.ldo[1] + c, w.good ? a.alpha * d : 0.f);
+            if (a.out[2]) store_f32(static_cast<T*>(a.out[2]) + r * a.ldo[2] + c, w.good ? d * (zv * w.r1) * g : 0.f);
+            d *= gv;
+            if (a.out[0]) store_f32(static_cast<T*>(a.out[0]) + r * a.ldo[0] + c, w.good ? fmaf(-w.k1, zv, w.r1 * (d * g)) : 0.f);
+            if (part) {                                   // this block's own sums: a thread always has the same columns
+                const float sp = w.good ? d * (zv * w.r1) : 0.f;
+                const bool first = r == blockIdx.x;
+                part[c] = first ? sp : part[c] + sp;
+                part[int64_t(a.N) + c] = first ? (w.good ? tp : 0.f) : part[int64_t(a.N) + c] + (w.good ? tp : 0.f);
+            }
+        }
+    }
+}
+
+// Adds the blocks' partial rows up in a fixed order (eight strands of them) and finishes the gradients:
+//     dgamma_post = gate row * S, dgate row = gamma_post * S, dgamma_pre = the second sum.
+struct JoinSumArgs {
+    const float* partial; int64_t rows; int32_t N;
+    const void* gate_row; const void* gamma_post;
+    void* dgate_row; void* dgamma_post; void* dgamma_pre; int32_t p32;
+};
+__global__ void __launch_bounds__(256) join_sum_kernel(const JoinSumArgs a) {
+    __shared__ float red[8][32];
+    pdl_launch();
+    pdl_wait();
+    const int lane = threadIdx.x & 31, strand = threadIdx.x >> 5;
+    const int64_t col = int64_t(blockIdx.x) * 32 + lane, all = int64_t(2) * a.N;
+    float v = 0;
+    if (col < all) {
+#pragma unroll 8
+        for (int64_t r = strand; r < a.rows; r += 8) v += __ldcg(a.partial + r * all + col);
+    }
+    red[strand][lane] = v;
+    __syncthreads();
+    if (strand != 0 || col >= all) return;
+    for (int i = 1; i < 8; ++i) v += red[i][lane];
+    if (col < a.N) {
+        if (a.dgamma_post) put_param(a.dgamma_post, col, a.p32, v * param(a.gate_row, col, a.p32));
+        if (a.dgate_row) put_param(a.dgate_row, col, a.p32, v * param(a.gamma_post, col, a.p32));
+    } else if (a.dgamma_pre) {
+        put_param(a.dgamma_pre, col - a.N, a.p32, v);
+    }
+}
+
+// ---- host side --------------------------------------------------------------------------------------------------
+struct JoinPlan { int E = 0, grid = 0; size_t smem = 0; };        // E = 0: the kernels for any row
+
+// Groups, stages and elements per thread of the ring kernels.  `most`: elements a thread can hold; `count`: matrices.
+//   Many rows: as few threads per row as hold it (a barrier of four warps is cheaper than one of sixteen, and more
+//   rows are on their way at once), and as many groups as leave two stages each.
+//   Few rows: all of a block's threads for one row.
+// Rows that start at changing places of a piece come in classes; a grid of a multiple of eight keeps a block in one.
+JoinPlan join_plan(JoinArgs& a, const int* elements, int kinds, int vec, bool fwd) {
+    JoinPlan p;
+    const bool shifts = a.shift_step % vec != 0 || reinterpret_cast<uintptr_t>(a.in[kZ]) % 16 != 0;
+    const int64_t pieces = (int64_t(a.N) + (shifts ? vec - 1 : 0) + vec - 1) / vec;
+    const int most = elements[kinds - 1];
+    if (pieces * vec > int64_t(kJoinThreads) * most) return p;
+    const int width = int(pieces) * vec;
+    a.T = (width + 32 * most - 1) / (32 * most) * 32;
+    int groups = kJoinThreads / a.T;
+    if (a.T > 32 && groups > 15) groups = 15;             // hardware barriers
+    if (a.M < int64_t(kNumSms) * groups) {
+        groups = int((a.M + kNumSms - 1) / kNumSms);
+        const int wide = kJoinThreads / groups / 32 * 32, enough = (width + 32 * elements[0] - 1) / (32 * elements[0]) * 32;
+        if (wide > a.T) a.T = wide < enough ? wide : enough;
+        if (a.T > 32 && groups > 15) groups = 15;
+    }
+    for (int i = kinds - 1; i >= 0; --i)
+        if (int64_t(a.T) * elements[i] >= width) p.E = elements[i];
+    const int64_t row = int64_t(a.T) * p.E / vec * 16;    // bytes of a matrix' row in a stage
+    const int64_t params = int64_t(a.T) * p.E * 8 + kJoinRedBytes;
+    const int64_t slots = (kJoinSmem - params) / (row * a.arrays);
+    if (slots < 1) { p.E = 0; return p; }
+    if (groups > 1 && groups > slots / 2) groups = slots / 2 > 1 ? int(slots / 2) : 1;
+    a.groups = groups;
+    a.stages = int(slots / groups < kJoinStages ? slots / groups : kJoinStages);
+    int64_t blocks = (a.M + groups - 1) / groups;
+    if (blocks > kNumSms) blocks = kNumSms;
+    if (a.shift_step % vec != 0) blocks = blocks <= 144 ? (blocks + 7) / 8 * 8 : 144;
+    p.grid = int(blocks);
+    const int64_t sums = fwd ? 0 : int64_t(groups - 1) * a.T * p.E * 8 + kJoinRedBytes;
+    const int64_t ring = params + row * a.arrays * a.groups * a.stages;
+    p.smem = size_t(ring > sums ? ring : sums);
+    return p;
+}
+
+template <class T, int E>
+int launch_fwd(const JoinArgs& a, const JoinPlan& p, cudaStream_t s) {
+    TPPO_CUDA_CHECK(cudaFuncSetAttribute(join_fwd_kernel<T, E>, cudaFuncAttributeMaxDynamicSharedMemorySize, kJoinSmem));
+    TPPO_CUDA_CHECK(launch_dense(join_fwd_kernel<T, E>, dim3(p.grid), dim3(a.T * a.groups), p.smem, s, a));
+    return TPPO_OK;
+}
+template <class T, int E>
+int launch_bwd(const JoinArgs& a, const JoinPlan& p, cudaStream_t s) {
+    TPPO_CUDA_CHECK(cudaFuncSetAttribute(join_bwd_kernel<T, E>, cudaFuncAttributeMaxDynamicSharedMemorySize, kJoinSmem));
+    TPPO_CUDA_CHECK(launch_dense(join_bwd_kernel<T, E>, dim3(p.grid), dim3(a.T * a.groups), p.smem, s, a));
+    return TPPO_OK;
+}
+
+template <class T>
+int run_fwd(JoinArgs& a, bool same, cudaStream_t s) {
+    static const int kinds[5] = {8, 16, 24, 40, 48};
+    const JoinPlan p = same ? join_plan(a, kinds, 5, Join<T>::VEC, true) : JoinPlan{};
+    switch (p.E) {
+        case 8: return launch_fwd<T, 8>(a, p, s);
+        case 16: return launch_fwd<T, 16>(a, p, s);
+        case 24: return launch_fwd<T, 24>(a, p, s);
+        case 40: return launch_fwd<T, 40>(a, p, s);
+        case 48: return launch_fwd<T, 48>(a, p, s);
+    }
+    const int grid = int(a.M < kJoinAnyBlocks ? a.M : kJoinAnyBlocks);
+    a.T = kJoinAnyThreads;
+    TPPO_CUDA_CHECK(launch_dense(join_fwd_any_kernel<T>, dim3(grid), dim3(kJoinAnyThreads), 0, s, a));
+    return TPPO_OK;
+}
+
+template <class T>
+int run_bwd(JoinArgs& a, bool same, JoinSumArgs& sum, cudaStream_t s) {
+    static const int kinds[2] = {8, 16};
+    const JoinPlan p = same ? join_plan(a, kinds, 2, Join<T>::VEC, false) : JoinPlan{};
+    int r = TPPO_OK;
+    if (p.E) {
+        sum.rows = p.grid;
+        r = p.E == 8 ? launch_bwd<T, 8>(a, p, s) : launch_bwd<T, 16>(a, p, s);
+    } else {
+        const int grid = int(a.M < kJoinAnyBlocks ? a.M : kJoinAnyBlocks);
+        a.T = kJoinAnyThreads;
+        sum.rows = grid;
+        TPPO_CUDA_CHECK(launch_dense(join_bwd_any_kernel<T>, dim3(grid), dim3(kJoinAnyThreads), 0, s, a));
+    }
+    return r;
+}
+
+bool type_ok(int32_t t) { return t == TPPO_BF16 || t == TPPO_F32; }
+size_t size_of(int32_t t) { return t == TPPO_F32 ? 4 : 2; }
+
+// Whether the rows of two matrices start at the same place of a 16-byte piece, row by row.
+bool same_start(const void* p, int64_t ldp, const void* q, int64_t ldq, size_t e) {
+    if (!p || !q) return true;
+    return (reinterpret_cast<uintptr_t>(p) - reinterpret_cast<uintptr_t>(q)) % 16 == 0 && ((ldp - ldq) * int64_t(e)) % 16 == 0;
+}
+
+}  // namespace
+
+size_t residual_norm_workspace_bytes(int64_t M, int32_t N) {
+    if (N <= 0) return 0;
+    const int64_t rows = M < kJoinAnyBlocks ? (M + 7) / 8 * 8 : kJoinAnyBlocks;
+    return align_up(size_t(rows > 0 ? rows : 1) * 2 * size_t(N) * sizeof(float), kWsAlign);
+}
+
+}  // namespace tppo
+
+TPPO_API int tppo_residual_norm_fwd(const void* z, int64_t ldz, const void* residual, int64_t ldr, const void* gate, int64_t ldg,
+                                    int32_t dtype, int64_t M, int32_t N, const void* gamma_post, const void* gamma_pre,
+                                    int32_t param_dtype, float alpha, float eps, int32_t norms, void* h, int64_t ldh, void* n, int64_t ldn,
+                                    float* rstd_post, float* rstd_pre, int32_t* status, void* stream) {
+    using namespace tppo;
+    if (M < 0 || N < 1 || !type_ok(dtype) || !type_ok(param_dtype) || (norms & ~3) || !is_finite_host(alpha) || !(eps >= 0.f) ||
+        !is_finite_host(eps))
+        return TPPO_ERR_INVALID_ARG;
+    const bool post = norms & TPPO_NORM_POST, pre = norms & TPPO_NORM_PRE;
+    const bool full = gate && ldg != 0;
+    if ((n != nullptr) != pre && M > 0) return TPPO_ERR_INVALID_ARG;
+    if ((gamma_post && !post) || (gamma_pre && !pre) || (rstd_post && !post) || (rstd_pre && !pre)) return TPPO_ERR_INVALID_ARG;
+    if (ldz < N || ldr < N || ldh < N || (pre && ldn < N) || (full && ldg < N)) return TPPO_ERR_INVALID_ARG;
+    const size_t e = size_of(dtype), pe = size_of(param_dtype);
+    if (!aligned(z, e) || !aligned(residual, e) || !aligned(h, e) || !aligned(n, e) || !aligned(gate, full ? e : pe) ||
+        !aligned(gamma_post, pe) || !aligned(gamma_pre, pe) || !aligned(rstd_post, 4) || !aligned(rstd_pre, 4) || !aligned(status, 4))
+        return TPPO_ERR_INVALID_ARG;
+    if (M > 0 && (!z || !residual || !h)) return TPPO_ERR_INVALID_ARG;
+    if (M > kDenseMaxSize || N > kDenseMaxSize) return TPPO_ERR_UNSUPPORTED;
+    if (M == 0) return TPPO_OK;
+    JoinArgs a{};
+    a.in[kZ] = z; a.in[kRes] = residual; a.in[kGate] = full ? gate : nullptr;
+    a.ld[kZ] = ldz; a.ld[kRes] = ldr; a.ld[kGate] = ldg;
+    a.slot[kRes] = 1; a.slot[kGate] = 2;
+    a.arrays = full ? 3 : 2;
+    a.gate_row = full ? nullptr : gate;
+    a.gamma_post = gamma_post; a.gamma_pre = gamma_pre; a.p32 = param_dtype == TPPO_F32;
+    a.out[0] = h; a.out[1] = n; a.ldo[0] = ldh; a.ldo[1] = ldn;
+    a.r_post = rstd_post; a.r_pre = rstd_pre; a.status = status;
+    a.M = M; a.N = N; a.alpha = alpha; a.eps = eps; a.norms = norms;
+    a.shift_step = int32_t(ldz % 16);
+    const bool same = same_start(z, ldz, residual, ldr, e) && same_start(z, ldz, a.in[kGate], ldg, e) && same_start(z, ldz, h, ldh, e) &&
+                      same_start(z, ldz, n, ldn, e);
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    return dtype == TPPO_F32 ? run_fwd<float>(a, same, s) : run_fwd<bf16_bits>(a, same, s);
+}
+
+TPPO_API int tppo_residual_norm_bwd(const void* dh, int64_t lddh, const void* dn, int64_t lddn, const void* z, int64_t ldz,
+                                    const void* h, int64_t ldh, const void* gate, int64_t ldg, int32_t dtype, int64_t M, int32_t N,
+                                    const void* gamma_post, const void* gamma_pre, int32_t param_dtype,
+                                    const float* rstd_post, const float* rstd_pre, float alpha, int32_t norms,
+                                    void* dz, int64_t lddz, void* dresidual, int64_t lddr, void* dgate, int64_t lddg,
+                                    void* dgamma_post, void* dgamma_pre, int32_t* status, void* workspace, size_t workspace_bytes,
+                                    void* stream) {
+    using namespace tppo;
+    if (M < 0 || N < 1 || !type_ok(dtype) || !type_ok(param_dtype) || (norms & ~3) || !is_finite_host(alpha)) return TPPO_ERR_INVALID_ARG;
+    const bool post = norms & TPPO_NORM_POST, pre = norms & TPPO_NORM_PRE;
+    const bool full = gate && ldg != 0;
+    if ((gamma_post && !post) || (gamma_pre && !pre) || (dgamma_post && !post) || (dgamma_pre && !pre) || (dgate && !gate))
+        return TPPO_ERR_INVALID_ARG;
+    if (M > 0 && (!z || (dn != nullptr) != pre || (h != nullptr) != pre || (rstd_post != nullptr) != post || (rstd_pre != nullptr) != pre))
+        return TPPO_ERR_INVALID_ARG;
+    if (ldz < N || (dh && lddh < N) || (pre && (lddn < N || ldh < N)) || (full && ldg < N) || (dz && lddz < N) || (dresidual && lddr < N) ||
+        (dgate && full && lddg < N))
+        return TPPO_ERR_INVALID_ARG;
+    const size_t e = size_of(dtype), pe = size_of(param_dtype);
+    if (!aligned(dh, e) || !aligned(dn, e) || !aligned(z, e) || !aligned(h, e) || !aligned(gate, full ? e : pe) || !aligned(dz, e) ||
+        !aligned(dresidual, e) || !aligned(dgate, full ? e : pe) || !aligned(gamma_post, pe) || !aligned(gamma_pre, pe) ||
+        !aligned(dgamma_post, pe) || !aligned(dgamma_pre, pe) || !aligned(rstd_post, 4) || !aligned(rstd_pre, 4) || !aligned(status, 4))
+        return TPPO_ERR_INVALID_ARG;
+    if (M > kDenseMaxSize || N > kDenseMaxSize) return TPPO_ERR_UNSUPPORTED;
+    const bool sums = dgamma_post || dgamma_pre || (dgate && !full);
+    if (sums && (!workspace || !aligned(workspace, kWsAlign) || workspace_bytes < residual_norm_workspace_bytes(M, N)))
+        return TPPO_ERR_WORKSPACE;
+    JoinArgs a{};
+    a.in[kZ] = z; a.ld[kZ] = ldz;
+    if (pre) { a.in[kH] = h; a.ld[kH] = ldh; a.in[kDn] = dn; a.ld[kDn] = lddn; }
+    if (dh) { a.in[kDh] = dh; a.ld[kDh] = lddh; }
+    if (full) { a.in[kGate] = gate; a.ld[kGate] = ldg; }
+    for (int i = 0; i < kBwdIn; ++i)
+        if (a.in[i]) a.slot[i] = a.arrays++;
+    a.gate_row = full ? nullptr : gate;
+    a.gamma_post = gamma_post; a.gamma_pre = gamma_pre; a.p32 = param_dtype == TPPO_F32;
+    a.out[0] = dz; a.out[1] = dresidual; a.out[2] = full ? dgate : nullptr;
+    a.ldo[0] = lddz; a.ldo[1] = lddr; a.ldo[2] = lddg;
+    a.r_post = const_cast<float*>(rstd_post); a.r_pre = const_cast<float*>(rstd_pre);
+    a.partial = sums ? static_cast<float*>(workspace) : nullptr;
+    a.status = status;
+    a.M = M; a.N = N; a.alpha = alpha; a.norms = norms;
+    a.shift_step = int32_t(ldz % 16);
+    bool same = true;
+    for (int i = 0; i < kBwdIn; ++i) same = same && same_start(z, ldz, a.in[i], a.ld[i], e);
+    for (int i = 0; i < 3; ++i) same = same && same_start(z, ldz, a.out[i], a.ldo[i], e);
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    JoinSumArgs sum{a.partial, 0, N, a.gate_row, gamma_post, full ? nullptr : dgate, dgamma_post, dgamma_pre, a.p32};
+    if (M > 0) {
+        const int r = dtype == TPPO_F32 ? run_bwd<float>(a, same, sum, s) : run_bwd<bf16_bits>(a, same, sum, s);
+        if (r != TPPO_OK) return r;
+    }
+    if (!sums) return TPPO_OK;
+    TPPO_CUDA_CHECK(launch_dense(join_sum_kernel, dim3(unsigned((int64_t(2) * N + 31) / 32)), dim3(256), 0, s, sum));
+    return TPPO_OK;
+}
