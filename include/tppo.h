@@ -645,8 +645,7 @@ enum {
  *   qt      [K, M] 8-bit out or NULL;  scale_t out:
  *             TPPO_FP8_ROWS    [ceil(M / 128), K] with row stride ldst
  *             TPPO_FP8_SQUARE  [ceil(K / 128), ceil(M / 128)] with row stride ldst: the transpose of scale
- * q, qt: base and row stride multiples of 16 bytes; with TPPO_FP8_ROWS scale, scale_t likewise (row strides multiples
- * of 4).  Padding between rows is not written.  An element that is not finite counts as 0 and raises TPPO_DEV_NONFINITE.
+ * q, qt: base and row stride multiples of 16 bytes (one row needs no stride).  Padding between rows is not written.  An element that is not finite counts as 0 and raises TPPO_DEV_NONFINITE.
  */
 int tppo_fp8_quantize(const void *x, int32_t dtype, int64_t ldx, int64_t M, int64_t K, int32_t block,
                       void *q, int64_t ldq, float *scale, int64_t lds,
@@ -663,9 +662,9 @@ int tppo_fp8_quantize(const void *x, int32_t dtype, int64_t ldx, int64_t M, int6
  *     x w        = product of x's q  and w's qt (TPPO_FP8_SQUARE)
  *     dy w^T     = product of dy's q and w's q  (TPPO_FP8_SQUARE)
  *     x^T dy     = product of x's qt and dy's qt (TPPO_FP8_ROWS)
- * Any fp32 scales are taken.  Sums within a block are those of the tensor cores, scaled and added up in fp32.
- * An element of y that is not finite or leaves the range of its type is written 0 and raises TPPO_DEV_NONFINITE.
- * K = 0 gives y = 0.  Alignment as for the quantiser; y may be strided at any element.  y may not overlap an input.
+ * Scales are powers of two, 2^-126 to 2^127; products and sums are those of the tensor cores, in fp32.  An element of y
+ * that is not finite, leaves the range of its type or has a scale of another kind in it is written 0 and raises
+ * TPPO_DEV_NONFINITE.  K = 0 gives y = 0.  Alignment of a and b as for the quantiser; y may be strided at any element.  y may not overlap an input.
  * The first call on a device looks up the driver's tensor-map encoder (TPPO_ERR_CUDA if absent).
  */
 int tppo_fp8_matmul(const void *a, int64_t lda, const float *a_scale, int64_t ldas,

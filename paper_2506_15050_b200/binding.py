@@ -467,7 +467,7 @@ def fp8_scales(rows, cols, block, device):
     kb = -(-cols // 128)
     if block == FP8_SQUARE:
         return torch.empty((-(-rows // 128), kb), dtype=torch.float32, device=device)
-    return torch.empty((kb, -(-rows // 4) * 4), dtype=torch.float32, device=device)[:, :rows]
+    return torch.empty((kb, rows), dtype=torch.float32, device=device)
 
 
 def _scales(t, here, rows, cols, block):

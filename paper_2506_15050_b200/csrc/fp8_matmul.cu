@@ -1,19 +1,21 @@
-// Products of 8-bit matrices with a scale per block of 128 elements of the contraction:
-//     y[m, n] = sum_b sa(b, m) sb(b, n) P_b[m, n],   P_b[m, n] = sum_{k in block b} a[m, k] b[n, k]
-// P_b comes from tcgen05.mma (kind::f8f6f4, e4m3, fp32 accumulators); it has to leave tensor memory for every
-// block, since the scales differ from block to block: eight warps read it (tcgen05.ld), scale it and add it to the
-// output tile, which they hold in registers in fp32, while the tensor cores fill the other accumulator.
+// Products of 8-bit matrices with a power-of-two scale per block of 128 elements of the contraction:
+//     y[m, n] = sum_b sa(b, m) sb(b, n) sum_{k in block b} a[m, k] b[n, k]
+// The tensor cores apply the scales: tcgen05.mma kind::mxf8f6f4 takes, beside its 8-bit operands, an 8-bit exponent per
+// operand row and 32 elements, here the same one for the four steps of a block.  Sums therefore stay in tensor memory
+// over the whole contraction, in fp32.  (With kind::f8f6f4 every block's sums have to be read, scaled and added in
+// registers: 255 instructions per warp and block, and a round trip between two kinds of warps per 512 clocks of
+// products: 16384 x 5120 x 5120 took 517 us, with a scale per column of the output 755-800.)
 //
-//   fp8_gemm_kernel   many output tiles: persistent CTAs, 128 x 256 tiles.  A block of the contraction is 512 clocks of
-//                     the tensor cores; scaling it costs a warp 128 columns: with one scale for all of them
-//                     (square blocks of b) one packed fma per two values, with a scale per column one packed
-//                     multiplication more.
+// The exponents have to lie in tensor memory: that of operand row r in lane r % 32 of column r / 32, in each of the four
+// quarters of 32 lanes; the instruction names the byte of that 32-bit cell which it uses.  Four warps write them there
+// from registers (tcgen05.st), four blocks of the contraction at a time, one per byte.  A scale that is not a power of
+// two becomes the exponent's NaN, and its outputs 0 with TPPO_DEV_NONFINITE.
+//
+//   fp8_gemm_kernel   many output tiles: persistent CTAs, 128 x 240 tiles: two accumulators, so that the output of
+//                     a tile overlaps the products of the next, and 32 columns of tensor memory for exponents.
 //   fp8_split_kernel  few output tiles (one to some hundred tokens): the output is taken TRANSPOSED, the 128 accumulator
 //                     rows running along n and the BN columns along m, and the contraction is split over the CTAs of
 //                     a cluster, whose partial sums meet in distributed shared memory in a fixed order.
-//
-// Roles of a CTA's warps: 0 TMA loads, 1 tcgen05.mma, 2-9 scaling and output.  Scales travel through a ring of their
-// own: an operand stage is free as soon as the tensor cores have read it, its scales only when the eight warps have.
 // Every wait is bounded; one that runs out raises TPPO_DEV_WAIT_TIMEOUT, outputs are then incomplete, the copies in
 // flight land and tensor memory is released.
 #include "dense_common.cuh"
@@ -22,55 +24,91 @@
 namespace tppo {
 
 bool make_u8_tensor_map(CUtensorMap* map, const void* base, uint64_t rows, uint64_t cols, uint64_t ld, uint32_t box_rows);
-bool make_f32_tensor_map(CUtensorMap* map, const void* base, uint64_t rows, uint64_t cols, uint64_t ld, uint32_t box_cols);
 
 namespace {
 
 constexpr int kF8TileM = 128, kF8Block = 128;             // accumulator rows; elements that share a scale = bytes of a swizzled row
-constexpr int kF8Threads = 320, kF8Warps = 8;
+constexpr int kF8Group = 4;                               // blocks whose exponents share a 32-bit cell
 constexpr uint32_t kF8ABytes = kF8TileM * kF8Block;
 
-// Instruction descriptor (fields as in umma::instr_desc_bf16): fp32 accumulators, both operands e4m3 (0), K-major.
-__host__ __device__ constexpr uint32_t f8_instr_desc(int n) {
-    return (1u << 4) | (uint32_t(n >> 3) << 17) | (uint32_t(kF8TileM >> 4) << 24);
+// Instruction descriptor of the block-scaled kind: both operands e4m3 (0) and K-major, N >> 3 in [17,23), exponent-only
+// scales in bit 23, M >> 4 in [24,29), the byte of the scale cells in [4,6) for B and [29,31) for A.
+__device__ __forceinline__ uint32_t f8_instr_desc(int n, int byte) {
+    return (uint32_t(byte) << 4) | (uint32_t(n >> 3) << 17) | (1u << 23) | (uint32_t(kF8TileM >> 4) << 24) | (uint32_t(byte) << 29);
 }
-// One 128 x N x 32 step, issued by one thread.
-__device__ __forceinline__ void mma_f8(uint32_t tmem_d, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
+// One 128 x N x 32 step, issued by one thread; sfa, sfb: tensor-memory addresses of the operands' scales.
+__device__ __forceinline__ void mma_f8(uint32_t tmem_d, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t sfa, uint32_t sfb,
+                                       uint32_t accumulate) {
     asm volatile(
         "{\n\t.reg .pred p;\n\t"
-        "setp.ne.b32 p, %4, 0;\n\t"
-        "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}"
-        ::"r"(tmem_d), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate) : "memory");
+        "setp.ne.b32 p, %6, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], %1, %2, %3, [%4], [%5], p;\n\t}"
+        ::"r"(tmem_d), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(sfa), "r"(sfb), "r"(accumulate) : "memory");
 }
 __device__ __forceinline__ void f8_tmem_ld8(uint32_t taddr, uint32_t (&v)[8]) {
     asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
                  : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7])
                  : "r"(taddr) : "memory");
 }
-__device__ __forceinline__ uint64_t f8_pair(uint32_t lo, uint32_t hi) { return uint64_t(lo) | uint64_t(hi) << 32; }
+__device__ __forceinline__ void f8_tmem_st4(uint32_t taddr, const uint32_t* v) {
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x4.b32 [%0], {%1, %2, %3, %4};"
+                 ::"r"(taddr), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]) : "memory");
+}
+__device__ __forceinline__ void f8_tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
-// The operand ring and the ring of scales.
-//   AROWS / BROWS: that operand has a scale per row, which the ring carries (128 / BN of them per block), each
-//   operand's on a 128-byte boundary, as tensor copies ask
-template <int BN> __host__ __device__ constexpr uint32_t f8_slot() { return kF8TileM * 4 + (BN * 4 < 128 ? 128 : BN * 4); }
-template <int BN, int STAGES, int SLOTS, bool AROWS, bool BROWS>
+// The scales of an operand: of (row, block) at p[block * by_block + (row >> shift) * by_row].
+struct F8Scales {
+    const float* p;
+    int64_t by_block, by_row;
+    int32_t shift, rows;
+};
+// The exponent byte of a scale.
+__device__ __forceinline__ uint32_t f8_exponent(float s) {
+    const uint32_t b = __float_as_uint(s), e = b >> 23;
+    return (b & 0x807fffffu) != 0 || e == 0 || e == 255 ? 0xffu : e;
+}
+// What a thread reads of a group of blocks: rows r0 + 32 c + lane of `COLS` columns of tensor memory.  Rows beyond the
+// operand and blocks beyond the contraction get 2^0; their products are 0.
+template <int COLS>
+__device__ __forceinline__ void f8_read_scales(const F8Scales& s, int r0, int kb, int k1, float (&v)[COLS][kF8Group]) {
+#pragma unroll
+    for (int c = 0; c < COLS; ++c) {
+        const int row = r0 + 32 * c + int(threadIdx.x & 31);
+        const float* p = s.p + int64_t(row >> s.shift) * s.by_row;
+#pragma unroll
+        for (int j = 0; j < kF8Group; ++j) v[c][j] = row < s.rows && kb + j < k1 ? p[(kb + j) * s.by_block] : 1.f;
+    }
+}
+template <int COLS>
+__device__ __forceinline__ void f8_write_scales(uint32_t taddr, const float (&v)[COLS][kF8Group]) {
+    static_assert(COLS % 4 == 0, "written four columns at a time");
+    uint32_t w[COLS];
+#pragma unroll
+    for (int c = 0; c < COLS; ++c)
+        w[c] = f8_exponent(v[c][0]) | f8_exponent(v[c][1]) << 8 | f8_exponent(v[c][2]) << 16 | f8_exponent(v[c][3]) << 24;
+#pragma unroll
+    for (int c = 0; c < COLS; c += 4) f8_tmem_st4(taddr + c, w + c);
+}
+
+// The rings of a CTA: operand stages in shared memory, and two sets of exponents in tensor memory (columns `sf`, A's
+// four followed by B's), each for a group of blocks.
+template <int BN, int STAGES>
 struct F8Ring {
     static constexpr uint32_t kStage = kF8ABytes + BN * kF8Block;
-    static constexpr uint32_t kSlot = f8_slot<BN>(), kScaleBytes = (AROWS ? kF8TileM * 4 : 0) + (BROWS ? BN * 4 : 0);
-    static_assert(AROWS || BROWS, "one of the operands has a scale per row");
-    uint32_t base, scales, full, empty, sfull, sempty;
-    int stage = 0, slot = 0;
-    uint32_t phase = 0, sphase = 0;
+    static constexpr int kBCols = BN <= 128 ? 4 : 8, kSet = 4 + kBCols;
+    uint32_t base, full, empty, sfull, sempty, sf;
+    int stage = 0;
+    uint32_t phase = 0, set = 0, sphase = 0;
 
     __device__ __forceinline__ void next() {
         if (++stage == STAGES) { stage = 0; phase ^= 1u; }
     }
-    __device__ __forceinline__ void next_slot() {
-        if (++slot == SLOTS) { slot = 0; sphase ^= 1u; }
+    __device__ __forceinline__ void next_set() {
+        set ^= 1u;
+        if (set == 0) sphase ^= 1u;
     }
     // Loads blocks [k0, k1) of the tile whose first A and B rows are am and bn.
-    __device__ __forceinline__ bool load(const CUtensorMap* ma, const CUtensorMap* mb, const CUtensorMap* msa, const CUtensorMap* msb,
-                                         int am, int bn, int k0, int k1) {
+    __device__ __forceinline__ bool load(const CUtensorMap* ma, const CUtensorMap* mb, int am, int bn, int k0, int k1) {
         for (int kb = k0; kb < k1; ++kb) {
             if (!ptx::mbar_wait<false>(empty + 8 * stage, phase ^ 1u)) return false;
             const uint32_t fb = full + 8 * stage, sa = base + stage * kStage;
@@ -78,12 +116,6 @@ struct F8Ring {
             umma::tma_load_2d(sa, ma, fb, kb * kF8Block, am);
             umma::tma_load_2d(sa + kF8ABytes, mb, fb, kb * kF8Block, bn);
             next();
-            if (!ptx::mbar_wait<false>(sempty + 8 * slot, sphase ^ 1u)) return false;
-            const uint32_t sb = sfull + 8 * slot, s = scales + slot * kSlot;
-            ptx::mbar_arrive_expect_tx(sb, kScaleBytes);
-            if (AROWS) umma::tma_load_2d(s, msa, sb, am, kb);
-            if (BROWS) umma::tma_load_2d(s + kF8TileM * 4, msb, sb, bn, kb);
-            next_slot();
         }
         return true;
     }
@@ -91,52 +123,52 @@ struct F8Ring {
     __device__ __forceinline__ void drain() {
         for (int s = 0; s < STAGES; ++s)
             if (!ptx::mbar_wait<false>(full + 8 * s, s < stage ? phase : phase ^ 1u)) return;
-        for (int s = 0; s < SLOTS; ++s)
-            if (!ptx::mbar_wait<false>(sfull + 8 * s, s < slot ? sphase : sphase ^ 1u)) return;
     }
-    // One block into accumulator d.
-    __device__ __forceinline__ bool multiply(uint32_t d) {
-        if (!ptx::mbar_wait<false>(full + 8 * stage, phase)) return false;
-        umma::fence_after_thread_sync();
-        const uint32_t sa = base + stage * kStage;
-        const uint64_t ad = umma::smem_desc(sa, 16, 1024), bd = umma::smem_desc(sa + kF8ABytes, 16, 1024);
+    // The exponents of blocks [k0, k1), by four warps, one per quarter of the lanes (`quarter`: the address of its first).
+    __device__ __forceinline__ bool scales(const F8Scales& a, const F8Scales& b, uint32_t quarter, int am, int bn, int k0, int k1) {
+        float va[4][kF8Group], vb[kBCols][kF8Group];
+        f8_read_scales<4>(a, am, k0, k1, va);
+        f8_read_scales<kBCols>(b, bn, k0, k1, vb);
+        for (int kb = k0; kb < k1; kb += kF8Group) {
+            if (!ptx::mbar_wait_warp<false>(sempty + 8 * set, sphase ^ 1u)) return false;
+            umma::fence_after_thread_sync();
+            f8_write_scales<4>(sf + quarter + set * kSet, va);
+            f8_write_scales<kBCols>(sf + quarter + set * kSet + 4, vb);
+            f8_tmem_st_wait();
+            umma::fence_before_thread_sync();
+            __syncwarp();
+            if ((threadIdx.x & 31) == 0) ptx::mbar_arrive(sfull + 8 * set);
+            next_set();
+            if (kb + kF8Group < k1) {                     // a group ahead
+                f8_read_scales<4>(a, am, kb + kF8Group, k1, va);
+                f8_read_scales<kBCols>(b, bn, kb + kF8Group, k1, vb);
+            }
+        }
+        return true;
+    }
+    // The products of blocks [k0, k1) into accumulator d.
+    __device__ __forceinline__ bool multiply(uint32_t d, int k0, int k1) {
+        for (int kb = k0; kb < k1; ++kb) {
+            const int byte = (kb - k0) % kF8Group;
+            if (byte == 0 && !ptx::mbar_wait<false>(sfull + 8 * set, sphase)) return false;
+            if (!ptx::mbar_wait<false>(full + 8 * stage, phase)) return false;
+            umma::fence_after_thread_sync();
+            const uint32_t sa = base + stage * kStage, sfa = sf + set * kSet, idesc = f8_instr_desc(BN, byte);
+            const uint64_t ad = umma::smem_desc(sa, 16, 1024), bd = umma::smem_desc(sa + kF8ABytes, 16, 1024);
 #pragma unroll
-        for (int j = 0; j < kF8Block / 32; ++j)
-            mma_f8(d, umma::smem_desc_advance(ad, j * 32), umma::smem_desc_advance(bd, j * 32), f8_instr_desc(BN), j != 0 ? 1u : 0u);
-        umma::mma_commit(empty + 8 * stage);
-        next();
+            for (int j = 0; j < kF8Block / 32; ++j)
+                mma_f8(d, umma::smem_desc_advance(ad, j * 32), umma::smem_desc_advance(bd, j * 32), idesc, sfa, sfa + 4,
+                       kb != k0 || j != 0 ? 1u : 0u);
+            umma::mma_commit(empty + 8 * stage);
+            next();
+            if (byte == kF8Group - 1 || kb + 1 == k1) {
+                umma::mma_commit(sempty + 8 * set);
+                next_set();
+            }
+        }
         return true;
     }
 };
-
-// A scale of square blocks: [row blocks, contraction blocks].
-struct F8Square { const float* p; int64_t ld; };
-
-// acc (COLS columns of this thread's accumulator row, as pairs) += f * column scales * the finished block at `taddr`.
-// `scales`: shared-memory address of the columns' scales, or 0: none.
-template <int COLS, bool BROWS>
-__device__ __forceinline__ void f8_scale(uint32_t taddr, float f, uint32_t scales, uint64_t (&acc)[COLS / 2]) {
-    constexpr int kChunk = COLS < 32 ? 8 : 32;
-    const uint64_t ff = ptx::pack_f32x2(f, f);
-#pragma unroll
-    for (int c = 0; c < COLS; c += kChunk) {
-        uint32_t v[kChunk];
-        if constexpr (kChunk == 32) umma::tmem_ld32(taddr + c, v);
-        else f8_tmem_ld8(taddr + c, v);
-        umma::tmem_ld_wait();
-#pragma unroll
-        for (int i = 0; i < kChunk; i += 4) {
-            uint64_t lo = f8_pair(v[i], v[i + 1]), hi = f8_pair(v[i + 2], v[i + 3]);
-            if (BROWS) {
-                const uint4 s = ptx::lds128(scales + (c + i) * 4);
-                lo = ptx::mul_f32x2(lo, f8_pair(s.x, s.y));
-                hi = ptx::mul_f32x2(hi, f8_pair(s.z, s.w));
-            }
-            acc[(c + i) / 2] = ptx::fma_f32x2(lo, ff, acc[(c + i) / 2]);
-            acc[(c + i) / 2 + 1] = ptx::fma_f32x2(hi, ff, acc[(c + i) / 2 + 1]);
-        }
-    }
-}
 
 struct F8Out {
     void* y; int64_t ldy, M; int32_t N; int32_t* status;
@@ -151,10 +183,12 @@ __device__ __forceinline__ float f8_finish(float v, bool& bad) {
 }
 
 // ---- many tiles -------------------------------------------------------------------------------------------------
-constexpr int kF8BN = 256, kF8Stages = 4, kF8Slots = 8;
-constexpr uint32_t kF8Staging = 2048;                     // per warp: 32 rows of 64 bytes
-constexpr size_t kF8Smem = size_t(kF8Stages) * (kF8ABytes + kF8BN * kF8Block) + kF8Slots * f8_slot<kF8BN>() + kF8Warps * kF8Staging +
-                           1024 /* alignment */ + 512 /* barriers */;
+constexpr int kF8BN = 240, kF8Stages = 4;
+constexpr int kF8GemmThreads = 448;                       // warps 0-3 exponents, 4-11 output, 12 TMA loads, 13 tcgen05.mma
+constexpr int kF8OutWarps = 8;
+constexpr uint32_t kF8Staging = 4096;                     // per output warp: 32 rows of 128 bytes
+constexpr size_t kF8Smem = size_t(kF8Stages) * (kF8ABytes + kF8BN * kF8Block) + kF8OutWarps * kF8Staging + 1024 /* alignment */ +
+                           128 /* barriers */;
 
 struct F8Shape { int32_t m_tiles, n_tiles, blocks, total, group_m; };
 
@@ -165,65 +199,70 @@ __device__ __forceinline__ void f8_tile(const F8Shape& g, int t, int& mt, int& n
     nt = in / gm;
 }
 
-// A warp's 32 rows by 128 columns of the output, turned through shared memory 64 bytes of each row at a time so that
-// four lanes store 64 consecutive bytes.
+// Where 16-byte piece j of row r of a warp's 32 x 128-byte staging sits.
+__device__ __forceinline__ uint32_t f8_piece(int r, int j) { return uint32_t(r * 128 + ((j ^ (r & 7)) << 4)); }
+
+// A warp's 32 rows from m0 of output columns [n0, n1), at tensor-memory address `taddr`: turned through shared memory 128
+// bytes of each row at a time, so that eight lanes store 128 consecutive bytes.
 template <class T>
-__device__ __forceinline__ void f8_store(const F8Out& o, int64_t m0, int n0, const uint64_t (&acc)[64], uint32_t sw) {
-    constexpr int kCols = 64 / int(sizeof(T)), kPer = 16 / int(sizeof(T));
+__device__ __forceinline__ void f8_store(const F8Out& o, int64_t m0, int n0, int n1, uint32_t taddr, uint32_t sw) {
+    constexpr int kCols = 128 / int(sizeof(T)), kPer = 16 / int(sizeof(T));
     const int lane = threadIdx.x & 31;
     bool bad = false;
+    if (m0 >= o.M) return;
+#pragma unroll 1
+    for (int n = n0; n < n1; n += kCols) {
+        __syncwarp();                        // the last chunk has been read
 #pragma unroll
-    for (int c = 0; c < 128; c += kCols) {
-        const int n = n0 + c;
-        if (m0 >= o.M || n >= o.N) break;
-        float f[kCols];
+        for (int part = 0; part < kCols / 32; ++part) {
+            uint32_t v[32];
+            umma::tmem_ld32(taddr + (n - n0) + part * 32, v);
+            umma::tmem_ld_wait();
+            float f[32];
 #pragma unroll
-        for (int i = 0; i < kCols; i += 2) {
-            ptx::unpack_f32x2(acc[(c + i) / 2], f[i], f[i + 1]);
-            if (m0 + lane < o.M) {                        // rows and columns beyond the matrix are sums of zeros
-                f[i] = f8_finish<T>(f[i], bad);
-                f[i + 1] = f8_finish<T>(f[i + 1], bad);
+            for (int i = 0; i < 32; ++i) {   // what lies beyond the tile is another one's
+                bool off = false;
+                f[i] = f8_finish<T>(__uint_as_float(v[i]), off);
+                bad |= off && n + part * 32 + i < n1 && m0 + lane < o.M;
             }
-        }
-        __syncwarp();
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            uint4 w;
-            if constexpr (sizeof(T) == 2)
-                w = make_uint4(pack_bf16x2(f[8 * j], f[8 * j + 1]), pack_bf16x2(f[8 * j + 2], f[8 * j + 3]),
-                               pack_bf16x2(f[8 * j + 4], f[8 * j + 5]), pack_bf16x2(f[8 * j + 6], f[8 * j + 7]));
-            else
-                w = make_uint4(__float_as_uint(f[4 * j]), __float_as_uint(f[4 * j + 1]), __float_as_uint(f[4 * j + 2]), __float_as_uint(f[4 * j + 3]));
-            ptx::sts128(sw + lane * 64 + ((j ^ ((lane >> 1) & 3)) << 4), w);
+            for (int j = 0; j < 32 / kPer; ++j) {
+                uint4 w;
+                if constexpr (sizeof(T) == 2)
+                    w = make_uint4(pack_bf16x2(f[8 * j], f[8 * j + 1]), pack_bf16x2(f[8 * j + 2], f[8 * j + 3]),
+                                   pack_bf16x2(f[8 * j + 4], f[8 * j + 5]), pack_bf16x2(f[8 * j + 6], f[8 * j + 7]));
+                else
+                    w = make_uint4(__float_as_uint(f[4 * j]), __float_as_uint(f[4 * j + 1]), __float_as_uint(f[4 * j + 2]), __float_as_uint(f[4 * j + 3]));
+                ptx::sts128(sw + f8_piece(lane, part * (32 / kPer) + j), w);
+            }
         }
         __syncwarp();
         if (o.aligned) {
 #pragma unroll
-            for (int it = 0; it < 4; ++it) {
-                const int r = it * 8 + (lane >> 2), j = lane & 3, col = n + j * kPer;
-                const uint4 w = ptx::lds128(sw + r * 64 + ((j ^ ((r >> 1) & 3)) << 4));
-                if (m0 + r >= o.M || col >= o.N) continue;
+            for (int it = 0; it < 8; ++it) {
+                const int r = it * 4 + (lane >> 3), j = lane & 7, col = n + j * kPer;
+                if (m0 + r >= o.M || col >= n1) continue;
+                const uint4 w = ptx::lds128(sw + f8_piece(r, j));
                 T* p = static_cast<T*>(o.y) + (m0 + r) * o.ldy + col;
-                if (col + kPer <= o.N) {
+                if (col + kPer <= n1) {
                     *reinterpret_cast<uint4*>(p) = w;
                 } else {
                     const uint32_t part[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
                     for (int i = 0; i < kPer; ++i) {
-                        if (col + i >= o.N) break;
+                        if (col + i >= n1) break;
                         if constexpr (sizeof(T) == 2) p[i] = T(part[i / 2] >> (i % 2 * 16));
                         else p[i] = __uint_as_float(part[i]);
                     }
                 }
             }
         } else {
-            // a warp stores 32 consecutive bf16, or two rows of 16 consecutive fp32
-            constexpr int kRows = 32 / kCols;
-            for (int r0 = 0; r0 < 32; r0 += kRows) {
-                const int r = r0 + lane / kCols, col = lane % kCols, j = col / kPer;
-                const uint32_t at = sw + r * 64 + ((j ^ ((r >> 1) & 3)) << 4) + (col % kPer) * int(sizeof(T));
-                if (m0 + r >= o.M || n + col >= o.N) continue;
-                T* p = static_cast<T*>(o.y) + (m0 + r) * o.ldy + n + col;
+#pragma unroll 4
+            for (int i = lane; i < 32 * kCols; i += 32) {                 // 32 consecutive elements at a time
+                const int r = i / kCols, c = i % kCols;
+                const uint32_t at = sw + f8_piece(r, c / kPer) + (c % kPer) * int(sizeof(T));
+                if (m0 + r >= o.M || n + c >= n1) continue;
+                T* p = static_cast<T*>(o.y) + (m0 + r) * o.ldy + n + c;
                 if constexpr (sizeof(T) == 2) {
                     *p = ptx::lds_u16(at);
                 } else {
@@ -237,17 +276,17 @@ __device__ __forceinline__ void f8_store(const F8Out& o, int64_t m0, int n0, con
     if (bad && o.status) atomicOr(o.status, TPPO_DEV_NONFINITE);
 }
 
-template <class T, bool BROWS>
-__global__ void __launch_bounds__(kF8Threads, 1)
-fp8_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ CUtensorMap map_sa,
-                const __grid_constant__ CUtensorMap map_sb, const F8Square square, const F8Shape g, const F8Out out) {
+template <class T>
+__global__ void __launch_bounds__(kF8GemmThreads, 1)
+fp8_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const F8Scales sa, const F8Scales sb,
+                const F8Shape g, const F8Out out) {
     extern __shared__ uint8_t smem_raw[];
     const uint32_t raw = ptx::smem_addr(smem_raw), base = (raw + 1023u) & ~1023u;
-    typedef F8Ring<kF8BN, kF8Stages, kF8Slots, true, BROWS> Ring;
-    const uint32_t scales = base + kF8Stages * Ring::kStage, staging = scales + kF8Slots * f8_slot<kF8BN>();
-    const uint32_t bars = staging + kF8Warps * kF8Staging;
-    const uint32_t full = bars, empty = full + 8 * kF8Stages, sfull = empty + 8 * kF8Stages, sempty = sfull + 8 * kF8Slots;
-    const uint32_t acc_full = sempty + 8 * kF8Slots, acc_empty = acc_full + 16, slot = acc_empty + 16;
+    typedef F8Ring<kF8BN, kF8Stages> Ring;
+    static_assert(2 * kF8BN + 2 * Ring::kSet <= 512, "two accumulators and two sets of exponents fit tensor memory");
+    const uint32_t staging = base + kF8Stages * Ring::kStage, bars = staging + kF8OutWarps * kF8Staging;
+    const uint32_t full = bars, empty = full + 8 * kF8Stages, sfull = empty + 8 * kF8Stages, sempty = sfull + 16;
+    const uint32_t acc_full = sempty + 16, acc_empty = acc_full + 16, slot = acc_empty + 16;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
     if (threadIdx.x == 0) {
@@ -255,21 +294,17 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
             ptx::mbar_init(full + 8 * s, 1);
             ptx::mbar_init(empty + 8 * s, 1);
         }
-        for (int s = 0; s < kF8Slots; ++s) {
-            ptx::mbar_init(sfull + 8 * s, 1);
-            ptx::mbar_init(sempty + 8 * s, kF8Warps);
-        }
         for (int a = 0; a < 2; ++a) {
+            ptx::mbar_init(sfull + 8 * a, 4);
+            ptx::mbar_init(sempty + 8 * a, 1);
             ptx::mbar_init(acc_full + 8 * a, 1);
-            ptx::mbar_init(acc_empty + 8 * a, kF8Warps);
+            ptx::mbar_init(acc_empty + 8 * a, kF8OutWarps);
         }
         ptx::fence_mbar_init_cluster();
         umma::prefetch_tensormap(&map_a);
         umma::prefetch_tensormap(&map_b);
-        umma::prefetch_tensormap(&map_sa);
-        if (BROWS) umma::prefetch_tensormap(&map_sb);
     }
-    if (warp == 1) {
+    if (warp == 13) {
         umma::tmem_alloc(slot, 512);
         umma::tmem_relinquish();
     }
@@ -281,69 +316,52 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
     pdl_wait();
 
     bool timed_out = false;
-    if (warp == 0) {
-        if (lane == 0) {
-            Ring ring{base, scales, full, empty, sfull, sempty};
-            for (int t = blockIdx.x; t < g.total && !timed_out; t += gridDim.x) {
-                int mt, nt;
-                f8_tile(g, t, mt, nt);
-                timed_out = !ring.load(&map_a, &map_b, &map_sa, &map_sb, mt * kF8TileM, nt * kF8BN, 0, g.blocks);
-            }
-            if (timed_out) ring.drain();
-        }
-    } else if (warp == 1) {
-        if (lane == 0) {
-            Ring ring{base, scales, full, empty, sfull, sempty};
-            uint32_t n = 0;              // blocks so far: they take the two accumulators in turn
-            for (int t = blockIdx.x; t < g.total && !timed_out; t += gridDim.x) {
-                for (int kb = 0; kb < g.blocks; ++kb, ++n) {
-                    const uint32_t acc = n & 1;
-                    if (!ptx::mbar_wait<false>(acc_empty + 8 * acc, ((n >> 1) & 1) ^ 1u)) { timed_out = true; break; }
-                    umma::fence_after_thread_sync();
-                    if (!ring.multiply(tmem + acc * kF8BN)) { timed_out = true; break; }
-                    umma::mma_commit(acc_full + 8 * acc);
-                }
-            }
-        }
-    } else {
-        const int q = warp & 3, half = (warp - 2) >> 2;
-        const uint32_t lanes = uint32_t(q * 32) << 16, sw = staging + (warp - 2) * kF8Staging;
-        uint32_t n = 0, sslot = 0, sphase = 0;
+    Ring ring{base, full, empty, sfull, sempty, tmem + 2 * kF8BN};
+    if (warp < 4) {
         for (int t = blockIdx.x; t < g.total && !timed_out; t += gridDim.x) {
             int mt, nt;
             f8_tile(g, t, mt, nt);
-            const int n0 = nt * kF8BN + half * 128;
-            const float* sq = nullptr;
-            if (!BROWS) sq = square.p + int64_t(n0 < out.N ? n0 / 128 : 0) * square.ld;
-            float sb = BROWS ? 1.f : __ldg(sq);
-            uint64_t acc[64];
-#pragma unroll
-            for (int i = 0; i < 64; ++i) acc[i] = 0;
-            for (int kb = 0; kb < g.blocks; ++kb, ++n) {
-                const float sb_next = !BROWS && kb + 1 < g.blocks ? __ldg(sq + kb + 1) : 1.f;
-                if (!ptx::mbar_wait_warp<false>(sfull + 8 * sslot, sphase)) { timed_out = true; break; }
-                const uint32_t s = scales + sslot * Ring::kSlot;
-                float sa;
-                asm volatile("ld.shared.f32 %0, [%1];" : "=f"(sa) : "r"(s + (q * 32 + lane) * 4));
-                if (!ptx::mbar_wait_warp<false>(acc_full + 8 * (n & 1), (n >> 1) & 1)) { timed_out = true; break; }
-                umma::fence_after_thread_sync();
-                f8_scale<128, BROWS>(tmem + lanes + (n & 1) * kF8BN + half * 128, sa * sb, s + kF8TileM * 4 + half * 512, acc);
-                umma::fence_before_thread_sync();
-                __syncwarp();
-                if (lane == 0) {
-                    ptx::mbar_arrive(acc_empty + 8 * (n & 1));
-                    ptx::mbar_arrive(sempty + 8 * sslot);
-                }
-                if (++sslot == kF8Slots) { sslot = 0; sphase ^= 1u; }
-                sb = sb_next;
+            timed_out = !ring.scales(sa, sb, uint32_t(warp * 32) << 16, mt * kF8TileM, nt * kF8BN, 0, g.blocks);
+        }
+    } else if (warp < 12) {
+        const int q = warp & 3, half = (warp - 4) >> 2;
+        const uint32_t sw = staging + (warp - 4) * kF8Staging;
+        int local = 0;
+        for (int t = blockIdx.x; t < g.total; t += gridDim.x, ++local) {
+            int mt, nt;
+            f8_tile(g, t, mt, nt);
+            const int acc = local & 1, first = nt * kF8BN, n0 = first + half * 128;
+            const int n1 = min(out.N, half == 0 ? first + 128 : first + kF8BN);
+            if (!ptx::mbar_wait_warp<false>(acc_full + 8 * acc, (local >> 1) & 1)) { timed_out = true; break; }
+            umma::fence_after_thread_sync();
+            f8_store<T>(out, int64_t(mt) * kF8TileM + q * 32, n0, n1, tmem + acc * kF8BN + (uint32_t(q * 32) << 16) + half * 128, sw);
+            umma::fence_before_thread_sync();
+            __syncwarp();
+            if (lane == 0) ptx::mbar_arrive(acc_empty + 8 * acc);
+        }
+    } else if (warp == 12) {
+        if (lane == 0) {
+            for (int t = blockIdx.x; t < g.total && !timed_out; t += gridDim.x) {
+                int mt, nt;
+                f8_tile(g, t, mt, nt);
+                timed_out = !ring.load(&map_a, &map_b, mt * kF8TileM, nt * kF8BN, 0, g.blocks);
             }
-            if (!timed_out) f8_store<T>(out, int64_t(mt) * kF8TileM + q * 32, n0, acc, sw);
+            if (timed_out) ring.drain();
+        }
+    } else if (lane == 0) {
+        int local = 0;
+        for (int t = blockIdx.x; t < g.total; t += gridDim.x, ++local) {
+            const int acc = local & 1;
+            if (!ptx::mbar_wait<false>(acc_empty + 8 * acc, ((local >> 1) & 1) ^ 1u)) { timed_out = true; break; }
+            umma::fence_after_thread_sync();
+            if (!ring.multiply(tmem + acc * kF8BN, 0, g.blocks)) { timed_out = true; break; }
+            umma::mma_commit(acc_full + 8 * acc);
         }
     }
     if (timed_out && out.status) atomicOr(out.status, TPPO_DEV_WAIT_TIMEOUT);
     umma::fence_before_thread_sync();
     __syncthreads();
-    if (warp == 1) {
+    if (warp == 13) {
         __syncwarp();
         umma::tmem_dealloc(tmem, 512);
     }
@@ -354,31 +372,29 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
 // CTAs) accumulator columns: every CTA stores its partial sums into the owner's shared memory, and after one cluster
 // barrier the owner adds them in rank order.  Up to 64 columns the sums have memory of their own and two CTAs share an
 // SM; 128 columns lay them over the operand ring, which needs one more barrier.
+// Warps: 0 TMA loads, 1 tcgen05.mma, 2-5 exponents, 2-9 output.
+constexpr int kF8SplitThreads = 320;
 template <int BN> __host__ __device__ constexpr bool f8_overlay() { return BN >= 128; }
 template <int BN> __host__ __device__ constexpr int f8_stages() { return BN <= 16 ? 5 : BN <= 32 ? 4 : BN <= 64 ? 3 : 6; }
-constexpr int kF8SplitSlots = 4;
 template <int BN> __host__ __device__ constexpr uint32_t f8_ring() { return uint32_t(f8_stages<BN>()) * (kF8ABytes + BN * kF8Block); }
 template <int BN> __host__ __device__ constexpr uint32_t f8_body() { return f8_ring<BN>() + (f8_overlay<BN>() ? 0u : (BN + 8) * 128 * 4); }
-template <int BN> __host__ __device__ constexpr size_t f8_split_smem() {
-    return f8_body<BN>() + kF8SplitSlots * f8_slot<BN>() + 1024 /* alignment */ + 256 /* barriers */;
-}
+template <int BN> __host__ __device__ constexpr size_t f8_split_smem() { return f8_body<BN>() + 1024 /* alignment */ + 192 /* barriers */; }
 
 struct F8SplitShape { int32_t col_tiles, blocks; };
 
-template <class T, int BN, bool AROWS>
-__global__ void __launch_bounds__(kF8Threads, BN <= 64 ? 2 : 1)
-fp8_split_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ CUtensorMap map_sa,
-                 const __grid_constant__ CUtensorMap map_sb, const F8Square square, const F8SplitShape g, const F8Out out) {
-    constexpr int STAGES = f8_stages<BN>(), kEpiThreads = kF8Threads - 64, kHalf = BN / 2;
-    constexpr uint32_t kCols = 2 * BN < 32 ? 32 : 2 * BN;             // two accumulators
+template <class T, int BN>
+__global__ void __launch_bounds__(kF8SplitThreads)
+fp8_split_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const F8Scales sa, const F8Scales sb,
+                 const F8SplitShape g, const F8Out out) {
+    constexpr int STAGES = f8_stages<BN>(), kEpiThreads = kF8SplitThreads - 64;
+    typedef F8Ring<BN, STAGES> Ring;
+    constexpr uint32_t kCols = BN + 2 * Ring::kSet <= 32 ? 32 : 2 * BN;       // accumulator and exponents
+    static_assert(BN + 2 * Ring::kSet <= kCols, "");
     extern __shared__ uint8_t smem_raw[];
     // dynamic shared memory starts at the same address in every CTA of a kernel, so `sums` is common to the cluster
     const uint32_t raw = ptx::smem_addr(smem_raw), base = (raw + 1023u) & ~1023u;
-    typedef F8Ring<BN, STAGES, kF8SplitSlots, AROWS, true> Ring;
-    const uint32_t sums = base + (f8_overlay<BN>() ? 0u : f8_ring<BN>()), scales = base + f8_body<BN>();
-    const uint32_t bars = scales + kF8SplitSlots * f8_slot<BN>();
-    const uint32_t full = bars, empty = full + 8 * STAGES, sfull = empty + 8 * STAGES, sempty = sfull + 8 * kF8SplitSlots;
-    const uint32_t acc_full = sempty + 8 * kF8SplitSlots, acc_empty = acc_full + 16, slot = acc_empty + 16;
+    const uint32_t sums = base + (f8_overlay<BN>() ? 0u : f8_ring<BN>()), bars = base + f8_body<BN>();
+    const uint32_t full = bars, empty = full + 8 * STAGES, sfull = empty + 8 * STAGES, sempty = sfull + 16, acc_full = sempty + 16, slot = acc_full + 8;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int rank = int(ptx::cluster_ctarank());
     int splits;
@@ -392,19 +408,14 @@ fp8_split_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
             ptx::mbar_init(full + 8 * s, 1);
             ptx::mbar_init(empty + 8 * s, 1);
         }
-        for (int s = 0; s < kF8SplitSlots; ++s) {
-            ptx::mbar_init(sfull + 8 * s, 1);
-            ptx::mbar_init(sempty + 8 * s, kF8Warps);
-        }
         for (int a = 0; a < 2; ++a) {
-            ptx::mbar_init(acc_full + 8 * a, 1);
-            ptx::mbar_init(acc_empty + 8 * a, kF8Warps);
+            ptx::mbar_init(sfull + 8 * a, 4);
+            ptx::mbar_init(sempty + 8 * a, 1);
         }
+        ptx::mbar_init(acc_full, 1);
         ptx::fence_mbar_init_cluster();
         umma::prefetch_tensormap(&map_a);
         umma::prefetch_tensormap(&map_b);
-        if (AROWS) umma::prefetch_tensormap(&map_sa);
-        umma::prefetch_tensormap(&map_sb);
     }
     if (warp == 1) {
         umma::tmem_alloc(slot, kCols);
@@ -419,65 +430,44 @@ fp8_split_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
     pdl_wait();
 
     bool timed_out = false;
-    uint64_t acc[kHalf / 2];
-#pragma unroll
-    for (int i = 0; i < kHalf / 2; ++i) acc[i] = 0;
+    Ring ring{base, full, empty, sfull, sempty, tmem + BN};
     const int q = warp & 3, half = (warp - 2) >> 2;
     if (warp == 0) {
         if (lane == 0) {
-            Ring ring{base, scales, full, empty, sfull, sempty};
-            timed_out = !ring.load(&map_a, &map_b, &map_sa, &map_sb, rt * kF8TileM, ct * BN, k0, k1);
+            timed_out = !ring.load(&map_a, &map_b, rt * kF8TileM, ct * BN, k0, k1);
             if (timed_out) ring.drain();
         }
         __syncwarp();
     } else if (warp == 1) {
         if (lane == 0) {
-            Ring ring{base, scales, full, empty, sfull, sempty};
-            for (uint32_t n = 0; n < uint32_t(k1 - k0); ++n) {
-                if (!ptx::mbar_wait<false>(acc_empty + 8 * (n & 1), ((n >> 1) & 1) ^ 1u)) { timed_out = true; break; }
-                umma::fence_after_thread_sync();
-                if (!ring.multiply(tmem + (n & 1) * BN)) { timed_out = true; break; }
-                umma::mma_commit(acc_full + 8 * (n & 1));
-            }
+            timed_out = !ring.multiply(tmem, k0, k1);
+            if (!timed_out) umma::mma_commit(acc_full);
         }
         __syncwarp();
     } else {
-        const uint32_t lanes = uint32_t(q * 32) << 16;
-        const float* sq = AROWS ? nullptr : square.p + int64_t(rt) * square.ld;
-        uint32_t sslot = 0, sphase = 0;
-        float sa_next = AROWS || k0 >= k1 ? 1.f : __ldg(sq + k0);
-        for (int kb = k0; kb < k1; ++kb) {
-            const uint32_t n = uint32_t(kb - k0);
-            float sa = sa_next;
-            if (!AROWS && kb + 1 < k1) sa_next = __ldg(sq + kb + 1);
-            if (!ptx::mbar_wait_warp<false>(sfull + 8 * sslot, sphase)) { timed_out = true; break; }
-            const uint32_t s = scales + sslot * Ring::kSlot;
-            if (AROWS) asm volatile("ld.shared.f32 %0, [%1];" : "=f"(sa) : "r"(s + (q * 32 + lane) * 4));
-            if (!ptx::mbar_wait_warp<false>(acc_full + 8 * (n & 1), (n >> 1) & 1)) { timed_out = true; break; }
-            umma::fence_after_thread_sync();
-            f8_scale<kHalf, true>(tmem + lanes + (n & 1) * BN + half * kHalf, sa, s + kF8TileM * 4 + half * kHalf * 4, acc);
-            umma::fence_before_thread_sync();
-            __syncwarp();
-            if (lane == 0) {
-                ptx::mbar_arrive(acc_empty + 8 * (n & 1));
-                ptx::mbar_arrive(sempty + 8 * sslot);
-            }
-            if (++sslot == kF8SplitSlots) { sslot = 0; sphase ^= 1u; }
-        }
+        if (warp < 6) timed_out = !ring.scales(sa, sb, uint32_t(q * 32) << 16, rt * kF8TileM, ct * BN, k0, k1);
+        timed_out = !ptx::mbar_wait_warp<false>(acc_full, 0) || timed_out;
     }
     if (f8_overlay<BN>()) ptx::cluster_sync_all();       // every ring of the cluster has been consumed
     const int own = (BN + splits - 1) / splits, c0 = rank * own;
     if (warp >= 2 && !timed_out) {
         const int r = q * 32 + lane;
-        int owner = half * kHalf / own, in = half * kHalf - owner * own;
+        constexpr int kChunk = BN >= 64 ? 32 : 8;
+        umma::fence_after_thread_sync();
+#pragma unroll 1
+        for (int c = half * (BN / 2); c < (half + 1) * (BN / 2); c += kChunk) {
+            uint32_t v[kChunk];
+            if constexpr (kChunk == 32) umma::tmem_ld32(tmem + (uint32_t(q * 32) << 16) + c, v);
+            else f8_tmem_ld8(tmem + (uint32_t(q * 32) << 16) + c, v);
+            umma::tmem_ld_wait();
+            int owner = c / own, in = c - owner * own;
 #pragma unroll
-        for (int i = 0; i < kHalf; ++i) {
-            // [source rank][owned column][128 rows] at the owner
-            float lo, hi;
-            ptx::unpack_f32x2(acc[i / 2], lo, hi);
-            const uint32_t at = ptx::map_to_cta(sums + ((rank * own + in) * 128 + r) * 4, uint32_t(owner));
-            asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(at), "f"(i & 1 ? hi : lo) : "memory");
-            if (++in == own) { in = 0; ++owner; }
+            for (int i = 0; i < kChunk; ++i) {
+                // [source rank][owned column][128 rows] at the owner
+                const uint32_t at = ptx::map_to_cta(sums + ((rank * own + in) * 128 + r) * 4, uint32_t(owner));
+                asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(at), "r"(v[i]) : "memory");
+                if (++in == own) { in = 0; ++owner; }
+            }
         }
     }
     umma::fence_before_thread_sync();
@@ -502,7 +492,11 @@ fp8_split_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
             }
             T* y = static_cast<T*>(out.y) + m * out.ldy + n;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) w[i] = f8_finish<T>(w[i], bad);
+            for (int i = 0; i < 8; ++i) {
+                bool off = false;
+                w[i] = f8_finish<T>(w[i], off);
+                bad |= off && n + i < out.N;
+            }
             if (out.aligned && n + 8 <= out.N) {
                 store_vec<8>(y, w);
             } else {
@@ -519,7 +513,7 @@ fp8_split_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
 }
 
 // ---- host side --------------------------------------------------------------------------------------------------
-struct F8Operand { const void* p; int64_t rows, ld; const float* scale; int64_t lds; bool by_rows; };
+struct F8Operand { const void* p; int64_t rows, ld; F8Scales s; };
 
 // How a product is cut: bn 0 = the persistent kernel, else the split kernel's columns (output rows) per tile and the
 // CTAs that share a tile's contraction: the least estimated time in SM clocks.  A block of 128 bytes moves as many
@@ -529,9 +523,9 @@ F8Cut f8_cut(int64_t m, int64_t n, int64_t blocks) {
     // CTAs that fit on the GPU at once in clusters of s, at two and at one per SM (the driver's count)
     static const int64_t pair[9] = {0, 296, 296, 279, 284, 280, 270, 259, 264};
     static const int64_t alone[9] = {0, 148, 148, 135, 132, 130, 132, 105, 120};
-    const int64_t rows = (n + 127) / 128, big = (m + 127) / 128 * ((n + 255) / 256);
+    const int64_t rows = (n + 127) / 128, big = (m + 127) / 128 * ((n + kF8BN - 1) / kF8BN);
     F8Cut best{0, 1};
-    int64_t least = 5000 + (big + kNumSms - 1) / kNumSms * blocks * 600 + 4000;
+    int64_t least = 5000 + (big + kNumSms - 1) / kNumSms * blocks * 600 + 6000;
     for (int bn = 16; bn <= 128; bn *= 2) {
         const int64_t tiles = rows * ((m + bn - 1) / bn);
         const int64_t stages = bn <= 16 ? 5 : bn <= 32 ? 4 : bn <= 64 ? 3 : 6;
@@ -549,13 +543,10 @@ F8Cut f8_cut(int64_t m, int64_t n, int64_t blocks) {
     return best;
 }
 
-template <class T, bool BROWS>
+template <class T>
 int f8_gemm(const F8Operand& a, const F8Operand& b, int64_t K, int64_t blocks, const F8Out& out, cudaStream_t s) {
-    CUtensorMap ma, mb, msa, msb{};
-    if (!make_u8_tensor_map(&ma, a.p, a.rows, K, a.ld, kF8TileM) || !make_u8_tensor_map(&mb, b.p, b.rows, K, b.ld, kF8BN) ||
-        !make_f32_tensor_map(&msa, a.scale, blocks, a.rows, a.lds, kF8TileM) ||
-        (BROWS && !make_f32_tensor_map(&msb, b.scale, blocks, b.rows, b.lds, kF8BN)))
-        return TPPO_ERR_CUDA;
+    CUtensorMap ma, mb;
+    if (!make_u8_tensor_map(&ma, a.p, a.rows, K, a.ld, kF8TileM) || !make_u8_tensor_map(&mb, b.p, b.rows, K, b.ld, kF8BN)) return TPPO_ERR_CUDA;
     F8Shape g;
     g.m_tiles = int32_t((a.rows + kF8TileM - 1) / kF8TileM);
     g.n_tiles = int32_t((b.rows + kF8BN - 1) / kF8BN);
@@ -564,31 +555,28 @@ int f8_gemm(const F8Operand& a, const F8Operand& b, int64_t K, int64_t blocks, c
     const int64_t total = int64_t(g.m_tiles) * g.n_tiles;
     if (total > 0x7fffffff - kNumSms) return TPPO_ERR_UNSUPPORTED;
     g.total = int32_t(total);
-    auto kernel = fp8_gemm_kernel<T, BROWS>;
+    auto kernel = fp8_gemm_kernel<T>;
     TPPO_CUDA_CHECK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, int(kF8Smem)));
     const int grid = g.total < kNumSms ? g.total : kNumSms;
-    TPPO_CUDA_CHECK(launch_dense(kernel, dim3(grid), dim3(kF8Threads), kF8Smem, s, ma, mb, msa, msb, F8Square{b.scale, b.lds}, g, out));
+    TPPO_CUDA_CHECK(launch_dense(kernel, dim3(grid), dim3(kF8GemmThreads), kF8Smem, s, ma, mb, a.s, b.s, g, out));
     return TPPO_OK;
 }
 
-template <class T, int BN, bool AROWS>
+template <class T, int BN>
 int f8_split(const F8Operand& a, const F8Operand& b, int64_t K, int64_t blocks, int splits, const F8Out& out, cudaStream_t s) {
-    CUtensorMap ma, mb, msa{}, msb;
-    if (!make_u8_tensor_map(&ma, a.p, a.rows, K, a.ld, kF8TileM) || !make_u8_tensor_map(&mb, b.p, b.rows, K, b.ld, BN) ||
-        (AROWS && !make_f32_tensor_map(&msa, a.scale, blocks, a.rows, a.lds, kF8TileM)) ||
-        !make_f32_tensor_map(&msb, b.scale, blocks, b.rows, b.lds, BN))
-        return TPPO_ERR_CUDA;
+    CUtensorMap ma, mb;
+    if (!make_u8_tensor_map(&ma, a.p, a.rows, K, a.ld, kF8TileM) || !make_u8_tensor_map(&mb, b.p, b.rows, K, b.ld, BN)) return TPPO_ERR_CUDA;
     F8SplitShape g;
     const int64_t row_tiles = (a.rows + kF8TileM - 1) / kF8TileM, col_tiles = (b.rows + BN - 1) / BN;
     if (row_tiles * col_tiles * splits > 0x7fffffff) return TPPO_ERR_UNSUPPORTED;
     g.col_tiles = int32_t(col_tiles);
     g.blocks = int32_t(blocks);
-    auto kernel = fp8_split_kernel<T, BN, AROWS>;
+    auto kernel = fp8_split_kernel<T, BN>;
     constexpr size_t smem = f8_split_smem<BN>();
     TPPO_CUDA_CHECK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, int(smem)));
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3(unsigned(row_tiles * col_tiles * splits));
-    cfg.blockDim = dim3(kF8Threads);
+    cfg.blockDim = dim3(kF8SplitThreads);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = s;
     cudaLaunchAttribute attr[2];
@@ -599,21 +587,25 @@ int f8_split(const F8Operand& a, const F8Operand& b, int64_t K, int64_t blocks, 
     attr[1].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 2;
-    TPPO_CUDA_CHECK(cudaLaunchKernelEx(&cfg, kernel, ma, mb, msa, msb, F8Square{a.scale, a.lds}, g, out));
+    TPPO_CUDA_CHECK(cudaLaunchKernelEx(&cfg, kernel, ma, mb, a.s, b.s, g, out));
     return TPPO_OK;
 }
 
-template <class T, bool BROWS>
+template <class T>
 int f8_product(const F8Operand& a, const F8Operand& b, int64_t K, const F8Out& out, cudaStream_t s) {
     const int64_t blocks = (K + kF8Block - 1) / kF8Block;
     const F8Cut c = f8_cut(a.rows, b.rows, blocks);
     switch (c.bn) {                          // the split kernel's rows are the output's columns
-        case 16: return f8_split<T, 16, BROWS>(b, a, K, blocks, c.splits, out, s);
-        case 32: return f8_split<T, 32, BROWS>(b, a, K, blocks, c.splits, out, s);
-        case 64: return f8_split<T, 64, BROWS>(b, a, K, blocks, c.splits, out, s);
-        case 128: return f8_split<T, 128, BROWS>(b, a, K, blocks, c.splits, out, s);
-        default: return f8_gemm<T, BROWS>(a, b, K, blocks, out, s);
+        case 16: return f8_split<T, 16>(b, a, K, blocks, c.splits, out, s);
+        case 32: return f8_split<T, 32>(b, a, K, blocks, c.splits, out, s);
+        case 64: return f8_split<T, 64>(b, a, K, blocks, c.splits, out, s);
+        case 128: return f8_split<T, 128>(b, a, K, blocks, c.splits, out, s);
+        default: return f8_gemm<T>(a, b, K, blocks, out, s);
     }
+}
+
+F8Scales scales_of(const float* p, int64_t ld, int64_t rows, bool by_rows) {
+    return by_rows ? F8Scales{p, ld, 1, 0, int32_t(rows)} : F8Scales{p, 1, ld, 7, int32_t(rows)};
 }
 
 int64_t whole(int64_t ld, int64_t unit) { return (ld + unit - 1) / unit * unit; }
@@ -639,15 +631,13 @@ TPPO_API int tppo_fp8_matmul(const void* a, int64_t lda, const float* a_scale, i
     }
     const int64_t kb = (K + kF8Block - 1) / kF8Block;
     const bool rows = b_block == TPPO_FP8_ROWS;
-    if (!a || !a_scale || !b || !b_scale || !aligned(a, 16) || !aligned(b, 16) || !aligned(a_scale, 16) || !aligned(b_scale, rows ? 16 : 4))
+    if (!a || !a_scale || !b || !b_scale || !aligned(a, 16) || !aligned(b, 16) || !aligned(a_scale, 4) || !aligned(b_scale, 4))
         return TPPO_ERR_INVALID_ARG;
     // a matrix of one row needs no stride
-    if (lda < K || ldb < K || (M > 1 && lda % 16) || (N > 1 && ldb % 16) || ldas < M || (kb > 1 && ldas % 4) || ldbs < (rows ? N : kb) ||
-        (rows && kb > 1 && ldbs % 4))
+    if (lda < K || ldb < K || (M > 1 && lda % 16) || (N > 1 && ldb % 16) || ldas < M || ldbs < (rows ? N : kb))
         return TPPO_ERR_INVALID_ARG;
-    const F8Operand oa{a, M, whole(lda, 16), a_scale, whole(ldas, 4), true};
-    const F8Operand ob{b, N, whole(ldb, 16), b_scale, rows ? whole(ldbs, 4) : ldbs, rows};
+    const F8Operand oa{a, M, whole(lda, 16), scales_of(a_scale, ldas, M, true)};
+    const F8Operand ob{b, N, whole(ldb, 16), scales_of(b_scale, ldbs, N, rows)};
     const F8Out out{y, ldy, M, int32_t(N), status, rows_aligned(y, ldy, e)};
-    if (y_dtype == TPPO_F32) return rows ? f8_product<float, true>(oa, ob, K, out, s) : f8_product<float, false>(oa, ob, K, out, s);
-    return rows ? f8_product<bf16_bits, true>(oa, ob, K, out, s) : f8_product<bf16_bits, false>(oa, ob, K, out, s);
+    return y_dtype == TPPO_F32 ? f8_product<float>(oa, ob, K, out, s) : f8_product<bf16_bits>(oa, ob, K, out, s);
 }

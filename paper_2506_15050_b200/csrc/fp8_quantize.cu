@@ -188,11 +188,9 @@ TPPO_API int tppo_fp8_quantize(const void* x, int32_t dtype, int64_t ldx, int64_
     if (!x || ldx < K || !aligned(x, dtype == TPPO_F32 ? 4 : 2) || (q == nullptr) != (scale == nullptr) || (qt == nullptr) != (scale_t == nullptr))
         return TPPO_ERR_INVALID_ARG;
     // rows of one element's height need no stride
-    if (q && (!aligned(q, 16) || ldq < K || (M > 1 && ldq % 16) || !aligned(scale, rows ? 16 : 4) || lds < (rows ? M : kb) ||
-              (rows && kb > 1 && lds % 4)))
+    if (q && (!aligned(q, 16) || ldq < K || (M > 1 && ldq % 16) || !aligned(scale, 4) || lds < (rows ? M : kb)))
         return TPPO_ERR_INVALID_ARG;
-    if (qt && (!aligned(qt, 16) || ldqt < M || (K > 1 && ldqt % 16) || !aligned(scale_t, rows ? 16 : 4) || ldst < (rows ? K : mb) ||
-               (rows && mb > 1 && ldst % 4)))
+    if (qt && (!aligned(qt, 16) || ldqt < M || (K > 1 && ldqt % 16) || !aligned(scale_t, 4) || ldst < (rows ? K : mb)))
         return TPPO_ERR_INVALID_ARG;
     if (mb * kb > 0x7fffffff) return TPPO_ERR_UNSUPPORTED;
     if (!q && !qt) return TPPO_OK;
