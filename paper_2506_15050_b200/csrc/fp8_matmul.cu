@@ -67,35 +67,13 @@ __device__ __forceinline__ uint32_t f8_exponent(float s) {
     const uint32_t b = __float_as_uint(s), e = b >> 23;
     return (b & 0x807fffffu) != 0 || e == 0 || e == 255 ? 0xffu : e;
 }
-// What a thread reads of a group of blocks: rows r0 + 32 c + lane of `COLS` columns of tensor memory.  Rows beyond the
-// operand and blocks beyond the contraction get 2^0; their products are 0.
-template <int COLS>
-__device__ __forceinline__ void f8_read_scales(const F8Scales& s, int r0, int kb, int k1, float (&v)[COLS][kF8Group]) {
-#pragma unroll
-    for (int c = 0; c < COLS; ++c) {
-        const int row = r0 + 32 * c + int(threadIdx.x & 31);
-        const float* p = s.p + int64_t(row >> s.shift) * s.by_row;
-#pragma unroll
-        for (int j = 0; j < kF8Group; ++j) v[c][j] = row < s.rows && kb + j < k1 ? p[(kb + j) * s.by_block] : 1.f;
-    }
-}
-template <int COLS>
-__device__ __forceinline__ void f8_write_scales(uint32_t taddr, const float (&v)[COLS][kF8Group]) {
-    static_assert(COLS % 4 == 0, "written four columns at a time");
-    uint32_t w[COLS];
-#pragma unroll
-    for (int c = 0; c < COLS; ++c)
-        w[c] = f8_exponent(v[c][0]) | f8_exponent(v[c][1]) << 8 | f8_exponent(v[c][2]) << 16 | f8_exponent(v[c][3]) << 24;
-#pragma unroll
-    for (int c = 0; c < COLS; c += 4) f8_tmem_st4(taddr + c, w + c);
-}
-
 // The rings of a CTA: operand stages in shared memory, and two sets of exponents in tensor memory (columns `sf`, A's
 // four followed by B's), each for a group of blocks.
 template <int BN, int STAGES>
 struct F8Ring {
     static constexpr uint32_t kStage = kF8ABytes + BN * kF8Block;
     static constexpr int kBCols = BN <= 128 ? 4 : 8, kSet = 4 + kBCols;
+    static constexpr uint32_t kCells = 2 * kSet * 32 * 4;
     uint32_t base, full, empty, sfull, sempty, sf;
     int stage = 0;
     uint32_t phase = 0, set = 0, sphase = 0;
@@ -124,25 +102,69 @@ struct F8Ring {
         for (int s = 0; s < STAGES; ++s)
             if (!ptx::mbar_wait<false>(full + 8 * s, s < stage ? phase : phase ^ 1u)) return;
     }
-    // The exponents of blocks [k0, k1), by four warps, one per quarter of the lanes (`quarter`: the address of its first).
-    __device__ __forceinline__ bool scales(const F8Scales& a, const F8Scales& b, uint32_t quarter, int am, int bn, int k0, int k1) {
-        float va[4][kF8Group], vb[kBCols][kF8Group];
-        f8_read_scales<4>(a, am, k0, k1, va);
-        f8_read_scales<kBCols>(b, bn, k0, k1, vb);
+    // The exponents of blocks [k0, k1), by four warps.  Each reads the scales of a quarter of the columns, three groups
+    // ahead -- under the operands' traffic a load takes some 2000 clocks -- and makes their cells; through shared
+    // memory (`cells`: two sets of [kSet][32] words) every warp gets all of them and writes them to the quarter of the lanes
+    // that it can reach.  `w`: the warp's number among the four, `quarter`: the address of its lanes.
+    __device__ __forceinline__ bool scales(const F8Scales& a, const F8Scales& b, uint32_t cells, int w, uint32_t quarter, int am, int bn,
+                                           int k0, int k1) {
+        constexpr int kMine = kSet / 4, kAhead = 3;
+        const int lane = threadIdx.x & 31;
+        const float* p[kMine];
+        int64_t by_block[kMine];
+        bool in[kMine];
+#pragma unroll
+        for (int i = 0; i < kMine; ++i) {
+            const int c = w * kMine + i;
+            const bool of_a = c < 4;
+            const F8Scales& s = of_a ? a : b;
+            const int row = of_a ? am + 32 * c + lane : bn + 32 * (c - 4) + lane;
+            in[i] = row < s.rows;            // rows beyond the operand, blocks beyond the contraction: 2^0; their products are 0
+            by_block[i] = s.by_block;
+            p[i] = s.p + int64_t(row >> s.shift) * s.by_row + k0 * s.by_block;
+        }
+        float v[kAhead][kMine][kF8Group];
+        int next = k0;                       // the first block not yet read
+        auto read = [&](float (&to)[kMine][kF8Group]) {
+#pragma unroll
+            for (int i = 0; i < kMine; ++i) {
+#pragma unroll
+                for (int j = 0; j < kF8Group; ++j) to[i][j] = in[i] && next + j < k1 ? p[i][j * by_block[i]] : 1.f;
+                p[i] += kF8Group * by_block[i];
+            }
+            next += kF8Group;
+        };
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) read(v[i]);
         for (int kb = k0; kb < k1; kb += kF8Group) {
+            const uint32_t mine = cells + (set * kSet + w * kMine) * 128 + lane * 4;
+#pragma unroll
+            for (int i = 0; i < kMine; ++i) {
+                const uint32_t cell = f8_exponent(v[0][i][0]) | f8_exponent(v[0][i][1]) << 8 | f8_exponent(v[0][i][2]) << 16 |
+                                      f8_exponent(v[0][i][3]) << 24;
+                asm volatile("st.shared.u32 [%0], %1;" ::"r"(mine + i * 128), "r"(cell) : "memory");
+            }
+            asm volatile("bar.sync 1, 128;" ::: "memory");
+            uint32_t all[kSet];
+#pragma unroll
+            for (int c = 0; c < kSet; ++c)
+                asm volatile("ld.shared.u32 %0, [%1];" : "=r"(all[c]) : "r"(cells + (set * kSet + c) * 128 + lane * 4));
             if (!ptx::mbar_wait_warp<false>(sempty + 8 * set, sphase ^ 1u)) return false;
             umma::fence_after_thread_sync();
-            f8_write_scales<4>(sf + quarter + set * kSet, va);
-            f8_write_scales<kBCols>(sf + quarter + set * kSet + 4, vb);
+#pragma unroll
+            for (int c = 0; c < kSet; c += 4) f8_tmem_st4(sf + quarter + set * kSet + c, all + c);
             f8_tmem_st_wait();
             umma::fence_before_thread_sync();
             __syncwarp();
-            if ((threadIdx.x & 31) == 0) ptx::mbar_arrive(sfull + 8 * set);
+            if (lane == 0) ptx::mbar_arrive(sfull + 8 * set);
             next_set();
-            if (kb + kF8Group < k1) {                     // a group ahead
-                f8_read_scales<4>(a, am, kb + kF8Group, k1, va);
-                f8_read_scales<kBCols>(b, bn, kb + kF8Group, k1, vb);
-            }
+#pragma unroll
+            for (int i = 0; i + 1 < kAhead; ++i)
+#pragma unroll
+                for (int j = 0; j < kMine; ++j)
+#pragma unroll
+                    for (int l = 0; l < kF8Group; ++l) v[i][j][l] = v[i + 1][j][l];
+            read(v[kAhead - 1]);
         }
         return true;
     }
@@ -187,8 +209,8 @@ constexpr int kF8BN = 240, kF8Stages = 4;
 constexpr int kF8GemmThreads = 448;                       // warps 0-3 exponents, 4-11 output, 12 TMA loads, 13 tcgen05.mma
 constexpr int kF8OutWarps = 8;
 constexpr uint32_t kF8Staging = 4096;                     // per output warp: 32 rows of 128 bytes
-constexpr size_t kF8Smem = size_t(kF8Stages) * (kF8ABytes + kF8BN * kF8Block) + kF8OutWarps * kF8Staging + 1024 /* alignment */ +
-                           128 /* barriers */;
+constexpr size_t kF8Smem = size_t(kF8Stages) * (kF8ABytes + kF8BN * kF8Block) + kF8OutWarps * kF8Staging +
+                           F8Ring<kF8BN, kF8Stages>::kCells + 1024 /* alignment */ + 128 /* barriers */;
 
 struct F8Shape { int32_t m_tiles, n_tiles, blocks, total, group_m; };
 
@@ -284,7 +306,8 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
     const uint32_t raw = ptx::smem_addr(smem_raw), base = (raw + 1023u) & ~1023u;
     typedef F8Ring<kF8BN, kF8Stages> Ring;
     static_assert(2 * kF8BN + 2 * Ring::kSet <= 512, "two accumulators and two sets of exponents fit tensor memory");
-    const uint32_t staging = base + kF8Stages * Ring::kStage, bars = staging + kF8OutWarps * kF8Staging;
+    const uint32_t staging = base + kF8Stages * Ring::kStage, cells = staging + kF8OutWarps * kF8Staging;
+    const uint32_t bars = cells + Ring::kCells;
     const uint32_t full = bars, empty = full + 8 * kF8Stages, sfull = empty + 8 * kF8Stages, sempty = sfull + 16;
     const uint32_t acc_full = sempty + 16, acc_empty = acc_full + 16, slot = acc_empty + 16;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -321,7 +344,7 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
         for (int t = blockIdx.x; t < g.total && !timed_out; t += gridDim.x) {
             int mt, nt;
             f8_tile(g, t, mt, nt);
-            timed_out = !ring.scales(sa, sb, uint32_t(warp * 32) << 16, mt * kF8TileM, nt * kF8BN, 0, g.blocks);
+            timed_out = !ring.scales(sa, sb, cells, warp, uint32_t(warp * 32) << 16, mt * kF8TileM, nt * kF8BN, 0, g.blocks);
         }
     } else if (warp < 12) {
         const int q = warp & 3, half = (warp - 4) >> 2;
@@ -378,7 +401,7 @@ template <int BN> __host__ __device__ constexpr bool f8_overlay() { return BN >=
 template <int BN> __host__ __device__ constexpr int f8_stages() { return BN <= 16 ? 5 : BN <= 32 ? 4 : BN <= 64 ? 3 : 6; }
 template <int BN> __host__ __device__ constexpr uint32_t f8_ring() { return uint32_t(f8_stages<BN>()) * (kF8ABytes + BN * kF8Block); }
 template <int BN> __host__ __device__ constexpr uint32_t f8_body() { return f8_ring<BN>() + (f8_overlay<BN>() ? 0u : (BN + 8) * 128 * 4); }
-template <int BN> __host__ __device__ constexpr size_t f8_split_smem() { return f8_body<BN>() + 1024 /* alignment */ + 192 /* barriers */; }
+template <int BN> __host__ __device__ constexpr size_t f8_split_smem() { return f8_body<BN>() + F8Ring<BN, f8_stages<BN>()>::kCells + 1024 /* alignment */ + 192 /* barriers */; }
 
 struct F8SplitShape { int32_t col_tiles, blocks; };
 
@@ -393,8 +416,8 @@ fp8_split_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
     extern __shared__ uint8_t smem_raw[];
     // dynamic shared memory starts at the same address in every CTA of a kernel, so `sums` is common to the cluster
     const uint32_t raw = ptx::smem_addr(smem_raw), base = (raw + 1023u) & ~1023u;
-    const uint32_t sums = base + (f8_overlay<BN>() ? 0u : f8_ring<BN>()), bars = base + f8_body<BN>();
-    const uint32_t full = bars, empty = full + 8 * STAGES, sfull = empty + 8 * STAGES, sempty = sfull + 16, acc_full = sempty + 16, slot = acc_full + 8;
+    const uint32_t sums = base + (f8_overlay<BN>() ? 0u : f8_ring<BN>()), cells = base + f8_body<BN>();
+    const uint32_t bars = cells + Ring::kCells, full = bars, empty = full + 8 * STAGES, sfull = empty + 8 * STAGES, sempty = sfull + 16, acc_full = sempty + 16, slot = acc_full + 8;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int rank = int(ptx::cluster_ctarank());
     int splits;
@@ -445,7 +468,7 @@ fp8_split_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
         }
         __syncwarp();
     } else {
-        if (warp < 6) timed_out = !ring.scales(sa, sb, uint32_t(q * 32) << 16, rt * kF8TileM, ct * BN, k0, k1);
+        if (warp < 6) timed_out = !ring.scales(sa, sb, cells, warp - 2, uint32_t(q * 32) << 16, rt * kF8TileM, ct * BN, k0, k1);
         timed_out = !ptx::mbar_wait_warp<false>(acc_full, 0) || timed_out;
     }
     if (f8_overlay<BN>()) ptx::cluster_sync_all();       // every ring of the cluster has been consumed
