@@ -38,10 +38,114 @@ __device__ __forceinline__ uint32_t pack_e4m3x2(float lo, float hi) {
     return r;
 }
 
+// A thread's 8 x 8 elements as loaded (32 registers of bf16, 64 of fp32), magnitudes as bit patterns, which order
+// like the numbers: their maxima take one packed instruction per two bf16 elements, and a NaN or infinity shows in them.
+template <class T> struct QuantTile;
+template <> struct QuantTile<bf16_bits> {
+    uint32_t w[8][4];
+    static constexpr uint32_t kInfinity = 0x7f80;
+    __device__ __forceinline__ void load(int i, const bf16_bits* p, int cols, bool vec) {
+        if (cols >= 8 && vec) {
+            const uint4 v = __ldcs(reinterpret_cast<const uint4*>(p));
+            w[i][0] = v.x; w[i][1] = v.y; w[i][2] = v.z; w[i][3] = v.w;
+        } else {
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                w[i][j] = (2 * j < cols ? uint32_t(p[2 * j]) : 0u) | (2 * j + 1 < cols ? uint32_t(p[2 * j + 1]) << 16 : 0u);
+        }
+    }
+    __device__ __forceinline__ float get(int i, int j) const { return j % 2 ? bf16_hi(w[i][j / 2]) : bf16_lo(w[i][j / 2]); }
+    __device__ __forceinline__ void clear_bad() {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                if ((w[i][j] & 0x7f80u) == 0x7f80u) w[i][j] &= 0xffff0000u;
+                if ((w[i][j] & 0x7f800000u) == 0x7f800000u) w[i][j] &= 0xffffu;
+            }
+    }
+    // Largest magnitudes of the columns, and of the thread.
+    __device__ __forceinline__ uint32_t columns(uint32_t (&top)[8]) const {
+        uint32_t all = 0;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            uint32_t m = 0;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) m = __vmaxu2(m, w[i][j] & 0x7fff7fffu);
+            top[2 * j] = m & 0xffffu;
+            top[2 * j + 1] = m >> 16;
+            all = __vmaxu2(all, m);
+        }
+        return max(all & 0xffffu, all >> 16);
+    }
+    // ... of the rows, over the 16 lanes that share them
+    __device__ __forceinline__ void rows(uint32_t (&top)[8]) const {
+#pragma unroll
+        for (int i = 0; i < 8; i += 2) {
+            uint32_t m[2];
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                m[k] = __vmaxu2(__vmaxu2(w[i + k][0] & 0x7fff7fffu, w[i + k][1] & 0x7fff7fffu),
+                                __vmaxu2(w[i + k][2] & 0x7fff7fffu, w[i + k][3] & 0x7fff7fffu));
+                m[k] = __vmaxu2(m[k], m[k] >> 16);
+            }
+            uint32_t both = (m[0] & 0xffffu) | m[1] << 16;
+#pragma unroll
+            for (int o = 8; o > 0; o >>= 1) both = __vmaxu2(both, __shfl_xor_sync(0xffffffffu, both, o));
+            top[i] = both & 0xffffu;
+            top[i + 1] = both >> 16;
+        }
+    }
+    static __device__ __forceinline__ float magnitude(uint32_t bits) { return __uint_as_float(bits << 16); }
+};
+template <> struct QuantTile<float> {
+    float v[8][8];
+    static constexpr uint32_t kInfinity = 0x7f800000;
+    __device__ __forceinline__ void load(int i, const float* p, int cols, bool vec) {
+        if (cols >= 8 && vec) {
+            load_vec<8>(p, v[i]);
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[i][j] = j < cols ? p[j] : 0.f;
+        }
+    }
+    __device__ __forceinline__ float get(int i, int j) const { return v[i][j]; }
+    __device__ __forceinline__ void clear_bad() {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                if (!is_finite(v[i][j])) v[i][j] = 0;
+    }
+    __device__ __forceinline__ uint32_t bits(int i, int j) const { return __float_as_uint(v[i][j]) & 0x7fffffffu; }
+    __device__ __forceinline__ uint32_t columns(uint32_t (&top)[8]) const {
+        uint32_t all = 0;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            top[j] = 0;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) top[j] = max(top[j], bits(i, j));
+            all = max(all, top[j]);
+        }
+        return all;
+    }
+    __device__ __forceinline__ void rows(uint32_t (&top)[8]) const {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            top[i] = 0;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) top[i] = max(top[i], bits(i, j));
+#pragma unroll
+            for (int o = 8; o > 0; o >>= 1) top[i] = max(top[i], __shfl_xor_sync(0xffffffffu, top[i], o));
+        }
+    }
+    static __device__ __forceinline__ float magnitude(uint32_t bits) { return __uint_as_float(bits); }
+};
+
 template <class T, bool SQUARE>
-__global__ void __launch_bounds__(kQThreads) fp8_quantize_kernel(const QuantArgs a) {
+__global__ void __launch_bounds__(kQThreads, sizeof(T) == 2 ? 4 : 2) fp8_quantize_kernel(const QuantArgs a) {
     __shared__ __align__(16) uint8_t turned[kQTile * kQTile];
-    __shared__ float tops[8][kQTile];
+    __shared__ __align__(16) uint32_t tops[8][kQTile];
     __shared__ __align__(16) float inverse[kQTile];
     pdl_launch();
     pdl_wait();
@@ -49,60 +153,60 @@ __global__ void __launch_bounds__(kQThreads) fp8_quantize_kernel(const QuantArgs
     const int64_t mb = blockIdx.x / a.k_tiles, kb = blockIdx.x % a.k_tiles;
     const int64_t r0 = mb * kQTile + warp * 16 + half * 8, c0 = kb * kQTile + piece * 8;
     const int rows = int(a.M - r0 < 8 ? a.M - r0 : 8), cols = int(a.K - c0 < 8 ? a.K - c0 : 8);      // may be negative
-    float v[8][8];
+    QuantTile<T> x;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const T* p = static_cast<const T*>(a.x) + (r0 + i) * a.ldx + c0;
-        if (i < rows && cols == 8 && a.vec) {
-            load_vec<8>(p, v[i]);
-        } else {
+    for (int i = 0; i < 8; ++i) x.load(i, static_cast<const T*>(a.x) + (r0 + i) * a.ldx + c0, i < rows ? cols : 0, a.vec);
+    uint32_t top[8];
+    uint32_t most = x.columns(top);
+    if (most >= QuantTile<T>::kInfinity) {
+        x.clear_bad();
+        most = x.columns(top);
+        if (a.status) atomicOr(a.status, TPPO_DEV_NONFINITE);
+    }
+    // column maxima over the block: only what is transposed needs them
+    const bool columns = !SQUARE && a.qt;
+    if (columns) {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) v[i][j] = i < rows && j < cols ? load_f32(p + j) : 0.f;
+        for (int j = 0; j < 8; ++j) top[j] = max(top[j], __shfl_xor_sync(0xffffffffu, top[j], 16));
+        if (half == 0) {
+            *reinterpret_cast<uint4*>(&tops[warp][piece * 8]) = make_uint4(top[0], top[1], top[2], top[3]);
+            *reinterpret_cast<uint4*>(&tops[warp][piece * 8 + 4]) = make_uint4(top[4], top[5], top[6], top[7]);
         }
     }
-    bool bad = false;
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-#pragma unroll
-        for (int j = 0; j < 8; ++j)
-            if (!is_finite(v[i][j])) { v[i][j] = 0; bad = true; }
-    if (bad && a.status) atomicOr(a.status, TPPO_DEV_NONFINITE);
-
     int e_tile = 0;
     if (SQUARE) {
-        float top = 0;
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-#pragma unroll
-            for (int j = 0; j < 8; ++j) top = fmaxf(top, fabsf(v[i][j]));
-        top = warp_max(top);
-        if (lane == 0) tops[warp][0] = top;
+        most = __reduce_max_sync(0xffffffffu, most);
+        if (lane == 0) tops[warp][0] = most;
         __syncthreads();
-        for (int w = 0; w < 8; ++w) top = fmaxf(top, tops[w][0]);
-        e_tile = scale_exponent(top);
+        for (int w = 0; w < 8; ++w) most = max(most, tops[w][0]);
+        e_tile = scale_exponent(QuantTile<T>::magnitude(most));
         if (threadIdx.x == 0) {
             if (a.q) a.scale[mb * a.lds + kb] = power_of_two(e_tile);
             if (a.qt) a.scale_t[kb * a.ldst + mb] = power_of_two(e_tile);
         }
+    } else if (columns) {
+        __syncthreads();
+        if (threadIdx.x < kQTile) {
+            uint32_t t = 0;
+#pragma unroll
+            for (int w = 0; w < 8; ++w) t = max(t, tops[w][threadIdx.x]);
+            const int e = scale_exponent(QuantTile<T>::magnitude(t));
+            inverse[threadIdx.x] = power_of_two(-e);
+            const int64_t c = kb * kQTile + threadIdx.x;
+            if (c < a.K) a.scale_t[mb * a.ldst + c] = power_of_two(e);
+        }
     }
     if (a.q) {
+        if (!SQUARE) x.rows(top);
         float mine = 0;                                   // lane `piece` of the half keeps the scale of row `piece`
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            int e = e_tile;
-            if (!SQUARE) {
-                float top = 0;
-#pragma unroll
-                for (int j = 0; j < 8; ++j) top = fmaxf(top, fabsf(v[i][j]));
-#pragma unroll
-                for (int o = 8; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-                e = scale_exponent(top);
-                if (piece == i) mine = power_of_two(e);
-            }
+            const int e = SQUARE ? e_tile : scale_exponent(QuantTile<T>::magnitude(top[i]));
+            if (piece == i) mine = power_of_two(e);
             const float inv = power_of_two(-e);
             uint32_t w[4];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) w[j] = pack_e4m3x2(v[i][2 * j] * inv, v[i][2 * j + 1] * inv);
+            for (int j = 0; j < 4; ++j) w[j] = pack_e4m3x2(x.get(i, 2 * j) * inv, x.get(i, 2 * j + 1) * inv);
             if (i < rows && cols > 0) {
                 uint8_t* p = a.q + (r0 + i) * a.ldq + c0;
                 if (cols == 8) {
@@ -117,36 +221,13 @@ __global__ void __launch_bounds__(kQThreads) fp8_quantize_kernel(const QuantArgs
         if (!SQUARE && piece < rows) a.scale[kb * a.lds + r0 + piece] = mine;
     }
     if (!a.qt) return;
-    if (!SQUARE) {
-        float top[8];
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            top[j] = 0;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) top[j] = fmaxf(top[j], fabsf(v[i][j]));
-            top[j] = fmaxf(top[j], __shfl_xor_sync(0xffffffffu, top[j], 16));
-        }
-        if (half == 0) {
-#pragma unroll
-            for (int j = 0; j < 8; ++j) tops[warp][piece * 8 + j] = top[j];
-        }
-        __syncthreads();
-        if (threadIdx.x < kQTile) {
-            float t = 0;
-            for (int w = 0; w < 8; ++w) t = fmaxf(t, tops[w][threadIdx.x]);
-            const int e = scale_exponent(t);
-            inverse[threadIdx.x] = power_of_two(-e);
-            const int64_t c = kb * kQTile + threadIdx.x;
-            if (c < a.K) a.scale_t[mb * a.ldst + c] = power_of_two(e);
-        }
-        __syncthreads();
-    }
+    if (columns) __syncthreads();
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
         const float inv = SQUARE ? power_of_two(-e_tile) : inverse[piece * 8 + j];
         uint32_t w[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) w[i] = pack_e4m3x2(v[2 * i][j] * inv, v[2 * i + 1][j] * inv);
+        for (int i = 0; i < 4; ++i) w[i] = pack_e4m3x2(x.get(2 * i, j) * inv, x.get(2 * i + 1, j) * inv);
         const int unit = (warp * 2 + half) ^ piece;
         *reinterpret_cast<uint2*>(turned + (piece * 8 + j) * kQTile + unit * 8) = make_uint2(w[0] | w[1] << 16, w[2] | w[3] << 16);
     }
