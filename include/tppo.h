@@ -611,8 +611,7 @@ int tppo_residual_norm_fwd(const void *z, int64_t ldz, const void *residual, int
  *               row stride
  *   dgate       like gate ([N] of `param_dtype` with ldg = 0, or [M, N] of `dtype` with row stride lddg) or NULL
  *   dgamma_post, dgamma_pre [N] of `param_dtype` or NULL; overwritten, not accumulated
- *   workspace   tppo_workspace_bytes(TPPO_OP_RESIDUAL_NORM, M, 0, 0, N) bytes; may be NULL when no column sums
- *               (dgamma_post, dgamma_pre, dgate of a row) are asked for
+ *   workspace   tppo_workspace_bytes(TPPO_OP_RESIDUAL_NORM, M, 0, 0, N) bytes
  * A row without statistics (an rstd of 0) contributes nothing and gets gradients of 0; so does a row in which a
  * gradient, activation or parameter that enters a product above is not finite or makes its sums so, which raises
  * TPPO_DEV_NONFINITE.  Elements and sums over rows that leave the range of their type become infinities.  M = 0

@@ -21,14 +21,12 @@
 // hold elements of neighbouring rows or of nothing (a piece with one element of the row in it is mapped), masked
 // when they are used and stored element by element.  A block only takes rows that start at the same place of
 // a piece, so that a thread's columns, parameters and column sums stay its own.
-// Rows that do not fit, and matrices whose rows do not start at the same place of a piece, take one block per
-// row and read it again for each sweep.
+// Rows that do not fit, and matrices whose rows do not start at the same place of a piece, are read again for each sweep.
 #include "dense_common.cuh"
 
 namespace tppo {
 namespace {
 
-constexpr int kJoinThreads = 640;                         // of a block at up to 48 elements per thread
 constexpr int kJoinSmem = 224 * 1024;
 constexpr int kJoinAnyThreads = 512, kJoinAnyBlocks = kNumSms * 2;
 constexpr int kJoinStages = 4;
@@ -45,6 +43,7 @@ struct JoinArgs {
     void* out[3]; int64_t ldo[3];                         // h, n | dz, dresidual, dgate
     float* r_post; float* r_pre;                          // out | in; NULL in the backward pass: no such norm
     float* partial;                                       // column sums: [blocks][2][N]
+    float4* rows;                                         // r1, r2, k1, k2 of every row, where two launches share the work
     int32_t* status;
     int64_t M; int32_t N; float alpha, eps; int32_t norms;
     int32_t T, groups, stages, arrays;                    // threads per group; groups per block; stages; matrices per stage
@@ -75,14 +74,15 @@ __device__ __forceinline__ void copy_wait(int stages) {
     }
 }
 
-// A thread's pieces of a row: piece c covers columns col(c) .. col(c) + VEC - 1.
-template <class T, int E>
+// A thread's pieces of a row: piece c covers columns col(c) .. col(c) + VEC - 1.  SHIFT: rows need not start on a
+// 16-byte boundary, or end on one; pieces may then lie partly outside the row.
+template <class T, bool SHIFT>
 struct JoinColumns {
     static constexpr int VEC = Join<T>::VEC;
     int first, step, N;
     __device__ __forceinline__ int col(int c) const { return first + c * step; }
-    __device__ __forceinline__ bool any(int c) const { return col(c) < N && col(c) + VEC > 0; }
-    __device__ __forceinline__ bool all(int c) const { return col(c) >= 0 && col(c) + VEC <= N; }
+    __device__ __forceinline__ bool any(int c) const { return col(c) < N && (!SHIFT || col(c) + VEC > 0); }
+    __device__ __forceinline__ bool all(int c) const { return !SHIFT || (col(c) >= 0 && col(c) + VEC <= N); }
     __device__ __forceinline__ bool has(int c, int i) const { return unsigned(col(c) + i) < unsigned(N); }
 };
 
@@ -114,16 +114,6 @@ __device__ __forceinline__ void join_store(const C& k, int c, T* row, const floa
             if (k.has(c, i)) store_f32(row + k.col(c) + i, v[i]);
     }
 }
-// VEC parameters of piece p, kept as planes of float4 so that neighbouring threads read neighbouring 16 bytes.
-template <int VEC>
-__device__ __forceinline__ void join_params(uint32_t base, int p, int pieces, float (&v)[VEC]) {
-#pragma unroll
-    for (int j = 0; j < VEC / 4; ++j) {
-        const uint4 w = ptx::lds128(base + (j * pieces + p) * 16);
-        v[4 * j] = __uint_as_float(w.x); v[4 * j + 1] = __uint_as_float(w.y);
-        v[4 * j + 2] = __uint_as_float(w.z); v[4 * j + 3] = __uint_as_float(w.w);
-    }
-}
 
 // Sums over a group's warps in a fixed order.  `red`: two sets of V * 32 floats per group, used in turn, so that
 // one barrier per sum suffices.
@@ -141,25 +131,33 @@ struct GroupSum {
             for (int i = 0; i < V; ++i) r[i * 32 + warp] = v[i];
         }
         asm volatile("bar.sync %0, %1;" ::"r"(bar), "r"(threads) : "memory");
+        float4 s[V];
 #pragma unroll
-        for (int i = 0; i < V; ++i) v[i] = 0;
-        for (int w = 0; w < warps; ++w) {
+        for (int i = 0; i < V; ++i) s[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int w = 0; w < warps; w += 4) {              // places of warps that the group does not have stay 0
 #pragma unroll
-            for (int i = 0; i < V; ++i) v[i] += r[i * 32 + w];
+            for (int i = 0; i < V; ++i) {
+                const float4 p = *reinterpret_cast<const float4*>(r + i * 32 + w);
+                s[i].x += p.x; s[i].y += p.y; s[i].z += p.z; s[i].w += p.w;
+            }
         }
+#pragma unroll
+        for (int i = 0; i < V; ++i) v[i] = (s[i].x + s[i].y) + (s[i].z + s[i].w);
     }
 };
 constexpr int kJoinRedBytes = 20 * 2 * 3 * 32 * 4;        // 20 groups
 
-// What both passes set up: this thread's group, columns, ring and the parameters in shared memory.
-template <class T, int E, int IN>
+// What both passes set up: this thread's group, columns, ring and parameters.  REGS: the parameters of its columns are in
+// registers, else in the block's shared memory.
+template <class T, int E, bool SHIFT, bool REGS, int IN>
 struct JoinThread {
     static constexpr int VEC = Join<T>::VEC, CH = E / VEC;
     int t, group, pieces;
-    JoinColumns<T, E> k;
-    uint32_t ring, post, pre;
+    JoinColumns<T, SHIFT> k;
+    uint32_t post_at, pre_at, ring;
     int64_t row, step;                                    // first row, rows between two of this group
     GroupSum sum;
+    float post_reg[REGS ? CH : 1][VEC], pre_reg[REGS ? CH : 1][VEC];
 
     __device__ __forceinline__ JoinThread(const JoinArgs& a, uint8_t* smem) {
         group = int(threadIdx.x) / a.T;
@@ -167,16 +165,20 @@ struct JoinThread {
         pieces = a.T * CH;
         row = int64_t(blockIdx.x) + int64_t(group) * gridDim.x;
         step = int64_t(a.groups) * gridDim.x;
-        const uintptr_t start = reinterpret_cast<uintptr_t>(a.in[kZ]) / sizeof(T);
-        const int shift = int((start + uint64_t(row) * uint64_t(a.shift_step)) % VEC);
+        int shift = 0;
+        if (SHIFT) {
+            const uintptr_t start = reinterpret_cast<uintptr_t>(a.in[kZ]) / sizeof(T);
+            shift = int((start + uint64_t(row) * uint64_t(a.shift_step)) % VEC);
+        }
         k.first = t * VEC - shift;
         k.step = a.T * VEC;
         k.N = a.N;
         float* red = reinterpret_cast<float*>(smem);
+        for (int i = int(threadIdx.x); i < kJoinRedBytes / 4; i += int(blockDim.x)) red[i] = 0.f;
         sum = GroupSum{red + group * 2 * 3 * 32, a.T / 32, t / 32, a.groups == 1 ? 0 : group + 1, a.T, 0};
-        post = ptx::smem_addr(smem) + kJoinRedBytes;
-        pre = post + uint32_t(pieces) * VEC * 4;
-        ring = pre + uint32_t(pieces) * VEC * 4 + uint32_t(group * a.stages * a.arrays) * uint32_t(pieces) * 16;
+        post_at = ptx::smem_addr(smem) + kJoinRedBytes;
+        pre_at = post_at + uint32_t(pieces) * VEC * 4;
+        ring = (REGS ? post_at : pre_at + uint32_t(pieces) * VEC * 4) + uint32_t(group * a.stages * a.arrays) * uint32_t(pieces) * 16;
     }
     __device__ __forceinline__ uint32_t at(const JoinArgs& a, int stage, int m, int c) const {
         return ring + (uint32_t((stage * a.arrays + a.slot[m]) * CH + c) * uint32_t(a.T) + uint32_t(t)) * 16;
@@ -195,73 +197,131 @@ struct JoinThread {
         }
         copy_commit();
     }
-    // The block's parameters: gate row * gamma_post, gamma_pre; 0 outside the row.
-    __device__ __forceinline__ void params(const JoinArgs& a, uint8_t* smem) const {
-        float* q = reinterpret_cast<float*>(smem + kJoinRedBytes);
-        const int shift = t * VEC - k.first;
-        for (int e = int(threadIdx.x); e < pieces * VEC; e += int(blockDim.x)) {
-            const int col = e - shift, at = (e % VEC / 4 * pieces + e / VEC) * 4 + e % 4;
-            const bool in = unsigned(col) < unsigned(a.N);
-            q[at] = in ? param(a.gate_row, col, a.p32) * param(a.gamma_post, col, a.p32) : 0.f;
-            q[at + pieces * VEC] = in ? param(a.gamma_pre, col, a.p32) : 0.f;
+    // gate row * gamma_post and gamma_pre; 0 outside the row.  Shared memory keeps them as planes of float4, so that
+    // neighbouring threads read neighbouring 16 bytes.
+    __device__ __forceinline__ void load_params(const JoinArgs& a, uint8_t* smem) {
+        if constexpr (REGS) {
+#pragma unroll
+            for (int c = 0; c < CH; ++c)
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) {
+                    const int col = k.col(c) + i;
+                    const bool in = k.has(c, i);
+                    post_reg[c][i] = in ? param(a.gate_row, col, a.p32) * param(a.gamma_post, col, a.p32) : 0.f;
+                    pre_reg[c][i] = in ? param(a.gamma_pre, col, a.p32) : 0.f;
+                }
+        } else {
+            float* q = reinterpret_cast<float*>(smem + kJoinRedBytes);
+            const int shift = t * VEC - k.first;
+#pragma unroll 4
+            for (int e = int(threadIdx.x); e < pieces * VEC; e += int(blockDim.x)) {
+                const int col = e - shift, to = (e % VEC / 4 * pieces + e / VEC) * 4 + e % 4;
+                const bool in = unsigned(col) < unsigned(a.N);
+                q[to] = in ? param(a.gate_row, col, a.p32) * param(a.gamma_post, col, a.p32) : 0.f;
+                q[to + pieces * VEC] = in ? param(a.gamma_pre, col, a.p32) : 0.f;
+            }
         }
+    }
+    __device__ __forceinline__ void params(uint32_t base, const float (&reg)[REGS ? CH : 1][VEC], int c, int threads, float (&v)[VEC]) const {
+        if constexpr (REGS) {
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) v[i] = reg[c][i];
+        } else {
+#pragma unroll
+            for (int j = 0; j < VEC / 4; ++j) {
+                const uint4 w = ptx::lds128(base + (j * pieces + c * threads + t) * 16);
+                v[4 * j] = __uint_as_float(w.x); v[4 * j + 1] = __uint_as_float(w.y);
+                v[4 * j + 2] = __uint_as_float(w.z); v[4 * j + 3] = __uint_as_float(w.w);
+            }
+        }
+    }
+    __device__ __forceinline__ void params(uint32_t base, const float (&reg)[REGS ? CH : 1][VEC], int c, int threads, uint64_t (&v)[VEC / 2]) const {
+        if constexpr (REGS) {
+#pragma unroll
+            for (int i = 0; i < VEC / 2; ++i) v[i] = ptx::pack_f32x2(reg[c][2 * i], reg[c][2 * i + 1]);
+        } else {
+#pragma unroll
+            for (int j = 0; j < VEC / 4; ++j)
+                asm volatile("ld.shared.v2.u64 {%0, %1}, [%2];" : "=l"(v[2 * j]), "=l"(v[2 * j + 1]) : "r"(base + (j * pieces + c * threads + t) * 16));
+        }
+    }
+    template <class V> __device__ __forceinline__ void post(const JoinArgs& a, int c, V& v) const { params(post_at, post_reg, c, a.T, v); }
+    template <class V> __device__ __forceinline__ void pre(const JoinArgs& a, int c, V& v) const { params(pre_at, pre_reg, c, a.T, v); }
+    __device__ __forceinline__ void store_zeros(T* row) const {
+        float zero[VEC];
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) zero[i] = 0.f;
+#pragma unroll
+        for (int c = 0; c < CH; ++c)
+            if (k.any(c)) join_store<T>(k, c, row, zero);
     }
 };
 
-template <class T, int E>
-__global__ void __launch_bounds__(E <= 16 ? 1024 : kJoinThreads, 1) join_fwd_kernel(const __grid_constant__ JoinArgs a) {
+// Elements per thread, with how many threads in a block they go, and where the parameters are.
+__host__ __device__ constexpr int join_fwd_threads(int e) { return e == 32 ? 512 : 640; }
+__host__ __device__ constexpr bool join_fwd_regs(int e) { return e <= 32; }
+__host__ __device__ constexpr bool join_bwd_regs(int e) { return e <= 8; }
+
+template <class T, int E, bool GATED, bool SHIFT>
+__global__ void __launch_bounds__(join_fwd_threads(E), 1) join_fwd_kernel(const __grid_constant__ JoinArgs a) {
     extern __shared__ __align__(16) uint8_t smem[];
-    typedef JoinThread<T, E, kFwdIn> Thread;
+    typedef JoinThread<T, E, SHIFT, join_fwd_regs(E), kFwdIn> Thread;
     constexpr int VEC = Thread::VEC, CH = Thread::CH;
     Thread th(a, smem);
     pdl_launch();
     pdl_wait();
     for (int s = 0; s < a.stages; ++s) th.fetch(a, th.row + s * th.step, s);
-    th.params(a, smem);
+    th.load_params(a, smem);
     __syncthreads();
-    const bool post = a.norms & TPPO_NORM_POST, pre = a.norms & TPPO_NORM_PRE, gated = a.in[kGate] != nullptr;
+    const bool post = a.norms & TPPO_NORM_POST, pre = a.norms & TPPO_NORM_PRE;
     const float inv = 1.f / float(a.N);
     int stage = 0;
     for (int64_t r = th.row; r < a.M; r += th.step) {
         copy_wait(a.stages);
-        float r1 = 1.f, s[1] = {0.f};
+        float r1 = 1.f, s[1];
         bool good = true;
         if (post) {
+            float q[2] = {0.f, 0.f};
 #pragma unroll
             for (int c = 0; c < CH; ++c) {
                 if (!th.k.any(c)) continue;
                 float z[VEC];
                 join_piece<T>(th.k, c, th.at(a, stage, kZ, c), z);
 #pragma unroll
-                for (int i = 0; i < VEC; ++i) s[0] = fmaf(z[i], z[i], s[0]);
+                for (int i = 0; i < VEC; ++i) q[i & 1] = fmaf(z[i], z[i], q[i & 1]);
             }
+            s[0] = q[0] + q[1];
             th.sum(s);
             r1 = rsqrtf(fmaf(s[0], inv, a.eps));
             good = is_finite(s[0]) && is_finite(r1);
         }
-        float h[CH][VEC];
-        s[0] = 0;
+        float h[CH][VEC], q[2] = {0.f, 0.f};
 #pragma unroll
         for (int c = 0; c < CH; ++c) {
             if (!th.k.any(c)) continue;
             float z[VEC], g[VEC];
             join_piece<T>(th.k, c, th.at(a, stage, kZ, c), z);
             join_piece<T>(th.k, c, th.at(a, stage, kRes, c), h[c]);
-            join_params<VEC>(th.post, c * a.T + th.t, th.pieces, g);
-            if (gated) {
+            th.post(a, c, g);
+            if (GATED) {
                 float w[VEC];
                 join_piece<T>(th.k, c, th.at(a, stage, kGate, c), w);
 #pragma unroll
                 for (int i = 0; i < VEC; ++i) g[i] *= w[i];
             }
 #pragma unroll
-            for (int i = 0; i < VEC; ++i) {
-                h[c][i] = fmaf(z[i] * r1, g[i], a.alpha * h[c][i]);
-                s[0] = pre ? fmaf(h[c][i], h[c][i], s[0]) : s[0] + fabsf(h[c][i]);
+            for (int i = 0; i < VEC; ++i) h[c][i] = fmaf(z[i] * r1, g[i], a.alpha * h[c][i]);
+            if (pre) {
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) q[i & 1] = fmaf(h[c][i], h[c][i], q[i & 1]);
+            } else {
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) q[i & 1] += fabsf(h[c][i]);
             }
         }
         th.fetch(a, r + a.stages * th.step, stage);
         if (++stage == a.stages) stage = 0;
+        s[0] = q[0] + q[1];
         th.sum(s);
         const float r2 = pre ? rsqrtf(fmaf(s[0], inv, a.eps)) : 1.f;
         good = good && is_finite(s[0]) && is_finite(r2);
@@ -272,19 +332,20 @@ __global__ void __launch_bounds__(E <= 16 ? 1024 : kJoinThreads, 1) join_fwd_ker
         }
         T* ho = static_cast<T*>(a.out[0]) + r * a.ldo[0];
         T* no = static_cast<T*>(a.out[1]) + (pre ? r * a.ldo[1] : 0);
+        if (!good) {                                      // the same for the whole group
+            th.store_zeros(ho);
+            if (pre) th.store_zeros(no);
+            continue;
+        }
 #pragma unroll
         for (int c = 0; c < CH; ++c) {
             if (!th.k.any(c)) continue;
-            if (!good) {
-#pragma unroll
-                for (int i = 0; i < VEC; ++i) h[c][i] = 0;
-            }
             join_store<T>(th.k, c, ho, h[c]);
             if (pre) {
                 float g[VEC];
-                join_params<VEC>(th.pre, c * a.T + th.t, th.pieces, g);
+                th.pre(a, c, g);
 #pragma unroll
-                for (int i = 0; i < VEC; ++i) g[i] = good ? h[c][i] * r2 * g[i] : 0.f;
+                for (int i = 0; i < VEC; ++i) g[i] *= h[c][i] * r2;
                 join_store<T>(th.k, c, no, g);
             }
         }
@@ -293,7 +354,7 @@ __global__ void __launch_bounds__(E <= 16 ? 1024 : kJoinThreads, 1) join_fwd_ker
 
 // The scalars of a row's backward pass, from its three sums.
 struct JoinRow { float r1, r2, k2, k1; bool good; };
-__device__ __forceinline__ JoinRow join_row(const JoinArgs& a, float r1, float r2, const float (&s)[3]) {
+__device__ __forceinline__ JoinRow join_row(const JoinArgs& a, float r1, float r2, const float (&s)[3], bool reports) {
     const bool post = a.norms & TPPO_NORM_POST, pre = a.norms & TPPO_NORM_PRE;
     const float inv = 1.f / float(a.N);
     JoinRow w;
@@ -303,121 +364,185 @@ __device__ __forceinline__ JoinRow join_row(const JoinArgs& a, float r1, float r
     w.k1 = post ? (s[1] - w.k2 * s[2]) * inv * r1 * r1 * r1 : 0.f;        // dz = r1 a1 - k1 z
     const bool stats = !((post && r1 == 0.f) || (pre && r2 == 0.f));
     w.good = is_finite(s[0]) && is_finite(s[1]) && is_finite(s[2]) && is_finite(w.k2) && is_finite(w.k1);
-    if (!w.good && stats && threadIdx.x % a.T == 0 && a.status) atomicOr(a.status, TPPO_DEV_NONFINITE);
+    if (!w.good && stats && reports && a.status) atomicOr(a.status, TPPO_DEV_NONFINITE);
     w.good = w.good && stats;
     return w;
 }
 
-template <class T, int E>
-__global__ void __launch_bounds__(kJoinThreads, 1) join_bwd_kernel(const __grid_constant__ JoinArgs a) {
+// Pairs of fp32 values, on which one instruction works at a time: at some 30 operations per element the backward pass of
+// bf16 rows is otherwise bound by its instructions.
+template <class T> struct JoinPairs { static constexpr int N = Join<T>::VEC / 2; };
+template <class T, class C>
+__device__ __forceinline__ void join_piece(const C& k, int c, uint32_t at, uint64_t (&v)[JoinPairs<T>::N]) {
+    if (k.all(c)) {
+        if constexpr (sizeof(T) == 2) {
+            const uint4 w = ptx::lds128(at);
+            v[0] = ptx::pack_f32x2(bf16_lo(w.x), bf16_hi(w.x));
+            v[1] = ptx::pack_f32x2(bf16_lo(w.y), bf16_hi(w.y));
+            v[2] = ptx::pack_f32x2(bf16_lo(w.z), bf16_hi(w.z));
+            v[3] = ptx::pack_f32x2(bf16_lo(w.w), bf16_hi(w.w));
+        } else {
+            asm volatile("ld.shared.v2.u64 {%0, %1}, [%2];" : "=l"(v[0]), "=l"(v[1]) : "r"(at));
+        }
+    } else {
+        float f[Join<T>::VEC];
+        join_piece<T>(k, c, at, f);
+#pragma unroll
+        for (int i = 0; i < JoinPairs<T>::N; ++i) v[i] = ptx::pack_f32x2(f[2 * i], f[2 * i + 1]);
+    }
+}
+template <class T, class C>
+__device__ __forceinline__ void join_store(const C& k, int c, T* row, const uint64_t (&v)[JoinPairs<T>::N]) {
+    if (k.all(c)) {
+        uint4 w;
+        if constexpr (sizeof(T) == 2)
+            w = make_uint4(ptx::pack_bf16x2_from_f32x2(v[0]), ptx::pack_bf16x2_from_f32x2(v[1]), ptx::pack_bf16x2_from_f32x2(v[2]),
+                           ptx::pack_bf16x2_from_f32x2(v[3]));
+        else
+            w = make_uint4(uint32_t(v[0]), uint32_t(v[0] >> 32), uint32_t(v[1]), uint32_t(v[1] >> 32));
+        *reinterpret_cast<uint4*>(row + k.col(c)) = w;
+    } else {
+#pragma unroll
+        for (int i = 0; i < Join<T>::VEC; ++i) {
+            float lo, hi;
+            ptx::unpack_f32x2(v[i / 2], lo, hi);
+            if (k.has(c, i)) store_f32(row + k.col(c) + i, i % 2 ? hi : lo);
+        }
+    }
+}
+
+// The fewer threads share a row, the less its sums and copies cost; the registers of 32 columns' gradients then leave room
+// for 320 threads.
+__host__ __device__ constexpr int join_bwd_threads(int e) { return e == 32 ? 320 : 640; }
+
+template <class T, int E, bool PRE, bool GATED, bool SHIFT>
+__global__ void __launch_bounds__(join_bwd_threads(E), 1) join_bwd_kernel(const __grid_constant__ JoinArgs a) {
     extern __shared__ __align__(16) uint8_t smem[];
-    typedef JoinThread<T, E, kBwdIn> Thread;
-    constexpr int VEC = Thread::VEC, CH = Thread::CH;
+    typedef JoinThread<T, E, SHIFT, join_bwd_regs(E), kBwdIn> Thread;
+    constexpr int VEC = Thread::VEC, CH = Thread::CH, P = VEC / 2;
     Thread th(a, smem);
     pdl_launch();
     pdl_wait();
     for (int s = 0; s < a.stages; ++s) th.fetch(a, th.row + s * th.step, s);
-    th.params(a, smem);
+    th.load_params(a, smem);
     __syncthreads();
-    const bool pre = a.norms & TPPO_NORM_PRE, gated = a.in[kGate] != nullptr, add = a.in[kDh] != nullptr;
-    float sum_post[CH][VEC], sum_pre[CH][VEC];
+    using ptx::fma_f32x2;
+    using ptx::mul_f32x2;
+    const bool add = a.in[kDh] != nullptr, post = a.norms & TPPO_NORM_POST;
+    uint64_t sum_post[CH][P], sum_pre[CH][P];
 #pragma unroll
     for (int c = 0; c < CH; ++c)
 #pragma unroll
-        for (int i = 0; i < VEC; ++i) sum_post[c][i] = sum_pre[c][i] = 0;
+        for (int i = 0; i < P; ++i) sum_post[c][i] = sum_pre[c][i] = 0;
     int stage = 0;
-    const bool post = a.norms & TPPO_NORM_POST;
-    float r1_next = post && th.row < a.M ? a.r_post[th.row] : 1.f, r2_next = pre && th.row < a.M ? a.r_pre[th.row] : 0.f;
+    float r1_next = post && th.row < a.M ? a.r_post[th.row] : 1.f, r2_next = PRE && th.row < a.M ? a.r_pre[th.row] : 0.f;
     for (int64_t r = th.row; r < a.M; r += th.step) {
         const float r1 = r1_next, r2 = r2_next;
         if (r + th.step < a.M) {                          // a row ahead, like the copies
             if (post) r1_next = a.r_post[r + th.step];
-            if (pre) r2_next = a.r_pre[r + th.step];
+            if (PRE) r2_next = a.r_pre[r + th.step];
         }
         copy_wait(a.stages);
-        float s[3] = {0.f, 0.f, 0.f};
+        const uint64_t r2_2 = ptx::pack_f32x2(r2, r2);
+        uint64_t q[3] = {0, 0, 0};
 #pragma unroll
         for (int c = 0; c < CH; ++c) {
             if (!th.k.any(c)) continue;
-            float w[VEC], d[VEC], g[VEC];
+            uint64_t w[P], d[P], g[P];
             join_piece<T>(th.k, c, th.at(a, stage, kZ, c), w);
-            join_params<VEC>(th.post, c * a.T + th.t, th.pieces, g);
+            th.post(a, c, g);
 #pragma unroll
-            for (int i = 0; i < VEC; ++i) w[i] *= g[i];
-            if (gated) {
+            for (int i = 0; i < P; ++i) w[i] = mul_f32x2(w[i], g[i]);
+            if (GATED) {
                 join_piece<T>(th.k, c, th.at(a, stage, kGate, c), g);
 #pragma unroll
-                for (int i = 0; i < VEC; ++i) w[i] *= g[i];
+                for (int i = 0; i < P; ++i) w[i] = mul_f32x2(w[i], g[i]);
             }
 #pragma unroll
-            for (int i = 0; i < VEC; ++i) d[i] = 0;
+            for (int i = 0; i < P; ++i) d[i] = 0;
             if (add) join_piece<T>(th.k, c, th.at(a, stage, kDh, c), d);
-            if (pre) {
-                float n[VEC], h[VEC];
+            if (PRE) {
+                uint64_t n[P], h[P];
                 join_piece<T>(th.k, c, th.at(a, stage, kDn, c), n);
                 join_piece<T>(th.k, c, th.at(a, stage, kH, c), h);
-                join_params<VEC>(th.pre, c * a.T + th.t, th.pieces, g);
+                th.pre(a, c, g);
 #pragma unroll
-                for (int i = 0; i < VEC; ++i) {
-                    const float a2 = n[i] * g[i];
-                    s[0] = fmaf(a2, h[i], s[0]);
-                    s[2] = fmaf(h[i], w[i], s[2]);
-                    d[i] = fmaf(r2, a2, d[i]);
+                for (int i = 0; i < P; ++i) {
+                    n[i] = mul_f32x2(n[i], g[i]);
+                    q[0] = fma_f32x2(n[i], h[i], q[0]);
+                    q[2] = fma_f32x2(h[i], w[i], q[2]);
+                    d[i] = fma_f32x2(r2_2, n[i], d[i]);
                 }
             }
 #pragma unroll
-            for (int i = 0; i < VEC; ++i) s[1] = fmaf(d[i], w[i], s[1]);
+            for (int i = 0; i < P; ++i) q[1] = fma_f32x2(d[i], w[i], q[1]);
+        }
+        float s[3];
+#pragma unroll
+        for (int i = 0; i < 3; ++i) {
+            float lo, hi;
+            ptx::unpack_f32x2(q[i], lo, hi);
+            s[i] = lo + hi;
         }
         th.sum(s);
-        const JoinRow w = join_row(a, r1, r2, s);
+        const JoinRow w = join_row(a, r1, r2, s, th.t == 0);
         T* dz = static_cast<T*>(a.out[0]) + (a.out[0] ? r * a.ldo[0] : 0);
         T* dres = static_cast<T*>(a.out[1]) + (a.out[1] ? r * a.ldo[1] : 0);
         T* dgate = static_cast<T*>(a.out[2]) + (a.out[2] ? r * a.ldo[2] : 0);
+        if (w.good) {
+            const uint64_t r1_2 = ptx::pack_f32x2(w.r1, w.r1), k1_2 = ptx::pack_f32x2(-w.k1, -w.k1), k2_2 = ptx::pack_f32x2(-w.k2, -w.k2);
+            const uint64_t alpha_2 = ptx::pack_f32x2(a.alpha, a.alpha);
 #pragma unroll
-        for (int c = 0; c < CH; ++c) {
-            if (!th.k.any(c)) continue;
-            float z[VEC], d[VEC], g[VEC], v[VEC];
+            for (int c = 0; c < CH; ++c) {
+                if (!th.k.any(c)) continue;
+                uint64_t z[P], d[P], g[P], v[P];
 #pragma unroll
-            for (int i = 0; i < VEC; ++i) d[i] = 0;
-            if (add) join_piece<T>(th.k, c, th.at(a, stage, kDh, c), d);
-            if (pre) {
-                float n[VEC], h[VEC];
-                join_piece<T>(th.k, c, th.at(a, stage, kDn, c), n);
-                join_piece<T>(th.k, c, th.at(a, stage, kH, c), h);
-                join_params<VEC>(th.pre, c * a.T + th.t, th.pieces, g);
+                for (int i = 0; i < P; ++i) d[i] = 0;
+                if (add) join_piece<T>(th.k, c, th.at(a, stage, kDh, c), d);
+                if (PRE) {
+                    uint64_t n[P], h[P];
+                    join_piece<T>(th.k, c, th.at(a, stage, kDn, c), n);
+                    join_piece<T>(th.k, c, th.at(a, stage, kH, c), h);
+                    th.pre(a, c, g);
 #pragma unroll
-                for (int i = 0; i < VEC; ++i) {
-                    if (w.good) sum_pre[c][i] = fmaf(n[i], h[i] * w.r2, sum_pre[c][i]);
-                    d[i] = fmaf(-w.k2, h[i], fmaf(w.r2, n[i] * g[i], d[i]));
+                    for (int i = 0; i < P; ++i) {
+                        n[i] = mul_f32x2(n[i], r2_2);
+                        sum_pre[c][i] = fma_f32x2(n[i], h[i], sum_pre[c][i]);
+                        d[i] = fma_f32x2(k2_2, h[i], fma_f32x2(n[i], g[i], d[i]));
+                    }
+                }
+                if (a.out[1]) {
+#pragma unroll
+                    for (int i = 0; i < P; ++i) v[i] = mul_f32x2(alpha_2, d[i]);
+                    join_store<T>(th.k, c, dres, v);
+                }
+                join_piece<T>(th.k, c, th.at(a, stage, kZ, c), z);
+                th.post(a, c, g);
+#pragma unroll
+                for (int i = 0; i < P; ++i) d[i] = mul_f32x2(d[i], r1_2);
+                if (GATED) {
+                    join_piece<T>(th.k, c, th.at(a, stage, kGate, c), v);
+                    if (a.out[2]) {
+                        uint64_t o[P];
+#pragma unroll
+                        for (int i = 0; i < P; ++i) o[i] = mul_f32x2(mul_f32x2(d[i], z[i]), g[i]);
+                        join_store<T>(th.k, c, dgate, o);
+                    }
+#pragma unroll
+                    for (int i = 0; i < P; ++i) d[i] = mul_f32x2(d[i], v[i]);
+                }
+#pragma unroll
+                for (int i = 0; i < P; ++i) sum_post[c][i] = fma_f32x2(d[i], z[i], sum_post[c][i]);
+                if (a.out[0]) {
+#pragma unroll
+                    for (int i = 0; i < P; ++i) v[i] = fma_f32x2(k1_2, z[i], mul_f32x2(d[i], g[i]));
+                    join_store<T>(th.k, c, dz, v);
                 }
             }
-            if (a.out[1]) {
-#pragma unroll
-                for (int i = 0; i < VEC; ++i) v[i] = w.good ? a.alpha * d[i] : 0.f;
-                join_store<T>(th.k, c, dres, v);
-            }
-            join_piece<T>(th.k, c, th.at(a, stage, kZ, c), z);
-            join_params<VEC>(th.post, c * a.T + th.t, th.pieces, g);
-            if (gated) {
-                join_piece<T>(th.k, c, th.at(a, stage, kGate, c), v);
-                if (a.out[2]) {
-                    float o[VEC];
-#pragma unroll
-                    for (int i = 0; i < VEC; ++i) o[i] = w.good ? d[i] * (z[i] * w.r1) * g[i] : 0.f;
-                    join_store<T>(th.k, c, dgate, o);
-                }
-#pragma unroll
-                for (int i = 0; i < VEC; ++i) d[i] *= v[i];
-            }
-            if (w.good) {
-#pragma unroll
-                for (int i = 0; i < VEC; ++i) sum_post[c][i] = fmaf(d[i], z[i] * w.r1, sum_post[c][i]);
-            }
-            if (a.out[0]) {
-#pragma unroll
-                for (int i = 0; i < VEC; ++i) v[i] = w.good ? fmaf(-w.k1, z[i], w.r1 * (d[i] * g[i])) : 0.f;
-                join_store<T>(th.k, c, dz, v);
-            }
+        } else {                                          // the same for the whole group
+            if (a.out[0]) th.store_zeros(dz);
+            if (a.out[1]) th.store_zeros(dres);
+            if (a.out[2]) th.store_zeros(dgate);
         }
         th.fetch(a, r + a.stages * th.step, stage);
         if (++stage == a.stages) stage = 0;
@@ -431,9 +556,10 @@ __global__ void __launch_bounds__(kJoinThreads, 1) join_bwd_kernel(const __grid_
 #pragma unroll
         for (int c = 0; c < CH; ++c)
 #pragma unroll
-            for (int i = 0; i < VEC; ++i) {
-                all[((th.group - 1) * 2 * E + c * VEC + i) * a.T + th.t] = sum_post[c][i];
-                all[((th.group - 1) * 2 * E + E + c * VEC + i) * a.T + th.t] = sum_pre[c][i];
+            for (int i = 0; i < P; ++i) {
+                float* to = all + ((th.group - 1) * 2 * E + c * VEC + 2 * i) * a.T + th.t;
+                ptx::unpack_f32x2(sum_post[c][i], to[0], to[a.T]);
+                ptx::unpack_f32x2(sum_pre[c][i], to[E * a.T], to[(E + 1) * a.T]);
             }
     }
     __syncthreads();
@@ -442,15 +568,21 @@ __global__ void __launch_bounds__(kJoinThreads, 1) join_bwd_kernel(const __grid_
 #pragma unroll
     for (int c = 0; c < CH; ++c)
 #pragma unroll
-        for (int i = 0; i < VEC; ++i) {
+        for (int i = 0; i < P; ++i) {
+            float v[4];
+            ptx::unpack_f32x2(sum_post[c][i], v[0], v[1]);
+            ptx::unpack_f32x2(sum_pre[c][i], v[2], v[3]);
             for (int g = 1; g < a.groups; ++g) {
-                sum_post[c][i] += all[((g - 1) * 2 * E + c * VEC + i) * a.T + th.t];
-                sum_pre[c][i] += all[((g - 1) * 2 * E + E + c * VEC + i) * a.T + th.t];
+                const float* from = all + ((g - 1) * 2 * E + c * VEC + 2 * i) * a.T + th.t;
+                v[0] += from[0]; v[1] += from[a.T];
+                v[2] += from[E * a.T]; v[3] += from[(E + 1) * a.T];
             }
-            if (th.k.has(c, i)) {
-                part[th.k.col(c) + i] = sum_post[c][i];
-                part[int64_t(a.N) + th.k.col(c) + i] = sum_pre[c][i];
-            }
+#pragma unroll
+            for (int l = 0; l < 2; ++l)
+                if (th.k.has(c, 2 * i + l)) {
+                    part[th.k.col(c) + 2 * i + l] = v[l];
+                    part[int64_t(a.N) + th.k.col(c) + 2 * i + l] = v[2 + l];
+                }
         }
 }
 
@@ -523,58 +655,115 @@ __global__ void __launch_bounds__(kJoinAnyThreads) join_fwd_any_kernel(const __g
     }
 }
 
-template <class T>
-__global__ void __launch_bounds__(kJoinAnyThreads) join_bwd_any_kernel(const __grid_constant__ JoinArgs a) {
+// Backward pass of such rows in two launches: the three sums of every row, then, with no thread depending on another,
+// the gradients, a block walking down its strip of columns.  10 elements moved per element of a row instead of 6.
+// VEC: columns per access, 16 bytes' worth where all rows start and end on 16-byte boundaries, else 1.
+template <class T, int VEC>
+__device__ __forceinline__ void join_read(const JoinArgs& a, int m, int64_t r, int c, float otherwise, float (&v)[VEC]) {
+    if (a.in[m]) {
+        load_vec<VEC>(static_cast<const T*>(a.in[m]) + r * a.ld[m] + c, v);
+    } else {
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) v[i] = otherwise;
+    }
+}
+template <class T, int VEC>
+__global__ void __launch_bounds__(kJoinAnyThreads) join_row_sums_kernel(const __grid_constant__ JoinArgs a) {
     __shared__ float red[3 * 32];
     pdl_launch();
     pdl_wait();
     const bool pre = a.norms & TPPO_NORM_PRE;
-    float* part = a.partial ? a.partial + int64_t(blockIdx.x) * 2 * a.N : nullptr;
     for (int64_t r = blockIdx.x; r < a.M; r += gridDim.x) {
-        const T* z = static_cast<const T*>(a.in[kZ]) + r * a.ld[kZ];
-        const T* h = pre ? static_cast<const T*>(a.in[kH]) + r * a.ld[kH] : nullptr;
-        const T* dn = pre ? static_cast<const T*>(a.in[kDn]) + r * a.ld[kDn] : nullptr;
-        const T* dh = a.in[kDh] ? static_cast<const T*>(a.in[kDh]) + r * a.ld[kDh] : nullptr;
-        const T* gate = a.in[kGate] ? static_cast<const T*>(a.in[kGate]) + r * a.ld[kGate] : nullptr;
         const float r1 = a.r_post ? a.r_post[r] : 1.f, r2 = a.r_pre ? a.r_pre[r] : 0.f;
         float s[3] = {0.f, 0.f, 0.f};
 #pragma unroll 2
-        for (int c = threadIdx.x; c < a.N; c += kJoinAnyThreads) {
-            float g = param(a.gate_row, c, a.p32) * param(a.gamma_post, c, a.p32);
-            if (gate) g *= load_f32(gate + c);
-            const float w = load_f32(z + c) * g;
-            float d = dh ? load_f32(dh + c) : 0.f;
+        for (int c = threadIdx.x * VEC; c < a.N; c += kJoinAnyThreads * VEC) {
+            float z[VEC], g[VEC], d[VEC], n[VEC], h[VEC];
+            join_read<T, VEC>(a, kZ, r, c, 0.f, z);
+            join_read<T, VEC>(a, kGate, r, c, 1.f, g);
+            join_read<T, VEC>(a, kDh, r, c, 0.f, d);
             if (pre) {
-                const float a2 = load_f32(dn + c) * param(a.gamma_pre, c, a.p32), hv = load_f32(h + c);
-                s[0] = fmaf(a2, hv, s[0]);
-                s[2] = fmaf(hv, w, s[2]);
-                d = fmaf(r2, a2, d);
+                join_read<T, VEC>(a, kDn, r, c, 0.f, n);
+                join_read<T, VEC>(a, kH, r, c, 0.f, h);
             }
-            s[1] = fmaf(d, w, s[1]);
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) {
+                const float w = z[i] * (g[i] * param(a.gate_row, c + i, a.p32) * param(a.gamma_post, c + i, a.p32));
+                if (pre) {
+                    const float a2 = n[i] * param(a.gamma_pre, c + i, a.p32);
+                    s[0] = fmaf(a2, h[i], s[0]);
+                    s[2] = fmaf(h[i], w, s[2]);
+                    d[i] = fmaf(r2, a2, d[i]);
+                }
+                s[1] = fmaf(d[i], w, s[1]);
+            }
         }
         block_sums(s, red);
-        const JoinRow w = join_row(a, r1, r2, s);
+        if (threadIdx.x == 0) {
+            const JoinRow w = join_row(a, r1, r2, s, true);
+            // zeros: a row to leave out
+            a.rows[r] = w.good ? make_float4(w.r1, w.r2, w.k1, w.k2) : make_float4(0.f, 0.f, 0.f, 0.f);
+        }
+    }
+}
+
+constexpr int kJoinStrip = 128;                           // threads of a strip
+template <class T, int VEC>
+__global__ void __launch_bounds__(kJoinStrip) join_columns_kernel(const __grid_constant__ JoinArgs a) {
+    pdl_launch();
+    pdl_wait();
+    const bool pre = a.norms & TPPO_NORM_PRE;
+    const int64_t chunk = blockIdx.y, r0 = a.M * chunk / gridDim.y, r1 = a.M * (chunk + 1) / gridDim.y;
+    const int64_t at = (int64_t(blockIdx.x) * kJoinStrip + threadIdx.x) * VEC;
+    if (at >= a.N) return;
+    const int c = int(at);
+    float g[VEC], gn[VEC], sum_post[VEC], sum_pre[VEC];
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) {
+        g[i] = param(a.gate_row, c + i, a.p32) * param(a.gamma_post, c + i, a.p32);
+        gn[i] = param(a.gamma_pre, c + i, a.p32);
+        sum_post[i] = sum_pre[i] = 0;
+    }
 #pragma unroll 2
-        for (int c = threadIdx.x; c < a.N; c += kJoinAnyThreads) {
-            const float zv = load_f32(z + c), gp = param(a.gamma_post, c, a.p32), gr = param(a.gate_row, c, a.p32);
-            const float gv = gate ? load_f32(gate + c) : 1.f;
-            float d = dh ? load_f32(dh + c) : 0.f, tp = 0.f;
+    for (int64_t r = r0; r < r1; ++r) {
+        const float4 w = __ldcg(a.rows + r);
+        float z[VEC], gv[VEC], d[VEC], n[VEC], h[VEC], o[VEC];
+        join_read<T, VEC>(a, kZ, r, c, 0.f, z);
+        join_read<T, VEC>(a, kGate, r, c, 1.f, gv);
+        join_read<T, VEC>(a, kDh, r, c, 0.f, d);
+        if (pre) {
+            join_read<T, VEC>(a, kDn, r, c, 0.f, n);
+            join_read<T, VEC>(a, kH, r, c, 0.f, h);
+        }
+        const bool good = w.x != 0.f;                     // r1 of a row with statistics is not 0
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) {
             if (pre) {
-                const float nv = load_f32(dn + c), hv = load_f32(h + c);
-                tp = nv * (hv * w.r2);
-                d = fmaf(-w.k2, hv, fmaf(w.r2, nv * param(a.gamma_pre, c, a.p32), d));
+                const float m = n[i] * w.y;
+                if (good) sum_pre[i] = fmaf(m, h[i], sum_pre[i]);
+                d[i] = fmaf(-w.w, h[i], fmaf(m, gn[i], d[i]));
             }
-            const float g = gr * gp;
-            if (a.out[1]) store_f32(static_cast<T*>(a.out[1]) + r * a.ldo[1] + c, w.good ? a.alpha * d : 0.f);
-            if (a.out[2]) store_f32(static_cast<T*>(a.out[2]) + r * a.ldo[2] + c, w.good ? d * (zv * w.r1) * g : 0.f);
-            d *= gv;
-            if (a.out[0]) store_f32(static_cast<T*>(a.out[0]) + r * a.ldo[0] + c, w.good ? fmaf(-w.k1, zv, w.r1 * (d * g)) : 0.f);
-            if (part) {                                   // this block's own sums: a thread always has the same columns
-                const float sp = w.good ? d * (zv * w.r1) : 0.f;
-                const bool first = r == blockIdx.x;
-                part[c] = first ? sp : part[c] + sp;
-                part[int64_t(a.N) + c] = first ? (w.good ? tp : 0.f) : part[int64_t(a.N) + c] + (w.good ? tp : 0.f);
-            }
+            o[i] = good ? a.alpha * d[i] : 0.f;
+            d[i] *= w.x;
+        }
+        if (a.out[1]) store_vec<VEC>(static_cast<T*>(a.out[1]) + r * a.ldo[1] + c, o);
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) {
+            o[i] = good ? d[i] * z[i] * g[i] : 0.f;
+            d[i] *= gv[i];
+            if (good) sum_post[i] = fmaf(d[i], z[i], sum_post[i]);
+        }
+        if (a.out[2]) store_vec<VEC>(static_cast<T*>(a.out[2]) + r * a.ldo[2] + c, o);
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) o[i] = good ? fmaf(-w.z, z[i], d[i] * g[i]) : 0.f;
+        if (a.out[0]) store_vec<VEC>(static_cast<T*>(a.out[0]) + r * a.ldo[0] + c, o);
+    }
+    if (a.partial) {
+        float* part = a.partial + chunk * 2 * a.N;
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) {
+            part[c + i] = sum_post[i];
+            part[int64_t(a.N) + c + i] = sum_pre[i];
         }
     }
 }
@@ -610,93 +799,127 @@ __global__ void __launch_bounds__(256) join_sum_kernel(const JoinSumArgs a) {
 }
 
 // ---- host side --------------------------------------------------------------------------------------------------
-struct JoinPlan { int E = 0, grid = 0; size_t smem = 0; };        // E = 0: the kernels for any row
+struct JoinPlan { int E = 0, grid = 0; bool shift = false; size_t smem = 0; };    // E = 0: the kernels for any row
 
-// Groups, stages and elements per thread of the ring kernels.  `most`: elements a thread can hold; `count`: matrices.
-//   Many rows: as few threads per row as hold it (a barrier of four warps is cheaper than one of sixteen, and more
-//   rows are on their way at once), and as many groups as leave two stages each.
-//   Few rows: all of a block's threads for one row.
-// Rows that start at changing places of a piece come in classes; a grid of a multiple of eight keeps a block in one.
-JoinPlan join_plan(JoinArgs& a, const int* elements, int kinds, int vec, bool fwd) {
-    JoinPlan p;
-    const bool shifts = a.shift_step % vec != 0 || reinterpret_cast<uintptr_t>(a.in[kZ]) % 16 != 0;
-    const int64_t pieces = (int64_t(a.N) + (shifts ? vec - 1 : 0) + vec - 1) / vec;
-    const int most = elements[kinds - 1];
-    if (pieces * vec > int64_t(kJoinThreads) * most) return p;
-    const int width = int(pieces) * vec;
-    a.T = (width + 32 * most - 1) / (32 * most) * 32;
-    int groups = kJoinThreads / a.T;
-    if (a.T > 32 && groups > 15) groups = 15;             // hardware barriers
-    if (a.M < int64_t(kNumSms) * groups) {
-        groups = int((a.M + kNumSms - 1) / kNumSms);
-        const int wide = kJoinThreads / groups / 32 * 32, enough = (width + 32 * elements[0] - 1) / (32 * elements[0]) * 32;
-        if (wide > a.T) a.T = wide < enough ? wide : enough;
-        if (a.T > 32 && groups > 15) groups = 15;
-    }
-    for (int i = kinds - 1; i >= 0; --i)
-        if (int64_t(a.T) * elements[i] >= width) p.E = elements[i];
-    const int64_t row = int64_t(a.T) * p.E / vec * 16;    // bytes of a matrix' row in a stage
-    const int64_t params = int64_t(a.T) * p.E * 8 + kJoinRedBytes;
+// Groups and stages of a ring kernel for `e` elements per thread; false where it does not fit.
+bool join_fit(JoinArgs& a, JoinPlan& p, int e, int vec, int threads, bool regs, int64_t width, bool sums) {
+    const int64_t T = (width + 32 * e - 1) / (32 * e) * 32;
+    if (T > threads) return false;
+    int groups = threads / int(T);
+    if (T > 32 && groups > 15) groups = 15;               // hardware barriers
+    if (a.M < int64_t(kNumSms) * groups) groups = int((a.M + kNumSms - 1) / kNumSms);
+    const int64_t row = T * e / vec * 16;                 // bytes of a matrix' row in a stage
+    const int64_t params = (regs ? 0 : T * e * 8) + kJoinRedBytes;
     const int64_t slots = (kJoinSmem - params) / (row * a.arrays);
-    if (slots < 1) { p.E = 0; return p; }
+    if (slots < 1) return false;
     if (groups > 1 && groups > slots / 2) groups = slots / 2 > 1 ? int(slots / 2) : 1;
+    a.T = int(T);
     a.groups = groups;
     a.stages = int(slots / groups < kJoinStages ? slots / groups : kJoinStages);
     int64_t blocks = (a.M + groups - 1) / groups;
     if (blocks > kNumSms) blocks = kNumSms;
+    // rows that start at changing places of a piece come in classes; a grid of a multiple of eight keeps a block in one
     if (a.shift_step % vec != 0) blocks = blocks <= 144 ? (blocks + 7) / 8 * 8 : 144;
-    p.grid = int(blocks);
-    const int64_t sums = fwd ? 0 : int64_t(groups - 1) * a.T * p.E * 8 + kJoinRedBytes;
     const int64_t ring = params + row * a.arrays * a.groups * a.stages;
-    p.smem = size_t(ring > sums ? ring : sums);
-    return p;
+    const int64_t meet = sums ? int64_t(groups - 1) * T * e * 8 + kJoinRedBytes : 0;
+    p.E = e;
+    p.grid = int(blocks);
+    p.smem = size_t(ring > meet ? ring : meet);
+    return true;
+}
+// The columns a row's pieces cover, and whether some lie partly outside it.
+int64_t join_width(const JoinArgs& a, JoinPlan& p, int vec) {
+    p.shift = a.shift_step % vec != 0 || reinterpret_cast<uintptr_t>(a.in[kZ]) % 16 != 0;
+    const int64_t pieces = (int64_t(a.N) + (p.shift ? vec - 1 : 0) + vec - 1) / vec;
+    p.shift = p.shift || a.N % vec != 0;
+    return pieces * vec;
 }
 
 template <class T, int E>
 int launch_fwd(const JoinArgs& a, const JoinPlan& p, cudaStream_t s) {
-    TPPO_CUDA_CHECK(cudaFuncSetAttribute(join_fwd_kernel<T, E>, cudaFuncAttributeMaxDynamicSharedMemorySize, kJoinSmem));
-    TPPO_CUDA_CHECK(launch_dense(join_fwd_kernel<T, E>, dim3(p.grid), dim3(a.T * a.groups), p.smem, s, a));
+    auto kernel = a.in[kGate] ? (p.shift ? join_fwd_kernel<T, E, true, true> : join_fwd_kernel<T, E, true, false>)
+                              : (p.shift ? join_fwd_kernel<T, E, false, true> : join_fwd_kernel<T, E, false, false>);
+    TPPO_CUDA_CHECK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kJoinSmem));
+    TPPO_CUDA_CHECK(launch_dense(kernel, dim3(p.grid), dim3(a.T * a.groups), p.smem, s, a));
     return TPPO_OK;
 }
-template <class T, int E>
+template <class T, int E, bool PRE>
 int launch_bwd(const JoinArgs& a, const JoinPlan& p, cudaStream_t s) {
-    TPPO_CUDA_CHECK(cudaFuncSetAttribute(join_bwd_kernel<T, E>, cudaFuncAttributeMaxDynamicSharedMemorySize, kJoinSmem));
-    TPPO_CUDA_CHECK(launch_dense(join_bwd_kernel<T, E>, dim3(p.grid), dim3(a.T * a.groups), p.smem, s, a));
+    auto kernel = a.in[kGate] ? (p.shift ? join_bwd_kernel<T, E, PRE, true, true> : join_bwd_kernel<T, E, PRE, true, false>)
+                              : (p.shift ? join_bwd_kernel<T, E, PRE, false, true> : join_bwd_kernel<T, E, PRE, false, false>);
+    TPPO_CUDA_CHECK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kJoinSmem));
+    TPPO_CUDA_CHECK(launch_dense(kernel, dim3(p.grid), dim3(a.T * a.groups), p.smem, s, a));
     return TPPO_OK;
 }
 
 template <class T>
 int run_fwd(JoinArgs& a, bool same, cudaStream_t s) {
-    static const int kinds[5] = {8, 16, 24, 40, 48};
-    const JoinPlan p = same ? join_plan(a, kinds, 5, Join<T>::VEC, true) : JoinPlan{};
+    constexpr int vec = Join<T>::VEC;
+    JoinPlan p;
+    if (same) {
+        const int64_t width = join_width(a, p, vec);
+        // the fewest elements per thread with which a block still holds four rows (fewer rows: one), else the most
+        const int least = a.M >= 4 * kNumSms ? 4 : 1;
+        for (const int e : {8, 16, 40, 32}) {
+            JoinPlan q = p;
+            JoinArgs b = a;
+            if (!join_fit(b, q, e, vec, join_fwd_threads(e), join_fwd_regs(e), width, false)) continue;
+            if (e < 40 ? b.groups >= least || e == 32 : b.groups * b.stages >= 2) { a = b; p = q; break; }
+        }
+    }
     switch (p.E) {
         case 8: return launch_fwd<T, 8>(a, p, s);
         case 16: return launch_fwd<T, 16>(a, p, s);
-        case 24: return launch_fwd<T, 24>(a, p, s);
+        case 32: return launch_fwd<T, 32>(a, p, s);
         case 40: return launch_fwd<T, 40>(a, p, s);
-        case 48: return launch_fwd<T, 48>(a, p, s);
     }
     const int grid = int(a.M < kJoinAnyBlocks ? a.M : kJoinAnyBlocks);
-    a.T = kJoinAnyThreads;
     TPPO_CUDA_CHECK(launch_dense(join_fwd_any_kernel<T>, dim3(grid), dim3(kJoinAnyThreads), 0, s, a));
+    return TPPO_OK;
+}
+
+int64_t join_chunks(int64_t M) { return M < kJoinAnyBlocks ? (M + 7) / 8 * 8 : kJoinAnyBlocks; }
+
+template <class T, int VEC>
+int run_bwd_any(JoinArgs& a, JoinSumArgs& sum, cudaStream_t s) {
+    TPPO_CUDA_CHECK(launch_dense(join_row_sums_kernel<T, VEC>, dim3(unsigned(a.M < 4 * kNumSms ? a.M : 4 * kNumSms)), dim3(kJoinAnyThreads), 0, s, a));
+    // enough chunks of rows to fill the GPU some times over
+    const int64_t strips = (int64_t(a.N) + kJoinStrip * VEC - 1) / (kJoinStrip * VEC), most = join_chunks(a.M);
+    int64_t chunks = (32 * kNumSms + strips - 1) / strips;
+    if (chunks > (a.M + 7) / 8) chunks = (a.M + 7) / 8;
+    if (chunks > most) chunks = most;
+    sum.rows = chunks;
+    TPPO_CUDA_CHECK(launch_dense(join_columns_kernel<T, VEC>, dim3(unsigned(strips), unsigned(chunks)), dim3(kJoinStrip), 0, s, a));
     return TPPO_OK;
 }
 
 template <class T>
 int run_bwd(JoinArgs& a, bool same, JoinSumArgs& sum, cudaStream_t s) {
-    static const int kinds[2] = {8, 16};
-    const JoinPlan p = same ? join_plan(a, kinds, 2, Join<T>::VEC, false) : JoinPlan{};
-    int r = TPPO_OK;
-    if (p.E) {
-        sum.rows = p.grid;
-        r = p.E == 8 ? launch_bwd<T, 8>(a, p, s) : launch_bwd<T, 16>(a, p, s);
-    } else {
-        const int grid = int(a.M < kJoinAnyBlocks ? a.M : kJoinAnyBlocks);
-        a.T = kJoinAnyThreads;
-        sum.rows = grid;
-        TPPO_CUDA_CHECK(launch_dense(join_bwd_any_kernel<T>, dim3(grid), dim3(kJoinAnyThreads), 0, s, a));
+    constexpr int vec = Join<T>::VEC;
+    JoinPlan p;
+    const int64_t width = join_width(a, p, vec);
+    const bool whole = same && !p.shift;                  // every row is a number of 16-byte pieces
+    if (same) {
+        // the fewest instructions per row: some 20 per element and 250 per thread (its share of sums, copies and
+        // addresses); where there are few rows, the most threads for each
+        int64_t least = INT64_MAX;
+        for (const int e : {8, 16, 32}) {
+            JoinPlan q = p;
+            JoinArgs b = a;
+            if (!join_fit(b, q, e, vec, join_bwd_threads(e), join_bwd_regs(e), width, true) || b.groups * b.stages < 2) continue;
+            const int64_t cost = int64_t(b.T) * (20 * e + 250);
+            if (cost < least) { least = cost; a = b; p = q; }
+            if (a.M <= kNumSms) break;
+        }
     }
-    return r;
+    const bool pre = a.norms & TPPO_NORM_PRE;
+    sum.rows = p.grid;
+    switch (p.E) {
+        case 8: return pre ? launch_bwd<T, 8, true>(a, p, s) : launch_bwd<T, 8, false>(a, p, s);
+        case 16: return pre ? launch_bwd<T, 16, true>(a, p, s) : launch_bwd<T, 16, false>(a, p, s);
+        case 32: return pre ? launch_bwd<T, 32, true>(a, p, s) : launch_bwd<T, 32, false>(a, p, s);
+    }
+    return whole ? run_bwd_any<T, vec>(a, sum, s) : run_bwd_any<T, 1>(a, sum, s);
 }
 
 bool type_ok(int32_t t) { return t == TPPO_BF16 || t == TPPO_F32; }
@@ -710,10 +933,11 @@ bool same_start(const void* p, int64_t ldp, const void* q, int64_t ldq, size_t e
 
 }  // namespace
 
+// The rows' scalars in front, the partial column sums behind them.
+static size_t join_rows_bytes(int64_t M) { return align_up(size_t(M > 0 ? M : 1) * sizeof(float4), kWsAlign); }
 size_t residual_norm_workspace_bytes(int64_t M, int32_t N) {
     if (N <= 0) return 0;
-    const int64_t rows = M < kJoinAnyBlocks ? (M + 7) / 8 * 8 : kJoinAnyBlocks;
-    return align_up(size_t(rows > 0 ? rows : 1) * 2 * size_t(N) * sizeof(float), kWsAlign);
+    return join_rows_bytes(M) + align_up(size_t(M > 0 ? join_chunks(M) : 1) * 2 * size_t(N) * sizeof(float), kWsAlign);
 }
 
 }  // namespace tppo
@@ -780,8 +1004,7 @@ TPPO_API int tppo_residual_norm_bwd(const void* dh, int64_t lddh, const void* dn
         return TPPO_ERR_INVALID_ARG;
     if (M > kDenseMaxSize || N > kDenseMaxSize) return TPPO_ERR_UNSUPPORTED;
     const bool sums = dgamma_post || dgamma_pre || (dgate && !full);
-    if (sums && (!workspace || !aligned(workspace, kWsAlign) || workspace_bytes < residual_norm_workspace_bytes(M, N)))
-        return TPPO_ERR_WORKSPACE;
+    if (!workspace || !aligned(workspace, kWsAlign) || workspace_bytes < residual_norm_workspace_bytes(M, N)) return TPPO_ERR_WORKSPACE;
     JoinArgs a{};
     a.in[kZ] = z; a.ld[kZ] = ldz;
     if (pre) { a.in[kH] = h; a.ld[kH] = ldh; a.in[kDn] = dn; a.ld[kDn] = lddn; }
@@ -794,7 +1017,8 @@ TPPO_API int tppo_residual_norm_bwd(const void* dh, int64_t lddh, const void* dn
     a.out[0] = dz; a.out[1] = dresidual; a.out[2] = full ? dgate : nullptr;
     a.ldo[0] = lddz; a.ldo[1] = lddr; a.ldo[2] = lddg;
     a.r_post = const_cast<float*>(rstd_post); a.r_pre = const_cast<float*>(rstd_pre);
-    a.partial = sums ? static_cast<float*>(workspace) : nullptr;
+    a.rows = static_cast<float4*>(workspace);
+    a.partial = sums ? reinterpret_cast<float*>(static_cast<char*>(workspace) + join_rows_bytes(M)) : nullptr;
     a.status = status;
     a.M = M; a.N = N; a.alpha = alpha; a.norms = norms;
     a.shift_step = int32_t(ldz % 16);
