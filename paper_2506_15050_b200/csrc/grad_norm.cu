@@ -1,11 +1,12 @@
 // The global norm of many gradients, and clipping by it:
 //     sum_sq = sum_i |g_i|^2,   coef = min(1, max_norm / sqrt(sum_sq)),   out_i = coef * g_i
 // Both calls stream: the norm reads every element once, clipping reads it once more and writes it once, so
-// HBM bounds them (or L2, for gradients that fit there).  The list of tensors travels in the kernel's
+// HBM bounds them (or L2, for gradients that fit there): 600 million bf16 elements are read in 184 us (6.5 TB/s) and
+// scaled into other buffers in 362 (6.6 TB/s).  The list of tensors travels in the kernel's
 // parameters -- no copy to the device, nothing to keep in step with it, and a captured graph carries it along.
-// Work is cut into chunks of 8192 elements of one tensor; a unit of 256 threads owns a contiguous range of
-// chunks, so that it searches its first tensor once and then only steps on.  Clipping walks the same ranges
-// backwards: what the norm read last is what L2 still holds.
+// Work is cut into chunks of 8192 elements of one tensor; units of 256 threads take them in turn, so that a
+// unit searches its first tensor once and then only steps on.  Clipping walks backwards: what the norm read last is
+// what L2 still holds.
 //
 // A thread squares 32 elements of a chunk in fp32 and adds their sum to a 64-bit total.  Where that sum could
 // have lost something -- it is not finite, or below 2^-100 -- the 32 squares are taken again in 64 bits, so the
@@ -21,6 +22,7 @@ constexpr int kGradUnit = 256;                  // threads that walk a range of 
 constexpr int kGradPieces = 4;                  // 8-element pieces of a chunk per thread
 constexpr int kGradChunk = kGradUnit * kGradPieces * 8;
 constexpr int kGradGrid = kNumSms * 4;
+constexpr int kClipInPlaceGrid = kNumSms * 64;
 constexpr int kGradCluster = 8, kGradClusterThreads = 1024;
 constexpr int kGradClusterChunks = 4 * kGradCluster * kGradClusterThreads / kGradUnit;
 constexpr int kGradFew = 64, kGradMany = 1024;  // tensors per launch: 29 bytes each of the 32764 for parameters
@@ -33,7 +35,7 @@ struct GradList {
     void* dst[CAP];
     int64_t n[CAP];
     int32_t first[CAP + 1];                     // first chunk of each tensor
-    int32_t count;
+    int32_t count, in_place;                    // in_place: every tensor is its own output
     uint8_t kind[CAP];
 };
 
@@ -87,25 +89,57 @@ __device__ __forceinline__ void grad_load(const T* p, int len, bool vec, int tid
         }
     }
 }
-template <class T>
-__device__ __forceinline__ void grad_store(T* p, int len, bool vec, int tid, const float (&v)[kGradPieces][8]) {
-    if (vec && len == kGradChunk) {
+// Eight elements as loaded, widened and scaled by f0 * f1.
+template <class S> struct GradPiece;
+template <> struct GradPiece<bf16_bits> {
+    uint4 w;
+    __device__ __forceinline__ void load(const bf16_bits* p) { w = __ldcs(reinterpret_cast<const uint4*>(p)); }
+    __device__ __forceinline__ void scaled(float f0, float f1, float (&v)[8]) const {
+        const uint32_t u[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
-        for (int i = 0; i < kGradPieces; ++i) store_vec<8>(p + (tid + i * kGradUnit) * 8, v[i]);
-        return;
+        for (int j = 0; j < 4; ++j) {
+            v[2 * j] = bf16_lo(u[j]) * f0 * f1;
+            v[2 * j + 1] = bf16_hi(u[j]) * f0 * f1;
+        }
     }
+};
+template <> struct GradPiece<float> {
+    float4 a, b;
+    __device__ __forceinline__ void load(const float* p) {
+        a = __ldcs(reinterpret_cast<const float4*>(p));
+        b = __ldcs(reinterpret_cast<const float4*>(p) + 1);
+    }
+    __device__ __forceinline__ void scaled(float f0, float f1, float (&v)[8]) const {
+        v[0] = a.x * f0 * f1; v[1] = a.y * f0 * f1; v[2] = a.z * f0 * f1; v[3] = a.w * f0 * f1;
+        v[4] = b.x * f0 * f1; v[5] = b.y * f0 * f1; v[6] = b.z * f0 * f1; v[7] = b.w * f0 * f1;
+    }
+};
+// A chunk scaled by f0 * f1; with f1 = 0 it becomes 0 whatever it holds.  Whole aligned chunks, which nearly all are,
+// have their loads issued together; the rest goes element by element.
+template <class S, class D>
+__device__ __forceinline__ void grad_scale(const S* p, D* q, int len, bool vec, int tid, float f0, float f1) {
+    const bool zero = f1 == 0.f;
+    if (vec && len == kGradChunk) {
+        constexpr int kBatch = kGradPieces * 2 / int(sizeof(S));         // 64 bytes in flight per thread
+        GradPiece<S> w[kBatch];
 #pragma unroll
-    for (int i = 0; i < kGradPieces; ++i) {
-        const int at = (tid + i * kGradUnit) * 8;
-        if (vec && at + 8 <= len) {
-            store_vec<8>(p + at, v[i]);
-        } else {
+        for (int first = 0; first < kGradPieces; first += kBatch) {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const int e = vec ? at + j : tid + (i * 8 + j) * kGradUnit;
-                if (e < len) store_f32(p + e, v[i][j]);
+            for (int i = 0; i < kBatch; ++i) w[i].load(p + (tid + (first + i) * kGradUnit) * 8);
+#pragma unroll
+            for (int i = 0; i < kBatch; ++i) {
+                float v[8];
+                w[i].scaled(f0, f1, v);
+                if (zero) {
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) v[j] = 0.f;
+                }
+                store_vec<8>(q + (tid + (first + i) * kGradUnit) * 8, v);
             }
         }
+    } else {
+#pragma unroll 4
+        for (int e = tid; e < len; e += kGradUnit) store_f32(q + e, zero ? 0.f : load_f32(p + e) * f0 * f1);
     }
 }
 __device__ __forceinline__ float grad_element(const void* p, int64_t e, bool f32) {
@@ -141,10 +175,9 @@ grad_norm_kernel(const __grid_constant__ GradList<CAP> l, double* partial, doubl
     pdl_wait();
     const int per = int(blockDim.x) / kGradUnit, unit = int(blockIdx.x) * per + int(threadIdx.x) / kGradUnit;
     const int units = int(gridDim.x) * per, tid = int(threadIdx.x) % kGradUnit, chunks = l.first[l.count];
-    const int c0 = int(int64_t(chunks) * unit / units), c1 = int(int64_t(chunks) * (unit + 1) / units);
-    int t = c0 < c1 ? grad_find(l, c0) : 0;
+    int t = unit < chunks ? grad_find(l, unit) : 0;
     double sum = 0;
-    for (int c = c0; c < c1; ++c) {
+    for (int c = unit; c < chunks; c += units) {
         while (c >= l.first[t + 1]) ++t;
         const GradChunk k = grad_chunk(l, t, c);
         const bool f32 = l.kind[t] & kSrcF32, vec = l.kind[t] & kAligned;
@@ -197,7 +230,7 @@ __global__ void __launch_bounds__(1024) grad_sum_kernel(const double* partial, i
 }
 
 template <int CAP>
-__global__ void __launch_bounds__(kGradUnit, 3)
+__global__ void __launch_bounds__(kGradUnit, 8)
 grad_clip_kernel(const __grid_constant__ GradList<CAP> l, const double* sum_sq, double max_norm, float* coef, int32_t* status) {
     __shared__ float factor[2];
     pdl_launch();
@@ -217,28 +250,24 @@ grad_clip_kernel(const __grid_constant__ GradList<CAP> l, const double* sum_sq, 
     }
     __syncthreads();
     const float f0 = factor[0], f1 = factor[1];
+    const bool stays = f0 == 1.f && f1 == 1.f;
+    if (stays && l.in_place) return;
     const int units = int(gridDim.x), unit = int(blockIdx.x), tid = int(threadIdx.x), chunks = l.first[l.count];
-    const int c0 = int(int64_t(chunks) * unit / units), c1 = int(int64_t(chunks) * (unit + 1) / units);
-    int t = c0 < c1 ? grad_find(l, c1 - 1) : 0;
-    for (int c = c1 - 1; c >= c0; --c) {
+    int t = unit < chunks ? grad_find(l, chunks - 1 - unit) : 0;
+    for (int c = chunks - 1 - unit; c >= 0; c -= units) {
         while (c < l.first[t]) --t;
         const bool f32 = l.kind[t] & kSrcF32, to_f32 = l.kind[t] & kDstF32, vec = l.kind[t] & kAligned;
-        if (f1 == 1.f && f0 == 1.f && l.src[t] == l.dst[t]) continue;           // stays as it is
+        if (stays && l.src[t] == l.dst[t] && f32 == to_f32) continue;
         const GradChunk k = grad_chunk(l, t, c);
-        float v[kGradPieces][8];
-        if (f32) grad_load(static_cast<const float*>(l.src[t]) + k.at, k.len, vec, tid, v);
-        else grad_load(static_cast<const bf16_bits*>(l.src[t]) + k.at, k.len, vec, tid, v);
-        const bool zero = f1 == 0.f;            // also what is not finite
-#pragma unroll
-        for (int i = 0; i < kGradPieces; ++i)
-#pragma unroll
-            for (int j = 0; j < 8; ++j) v[i][j] = zero ? 0.f : v[i][j] * f0 * f1;
-        if (to_f32) grad_store(static_cast<float*>(l.dst[t]) + k.at, k.len, vec, tid, v);
-        else grad_store(static_cast<bf16_bits*>(l.dst[t]) + k.at, k.len, vec, tid, v);
-        if (tid < k.head) {
-            const float e = grad_element(l.src[t], tid, f32);
-            grad_put(l.dst[t], tid, to_f32, zero ? 0.f : e * f0 * f1);
-        }
+        const float* s32 = static_cast<const float*>(l.src[t]) + k.at;
+        const bf16_bits* s16 = static_cast<const bf16_bits*>(l.src[t]) + k.at;
+        float* d32 = static_cast<float*>(l.dst[t]) + k.at;
+        bf16_bits* d16 = static_cast<bf16_bits*>(l.dst[t]) + k.at;
+        if (f32 && to_f32) grad_scale(s32, d32, k.len, vec, tid, f0, f1);
+        else if (f32) grad_scale(s32, d16, k.len, vec, tid, f0, f1);
+        else if (to_f32) grad_scale(s16, d32, k.len, vec, tid, f0, f1);
+        else grad_scale(s16, d16, k.len, vec, tid, f0, f1);
+        if (tid < k.head) grad_put(l.dst[t], tid, to_f32, f1 == 0.f ? 0.f : grad_element(l.src[t], tid, f32) * f0 * f1);
     }
 }
 
@@ -271,6 +300,7 @@ template <int CAP>
 void fill(GradList<CAP>& l, const tppo_tensor* a, const tppo_tensor* out, int32_t count) {
     int64_t chunks = 0;
     l.count = 0;
+    l.in_place = 1;
     for (int32_t i = 0; i < count; ++i) {
         if (a[i].n == 0) continue;
         const tppo_tensor& o = out ? out[i] : a[i];
@@ -284,6 +314,7 @@ void fill(GradList<CAP>& l, const tppo_tensor* a, const tppo_tensor* out, int32_
         const int k = l.count++;
         l.src[k] = a[i].data;
         l.dst[k] = o.data;
+        if (o.data != a[i].data || o.dtype != a[i].dtype) l.in_place = 0;
         l.n[k] = a[i].n;
         l.first[k] = int32_t(chunks);
         l.kind[k] = uint8_t((a[i].dtype == TPPO_F32 ? kSrcF32 : 0) | (o.dtype == TPPO_F32 ? kDstF32 : 0) | (vec ? kAligned : 0) | head << 4);
@@ -326,7 +357,10 @@ int clip_part(const tppo_tensor* a, const tppo_tensor* out, int32_t count, const
     GradList<CAP> l;
     fill(l, a, out, count);
     const int chunks = l.first[l.count];
-    const int grid = chunks < 1 ? 1 : chunks < kGradGrid ? chunks : kGradGrid;
+    // A block per chunk, in the order of their addresses: 600 million bf16 elements in 362 us, the copy rate.  Blocks that
+    // take several drift apart, and HBM's pages suffer: 408 with 64 per SM, 490 with the 8 that fit.  In place there may
+    // be nothing to do, and 73 thousand blocks that find that out take 78 us, 64 per SM 15.
+    const int most = l.in_place ? kClipInPlaceGrid : 0x7fffffff, grid = chunks < 1 ? 1 : chunks < most ? chunks : most;
     TPPO_CUDA_CHECK(launch_dense(grad_clip_kernel<CAP>, dim3(grid), dim3(kGradUnit), 0, s, l, sum_sq, max_norm, coef, status));
     return TPPO_OK;
 }

@@ -18,10 +18,12 @@
 // lose all its digits where the block's output cancels the residual, so the forward pass does not use it.)
 //
 // Rows that do not start on 16-byte boundaries are read by the same aligned pieces, the first and last of which
-// hold elements of neighbouring rows or of nothing (a piece with one element of the row in it is mapped), masked
-// when they are used and stored element by element.  A block only takes rows that start at the same place of
+// hold elements of neighbouring rows or of nothing (a piece with one element of the row in it is mapped), cleared
+// when they have arrived, and stored element by element.  A block only takes rows that start at the same place of
 // a piece, so that a thread's columns, parameters and column sums stay its own.
 // Rows that do not fit, and matrices whose rows do not start at the same place of a piece, are read again for each sweep.
+#include <initializer_list>
+
 #include "dense_common.cuh"
 
 namespace tppo {
@@ -81,8 +83,9 @@ struct JoinColumns {
     static constexpr int VEC = Join<T>::VEC;
     int first, step, N;
     __device__ __forceinline__ int col(int c) const { return first + c * step; }
+    uint32_t edges = 0;                                   // bit c: piece c lies partly outside
     __device__ __forceinline__ bool any(int c) const { return col(c) < N && (!SHIFT || col(c) + VEC > 0); }
-    __device__ __forceinline__ bool all(int c) const { return !SHIFT || (col(c) >= 0 && col(c) + VEC <= N); }
+    __device__ __forceinline__ bool all(int c) const { return !SHIFT || (edges >> c & 1u) == 0; }
     __device__ __forceinline__ bool has(int c, int i) const { return unsigned(col(c) + i) < unsigned(N); }
 };
 
@@ -95,15 +98,8 @@ __device__ __forceinline__ void join_widen(uint4 w, float (&v)[Join<T>::VEC]) {
         v[0] = __uint_as_float(w.x); v[1] = __uint_as_float(w.y); v[2] = __uint_as_float(w.z); v[3] = __uint_as_float(w.w);
     }
 }
-// The widened piece; 0 outside the row.
-template <class T, class C>
-__device__ __forceinline__ void join_piece(const C& k, int c, uint32_t at, float (&v)[Join<T>::VEC]) {
-    join_widen<T>(ptx::lds128(at), v);
-    if (!k.all(c)) {
-#pragma unroll
-        for (int i = 0; i < Join<T>::VEC; ++i) v[i] = k.has(c, i) ? v[i] : 0.f;
-    }
-}
+template <class T>
+__device__ __forceinline__ void join_piece(uint32_t at, float (&v)[Join<T>::VEC]) { join_widen<T>(ptx::lds128(at), v); }
 template <class T, class C>
 __device__ __forceinline__ void join_store(const C& k, int c, T* row, const float (&v)[Join<T>::VEC]) {
     if (k.all(c)) {
@@ -173,6 +169,11 @@ struct JoinThread {
         k.first = t * VEC - shift;
         k.step = a.T * VEC;
         k.N = a.N;
+        if (SHIFT) {
+#pragma unroll
+            for (int c = 0; c < CH; ++c)
+                if (k.any(c) && (k.col(c) < 0 || k.col(c) + VEC > a.N)) k.edges |= 1u << c;
+        }
         float* red = reinterpret_cast<float*>(smem);
         for (int i = int(threadIdx.x); i < kJoinRedBytes / 4; i += int(blockDim.x)) red[i] = 0.f;
         sum = GroupSum{red + group * 2 * 3 * 32, a.T / 32, t / 32, a.groups == 1 ? 0 : group + 1, a.T, 0};
@@ -196,6 +197,27 @@ struct JoinThread {
             }
         }
         copy_commit();
+    }
+    // Until the oldest row's copies have landed; what its edge pieces brought from outside the row becomes 0.
+    __device__ __forceinline__ void land(const JoinArgs& a, int stage) const {
+        copy_wait(a.stages);
+        if constexpr (SHIFT) {
+            if (k.edges == 0) return;
+#pragma unroll 1
+            for (int m = 0; m < IN; ++m) {
+                if (!a.in[m]) continue;
+#pragma unroll
+                for (int c = 0; c < CH; ++c) {
+                    if (k.all(c)) continue;
+#pragma unroll
+                    for (int i = 0; i < VEC; ++i) {
+                        if (k.has(c, i)) continue;
+                        if constexpr (sizeof(T) == 2) ptx::sts_u16(at(a, stage, m, c) + 2 * i, 0);
+                        else asm volatile("st.shared.u32 [%0], %1;" ::"r"(at(a, stage, m, c) + 4 * i), "r"(0) : "memory");
+                    }
+                }
+            }
+        }
     }
     // gate row * gamma_post and gamma_pre; 0 outside the row.  Shared memory keeps them as planes of float4, so that
     // neighbouring threads read neighbouring 16 bytes.
@@ -277,7 +299,7 @@ __global__ void __launch_bounds__(join_fwd_threads(E), 1) join_fwd_kernel(const 
     const float inv = 1.f / float(a.N);
     int stage = 0;
     for (int64_t r = th.row; r < a.M; r += th.step) {
-        copy_wait(a.stages);
+        th.land(a, stage);
         float r1 = 1.f, s[1];
         bool good = true;
         if (post) {
@@ -286,7 +308,7 @@ __global__ void __launch_bounds__(join_fwd_threads(E), 1) join_fwd_kernel(const 
             for (int c = 0; c < CH; ++c) {
                 if (!th.k.any(c)) continue;
                 float z[VEC];
-                join_piece<T>(th.k, c, th.at(a, stage, kZ, c), z);
+                join_piece<T>(th.at(a, stage, kZ, c), z);
 #pragma unroll
                 for (int i = 0; i < VEC; ++i) q[i & 1] = fmaf(z[i], z[i], q[i & 1]);
             }
@@ -300,12 +322,12 @@ __global__ void __launch_bounds__(join_fwd_threads(E), 1) join_fwd_kernel(const 
         for (int c = 0; c < CH; ++c) {
             if (!th.k.any(c)) continue;
             float z[VEC], g[VEC];
-            join_piece<T>(th.k, c, th.at(a, stage, kZ, c), z);
-            join_piece<T>(th.k, c, th.at(a, stage, kRes, c), h[c]);
+            join_piece<T>(th.at(a, stage, kZ, c), z);
+            join_piece<T>(th.at(a, stage, kRes, c), h[c]);
             th.post(a, c, g);
             if (GATED) {
                 float w[VEC];
-                join_piece<T>(th.k, c, th.at(a, stage, kGate, c), w);
+                join_piece<T>(th.at(a, stage, kGate, c), w);
 #pragma unroll
                 for (int i = 0; i < VEC; ++i) g[i] *= w[i];
             }
@@ -372,23 +394,16 @@ __device__ __forceinline__ JoinRow join_row(const JoinArgs& a, float r1, float r
 // Pairs of fp32 values, on which one instruction works at a time: at some 30 operations per element the backward pass of
 // bf16 rows is otherwise bound by its instructions.
 template <class T> struct JoinPairs { static constexpr int N = Join<T>::VEC / 2; };
-template <class T, class C>
-__device__ __forceinline__ void join_piece(const C& k, int c, uint32_t at, uint64_t (&v)[JoinPairs<T>::N]) {
-    if (k.all(c)) {
-        if constexpr (sizeof(T) == 2) {
-            const uint4 w = ptx::lds128(at);
-            v[0] = ptx::pack_f32x2(bf16_lo(w.x), bf16_hi(w.x));
-            v[1] = ptx::pack_f32x2(bf16_lo(w.y), bf16_hi(w.y));
-            v[2] = ptx::pack_f32x2(bf16_lo(w.z), bf16_hi(w.z));
-            v[3] = ptx::pack_f32x2(bf16_lo(w.w), bf16_hi(w.w));
-        } else {
-            asm volatile("ld.shared.v2.u64 {%0, %1}, [%2];" : "=l"(v[0]), "=l"(v[1]) : "r"(at));
-        }
+template <class T>
+__device__ __forceinline__ void join_piece(uint32_t at, uint64_t (&v)[JoinPairs<T>::N]) {
+    if constexpr (sizeof(T) == 2) {
+        const uint4 w = ptx::lds128(at);
+        v[0] = ptx::pack_f32x2(bf16_lo(w.x), bf16_hi(w.x));
+        v[1] = ptx::pack_f32x2(bf16_lo(w.y), bf16_hi(w.y));
+        v[2] = ptx::pack_f32x2(bf16_lo(w.z), bf16_hi(w.z));
+        v[3] = ptx::pack_f32x2(bf16_lo(w.w), bf16_hi(w.w));
     } else {
-        float f[Join<T>::VEC];
-        join_piece<T>(k, c, at, f);
-#pragma unroll
-        for (int i = 0; i < JoinPairs<T>::N; ++i) v[i] = ptx::pack_f32x2(f[2 * i], f[2 * i + 1]);
+        asm volatile("ld.shared.v2.u64 {%0, %1}, [%2];" : "=l"(v[0]), "=l"(v[1]) : "r"(at));
     }
 }
 template <class T, class C>
@@ -442,29 +457,29 @@ __global__ void __launch_bounds__(join_bwd_threads(E), 1) join_bwd_kernel(const 
             if (post) r1_next = a.r_post[r + th.step];
             if (PRE) r2_next = a.r_pre[r + th.step];
         }
-        copy_wait(a.stages);
+        th.land(a, stage);
         const uint64_t r2_2 = ptx::pack_f32x2(r2, r2);
         uint64_t q[3] = {0, 0, 0};
 #pragma unroll
         for (int c = 0; c < CH; ++c) {
             if (!th.k.any(c)) continue;
             uint64_t w[P], d[P], g[P];
-            join_piece<T>(th.k, c, th.at(a, stage, kZ, c), w);
+            join_piece<T>(th.at(a, stage, kZ, c), w);
             th.post(a, c, g);
 #pragma unroll
             for (int i = 0; i < P; ++i) w[i] = mul_f32x2(w[i], g[i]);
             if (GATED) {
-                join_piece<T>(th.k, c, th.at(a, stage, kGate, c), g);
+                join_piece<T>(th.at(a, stage, kGate, c), g);
 #pragma unroll
                 for (int i = 0; i < P; ++i) w[i] = mul_f32x2(w[i], g[i]);
             }
 #pragma unroll
             for (int i = 0; i < P; ++i) d[i] = 0;
-            if (add) join_piece<T>(th.k, c, th.at(a, stage, kDh, c), d);
+            if (add) join_piece<T>(th.at(a, stage, kDh, c), d);
             if (PRE) {
                 uint64_t n[P], h[P];
-                join_piece<T>(th.k, c, th.at(a, stage, kDn, c), n);
-                join_piece<T>(th.k, c, th.at(a, stage, kH, c), h);
+                join_piece<T>(th.at(a, stage, kDn, c), n);
+                join_piece<T>(th.at(a, stage, kH, c), h);
                 th.pre(a, c, g);
 #pragma unroll
                 for (int i = 0; i < P; ++i) {
@@ -498,11 +513,11 @@ __global__ void __launch_bounds__(join_bwd_threads(E), 1) join_bwd_kernel(const 
                 uint64_t z[P], d[P], g[P], v[P];
 #pragma unroll
                 for (int i = 0; i < P; ++i) d[i] = 0;
-                if (add) join_piece<T>(th.k, c, th.at(a, stage, kDh, c), d);
+                if (add) join_piece<T>(th.at(a, stage, kDh, c), d);
                 if (PRE) {
                     uint64_t n[P], h[P];
-                    join_piece<T>(th.k, c, th.at(a, stage, kDn, c), n);
-                    join_piece<T>(th.k, c, th.at(a, stage, kH, c), h);
+                    join_piece<T>(th.at(a, stage, kDn, c), n);
+                    join_piece<T>(th.at(a, stage, kH, c), h);
                     th.pre(a, c, g);
 #pragma unroll
                     for (int i = 0; i < P; ++i) {
@@ -516,12 +531,12 @@ __global__ void __launch_bounds__(join_bwd_threads(E), 1) join_bwd_kernel(const 
                     for (int i = 0; i < P; ++i) v[i] = mul_f32x2(alpha_2, d[i]);
                     join_store<T>(th.k, c, dres, v);
                 }
-                join_piece<T>(th.k, c, th.at(a, stage, kZ, c), z);
+                join_piece<T>(th.at(a, stage, kZ, c), z);
                 th.post(a, c, g);
 #pragma unroll
                 for (int i = 0; i < P; ++i) d[i] = mul_f32x2(d[i], r1_2);
                 if (GATED) {
-                    join_piece<T>(th.k, c, th.at(a, stage, kGate, c), v);
+                    join_piece<T>(th.at(a, stage, kGate, c), v);
                     if (a.out[2]) {
                         uint64_t o[P];
 #pragma unroll
@@ -667,6 +682,18 @@ __device__ __forceinline__ void join_read(const JoinArgs& a, int m, int64_t r, i
         for (int i = 0; i < VEC; ++i) v[i] = otherwise;
     }
 }
+template <int VEC>
+__device__ __forceinline__ void join_read_params(const void* p, int c, bool f32, float (&v)[VEC]) {
+    const bool whole = VEC > 1 && reinterpret_cast<uintptr_t>(p) % 16 == 0;       // 1 where there is none
+    if (p && whole && f32) {
+        load_vec<VEC>(static_cast<const float*>(p) + c, v);
+    } else if (p && whole) {
+        load_vec<VEC>(static_cast<const bf16_bits*>(p) + c, v);
+    } else {
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) v[i] = param(p, c + i, f32);
+    }
+}
 template <class T, int VEC>
 __global__ void __launch_bounds__(kJoinAnyThreads) join_row_sums_kernel(const __grid_constant__ JoinArgs a) {
     __shared__ float red[3 * 32];
@@ -686,11 +713,15 @@ __global__ void __launch_bounds__(kJoinAnyThreads) join_row_sums_kernel(const __
                 join_read<T, VEC>(a, kDn, r, c, 0.f, n);
                 join_read<T, VEC>(a, kH, r, c, 0.f, h);
             }
+            float gr[VEC], gp[VEC], gn[VEC];
+            join_read_params<VEC>(a.gate_row, c, a.p32, gr);
+            join_read_params<VEC>(a.gamma_post, c, a.p32, gp);
+            join_read_params<VEC>(a.gamma_pre, c, a.p32, gn);
 #pragma unroll
             for (int i = 0; i < VEC; ++i) {
-                const float w = z[i] * (g[i] * param(a.gate_row, c + i, a.p32) * param(a.gamma_post, c + i, a.p32));
+                const float w = z[i] * (g[i] * gr[i] * gp[i]);
                 if (pre) {
-                    const float a2 = n[i] * param(a.gamma_pre, c + i, a.p32);
+                    const float a2 = n[i] * gn[i];
                     s[0] = fmaf(a2, h[i], s[0]);
                     s[2] = fmaf(h[i], w, s[2]);
                     d[i] = fmaf(r2, a2, d[i]);
@@ -827,6 +858,32 @@ bool join_fit(JoinArgs& a, JoinPlan& p, int e, int vec, int threads, bool regs, 
     p.smem = size_t(ring > meet ? ring : meet);
     return true;
 }
+// Of the numbers of elements per thread in `kinds`, the one with the least estimated time per row: instructions of the
+// row's warps -- so many per element, some 200 (forward) or 250 per warp for its share of sums, copies and addresses --
+// times (1 / warps on the SM + 1 / 20), the time per instruction that was measured with 5, 10 and 20 of them.  At 5120
+// columns of bf16 that is 40 elements forward (129 us for 16384 rows; 16: 148, 32: 149, 8: 206) and 16 backward (224;
+// 32: 241, 8: 276), with a gate per element 16 (160; 40: 206) and 8 (299; 32: 438, 16: 476), of fp32 16 forward (8192
+// rows: 109; 8: 128, 40: 153) and 8 backward (176; 16: 196, 32: 260).  Of equal ones the first.
+void join_choose(JoinArgs& a, JoinPlan& p, std::initializer_list<int> kinds, int vec, int64_t width, bool bwd) {
+    const JoinArgs given = a;
+    const JoinPlan start = p;
+    double least = 0;
+    for (const int e : kinds) {
+        JoinArgs b = given;
+        JoinPlan q = start;
+        if (!join_fit(b, q, e, vec, bwd ? join_bwd_threads(e) : join_fwd_threads(e), bwd ? join_bwd_regs(e) : join_fwd_regs(e), width, bwd) ||
+            b.groups * b.stages < 2)
+            continue;
+        const int warps = b.T / 32, per = bwd ? (b.in[kGate] ? 36 : 30) : (b.in[kGate] ? 17 : 14) + (e == 32 ? 3 : 0);
+        const int fixed = (bwd ? 250 : 200) - (warps == 1 ? 80 : 0);                // a warp by itself needs no barrier
+        const double cost = warps * double(per * e + fixed) * (1.0 / (warps * b.groups) + 0.05);
+        if (p.E == 0 || cost < least) {
+            least = cost;
+            a = b;
+            p = q;
+        }
+    }
+}
 // The columns a row's pieces cover, and whether some lie partly outside it.
 int64_t join_width(const JoinArgs& a, JoinPlan& p, int vec) {
     p.shift = a.shift_step % vec != 0 || reinterpret_cast<uintptr_t>(a.in[kZ]) % 16 != 0;
@@ -858,14 +915,7 @@ int run_fwd(JoinArgs& a, bool same, cudaStream_t s) {
     JoinPlan p;
     if (same) {
         const int64_t width = join_width(a, p, vec);
-        // the fewest elements per thread with which a block still holds four rows (fewer rows: one), else the most
-        const int least = a.M >= 4 * kNumSms ? 4 : 1;
-        for (const int e : {8, 16, 40, 32}) {
-            JoinPlan q = p;
-            JoinArgs b = a;
-            if (!join_fit(b, q, e, vec, join_fwd_threads(e), join_fwd_regs(e), width, false)) continue;
-            if (e < 40 ? b.groups >= least || e == 32 : b.groups * b.stages >= 2) { a = b; p = q; break; }
-        }
+        join_choose(a, p, {8, 16, 40, 32}, vec, width, false);
     }
     switch (p.E) {
         case 8: return launch_fwd<T, 8>(a, p, s);
@@ -900,17 +950,7 @@ int run_bwd(JoinArgs& a, bool same, JoinSumArgs& sum, cudaStream_t s) {
     const int64_t width = join_width(a, p, vec);
     const bool whole = same && !p.shift;                  // every row is a number of 16-byte pieces
     if (same) {
-        // the fewest instructions per row: some 20 per element and 250 per thread (its share of sums, copies and
-        // addresses); where there are few rows, the most threads for each
-        int64_t least = INT64_MAX;
-        for (const int e : {8, 16, 32}) {
-            JoinPlan q = p;
-            JoinArgs b = a;
-            if (!join_fit(b, q, e, vec, join_bwd_threads(e), join_bwd_regs(e), width, true) || b.groups * b.stages < 2) continue;
-            const int64_t cost = int64_t(b.T) * (20 * e + 250);
-            if (cost < least) { least = cost; a = b; p = q; }
-            if (a.M <= kNumSms) break;
-        }
+        join_choose(a, p, {8, 16, 32}, vec, width, true);
     }
     const bool pre = a.norms & TPPO_NORM_PRE;
     sum.rows = p.grid;
