@@ -1,0 +1,497 @@
+// Backward pass of the residual join; see residual_norm.cuh.
+#include "residual_norm.cuh"
+
+namespace tppo {
+namespace {
+
+// The scalars of a row's backward pass, from its three sums.
+struct JoinRow { float r1, r2, k2, k1; bool good; };
+__device__ __forceinline__ JoinRow join_row(const JoinArgs& a, float r1, float r2, const float (&s)[3], bool reports) {
+    const bool post = a.norms & TPPO_NORM_POST, pre = a.norms & TPPO_NORM_PRE;
+    const float inv = 1.f / float(a.N);
+    JoinRow w;
+    w.r1 = post ? r1 : 1.f;
+    w.r2 = pre ? r2 : 0.f;
+    w.k2 = pre ? s[0] * inv * r2 * r2 * r2 : 0.f;                         // d = dh + r2 a2 - k2 h
+    w.k1 = post ? (s[1] - w.k2 * s[2]) * inv * r1 * r1 * r1 : 0.f;        // dz = r1 a1 - k1 z
+    const bool stats = !((post && r1 == 0.f) || (pre && r2 == 0.f));
+    w.good = is_finite(s[0]) && is_finite(s[1]) && is_finite(s[2]) && is_finite(w.k2) && is_finite(w.k1);
+    if (!w.good && stats && reports && a.status) atomicOr(a.status, TPPO_DEV_NONFINITE);
+    w.good = w.good && stats;
+    return w;
+}
+
+// Pairs of fp32 values, on which one instruction works at a time: at some 30 operations per element the backward pass of
+// bf16 rows is otherwise bound by its instructions.
+template <class T> struct JoinPairs { static constexpr int N = Join<T>::VEC / 2; };
+template <class T>
+__device__ __forceinline__ void join_piece(uint32_t at, uint64_t (&v)[JoinPairs<T>::N]) {
+    if constexpr (sizeof(T) == 2) {
+        const uint4 w = ptx::lds128(at);
+        v[0] = ptx::pack_f32x2(bf16_lo(w.x), bf16_hi(w.x));
+        v[1] = ptx::pack_f32x2(bf16_lo(w.y), bf16_hi(w.y));
+        v[2] = ptx::pack_f32x2(bf16_lo(w.z), bf16_hi(w.z));
+        v[3] = ptx::pack_f32x2(bf16_lo(w.w), bf16_hi(w.w));
+    } else {
+        asm volatile("ld.shared.v2.u64 {%0, %1}, [%2];" : "=l"(v[0]), "=l"(v[1]) : "r"(at));
+    }
+}
+template <class T, class C>
+__device__ __forceinline__ void join_store(const C& k, int c, T* row, const uint64_t (&v)[JoinPairs<T>::N]) {
+    if (k.all(c)) {
+        uint4 w;
+        if constexpr (sizeof(T) == 2)
+            w = make_uint4(ptx::pack_bf16x2_from_f32x2(v[0]), ptx::pack_bf16x2_from_f32x2(v[1]), ptx::pack_bf16x2_from_f32x2(v[2]),
+                           ptx::pack_bf16x2_from_f32x2(v[3]));
+        else
+            w = make_uint4(uint32_t(v[0]), uint32_t(v[0] >> 32), uint32_t(v[1]), uint32_t(v[1] >> 32));
+        *reinterpret_cast<uint4*>(row + k.col(c)) = w;
+    } else {
+#pragma unroll
+        for (int i = 0; i < Join<T>::VEC; ++i) {
+            float lo, hi;
+            ptx::unpack_f32x2(v[i / 2], lo, hi);
+            if (k.has(c, i)) store_f32(row + k.col(c) + i, i % 2 ? hi : lo);
+        }
+    }
+}
+
+template <class T, int E, bool PRE, bool GATED, bool SHIFT>
+__global__ void __launch_bounds__(join_threads(E), 1) join_bwd_kernel(const __grid_constant__ JoinArgs a) {
+    extern __shared__ __align__(16) uint8_t smem[];
+    typedef JoinThread<T, E, SHIFT, join_bwd_regs(E), kBwdIn> Thread;
+    constexpr int VEC = Thread::VEC, CH = Thread::CH, P = VEC / 2;
+    Thread th(a, smem);
+    pdl_launch();
+    pdl_wait();
+    for (int s = 0; s < a.stages; ++s) th.fetch(a, th.row + s * th.step, s);
+    th.load_params(a, smem);
+    __syncthreads();
+    using ptx::fma_f32x2;
+    using ptx::mul_f32x2;
+    const bool add = a.in[kDh] != nullptr, post = a.norms & TPPO_NORM_POST;
+    uint64_t sum_post[CH][P], sum_pre[CH][P];
+#pragma unroll
+    for (int c = 0; c < CH; ++c)
+#pragma unroll
+        for (int i = 0; i < P; ++i) sum_post[c][i] = sum_pre[c][i] = 0;
+    int stage = 0;
+    float r1_next = post && th.row < a.M ? a.r_post[th.row] : 1.f, r2_next = PRE && th.row < a.M ? a.r_pre[th.row] : 0.f;
+    for (int64_t r = th.row; r < a.M; r += th.step) {
+        const float r1 = r1_next, r2 = r2_next;
+        if (r + th.step < a.M) {                          // a row ahead, like the copies
+            if (post) r1_next = a.r_post[r + th.step];
+            if (PRE) r2_next = a.r_pre[r + th.step];
+        }
+        th.land(a, stage);
+        const uint64_t r2_2 = ptx::pack_f32x2(r2, r2);
+        uint64_t q[3] = {0, 0, 0};
+#pragma unroll
+        for (int c = 0; c < CH; ++c) {
+            if (!th.k.any(c)) continue;
+            uint64_t w[P], d[P], g[P];
+            join_piece<T>(th.at(a, stage, kZ, c), w);
+            th.post(a, c, g);
+#pragma unroll
+            for (int i = 0; i < P; ++i) w[i] = mul_f32x2(w[i], g[i]);
+            if (GATED) {
+                join_piece<T>(th.at(a, stage, kGate, c), g);
+#pragma unroll
+                for (int i = 0; i < P; ++i) w[i] = mul_f32x2(w[i], g[i]);
+            }
+#pragma unroll
+            for (int i = 0; i < P; ++i) d[i] = 0;
+            if (add) join_piece<T>(th.at(a, stage, kDh, c), d);
+            if (PRE) {
+                uint64_t n[P], h[P];
+                join_piece<T>(th.at(a, stage, kDn, c), n);
+                join_piece<T>(th.at(a, stage, kH, c), h);
+                th.pre(a, c, g);
+#pragma unroll
+                for (int i = 0; i < P; ++i) {
+                    n[i] = mul_f32x2(n[i], g[i]);
+                    q[0] = fma_f32x2(n[i], h[i], q[0]);
+                    q[2] = fma_f32x2(h[i], w[i], q[2]);
+                    d[i] = fma_f32x2(r2_2, n[i], d[i]);
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < P; ++i) q[1] = fma_f32x2(d[i], w[i], q[1]);
+        }
+        float s[3];
+#pragma unroll
+        for (int i = 0; i < 3; ++i) {
+            float lo, hi;
+            ptx::unpack_f32x2(q[i], lo, hi);
+            s[i] = lo + hi;
+        }
+        th.sum(s);
+        const JoinRow w = join_row(a, r1, r2, s, th.t == 0);
+        T* dz = static_cast<T*>(a.out[0]) + (a.out[0] ? r * a.ldo[0] : 0);
+        T* dres = static_cast<T*>(a.out[1]) + (a.out[1] ? r * a.ldo[1] : 0);
+        T* dgate = static_cast<T*>(a.out[2]) + (a.out[2] ? r * a.ldo[2] : 0);
+        if (w.good) {
+            const uint64_t r1_2 = ptx::pack_f32x2(w.r1, w.r1), k1_2 = ptx::pack_f32x2(-w.k1, -w.k1), k2_2 = ptx::pack_f32x2(-w.k2, -w.k2);
+            const uint64_t alpha_2 = ptx::pack_f32x2(a.alpha, a.alpha);
+#pragma unroll
+            for (int c = 0; c < CH; ++c) {
+                if (!th.k.any(c)) continue;
+                uint64_t z[P], d[P], g[P], v[P];
+#pragma unroll
+                for (int i = 0; i < P; ++i) d[i] = 0;
+                if (add) join_piece<T>(th.at(a, stage, kDh, c), d);
+                if (PRE) {
+                    uint64_t n[P], h[P];
+                    join_piece<T>(th.at(a, stage, kDn, c), n);
+                    join_piece<T>(th.at(a, stage, kH, c), h);
+                    th.pre(a, c, g);
+#pragma unroll
+                    for (int i = 0; i < P; ++i) {
+                        n[i] = mul_f32x2(n[i], r2_2);
+                        sum_pre[c][i] = fma_f32x2(n[i], h[i], sum_pre[c][i]);
+                        d[i] = fma_f32x2(k2_2, h[i], fma_f32x2(n[i], g[i], d[i]));
+                    }
+                }
+                if (a.out[1]) {
+#pragma unroll
+                    for (int i = 0; i < P; ++i) v[i] = mul_f32x2(alpha_2, d[i]);
+                    join_store<T>(th.k, c, dres, v);
+                }
+                join_piece<T>(th.at(a, stage, kZ, c), z);
+                th.post(a, c, g);
+#pragma unroll
+                for (int i = 0; i < P; ++i) d[i] = mul_f32x2(d[i], r1_2);
+                if (GATED) {
+                    join_piece<T>(th.at(a, stage, kGate, c), v);
+                    if (a.out[2]) {
+                        uint64_t o[P];
+#pragma unroll
+                        for (int i = 0; i < P; ++i) o[i] = mul_f32x2(mul_f32x2(d[i], z[i]), g[i]);
+                        join_store<T>(th.k, c, dgate, o);
+                    }
+#pragma unroll
+                    for (int i = 0; i < P; ++i) d[i] = mul_f32x2(d[i], v[i]);
+                }
+#pragma unroll
+                for (int i = 0; i < P; ++i) sum_post[c][i] = fma_f32x2(d[i], z[i], sum_post[c][i]);
+                if (a.out[0]) {
+#pragma unroll
+                    for (int i = 0; i < P; ++i) v[i] = fma_f32x2(k1_2, z[i], mul_f32x2(d[i], g[i]));
+                    join_store<T>(th.k, c, dz, v);
+                }
+            }
+        } else {                                          // the same for the whole group
+            if (a.out[0]) th.store_zeros(dz);
+            if (a.out[1]) th.store_zeros(dres);
+            if (a.out[2]) th.store_zeros(dgate);
+        }
+        th.fetch(a, r + a.stages * th.step, stage);
+        if (++stage == a.stages) stage = 0;
+    }
+    if (!a.partial) return;
+    // the groups' sums meet in the ring's memory: group 0 adds the others' to its own, in order
+    asm volatile("cp.async.wait_group 0;" ::: "memory");
+    __syncthreads();
+    float* all = reinterpret_cast<float*>(smem + kJoinRedBytes);           // [group][2 * E][T]
+    if (th.group > 0) {
+#pragma unroll
+        for (int c = 0; c < CH; ++c)
+#pragma unroll
+            for (int i = 0; i < P; ++i) {
+                float* to = all + ((th.group - 1) * 2 * E + c * VEC + 2 * i) * a.T + th.t;
+                ptx::unpack_f32x2(sum_post[c][i], to[0], to[a.T]);
+                ptx::unpack_f32x2(sum_pre[c][i], to[E * a.T], to[(E + 1) * a.T]);
+            }
+    }
+    __syncthreads();
+    if (th.group > 0) return;
+    float* part = a.partial + int64_t(blockIdx.x) * 2 * a.N;
+#pragma unroll
+    for (int c = 0; c < CH; ++c)
+#pragma unroll
+        for (int i = 0; i < P; ++i) {
+            float v[4];
+            ptx::unpack_f32x2(sum_post[c][i], v[0], v[1]);
+            ptx::unpack_f32x2(sum_pre[c][i], v[2], v[3]);
+            for (int g = 1; g < a.groups; ++g) {
+                const float* from = all + ((g - 1) * 2 * E + c * VEC + 2 * i) * a.T + th.t;
+                v[0] += from[0]; v[1] += from[a.T];
+                v[2] += from[E * a.T]; v[3] += from[(E + 1) * a.T];
+            }
+#pragma unroll
+            for (int l = 0; l < 2; ++l)
+                if (th.k.has(c, 2 * i + l)) {
+                    part[th.k.col(c) + 2 * i + l] = v[l];
+                    part[int64_t(a.N) + th.k.col(c) + 2 * i + l] = v[2 + l];
+                }
+        }
+}
+
+// ---- any length and alignment --------------------------------------------------------------------------------
+// Backward pass of such rows in two launches: the three sums of every row, then, with no thread depending on another,
+// the gradients, a block walking down its strip of columns.  10 elements moved per element of a row instead of 6.
+// VEC: columns per access, 16 bytes' worth where all rows start and end on 16-byte boundaries, else 1.
+template <class T, int VEC>
+__device__ __forceinline__ void join_read(const JoinArgs& a, int m, int64_t r, int c, float otherwise, float (&v)[VEC]) {
+    if (a.in[m]) {
+        load_vec<VEC>(static_cast<const T*>(a.in[m]) + r * a.ld[m] + c, v);
+    } else {
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) v[i] = otherwise;
+    }
+}
+template <int VEC>
+__device__ __forceinline__ void join_read_params(const void* p, int c, bool f32, float (&v)[VEC]) {
+    const bool whole = VEC > 1 && reinterpret_cast<uintptr_t>(p) % 16 == 0;       // 1 where there is none
+    if (p && whole && f32) {
+        load_vec<VEC>(static_cast<const float*>(p) + c, v);
+    } else if (p && whole) {
+        load_vec<VEC>(static_cast<const bf16_bits*>(p) + c, v);
+    } else {
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) v[i] = param(p, c + i, f32);
+    }
+}
+template <class T, int VEC>
+__global__ void __launch_bounds__(kJoinAnyThreads) join_row_sums_kernel(const __grid_constant__ JoinArgs a) {
+    __shared__ float red[3 * 32];
+    pdl_launch();
+    pdl_wait();
+    const bool pre = a.norms & TPPO_NORM_PRE;
+    for (int64_t r = blockIdx.x; r < a.M; r += gridDim.x) {
+        const float r1 = a.r_post ? a.r_post[r] : 1.f, r2 = a.r_pre ? a.r_pre[r] : 0.f;
+        float s[3] = {0.f, 0.f, 0.f};
+#pragma unroll 2
+        for (int c = threadIdx.x * VEC; c < a.N; c += kJoinAnyThreads * VEC) {
+            float z[VEC], g[VEC], d[VEC], n[VEC], h[VEC];
+            join_read<T, VEC>(a, kZ, r, c, 0.f, z);
+            join_read<T, VEC>(a, kGate, r, c, 1.f, g);
+            join_read<T, VEC>(a, kDh, r, c, 0.f, d);
+            if (pre) {
+                join_read<T, VEC>(a, kDn, r, c, 0.f, n);
+                join_read<T, VEC>(a, kH, r, c, 0.f, h);
+            }
+            float gr[VEC], gp[VEC], gn[VEC];
+            join_read_params<VEC>(a.gate_row, c, a.p32, gr);
+            join_read_params<VEC>(a.gamma_post, c, a.p32, gp);
+            join_read_params<VEC>(a.gamma_pre, c, a.p32, gn);
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) {
+                const float w = z[i] * (g[i] * gr[i] * gp[i]);
+                if (pre) {
+                    const float a2 = n[i] * gn[i];
+                    s[0] = fmaf(a2, h[i], s[0]);
+                    s[2] = fmaf(h[i], w, s[2]);
+                    d[i] = fmaf(r2, a2, d[i]);
+                }
+                s[1] = fmaf(d[i], w, s[1]);
+            }
+        }
+        block_sums(s, red);
+        if (threadIdx.x == 0) {
+            const JoinRow w = join_row(a, r1, r2, s, true);
+            // zeros: a row to leave out
+            a.rows[r] = w.good ? make_float4(w.r1, w.r2, w.k1, w.k2) : make_float4(0.f, 0.f, 0.f, 0.f);
+        }
+    }
+}
+
+constexpr int kJoinStrip = 128;                           // threads of a strip
+template <class T, int VEC>
+__global__ void __launch_bounds__(kJoinStrip) join_columns_kernel(const __grid_constant__ JoinArgs a) {
+    pdl_launch();
+    pdl_wait();
+    const bool pre = a.norms & TPPO_NORM_PRE;
+    const int64_t chunk = blockIdx.y, r0 = a.M * chunk / gridDim.y, r1 = a.M * (chunk + 1) / gridDim.y;
+    const int64_t at = (int64_t(blockIdx.x) * kJoinStrip + threadIdx.x) * VEC;
+    if (at >= a.N) return;
+    const int c = int(at);
+    float g[VEC], gn[VEC], sum_post[VEC], sum_pre[VEC];
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) {
+        g[i] = param(a.gate_row, c + i, a.p32) * param(a.gamma_post, c + i, a.p32);
+        gn[i] = param(a.gamma_pre, c + i, a.p32);
+        sum_post[i] = sum_pre[i] = 0;
+    }
+#pragma unroll 2
+    for (int64_t r = r0; r < r1; ++r) {
+        const float4 w = __ldcg(a.rows + r);
+        float z[VEC], gv[VEC], d[VEC], n[VEC], h[VEC], o[VEC];
+        join_read<T, VEC>(a, kZ, r, c, 0.f, z);
+        join_read<T, VEC>(a, kGate, r, c, 1.f, gv);
+        join_read<T, VEC>(a, kDh, r, c, 0.f, d);
+        if (pre) {
+            join_read<T, VEC>(a, kDn, r, c, 0.f, n);
+            join_read<T, VEC>(a, kH, r, c, 0.f, h);
+        }
+        const bool good = w.x != 0.f;                     // r1 of a row with statistics is not 0
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) {
+            if (pre) {
+                const float m = n[i] * w.y;
+                if (good) sum_pre[i] = fmaf(m, h[i], sum_pre[i]);
+                d[i] = fmaf(-w.w, h[i], fmaf(m, gn[i], d[i]));
+            }
+            o[i] = good ? a.alpha * d[i] : 0.f;
+            d[i] *= w.x;
+        }
+        if (a.out[1]) store_vec<VEC>(static_cast<T*>(a.out[1]) + r * a.ldo[1] + c, o);
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) {
+            o[i] = good ? d[i] * z[i] * g[i] : 0.f;
+            d[i] *= gv[i];
+            if (good) sum_post[i] = fmaf(d[i], z[i], sum_post[i]);
+        }
+        if (a.out[2]) store_vec<VEC>(static_cast<T*>(a.out[2]) + r * a.ldo[2] + c, o);
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) o[i] = good ? fmaf(-w.z, z[i], d[i] * g[i]) : 0.f;
+        if (a.out[0]) store_vec<VEC>(static_cast<T*>(a.out[0]) + r * a.ldo[0] + c, o);
+    }
+    if (a.partial) {
+        float* part = a.partial + chunk * 2 * a.N;
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) {
+            part[c + i] = sum_post[i];
+            part[int64_t(a.N) + c + i] = sum_pre[i];
+        }
+    }
+}
+
+// Adds the blocks' partial rows up in a fixed order (eight strands of them) and finishes the gradients:
+//     dgamma_post = gate row * S, dgate row = gamma_post * S, dgamma_pre = the second sum.
+struct JoinSumArgs {
+    const float* partial; int64_t rows; int32_t N;
+    const void* gate_row; const void* gamma_post;
+    void* dgate_row; void* dgamma_post; void* dgamma_pre; int32_t p32;
+};
+__global__ void __launch_bounds__(256) join_sum_kernel(const JoinSumArgs a) {
+    __shared__ float red[8][32];
+    pdl_launch();
+    pdl_wait();
+    const int lane = threadIdx.x & 31, strand = threadIdx.x >> 5;
+    const int64_t col = int64_t(blockIdx.x) * 32 + lane, all = int64_t(2) * a.N;
+    float v = 0;
+    if (col < all) {
+#pragma unroll 8
+        for (int64_t r = strand; r < a.rows; r += 8) v += __ldcg(a.partial + r * all + col);
+    }
+    red[strand][lane] = v;
+    __syncthreads();
+    if (strand != 0 || col >= all) return;
+    for (int i = 1; i < 8; ++i) v += red[i][lane];
+    if (col < a.N) {
+        if (a.dgamma_post) put_param(a.dgamma_post, col, a.p32, v * param(a.gate_row, col, a.p32));
+        if (a.dgate_row) put_param(a.dgate_row, col, a.p32, v * param(a.gamma_post, col, a.p32));
+    } else if (a.dgamma_pre) {
+        put_param(a.dgamma_pre, col - a.N, a.p32, v);
+    }
+}
+
+// ---- host side --------------------------------------------------------------------------------------------------
+template <class T, int E, bool PRE>
+int launch_bwd(const JoinArgs& a, const JoinPlan& p, cudaStream_t s) {
+    auto kernel = a.in[kGate] ? (p.shift ? join_bwd_kernel<T, E, PRE, true, true> : join_bwd_kernel<T, E, PRE, true, false>)
+                              : (p.shift ? join_bwd_kernel<T, E, PRE, false, true> : join_bwd_kernel<T, E, PRE, false, false>);
+    TPPO_CUDA_CHECK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kJoinSmem));
+    TPPO_CUDA_CHECK(launch_dense(kernel, dim3(p.grid), dim3(a.T * a.groups), p.smem, s, a));
+    return TPPO_OK;
+}
+
+int64_t join_chunks(int64_t M) { return M < kJoinAnyBlocks ? (M + 7) / 8 * 8 : kJoinAnyBlocks; }
+
+template <class T, int VEC>
+int run_bwd_any(JoinArgs& a, JoinSumArgs& sum, cudaStream_t s) {
+    TPPO_CUDA_CHECK(launch_dense(join_row_sums_kernel<T, VEC>, dim3(unsigned(a.M < 4 * kNumSms ? a.M : 4 * kNumSms)), dim3(kJoinAnyThreads), 0, s, a));
+    // enough chunks of rows to fill the GPU some times over
+    const int64_t strips = (int64_t(a.N) + kJoinStrip * VEC - 1) / (kJoinStrip * VEC), most = join_chunks(a.M);
+    int64_t chunks = (32 * kNumSms + strips - 1) / strips;
+    if (chunks > (a.M + 7) / 8) chunks = (a.M + 7) / 8;
+    if (chunks > most) chunks = most;
+    sum.rows = chunks;
+    TPPO_CUDA_CHECK(launch_dense(join_columns_kernel<T, VEC>, dim3(unsigned(strips), unsigned(chunks)), dim3(kJoinStrip), 0, s, a));
+    return TPPO_OK;
+}
+
+template <class T>
+int run_bwd(JoinArgs& a, bool same, JoinSumArgs& sum, cudaStream_t s) {
+    constexpr int vec = Join<T>::VEC;
+    JoinPlan p;
+    const int64_t width = join_width(a, p, vec);
+    const bool whole = same && !p.shift;                  // every row is a number of 16-byte pieces
+    if (same) {
+        join_choose(a, p, {8, 16}, vec, width, true);
+    }
+    sum.rows = p.grid;
+    const bool pre = a.norms & TPPO_NORM_PRE;
+    if (p.E == 8) return pre ? launch_bwd<T, 8, true>(a, p, s) : launch_bwd<T, 8, false>(a, p, s);
+    if (p.E == 16) return pre ? launch_bwd<T, 16, true>(a, p, s) : launch_bwd<T, 16, false>(a, p, s);
+    return whole ? run_bwd_any<T, vec>(a, sum, s) : run_bwd_any<T, 1>(a, sum, s);
+}
+
+}  // namespace
+
+// The rows' scalars in front, the partial column sums behind them.
+static size_t join_rows_bytes(int64_t M) { return align_up(size_t(M > 0 ? M : 1) * sizeof(float4), kWsAlign); }
+size_t residual_norm_workspace_bytes(int64_t M, int32_t N) {
+    if (N <= 0) return 0;
+    return join_rows_bytes(M) + align_up(size_t(M > 0 ? join_chunks(M) : 1) * 2 * size_t(N) * sizeof(float), kWsAlign);
+}
+
+}  // namespace tppo
+
+TPPO_API int tppo_residual_norm_bwd(const void* dh, int64_t lddh, const void* dn, int64_t lddn, const void* z, int64_t ldz,
+                                    const void* h, int64_t ldh, const void* gate, int64_t ldg, int32_t dtype, int64_t M, int32_t N,
+                                    const void* gamma_post, const void* gamma_pre, int32_t param_dtype,
+                                    const float* rstd_post, const float* rstd_pre, float alpha, int32_t norms,
+                                    void* dz, int64_t lddz, void* dresidual, int64_t lddr, void* dgate, int64_t lddg,
+                                    void* dgamma_post, void* dgamma_pre, int32_t* status, void* workspace, size_t workspace_bytes,
+                                    void* stream) {
+    using namespace tppo;
+    if (M < 0 || N < 1 || !type_ok(dtype) || !type_ok(param_dtype) || (norms & ~3) || !is_finite_host(alpha)) return TPPO_ERR_INVALID_ARG;
+    const bool post = norms & TPPO_NORM_POST, pre = norms & TPPO_NORM_PRE;
+    const bool full = gate && ldg != 0;
+    if ((gamma_post && !post) || (gamma_pre && !pre) || (dgamma_post && !post) || (dgamma_pre && !pre) || (dgate && !gate))
+        return TPPO_ERR_INVALID_ARG;
+    if (M > 0 && (!z || (dn != nullptr) != pre || (h != nullptr) != pre || (rstd_post != nullptr) != post || (rstd_pre != nullptr) != pre))
+        return TPPO_ERR_INVALID_ARG;
+    if (ldz < N || (dh && lddh < N) || (pre && (lddn < N || ldh < N)) || (full && ldg < N) || (dz && lddz < N) || (dresidual && lddr < N) ||
+        (dgate && full && lddg < N))
+        return TPPO_ERR_INVALID_ARG;
+    const size_t e = size_of(dtype), pe = size_of(param_dtype);
+    if (!aligned(dh, e) || !aligned(dn, e) || !aligned(z, e) || !aligned(h, e) || !aligned(gate, full ? e : pe) || !aligned(dz, e) ||
+        !aligned(dresidual, e) || !aligned(dgate, full ? e : pe) || !aligned(gamma_post, pe) || !aligned(gamma_pre, pe) ||
+        !aligned(dgamma_post, pe) || !aligned(dgamma_pre, pe) || !aligned(rstd_post, 4) || !aligned(rstd_pre, 4) || !aligned(status, 4))
+        return TPPO_ERR_INVALID_ARG;
+    if (M > kDenseMaxSize || N > kDenseMaxSize) return TPPO_ERR_UNSUPPORTED;
+    const bool sums = dgamma_post || dgamma_pre || (dgate && !full);
+    if (!workspace || !aligned(workspace, kWsAlign) || workspace_bytes < residual_norm_workspace_bytes(M, N)) return TPPO_ERR_WORKSPACE;
+    JoinArgs a{};
+    a.in[kZ] = z; a.ld[kZ] = ldz;
+    if (pre) { a.in[kH] = h; a.ld[kH] = ldh; a.in[kDn] = dn; a.ld[kDn] = lddn; }
+    if (dh) { a.in[kDh] = dh; a.ld[kDh] = lddh; }
+    if (full) { a.in[kGate] = gate; a.ld[kGate] = ldg; }
+    for (int i = 0; i < kBwdIn; ++i)
+        if (a.in[i]) a.slot[i] = a.arrays++;
+    a.gate_row = full ? nullptr : gate;
+    a.gamma_post = gamma_post; a.gamma_pre = gamma_pre; a.p32 = param_dtype == TPPO_F32;
+    a.out[0] = dz; a.out[1] = dresidual; a.out[2] = full ? dgate : nullptr;
+    a.ldo[0] = lddz; a.ldo[1] = lddr; a.ldo[2] = lddg;
+    a.r_post = const_cast<float*>(rstd_post); a.r_pre = const_cast<float*>(rstd_pre);
+    a.rows = static_cast<float4*>(workspace);
+    a.partial = sums ? reinterpret_cast<float*>(static_cast<char*>(workspace) + join_rows_bytes(M)) : nullptr;
+    a.status = status;
+    a.M = M; a.N = N; a.alpha = alpha; a.norms = norms;
+    a.shift_step = int32_t(ldz % 16);
+    bool same = true;
+    for (int i = 0; i < kBwdIn; ++i) same = same && same_start(z, ldz, a.in[i], a.ld[i], e);
+    for (int i = 0; i < 3; ++i) same = same && same_start(z, ldz, a.out[i], a.ldo[i], e);
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    JoinSumArgs sum{a.partial, 0, N, a.gate_row, gamma_post, full ? nullptr : dgate, dgamma_post, dgamma_pre, a.p32};
+    if (M > 0) {
+        const int r = dtype == TPPO_F32 ? run_bwd<float>(a, same, sum, s) : run_bwd<bf16_bits>(a, same, sum, s);
+        if (r != TPPO_OK) return r;
+    }
+    if (!sums) return TPPO_OK;
+    TPPO_CUDA_CHECK(launch_dense(join_sum_kernel, dim3(unsigned((int64_t(2) * N + 31) / 32)), dim3(256), 0, s, sum));
+    return TPPO_OK;
+}

@@ -133,3 +133,16 @@ def vocab_parallel_step(stats_fn, rescale_fn, grads_fn, group=None):
     if dhidden is not None and multi:
         dist.all_reduce(dhidden, op=dist.ReduceOp.SUM, group=group)
     return dhidden
+
+
+def global_sum_sq(sum_sq, group=None):
+    """The sum of squares over the gradients of all ranks, in place, from each rank's own.
+
+    sum_sq: this rank's [1] float64 tensor (on a GPU: of `binding.tppo_grad_norm` over the gradients that this rank alone
+    holds -- a gradient that several ranks hold is listed on one of them).  One all-reduce of eight bytes; every rank then
+    passes the result to `binding.tppo_grad_clip` and scales its gradients by the same coefficient.  A rank whose gradients
+    are not finite reports +infinity, which stays so in the sum, and all ranks skip the step alike."""
+    import torch.distributed as dist
+    if dist.is_available() and dist.is_initialized() and dist.get_world_size(group) > 1:
+        dist.all_reduce(sum_sq, op=dist.ReduceOp.SUM, group=group)
+    return sum_sq
