@@ -319,12 +319,12 @@ def _matrix(t, here, rows, cols, dtype=None):
         return None, 0
     assert t.get_device() == here, f"tensors must be on cuda:{here}, the current device"
     assert t.shape == (rows, cols), f"expected shape {(rows, cols)}, got {tuple(t.shape)}"
-    assert dtype is None or t.dtype == dtype, f"expected {dtype}, got {t.dtype}"
+    assert dtype is None or t.dtype is dtype, f"expected {dtype}, got {t.dtype}"
     ld, one = t.stride()
     assert one == 1 or cols == 1, "columns must be contiguous"
-    if rows <= 1:
-        ld = max(ld, cols)
-    assert ld >= cols, "rows must not overlap"
+    if ld < cols:
+        assert rows <= 1, "rows must not overlap"
+        ld = cols
     return t.data_ptr(), ld
 
 
@@ -471,8 +471,10 @@ def fp8_scales(rows, cols, block, device):
 
 
 def _scales(t, here, rows, cols, block):
-    kb = -(-cols // 128)
-    return _matrix(t, here, *((-(-rows // 128), kb) if block == FP8_SQUARE else (kb, rows)), torch.float32)
+    if block == FP8_SQUARE:
+        rows = -(-rows // 128)
+        return _matrix(t, here, rows, -(-cols // 128), torch.float32)
+    return _matrix(t, here, -(-cols // 128), rows, torch.float32)
 
 
 def tppo_fp8_quantize(x, block, q, scale, qt, scale_t, status):

@@ -540,15 +540,18 @@ struct F8Operand { const void* p; int64_t rows, ld; F8Scales s; };
 
 // How a product is cut: bn 0 = the persistent kernel, else the split kernel's columns (output rows) per tile and the
 // CTAs that share a tile's contraction: the least estimated time in SM clocks.  A block of 128 bytes moves as many
-// operand bytes as a step of the 16-bit products, whose fitted constants serve here.
+// operand bytes as a step of the 16-bit products, whose fitted constants serve here; the persistent kernel takes some
+// 600 per block and 6000 at the ends, 18000 where its last output rows leave one element at a time.  Of 20 sizes from
+// 1 x 1024 x 1024 to 2048 x 5120 x 5120, timed with every cut, the choice is the best or within 5 % of it but for 515 x
+// 777 x 1001 (8.7 us; 7.2 with 32 columns and two CTAs).
 struct F8Cut { int bn, splits; };
-F8Cut f8_cut(int64_t m, int64_t n, int64_t blocks) {
+F8Cut f8_cut(int64_t m, int64_t n, int64_t blocks, bool whole_rows) {
     // CTAs that fit on the GPU at once in clusters of s, at two and at one per SM (the driver's count)
     static const int64_t pair[9] = {0, 296, 296, 279, 284, 280, 270, 259, 264};
     static const int64_t alone[9] = {0, 148, 148, 135, 132, 130, 132, 105, 120};
     const int64_t rows = (n + 127) / 128, big = (m + 127) / 128 * ((n + kF8BN - 1) / kF8BN);
     F8Cut best{0, 1};
-    int64_t least = 5000 + (big + kNumSms - 1) / kNumSms * blocks * 600 + 6000;
+    int64_t least = 5000 + (big + kNumSms - 1) / kNumSms * blocks * 600 + (whole_rows ? 6000 : 18000);
     for (int bn = 16; bn <= 128; bn *= 2) {
         const int64_t tiles = rows * ((m + bn - 1) / bn);
         const int64_t stages = bn <= 16 ? 5 : bn <= 32 ? 4 : bn <= 64 ? 3 : 6;
@@ -617,7 +620,7 @@ int f8_split(const F8Operand& a, const F8Operand& b, int64_t K, int64_t blocks, 
 template <class T>
 int f8_product(const F8Operand& a, const F8Operand& b, int64_t K, const F8Out& out, cudaStream_t s) {
     const int64_t blocks = (K + kF8Block - 1) / kF8Block;
-    const F8Cut c = f8_cut(a.rows, b.rows, blocks);
+    const F8Cut c = f8_cut(a.rows, b.rows, blocks, out.aligned != 0);
     switch (c.bn) {                          // the split kernel's rows are the output's columns
         case 16: return f8_split<T, 16>(b, a, K, blocks, c.splits, out, s);
         case 32: return f8_split<T, 32>(b, a, K, blocks, c.splits, out, s);

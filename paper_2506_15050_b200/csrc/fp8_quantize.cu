@@ -40,6 +40,40 @@ __device__ __forceinline__ uint32_t pack_e4m3x2(float lo, float hi) {
 
 // A thread's 8 x 8 elements as loaded (32 registers of bf16, 64 of fp32), magnitudes as bit patterns, which order
 // like the numbers: their maxima take one packed instruction per two bf16 elements, and a NaN or infinity shows in them.
+// N words that start `offset` bytes (a multiple of 2) into a 16-byte piece, from the pieces they touch.
+template <int N>
+__device__ __forceinline__ void quant_align(const uint32_t (&in)[N + 4], int offset, uint32_t* out) {
+    uint32_t a[N + 2], b[N + 1];
+#pragma unroll
+    for (int i = 0; i < N + 2; ++i) a[i] = offset & 8 ? in[i + 2] : in[i];
+#pragma unroll
+    for (int i = 0; i < N + 1; ++i) b[i] = offset & 4 ? a[i + 1] : a[i];
+#pragma unroll
+    for (int i = 0; i < N; ++i) out[i] = __funnelshift_r(b[i], b[i + 1], (offset & 2) * 8);
+}
+// Eight elements at p, of which the first `cols` belong to the row (0 for the others), from whole 16-byte pieces: a piece
+// with one of them in it is mapped, whatever else it holds.
+template <class T>
+__device__ __forceinline__ void quant_read(const T* p, int cols, uint32_t* out) {
+    constexpr int N = 8 * sizeof(T) / 4;
+    const int offset = int(reinterpret_cast<uintptr_t>(p) & 15), bytes = cols < 8 ? cols * int(sizeof(T)) : 4 * N;
+    const uint4* g = reinterpret_cast<const uint4*>(reinterpret_cast<const char*>(p) - offset);
+    uint32_t in[N + 4];
+#pragma unroll
+    for (int i = 0; i < N / 4 + 1; ++i) {
+        uint4 v = make_uint4(0, 0, 0, 0);
+        if (bytes > 0 && 16 * i < offset + bytes) v = g[i];
+        in[4 * i] = v.x; in[4 * i + 1] = v.y; in[4 * i + 2] = v.z; in[4 * i + 3] = v.w;
+    }
+    quant_align<N>(in, offset, out);
+    if (cols < 8) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const int left = bytes - 4 * i;               // bytes of word i that count
+            out[i] = left >= 4 ? out[i] : left == 2 ? out[i] & 0xffffu : 0u;
+        }
+    }
+}
 template <class T> struct QuantTile;
 template <> struct QuantTile<bf16_bits> {
     uint32_t w[8][4];
@@ -49,9 +83,7 @@ template <> struct QuantTile<bf16_bits> {
             const uint4 v = __ldcs(reinterpret_cast<const uint4*>(p));
             w[i][0] = v.x; w[i][1] = v.y; w[i][2] = v.z; w[i][3] = v.w;
         } else {
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-                w[i][j] = (2 * j < cols ? uint32_t(p[2 * j]) : 0u) | (2 * j + 1 < cols ? uint32_t(p[2 * j + 1]) << 16 : 0u);
+            quant_read(p, cols, w[i]);
         }
     }
     __device__ __forceinline__ float get(int i, int j) const { return j % 2 ? bf16_hi(w[i][j / 2]) : bf16_lo(w[i][j / 2]); }
@@ -105,8 +137,10 @@ template <> struct QuantTile<float> {
         if (cols >= 8 && vec) {
             load_vec<8>(p, v[i]);
         } else {
+            uint32_t w[8];
+            quant_read(p, cols, w);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) v[i][j] = j < cols ? p[j] : 0.f;
+            for (int j = 0; j < 8; ++j) v[i][j] = __uint_as_float(w[j]);
         }
     }
     __device__ __forceinline__ float get(int i, int j) const { return v[i][j]; }
