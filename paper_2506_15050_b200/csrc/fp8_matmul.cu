@@ -11,7 +11,12 @@
 // from registers (tcgen05.st), four blocks of the contraction at a time, one per byte.  A scale that is not a power of
 // two becomes the exponent's NaN, and its outputs 0 with TPPO_DEV_NONFINITE.
 //
-//   fp8_gemm_kernel   many output tiles: persistent CTAs, 128 x 240 tiles: two accumulators, so that the output of
+// The tensor cores drop what lies below the accumulator's last bit at every step of 32: over a contraction of 4096 that
+// is 2e-7 of the result, and it grows with the length.  For bf16 outputs it does not show; for fp32 ones the output
+// warps take the sums over eight blocks at a time and add them up in registers (5e-8, whatever the length), on narrower
+// tiles whose sums the registers hold.
+//
+//   fp8_gemm_kernel   many output tiles: persistent CTAs, 128 x 240 tiles (192 for fp32): two accumulators, so that the output of
 //                     a tile overlaps the products of the next, and 32 columns of tensor memory for exponents.
 //   fp8_split_kernel  few output tiles (one to some hundred tokens): the output is taken TRANSPOSED, the 128 accumulator
 //                     rows running along n and the BN columns along m, and the contraction is split over the CTAs of
@@ -49,6 +54,13 @@ __device__ __forceinline__ void f8_tmem_ld8(uint32_t taddr, uint32_t (&v)[8]) {
     asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
                  : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7])
                  : "r"(taddr) : "memory");
+}
+__device__ __forceinline__ void f8_tmem_ld16(uint32_t taddr, uint32_t (&v)[16]) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+        : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]), "=r"(v[8]), "=r"(v[9]),
+          "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15])
+        : "r"(taddr) : "memory");
 }
 __device__ __forceinline__ void f8_tmem_st4(uint32_t taddr, const uint32_t* v) {
     asm volatile("tcgen05.st.sync.aligned.32x32b.x4.b32 [%0], {%1, %2, %3, %4};"
@@ -205,12 +217,16 @@ __device__ __forceinline__ float f8_finish(float v, bool& bad) {
 }
 
 // ---- many tiles -------------------------------------------------------------------------------------------------
-constexpr int kF8BN = 240, kF8Stages = 4;
+template <class T> __host__ __device__ constexpr int f8_bn() { return sizeof(T) == 4 ? 192 : 240; }
+template <class T> __host__ __device__ constexpr int f8_segment() { return sizeof(T) == 4 ? 8 : 1 << 30; }       // blocks summed by the tensor cores
+constexpr int kF8Stages = 4;
 constexpr int kF8GemmThreads = 448;                       // warps 0-3 exponents, 4-11 output, 12 TMA loads, 13 tcgen05.mma
 constexpr int kF8OutWarps = 8;
 constexpr uint32_t kF8Staging = 4096;                     // per output warp: 32 rows of 128 bytes
-constexpr size_t kF8Smem = size_t(kF8Stages) * (kF8ABytes + kF8BN * kF8Block) + kF8OutWarps * kF8Staging +
-                           F8Ring<kF8BN, kF8Stages>::kCells + 1024 /* alignment */ + 128 /* barriers */;
+template <class T> __host__ __device__ constexpr size_t f8_smem() {
+    return size_t(kF8Stages) * (kF8ABytes + f8_bn<T>() * kF8Block) + kF8OutWarps * kF8Staging + F8Ring<f8_bn<T>(), kF8Stages>::kCells +
+           1024 /* alignment */ + 128 /* barriers */;
+}
 
 struct F8Shape { int32_t m_tiles, n_tiles, blocks, total, group_m; };
 
@@ -224,27 +240,42 @@ __device__ __forceinline__ void f8_tile(const F8Shape& g, int t, int& mt, int& n
 // Where 16-byte piece j of row r of a warp's 32 x 128-byte staging sits.
 __device__ __forceinline__ uint32_t f8_piece(int r, int j) { return uint32_t(r * 128 + ((j ^ (r & 7)) << 4)); }
 
-// A warp's 32 rows from m0 of output columns [n0, n1), at tensor-memory address `taddr`: turned through shared memory 128
-// bytes of each row at a time, so that eight lanes store 128 consecutive bytes.
-template <class T>
-__device__ __forceinline__ void f8_store(const F8Out& o, int64_t m0, int n0, int n1, uint32_t taddr, uint32_t sw) {
+// Sums of a thread's accumulator row over the segments of the contraction: acc += columns [0, COLS) at `taddr`.
+template <int COLS>
+__device__ __forceinline__ void f8_add(uint32_t taddr, float (&acc)[COLS]) {
+    constexpr int kChunk = COLS % 16 == 0 ? 16 : 8;
+#pragma unroll
+    for (int c = 0; c < COLS; c += kChunk) {
+        uint32_t v[kChunk];
+        if constexpr (kChunk == 16) f8_tmem_ld16(taddr + c, v);
+        else f8_tmem_ld8(taddr + c, v);
+        umma::tmem_ld_wait();
+#pragma unroll
+        for (int i = 0; i < kChunk; ++i) acc[c + i] += __uint_as_float(v[i]);
+    }
+}
+
+// A warp's 32 rows from m0 of output columns [n0, n1): turned through shared memory 128 bytes of each row at a time, so
+// that eight lanes store 128 consecutive bytes.  fetch(c, f): this lane's columns n0 + c .. n0 + c + 31.
+template <class T, bool UNROLL, int SPAN, class Fetch>
+__device__ __forceinline__ void f8_store(const F8Out& o, int64_t m0, int n0, int n1, uint32_t sw, const Fetch& fetch) {
     constexpr int kCols = 128 / int(sizeof(T)), kPer = 16 / int(sizeof(T));
     const int lane = threadIdx.x & 31;
     bool bad = false;
     if (m0 >= o.M) return;
-#pragma unroll 1
-    for (int n = n0; n < n1; n += kCols) {
+#pragma unroll(UNROLL ? SPAN / kCols : 1)
+    for (int c0 = 0; c0 < SPAN; c0 += kCols) {
+        const int n = n0 + c0;
+        if (n >= n1) break;
         __syncwarp();                        // the last chunk has been read
 #pragma unroll
         for (int part = 0; part < kCols / 32; ++part) {
-            uint32_t v[32];
-            umma::tmem_ld32(taddr + (n - n0) + part * 32, v);
-            umma::tmem_ld_wait();
             float f[32];
+            fetch(c0 + part * 32, f);
 #pragma unroll
             for (int i = 0; i < 32; ++i) {   // what lies beyond the tile is another one's
                 bool off = false;
-                f[i] = f8_finish<T>(__uint_as_float(v[i]), off);
+                f[i] = f8_finish<T>(f[i], off);
                 bad |= off && n + part * 32 + i < n1 && m0 + lane < o.M;
             }
 #pragma unroll
@@ -304,6 +335,7 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
                 const F8Shape g, const F8Out out) {
     extern __shared__ uint8_t smem_raw[];
     const uint32_t raw = ptx::smem_addr(smem_raw), base = (raw + 1023u) & ~1023u;
+    constexpr int kF8BN = f8_bn<T>(), kSegment = f8_segment<T>();
     typedef F8Ring<kF8BN, kF8Stages> Ring;
     static_assert(2 * kF8BN + 2 * Ring::kSet <= 512, "two accumulators and two sets of exponents fit tensor memory");
     const uint32_t staging = base + kF8Stages * Ring::kStage, cells = staging + kF8OutWarps * kF8Staging;
@@ -347,20 +379,50 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
             timed_out = !ring.scales(sa, sb, cells, warp, uint32_t(warp * 32) << 16, mt * kF8TileM, nt * kF8BN, 0, g.blocks);
         }
     } else if (warp < 12) {
+        // two groups of four warps share the columns: 128 and the rest, or halves where the sums are in registers
+        constexpr int kSpan = kSegment < (1 << 30) ? kF8BN / 2 : 128;
         const int q = warp & 3, half = (warp - 4) >> 2;
-        const uint32_t sw = staging + (warp - 4) * kF8Staging;
-        int local = 0;
-        for (int t = blockIdx.x; t < g.total; t += gridDim.x, ++local) {
+        const uint32_t sw = staging + (warp - 4) * kF8Staging, at = tmem + (uint32_t(q * 32) << 16) + half * kSpan;
+        uint32_t n = 0;                      // accumulators so far
+        for (int t = blockIdx.x; t < g.total && !timed_out; t += gridDim.x) {
             int mt, nt;
             f8_tile(g, t, mt, nt);
-            const int acc = local & 1, first = nt * kF8BN, n0 = first + half * 128;
-            const int n1 = min(out.N, half == 0 ? first + 128 : first + kF8BN);
-            if (!ptx::mbar_wait_warp<false>(acc_full + 8 * acc, (local >> 1) & 1)) { timed_out = true; break; }
-            umma::fence_after_thread_sync();
-            f8_store<T>(out, int64_t(mt) * kF8TileM + q * 32, n0, n1, tmem + acc * kF8BN + (uint32_t(q * 32) << 16) + half * 128, sw);
-            umma::fence_before_thread_sync();
-            __syncwarp();
-            if (lane == 0) ptx::mbar_arrive(acc_empty + 8 * acc);
+            const int first = nt * kF8BN, n0 = first + half * kSpan;
+            const int n1 = min(out.N, half == 0 ? first + kSpan : first + kF8BN);
+            const int64_t m0 = int64_t(mt) * kF8TileM + q * 32;
+            auto done = [&] {
+                umma::fence_before_thread_sync();
+                __syncwarp();
+                if (lane == 0) ptx::mbar_arrive(acc_empty + 8 * (n & 1));
+                ++n;
+            };
+            if constexpr (kSegment < (1 << 30)) {
+                float acc[kSpan];
+#pragma unroll
+                for (int i = 0; i < kSpan; ++i) acc[i] = 0.f;
+                for (int kb = 0; kb < g.blocks; kb += kSegment) {
+                    if (!ptx::mbar_wait_warp<false>(acc_full + 8 * (n & 1), (n >> 1) & 1)) { timed_out = true; break; }
+                    umma::fence_after_thread_sync();
+                    f8_add(at + (n & 1) * kF8BN, acc);
+                    done();
+                }
+                if (!timed_out)
+                    f8_store<T, true, kSpan>(out, m0, n0, n1, sw, [&](int c, float (&f)[32]) {
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) f[i] = acc[c + i];
+                    });
+            } else {
+                if (!ptx::mbar_wait_warp<false>(acc_full + 8 * (n & 1), (n >> 1) & 1)) { timed_out = true; break; }
+                umma::fence_after_thread_sync();
+                f8_store<T, false, kSpan>(out, m0, n0, n1, sw, [&](int c, float (&f)[32]) {
+                    uint32_t v[32];
+                    umma::tmem_ld32(at + (n & 1) * kF8BN + c, v);
+                    umma::tmem_ld_wait();
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) f[i] = __uint_as_float(v[i]);
+                });
+                done();
+            }
         }
     } else if (warp == 12) {
         if (lane == 0) {
@@ -372,13 +434,17 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
             if (timed_out) ring.drain();
         }
     } else if (lane == 0) {
-        int local = 0;
-        for (int t = blockIdx.x; t < g.total; t += gridDim.x, ++local) {
-            const int acc = local & 1;
-            if (!ptx::mbar_wait<false>(acc_empty + 8 * acc, ((local >> 1) & 1) ^ 1u)) { timed_out = true; break; }
-            umma::fence_after_thread_sync();
-            if (!ring.multiply(tmem + acc * kF8BN, 0, g.blocks)) { timed_out = true; break; }
-            umma::mma_commit(acc_full + 8 * acc);
+        uint32_t n = 0;
+        for (int t = blockIdx.x; t < g.total && !timed_out; t += gridDim.x) {
+            for (int kb = 0; kb < g.blocks; ++n) {
+                const int next = g.blocks - kb > kSegment ? kb + kSegment : g.blocks;
+                const uint32_t acc = n & 1;
+                if (!ptx::mbar_wait<false>(acc_empty + 8 * acc, ((n >> 1) & 1) ^ 1u)) { timed_out = true; break; }
+                umma::fence_after_thread_sync();
+                if (!ring.multiply(tmem + acc * kF8BN, kb, next)) { timed_out = true; break; }
+                umma::mma_commit(acc_full + 8 * acc);
+                kb = next;
+            }
         }
     }
     if (timed_out && out.status) atomicOr(out.status, TPPO_DEV_WAIT_TIMEOUT);
@@ -395,8 +461,8 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
 // CTAs) accumulator columns: every CTA stores its partial sums into the owner's shared memory, and after one cluster
 // barrier the owner adds them in rank order.  Up to 64 columns the sums have memory of their own and two CTAs share an
 // SM; 128 columns lay them over the operand ring, which needs one more barrier.
-// Warps: 0 TMA loads, 1 tcgen05.mma, 2-5 exponents, 2-9 output.
-constexpr int kF8SplitThreads = 320;
+// Warps: 0 TMA loads, 1 tcgen05.mma, 2-9 output, 10-13 exponents.
+constexpr int kF8SplitThreads = 448;
 template <int BN> __host__ __device__ constexpr bool f8_overlay() { return BN >= 128; }
 template <int BN> __host__ __device__ constexpr int f8_stages() { return BN <= 16 ? 5 : BN <= 32 ? 4 : BN <= 64 ? 3 : 6; }
 template <int BN> __host__ __device__ constexpr uint32_t f8_ring() { return uint32_t(f8_stages<BN>()) * (kF8ABytes + BN * kF8Block); }
@@ -406,18 +472,19 @@ template <int BN> __host__ __device__ constexpr size_t f8_split_smem() { return 
 struct F8SplitShape { int32_t col_tiles, blocks; };
 
 template <class T, int BN>
-__global__ void __launch_bounds__(kF8SplitThreads)
+__global__ void __launch_bounds__(kF8SplitThreads, BN <= 64 ? 2 : 1)
 fp8_split_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const F8Scales sa, const F8Scales sb,
                  const F8SplitShape g, const F8Out out) {
-    constexpr int STAGES = f8_stages<BN>(), kEpiThreads = kF8SplitThreads - 64;
+    constexpr int STAGES = f8_stages<BN>(), kEpiThreads = kF8OutWarps * 32, kHalf = BN / 2;
     typedef F8Ring<BN, STAGES> Ring;
-    constexpr uint32_t kCols = BN + 2 * Ring::kSet <= 32 ? 32 : 2 * BN;       // accumulator and exponents
-    static_assert(BN + 2 * Ring::kSet <= kCols, "");
+    constexpr int kSegment = f8_segment<T>(), kAccs = kSegment < (1 << 30) ? 2 : 1;
+    constexpr uint32_t kUsed = kAccs * BN + 2 * Ring::kSet, kCols = kUsed <= 32 ? 32 : kUsed <= 64 ? 64 : kUsed <= 128 ? 128 : kUsed <= 256 ? 256 : 512;
     extern __shared__ uint8_t smem_raw[];
     // dynamic shared memory starts at the same address in every CTA of a kernel, so `sums` is common to the cluster
     const uint32_t raw = ptx::smem_addr(smem_raw), base = (raw + 1023u) & ~1023u;
     const uint32_t sums = base + (f8_overlay<BN>() ? 0u : f8_ring<BN>()), cells = base + f8_body<BN>();
-    const uint32_t bars = cells + Ring::kCells, full = bars, empty = full + 8 * STAGES, sfull = empty + 8 * STAGES, sempty = sfull + 16, acc_full = sempty + 16, slot = acc_full + 8;
+    const uint32_t bars = cells + Ring::kCells, full = bars, empty = full + 8 * STAGES, sfull = empty + 8 * STAGES, sempty = sfull + 16, acc_full = sempty + 16;
+    const uint32_t acc_empty = acc_full + 16, slot = acc_empty + 16;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int rank = int(ptx::cluster_ctarank());
     int splits;
@@ -434,8 +501,9 @@ fp8_split_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
         for (int a = 0; a < 2; ++a) {
             ptx::mbar_init(sfull + 8 * a, 4);
             ptx::mbar_init(sempty + 8 * a, 1);
+            ptx::mbar_init(acc_full + 8 * a, 1);
+            ptx::mbar_init(acc_empty + 8 * a, 8);
         }
-        ptx::mbar_init(acc_full, 1);
         ptx::fence_mbar_init_cluster();
         umma::prefetch_tensormap(&map_a);
         umma::prefetch_tensormap(&map_b);
@@ -453,8 +521,11 @@ fp8_split_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
     pdl_wait();
 
     bool timed_out = false;
-    Ring ring{base, full, empty, sfull, sempty, tmem + BN};
+    Ring ring{base, full, empty, sfull, sempty, tmem + kAccs * BN};
     const int q = warp & 3, half = (warp - 2) >> 2;
+    float acc[kAccs == 2 ? kHalf : 1];       // sums over the segments of the contraction
+#pragma unroll
+    for (int i = 0; i < (kAccs == 2 ? kHalf : 1); ++i) acc[i] = 0.f;
     if (warp == 0) {
         if (lane == 0) {
             timed_out = !ring.load(&map_a, &map_b, rt * kF8TileM, ct * BN, k0, k1);
@@ -463,40 +534,66 @@ fp8_split_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constan
         __syncwarp();
     } else if (warp == 1) {
         if (lane == 0) {
-            timed_out = !ring.multiply(tmem, k0, k1);
-            if (!timed_out) umma::mma_commit(acc_full);
+            uint32_t n = 0;
+            for (int kb = k0; kb < k1 && !timed_out; ++n) {
+                const int next = k1 - kb > kSegment ? kb + kSegment : k1;
+                timed_out = !ptx::mbar_wait<false>(acc_empty + 8 * (n & 1), ((n >> 1) & 1) ^ 1u);
+                umma::fence_after_thread_sync();
+                if (!timed_out) timed_out = !ring.multiply(tmem + (n & 1) * BN, kb, next);
+                if (!timed_out) umma::mma_commit(acc_full + 8 * (n & 1));
+                kb = next;
+            }
         }
         __syncwarp();
+    } else if (warp < 10) {
+        uint32_t n = 0;
+        if constexpr (kAccs == 2) {
+            for (int kb = k0; kb < k1 && !timed_out; kb += kSegment, ++n) {
+                timed_out = !ptx::mbar_wait_warp<false>(acc_full + 8 * (n & 1), (n >> 1) & 1);
+                if (timed_out) break;
+                umma::fence_after_thread_sync();
+                f8_add(tmem + (uint32_t(q * 32) << 16) + (n & 1) * BN + half * kHalf, acc);
+                umma::fence_before_thread_sync();
+                __syncwarp();
+                if (lane == 0) ptx::mbar_arrive(acc_empty + 8 * (n & 1));
+            }
+        } else {
+            timed_out = !ptx::mbar_wait_warp<false>(acc_full, 0);
+        }
     } else {
-        if (warp < 6) timed_out = !ring.scales(sa, sb, cells, warp - 2, uint32_t(q * 32) << 16, rt * kF8TileM, ct * BN, k0, k1);
-        timed_out = !ptx::mbar_wait_warp<false>(acc_full, 0) || timed_out;
+        timed_out = !ring.scales(sa, sb, cells, warp - 10, uint32_t(q * 32) << 16, rt * kF8TileM, ct * BN, k0, k1);
     }
     if (f8_overlay<BN>()) ptx::cluster_sync_all();       // every ring of the cluster has been consumed
     const int own = (BN + splits - 1) / splits, c0 = rank * own;
-    if (warp >= 2 && !timed_out) {
+    if (warp >= 2 && warp < 10 && !timed_out) {
         const int r = q * 32 + lane;
-        constexpr int kChunk = BN >= 64 ? 32 : 8;
-        umma::fence_after_thread_sync();
-#pragma unroll 1
-        for (int c = half * (BN / 2); c < (half + 1) * (BN / 2); c += kChunk) {
-            uint32_t v[kChunk];
-            if constexpr (kChunk == 32) umma::tmem_ld32(tmem + (uint32_t(q * 32) << 16) + c, v);
-            else f8_tmem_ld8(tmem + (uint32_t(q * 32) << 16) + c, v);
-            umma::tmem_ld_wait();
-            int owner = c / own, in = c - owner * own;
+        int owner = half * kHalf / own, in = half * kHalf - owner * own;
+        auto send = [&](uint32_t v) {        // [source rank][owned column][128 rows] at the owner
+            const uint32_t at = ptx::map_to_cta(sums + ((rank * own + in) * 128 + r) * 4, uint32_t(owner));
+            asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(at), "r"(v) : "memory");
+            if (++in == own) { in = 0; ++owner; }
+        };
+        if constexpr (kAccs == 2) {
 #pragma unroll
-            for (int i = 0; i < kChunk; ++i) {
-                // [source rank][owned column][128 rows] at the owner
-                const uint32_t at = ptx::map_to_cta(sums + ((rank * own + in) * 128 + r) * 4, uint32_t(owner));
-                asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(at), "r"(v[i]) : "memory");
-                if (++in == own) { in = 0; ++owner; }
+            for (int i = 0; i < kHalf; ++i) send(__float_as_uint(acc[i]));
+        } else {
+            constexpr int kChunk = BN >= 64 ? 32 : 8;
+            umma::fence_after_thread_sync();
+#pragma unroll 1
+            for (int c = half * kHalf; c < (half + 1) * kHalf; c += kChunk) {
+                uint32_t v[kChunk];
+                if constexpr (kChunk == 32) umma::tmem_ld32(tmem + (uint32_t(q * 32) << 16) + c, v);
+                else f8_tmem_ld8(tmem + (uint32_t(q * 32) << 16) + c, v);
+                umma::tmem_ld_wait();
+#pragma unroll
+                for (int i = 0; i < kChunk; ++i) send(v[i]);
             }
         }
     }
     umma::fence_before_thread_sync();
     ptx::cluster_sync_all();                 // all partial sums have arrived; nobody writes here any more
     umma::fence_after_thread_sync();
-    if (warp >= 2) {
+    if (warp >= 2 && warp < 10) {
         const int units = max(0, min(own, BN - c0)) * 16;
         bool bad = false;
 #pragma unroll 1
@@ -545,13 +642,13 @@ struct F8Operand { const void* p; int64_t rows, ld; F8Scales s; };
 // 1 x 1024 x 1024 to 2048 x 5120 x 5120, timed with every cut, the choice is the best or within 5 % of it but for 515 x
 // 777 x 1001 (8.7 us; 7.2 with 32 columns and two CTAs).
 struct F8Cut { int bn, splits; };
-F8Cut f8_cut(int64_t m, int64_t n, int64_t blocks, bool whole_rows) {
+F8Cut f8_cut(int64_t m, int64_t n, int64_t blocks, int big_n, bool whole_rows) {
     // CTAs that fit on the GPU at once in clusters of s, at two and at one per SM (the driver's count)
     static const int64_t pair[9] = {0, 296, 296, 279, 284, 280, 270, 259, 264};
     static const int64_t alone[9] = {0, 148, 148, 135, 132, 130, 132, 105, 120};
-    const int64_t rows = (n + 127) / 128, big = (m + 127) / 128 * ((n + kF8BN - 1) / kF8BN);
+    const int64_t rows = (n + 127) / 128, big = (m + 127) / 128 * ((n + big_n - 1) / big_n);
     F8Cut best{0, 1};
-    int64_t least = 5000 + (big + kNumSms - 1) / kNumSms * blocks * 600 + (whole_rows ? 6000 : 18000);
+    int64_t least = 5000 + (big + kNumSms - 1) / kNumSms * blocks * (big_n * 5 / 2) + (whole_rows ? 6000 : 18000);
     for (int bn = 16; bn <= 128; bn *= 2) {
         const int64_t tiles = rows * ((m + bn - 1) / bn);
         const int64_t stages = bn <= 16 ? 5 : bn <= 32 ? 4 : bn <= 64 ? 3 : 6;
@@ -572,19 +669,19 @@ F8Cut f8_cut(int64_t m, int64_t n, int64_t blocks, bool whole_rows) {
 template <class T>
 int f8_gemm(const F8Operand& a, const F8Operand& b, int64_t K, int64_t blocks, const F8Out& out, cudaStream_t s) {
     CUtensorMap ma, mb;
-    if (!make_u8_tensor_map(&ma, a.p, a.rows, K, a.ld, kF8TileM) || !make_u8_tensor_map(&mb, b.p, b.rows, K, b.ld, kF8BN)) return TPPO_ERR_CUDA;
+    if (!make_u8_tensor_map(&ma, a.p, a.rows, K, a.ld, kF8TileM) || !make_u8_tensor_map(&mb, b.p, b.rows, K, b.ld, f8_bn<T>())) return TPPO_ERR_CUDA;
     F8Shape g;
     g.m_tiles = int32_t((a.rows + kF8TileM - 1) / kF8TileM);
-    g.n_tiles = int32_t((b.rows + kF8BN - 1) / kF8BN);
+    g.n_tiles = int32_t((b.rows + f8_bn<T>() - 1) / f8_bn<T>());
     g.blocks = int32_t(blocks);
     g.group_m = 16;
     const int64_t total = int64_t(g.m_tiles) * g.n_tiles;
     if (total > 0x7fffffff - kNumSms) return TPPO_ERR_UNSUPPORTED;
     g.total = int32_t(total);
     auto kernel = fp8_gemm_kernel<T>;
-    TPPO_CUDA_CHECK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, int(kF8Smem)));
+    TPPO_CUDA_CHECK(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, int(f8_smem<T>())));
     const int grid = g.total < kNumSms ? g.total : kNumSms;
-    TPPO_CUDA_CHECK(launch_dense(kernel, dim3(grid), dim3(kF8GemmThreads), kF8Smem, s, ma, mb, a.s, b.s, g, out));
+    TPPO_CUDA_CHECK(launch_dense(kernel, dim3(grid), dim3(kF8GemmThreads), f8_smem<T>(), s, ma, mb, a.s, b.s, g, out));
     return TPPO_OK;
 }
 
@@ -620,7 +717,7 @@ int f8_split(const F8Operand& a, const F8Operand& b, int64_t K, int64_t blocks, 
 template <class T>
 int f8_product(const F8Operand& a, const F8Operand& b, int64_t K, const F8Out& out, cudaStream_t s) {
     const int64_t blocks = (K + kF8Block - 1) / kF8Block;
-    const F8Cut c = f8_cut(a.rows, b.rows, blocks, out.aligned != 0);
+    const F8Cut c = f8_cut(a.rows, b.rows, blocks, f8_bn<T>(), out.aligned != 0);
     switch (c.bn) {                          // the split kernel's rows are the output's columns
         case 16: return f8_split<T, 16>(b, a, K, blocks, c.splits, out, s);
         case 32: return f8_split<T, 32>(b, a, K, blocks, c.splits, out, s);
