@@ -13,10 +13,11 @@
 //
 // The tensor cores drop what lies below the accumulator's last bit at every step of 32: over a contraction of 4096 that
 // is 2e-7 of the result, and it grows with the length.  For bf16 outputs it does not show; for fp32 ones the output
-// warps take the sums over eight blocks at a time and add them up in registers (5e-8, whatever the length), on narrower
-// tiles whose sums the registers hold.
+// warps take the sums over eight blocks at a time and add them up in registers (under 1e-7, whatever the length; sixteen
+// would be 1.2e-7, more than fp32 sums in the usual order have), on narrower tiles whose sums the registers hold (5120 x
+// 5120 of a contraction of 16384: 443 us; with sixteen blocks 414, in one go 374).
 //
-//   fp8_gemm_kernel   many output tiles: persistent CTAs, 128 x 240 tiles (192 for fp32): two accumulators, so that the output of
+//   fp8_gemm_kernel   many output tiles: persistent CTAs, 128 x 240 tiles (208 for fp32): two accumulators, so that the output of
 //                     a tile overlaps the products of the next, and 32 columns of tensor memory for exponents.
 //   fp8_split_kernel  few output tiles (one to some hundred tokens): the output is taken TRANSPOSED, the 128 accumulator
 //                     rows running along n and the BN columns along m, and the contraction is split over the CTAs of
@@ -217,7 +218,7 @@ __device__ __forceinline__ float f8_finish(float v, bool& bad) {
 }
 
 // ---- many tiles -------------------------------------------------------------------------------------------------
-template <class T> __host__ __device__ constexpr int f8_bn() { return sizeof(T) == 4 ? 192 : 240; }
+template <class T> __host__ __device__ constexpr int f8_bn() { return sizeof(T) == 4 ? 208 : 240; }
 template <class T> __host__ __device__ constexpr int f8_segment() { return sizeof(T) == 4 ? 8 : 1 << 30; }       // blocks summed by the tensor cores
 constexpr int kF8Stages = 4;
 constexpr int kF8GemmThreads = 448;                       // warps 0-3 exponents, 4-11 output, 12 TMA loads, 13 tcgen05.mma
@@ -263,7 +264,7 @@ __device__ __forceinline__ void f8_store(const F8Out& o, int64_t m0, int n0, int
     const int lane = threadIdx.x & 31;
     bool bad = false;
     if (m0 >= o.M) return;
-#pragma unroll(UNROLL ? SPAN / kCols : 1)
+#pragma unroll(UNROLL ? (SPAN + kCols - 1) / kCols : 1)
     for (int c0 = 0; c0 < SPAN; c0 += kCols) {
         const int n = n0 + c0;
         if (n >= n1) break;
@@ -409,7 +410,7 @@ fp8_gemm_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant
                 if (!timed_out)
                     f8_store<T, true, kSpan>(out, m0, n0, n1, sw, [&](int c, float (&f)[32]) {
 #pragma unroll
-                        for (int i = 0; i < 32; ++i) f[i] = acc[c + i];
+                        for (int i = 0; i < 32; ++i) f[i] = c + i < kSpan ? acc[c + i < kSpan ? c + i : 0] : 0.f;
                     });
             } else {
                 if (!ptx::mbar_wait_warp<false>(acc_full + 8 * (n & 1), (n >> 1) & 1)) { timed_out = true; break; }
