@@ -114,29 +114,40 @@ template <> struct GradPiece<float> {
         v[4] = b.x * f0 * f1; v[5] = b.y * f0 * f1; v[6] = b.z * f0 * f1; v[7] = b.w * f0 * f1;
     }
 };
-// A chunk scaled by f0 * f1; with f1 = 0 it becomes 0 whatever it holds.  Whole aligned chunks, which nearly all are,
-// have their loads issued together; the rest goes element by element.
+template <class S, class D>
+__device__ __forceinline__ void grad_scale_piece(const GradPiece<S>& w, D* q, bool zero, float f0, float f1) {
+    float v[8];
+    w.scaled(f0, f1, v);
+    if (zero) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = 0.f;
+    }
+    store_vec<8>(q, v);
+}
+// A chunk scaled by f0 * f1; with f1 = 0 it becomes 0 whatever it holds.  Whole chunks, which nearly all of a large list
+// are, have 64 bytes per thread on their way; the others go a piece at a time.
 template <class S, class D>
 __device__ __forceinline__ void grad_scale(const S* p, D* q, int len, bool vec, int tid, float f0, float f1) {
     const bool zero = f1 == 0.f;
     if (vec && len == kGradChunk) {
-        constexpr int kBatch = kGradPieces * 2 / int(sizeof(S));         // 64 bytes in flight per thread
+        constexpr int kBatch = kGradPieces * 2 / int(sizeof(S));
         GradPiece<S> w[kBatch];
 #pragma unroll
         for (int first = 0; first < kGradPieces; first += kBatch) {
 #pragma unroll
             for (int i = 0; i < kBatch; ++i) w[i].load(p + (tid + (first + i) * kGradUnit) * 8);
 #pragma unroll
-            for (int i = 0; i < kBatch; ++i) {
-                float v[8];
-                w[i].scaled(f0, f1, v);
-                if (zero) {
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) v[j] = 0.f;
-                }
-                store_vec<8>(q + (tid + (first + i) * kGradUnit) * 8, v);
-            }
+            for (int i = 0; i < kBatch; ++i) grad_scale_piece(w[i], q + (tid + (first + i) * kGradUnit) * 8, zero, f0, f1);
         }
+    } else if (vec) {
+#pragma unroll 1
+        for (int at = tid * 8; at + 8 <= len; at += kGradUnit * 8) {
+            GradPiece<S> w;
+            w.load(p + at);
+            grad_scale_piece(w, q + at, zero, f0, f1);
+        }
+        const int e = (len & ~7) + tid;                   // what is left of the last piece
+        if (e < len) store_f32(q + e, zero ? 0.f : load_f32(p + e) * f0 * f1);
     } else {
 #pragma unroll 4
         for (int e = tid; e < len; e += kGradUnit) store_f32(q + e, zero ? 0.f : load_f32(p + e) * f0 * f1);
