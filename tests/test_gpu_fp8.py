@@ -276,3 +276,32 @@ def test_refusals_of_the_binding():
         b.tppo_fp8_matmul(a.view(torch.uint8), s, w, sw, SQUARE, y, None)
     with pytest.raises(b.TppoError):
         b.tppo_fp8_quantize(torch.zeros((4, 8), device=DEV), 3, None, None, None, None, None)
+
+
+def test_more_than_two_to_the_31_elements():
+    from paper_2506_15050_b200 import binding as b
+    M, K, N = (1 << 21) + 77, 1040, 24
+    x = torch.zeros((M, K), dtype=BF, device=DEV)
+    x[-300:] = sample(300, K, BF, 4, 0.7)
+    q, s = b.fp8_empty(M, K, DEV), b.fp8_scales(M, K, ROWS, DEV)
+    qt, ts = b.fp8_empty(K, M, DEV), b.fp8_scales(K, M, ROWS, DEV)
+    st = torch.zeros(1, dtype=torch.int32, device=DEV)
+    b.tppo_fp8_quantize(x, ROWS, q, s, qt, ts, st)
+    first = M // 128 * 128 - 128                            # whole blocks of rows from here on
+    want = expected(x[first:], ROWS)
+    assert torch.equal(q[first:].to(F64), want[0]) and torch.equal(s[:, first:].double(), want[1])
+    assert torch.equal(qt[:, first:].to(F64), want[2]) and torch.equal(ts[first // 128:].double(), want[3])
+    w, sw, W = operand(N, K, SQUARE, 6)
+    y = torch.empty((M, N), device=DEV)
+    b.tppo_fp8_matmul(q, s, w, sw, SQUARE, y, st)
+    A = want[0] * spread(want[1].t(), 1, 128, M - first, K)
+    assert bool(((y[first:].double() - A @ W.t()).abs() <= 2 * (K + 2) * U32 * (A.abs() @ W.abs().t())).all())
+    assert not bool(y[:M - 300].any()) and int(st) == 0
+    # contraction over the long side: what is not 0 begins 300 rows from its end, within 256 rows of `first`
+    dw = torch.empty((K, K), device=DEV)
+    b.tppo_fp8_matmul(qt, ts, qt, ts, ROWS, dw, st)
+    T = want[2] * spread(want[3].t(), 1, 128, K, M - first)
+    h0 = expected(x[first - 256:first], ROWS)
+    H = h0[2] * spread(h0[3].t(), 1, 128, K, 256)
+    ref, mag = T @ T.t() + H @ H.t(), T.abs() @ T.abs().t() + H.abs() @ H.abs().t()
+    assert bool(((dw.double() - ref).abs() <= 2 * (600 + 2) * U32 * mag).all())

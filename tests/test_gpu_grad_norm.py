@@ -203,3 +203,16 @@ def test_refusals_of_the_binding():
         b.tppo_grad_clip(t, sq, 1.0, b.tensor_list([]), None, None)
     with pytest.raises(b.TppoError):
         b.tppo_grad_clip(t, sq, -1.0, None, None, None)
+
+
+def test_more_than_two_to_the_31_elements():
+    n = (1 << 31) + 4099
+    t = torch.zeros(n, dtype=BF, device=DEV)
+    t[:1000], t[-5000:] = 3.0, -0.5
+    ref = math.sqrt(9 * 1000 + 0.25 * 5000)
+    sq, norm, coef, st = call([t, torch.ones(7, device=DEV)], 1.0)
+    whole = math.sqrt(ref * ref + 7)
+    assert st == 0 and abs(norm - whole) <= 7 * U * whole
+    assert bool(((t[:1000].double() - 3 / whole).abs() <= (10 * U + half_step(BF)) * 3 / whole).all())
+    assert bool(((t[-5000:].double() + 0.5 / whole).abs() <= (10 * U + half_step(BF)) * 0.5 / whole).all())
+    assert not bool(t[1000:-5000].any())

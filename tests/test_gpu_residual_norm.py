@@ -351,3 +351,29 @@ def test_gradients_against_differences():
         size = (grad.double() * v).abs().sum()
         noise = 16 * U * ((h.double() * wh.double()).abs().sum() + (n.double() * wn.double()).abs().sum()) / step
         assert abs(diff - want) <= 4 * step ** 2 * size + noise, k
+
+
+def test_more_than_two_to_the_31_elements():
+    from paper_2506_15050_b200 import binding as b
+    M, N = (1 << 20) + 3, 2056
+    z, res = (torch.empty((M, N), dtype=BF, device=DEV) for _ in range(2))
+    z.fill_(0.5), res.fill_(-0.25)
+    last = inputs(5, N, BF, "row", 3)
+    z[-5:], res[-5:] = last["z"], last["res"]
+    h, n = torch.empty_like(z), torch.empty_like(z)
+    r1, r2, st = torch.empty(M, device=DEV), torch.empty(M, device=DEV), torch.zeros(1, dtype=torch.int32, device=DEV)
+    b.tppo_residual_norm_fwd(z, res, last["gate"], last["gp"], last["gn"], 0.75, 1e-6, 3, h, n, r1, r2, st)
+    rh, rn, q1, q2, eh, en, e1, e2 = forward64(last["z"], last["res"], last["gate"], last["gp"], last["gn"], 0.75, 1e-6, 3)
+    within(h[-5:], rh, eh + half_step(BF) * rh.abs())
+    within(n[-5:], rn, en + (half_step(BF) + U) * rn.abs())
+    assert torch.equal(h[0], h[M - 6]) and torch.equal(n[0], n[M // 2])
+    dh, dn = torch.zeros_like(z), torch.zeros_like(z)
+    dh[-5:], dn[-5:] = last["dh"], last["dn"]
+    dz, dres = res, torch.empty_like(z)
+    dg, dgp, dgn = (torch.empty_like(last["gp"]) for _ in range(3))
+    b.tppo_residual_norm_bwd(dh, dn, z, h, last["gate"], last["gp"], last["gn"], r1, r2, 0.75, 3, dz, dres, dg, dgp, dgn, st,
+                             b.workspace(b.OP_RESIDUAL_NORM, M, 0, 0, N, DEV))
+    ref = backward64(last["dh"], last["dn"], last["z"], h[-5:], last["gate"], last["gp"], last["gn"], r1[-5:], r2[-5:], 0.75, 3)
+    for got, k in ((dz[-5:], "dz"), (dres[-5:], "dresidual"), (dg, "dgate"), (dgp, "dgamma_post"), (dgn, "dgamma_pre")):
+        within(got, ref[k][0], ref[k][1] + 1e-6 * ref[k][0].abs() + (half_step(BF) + U) * ref[k][0].abs() + 1e-37, k)
+    assert not bool(dz[:-5].any()) and not bool(dres[:-5].any()) and int(st) == 0
