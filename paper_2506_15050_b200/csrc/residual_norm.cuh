@@ -52,6 +52,7 @@ struct JoinArgs {
     int64_t M; int32_t N; float alpha, eps; int32_t norms;
     int32_t T, groups, stages, arrays;                    // threads per group; groups per block; stages; matrices per stage
     int32_t shift_step;                                   // rows start (first row's + r * this) elements into a piece
+    int32_t one_ld;                                       // all matrices have the row stride of the first
 };
 
 template <class T> struct Join { static constexpr int VEC = 16 / sizeof(T); };
@@ -183,25 +184,34 @@ struct JoinThread {
         pre_at = post_at + uint32_t(pieces) * VEC * 4;
         ring = (REGS ? post_at : pre_at + uint32_t(pieces) * VEC * 4) + uint32_t(group * a.stages * a.arrays) * uint32_t(pieces) * 16;
     }
-    __device__ __forceinline__ uint32_t at(const JoinArgs& a, int stage, int m, int c) const {
-        return ring + (uint32_t((stage * a.arrays + a.slot[m]) * CH + c) * uint32_t(a.T) + uint32_t(t)) * 16;
+    // This thread's part of a stage, and its place of piece c of matrix m in it.
+    __device__ __forceinline__ uint32_t stage_at(const JoinArgs& a, int stage) const {
+        return ring + uint32_t(t) * 16 + uint32_t(stage * a.arrays) * uint32_t(CH * a.T * 16);
+    }
+    __device__ __forceinline__ uint32_t at(const JoinArgs& a, uint32_t stage, int m, int c) const {
+        return stage + uint32_t(a.slot[m] * CH + c) * uint32_t(a.T * 16);
     }
     // Starts the copies of row r; always one group of copies, so that waits can count them.
-    __device__ __forceinline__ void fetch(const JoinArgs& a, int64_t r, int stage) const {
+    __device__ __forceinline__ void fetch(const JoinArgs& a, int64_t r, uint32_t stage) const {
         if (r < a.M) {
+            const int64_t common = r * a.ld[0] + k.first;
 #pragma unroll
             for (int m = 0; m < IN; ++m) {
                 if (!a.in[m]) continue;
-                const T* p = static_cast<const T*>(a.in[m]) + r * a.ld[m];
+                const T* p = static_cast<const T*>(a.in[m]) + (a.one_ld ? common : r * a.ld[m] + k.first);
 #pragma unroll
                 for (int c = 0; c < CH; ++c)
-                    if (k.any(c)) copy16(at(a, stage, m, c), p + k.col(c));
+                    if (k.any(c)) copy16(at(a, stage, m, c), p + c * k.step);
             }
         }
         copy_commit();
     }
+    // Row r of an output.
+    __device__ __forceinline__ T* out(const JoinArgs& a, int i, int64_t r) const {
+        return a.out[i] ? static_cast<T*>(a.out[i]) + r * (a.one_ld ? a.ld[0] : a.ldo[i]) : nullptr;
+    }
     // Until the oldest row's copies have landed; what its edge pieces brought from outside the row becomes 0.
-    __device__ __forceinline__ void land(const JoinArgs& a, int stage) const {
+    __device__ __forceinline__ void land(const JoinArgs& a, uint32_t stage) const {
         copy_wait(a.stages);
         if constexpr (SHIFT) {
             if (k.edges == 0) return;

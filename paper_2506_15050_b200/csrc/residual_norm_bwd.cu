@@ -64,7 +64,7 @@ __global__ void __launch_bounds__(join_threads(E), 1) join_bwd_kernel(const __gr
     Thread th(a, smem);
     pdl_launch();
     pdl_wait();
-    for (int s = 0; s < a.stages; ++s) th.fetch(a, th.row + s * th.step, s);
+    for (int s = 0; s < a.stages; ++s) th.fetch(a, th.row + s * th.step, th.stage_at(a, s));
     th.load_params(a, smem);
     __syncthreads();
     using ptx::fma_f32x2;
@@ -75,7 +75,8 @@ __global__ void __launch_bounds__(join_threads(E), 1) join_bwd_kernel(const __gr
     for (int c = 0; c < CH; ++c)
 #pragma unroll
         for (int i = 0; i < P; ++i) sum_post[c][i] = sum_pre[c][i] = 0;
-    int stage = 0;
+    int turn = 0;
+    uint32_t stage = th.stage_at(a, 0);
     float r1_next = post && th.row < a.M ? a.r_post[th.row] : 1.f, r2_next = PRE && th.row < a.M ? a.r_pre[th.row] : 0.f;
     for (int64_t r = th.row; r < a.M; r += th.step) {
         const float r1 = r1_next, r2 = r2_next;
@@ -127,9 +128,7 @@ __global__ void __launch_bounds__(join_threads(E), 1) join_bwd_kernel(const __gr
         }
         th.sum(s);
         const JoinRow w = join_row(a, r1, r2, s, th.t == 0);
-        T* dz = static_cast<T*>(a.out[0]) + (a.out[0] ? r * a.ldo[0] : 0);
-        T* dres = static_cast<T*>(a.out[1]) + (a.out[1] ? r * a.ldo[1] : 0);
-        T* dgate = static_cast<T*>(a.out[2]) + (a.out[2] ? r * a.ldo[2] : 0);
+        T *dz = th.out(a, 0, r), *dres = th.out(a, 1, r), *dgate = th.out(a, 2, r);
         if (w.good) {
             const uint64_t r1_2 = ptx::pack_f32x2(w.r1, w.r1), k1_2 = ptx::pack_f32x2(-w.k1, -w.k1), k2_2 = ptx::pack_f32x2(-w.k2, -w.k2);
             const uint64_t alpha_2 = ptx::pack_f32x2(a.alpha, a.alpha);
@@ -186,7 +185,8 @@ __global__ void __launch_bounds__(join_threads(E), 1) join_bwd_kernel(const __gr
             if (a.out[2]) th.store_zeros(dgate);
         }
         th.fetch(a, r + a.stages * th.step, stage);
-        if (++stage == a.stages) stage = 0;
+        if (++turn == a.stages) turn = 0;
+        stage = th.stage_at(a, turn);
     }
     if (!a.partial) return;
     // the groups' sums meet in the ring's memory: group 0 adds the others' to its own, in order
@@ -482,6 +482,9 @@ TPPO_API int tppo_residual_norm_bwd(const void* dh, int64_t lddh, const void* dn
     a.status = status;
     a.M = M; a.N = N; a.alpha = alpha; a.norms = norms;
     a.shift_step = int32_t(ldz % 16);
+    a.one_ld = 1;
+    for (int i = 0; i < kBwdIn; ++i) a.one_ld &= !a.in[i] || a.ld[i] == ldz;
+    for (int i = 0; i < 3; ++i) a.one_ld &= !a.out[i] || a.ldo[i] == ldz;
     bool same = true;
     for (int i = 0; i < kBwdIn; ++i) same = same && same_start(z, ldz, a.in[i], a.ld[i], e);
     for (int i = 0; i < 3; ++i) same = same && same_start(z, ldz, a.out[i], a.ldo[i], e);

@@ -12,12 +12,13 @@ __global__ void __launch_bounds__(join_threads(E), 1) join_fwd_kernel(const __gr
     Thread th(a, smem);
     pdl_launch();
     pdl_wait();
-    for (int s = 0; s < a.stages; ++s) th.fetch(a, th.row + s * th.step, s);
+    for (int s = 0; s < a.stages; ++s) th.fetch(a, th.row + s * th.step, th.stage_at(a, s));
     th.load_params(a, smem);
     __syncthreads();
     const bool post = a.norms & TPPO_NORM_POST, pre = a.norms & TPPO_NORM_PRE;
     const float inv = 1.f / float(a.N);
-    int stage = 0;
+    int turn = 0;
+    uint32_t stage = th.stage_at(a, 0);
     for (int64_t r = th.row; r < a.M; r += th.step) {
         th.land(a, stage);
         float r1 = 1.f, s[1];
@@ -62,7 +63,8 @@ __global__ void __launch_bounds__(join_threads(E), 1) join_fwd_kernel(const __gr
             }
         }
         th.fetch(a, r + a.stages * th.step, stage);
-        if (++stage == a.stages) stage = 0;
+        if (++turn == a.stages) turn = 0;
+        stage = th.stage_at(a, turn);
         s[0] = q[0] + q[1];
         th.sum(s);
         const float r2 = pre ? rsqrtf(fmaf(s[0], inv, a.eps)) : 1.f;
@@ -72,8 +74,7 @@ __global__ void __launch_bounds__(join_threads(E), 1) join_fwd_kernel(const __gr
             if (a.r_pre) a.r_pre[r] = good ? r2 : 0.f;
             if (!good && a.status) atomicOr(a.status, TPPO_DEV_NONFINITE);
         }
-        T* ho = static_cast<T*>(a.out[0]) + r * a.ldo[0];
-        T* no = static_cast<T*>(a.out[1]) + (pre ? r * a.ldo[1] : 0);
+        T *ho = th.out(a, 0, r), *no = th.out(a, 1, r);
         if (!good) {                                      // the same for the whole group
             th.store_zeros(ho);
             if (pre) th.store_zeros(no);
@@ -208,6 +209,7 @@ TPPO_API int tppo_residual_norm_fwd(const void* z, int64_t ldz, const void* resi
     a.r_post = rstd_post; a.r_pre = rstd_pre; a.status = status;
     a.M = M; a.N = N; a.alpha = alpha; a.eps = eps; a.norms = norms;
     a.shift_step = int32_t(ldz % 16);
+    a.one_ld = ldr == ldz && ldh == ldz && (!pre || ldn == ldz) && (!full || ldg == ldz);
     const bool same = same_start(z, ldz, residual, ldr, e) && same_start(z, ldz, a.in[kGate], ldg, e) && same_start(z, ldz, h, ldh, e) &&
                       same_start(z, ldz, n, ldn, e);
     cudaStream_t s = static_cast<cudaStream_t>(stream);
