@@ -292,7 +292,7 @@ struct JoinThread {
 };
 
 // Elements per thread, with how many threads in a block they go, and where the parameters are.
-__host__ __device__ constexpr int join_threads(int e) { return e == 32 ? 512 : 640; }
+__host__ __device__ constexpr int join_threads(int e) { return e == 32 ? 512 : e == 24 ? 480 : 640; }
 __host__ __device__ constexpr bool join_fwd_regs(int e) { return e <= 32; }
 __host__ __device__ constexpr bool join_bwd_regs(int e) { return e <= 8; }
 
@@ -328,7 +328,7 @@ inline bool join_fit(JoinArgs& a, JoinPlan& p, int e, int vec, int threads, bool
     const int64_t params = (regs ? 0 : T * e * 8) + kJoinRedBytes;
     const int64_t slots = (kJoinSmem - params) / (row * a.arrays);
     if (slots < 1) return false;
-    if (groups > 1 && groups > slots / 2) groups = slots / 2 > 1 ? int(slots / 2) : 1;
+    if (groups > 1 && groups > slots / 2) groups = slots / 2 > 1 ? int(slots / 2) : slots > 1 ? 2 : 1;
     a.T = int(T);
     a.groups = groups;
     a.stages = int(slots / groups < kJoinStages ? slots / groups : kJoinStages);
@@ -347,8 +347,9 @@ inline bool join_fit(JoinArgs& a, JoinPlan& p, int e, int vec, int threads, bool
 // row's warps -- so many per element, some 200 (forward) or 250 per warp for its share of sums, copies and addresses --
 // times (1 / warps on the SM + 1 / 20), the time per instruction that was measured with 5, 10 and 20 of them.  At 5120
 // columns of bf16 that is 40 elements forward (129 us for 16384 rows; 16: 148, 32: 149, 8: 206) and 16 backward (224;
-// 8: 276, 32 with half the threads 241), with a gate per element 16 (160; 40: 206) and 8 (299; 16: 476), of fp32 16
-// forward (8192 rows: 109; 8: 128, 40: 153) and 8 backward (176; 16: 196).  Of equal ones the first.
+// 8: 276, 32 with half the threads 241), with a gate per element 16 (160; 40: 206) and 8 (299; 16 with one group 476), of
+// fp32 16 forward (8192 rows: 109; 8: 128, 40: 153) and 8 backward (176; 16 with one group 196, with two of a single
+// stage 6 % more than 8), and of 5121 bf16 columns 24 backward, two groups of a single stage (325; 16 in one group 406).  Of equal ones the first.
 inline void join_choose(JoinArgs& a, JoinPlan& p, std::initializer_list<int> kinds, int vec, int64_t width, bool bwd) {
     const JoinArgs given = a;
     const JoinPlan start = p;
@@ -361,7 +362,8 @@ inline void join_choose(JoinArgs& a, JoinPlan& p, std::initializer_list<int> kin
             continue;
         const int warps = b.T / 32, per = bwd ? (b.in[kGate] ? 36 : 30) : (b.in[kGate] ? 17 : 14) + (e == 32 ? 3 : 0);
         const int fixed = (bwd ? 250 : 200) - (warps == 1 ? 80 : 0);                // a warp by itself needs no barrier
-        const double cost = warps * double(per * e + fixed) * (1.0 / (warps * b.groups) + 0.05);
+        double cost = warps * double(per * e + fixed) * (1.0 / (warps * b.groups) + 0.05);
+        if (b.stages == 1) cost *= 1.35;                  // nothing on its way while a row is worked on
         if (p.E == 0 || cost < least) {
             least = cost;
             a = b;

@@ -253,7 +253,7 @@ __device__ __forceinline__ void join_read_params(const void* p, int c, bool f32,
     }
 }
 template <class T, int VEC>
-__global__ void __launch_bounds__(kJoinAnyThreads) join_row_sums_kernel(const __grid_constant__ JoinArgs a) {
+__global__ void __launch_bounds__(kJoinAnyThreads, 2) join_row_sums_kernel(const __grid_constant__ JoinArgs a) {
     __shared__ float red[3 * 32];
     pdl_launch();
     pdl_wait();
@@ -298,7 +298,7 @@ __global__ void __launch_bounds__(kJoinAnyThreads) join_row_sums_kernel(const __
 
 constexpr int kJoinStrip = 128;                           // threads of a strip
 template <class T, int VEC>
-__global__ void __launch_bounds__(kJoinStrip) join_columns_kernel(const __grid_constant__ JoinArgs a) {
+__global__ void __launch_bounds__(kJoinStrip, 5) join_columns_kernel(const __grid_constant__ JoinArgs a) {
     pdl_launch();
     pdl_wait();
     const bool pre = a.norms & TPPO_NORM_PRE;
@@ -419,11 +419,12 @@ int run_bwd(JoinArgs& a, bool same, JoinSumArgs& sum, cudaStream_t s) {
     const int64_t width = join_width(a, p, vec);
     const bool whole = same && !p.shift;                  // every row is a number of 16-byte pieces
     if (same) {
-        join_choose(a, p, {8, 16}, vec, width, true);
+        join_choose(a, p, {8, 16, 24}, vec, width, true);
     }
     sum.rows = p.grid;
     const bool pre = a.norms & TPPO_NORM_PRE;
     if (p.E == 8) return pre ? launch_bwd<T, 8, true>(a, p, s) : launch_bwd<T, 8, false>(a, p, s);
+    if (p.E == 24) return pre ? launch_bwd<T, 24, true>(a, p, s) : launch_bwd<T, 24, false>(a, p, s);
     if (p.E == 16) return pre ? launch_bwd<T, 16, true>(a, p, s) : launch_bwd<T, 16, false>(a, p, s);
     return whole ? run_bwd_any<T, vec>(a, sum, s) : run_bwd_any<T, 1>(a, sum, s);
 }
