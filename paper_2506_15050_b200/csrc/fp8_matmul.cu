@@ -18,7 +18,7 @@
 // 5120 of a contraction of 16384: 443 us; with sixteen blocks 414, in one go 374).
 //
 //   fp8_gemm_kernel   many output tiles: persistent CTAs, 128 x 240 tiles (208 for fp32): two accumulators, so that the output of
-//                     a tile overlaps the products of the next, and 32 columns of tensor memory for exponents.
+//                     a tile overlaps the products of the next, and two sets of exponents.
 //   fp8_split_kernel  few output tiles (one to some hundred tokens): the output is taken TRANSPOSED, the 128 accumulator
 //                     rows running along n and the BN columns along m, and the contraction is split over the CTAs of
 //                     a cluster, whose partial sums meet in distributed shared memory in a fixed order.
@@ -69,6 +69,18 @@ __device__ __forceinline__ void f8_tmem_st4(uint32_t taddr, const uint32_t* v) {
 }
 __device__ __forceinline__ void f8_tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
+// A barrier of four warps that tells each whether all of them came with `ok`.
+__device__ __forceinline__ bool f8_meet(bool ok) {
+    uint32_t all;
+    asm volatile(
+        "{\n\t.reg .pred p, q;\n\t"
+        "setp.ne.u32 p, %1, 0;\n\t"
+        "barrier.cta.red.and.pred q, 1, 128, p;\n\t"
+        "selp.u32 %0, 1, 0, q;\n\t}"
+        : "=r"(all) : "r"(ok ? 1u : 0u) : "memory");
+    return all != 0;
+}
+
 // The scales of an operand: of (row, block) at p[block * by_block + (row >> shift) * by_row].
 struct F8Scales {
     const float* p;
@@ -118,7 +130,8 @@ struct F8Ring {
     // The exponents of blocks [k0, k1), by four warps.  Each reads the scales of a quarter of the columns, three groups
     // ahead -- under the operands' traffic a load takes some 2000 clocks -- and makes their cells; through shared
     // memory (`cells`: two sets of [kSet][32] words) every warp gets all of them and writes them to the quarter of the lanes
-    // that it can reach.  `w`: the warp's number among the four, `quarter`: the address of its lanes.
+    // that it can reach.  `w`: the warp's number among the four, `quarter`: the address of its lanes.  A warp whose wait ran
+    // out still comes to the next meeting, from which all four leave.
     __device__ __forceinline__ bool scales(const F8Scales& a, const F8Scales& b, uint32_t cells, int w, uint32_t quarter, int am, int bn,
                                            int k0, int k1) {
         constexpr int kMine = kSet / 4, kAhead = 3;
@@ -149,6 +162,7 @@ struct F8Ring {
         };
 #pragma unroll
         for (int i = 0; i < kAhead; ++i) read(v[i]);
+        bool ok = true;
         for (int kb = k0; kb < k1; kb += kF8Group) {
             const uint32_t mine = cells + (set * kSet + w * kMine) * 128 + lane * 4;
 #pragma unroll
@@ -157,12 +171,13 @@ struct F8Ring {
                                       f8_exponent(v[0][i][3]) << 24;
                 asm volatile("st.shared.u32 [%0], %1;" ::"r"(mine + i * 128), "r"(cell) : "memory");
             }
-            asm volatile("bar.sync 1, 128;" ::: "memory");
+            if (!f8_meet(ok)) return false;
             uint32_t all[kSet];
 #pragma unroll
             for (int c = 0; c < kSet; ++c)
                 asm volatile("ld.shared.u32 %0, [%1];" : "=r"(all[c]) : "r"(cells + (set * kSet + c) * 128 + lane * 4));
-            if (!ptx::mbar_wait_warp<false>(sempty + 8 * set, sphase ^ 1u)) return false;
+            ok = ptx::mbar_wait_warp<false>(sempty + 8 * set, sphase ^ 1u);
+            if (!ok) continue;
             umma::fence_after_thread_sync();
 #pragma unroll
             for (int c = 0; c < kSet; c += 4) f8_tmem_st4(sf + quarter + set * kSet + c, all + c);
@@ -179,7 +194,7 @@ struct F8Ring {
                     for (int l = 0; l < kF8Group; ++l) v[i][j][l] = v[i + 1][j][l];
             read(v[kAhead - 1]);
         }
-        return true;
+        return f8_meet(ok);
     }
     // The products of blocks [k0, k1) into accumulator d.
     __device__ __forceinline__ bool multiply(uint32_t d, int k0, int k1) {
