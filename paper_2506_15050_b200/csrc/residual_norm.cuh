@@ -357,13 +357,12 @@ inline void join_choose(JoinArgs& a, JoinPlan& p, std::initializer_list<int> kin
     for (const int e : kinds) {
         JoinArgs b = given;
         JoinPlan q = start;
-        if (!join_fit(b, q, e, vec, join_threads(e), bwd ? join_bwd_regs(e) : join_fwd_regs(e), width, bwd) ||
-            b.groups * b.stages < 2)
+        if (!join_fit(b, q, e, vec, join_threads(e), bwd ? join_bwd_regs(e) : join_fwd_regs(e), width, bwd))
             continue;
         const int warps = b.T / 32, per = bwd ? (b.in[kGate] ? 36 : 30) : (b.in[kGate] ? 17 : 14) + (e == 32 ? 3 : 0);
         const int fixed = (bwd ? 250 : 200) - (warps == 1 ? 80 : 0);                // a warp by itself needs no barrier
         double cost = warps * double(per * e + fixed) * (1.0 / (warps * b.groups) + 0.05);
-        if (b.stages == 1) cost *= 1.35;                  // nothing on its way while a row is worked on
+        if (b.stages == 1) cost *= b.groups == 1 ? 2.5 : 1.35;        // nothing on its way while a row is worked on
         if (p.E == 0 || cost < least) {
             least = cost;
             a = b;
