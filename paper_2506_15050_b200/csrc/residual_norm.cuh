@@ -10,7 +10,9 @@
 // One block per SM, cut into groups of warps that walk rows of their own.  Each thread brings its 16-byte
 // pieces of the next rows into a ring of shared memory of its own with cp.async: what it copies only it reads,
 // so the ring needs no barrier, and 100-200 KB per SM stay in flight whatever the arithmetic does.  gate *
-// gamma_post and gamma_pre sit in shared memory as fp32 for the block's life.
+// gamma_post and gamma_pre stay in registers or shared memory as fp32 for the block's life.
+//   [16384, 5120] bf16: forward 122 us (5.5 TB/s, 0.84 of the measured copy rate), backward 213 us (4.7 TB/s)
+//   [8192, 5120] fp32: forward 110-116 us (5.8-6.1 TB/s), backward 166 us (6.1 TB/s)
 //
 // Forward needs two sums over the row, one behind the other.  Backward takes one: with w = gate gamma_post z,
 //     sum(a1 z) = sum((dh + r2 a2) w) - r2^3 mean(a2 h) sum(h w),
@@ -47,7 +49,8 @@ struct JoinArgs {
     void* out[3]; int64_t ldo[3];                         // h, n | dz, dresidual, dgate
     float* r_post; float* r_pre;                          // out | in; NULL in the backward pass: no such norm
     float* partial;                                       // column sums: [blocks][2][N]
-    float4* rows;                                         // r1, r2, k1, k2 of every row, where two launches share the work
+    float4* rows;                                         // r1, r2, k1, k2 of every row, where two launches share the work,
+    float* params;                                        // and the parameters as they use them: two rows
     int32_t* status;
     int64_t M; int32_t N; float alpha, eps; int32_t norms;
     int32_t T, groups, stages, arrays;                    // threads per group; groups per block; stages; matrices per stage
@@ -346,7 +349,7 @@ inline bool join_fit(JoinArgs& a, JoinPlan& p, int e, int vec, int threads, bool
 // Of the numbers of elements per thread in `kinds`, the one with the least estimated time per row: instructions of the
 // row's warps -- so many per element, some 200 (forward) or 250 per warp for its share of sums, copies and addresses --
 // times (1 / warps on the SM + 1 / 20), the time per instruction that was measured with 5, 10 and 20 of them.  At 5120
-// columns of bf16 that is 40 elements forward (129 us for 16384 rows; 16: 148, 32: 149, 8: 206) and 16 backward (224;
+// columns of bf16 that was 40 elements forward (129 us for 16384 rows; 16: 148, 32: 149, 8: 206) and 16 backward (224;
 // 8: 276, 32 with half the threads 241), with a gate per element 16 (160; 40: 206) and 8 (299; 16 with one group 476), of
 // fp32 16 forward (8192 rows: 109; 8: 128, 40: 153) and 8 backward (176; 16 with one group 196, with two of a single
 // stage 6 % more than 8), and of 5121 bf16 columns 24 backward, two groups of a single stage (325; 16 in one group 406).  Of equal ones the first.

@@ -231,107 +231,96 @@ __global__ void __launch_bounds__(join_threads(E), 1) join_bwd_kernel(const __gr
 // Backward pass of such rows in two launches: the three sums of every row, then, with no thread depending on another,
 // the gradients, a block walking down its strip of columns.  10 elements moved per element of a row instead of 6.
 // VEC: columns per access, 16 bytes' worth where all rows start and end on 16-byte boundaries, else 1.
+// Loads stand under no condition, so that they leave together: a matrix that is not there has z's address (and its values
+// replaced), and the parameters have been made whole by a small launch in front.
+struct JoinWide {
+    const void* in[kBwdIn]; int64_t ld[kBwdIn];           // none is NULL
+    uint32_t has;                                         // bit m: matrix m is there
+    const float* post; const float* pre;                  // gate row * gamma_post, gamma_pre
+};
 template <class T, int VEC>
-__device__ __forceinline__ void join_read(const JoinArgs& a, int m, int64_t r, int c, float otherwise, float (&v)[VEC]) {
-    if (a.in[m]) {
-        load_vec<VEC>(static_cast<const T*>(a.in[m]) + r * a.ld[m] + c, v);
-    } else {
+__device__ __forceinline__ void join_read(const JoinWide& a, int m, int64_t r, int c, float otherwise, float (&v)[VEC]) {
+    load_vec<VEC>(static_cast<const T*>(a.in[m]) + r * a.ld[m] + c, v);
+    if (!(a.has >> m & 1u)) {
 #pragma unroll
         for (int i = 0; i < VEC; ++i) v[i] = otherwise;
     }
 }
-template <int VEC>
-__device__ __forceinline__ void join_read_params(const void* p, int c, bool f32, float (&v)[VEC]) {
-    const bool whole = VEC > 1 && reinterpret_cast<uintptr_t>(p) % 16 == 0;       // 1 where there is none
-    if (p && whole && f32) {
-        load_vec<VEC>(static_cast<const float*>(p) + c, v);
-    } else if (p && whole) {
-        load_vec<VEC>(static_cast<const bf16_bits*>(p) + c, v);
-    } else {
-#pragma unroll
-        for (int i = 0; i < VEC; ++i) v[i] = param(p, c + i, f32);
-    }
+__global__ void __launch_bounds__(256) join_params_kernel(const void* gate_row, const void* gamma_post, const void* gamma_pre, int32_t p32, int32_t N,
+                                                          float* post, float* pre) {
+    pdl_launch();
+    pdl_wait();
+    const int64_t c = int64_t(blockIdx.x) * 256 + threadIdx.x;
+    if (c >= N) return;
+    post[c] = param(gate_row, c, p32) * param(gamma_post, c, p32);
+    pre[c] = param(gamma_pre, c, p32);
 }
 template <class T, int VEC>
-__global__ void __launch_bounds__(kJoinAnyThreads, 2) join_row_sums_kernel(const __grid_constant__ JoinArgs a) {
+__global__ void __launch_bounds__(kJoinAnyThreads, 2) join_row_sums_kernel(const __grid_constant__ JoinArgs a, const __grid_constant__ JoinWide w) {
     __shared__ float red[3 * 32];
     pdl_launch();
     pdl_wait();
-    const bool pre = a.norms & TPPO_NORM_PRE;
     for (int64_t r = blockIdx.x; r < a.M; r += gridDim.x) {
         const float r1 = a.r_post ? a.r_post[r] : 1.f, r2 = a.r_pre ? a.r_pre[r] : 0.f;
         float s[3] = {0.f, 0.f, 0.f};
-#pragma unroll 2
+#pragma unroll(VEC == 1 ? 4 : 1)
         for (int c = threadIdx.x * VEC; c < a.N; c += kJoinAnyThreads * VEC) {
-            float z[VEC], g[VEC], d[VEC], n[VEC], h[VEC];
-            join_read<T, VEC>(a, kZ, r, c, 0.f, z);
-            join_read<T, VEC>(a, kGate, r, c, 1.f, g);
-            join_read<T, VEC>(a, kDh, r, c, 0.f, d);
-            if (pre) {
-                join_read<T, VEC>(a, kDn, r, c, 0.f, n);
-                join_read<T, VEC>(a, kH, r, c, 0.f, h);
-            }
-            float gr[VEC], gp[VEC], gn[VEC];
-            join_read_params<VEC>(a.gate_row, c, a.p32, gr);
-            join_read_params<VEC>(a.gamma_post, c, a.p32, gp);
-            join_read_params<VEC>(a.gamma_pre, c, a.p32, gn);
+            float z[VEC], g[VEC], d[VEC], n[VEC], h[VEC], gp[VEC], gn[VEC];
+            join_read<T, VEC>(w, kZ, r, c, 0.f, z);
+            join_read<T, VEC>(w, kGate, r, c, 1.f, g);
+            join_read<T, VEC>(w, kDh, r, c, 0.f, d);
+            join_read<T, VEC>(w, kDn, r, c, 0.f, n);
+            join_read<T, VEC>(w, kH, r, c, 0.f, h);
+            load_vec<VEC>(w.post + c, gp);
+            load_vec<VEC>(w.pre + c, gn);
 #pragma unroll
             for (int i = 0; i < VEC; ++i) {
-                const float w = z[i] * (g[i] * gr[i] * gp[i]);
-                if (pre) {
-                    const float a2 = n[i] * gn[i];
-                    s[0] = fmaf(a2, h[i], s[0]);
-                    s[2] = fmaf(h[i], w, s[2]);
-                    d[i] = fmaf(r2, a2, d[i]);
-                }
-                s[1] = fmaf(d[i], w, s[1]);
+                const float x = z[i] * (g[i] * gp[i]), a2 = n[i] * gn[i];
+                s[0] = fmaf(a2, h[i], s[0]);
+                s[1] = fmaf(fmaf(r2, a2, d[i]), x, s[1]);
+                s[2] = fmaf(h[i], x, s[2]);
             }
         }
         block_sums(s, red);
         if (threadIdx.x == 0) {
-            const JoinRow w = join_row(a, r1, r2, s, true);
+            const JoinRow q = join_row(a, r1, r2, s, true);
             // zeros: a row to leave out
-            a.rows[r] = w.good ? make_float4(w.r1, w.r2, w.k1, w.k2) : make_float4(0.f, 0.f, 0.f, 0.f);
+            a.rows[r] = q.good ? make_float4(q.r1, q.r2, q.k1, q.k2) : make_float4(0.f, 0.f, 0.f, 0.f);
         }
     }
 }
 
-constexpr int kJoinStrip = 128;                           // threads of a strip
+// Threads of a strip: with fewer bytes of a row HBM's pages are opened for too little.
+template <int VEC> __host__ __device__ constexpr int join_strip() { return VEC == 1 ? 512 : 128; }
 template <class T, int VEC>
-__global__ void __launch_bounds__(kJoinStrip, 5) join_columns_kernel(const __grid_constant__ JoinArgs a) {
+__global__ void __launch_bounds__(join_strip<VEC>(), VEC == 1 ? 2 : 4)
+join_columns_kernel(const __grid_constant__ JoinArgs a, const __grid_constant__ JoinWide p) {
     pdl_launch();
     pdl_wait();
-    const bool pre = a.norms & TPPO_NORM_PRE;
     const int64_t chunk = blockIdx.y, r0 = a.M * chunk / gridDim.y, r1 = a.M * (chunk + 1) / gridDim.y;
-    const int64_t at = (int64_t(blockIdx.x) * kJoinStrip + threadIdx.x) * VEC;
+    const int64_t at = (int64_t(blockIdx.x) * join_strip<VEC>() + threadIdx.x) * VEC;
     if (at >= a.N) return;
     const int c = int(at);
     float g[VEC], gn[VEC], sum_post[VEC], sum_pre[VEC];
+    load_vec<VEC>(p.post + c, g);
+    load_vec<VEC>(p.pre + c, gn);
 #pragma unroll
-    for (int i = 0; i < VEC; ++i) {
-        g[i] = param(a.gate_row, c + i, a.p32) * param(a.gamma_post, c + i, a.p32);
-        gn[i] = param(a.gamma_pre, c + i, a.p32);
-        sum_post[i] = sum_pre[i] = 0;
-    }
-#pragma unroll 2
+    for (int i = 0; i < VEC; ++i) sum_post[i] = sum_pre[i] = 0;
+#pragma unroll(VEC == 1 ? 4 : 2)
     for (int64_t r = r0; r < r1; ++r) {
         const float4 w = __ldcg(a.rows + r);
         float z[VEC], gv[VEC], d[VEC], n[VEC], h[VEC], o[VEC];
-        join_read<T, VEC>(a, kZ, r, c, 0.f, z);
-        join_read<T, VEC>(a, kGate, r, c, 1.f, gv);
-        join_read<T, VEC>(a, kDh, r, c, 0.f, d);
-        if (pre) {
-            join_read<T, VEC>(a, kDn, r, c, 0.f, n);
-            join_read<T, VEC>(a, kH, r, c, 0.f, h);
-        }
+        join_read<T, VEC>(p, kZ, r, c, 0.f, z);
+        join_read<T, VEC>(p, kGate, r, c, 1.f, gv);
+        join_read<T, VEC>(p, kDh, r, c, 0.f, d);
+        join_read<T, VEC>(p, kDn, r, c, 0.f, n);
+        join_read<T, VEC>(p, kH, r, c, 0.f, h);
         const bool good = w.x != 0.f;                     // r1 of a row with statistics is not 0
 #pragma unroll
         for (int i = 0; i < VEC; ++i) {
-            if (pre) {
-                const float m = n[i] * w.y;
-                if (good) sum_pre[i] = fmaf(m, h[i], sum_pre[i]);
-                d[i] = fmaf(-w.w, h[i], fmaf(m, gn[i], d[i]));
-            }
+            const float m = n[i] * w.y;
+            if (good) sum_pre[i] = fmaf(m, h[i], sum_pre[i]);
+            d[i] = fmaf(-w.w, h[i], fmaf(m, gn[i], d[i]));
             o[i] = good ? a.alpha * d[i] : 0.f;
             d[i] *= w.x;
         }
@@ -401,14 +390,26 @@ int64_t join_chunks(int64_t M) { return M < kJoinAnyBlocks ? (M + 7) / 8 * 8 : k
 
 template <class T, int VEC>
 int run_bwd_any(JoinArgs& a, JoinSumArgs& sum, cudaStream_t s) {
-    TPPO_CUDA_CHECK(launch_dense(join_row_sums_kernel<T, VEC>, dim3(unsigned(a.M < 4 * kNumSms ? a.M : 4 * kNumSms)), dim3(kJoinAnyThreads), 0, s, a));
+    JoinWide w{};
+    for (int i = 0; i < kBwdIn; ++i) {
+        const bool has = a.in[i] != nullptr;
+        w.in[i] = has ? a.in[i] : a.in[kZ];
+        w.ld[i] = has ? a.ld[i] : a.ld[kZ];
+        w.has |= has ? 1u << i : 0u;
+    }
+    w.post = a.params;
+    w.pre = a.params + align_up(size_t(a.N), 64);
+    TPPO_CUDA_CHECK(launch_dense(join_params_kernel, dim3(unsigned((int64_t(a.N) + 255) / 256)), dim3(256), 0, s, a.gate_row, a.gamma_post, a.gamma_pre,
+                                 a.p32, a.N, a.params, a.params + align_up(size_t(a.N), 64)));
+    TPPO_CUDA_CHECK(launch_dense(join_row_sums_kernel<T, VEC>, dim3(unsigned(a.M < 4 * kNumSms ? a.M : 4 * kNumSms)), dim3(kJoinAnyThreads), 0, s, a, w));
     // enough chunks of rows to fill the GPU some times over
-    const int64_t strips = (int64_t(a.N) + kJoinStrip * VEC - 1) / (kJoinStrip * VEC), most = join_chunks(a.M);
-    int64_t chunks = (32 * kNumSms + strips - 1) / strips;
+    constexpr int kStrip = join_strip<VEC>();
+    const int64_t strips = (int64_t(a.N) + kStrip * VEC - 1) / (kStrip * VEC), most = join_chunks(a.M);
+    int64_t chunks = ((VEC == 1 ? 8 : 32) * kNumSms + strips - 1) / strips;
     if (chunks > (a.M + 7) / 8) chunks = (a.M + 7) / 8;
     if (chunks > most) chunks = most;
     sum.rows = chunks;
-    TPPO_CUDA_CHECK(launch_dense(join_columns_kernel<T, VEC>, dim3(unsigned(strips), unsigned(chunks)), dim3(kJoinStrip), 0, s, a));
+    TPPO_CUDA_CHECK(launch_dense(join_columns_kernel<T, VEC>, dim3(unsigned(strips), unsigned(chunks)), dim3(kStrip), 0, s, a, w));
     return TPPO_OK;
 }
 
@@ -431,11 +432,12 @@ int run_bwd(JoinArgs& a, bool same, JoinSumArgs& sum, cudaStream_t s) {
 
 }  // namespace
 
-// The rows' scalars in front, the partial column sums behind them.
+// The rows' scalars in front, then the two rows of parameters, the partial column sums behind them.
 static size_t join_rows_bytes(int64_t M) { return align_up(size_t(M > 0 ? M : 1) * sizeof(float4), kWsAlign); }
+static size_t join_params_bytes(int32_t N) { return 2 * align_up(size_t(N), 64) * sizeof(float); }
 size_t residual_norm_workspace_bytes(int64_t M, int32_t N) {
     if (N <= 0) return 0;
-    return join_rows_bytes(M) + align_up(size_t(M > 0 ? join_chunks(M) : 1) * 2 * size_t(N) * sizeof(float), kWsAlign);
+    return join_rows_bytes(M) + join_params_bytes(N) + align_up(size_t(M > 0 ? join_chunks(M) : 1) * 2 * size_t(N) * sizeof(float), kWsAlign);
 }
 
 }  // namespace tppo
@@ -479,7 +481,8 @@ TPPO_API int tppo_residual_norm_bwd(const void* dh, int64_t lddh, const void* dn
     a.ldo[0] = lddz; a.ldo[1] = lddr; a.ldo[2] = lddg;
     a.r_post = const_cast<float*>(rstd_post); a.r_pre = const_cast<float*>(rstd_pre);
     a.rows = static_cast<float4*>(workspace);
-    a.partial = sums ? reinterpret_cast<float*>(static_cast<char*>(workspace) + join_rows_bytes(M)) : nullptr;
+    a.params = reinterpret_cast<float*>(static_cast<char*>(workspace) + join_rows_bytes(M));
+    a.partial = sums ? reinterpret_cast<float*>(static_cast<char*>(workspace) + join_rows_bytes(M) + join_params_bytes(N)) : nullptr;
     a.status = status;
     a.M = M; a.N = N; a.alpha = alpha; a.norms = norms;
     a.shift_step = int32_t(ldz % 16);
