@@ -182,6 +182,7 @@ template <int CAP, bool CLUSTER>
 __global__ void __launch_bounds__(CLUSTER ? kGradClusterThreads : kGradUnit, CLUSTER ? 1 : 4)
 grad_norm_kernel(const __grid_constant__ GradList<CAP> l, double* partial, double* sum_sq, float* norm, int32_t* status) {
     __shared__ double red[32], parts[kGradCluster];
+    if constexpr (CLUSTER) ptx::cluster_arrive();         // the wait is in front of the first store into another block
     pdl_launch();
     pdl_wait();
     const int per = int(blockDim.x) / kGradUnit, unit = int(blockIdx.x) * per + int(threadIdx.x) / kGradUnit;
@@ -215,6 +216,8 @@ grad_norm_kernel(const __grid_constant__ GradList<CAP> l, double* partial, doubl
     }
     sum = block_sum(sum, red);
     if constexpr (CLUSTER) {
+        __syncwarp();
+        ptx::cluster_wait();                              // every block of the cluster runs: its shared memory may be written
         if (threadIdx.x == 0) {
             const uint32_t at = ptx::map_to_cta(ptx::smem_addr(parts + ptx::cluster_ctarank()), 0);
             asm volatile("st.shared::cluster.f64 [%0], %1;" ::"r"(at), "d"(sum) : "memory");

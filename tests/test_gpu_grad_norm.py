@@ -216,3 +216,35 @@ def test_more_than_two_to_the_31_elements():
     assert bool(((t[:1000].double() - 3 / whole).abs() <= (10 * U + half_step(BF)) * 3 / whole).all())
     assert bool(((t[-5000:].double() + 0.5 / whole).abs() <= (10 * U + half_step(BF)) * 0.5 / whole).all())
     assert not bool(t[1000:-5000].any())
+
+
+@pytest.mark.parametrize("sizes", [[], [0], [1], [5, 0, 3], [8192 * 3 + 1], [300] * 64, [3000] * 40, [8192 * 127, 9]])
+def test_short_lists_over_and_over(sizes):
+    """Lists that one cluster takes, most of its blocks with nothing to read: the same bits every time, alone, replayed back to
+    back, and beside the same on a second stream."""
+    from paper_2506_15050_b200 import binding as b
+    _, ts = tensors(sizes, [(BF, F32)[i % 2] for i in range(len(sizes))], 11)
+    grads, ref = b.tensor_list(ts), norm64(ts)
+    def buffers():
+        return torch.zeros(1, dtype=torch.float64, device=DEV), torch.zeros(1, device=DEV), b.workspace(b.OP_GRAD_NORM, len(ts), 0, 0, 0, DEV)
+    (sq, norm, ws), (sq2, norm2, ws2) = buffers(), buffers()
+    b.tppo_grad_norm(grads, sq, norm, None, ws)
+    first = float(sq), float(norm)
+    assert abs(first[0] - ref * ref) <= 11 * U * ref * ref and abs(first[1] - ref) <= 7 * U * ref
+    graph, side = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    seen = torch.zeros(200, 2, dtype=torch.float64, device=DEV)
+    with torch.cuda.graph(graph):
+        for i in range(100):
+            b.tppo_grad_norm(grads, sq, norm, None, ws)
+            seen[i, 0] = sq[0]
+            sq.zero_()
+    side.wait_stream(torch.cuda.current_stream())
+    graph.replay()
+    with torch.cuda.stream(side):
+        for i in range(100):
+            b.tppo_grad_norm(grads, sq2, norm2, None, ws2)
+            seen[100 + i, 0] = sq2[0]
+            sq2.zero_()
+    torch.cuda.synchronize()
+    assert bool((seen[:, 0] == first[0]).all()) and float(norm) == float(norm2) == first[1]
