@@ -216,7 +216,6 @@ grad_norm_kernel(const __grid_constant__ GradList<CAP> l, double* partial, doubl
     }
     sum = block_sum(sum, red);
     if constexpr (CLUSTER) {
-        __syncwarp();
         ptx::cluster_wait();                              // every block of the cluster runs: its shared memory may be written
         if (threadIdx.x == 0) {
             const uint32_t at = ptx::map_to_cta(ptx::smem_addr(parts + ptx::cluster_ctarank()), 0);

@@ -116,12 +116,21 @@ __device__ __forceinline__ uint32_t num_clusters_x() {
     asm volatile("mov.u32 %0, %nclusterid.x;" : "=r"(r));
     return r;
 }
+// Barriers of the whole cluster.  The aligned forms want all lanes of a warp at the same instruction; lanes that come out of a
+// branch of their own (one thread that set up barriers, or stored a result) meet first.
 __device__ __forceinline__ void cluster_sync_all() {
+    __syncwarp();
     asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 // Its two halves: what stands between them runs while the other CTAs arrive.
-__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory"); }
-__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+__device__ __forceinline__ void cluster_arrive() {
+    __syncwarp();
+    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void cluster_wait() {
+    __syncwarp();
+    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
 // shared::cluster address of `local_smem_addr` in the CTA with rank `cta`
 __device__ __forceinline__ uint32_t map_to_cta(uint32_t local_smem_addr, uint32_t cta) {
     uint32_t r;

@@ -28,3 +28,15 @@ def test_kernels_are_found():
 def test_a_barrier_stands_before_the_first_remote_address(file, text):
     first = BARRIER.search(text)
     assert first and first.start() < text.index("map_to_cta("), file
+
+
+def test_a_warp_meets_in_front_of_each_aligned_barrier():
+    """The warp-aligned barriers follow code that a single thread ran (it set up mbarriers, or stored a sum)."""
+    found = 0
+    for path in sorted(glob.glob(os.path.join(CSRC, "*.cu*"))):
+        with open(path) as f:
+            text = f.read()
+        for m in re.finditer(r'asm volatile\("barrier\.cluster\.', text):
+            found += 1
+            assert text[:m.start()].rstrip().endswith("__syncwarp();"), os.path.basename(path)
+    assert found >= 1
