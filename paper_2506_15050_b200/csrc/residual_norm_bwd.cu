@@ -348,11 +348,13 @@ join_columns_kernel(const __grid_constant__ JoinArgs a, const __grid_constant__ 
 
 // Adds the blocks' partial rows up in a fixed order (eight strands of them) and finishes the gradients:
 //     dgamma_post = gate row * S, dgate row = gamma_post * S, dgamma_pre = the second sum.
+// A factor that is not finite leaves every row out, so that S is 0 and so is the gradient.
 struct JoinSumArgs {
     const float* partial; int64_t rows; int32_t N;
     const void* gate_row; const void* gamma_post;
     void* dgate_row; void* dgamma_post; void* dgamma_pre; int32_t p32;
 };
+__device__ __forceinline__ float join_scaled(float sum, float factor) { return sum == 0.f || factor == 0.f ? 0.f : sum * factor; }
 __global__ void __launch_bounds__(256) join_sum_kernel(const JoinSumArgs a) {
     __shared__ float red[8][32];
     pdl_launch();
@@ -369,8 +371,8 @@ __global__ void __launch_bounds__(256) join_sum_kernel(const JoinSumArgs a) {
     if (strand != 0 || col >= all) return;
     for (int i = 1; i < 8; ++i) v += red[i][lane];
     if (col < a.N) {
-        if (a.dgamma_post) put_param(a.dgamma_post, col, a.p32, v * param(a.gate_row, col, a.p32));
-        if (a.dgate_row) put_param(a.dgate_row, col, a.p32, v * param(a.gamma_post, col, a.p32));
+        if (a.dgamma_post) put_param(a.dgamma_post, col, a.p32, join_scaled(v, param(a.gate_row, col, a.p32)));
+        if (a.dgate_row) put_param(a.dgate_row, col, a.p32, join_scaled(v, param(a.gamma_post, col, a.p32)));
     } else if (a.dgamma_pre) {
         put_param(a.dgamma_pre, col - a.N, a.p32, v);
     }

@@ -377,3 +377,30 @@ def test_more_than_two_to_the_31_elements():
     for got, k in ((dz[-5:], "dz"), (dres[-5:], "dresidual"), (dg, "dgate"), (dgp, "dgamma_post"), (dgn, "dgamma_pre")):
         within(got, ref[k][0], ref[k][1] + 1e-6 * ref[k][0].abs() + (half_step(BF) + U) * ref[k][0].abs() + 1e-37, k)
     assert not bool(dz[:-5].any()) and not bool(dres[:-5].any()) and int(st) == 0
+
+
+@pytest.mark.parametrize("dtype,M,N", [(BF, 40, 520), (F32, 40, 519), (BF, 9, 20000)])
+@pytest.mark.parametrize("norms", [0, POST, 3])
+@pytest.mark.parametrize("which,value", [("gate", float("inf")), ("gate", float("nan")), ("gp", float("-inf")), ("gp", float("nan"))])
+def test_a_row_parameter_that_is_not_finite_gives_zeros(dtype, M, N, norms, which, value):
+    """It enters every row, so no row contributes: all gradients are 0, the parameter's own among them."""
+    from paper_2506_15050_b200 import binding as b
+    if which == "gp" and not norms & POST:
+        return
+    c = inputs(M, N, dtype, "row", norms)
+    c[which][N // 3] = value
+    h, n = torch.empty_like(c["z"]), torch.empty_like(c["z"]) if norms & PRE else None
+    r1, r2 = torch.empty(M, device=DEV) if norms & POST else None, torch.empty(M, device=DEV) if norms & PRE else None
+    st = torch.zeros(1, dtype=torch.int32, device=DEV)
+    b.tppo_residual_norm_fwd(c["z"], c["res"], c["gate"], c["gp"], c["gn"], 0.75, 1e-6, norms, h, n, r1, r2, st)
+    assert int(st) == b.DEV_NONFINITE and not bool(h.any())
+    o = [None if c[k] is None else torch.full_like(c[k], 7) for k in ("z", "res", "gate", "gp", "gn")]
+    b.tppo_residual_norm_bwd(c["dh"], c["dn"], c["z"], h, c["gate"], c["gp"], c["gn"], r1, r2, 0.75, norms, *o, st,
+                             b.workspace(b.OP_RESIDUAL_NORM, M, 0, 0, N, DEV))
+    assert not any(bool(t.ne(0).any()) for t in o if t is not None)
+    # nor does it without a single row
+    e, v = c["z"][:0], torch.empty(0, device=DEV)
+    o = [None if c[k] is None else torch.full_like(c[k], 7) for k in ("gate", "gp", "gn")]
+    b.tppo_residual_norm_bwd(e, e if norms & PRE else None, e, e, c["gate"], c["gp"], c["gn"], v if norms & POST else None, v if norms & PRE else None,
+                             0.75, norms, e, e, *o, None, b.workspace(b.OP_RESIDUAL_NORM, 0, 0, 0, N, DEV))
+    assert not any(bool(t.ne(0).any()) for t in o if t is not None)
