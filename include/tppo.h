@@ -588,8 +588,9 @@ enum {
  *   rstd_post, rstd_pre [M] fp32 out or NULL: what the backward call takes
  *   alpha finite, eps >= 0
  * Each output is rounded once; n is formed from the unrounded h.  A row that has no statistics (a NaN or
- * infinity in it, in its gate or in gamma_post; sums of squares or of magnitudes outside fp32; with eps = 0 a row
- * of zeros to be normed) gets h, n and rstd of 0 and raises TPPO_DEV_NONFINITE.  gamma_pre is taken as it is,
+ * infinity in it, in its gate or in gamma_post; sums of squares or of magnitudes beyond fp32; a mean square plus eps
+ * below 2^-126, which with eps = 0 is a row of zeros or of numbers whose squares lose bits in fp32) gets h, n and
+ * rstd of 0 and raises TPPO_DEV_NONFINITE.  gamma_pre is taken as it is,
  * and elements that leave the range of their type become infinities.
  */
 int tppo_residual_norm_fwd(const void *z, int64_t ldz, const void *residual, int64_t ldr,

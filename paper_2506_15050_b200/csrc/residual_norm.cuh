@@ -317,6 +317,15 @@ __device__ __forceinline__ void block_sums(float (&v)[V], float* red) {
     }
 }
 
+// 1 / sqrt(sum / N + eps) of a row's sum of squares, and whether it stands for the row.  A square below fp32's normal
+// range is off by up to 2^-150, and so is the mean of many: from 2^-126 on that is a rounding, below it takes bits.
+constexpr float kJoinLeastMean = 0x1p-126f;
+__device__ __forceinline__ float join_rstd(float sum, float inv, float eps, bool& good) {
+    const float mean = fmaf(sum, inv, eps);
+    good = good && is_finite(sum) && mean >= kJoinLeastMean;
+    return rsqrtf(mean);
+}
+
 // ---- host side --------------------------------------------------------------------------------------------------
 struct JoinPlan { int E = 0, grid = 0; bool shift = false; size_t smem = 0; };    // E = 0: the kernels for any row
 

@@ -35,8 +35,7 @@ __global__ void __launch_bounds__(join_threads(E), 1) join_fwd_kernel(const __gr
             }
             s[0] = q[0] + q[1];
             th.sum(s);
-            r1 = rsqrtf(fmaf(s[0], inv, a.eps));
-            good = is_finite(s[0]) && is_finite(r1);
+            r1 = join_rstd(s[0], inv, a.eps, good);
         }
         float h[CH][VEC], q[2] = {0.f, 0.f};
 #pragma unroll
@@ -67,8 +66,8 @@ __global__ void __launch_bounds__(join_threads(E), 1) join_fwd_kernel(const __gr
         stage = th.stage_at(a, turn);
         s[0] = q[0] + q[1];
         th.sum(s);
-        const float r2 = pre ? rsqrtf(fmaf(s[0], inv, a.eps)) : 1.f;
-        good = good && is_finite(s[0]) && is_finite(r2);
+        const float r2 = pre ? join_rstd(s[0], inv, a.eps, good) : 1.f;
+        good = good && is_finite(s[0]);
         if (th.t == 0) {
             if (a.r_post) a.r_post[r] = good ? r1 : 0.f;
             if (a.r_pre) a.r_pre[r] = good ? r2 : 0.f;
@@ -115,8 +114,7 @@ __global__ void __launch_bounds__(kJoinAnyThreads) join_fwd_any_kernel(const __g
 #pragma unroll 4
             for (int c = threadIdx.x; c < a.N; c += kJoinAnyThreads) s[0] = fmaf(load_f32(z + c), load_f32(z + c), s[0]);
             block_sums(s, red);
-            r1 = rsqrtf(fmaf(s[0], inv, a.eps));
-            good = is_finite(s[0]) && is_finite(r1);
+            r1 = join_rstd(s[0], inv, a.eps, good);
         }
         auto join = [&](int c) {
             float g = param(a.gate_row, c, a.p32) * param(a.gamma_post, c, a.p32);
@@ -130,8 +128,8 @@ __global__ void __launch_bounds__(kJoinAnyThreads) join_fwd_any_kernel(const __g
             s[0] = pre ? fmaf(h, h, s[0]) : s[0] + fabsf(h);
         }
         block_sums(s, red);
-        const float r2 = pre ? rsqrtf(fmaf(s[0], inv, a.eps)) : 1.f;
-        good = good && is_finite(s[0]) && is_finite(r2);
+        const float r2 = pre ? join_rstd(s[0], inv, a.eps, good) : 1.f;
+        good = good && is_finite(s[0]);
         if (threadIdx.x == 0) {
             if (a.r_post) a.r_post[r] = good ? r1 : 0.f;
             if (a.r_pre) a.r_pre[r] = good ? r2 : 0.f;

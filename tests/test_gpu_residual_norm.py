@@ -404,3 +404,29 @@ def test_a_row_parameter_that_is_not_finite_gives_zeros(dtype, M, N, norms, whic
     b.tppo_residual_norm_bwd(e, e if norms & PRE else None, e, e, c["gate"], c["gp"], c["gn"], v if norms & POST else None, v if norms & PRE else None,
                              0.75, norms, e, e, *o, None, b.workspace(b.OP_RESIDUAL_NORM, 0, 0, 0, N, DEV))
     assert not any(bool(t.ne(0).any()) for t in o if t is not None)
+
+
+@pytest.mark.parametrize("dtype,N", [(F32, 64), (BF, 519), (F32, 5120), (BF, 20000)])
+@pytest.mark.parametrize("norms", [POST, PRE])
+def test_small_rows_are_right_or_refused(dtype, N, norms):
+    """Without eps, a mean square below fp32's normal range has lost bits: such a row is 0 and raises a bit.  From 2^-126 on its
+    error of up to 2^-150 is within half a rounding of the mean, U / 4 of the rstd."""
+    from paper_2506_15050_b200 import binding as b
+    e = torch.arange(-76, -50, device=DEV)
+    z = (torch.randn((len(e), N), generator=gen(N), device=DEV) * torch.exp2(e.float())[:, None]).to(dtype)
+    res = torch.zeros_like(z)
+    mean = (z.double() ** 2).mean(1)
+    tiny, clear = mean < 2.0 ** -126 * (1 - 2.0 ** -20), mean > 2.0 ** -126 * (1 + 2.0 ** -20)
+    assert bool(tiny.any()) and bool(clear.any()) and bool((tiny | clear).all())
+    for eps in (0.0, 2.0 ** -100):
+        h, n, r, st = torch.empty_like(z), torch.empty_like(z), torch.empty(len(e), device=DEV), torch.zeros(1, dtype=torch.int32, device=DEV)
+        post = norms & POST
+        b.tppo_residual_norm_fwd(z, res, None, None, None, 1.0, eps, norms, h, None if post else n, r if post else None, None if post else r, st)
+        rh, rn, q1, q2, eh, en, e1, e2 = forward64(z, res, None, None, None, 1.0, eps, norms)
+        bad = tiny if eps == 0 else torch.zeros_like(tiny)
+        assert int(st) == (b.DEV_NONFINITE if eps == 0 else 0)
+        out, want, tol, q, eq = (h, rh, eh, q1, e1) if post else (n, rn, en, q2, e2)
+        assert not bool(out[bad].any()) and not bool(h[bad].any()) and not bool(r[bad].any())
+        eq = torch.as_tensor(eq, device=DEV).expand(len(e))
+        within(r[~bad], q[~bad], ((eq + 1.25 * U) * q)[~bad], "rstd")
+        within(out[~bad], want[~bad], (tol + (half_step(dtype) + 1.25 * U) * want.abs() + 1e-37)[~bad], "out")
