@@ -700,7 +700,8 @@ int tppo_grad_norm(const tppo_tensor *grads, int32_t count, double *sum_sq, floa
  *     coef = min(1, max_norm / sqrt(sum_sq)),   out_i = coef * g_i
  *   sum_sq    [1] fp64 from tppo_grad_norm, on the device;  max_norm finite, >= 0
  *   out       HOST array of `count` tensors of the same lengths, of either type each; or NULL: in place.  An
- *             output is its gradient itself or overlaps none of the tensors.  In place, a coefficient of 1 leaves the
+ *             output is its gradient itself, of the same type, or overlaps no gradient and no other output.  A gradient
+ *             that is listed twice and in place both times is scaled once.  In place, a coefficient of 1 leaves the
  *             gradients untouched (and unread).
  *   coef      [1] fp32 out or NULL
  * A sum_sq that is not finite gives coef = 0, outputs of 0 and TPPO_DEV_NONFINITE: a step without effect.

@@ -114,3 +114,25 @@ def test_grad_norm_refusals(lib, p):  # noqa: F811
     assert clip(coef=a + 1) == INVALID
     assert clip(out=tensors((a, 5, 1), (a, 6, 1), (None, 0, 0))) == INVALID        # lengths differ
     assert clip(out=tensors((a, 5, 1), (None, 7, 1), (None, 0, 0))) == INVALID
+
+
+@pytest.mark.parametrize("more", [0, 100, 1200])
+def test_clipping_refuses_outputs_at_the_place_of_another_tensor(lib, p, more):  # noqa: F811
+    """An element has one writer and no other reader.  Refused before anything is launched, in lists of any length."""
+    a, launched = p[1], 4                                  # TPPO_ERR_CUDA: past all checks, without a GPU
+    rest = [(a + 65536 + 256 * i, 8, 1) for i in range(more)]
+    def tensors(*t):
+        t = [*t[:1], *rest, *t[1:]]
+        return (Tensor * len(t))(*[Tensor(d, n, k, 0) for d, n, k in t])
+    clip = lambda g, out: lib.tppo_grad_clip(g, len(g), a, 1.0, out, None, None, None)
+    one, two, far = (a, 64, 1), (a + 256, 64, 1), (a + 4096, 64, 1)
+    for bad in ((one, (a, 63, 1)), (one, (a, 128, 0)), (one, two, one, (a + 256, 1, 1))):
+        assert clip(tensors(*bad), None) == INVALID and clip(tensors(*bad), tensors(*bad)) == INVALID
+    assert clip(tensors(one, two), tensors(one, one)) == INVALID                   # an output that is another entry's gradient
+    assert clip(tensors(one, one), tensors(one, far)) == INVALID
+    assert clip(tensors(one, one), tensors(far, one)) == INVALID
+    assert clip(tensors((a, 64, 1)), tensors((a, 64, 0))) == INVALID               # its own gradient in another type
+    if not __import__("torch").cuda.is_available():
+        for good in ((one, two), (two, one), (one, one), (one, two, one, two), (one, (None, 0, 0), (a, 0, 1), two)):
+            assert clip(tensors(*good), None) == launched
+        assert clip(tensors(one, one), tensors(two, far)) == launched and clip(tensors(two, one), tensors(two, far)) == launched

@@ -248,3 +248,19 @@ def test_short_lists_over_and_over(sizes):
             sq2.zero_()
     torch.cuda.synchronize()
     assert bool((seen[:, 0] == first[0]).all()) and float(norm) == float(norm2) == first[1]
+
+
+@pytest.mark.parametrize("others", [3, 200, 1500])
+def test_a_gradient_listed_twice_in_place_is_scaled_once(others):
+    """Tied weights: each occurrence counts for the norm, the tensor is scaled by the coefficient, not by its square -- in one
+    launch and where its two places are in different ones."""
+    for dt in (BF, F32):
+        _, ts = tensors([300] * others + [8192 * 5 + 3], [dt] * (others + 1), 12)
+        tied = ts[-1]
+        listed = [tied] + ts[:-1] + [tied, tied]
+        before, ref = [t.clone() for t in ts], norm64(listed)
+        sq, norm, coef, st = call(listed, 0.3 * ref)
+        assert st == 0 and abs(norm - ref) <= 7 * U * ref and abs(coef - 0.3) <= 8 * U * 0.3
+        for got, t in zip(ts, before):
+            r = t.double() * 0.3
+            assert bool(((got.double() - r).abs() <= (10 * U + half_step(dt)) * r.abs() + 2.0 ** -133).all())
