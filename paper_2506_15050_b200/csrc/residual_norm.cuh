@@ -1,9 +1,9 @@
 // The residual join: a block's output normed, gated and added to the scaled residual stream, and the sum normed
 // for the next block; forward and backward with the parameters' gradients.  With root-mean-square norms,
 //     h = alpha * residual + gate * gamma_post * z * r1,   n = h * r2 * gamma_pre
-//     d = dh + r2 * (a2 - h r2^2 mean(a2 h)),  a2 = dn * gamma_pre;   dresidual = alpha * d
-//     a1 = d * gate * gamma_post,   dz = r1 * (a1 - z r1^2 mean(a1 z)),   dgate = d * z * r1 * gamma_post
-//     dgamma_post = sum_rows d * gate * z * r1,   dgamma_pre = sum_rows dn * h * r2
+//     d = dh + r2 * (a2 - hh mean(a2 hh)),  a2 = dn * gamma_pre,  hh = h * r2;   dresidual = alpha * d
+//     a1 = d * gate * gamma_post,   dz = r1 * (a1 - zz mean(a1 zz)),  zz = z * r1;   dgate = d * zz * gamma_post
+//     dgamma_post = sum_rows d * gate * zz,   dgamma_pre = sum_rows dn * hh
 // All arithmetic is fp32; each input is read once, each output rounded once.  4 elements move forward and 6
 // backward per element of a row (one and two more with a gate per element), so HBM is the bound.
 //
@@ -14,8 +14,8 @@
 //   [16384, 5120] bf16: forward 122 us (5.5 TB/s, 0.84 of the measured copy rate), backward 213 us (4.7 TB/s)
 //   [8192, 5120] fp32: forward 110-116 us (5.8-6.1 TB/s), backward 166 us (6.1 TB/s)
 //
-// Forward needs two sums over the row, one behind the other.  Backward takes one: with w = gate gamma_post z,
-//     sum(a1 z) = sum((dh + r2 a2) w) - r2^3 mean(a2 h) sum(h w),
+// Forward needs two sums over the row, one behind the other.  Backward takes one: with w = gate gamma_post zz,
+//     sum(a1 zz) = sum((dh + r2 a2) w) - r2^2 mean(a2 hh) sum(h w),
 // three sums that do not wait for one another, met at one barrier per row.  (The same expansion of sum(h^2) would
 // lose all its digits where the block's output cancels the residual, so the forward pass does not use it.)
 //
@@ -49,7 +49,7 @@ struct JoinArgs {
     void* out[3]; int64_t ldo[3];                         // h, n | dz, dresidual, dgate
     float* r_post; float* r_pre;                          // out | in; NULL in the backward pass: no such norm
     float* partial;                                       // column sums: [blocks][2][N]
-    float4* rows;                                         // r1, r2, k1, k2 of every row, where two launches share the work,
+    float4* rows;                                         // r1, r2, m1, m2 of every row, where two launches share the work,
     float* params;                                        // and the parameters as they use them: two rows
     int32_t* status;
     int64_t M; int32_t N; float alpha, eps; int32_t norms;

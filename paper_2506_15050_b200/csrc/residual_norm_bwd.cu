@@ -1,21 +1,33 @@
 // Backward pass of the residual join; see residual_norm.cuh.
+#include <type_traits>
+
 #include "residual_norm.cuh"
 
 namespace tppo {
 namespace {
 
-// The scalars of a row's backward pass, from its three sums.
-struct JoinRow { float r1, r2, k2, k1; bool good; };
-__device__ __forceinline__ JoinRow join_row(const JoinArgs& a, float r1, float r2, const float (&s)[3], bool reports) {
+// The scalars of a row's backward pass, from its three sums: m2 = mean(a2 hh), m1 = mean(a1 zz), with hh = h r2 and zz = z r1.
+//     d = dh + r2 (a2 - m2 hh) = dh + r2 a2 - (m2 r2^2) h,      dz = r1 (a1 - m1 zz) = r1 a1 - (m1 r1^2) z
+// The right-hand forms save three operations per element, but their factors leave fp32 before the result does: at a mean square
+// of 2^100 they kept no bit of gradients of 2^-50.  With 16 elements per thread or more and no gate per element, rows with
+// scales from 2^-20 to 2^20, any that training meets, take them (gradients keep their precision down to 2^-86) and other rows
+// the left-hand ones, at one branch per row ([16384, 5120] bf16 215 us, 5121 columns 312; without the branch 223 and 330).  With 8
+// elements or a gate per element all rows take the left-hand forms: two forms cost such a kernel more registers than they
+// save operations ([16384, 5120] bf16 gated 297 us, with the branch 323; [65536, 256] 52 and 56; [8192, 5120] fp32 167 and 168).
+struct JoinRow { float r1, r2, m2, m1; bool good; };
+__host__ __device__ constexpr bool join_two_forms(int e, bool gated) { return e >= 16 && !gated; }
+__device__ __forceinline__ bool join_ordinary(float r) { return r >= 0x1p-20f && r <= 0x1p20f; }
+// zs: r1 where the sums were taken with z as it is, 1 where with zz.
+__device__ __forceinline__ JoinRow join_row(const JoinArgs& a, float r1, float r2, float zs, const float (&s)[3], bool reports) {
     const bool post = a.norms & TPPO_NORM_POST, pre = a.norms & TPPO_NORM_PRE;
     const float inv = 1.f / float(a.N);
     JoinRow w;
     w.r1 = post ? r1 : 1.f;
     w.r2 = pre ? r2 : 0.f;
-    w.k2 = pre ? s[0] * inv * r2 * r2 * r2 : 0.f;                         // d = dh + r2 a2 - k2 h
-    w.k1 = post ? (s[1] - w.k2 * s[2]) * inv * r1 * r1 * r1 : 0.f;        // dz = r1 a1 - k1 z
+    w.m2 = pre ? s[0] * inv * r2 : 0.f;
+    w.m1 = post ? (s[1] - (w.m2 * r2) * (s[2] * r2)) * inv * zs : 0.f;
     const bool stats = !((post && r1 == 0.f) || (pre && r2 == 0.f));
-    w.good = is_finite(s[0]) && is_finite(s[1]) && is_finite(s[2]) && is_finite(w.k2) && is_finite(w.k1);
+    w.good = is_finite(s[0]) && is_finite(s[1]) && is_finite(w.m2) && is_finite(w.m1);
     if (!w.good && stats && reports && a.status) atomicOr(a.status, TPPO_DEV_NONFINITE);
     w.good = w.good && stats;
     return w;
@@ -85,53 +97,60 @@ __global__ void __launch_bounds__(join_threads(E), 1) join_bwd_kernel(const __gr
             if (PRE) r2_next = a.r_pre[r + th.step];
         }
         th.land(a, stage);
-        const uint64_t r2_2 = ptx::pack_f32x2(r2, r2);
-        uint64_t q[3] = {0, 0, 0};
+        auto row = [&](auto scaled) {
+            constexpr bool SCALED = decltype(scaled)::value;
+            const uint64_t r1_2 = ptx::pack_f32x2(r1, r1), r2_2 = ptx::pack_f32x2(r2, r2);
+            uint64_t q[3] = {0, 0, 0};
 #pragma unroll
-        for (int c = 0; c < CH; ++c) {
-            if (!th.k.any(c)) continue;
-            uint64_t w[P], d[P], g[P];
-            join_piece<T>(th.at(a, stage, kZ, c), w);
-            th.post(a, c, g);
+            for (int c = 0; c < CH; ++c) {
+                if (!th.k.any(c)) continue;
+                uint64_t w[P], d[P], g[P];
+                join_piece<T>(th.at(a, stage, kZ, c), w);
+                th.post(a, c, g);
 #pragma unroll
-            for (int i = 0; i < P; ++i) w[i] = mul_f32x2(w[i], g[i]);
-            if (GATED) {
-                join_piece<T>(th.at(a, stage, kGate, c), g);
+                for (int i = 0; i < P; ++i) w[i] = mul_f32x2(SCALED ? mul_f32x2(w[i], r1_2) : w[i], g[i]);
+                if (GATED) {
+                    join_piece<T>(th.at(a, stage, kGate, c), g);
 #pragma unroll
-                for (int i = 0; i < P; ++i) w[i] = mul_f32x2(w[i], g[i]);
-            }
-#pragma unroll
-            for (int i = 0; i < P; ++i) d[i] = 0;
-            if (add) join_piece<T>(th.at(a, stage, kDh, c), d);
-            if (PRE) {
-                uint64_t n[P], h[P];
-                join_piece<T>(th.at(a, stage, kDn, c), n);
-                join_piece<T>(th.at(a, stage, kH, c), h);
-                th.pre(a, c, g);
-#pragma unroll
-                for (int i = 0; i < P; ++i) {
-                    n[i] = mul_f32x2(n[i], g[i]);
-                    q[0] = fma_f32x2(n[i], h[i], q[0]);
-                    q[2] = fma_f32x2(h[i], w[i], q[2]);
-                    d[i] = fma_f32x2(r2_2, n[i], d[i]);
+                    for (int i = 0; i < P; ++i) w[i] = mul_f32x2(w[i], g[i]);
                 }
+#pragma unroll
+                for (int i = 0; i < P; ++i) d[i] = 0;
+                if (add) join_piece<T>(th.at(a, stage, kDh, c), d);
+                if (PRE) {
+                    uint64_t n[P], h[P];
+                    join_piece<T>(th.at(a, stage, kDn, c), n);
+                    join_piece<T>(th.at(a, stage, kH, c), h);
+                    th.pre(a, c, g);
+#pragma unroll
+                    for (int i = 0; i < P; ++i) {
+                        n[i] = mul_f32x2(n[i], g[i]);
+                        q[0] = fma_f32x2(n[i], h[i], q[0]);
+                        q[2] = fma_f32x2(h[i], w[i], q[2]);
+                        d[i] = fma_f32x2(r2_2, n[i], d[i]);
+                    }
+                }
+#pragma unroll
+                for (int i = 0; i < P; ++i) q[1] = fma_f32x2(d[i], w[i], q[1]);
             }
+            float s[3];
 #pragma unroll
-            for (int i = 0; i < P; ++i) q[1] = fma_f32x2(d[i], w[i], q[1]);
-        }
-        float s[3];
-#pragma unroll
-        for (int i = 0; i < 3; ++i) {
-            float lo, hi;
-            ptx::unpack_f32x2(q[i], lo, hi);
-            s[i] = lo + hi;
-        }
-        th.sum(s);
-        const JoinRow w = join_row(a, r1, r2, s, th.t == 0);
-        T *dz = th.out(a, 0, r), *dres = th.out(a, 1, r), *dgate = th.out(a, 2, r);
-        if (w.good) {
-            const uint64_t r1_2 = ptx::pack_f32x2(w.r1, w.r1), k1_2 = ptx::pack_f32x2(-w.k1, -w.k1), k2_2 = ptx::pack_f32x2(-w.k2, -w.k2);
-            const uint64_t alpha_2 = ptx::pack_f32x2(a.alpha, a.alpha);
+            for (int i = 0; i < 3; ++i) {
+                float lo, hi;
+                ptx::unpack_f32x2(q[i], lo, hi);
+                s[i] = lo + hi;
+            }
+            th.sum(s);
+            const JoinRow w = join_row(a, r1, r2, SCALED ? 1.f : r1, s, th.t == 0);
+            T *dz = th.out(a, 0, r), *dres = th.out(a, 1, r), *dgate = th.out(a, 2, r);
+            if (!w.good) {                                // the same for the whole group
+                if (a.out[0]) th.store_zeros(dz);
+                if (a.out[1]) th.store_zeros(dres);
+                if (a.out[2]) th.store_zeros(dgate);
+                return;
+            }
+            const float k1 = SCALED ? w.m1 : w.m1 * r1 * r1, k2 = SCALED ? w.m2 : w.m2 * r2 * r2;
+            const uint64_t k1_2 = ptx::pack_f32x2(-k1, -k1), k2_2 = ptx::pack_f32x2(-k2, -k2), alpha_2 = ptx::pack_f32x2(a.alpha, a.alpha);
 #pragma unroll
             for (int c = 0; c < CH; ++c) {
                 if (!th.k.any(c)) continue;
@@ -146,9 +165,11 @@ __global__ void __launch_bounds__(join_threads(E), 1) join_bwd_kernel(const __gr
                     th.pre(a, c, g);
 #pragma unroll
                     for (int i = 0; i < P; ++i) {
-                        n[i] = mul_f32x2(n[i], r2_2);
+                        if (SCALED) h[i] = mul_f32x2(h[i], r2_2);
+                        else n[i] = mul_f32x2(n[i], r2_2);
                         sum_pre[c][i] = fma_f32x2(n[i], h[i], sum_pre[c][i]);
-                        d[i] = fma_f32x2(k2_2, h[i], fma_f32x2(n[i], g[i], d[i]));
+                        if (SCALED) d[i] = fma_f32x2(r2_2, fma_f32x2(k2_2, h[i], mul_f32x2(n[i], g[i])), d[i]);
+                        else d[i] = fma_f32x2(k2_2, h[i], fma_f32x2(n[i], g[i], d[i]));
                     }
                 }
                 if (a.out[1]) {
@@ -159,7 +180,10 @@ __global__ void __launch_bounds__(join_threads(E), 1) join_bwd_kernel(const __gr
                 join_piece<T>(th.at(a, stage, kZ, c), z);
                 th.post(a, c, g);
 #pragma unroll
-                for (int i = 0; i < P; ++i) d[i] = mul_f32x2(d[i], r1_2);
+                for (int i = 0; i < P; ++i) {
+                    if (SCALED) z[i] = mul_f32x2(z[i], r1_2);
+                    else d[i] = mul_f32x2(d[i], r1_2);
+                }
                 if (GATED) {
                     join_piece<T>(th.at(a, stage, kGate, c), v);
                     if (a.out[2]) {
@@ -175,14 +199,19 @@ __global__ void __launch_bounds__(join_threads(E), 1) join_bwd_kernel(const __gr
                 for (int i = 0; i < P; ++i) sum_post[c][i] = fma_f32x2(d[i], z[i], sum_post[c][i]);
                 if (a.out[0]) {
 #pragma unroll
-                    for (int i = 0; i < P; ++i) v[i] = fma_f32x2(k1_2, z[i], mul_f32x2(d[i], g[i]));
+                    for (int i = 0; i < P; ++i) {
+                        v[i] = fma_f32x2(k1_2, z[i], mul_f32x2(d[i], g[i]));
+                        if (SCALED) v[i] = mul_f32x2(r1_2, v[i]);
+                    }
                     join_store<T>(th.k, c, dz, v);
                 }
             }
-        } else {                                          // the same for the whole group
-            if (a.out[0]) th.store_zeros(dz);
-            if (a.out[1]) th.store_zeros(dres);
-            if (a.out[2]) th.store_zeros(dgate);
+        };
+        if constexpr (join_two_forms(E, GATED)) {
+            if ((!post || join_ordinary(r1)) && (!PRE || join_ordinary(r2))) row(std::false_type{});
+            else row(std::true_type{});
+        } else {
+            row(std::true_type{});
         }
         th.fetch(a, r + a.stages * th.step, stage);
         if (++turn == a.stages) turn = 0;
@@ -275,7 +304,7 @@ __global__ void __launch_bounds__(kJoinAnyThreads, 2) join_row_sums_kernel(const
             load_vec<VEC>(w.pre + c, gn);
 #pragma unroll
             for (int i = 0; i < VEC; ++i) {
-                const float x = z[i] * (g[i] * gp[i]), a2 = n[i] * gn[i];
+                const float x = z[i] * r1 * (g[i] * gp[i]), a2 = n[i] * gn[i];
                 s[0] = fmaf(a2, h[i], s[0]);
                 s[1] = fmaf(fmaf(r2, a2, d[i]), x, s[1]);
                 s[2] = fmaf(h[i], x, s[2]);
@@ -283,9 +312,9 @@ __global__ void __launch_bounds__(kJoinAnyThreads, 2) join_row_sums_kernel(const
         }
         block_sums(s, red);
         if (threadIdx.x == 0) {
-            const JoinRow q = join_row(a, r1, r2, s, true);
+            const JoinRow q = join_row(a, r1, r2, 1.f, s, true);
             // zeros: a row to leave out
-            a.rows[r] = q.good ? make_float4(q.r1, q.r2, q.k1, q.k2) : make_float4(0.f, 0.f, 0.f, 0.f);
+            a.rows[r] = q.good ? make_float4(q.r1, q.r2, q.m1, q.m2) : make_float4(0.f, 0.f, 0.f, 0.f);
         }
     }
 }
@@ -318,11 +347,11 @@ join_columns_kernel(const __grid_constant__ JoinArgs a, const __grid_constant__ 
         const bool good = w.x != 0.f;                     // r1 of a row with statistics is not 0
 #pragma unroll
         for (int i = 0; i < VEC; ++i) {
-            const float m = n[i] * w.y;
-            if (good) sum_pre[i] = fmaf(m, h[i], sum_pre[i]);
-            d[i] = fmaf(-w.w, h[i], fmaf(m, gn[i], d[i]));
+            h[i] *= w.y;
+            if (good) sum_pre[i] = fmaf(n[i], h[i], sum_pre[i]);
+            d[i] = fmaf(w.y, fmaf(-w.w, h[i], n[i] * gn[i]), d[i]);
             o[i] = good ? a.alpha * d[i] : 0.f;
-            d[i] *= w.x;
+            z[i] *= w.x;
         }
         if (a.out[1]) store_vec<VEC>(static_cast<T*>(a.out[1]) + r * a.ldo[1] + c, o);
 #pragma unroll
@@ -333,7 +362,7 @@ join_columns_kernel(const __grid_constant__ JoinArgs a, const __grid_constant__ 
         }
         if (a.out[2]) store_vec<VEC>(static_cast<T*>(a.out[2]) + r * a.ldo[2] + c, o);
 #pragma unroll
-        for (int i = 0; i < VEC; ++i) o[i] = good ? fmaf(-w.z, z[i], d[i] * g[i]) : 0.f;
+        for (int i = 0; i < VEC; ++i) o[i] = good ? w.x * fmaf(-w.z, z[i], d[i] * g[i]) : 0.f;
         if (a.out[0]) store_vec<VEC>(static_cast<T*>(a.out[0]) + r * a.ldo[0] + c, o);
     }
     if (a.partial) {

@@ -430,3 +430,32 @@ def test_small_rows_are_right_or_refused(dtype, N, norms):
         eq = torch.as_tensor(eq, device=DEV).expand(len(e))
         within(r[~bad], q[~bad], ((eq + 1.25 * U) * q)[~bad], "rstd")
         within(out[~bad], want[~bad], (tol + (half_step(dtype) + 1.25 * U) * want.abs() + 1e-37)[~bad], "out")
+
+
+@pytest.mark.parametrize("N", [64, 519, 5120, 20000])
+@pytest.mark.parametrize("norms", [POST, PRE, 3])
+@pytest.mark.parametrize("ez,er,eg", [(0, 0, -20), (20, -20, -80), (-20, 20, -80), (50, 0, -20), (55, 3, -60), (-50, 0, -20), (-50, -45, 10), (0, 50, -40), (50, 50, -30), (40, -40, -60),
+                                      (-60, 30, -60)])
+def test_gradients_of_large_and_small_rows(N, norms, ez, er, eg):
+    """Rows of scale 2^ez and 2^er, gradients of scale 2^eg: the result is in fp32's range, and so is every step towards it."""
+    from paper_2506_15050_b200 import binding as b
+    M = 40
+    r = lambda e, seed: torch.randn((M, N), generator=gen(seed + N), device=DEV) * 2.0 ** e
+    z, res = r(ez, 1), r(er, 2)
+    z[::3] *= 0.5                                          # rows on both sides of a power of two
+    h, n = torch.empty_like(z), torch.empty_like(z) if norms & PRE else None
+    r1, r2 = torch.empty(M, device=DEV) if norms & POST else None, torch.empty(M, device=DEV) if norms & PRE else None
+    st = torch.zeros(1, dtype=torch.int32, device=DEV)
+    b.tppo_residual_norm_fwd(z, res, None, None, None, 1.0, 0.0, norms, h, n, r1, r2, st)
+    assert int(st) == 0
+    dh = r(eg, 3) * (float(r2.median()) if norms & PRE else 1.0)
+    dn = r(eg, 4) if norms & PRE else None
+    dz, dres = torch.empty_like(z), torch.empty_like(z)
+    dgp, dgn = torch.empty(N, device=DEV) if norms & POST else None, torch.empty(N, device=DEV) if norms & PRE else None
+    b.tppo_residual_norm_bwd(dh, dn, z, h, None, None, None, r1, r2, 1.0, norms, dz, dres, None, dgp, dgn, st,
+                             b.workspace(b.OP_RESIDUAL_NORM, M, 0, 0, N, DEV))
+    assert int(st) == 0
+    ref = backward64(dh, dn, z, h, None, None, None, r1, r2, 1.0, norms)
+    got = dict(dz=dz, dresidual=dres, dgamma_post=dgp, dgamma_pre=dgn)
+    for k, (v, tol) in ref.items():
+        within(got[k], v, tol + 2 * U * v.abs() + 2.0 ** -148, k)
