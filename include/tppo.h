@@ -672,6 +672,11 @@ int tppo_fp8_matmul(const void *a, int64_t lda, const float *a_scale, int64_t ld
                     int64_t M, int64_t N, int64_t K, void *y, int32_t y_dtype, int64_t ldy,
                     int32_t *status, void *stream);
 
+/* For tests, host only: how tppo_fp8_matmul cuts a product -- 16 times the rows of y that a tile of its split kernel takes
+ * (0: the persistent kernel), plus the blocks that share a tile's contraction.  aligned_rows: y's rows start on 16-byte
+ * boundaries.  -1 for sizes outside [1, 2^30]. */
+int32_t tppo_test_fp8_cut(int64_t M, int64_t N, int64_t K, int32_t y_dtype, int32_t aligned_rows);
+
 /* One of many tensors: n contiguous elements of `dtype` (TPPO_BF16 or TPPO_F32) at the device address `data`,
  * which may be NULL when n is 0.  Any alignment of its element. */
 typedef struct {

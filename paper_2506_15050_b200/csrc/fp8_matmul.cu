@@ -780,3 +780,10 @@ TPPO_API int tppo_fp8_matmul(const void* a, int64_t lda, const float* a_scale, i
     const F8Out out{y, ldy, M, int32_t(N), status, rows_aligned(y, ldy, e)};
     return y_dtype == TPPO_F32 ? f8_product<float>(oa, ob, K, out, s) : f8_product<bf16_bits>(oa, ob, K, out, s);
 }
+
+TPPO_API int32_t tppo_test_fp8_cut(int64_t M, int64_t N, int64_t K, int32_t y_dtype, int32_t aligned_rows) {
+    using namespace tppo;
+    if (M < 1 || N < 1 || K < 1 || M > kDenseMaxSize || N > kDenseMaxSize || K > kDenseMaxSize) return -1;
+    const F8Cut c = f8_cut(M, N, (K + kF8Block - 1) / kF8Block, y_dtype == TPPO_F32 ? f8_bn<float>() : f8_bn<bf16_bits>(), aligned_rows != 0);
+    return c.bn * 16 + c.splits;
+}

@@ -136,3 +136,19 @@ def test_clipping_refuses_outputs_at_the_place_of_another_tensor(lib, p, more): 
         for good in ((one, two), (two, one), (one, one), (one, two, one, two), (one, (None, 0, 0), (a, 0, 1), two)):
             assert clip(tensors(*good), None) == launched
         assert clip(tensors(one, one), tensors(two, far)) == launched and clip(tensors(two, one), tensors(two, far)) == launched
+
+
+def test_sizes_of_the_product_tests_take_every_cut(lib):
+    """The sizes that test_gpu_fp8.py multiplies, by how the library cuts them."""
+    from fp8_shapes import LONG, RAGGED, TOKENS
+    cut = lib.tppo_test_fp8_cut
+    cut.argtypes = [I64, I64, I64, I32, I32]
+    assert set(RAGGED) == {(0, 1)} | {(bn, s) for bn in (16, 32, 64, 128) for s in range(1, 9)}
+    for dtype, e in ((0, 2), (1, 4)):
+        for (bn, splits), (m, n, k) in RAGGED.items():
+            assert n * e % 16 and cut(m, n, k, dtype, 0) == 16 * bn + splits, (m, n, k)
+        tiles = {cut(m, n, k, dtype, 1) // 16 for m, n, k in TOKENS}
+        assert {16, 64, 128} <= tiles
+    long = [cut(m, n, k, 1, 1) // 16 for m, n, k in LONG]
+    assert 0 in long and len(set(long)) >= 3
+    assert cut(0, 1, 1, 0, 1) == -1 and cut(1, 1, (1 << 30) + 1, 0, 1) == -1

@@ -5,6 +5,7 @@ import pytest
 import torch
 
 from dense_util import BF, DEV, F32, F64, U32, Guarded, gen, half_step, strided
+from fp8_shapes import LONG, RAGGED, TOKENS
 
 pytestmark = pytest.mark.gpu
 F8 = torch.float8_e4m3fn
@@ -305,3 +306,48 @@ def test_more_than_two_to_the_31_elements():
     H = h0[2] * spread(h0[3].t(), 1, 128, K, 256)
     ref, mag = T @ T.t() + H @ H.t(), T.abs() @ T.abs().t() + H.abs() @ H.abs().t()
     assert bool(((dw.double() - ref).abs() <= 2 * (600 + 2) * U32 * mag).all())
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("block", [ROWS, SQUARE])
+@pytest.mark.parametrize("M,N,K", list(RAGGED.values()) + TOKENS)
+def test_every_cut_of_the_product(M, N, K, block, dtype):
+    check_product(M, N, K, block, dtype)
+
+
+@pytest.mark.parametrize("M,N,K", LONG)
+def test_precision_of_long_contractions(M, N, K):
+    """fp32 outputs, by norms.  The tensor cores round (or cut) once per step of 32 elements, 32 times in each of S = K / 1024
+    segments, whose sums are added up in registers.  An error of at most a step of 2^-23 of the running sum is 2^-23 / sqrt(3) of it
+    (cut) or half of that (rounded); running sums of n parts have half of the variance of n whole ones on average.  So the result
+    is within 2^-23 sqrt(32 / 2 / 3 + S / 2 / 12) of its norm: 2.9e-7 at 16384, where sums left in the tensor cores have 1.2e-6."""
+    from paper_2506_15050_b200 import binding as b
+    g, ops = gen(K), []
+    for rows in (M, N):
+        x = torch.randn((rows, K), generator=g, device=DEV)
+        q, s = b.fp8_empty(rows, K, DEV), b.fp8_scales(rows, K, ROWS, DEV)
+        b.tppo_fp8_quantize(x, ROWS, q, s, None, None, None)
+        ops.append((q, s, q.to(F64) * spread(s.t(), 1, 128, rows, K)))
+    (a, sa, A), (w, sw, W) = ops
+    y, st = torch.empty((M, N), device=DEV), torch.zeros(1, dtype=torch.int32, device=DEV)
+    b.tppo_fp8_matmul(a, sa, w, sw, ROWS, y, st)
+    ref, S = A @ W.t(), -(-K // 1024)
+    err = float((y.double() - ref).norm() / ref.norm())
+    print(f"{M} x {N} x {K}: {err:.2e}")
+    assert int(st) == 0 and err <= 2.0 ** -23 * (32 / 6 + S / 24) ** 0.5
+
+
+@pytest.mark.parametrize("M,N", [(9, 200), (1500, 1400)])
+@pytest.mark.parametrize("e", [-126, -100, -60, 60, 100, 126])
+def test_scales_at_the_ends_of_their_range(M, N, e):
+    """2^e in one operand, 2^-e in the other: small whole numbers, exact."""
+    from paper_2506_15050_b200 import binding as b
+    K, g = 300, gen(e + 200)
+    a, w = b.fp8_empty(M, K, DEV), b.fp8_empty(N, K, DEV)
+    for t in (a, w):
+        t.copy_(torch.randint(-3, 4, t.shape, generator=g, device=DEV).float().to(F8))
+    sa, sw, st = b.fp8_scales(M, K, ROWS, DEV), b.fp8_scales(N, K, SQUARE, DEV), torch.zeros(1, dtype=torch.int32, device=DEV)
+    sa.fill_(2.0 ** e), sw.fill_(2.0 ** -e)
+    y = torch.empty((M, N), device=DEV)
+    b.tppo_fp8_matmul(a, sa, w, sw, SQUARE, y, st)
+    assert int(st) == 0 and torch.equal(y.double(), a.to(F64) @ w.to(F64).t())
