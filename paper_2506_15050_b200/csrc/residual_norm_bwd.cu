@@ -335,7 +335,9 @@ join_columns_kernel(const __grid_constant__ JoinArgs a, const __grid_constant__ 
     load_vec<VEC>(p.pre + c, gn);
 #pragma unroll
     for (int i = 0; i < VEC; ++i) sum_post[i] = sum_pre[i] = 0;
-#pragma unroll(VEC == 1 ? 4 : 2)
+    // two rows at a time: four of single elements need more than the 64 registers of this occupancy (5000 x 12001 bf16 704 us
+    // for the whole pass, with two 496)
+#pragma unroll 2
     for (int64_t r = r0; r < r1; ++r) {
         const float4 w = __ldcg(a.rows + r);
         float z[VEC], gv[VEC], d[VEC], n[VEC], h[VEC], o[VEC];
