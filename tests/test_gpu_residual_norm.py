@@ -459,3 +459,19 @@ def test_gradients_of_large_and_small_rows(N, norms, ez, er, eg):
     got = dict(dz=dz, dresidual=dres, dgamma_post=dgp, dgamma_pre=dgn)
     for k, (v, tol) in ref.items():
         within(got[k], v, tol + 2 * U * v.abs() + 2.0 ** -148, k)
+
+
+@pytest.mark.parametrize("dtype,M,N", [(BF, 70, 520), (F32, 70, 519), (BF, 9, 20000), (F32, 5, 30001)])
+def test_joined_stream_in_the_place_of_the_block_output(dtype, M, N):
+    from paper_2506_15050_b200 import binding as b
+    c = inputs(M, N, dtype, "full", 3)
+    out = []
+    for place in (False, True):
+        z = c["z"].clone()
+        h, n, r1, r2 = z if place else torch.empty_like(z), torch.empty_like(z), torch.empty(M, device=DEV), torch.empty(M, device=DEV)
+        b.tppo_residual_norm_fwd(z, c["res"], c["gate"], c["gp"], c["gn"], 0.75, 1e-6, 3, h, n, r1, r2, None)
+        out.append((h, n, r1, r2))
+    rh, rn, _, _, eh, en, _, _ = forward64(c["z"], c["res"], c["gate"], c["gp"], c["gn"], 0.75, 1e-6, 3)
+    within(out[1][0], rh, eh + half_step(dtype) * rh.abs(), "h")
+    within(out[1][1], rn, en + (half_step(dtype) + U) * rn.abs(), "n")
+    assert all(torch.equal(a, o) for a, o in zip(*out))
