@@ -635,8 +635,8 @@ enum {
 /*
  * 8-bit values (e4m3: four significant bits, up to 448) with one fp32 scale per block of 128: x ~ q * scale.  The
  * scale is the least power of two 2^e, e >= -126, for which the block's largest magnitude is at most 448 * 2^e (1 for
- * a block of zeros), so that x / scale is exact, q is x / scale rounded once (to nearest even), and q * scale is
- * exact in bf16.  q holds the rows of x as they are, for products that contract over x's columns; qt is x
+ * a block of zeros), so that q is x / scale rounded once (to nearest even), and q * scale is exact in fp32 -- in bf16 too
+ * from a scale of 2^-124 on, below which bf16's smallest numbers are coarser.  q holds the rows of x as they are, for products that contract over x's columns; qt is x
  * transposed, for products that contract over x's rows, with blocks of its own along them.
  *   x       [M, K] of `dtype` (TPPO_BF16 or TPPO_F32)
  *   q       [M, K] 8-bit out or NULL;  scale out:

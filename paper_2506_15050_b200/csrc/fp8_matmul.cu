@@ -11,11 +11,12 @@
 // from registers (tcgen05.st), four blocks of the contraction at a time, one per byte.  A scale that is not a power of
 // two becomes the exponent's NaN, and its outputs 0 with TPPO_DEV_NONFINITE.
 //
-// The tensor cores drop what lies below the accumulator's last bit at every step of 32: over a contraction of 4096 that
-// is 2e-7 of the result, and it grows with the length.  For bf16 outputs it does not show; for fp32 ones the output
-// warps take the sums over eight blocks at a time and add them up in registers (under 1e-7, whatever the length; sixteen
-// would be 1.2e-7, more than fp32 sums in the usual order have), on narrower tiles whose sums the registers hold (5120 x
-// 5120 of a contraction of 16384: 443 us; with sixteen blocks 414, in one go 374).
+// The tensor cores drop what lies below the accumulator's last bit at every step of 32: 1.2e-6 of the result (by norms, normal
+// inputs) over a contraction of 16384, 3.9e-6 over 40000.  For bf16 outputs it does not show; for fp32 ones the output warps
+// take the sums over eight blocks at a time and add them up in registers, on narrower tiles whose sums the registers hold
+// (5120 x 5120 of a contraction of 16384: 443 us; with sixteen blocks 414, in one go 374).  What is left is 7e-8 at 4096,
+// 1.0e-7 at 16384 and 1.3e-7 at 40000: the S = K / 1024 additions in registers round once each, which grows with the root
+// of S.  With the contraction split over CTAs 1.4e-7 at 131072 and 2.5e-7 at a million.
 //
 //   fp8_gemm_kernel   many output tiles: persistent CTAs, 128 x 240 tiles (208 for fp32): two accumulators, so that the output of
 //                     a tile overlaps the products of the next, and two sets of exponents.

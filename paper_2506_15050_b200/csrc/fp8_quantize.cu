@@ -1,6 +1,6 @@
 // 8-bit values with a power-of-two scale per block of 128: x ~ q * 2^e, q in e4m3, e the least with
-// max |x| <= 448 * 2^e over the block.  A power of two costs e4m3 no precision (its steps are relative), makes x / 2^e and
-// q * 2^e exact, and leaves one rounding, that of q.
+// max |x| <= 448 * 2^e over the block.  A power of two costs e4m3 no precision (its steps are relative) and leaves one rounding,
+// that of q: what x / 2^e loses in fp32 lies far below q's smallest step, and q * 2^e is exact (in bf16 from 2^-124 on).
 //
 // A block of 256 threads takes a tile of 128 x 128 elements into registers, 8 rows by 8 columns per thread, so that one
 // read serves both layouts: maxima along the rows need 16 lanes, along the columns the block; values along the rows leave

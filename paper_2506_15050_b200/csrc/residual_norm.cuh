@@ -11,8 +11,9 @@
 // pieces of the next rows into a ring of shared memory of its own with cp.async: what it copies only it reads,
 // so the ring needs no barrier, and 100-200 KB per SM stay in flight whatever the arithmetic does.  gate *
 // gamma_post and gamma_pre stay in registers or shared memory as fp32 for the block's life.
-//   [16384, 5120] bf16: forward 122 us (5.5 TB/s, 0.84 of the measured copy rate), backward 213 us (4.7 TB/s)
-//   [8192, 5120] fp32: forward 110-116 us (5.8-6.1 TB/s), backward 166 us (6.1 TB/s)
+//   [16384, 5120] bf16: forward 122-126 us (5.3-5.5 TB/s, 0.81-0.84 of the measured copy rate), backward 214-225 us (4.5-4.7
+//   TB/s); without a gate and the norm in front, "add and norm": 127 and 210 us
+//   [8192, 5120] fp32: forward 110-116 us (5.8-6.1 TB/s), backward 167 us (6.0 TB/s)
 //
 // Forward needs two sums over the row, one behind the other.  Backward takes one: with w = gate gamma_post zz,
 //     sum(a1 zz) = sum((dh + r2 a2) w) - r2^2 mean(a2 hh) sum(h w),
@@ -359,9 +360,9 @@ inline bool join_fit(JoinArgs& a, JoinPlan& p, int e, int vec, int threads, bool
 // row's warps -- so many per element, some 200 (forward) or 250 per warp for its share of sums, copies and addresses --
 // times (1 / warps on the SM + 1 / 20), the time per instruction that was measured with 5, 10 and 20 of them.  At 5120
 // columns of bf16 that was 40 elements forward (129 us for 16384 rows; 16: 148, 32: 149, 8: 206) and 16 backward (224;
-// 8: 276, 32 with half the threads 241), with a gate per element 16 (160; 40: 206) and 8 (299; 16 with one group 476), of
+// 8: 276, 32 with half the threads 241), with a gate per element 16 (155-160; 40: 206) and 8 (296; 16 with one group 476), of
 // fp32 16 forward (8192 rows: 109; 8: 128, 40: 153) and 8 backward (176; 16 with one group 196, with two of a single
-// stage 6 % more than 8), and of 5121 bf16 columns 24 backward, two groups of a single stage (325; 16 in one group 406).  Of equal ones the first.
+// stage 6 % more than 8), and of 5121 bf16 columns 24 backward, two groups of a single stage (311; 16 in one group 406).  Of equal ones the first.
 inline void join_choose(JoinArgs& a, JoinPlan& p, std::initializer_list<int> kinds, int vec, int64_t width, bool bwd) {
     const JoinArgs given = a;
     const JoinPlan start = p;
